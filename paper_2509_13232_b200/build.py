@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libspo.so")
 SOURCES = ["spo_api.cu", "spo_small.cu", "spo_loss_common.cu", "spo_loss_tc.cu"]
-HEADERS = [os.path.join(CSRC, "spo_internal.h"), os.path.join(ROOT, "include", "spo.h")]
+HEADERS = [os.path.join(CSRC, "spo_internal.h"), os.path.join(CSRC, "spo_ptx.cuh"), os.path.join(ROOT, "include", "spo.h")]
 
 
 def nvcc_path() -> str:
