@@ -79,6 +79,8 @@ extern "C" {
 #define SPO_WS_LOSS_BWD_ROWS  6
 #define SPO_WS_LOSS_FWD_BWD   7
 #define SPO_WS_LOSS_FWD_BWD_ROWS 8
+#define SPO_WS_LOGPROBS       9
+#define SPO_WS_LOGPROBS_BWD  10
 
 /*
  * Hyper-parameters.  Defaults (spo_default_params) are the values the paper prints:
@@ -512,6 +514,60 @@ int32_t spo_loss_fwd_bwd_rows(const void* H, const void* W, int32_t dtype,
 int32_t spo_loss_stats(const float* logp, const float* logp_old, const uint8_t* mask,
                        const int32_t* cu_seqlens, const float* a_norm, int64_t T, int32_t S,
                        float* out, const spo_params* params, void* stream);
+
+/*
+ * Log-probabilities of given tokens straight from hidden states: what a step needs before its loss (the
+ * rollout policy's or a reference policy's logp_old of Sec. 3.2, the divergence D(x) that Sec. 3.1's tracker
+ * update reads) and what a sampler reports about the tokens it drew.  Per token row t, s = inv_temperature:
+ *   z = W h_t (not kept), lse = log sum_v exp(s z_v), logp = s z[y_t] - lse,
+ *   entropy = -sum_v p log p = lse - s sum_v p_v z_v   (nats),
+ *   top_ids / top_logp: the top_k largest z in descending order, equal ones by ascending id, and their
+ *   log-probabilities.
+ *
+ *   H           device in  [T] rows of d elements, row pitch ldH >= d elements (bf16: d % 64 == 0, ldH % 8 == 0;
+ *               fp32: d % 4 == 0, ldH % 4 == 0), so the last-token rows of a padded batch need no copy
+ *   W           device in  [V][d], same dtype
+ *   y           device in  [T] int32, optional together with logp (both NULL: no target)
+ *   mask        device in  [T] uint8, optional: rows with mask 0 give logp = lse = entropy = 0, ids -1,
+ *               top_logp 0, whatever their H and y hold (NaN included), and set no status bit
+ *   inv_temperature   > 0, finite
+ *   top_k       0 .. SPO_MAX_TOP_K, at most V
+ *   logp, lse   device out [T] fp32;  entropy  device out [T] fp32, optional
+ *   top_ids     device out [T][top_k] int32;  top_logp  device out [T][top_k] fp32 (NULL when top_k = 0)
+ *   ws          device scratch, spo_workspace_bytes(SPO_WS_LOGPROBS, T, d, V, 0, top_k, 0) bytes
+ * A target outside [0,V) gives logp = -inf and SPO_DEV_ID_OUT_OF_RANGE; a row whose lse is not finite sets
+ * SPO_DEV_NONFINITE.  Logits that are NaN or -inf are never listed; where fewer than top_k are left the
+ * remaining ids are -1 with top_logp -inf.  T = 0 is allowed and launches nothing.
+ */
+#define SPO_MAX_TOP_K 20
+int32_t spo_logprobs(const void* H, int64_t ldH, const void* W, int32_t dtype, const int32_t* y, const uint8_t* mask,
+                     int64_t T, int32_t d, int32_t V, float inv_temperature, int32_t top_k,
+                     float* logp, float* lse, float* entropy, int32_t* top_ids, float* top_logp,
+                     void* ws, size_t ws_bytes, int32_t* d_status, void* stream);
+
+/*
+ * Gradients of spo_logprobs for upstream gradients of logp, lse and entropy (a loss of the caller's own over
+ * the log-probabilities, an entropy bonus, a penalty on lse; the alternatives are constants):
+ *   dz[t,v] = s ( g_logp_t (1[v = y_t] - p) + g_lse_t p - g_entropy_t p (log p + entropy_t) ),
+ *   dH = dz W,  dW (+)= dz^T H,      p = exp(s z - lse_t) recomputed tile by tile.
+ *
+ *   lse         device in  [T] fp32, spo_logprobs' output for the same H, W, inv_temperature
+ *   entropy     device in  [T] fp32, its entropy; required with g_entropy, otherwise optional
+ *   g_logp, g_lse, g_entropy   device in [T] fp32, each optional (NULL = zero); y is required with g_logp
+ *   mask        rows with mask 0 have dH = 0 and add nothing to dW, whatever their H holds
+ *   dH          device out [T][d];  dW  device out [V][d], overwritten or (dW_accumulate) added to.  Types:
+ *               bf16 H / W: dH and dW bf16 or fp32 each; fp32 H / W: both fp32.  A bf16 dW is summed over all
+ *               tokens in fp32 and rounded once.
+ *   ws          device scratch, spo_workspace_bytes(SPO_WS_LOGPROBS_BWD, T, d, V, 0, 0, 0) bytes: a chunk of dz (a few
+ *               thousand rows by V, bf16; fp32 for fp32 inputs), never all of it
+ * A target outside [0,V) contributes nothing through g_logp and sets SPO_DEV_ID_OUT_OF_RANGE (unless masked).
+ * T = 0 zeroes dW (unless accumulating).
+ */
+int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtype, const int32_t* y, const uint8_t* mask,
+                         const float* lse, const float* entropy, const float* g_logp, const float* g_lse,
+                         const float* g_entropy, int64_t T, int32_t d, int32_t V, float inv_temperature,
+                         void* dH, int32_t dH_dtype, void* dW, int32_t dW_dtype, int32_t dW_accumulate,
+                         void* ws, size_t ws_bytes, int32_t* d_status, void* stream);
 
 /* Scratch size in bytes for one call of the selected entry point (host only, no CUDA call
  * except a device-property query).  Arguments that the selected call does not use are ignored. */

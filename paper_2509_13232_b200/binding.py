@@ -21,14 +21,15 @@ ERR_UNSUPPORTED_DTYPE, ERR_UNSUPPORTED_ARCH, ERR_WORKSPACE_TOO_SMALL, ERR_CUDA =
 DEV_ID_OUT_OF_RANGE, DEV_NONFINITE, DEV_UNIFORMS_EXHAUSTED, DEV_TIMEOUT, DEV_ZERO_TOTAL_WEIGHT = 1, 2, 4, 8, 16
 DTYPE_F32, DTYPE_BF16 = 0, 1
 (WS_SAMPLE, WS_ADVANTAGES, WS_LOSS_FWD, WS_LOSS_BWD, WS_UPDATE_REPEATS, WS_ACTIVE_ROWS, WS_LOSS_BWD_ROWS,
- WS_LOSS_FWD_BWD, WS_LOSS_FWD_BWD_ROWS) = range(9)
+ WS_LOSS_FWD_BWD, WS_LOSS_FWD_BWD_ROWS, WS_LOGPROBS, WS_LOGPROBS_BWD) = range(11)
 AGG_TOKEN_MEAN, AGG_SEQ_MEAN = 0, 1
 SUR_PPO_CLIP, SUR_CISPO, SUR_GSPO = 0, 1, 2
 
 EXPORTS = [
     "spo_default_params", "spo_tracker_init", "spo_sample_prompts", "spo_advantages",
     "spo_advantages_static", "spo_advantages_apply", "spo_advantages_update",
-    "spo_tracker_update", "spo_tracker_update_repeats", "spo_loss_fwd", "spo_loss_bwd", "spo_loss_fwd_bwd", "spo_loss_fwd_bwd_slabs", "spo_dw_slab_rows", "spo_loss_fwd_bwd_scatter", "spo_loss_stats", "spo_loss_mask_rows", "spo_loss_fwd_bwd_rows", "spo_loss_active_rows", "spo_loss_bwd_rows", "spo_workspace_bytes",
+    "spo_tracker_update", "spo_tracker_update_repeats", "spo_loss_fwd", "spo_loss_bwd", "spo_loss_fwd_bwd", "spo_loss_fwd_bwd_slabs", "spo_dw_slab_rows", "spo_loss_fwd_bwd_scatter", "spo_loss_stats", "spo_loss_mask_rows", "spo_loss_fwd_bwd_rows", "spo_loss_active_rows", "spo_loss_bwd_rows",
+    "spo_logprobs", "spo_logprobs_bwd", "spo_workspace_bytes",
     "spo_status_string", "spo_last_cuda_error", "spo_version", "spo_selftest_bounded_wait",
 ]
 
@@ -114,6 +115,13 @@ def lib():
         L.spo_loss_bwd_rows.argtypes = [c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_float,
                                         c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int32, c_void_p,
                                         c_int32, c_void_p, c_size_t, P, c_void_p, c_void_p]
+        L.spo_logprobs.argtypes = [c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int32, c_int32,
+                                   c_float, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_size_t, c_void_p, c_void_p]
+        L.spo_logprobs_bwd.argtypes = [c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_float,
+                                       c_void_p, c_int32, c_void_p, c_int32, c_int32,
+                                       c_void_p, c_size_t, c_void_p, c_void_p]
         L.spo_selftest_bounded_wait.argtypes = [ctypes.c_uint32, c_void_p, c_void_p, c_void_p]
         L.spo_workspace_bytes.argtypes = [c_int32, c_int64, c_int32, c_int32, c_int64, c_int32, c_int32]
         L.spo_workspace_bytes.restype = c_size_t
@@ -343,3 +351,92 @@ def spo_loss_bwd_rows(H, W, y, lse, coef, grad_loss, rows, n_active, dH, dW, dW_
                                    c_float(grad_loss), T, d, V, _ptr(rows), int(n_active), _ptr(dH), _dtype_code(dH),
                                    _ptr(dW), int(dW_accumulate), _ptr(ws), ws.numel() * ws.element_size(),
                                    ctypes.byref(params), _ptr(d_status), _stream()), "spo_loss_bwd_rows")
+
+
+MAX_TOP_K = 20
+
+
+def _need(name, t, dtype, shape, optional=False):
+    """Checks one tensor argument: its type, shape, layout and device (the current one)."""
+    import torch
+    if t is None:
+        if optional:
+            return
+        raise ValueError("%s is required" % name)
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise TypeError("%s must be a %s tensor, got %s" % (name, dtype, getattr(t, "dtype", type(t))))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    _on_current_device(name, t)
+
+
+def _on_current_device(name, t):
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError("%s must be on the current CUDA device, is on %s" % (name, t.device))
+
+
+def _hidden_rows(H, W):
+    """Checks H [T, d] (rows contiguous, any row pitch) against W [V, d]; returns (T, d, V, row pitch of H)."""
+    import torch
+    if not isinstance(H, torch.Tensor) or not isinstance(W, torch.Tensor) or H.dim() != 2 or W.dim() != 2:
+        raise ValueError("H and W must be matrices")
+    (T, d), V = H.shape, W.shape[0]
+    _need("W", W, H.dtype, (V, d))
+    _on_current_device("H", H)
+    if T > 0 and d > 1 and H.stride(1) != 1:
+        raise ValueError("the rows of H must be contiguous")
+    ld = H.stride(0) if T > 1 else max(d, 1)
+    if ld < d:
+        raise ValueError("the rows of H overlap")
+    return T, d, V, ld
+
+
+def _scratch(ws):
+    import torch
+    if not isinstance(ws, torch.Tensor) or not ws.is_contiguous():
+        raise ValueError("ws must be a contiguous tensor")
+    _on_current_device("ws", ws)
+    return _ptr(ws), ws.numel() * ws.element_size()
+
+
+def spo_logprobs(H, W, y, mask, logp, lse, entropy, top_ids, top_logp, ws, d_status, inv_temperature=1.0):
+    """Log-probabilities of the tokens y under softmax(inv_temperature * H W^T), with log-sum-exp and, where the
+    tensors are given, entropy and the top_ids.shape[1] most likely alternatives.  H may be a slice of a wider buffer
+    (rows contiguous); y and logp may both be None."""
+    import torch
+    T, d, V, ld = _hidden_rows(H, W)
+    K = 0 if top_ids is None else top_ids.shape[-1]
+    _need("y", y, torch.int32, (T,), optional=True)
+    _need("mask", mask, torch.uint8, (T,), optional=True)
+    _need("logp", logp, torch.float32, (T,), optional=True)
+    _need("lse", lse, torch.float32, (T,))
+    _need("entropy", entropy, torch.float32, (T,), optional=True)
+    _need("top_ids", top_ids, torch.int32, (T, K), optional=True)
+    _need("top_logp", top_logp, torch.float32, (T, K), optional=K == 0)
+    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
+    w, n = _scratch(ws)
+    _check(lib().spo_logprobs(_ptr(H), ld, _ptr(W), _dtype_code(W), _ptr(y), _ptr(mask), T, d, V, c_float(inv_temperature),
+                              K, _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(top_ids), _ptr(top_logp), w, n,
+                              _ptr(d_status), _stream()), "spo_logprobs")
+
+
+def spo_logprobs_bwd(H, W, y, mask, lse, entropy, g_logp, g_lse, g_entropy, dH, dW, dW_accumulate, ws, d_status,
+                     inv_temperature=1.0):
+    """Gradients dH, dW of spo_logprobs for upstream gradients of logp, lse and entropy (None = zero)."""
+    import torch
+    T, d, V, ld = _hidden_rows(H, W)
+    for name, t in (("lse", lse), ("entropy", entropy), ("g_logp", g_logp), ("g_lse", g_lse), ("g_entropy", g_entropy)):
+        _need(name, t, torch.float32, (T,), optional=name != "lse")
+    _need("y", y, torch.int32, (T,), optional=True)
+    _need("mask", mask, torch.uint8, (T,), optional=True)
+    _need("dH", dH, dH.dtype, (T, d))
+    _need("dW", dW, dW.dtype, (V, d))
+    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
+    w, n = _scratch(ws)
+    _check(lib().spo_logprobs_bwd(_ptr(H), ld, _ptr(W), _dtype_code(W), _ptr(y), _ptr(mask), _ptr(lse), _ptr(entropy),
+                                  _ptr(g_logp), _ptr(g_lse), _ptr(g_entropy), T, d, V, c_float(inv_temperature),
+                                  _ptr(dH), _dtype_code(dH), _ptr(dW), _dtype_code(dW), int(dW_accumulate), w, n,
+                                  _ptr(d_status), _stream()), "spo_logprobs_bwd")

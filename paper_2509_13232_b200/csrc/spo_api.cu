@@ -620,6 +620,65 @@ int32_t spo_loss_stats(const float* logp, const float* logp_old, const uint8_t* 
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);
 }
 
+static int32_t check_lp_shape(int32_t dtype, int64_t T, int64_t ldH, int32_t d, int32_t V, float inv_t) {
+  if (dtype != SPO_DTYPE_F32 && dtype != SPO_DTYPE_BF16) return SPO_ERR_UNSUPPORTED_DTYPE;
+  if (T < 0 || d < 1 || V < 1 || ldH < d) return SPO_ERR_INVALID_ARG;
+  if (!(inv_t > 0.0f) || !(inv_t < 3.0e38f)) return SPO_ERR_INVALID_ARG;
+  if (T >= ((int64_t)1 << 31) - 256 || V >= (1 << 29)) return SPO_ERR_BAD_SHAPE;
+  const int lanes = dtype == SPO_DTYPE_BF16 ? 8 : 4;               // elements per 16 bytes
+  if ((d % (dtype == SPO_DTYPE_BF16 ? 64 : 4)) != 0 || (ldH % lanes) != 0) return SPO_ERR_BAD_SHAPE;
+  if (dtype == SPO_DTYPE_F32 && (V > 4000000 || d > 4000000)) return SPO_ERR_BAD_SHAPE;     // grid limits of the fp32 product
+  return SPO_OK;
+}
+
+int32_t spo_logprobs(const void* H, int64_t ldH, const void* W, int32_t dtype, const int32_t* y, const uint8_t* mask,
+                     int64_t T, int32_t d, int32_t V, float inv_temperature, int32_t top_k, float* logp, float* lse,
+                     float* entropy, int32_t* top_ids, float* top_logp, void* ws, size_t ws_bytes, int32_t* d_status,
+                     void* stream) {
+  const int32_t rc = check_lp_shape(dtype, T, ldH, d, V, inv_temperature);
+  if (rc != SPO_OK) return rc;
+  if (top_k < 0 || top_k > SPO_MAX_TOP_K || top_k > V) return SPO_ERR_INVALID_ARG;
+  if ((y == nullptr) != (logp == nullptr)) return SPO_ERR_INVALID_ARG;
+  if (T > 0 && (!H || !W || !lse || !ws || (top_k > 0 && (!top_ids || !top_logp)))) return SPO_ERR_INVALID_ARG;
+  if (!aligned16(H) || !aligned16(W) || !aligned16(y) || !aligned16(logp) || !aligned16(lse) || !aligned16(entropy) ||
+      !aligned16(top_ids) || !aligned16(top_logp) || !aligned16(ws))
+    return SPO_ERR_BAD_ALIGNMENT;
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  if (T > 0 && ws_bytes < lp_fwd_ws_bytes(T, d, V, top_k, dtype)) return SPO_ERR_WORKSPACE_TOO_SMALL;
+  LpFwd a{};
+  a.H = H; a.W = W; a.ldh = ldH; a.dtype = dtype; a.y = y; a.mask = mask; a.T = T; a.d = d; a.V = V;
+  a.inv_t = inv_temperature; a.top_k = top_k; a.logp = logp; a.lse = lse; a.entropy = entropy;
+  a.top_ids = top_ids; a.top_logp = top_logp; a.d_status = d_status;
+  cudaError_t e = lp_forward(a, (char*)ws, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
+int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtype, const int32_t* y, const uint8_t* mask,
+                         const float* lse, const float* entropy, const float* g_logp, const float* g_lse,
+                         const float* g_entropy, int64_t T, int32_t d, int32_t V, float inv_temperature, void* dH,
+                         int32_t dH_dtype, void* dW, int32_t dW_dtype, int32_t dW_accumulate, void* ws, size_t ws_bytes,
+                         int32_t* d_status, void* stream) {
+  const int32_t rc = check_lp_shape(dtype, T, ldH, d, V, inv_temperature);
+  if (rc != SPO_OK) return rc;
+  for (int32_t t : {dH_dtype, dW_dtype})
+    if ((t != SPO_DTYPE_F32 && t != SPO_DTYPE_BF16) || (dtype == SPO_DTYPE_F32 && t != SPO_DTYPE_F32))
+      return SPO_ERR_UNSUPPORTED_DTYPE;
+  if (!dW || (g_logp && !y) || (g_entropy && !entropy)) return SPO_ERR_INVALID_ARG;
+  if (T > 0 && (!H || !W || !lse || !dH || !ws)) return SPO_ERR_INVALID_ARG;
+  if (!aligned16(H) || !aligned16(W) || !aligned16(y) || !aligned16(lse) || !aligned16(entropy) || !aligned16(g_logp) ||
+      !aligned16(g_lse) || !aligned16(g_entropy) || !aligned16(dH) || !aligned16(dW) || !aligned16(ws))
+    return SPO_ERR_BAD_ALIGNMENT;
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  if (T > 0 && ws_bytes < lp_bwd_ws_bytes(T, d, V, dtype)) return SPO_ERR_WORKSPACE_TOO_SMALL;
+  LpBwd a{};
+  a.H = H; a.W = W; a.ldh = ldH; a.dtype = dtype; a.y = y; a.mask = mask; a.lse = lse; a.ent = entropy;
+  a.g_logp = g_logp; a.g_lse = g_lse; a.g_ent = g_entropy; a.T = T; a.d = d; a.V = V; a.inv_t = inv_temperature;
+  a.dH = dH; a.dH_dtype = dH_dtype; a.dW = dW; a.dW_dtype = dW_dtype; a.accumulate = dW_accumulate;
+  a.d_status = d_status;
+  cudaError_t e = lp_backward(a, (char*)ws, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
 size_t spo_workspace_bytes(int32_t which, int64_t T, int32_t d, int32_t V, int64_t N, int32_t B, int32_t M) {
   switch (which) {
     case SPO_WS_SAMPLE:
@@ -653,6 +712,18 @@ size_t spo_workspace_bytes(int32_t which, int64_t T, int32_t d, int32_t V, int64
       size_t bf16 = fused_ws_layout(T, d, V, B).total;
       const size_t two_call = align_up(fwd_ws_layout(T, d, V, SPO_DTYPE_BF16, B).total, 256) + bwd_ws_layout(T, d, V).total;
       if (two_call > bf16) bf16 = two_call;         // the sequence-level objective runs forward, then backward
+      return bf16 > f32 ? bf16 : f32;
+    }
+    case SPO_WS_LOGPROBS: {             /* B = top_k; enough for either element type */
+      if (T < 0 || V < 1 || d < 1 || B < 0 || B > SPO_MAX_TOP_K) return 0;
+      const size_t f32 = lp_fwd_ws_bytes(T, d, V, B, SPO_DTYPE_F32);
+      const size_t bf16 = (d % 64) == 0 ? lp_fwd_ws_bytes(T, d, V, B, SPO_DTYPE_BF16) : 0;
+      return bf16 > f32 ? bf16 : f32;
+    }
+    case SPO_WS_LOGPROBS_BWD: {
+      if (T < 0 || V < 1 || d < 1) return 0;
+      const size_t f32 = lp_bwd_ws_bytes(T, d, V, SPO_DTYPE_F32);
+      const size_t bf16 = (d % 64) == 0 ? lp_bwd_ws_bytes(T, d, V, SPO_DTYPE_BF16) : 0;
       return bf16 > f32 ? bf16 : f32;
     }
     default:

@@ -2,6 +2,7 @@
 // Nothing here is part of the public ABI (see include/spo.h).
 #pragma once
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -223,6 +224,55 @@ cudaError_t launch_gather_rows(const void* H, const int32_t* y, const float* lse
                                int32_t* y_act, float* lse_act, float* coef_act, int32_t* d_status, cudaStream_t st);
 cudaError_t launch_scatter_rows(const void* dH_act, const int32_t* rows, int64_t n_act, int64_t T, int32_t row_bytes,
                                 void* dH, cudaStream_t st);
+
+// ---- log-probability operators ---------------------------------------------
+constexpr int kMaxTopK = SPO_MAX_TOP_K;
+constexpr int kLpStreamRows = 128;        // bf16: up to this many token rows the vocabulary streams past them (one pass over W)
+struct LpFwd {
+  const void *H, *W;
+  int64_t ldh;
+  int32_t dtype;
+  const int32_t* y;
+  const uint8_t* mask;
+  int64_t T;
+  int32_t d, V;
+  float inv_t;
+  int top_k;
+  float *logp, *lse, *entropy;
+  int32_t* top_ids;
+  float* top_logp;
+  int32_t* d_status;
+};
+struct LpBwd {
+  const void *H, *W;
+  int64_t ldh;
+  int32_t dtype;
+  const int32_t* y;
+  const uint8_t* mask;
+  const float *lse, *ent, *g_logp, *g_lse, *g_ent;
+  int64_t T;
+  int32_t d, V;
+  float inv_t;
+  void* dH;
+  int32_t dH_dtype;
+  void* dW;
+  int32_t dW_dtype;
+  int accumulate;
+  int32_t* d_status;
+};
+int lp_list_len(int top_k);               // column groups listed per row, vocabulary split and column half
+int lp_fwd_lists(int64_t rows, int32_t d, int32_t V);   // lists (and partials) per row of a launch over `rows` rows
+cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
+                               float2* cand_max, uint32_t* progress, cudaStream_t st);
+cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_rows, int64_t ldg, float* partial,
+                               void* h_clean, uint32_t* progress, cudaStream_t st);
+// out[i][:] = H[t0 + i][:] (bf16, row pitch ldh), or zeros where mask[t0 + i] is 0
+cudaError_t launch_clean_rows(const void* H, int64_t ldh, const uint8_t* mask, int64_t t0, int64_t rows, int32_t d,
+                              void* out, cudaStream_t st);
+size_t lp_fwd_ws_bytes(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype);
+size_t lp_bwd_ws_bytes(int64_t T, int32_t d, int32_t V, int32_t dtype);
+cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st);
+cudaError_t lp_backward(const LpBwd& a, char* ws, cudaStream_t st);
 
 cudaError_t launch_bounded_wait_probe(int32_t* d_status, uint32_t limit_us, int32_t* reached_end, cudaStream_t st);
 

@@ -125,6 +125,16 @@ struct GemmParams {
   // a pair holds its loads back while it is more than `window` k-blocks ahead of the slowest pair.
   uint32_t* progress;
   int window;
+  // Log-probability operators (template argument LP >= 0)
+  float sc2;                                 // FWD / G: log2(e) / temperature
+  float* cand;                               // FWD: logits of the listed column groups, [list][cand_ld][top_k][32]
+  float2* cand_max;                          // FWD: (group maximum, group and slot) of the listed groups, [list][cand_ld][top_k]
+  int64_t cand_ld;                           // rows between two lists
+  int top_k;
+  const uint8_t* mask;                       // G: rows with mask 0 get g = 0
+  const float *ent, *g_logp, *g_lse, *g_ent; // G: entropy and upstream gradients per row (g_lse, g_ent + ent optional)
+  float inv_t;                               // G: 1 / temperature
+  const float* partial;                      // DW: fp32 sum of the earlier chunks, added before the rounding; NULL = none
 };
 
 // g = c_t (1[v = y_t] - 2^(z log2e - lse_t log2e)) for 32 consecutive columns, packed to bf16.
@@ -139,6 +149,36 @@ __device__ __forceinline__ void g_values(const uint32_t (&v)[32], int col0, floa
       const int jj = yt - col0;
 #pragma unroll
       for (int j = 0; j < 32; ++j) if (j == jj) g[j] += c;
+    }
+    if (col0 + 32 > cols_valid) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) if (col0 + j >= cols_valid) g[j] = 0.0f;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) g[j] = 0.0f;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    out4[q] = make_uint4(pack_bf16(g[8 * q + 0], g[8 * q + 1]), pack_bf16(g[8 * q + 2], g[8 * q + 3]),
+                         pack_bf16(g[8 * q + 4], g[8 * q + 5]), pack_bf16(g[8 * q + 6], g[8 * q + 7]));
+}
+
+// Gradient of a row's logits for upstream gradients of its log-prob, log-sum-exp and entropy:
+// with u = log2 p = z sc2 - lse2, g = 2^u (a + b u) + tgt 1[v = y_t] (a, b, tgt: see the row setup), packed to bf16.
+__device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, bool live, float sc2, float lse2, float a,
+                                            float b, float tgt, int yt, int cols_valid, uint4* out4) {
+  float g[32];
+  if (live) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float u = fmaf(__uint_as_float(v[j]), sc2, -lse2);
+      g[j] = fast_exp2(u) * fmaf(b, u, a);
+    }
+    if (yt >= col0 && yt < col0 + 32) {
+      const int jj = yt - col0;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) if (j == jj) g[j] += tgt;
     }
     if (col0 + 32 > cols_valid) {
 #pragma unroll
@@ -204,7 +244,15 @@ __device__ __forceinline__ Unit unit_of(int u, const GemmParams& p) {
 // ENT (FWD / E): also accumulate sum_v e z per row, from which the finalisation forms the entropy of
 // the row's softmax, lse - sum_v p z (one more multiply-add per logit; a separate instantiation so that
 // the kernels without it stay as they are).
-template <int MODE, bool ENT = false>
+// LP: the log-probability operators' variants.  -1: none (the policy loss).  FWD: logits carry a
+// temperature, and LP > 0 also lists, per row, vocabulary split and column half, the LP column groups (32
+// columns each) with the largest maxima: the K largest logits of a row lie in its K groups of largest
+// maximum, so a merge over the lists finds the row's top K.  The group maximum falls out of the online
+// softmax; the list is kept sorted in registers by LP compare-exchanges that the warp skips when none of its
+// rows has a group above its last entry, and a listed group's 32 logits are stored once, when it enters.
+// (A list of the logits themselves would be touched by nearly every group of 32 rows x 32 columns, in a
+// scan of every logit.)  G: general upstream gradients.  DW: bf16 result.
+template <int MODE, bool ENT = false, int LP = -1>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmParams p) {
   constexpr bool A_MN = (MODE == MODE_DW);
@@ -356,10 +404,36 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       float ez = 0.0f;                                                     // ENT: sum e z relative to m2
       int32_t yt = -1;
       float c = 0.0f, lse2 = 0.0f;                                         // G
+      constexpr int LIST = (MODE == MODE_FWD && LP > 0) ? LP : 1;
+      float top_v[LIST];                                                   // FWD with lists: group maxima, descending,
+      uint32_t top_p[LIST];                                                // ... and (group << 8 | slot)
+      if (MODE == MODE_FWD && LP > 0) {
+#pragma unroll
+        for (int i = 0; i < LIST; ++i) { top_v[i] = -CUDART_INF_F; top_p[i] = 0xFFFFFF00u | (uint32_t)i; }
+      }
+      const float sc2 = (MODE == MODE_FWD && LP >= 0) ? p.sc2 : kLog2e;
+      bool live = false;                                                   // G with LP: coefficients of g
+      float ga = 0.0f, gb = 0.0f, gt = 0.0f;
+      if (MODE == MODE_G && LP >= 0 && row_ok) {
+        // d logp: gl (1[v=y] - p);  d lse: glse p;  d entropy: -ge p (log p + ent);  all times 1/temperature
+        live = p.mask == nullptr || p.mask[grow] != 0;
+        float gl = p.g_logp ? p.g_logp[grow] : 0.0f;
+        const int32_t yy = p.y ? p.y[grow] : -1;
+        if (p.g_logp && (yy < 0 || yy >= p.cols_valid)) {                  // no such target: its log-prob is the constant -inf
+          if (live && p.d_status) atomicOr(p.d_status, SPO_DEV_ID_OUT_OF_RANGE);
+          gl = 0.0f;
+        }
+        const float ge = p.g_ent ? p.g_ent[grow] : 0.0f;
+        const float gs = p.g_lse ? p.g_lse[grow] : 0.0f;
+        gt = p.inv_t * gl;
+        ga = p.inv_t * (gs - gl - (p.g_ent ? ge * p.ent[grow] : 0.0f));
+        gb = -p.inv_t * ge * 0.69314718055994531f;
+        lse2 = p.lse[grow] * kLog2e;
+      }
       float rs = 1.0f;                                                     // DH: factor of this lane's output row
       if (MODE == MODE_FWD || MODE == MODE_G || MODE == MODE_E) {
-        if (row_ok) yt = p.y[grow];
-        if (MODE == MODE_G && row_ok) { c = p.grad_loss * p.coef[grow]; lse2 = p.lse[grow] * kLog2e; }
+        if (row_ok && (LP < 0 || p.y)) yt = p.y[grow];
+        if (MODE == MODE_G && LP < 0 && row_ok) { c = p.grad_loss * p.coef[grow]; lse2 = p.lse[grow] * kLog2e; }
         if (MODE == MODE_E) {
           // Reference exponent of the row: the largest logit of its first vocabulary tile (found by a
           // short launch beforehand) plus a margin, the same for every pair and column half that works
@@ -401,13 +475,41 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               mx0 = fmaxf(mx0, __uint_as_float(v[j]));
               mx1 = fmaxf(mx1, __uint_as_float(v[j + 1]));
             }
-            const float mn = fmaxf(m2, fmaxf(mx0, mx1) * kLog2e);
+            if (MODE == MODE_FWD && LP > 0) {
+              const float mx = row_ok ? fmaxf(mx0, mx1) : -CUDART_INF_F;
+              const bool enters = mx > top_v[LIST - 1];
+              if (__any_sync(0xffffffffu, enters)) {
+                const uint32_t slot = top_p[LIST - 1] & 255u;
+                float x = enters ? mx : -CUDART_INF_F;
+                uint32_t px = ((uint32_t)(col0 >> 5) << 8) | slot;
+                bool above = false;
+#pragma unroll
+                for (int i = 0; i < LIST; ++i) {                       // from its place on everything moves down one:
+                  above = above || x > top_v[i];                       // equal maxima keep their order of arrival
+                  const float tv = top_v[i];
+                  const uint32_t tp = top_p[i];
+                  top_v[i] = above ? x : tv;
+                  top_p[i] = above ? px : tp;
+                  x = above ? tv : x;
+                  px = above ? tp : px;
+                }
+                if (enters) {
+                  float4* dst = reinterpret_cast<float4*>(
+                      p.cand + (((int64_t)((u % p.nsplit) * 2 + half) * p.cand_ld + (grow - p.part_row0)) * LIST + slot) * 32);
+#pragma unroll
+                  for (int q = 0; q < 8; ++q)
+                    dst[q] = make_float4(__uint_as_float(v[4 * q]), __uint_as_float(v[4 * q + 1]),
+                                         __uint_as_float(v[4 * q + 2]), __uint_as_float(v[4 * q + 3]));
+                }
+              }
+            }
+            const float mn = fmaxf(m2, fmaxf(mx0, mx1) * sc2);
             const float neg = -mn;
             float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
-              const float e0 = fast_exp2(fmaf(__uint_as_float(v[j]), kLog2e, neg));
-              const float e1 = fast_exp2(fmaf(__uint_as_float(v[j + 1]), kLog2e, neg));
+              const float e0 = fast_exp2(fmaf(__uint_as_float(v[j]), sc2, neg));
+              const float e1 = fast_exp2(fmaf(__uint_as_float(v[j + 1]), sc2, neg));
               s0 += e0;
               s1 += e1;
               if (ENT) {
@@ -492,7 +594,8 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               }
             }
           }
-        } else if (MODE == MODE_G || (MODE == MODE_DH && p.out_bf16)) {
+        } else if (MODE == MODE_G || (MODE == MODE_DH && p.out_bf16) ||
+                   (MODE == MODE_DW && LP >= 0 && !p.partial && !p.accumulate)) {
           // bf16 outputs: 64 columns (128 bytes per row) per staging round
           __nv_bfloat16* obase = MODE == MODE_G
               ? p.G + ((int64_t)un.m_tile * GROUP_M + warp_row0) * p.ldg
@@ -509,10 +612,15 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             tmem_wait_ld(v1);
             uint4 piece[8];
             if (MODE == MODE_G) {
-              g_values(v0, col0, c, lse2, yt, p.cols_valid, piece);
-              g_values(v1, col0 + 32, c, lse2, yt, p.cols_valid, piece + 4);
+              if (LP >= 0) {
+                g_values_lp(v0, col0, live, p.sc2, lse2, ga, gb, gt, yt, p.cols_valid, piece);
+                g_values_lp(v1, col0 + 32, live, p.sc2, lse2, ga, gb, gt, yt, p.cols_valid, piece + 4);
+              } else {
+                g_values(v0, col0, c, lse2, yt, p.cols_valid, piece);
+                g_values(v1, col0 + 32, c, lse2, yt, p.cols_valid, piece + 4);
+              }
             } else {
-              if (p.rowscale) {                    // one-pass path: the row's factor (a zero factor gives exact zeros)
+              if (MODE == MODE_DH && p.rowscale) {                    // one-pass path: the row's factor (a zero factor gives exact zeros)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {
                   v0[j] = __float_as_uint(rs == 0.0f ? 0.0f : __uint_as_float(v0[j]) * rs);
@@ -556,6 +664,25 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               int r, cc;
               const uint4 raw4 = stage_get(stage, lane, i, r, cc);
               if (grow_warp0 + r < p.rows_valid) {
+                if (MODE == MODE_DW && LP >= 0) {
+                  // bf16 result: this launch's term, the earlier chunks' fp32 sum and (accumulating) the old
+                  // value are added in fp32 and rounded once
+                  const int64_t at = (grow_warp0 + r) * p.ldo + col0 + cc * 4;
+                  float4 val = make_float4(__uint_as_float(raw4.x), __uint_as_float(raw4.y), __uint_as_float(raw4.z),
+                                           __uint_as_float(raw4.w));
+                  if (p.partial) {
+                    const float4 old = *reinterpret_cast<const float4*>(p.partial + at);
+                    val.x += old.x; val.y += old.y; val.z += old.z; val.w += old.w;
+                  }
+                  uint2* dst16 = reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + at);
+                  if (p.accumulate) {
+                    const uint2 old = *dst16;
+                    val.x += __uint_as_float(old.x << 16); val.y += __uint_as_float(old.x & 0xFFFF0000u);
+                    val.z += __uint_as_float(old.y << 16); val.w += __uint_as_float(old.y & 0xFFFF0000u);
+                  }
+                  *dst16 = make_uint2(pack_bf16(val.x, val.y), pack_bf16(val.z, val.w));
+                  continue;
+                }
                 float* dst = obase + (int64_t)r * p.ldo + col0 + cc * 4;
                 if (MODE == MODE_DW && p.n_shards > 0) {
                   // reduce-scatter form: this tile, plus the sum of the earlier chunks' tiles held in `out`,
@@ -595,6 +722,11 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         FwdPartial part;
         part.m2 = m2; part.l = l; part.zt = zt; part.pad = ez;
         p.partials[(int64_t)((u % p.nsplit) * 2 + half) * p.T + (grow - p.part_row0)] = part;
+        if (MODE == MODE_FWD && LP > 0) {
+          float2* dst = p.cand_max + ((int64_t)((u % p.nsplit) * 2 + half) * p.cand_ld + (grow - p.part_row0)) * LIST;
+#pragma unroll
+          for (int i = 0; i < LIST; ++i) dst[i] = make_float2(top_v[i], __uint_as_float(top_p[i]));
+        }
       }
     }
   }
@@ -677,7 +809,7 @@ int group_count() { return sm_count() / CG; }
 // CTA pairs of this instantiation that can be resident together on a device (0 = not yet asked).
 // The kernel is persistent and its pairs pace one another, so a grid must not exceed it.  One slot
 // per device, filled once; concurrent first calls compute the same value (atomic stores).
-template <int MODE, bool ENT>
+template <int MODE, bool ENT, int LP>
 cudaError_t resident_groups(int* out) {
   static std::atomic<int> cached[64];
   int dev = 0;
@@ -686,7 +818,7 @@ cudaError_t resident_groups(int* out) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   int n = cached[dev].load(std::memory_order_acquire);
   if (n == 0) {
-    e = cudaFuncSetAttribute(spo_gemm_kernel<MODE, ENT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    e = cudaFuncSetAttribute(spo_gemm_kernel<MODE, ENT, LP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t q = {};
     q.gridDim = dim3(group_count() * CG, 1, 1);
@@ -699,7 +831,7 @@ cudaError_t resident_groups(int* out) {
     qa[0].val.clusterDim.z = 1;
     q.attrs = qa;
     q.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(&n, spo_gemm_kernel<MODE, ENT>, &q);
+    e = cudaOccupancyMaxActiveClusters(&n, spo_gemm_kernel<MODE, ENT, LP>, &q);
     if (e != cudaSuccess) return e;
     if (n < 1) return cudaErrorLaunchOutOfResources;
     if (n > group_count()) n = group_count();
@@ -709,11 +841,11 @@ cudaError_t resident_groups(int* out) {
   return cudaSuccess;
 }
 
-template <int MODE, bool ENT = false>
+template <int MODE, bool ENT = false, int LP = -1>
 cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmParams& p_in, uint32_t* progress,
                         cudaStream_t st) {
   int max_groups = 0;
-  cudaError_t e0 = resident_groups<MODE, ENT>(&max_groups);
+  cudaError_t e0 = resident_groups<MODE, ENT, LP>(&max_groups);
   if (e0 != cudaSuccess) return e0;
   const int units = p_in.m_tiles * p_in.nsplit;
   if (units <= 0) return cudaSuccess;
@@ -741,7 +873,7 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmPa
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, spo_gemm_kernel<MODE, ENT>, a, b, p);
+  return cudaLaunchKernelEx(&cfg, spo_gemm_kernel<MODE, ENT, LP>, a, b, p);
 }
 
 // Operand box heights (rows per TMA box) for K-major operands.
@@ -932,6 +1064,122 @@ cudaError_t launch_bwd_bf16(const void* H, const void* W, const int32_t* y, cons
     if ((e = launch_dw(mG_mn, mH_mn, t0, rows, d, V, dW, (accumulate || chunk > 0) ? 1 : 0, 0,
                        (int)ceil_div(V, GROUP_M), progress, d_status, st)) != cudaSuccess)
       return e;
+  }
+  return cudaSuccess;
+}
+
+// ---------------------------------------------------------------------------
+// Log-probability operators: the forward's contraction with a temperature and lists of the largest
+// column groups, and the chunked backward for general upstream gradients.
+// ---------------------------------------------------------------------------
+int lp_list_len(int top_k) { return top_k == 0 ? 0 : top_k <= 8 ? 8 : kMaxTopK; }
+
+int lp_fwd_lists(int64_t rows, int32_t d, int32_t V) { return 2 * fwd_unit_splits(rows, d, V); }
+
+cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
+                               float2* cand_max, uint32_t* progress, cudaStream_t st) {
+  CUtensorMap ma, mb;
+  if (!make_map(&ma, a.H, a.d, a.T, a.ldh, kBoxA) || !make_map(&mb, a.W, a.d, a.V, a.d, kBoxB))
+    return cudaErrorInvalidValue;
+  GemmParams p{};
+  p.m_tiles = (int)ceil_div(rows, GROUP_M);
+  p.n_tiles = (int)ceil_div(a.V, BN);
+  p.nsplit = fwd_unit_splits(rows, a.d, a.V);
+  p.per_split = (int)ceil_div(p.n_tiles, p.nsplit);
+  p.k_blocks = (int)ceil_div(a.d, BK);
+  p.a_row0 = (int)t0;
+  p.rows_valid = t0 + rows;
+  p.cols_valid = a.V;
+  p.out_row0 = t0;
+  p.y = a.y;
+  p.partials = partials;
+  p.T = rows;
+  p.part_row0 = t0;
+  p.d_status = a.d_status;
+  p.sc2 = kLog2e * a.inv_t;
+  p.cand = cand;
+  p.cand_max = cand_max;
+  p.cand_ld = rows;
+  const int list = lp_list_len(a.top_k);
+  const bool ent = a.entropy != nullptr;
+  if (list == 0) return ent ? launch_gemm<MODE_FWD, true, 0>(ma, mb, p, progress, st)
+                            : launch_gemm<MODE_FWD, false, 0>(ma, mb, p, progress, st);
+  if (list == 8) return ent ? launch_gemm<MODE_FWD, true, 8>(ma, mb, p, progress, st)
+                            : launch_gemm<MODE_FWD, false, 8>(ma, mb, p, progress, st);
+  return ent ? launch_gemm<MODE_FWD, true, kMaxTopK>(ma, mb, p, progress, st)
+             : launch_gemm<MODE_FWD, false, kMaxTopK>(ma, mb, p, progress, st);
+}
+
+// bf16 backward for general upstream gradients, chunk by chunk as launch_bwd_bf16: the chunk's logit
+// gradient, dH = G W, dW (+)= G^T H.  A bf16 dW over several chunks is summed in fp32 (`partial`) and
+// rounded once, in the last chunk's epilogue.
+cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_rows, int64_t ldg, float* partial,
+                               void* h_clean, uint32_t* progress, cudaStream_t st) {
+  CUtensorMap mH_k, mW_k, mW_mn, mH_mn;
+  if (!make_map(&mH_k, a.H, a.d, a.T, a.ldh, kBoxA) || !make_map(&mW_k, a.W, a.d, a.V, a.d, kBoxB) ||
+      !make_map(&mW_mn, a.W, a.d, a.V, a.d, 64))
+    return cudaErrorInvalidValue;
+  const int n_tiles_v = (int)ceil_div(a.V, BN), tiles_v = (int)ceil_div(a.V, GROUP_M);
+  cudaError_t e;
+  for (int64_t t0 = 0; t0 < a.T; t0 += chunk_rows) {
+    const int64_t rows = (a.T - t0) < chunk_rows ? (a.T - t0) : chunk_rows;
+    const int m_tiles = (int)ceil_div(rows, GROUP_M);
+    const bool last = t0 + rows >= a.T;
+    CUtensorMap mG_k, mG_mn;
+    if (!make_map(&mG_k, G, a.V, rows, ldg, kBoxA) || !make_map(&mG_mn, G, a.V, rows, ldg, 64))
+      return cudaErrorInvalidValue;
+    {
+      GemmParams p{};
+      p.m_tiles = m_tiles;
+      p.n_tiles = n_tiles_v;
+      p.nsplit = pick_fwd_split(m_tiles, n_tiles_v, a.d);
+      p.per_split = (int)ceil_div(n_tiles_v, p.nsplit);
+      p.k_blocks = (int)ceil_div(a.d, BK);
+      p.a_row0 = (int)t0;
+      p.rows_valid = a.T;
+      p.cols_valid = a.V;
+      p.out_row0 = t0;
+      p.y = a.y; p.lse = a.lse; p.mask = a.mask; p.ent = a.ent;
+      p.g_logp = a.g_logp; p.g_lse = a.g_lse; p.g_ent = a.g_ent;
+      p.inv_t = a.inv_t; p.sc2 = kLog2e * a.inv_t;
+      p.G = G; p.ldg = ldg;
+      p.d_status = a.d_status;
+      if ((e = launch_gemm<MODE_G, false, 0>(mH_k, mW_k, p, progress, st)) != cudaSuccess) return e;
+    }
+    if ((e = launch_dh(mG_k, mW_mn, t0, rows, a.T, a.d, a.V, a.dH, a.dH_dtype, nullptr, progress, a.d_status, st)) !=
+        cudaSuccess)
+      return e;
+    // The gradient of a masked row is zero, but zero times a NaN in that row of H is not: with a mask the
+    // dW contraction reads a copy of the chunk's rows in which the masked ones are zero.
+    int64_t h_row0 = t0;
+    if (a.mask) {
+      if ((e = launch_clean_rows(a.H, a.ldh, a.mask, t0, rows, a.d, h_clean, st)) != cudaSuccess) return e;
+      h_row0 = 0;
+      if (!make_map(&mH_mn, h_clean, a.d, rows, a.d, 64)) return cudaErrorInvalidValue;
+    } else if (!make_map(&mH_mn, a.H, a.d, a.T, a.ldh, 64)) {
+      return cudaErrorInvalidValue;
+    }
+    if (a.dW_dtype == SPO_DTYPE_F32) {
+      e = launch_dw(mG_mn, mH_mn, h_row0, rows, a.d, a.V, (float*)a.dW, (a.accumulate || t0 > 0) ? 1 : 0, 0, tiles_v,
+                    progress, a.d_status, st);
+    } else if (!last) {
+      e = launch_dw(mG_mn, mH_mn, h_row0, rows, a.d, a.V, partial, t0 > 0 ? 1 : 0, 0, tiles_v, progress, a.d_status, st);
+    } else {
+      GemmParams p{};
+      p.m_tiles = tiles_v;
+      p.n_tiles = (int)ceil_div(a.d, BN);
+      p.nsplit = p.n_tiles;
+      p.per_split = 1;
+      p.k_blocks = (int)ceil_div(rows, BK);
+      p.b_k0 = (int)h_row0;
+      p.rows_valid = a.V;
+      p.cols_valid = a.d;
+      p.out = a.dW; p.out_bf16 = 1; p.ldo = a.d; p.accumulate = a.accumulate;
+      p.partial = t0 > 0 ? partial : nullptr;
+      p.d_status = a.d_status;
+      e = launch_gemm<MODE_DW, false, 0>(mG_mn, mH_mn, p, progress, st);
+    }
+    if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
