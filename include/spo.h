@@ -81,6 +81,7 @@ extern "C" {
 #define SPO_WS_LOSS_FWD_BWD_ROWS 8
 #define SPO_WS_LOGPROBS       9
 #define SPO_WS_LOGPROBS_BWD  10
+#define SPO_WS_MUON          11   /* T = rows m, d = columns n, B = matrices */
 
 /*
  * Hyper-parameters.  Defaults (spo_default_params) are the values the paper prints:
@@ -568,6 +569,47 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
                          const float* g_entropy, int64_t T, int32_t d, int32_t V, float inv_temperature,
                          void* dH, int32_t dH_dtype, void* dW, int32_t dW_dtype, int32_t dW_accumulate,
                          void* ws, size_t ws_bytes, int32_t* d_status, void* stream);
+
+/*
+ * Orthogonalised (Muon) weight updates, the step that consumes a gradient such as the loss calls' dW
+ * (Algorithm 1, "update the policy parameters"; the paper leaves the optimiser open).  For each m x n matrix U:
+ *   X_0 = U / (|U|_F + eps);  `steps` times:  A = X X^T,  X <- coef_a X + (coef_b A + coef_c A A) X
+ * which drives the singular values of U towards one while keeping its singular vectors (for m > n the same
+ * polynomial through X^T X).  spo_muon_update puts momentum in front and the weights behind it:
+ *   M <- momentum M + G;  U = G + momentum M (nesterov) or M;
+ *   W <- (1 - lr weight_decay) W - lr scale X,  scale = 1 (SPO_MUON_SCALE_NONE), sqrt(max(1, m/n))
+ *   (SPO_MUON_SCALE_SPECTRAL) or 0.2 sqrt(max(m, n)) (SPO_MUON_SCALE_RMS).
+ * Iterates are pairs of fp16 numbers (22 bits), products fp16 with fp32 sums; the Frobenius norm is summed in
+ * fp64 in a fixed order, so results repeat bit for bit.
+ *
+ *   G         device in  [batch][m][n], fp32 or bf16 (dtype)
+ *   out       device out [batch][m][n], fp32 or bf16; may be G itself when the types agree
+ *   W         device in/out [batch][m][n], fp32 or bf16;  momentum  device in/out [batch][m][n] fp32
+ *   ws        device scratch, spo_workspace_bytes(SPO_WS_MUON, m, n, 0, 0, batch, 0) bytes
+ * A matrix whose U holds a NaN or an infinity sets SPO_DEV_NONFINITE; its out is zero, its W and momentum are
+ * left as they were (the other matrices of the batch are not affected).  A zero U gives X = 0.
+ * Limits: 1 <= m, n < 2^24, min(m, n) <= 65536, 0 <= batch <= 65535.
+ */
+#define SPO_MUON_SCALE_NONE      0
+#define SPO_MUON_SCALE_SPECTRAL  1
+#define SPO_MUON_SCALE_RMS       2
+typedef struct spo_muon_params {
+  float   lr;             /* 0.02 */
+  float   momentum;       /* 0.95, in [0, 1) */
+  float   weight_decay;   /* 0 */
+  float   eps;            /* 1e-7, > 0 */
+  float   coef_a, coef_b, coef_c;   /* 3.4445, -4.7750, 2.0315 */
+  int32_t steps;          /* 5, 1 .. 16 */
+  int32_t nesterov;       /* 1 */
+  int32_t scale_mode;     /* SPO_MUON_SCALE_SPECTRAL */
+} spo_muon_params;
+int32_t spo_default_muon_params(spo_muon_params* p /* host, out */);
+int32_t spo_orthogonalize(const void* G, int32_t G_dtype, int32_t batch, int64_t m, int64_t n,
+                          void* out, int32_t out_dtype, void* ws, size_t ws_bytes,
+                          const spo_muon_params* params, int32_t* d_status, void* stream);
+int32_t spo_muon_update(void* W, int32_t W_dtype, float* momentum, const void* G, int32_t G_dtype,
+                        int32_t batch, int64_t m, int64_t n, void* ws, size_t ws_bytes,
+                        const spo_muon_params* params, int32_t* d_status, void* stream);
 
 /* Scratch size in bytes for one call of the selected entry point (host only, no CUDA call
  * except a device-property query).  Arguments that the selected call does not use are ignored. */

@@ -83,3 +83,23 @@ def muon_update(w, momentum, g, lr, mu, weight_decay=0.0, nesterov=True, mode=0,
     m = mu * np.asarray(momentum, np.float64) + g
     o = newton_schulz(g + mu * m if nesterov else m, steps, coefficients, eps)
     return (1.0 - lr * weight_decay) * w - lr * muon_scale(*w.shape, mode) * o, m, o
+
+
+def newton_schulz_rounded(g, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7):
+    """The same iteration with fp16 roundings where the library documents them (iterate as a pair of fp16 numbers scaled
+    by a power of two, the Gram matrix and the polynomial once each), everything else in 64 bits: what those roundings
+    alone do to a given input, which is what a tolerance has to allow for."""
+    a, b, c = coefficients
+    x = np.asarray(g, np.float64)
+    tall = x.shape[0] > x.shape[1]
+    if tall:
+        x = x.T
+    half = lambda z: z.astype(np.float16).astype(np.float64)  # noqa: E731
+    s = 2.0 ** np.round(np.log2(np.sqrt(max(x.shape))))
+    x = x / (np.linalg.norm(x) + eps) * s
+    for _ in range(steps):
+        hi = half(x)
+        pair = hi + half(x - hi)
+        q = half(hi @ hi.T / s**2)
+        x = a * pair + half(b * q + c * (q @ q)) @ hi
+    return (x.T if tall else x) / s

@@ -21,15 +21,18 @@ ERR_UNSUPPORTED_DTYPE, ERR_UNSUPPORTED_ARCH, ERR_WORKSPACE_TOO_SMALL, ERR_CUDA =
 DEV_ID_OUT_OF_RANGE, DEV_NONFINITE, DEV_UNIFORMS_EXHAUSTED, DEV_TIMEOUT, DEV_ZERO_TOTAL_WEIGHT = 1, 2, 4, 8, 16
 DTYPE_F32, DTYPE_BF16 = 0, 1
 (WS_SAMPLE, WS_ADVANTAGES, WS_LOSS_FWD, WS_LOSS_BWD, WS_UPDATE_REPEATS, WS_ACTIVE_ROWS, WS_LOSS_BWD_ROWS,
- WS_LOSS_FWD_BWD, WS_LOSS_FWD_BWD_ROWS, WS_LOGPROBS, WS_LOGPROBS_BWD) = range(11)
+ WS_LOSS_FWD_BWD, WS_LOSS_FWD_BWD_ROWS, WS_LOGPROBS, WS_LOGPROBS_BWD,
+ WS_MUON) = range(12)
 AGG_TOKEN_MEAN, AGG_SEQ_MEAN = 0, 1
 SUR_PPO_CLIP, SUR_CISPO, SUR_GSPO = 0, 1, 2
+MUON_SCALE_NONE, MUON_SCALE_SPECTRAL, MUON_SCALE_RMS = 0, 1, 2
 
 EXPORTS = [
     "spo_default_params", "spo_tracker_init", "spo_sample_prompts", "spo_advantages",
     "spo_advantages_static", "spo_advantages_apply", "spo_advantages_update",
     "spo_tracker_update", "spo_tracker_update_repeats", "spo_loss_fwd", "spo_loss_bwd", "spo_loss_fwd_bwd", "spo_loss_fwd_bwd_slabs", "spo_dw_slab_rows", "spo_loss_fwd_bwd_scatter", "spo_loss_stats", "spo_loss_mask_rows", "spo_loss_fwd_bwd_rows", "spo_loss_active_rows", "spo_loss_bwd_rows",
-    "spo_logprobs", "spo_logprobs_bwd", "spo_workspace_bytes",
+    "spo_logprobs", "spo_logprobs_bwd", "spo_default_muon_params", "spo_orthogonalize", "spo_muon_update",
+    "spo_workspace_bytes",
     "spo_status_string", "spo_last_cuda_error", "spo_version", "spo_selftest_bounded_wait",
 ]
 
@@ -41,6 +44,14 @@ class SpoParams(Structure):
         ("agg_mode", c_int32), ("global_tokens", c_int32), ("global_responses", c_int32),
         ("surrogate", c_int32), ("dual_clip", c_float), ("near_zero_tau_lo", c_float),
         ("near_zero_tau_hi", c_float),
+    ]
+
+
+class SpoMuonParams(Structure):
+    _fields_ = [
+        ("lr", c_float), ("momentum", c_float), ("weight_decay", c_float), ("eps", c_float),
+        ("coef_a", c_float), ("coef_b", c_float), ("coef_c", c_float),
+        ("steps", c_int32), ("nesterov", c_int32), ("scale_mode", c_int32),
     ]
 
 
@@ -122,6 +133,12 @@ def lib():
                                        c_void_p, c_void_p, c_void_p, c_int64, c_int32, c_int32, c_float,
                                        c_void_p, c_int32, c_void_p, c_int32, c_int32,
                                        c_void_p, c_size_t, c_void_p, c_void_p]
+        PM = POINTER(SpoMuonParams)
+        L.spo_default_muon_params.argtypes = [PM]
+        L.spo_orthogonalize.argtypes = [c_void_p, c_int32, c_int32, c_int64, c_int64, c_void_p, c_int32,
+                                        c_void_p, c_size_t, PM, c_void_p, c_void_p]
+        L.spo_muon_update.argtypes = [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_int64, c_int64,
+                                      c_void_p, c_size_t, PM, c_void_p, c_void_p]
         L.spo_selftest_bounded_wait.argtypes = [ctypes.c_uint32, c_void_p, c_void_p, c_void_p]
         L.spo_workspace_bytes.argtypes = [c_int32, c_int64, c_int32, c_int32, c_int64, c_int32, c_int32]
         L.spo_workspace_bytes.restype = c_size_t
@@ -440,3 +457,44 @@ def spo_logprobs_bwd(H, W, y, mask, lse, entropy, g_logp, g_lse, g_entropy, dH, 
                                   _ptr(g_logp), _ptr(g_lse), _ptr(g_entropy), T, d, V, c_float(inv_temperature),
                                   _ptr(dH), _dtype_code(dH), _ptr(dW), _dtype_code(dW), int(dW_accumulate), w, n,
                                   _ptr(d_status), _stream()), "spo_logprobs_bwd")
+
+
+def default_muon_params(**overrides) -> SpoMuonParams:
+    p = SpoMuonParams()
+    _check(lib().spo_default_muon_params(ctypes.byref(p)), "spo_default_muon_params")
+    for k, v in overrides.items():
+        setattr(p, k, v)
+    return p
+
+
+def _matrices(G):
+    """(batch, m, n) of a matrix or a batch of them."""
+    import torch
+    if not isinstance(G, torch.Tensor) or G.dim() not in (2, 3):
+        raise ValueError("expected a matrix [m, n] or a batch of matrices [batch, m, n]")
+    return (1, *G.shape) if G.dim() == 2 else tuple(G.shape)
+
+
+def spo_orthogonalize(G, out, ws, params, d_status):
+    """out = the Newton-Schulz orthogonalisation of the matrix (or of each matrix of the batch) G."""
+    import torch
+    b, m, n = _matrices(G)
+    _need("G", G, G.dtype, G.shape)
+    _need("out", out, out.dtype, G.shape)
+    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
+    w, nb = _scratch(ws)
+    _check(lib().spo_orthogonalize(_ptr(G), _dtype_code(G), b, m, n, _ptr(out), _dtype_code(out), w, nb,
+                                   ctypes.byref(params), _ptr(d_status), _stream()), "spo_orthogonalize")
+
+
+def spo_muon_update(W, momentum, G, ws, params, d_status):
+    """One Muon step of W (in place) for the gradient G, with the fp32 momentum buffer (in place)."""
+    import torch
+    b, m, n = _matrices(G)
+    _need("G", G, G.dtype, G.shape)
+    _need("W", W, W.dtype, G.shape)
+    _need("momentum", momentum, torch.float32, G.shape)
+    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
+    w, nb = _scratch(ws)
+    _check(lib().spo_muon_update(_ptr(W), _dtype_code(W), _ptr(momentum), _ptr(G), _dtype_code(G), b, m, n, w, nb,
+                                 ctypes.byref(params), _ptr(d_status), _stream()), "spo_muon_update")

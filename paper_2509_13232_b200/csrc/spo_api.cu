@@ -1,6 +1,7 @@
 // C-ABI entry points of libspo: argument checks, workspace carving, dispatch.
 // See include/spo.h for the contract of every call.
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 #include <string.h>
 
@@ -679,6 +680,79 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);
 }
 
+int32_t spo_default_muon_params(spo_muon_params* p) {
+  if (!p) return SPO_ERR_INVALID_ARG;
+  p->lr = 0.02f;
+  p->momentum = 0.95f;
+  p->weight_decay = 0.0f;
+  p->eps = 1e-7f;
+  p->coef_a = 3.4445f;
+  p->coef_b = -4.7750f;
+  p->coef_c = 2.0315f;
+  p->steps = 5;
+  p->nesterov = 1;
+  p->scale_mode = SPO_MUON_SCALE_SPECTRAL;
+  return SPO_OK;
+}
+
+static bool muon_params_ok(const spo_muon_params* p) {
+  if (!p) return false;
+  const float big = 3.0e38f;
+  if (!(p->lr > -big && p->lr < big) || !(p->weight_decay > -big && p->weight_decay < big)) return false;
+  if (!(p->momentum >= 0.0f) || !(p->momentum < 1.0f) || !(p->eps > 0.0f) || !(p->eps < big)) return false;
+  for (float c : {p->coef_a, p->coef_b, p->coef_c})
+    if (!(c > -100.0f && c < 100.0f)) return false;
+  if (p->steps < 1 || p->steps > 16 || (p->nesterov != 0 && p->nesterov != 1)) return false;
+  return p->scale_mode >= SPO_MUON_SCALE_NONE && p->scale_mode <= SPO_MUON_SCALE_RMS;
+}
+
+static bool muon_shape_ok(int64_t batch, int64_t m, int64_t n) {
+  return batch >= 0 && batch <= 65535 && m >= 1 && n >= 1 && m < (1 << 24) && n < (1 << 24) && (m < n ? m : n) <= 65536;
+}
+
+static int32_t check_muon(const void* G, int32_t G_dtype, int32_t batch, int64_t m, int64_t n, const void* out,
+                          int32_t out_dtype, const float* momentum, bool update, const void* ws, size_t ws_bytes,
+                          const spo_muon_params* params) {
+  for (int32_t t : {G_dtype, out_dtype})
+    if (t != SPO_DTYPE_F32 && t != SPO_DTYPE_BF16) return SPO_ERR_UNSUPPORTED_DTYPE;
+  if (batch < 0 || m < 1 || n < 1 || !muon_params_ok(params)) return SPO_ERR_INVALID_ARG;
+  if (!muon_shape_ok(batch, m, n)) return SPO_ERR_BAD_SHAPE;
+  if (batch > 0 && (!G || !out || !ws || (update && !momentum))) return SPO_ERR_INVALID_ARG;
+  if (!aligned16(G) || !aligned16(out) || !aligned16(momentum) || !aligned16(ws)) return SPO_ERR_BAD_ALIGNMENT;
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  if (batch > 0 && ws_bytes < muon_ws_bytes(m, n, batch)) return SPO_ERR_WORKSPACE_TOO_SMALL;
+  return SPO_OK;
+}
+
+int32_t spo_orthogonalize(const void* G, int32_t G_dtype, int32_t batch, int64_t m, int64_t n, void* out,
+                          int32_t out_dtype, void* ws, size_t ws_bytes, const spo_muon_params* params,
+                          int32_t* d_status, void* stream) {
+  const int32_t rc = check_muon(G, G_dtype, batch, m, n, out, out_dtype, nullptr, false, ws, ws_bytes, params);
+  if (rc != SPO_OK) return rc;
+  MuonArgs a{};
+  a.G = G; a.G_dtype = G_dtype; a.batch = batch; a.m = m; a.n = n; a.out = out; a.out_dtype = out_dtype;
+  a.params = params; a.d_status = d_status;
+  cudaError_t e = muon_run(a, (char*)ws, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
+int32_t spo_muon_update(void* W, int32_t W_dtype, float* momentum, const void* G, int32_t G_dtype, int32_t batch,
+                        int64_t m, int64_t n, void* ws, size_t ws_bytes, const spo_muon_params* params,
+                        int32_t* d_status, void* stream) {
+  const int32_t rc = check_muon(G, G_dtype, batch, m, n, W, W_dtype, momentum, true, ws, ws_bytes, params);
+  if (rc != SPO_OK) return rc;
+  MuonArgs a{};
+  a.G = G; a.G_dtype = G_dtype; a.momentum = momentum; a.batch = batch; a.m = m; a.n = n; a.out = W; a.out_dtype = W_dtype;
+  a.update = 1;
+  const double longer = (double)(m > n ? m : n), ratio = (double)m / (double)n;
+  a.update_scale = params->scale_mode == SPO_MUON_SCALE_RMS        ? (float)(0.2 * sqrt(longer))
+                   : params->scale_mode == SPO_MUON_SCALE_SPECTRAL ? (float)sqrt(ratio > 1.0 ? ratio : 1.0)
+                                                                   : 1.0f;
+  a.params = params; a.d_status = d_status;
+  cudaError_t e = muon_run(a, (char*)ws, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
 size_t spo_workspace_bytes(int32_t which, int64_t T, int32_t d, int32_t V, int64_t N, int32_t B, int32_t M) {
   switch (which) {
     case SPO_WS_SAMPLE:
@@ -726,6 +800,9 @@ size_t spo_workspace_bytes(int32_t which, int64_t T, int32_t d, int32_t V, int64
       const size_t bf16 = (d % 64) == 0 ? lp_bwd_ws_bytes(T, d, V, SPO_DTYPE_BF16) : 0;
       return bf16 > f32 ? bf16 : f32;
     }
+    case SPO_WS_MUON:                   /* T = rows, d = columns, B = matrices */
+      if (!muon_shape_ok(B, T, d)) return 0;
+      return muon_ws_bytes(T, d, B);
     default:
       return 0;
   }

@@ -274,6 +274,23 @@ size_t lp_bwd_ws_bytes(int64_t T, int32_t d, int32_t V, int32_t dtype);
 cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st);
 cudaError_t lp_backward(const LpBwd& a, char* ws, cudaStream_t st);
 
+// ---- orthogonalised updates -------------------------------------------------
+struct MuonArgs {
+  const void* G;
+  int32_t G_dtype;
+  float* momentum;          // NULL: the update is G itself
+  int batch;
+  int64_t m, n;
+  void* out;                // orthogonalised update, or (update) the weights
+  int32_t out_dtype;
+  int update;
+  float update_scale;
+  const spo_muon_params* params;
+  int32_t* d_status;
+};
+size_t muon_ws_bytes(int64_t m, int64_t n, int64_t batch);
+cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st);
+
 cudaError_t launch_bounded_wait_probe(int32_t* d_status, uint32_t limit_us, int32_t* reached_end, cudaStream_t st);
 
 }  // namespace spo
