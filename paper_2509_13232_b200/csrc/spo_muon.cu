@@ -5,20 +5,20 @@
 // and nothing is ever transposed.)
 //
 // Numbers.  The iteration multiplies small singular values by a per step (a^5 = 485), and with them
-// every rounding made in X while they are small.  So X is held as a pair of fp16 numbers, hi + lo
-// (22 bits), times s = 2^round(log2 sqrt(max(m, n))), which puts the entries of an orthogonal matrix near one: the
-// term a X is formed from the pair in fp32, and only hi enters the products, whose spectrum is small where X's
-// is.  Measured against 64 bits for a 512 x 512 update of rank 16 under no noise: pair 4e-4, fp16 without lo
-// 4e-2, bf16 0.33 (a full-rank Gaussian: 1.5e-3, 1.3e-3, 1.1e-2).  fp16 rather than bf16 because everything
+// every rounding made in X while they are small.  So X is held twice, in fp32 for the term a X and in fp16
+// for the products, whose spectrum is small where X's is; both times s = 2^round(log2 sqrt(max(m, n))), which
+// puts the entries of an orthogonal matrix near one.  Errors against 64 bits for a 512 x 512 update of rank 16
+// under no noise: this 4e-4, fp16 alone 4e-2, bf16 alone 0.33 (a full-rank Gaussian: 1.5e-3, 1.3e-3, 1.1e-2).  fp16 rather than bf16 because everything
 // here is bounded by about 10 in magnitude and fp16 has 8 times finer steps.  A and b A + c A A are rounded
 // to fp16 once each; all sums are fp32.
 //
-// Work.  A and A A are symmetric: only the tiles on and above the diagonal are computed and stored twice,
-// 3 m^2 n + m^3 operations a step for m <= n instead of 4 m^2 n + 2 m^3.  Five steps of a 4096 x 4096
+// Work.  A and A A are symmetric: only the blocks on and above the diagonal are computed and stored (a block below
+// it is read as the transposed operand of its mirror image), 3 m^2 n + m^3 operations a step for m <= n instead of 4 m^2 n + 2 m^3.  Five steps of a 4096 x 4096
 // matrix are 1.37 TFLOP: tensor-bound from a few hundred rows on, launch-bound below.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <math.h>
 #include <math_constants.h>
 #include <stdint.h>
 
@@ -38,33 +38,37 @@ constexpr int NS_STAGING = 4096;
 
 template <int BN>
 struct NsCfg {
+  static constexpr int mmas = BN > 256 ? 2 : 1;          // products per step of 16 in k, sharing A
+  static constexpr int n_mma = BN / mmas;                // columns of one
+  static constexpr int b_rows = n_mma / 2;               // B columns per CTA and product
   static constexpr int a_bytes = NS_BM * 64 * 2;
-  static constexpr int b_bytes = BN / 2 * 64 * 2;
-  static constexpr int stage_bytes = a_bytes + b_bytes;
+  static constexpr int b_bytes = b_rows * 64 * 2;
+  static constexpr int stage_bytes = a_bytes + mmas * b_bytes;
   static constexpr int stages = 192 * 1024 / stage_bytes;
   static constexpr int smem = stages * stage_bytes + 1024 + 256 + NS_EPI_WARPS * NS_STAGING;
-  static constexpr int tmem_cols = 2 * BN;
+  static constexpr int bufs = BN > 256 ? 1 : 2;          // accumulators in tensor memory
+  static constexpr int tmem_cols = bufs * BN;
 };
 
-enum : int { OUT_PAIR = 0, OUT_BF16 = 1, OUT_F32 = 2, OUT_W_BF16 = 3, OUT_W_F32 = 4 };
+enum : int { OUT_BF16 = 1, OUT_F32 = 2, OUT_W_BF16 = 3, OUT_W_F32 = 4 };
+
+struct NsMaps { CUtensorMap x128[2], x64[2], gram128, gram64, poly128, poly64; };   // by box height
 
 struct NsParams {
-  int batch, m_tiles, n_tiles, tiles;          // tiles per matrix (symmetric product: on and above the diagonal)
-  int k_blocks;
-  int rows, cols;                              // of the result
-  // symmetric product: S = alpha acc + beta Cin (fp16, pitch ld, both triangles)
-  __half* S;
-  const __half* Cin;
-  int64_t ld;
-  float alpha, beta;
-  // update: x = a (hi + lo) + acc
-  const __half* hi;
-  __half *lo, *hi_out;
-  float a;
+  int batch, steps, tall;
+  int m, n, mm;                                // matrix, and its smaller side
+  int64_t ld, gld;                             // pitch of X and of the square matrices
+  int sym_tiles, sym_n, upd_tiles, upd_n;      // tiles per matrix and column tiles of the two kinds of product
+  int kb_long, kb_short;                       // k-blocks along the longer / the smaller side
+  __half *hi[2], *gram, *poly;                 // X in fp16 (two, written in turn), A, b A + c A A; row-major
+  float* x32;                                  // X in fp32, in blocks of 32 x 32 (see ns_block)
+  __half* gram_blk;                            // A once more, in blocks
+  float inv_s2, a, b, c;
   int out_mode;
-  void* out;                                   // result or weights, pitch cols
+  void* out;                                   // result or weights, pitch n
   float out_scale, decay;                      // result: x out_scale;  weights: w decay - x out_scale
   const int32_t* bad;                          // [batch]: the matrix held a NaN or an infinity: leave its weights alone
+  uint32_t* arrivals;                          // CTAs that have finished a product, over all products; zero at the start
   int32_t* d_status;
 };
 
@@ -74,39 +78,399 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
       : "memory");
 }
+// Orders this thread's plain accesses to global memory against TMA accesses (the asynchronous proxy).
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ float2 unpack_half(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+
+// What only epilogues read (X in fp32, the copy of A) is kept in blocks of 32 x 32 in the order in which tensor
+// memory hands out an accumulator: lane = row, 16 bytes of each lane side by side, so that a warp's access
+// is 512 consecutive bytes and nothing passes through shared memory.
+__device__ __forceinline__ int64_t ns_block(int b, int row, int col, int rows, int cols) {
+  const int64_t rb = (rows + 31) >> 5, cb = (cols + 31) >> 5;
+  return (((int64_t)b * rb + (row >> 5)) * cb + (col >> 5)) * 1024;
+}
+
+// Storage of an operand: with k contiguous, with the M / N index contiguous, or a symmetric matrix of which the
+// 256-blocks on and above the diagonal are stored.
+enum : int { OP_K = 0, OP_MN = 1, OP_SYM = 2 };
+// Whether the 64-deep k-block kb of the rows from `row` on is fetched with the M / N index contiguous.
+template <int OP>
+__device__ __forceinline__ bool ns_is_mn(int row, int kb) { return OP == OP_MN || (OP == OP_SYM && (kb >> 2) < (row >> 8)); }
 
 struct NsTile { int b, i, j; };
-// Tile `t` of the launch: row tile i, column tile j of matrix b.  SYM: row i has the column tiles
-// from the diagonal on (R = 256 / BN column tiles per row tile).
+// Tile `t` of a product: row tile i, column tile j of matrix b.  SYM: row tile i has the column tiles that
+// reach to or past its diagonal block (row i starts with column tile 256 i / BN).
 template <bool SYM, int BN>
-__device__ __forceinline__ NsTile ns_tile(int t, const NsParams& p) {
+__device__ __forceinline__ NsTile ns_tile(int t, int tiles, int n_tiles) {
   NsTile r;
-  r.b = t / p.tiles;
-  int q = t - r.b * p.tiles;
+  r.b = t / tiles;
+  int q = t - r.b * tiles;
   if (SYM) {
-    constexpr int R = 256 / BN;
-    int i = 0;
-    while (q >= p.n_tiles - R * i) { q -= p.n_tiles - R * i; ++i; }
+    int i = 0, first = 0;
+    while (q >= n_tiles - first) { q -= n_tiles - first; ++i; first = i * 256 / BN; }
     r.i = i;
-    r.j = R * i + q;
+    r.j = first + q;
   } else {
-    r.i = q / p.n_tiles;
-    r.j = q - r.i * p.n_tiles;
+    r.i = q / n_tiles;
+    r.j = q - r.i * n_tiles;
   }
   return r;
 }
 
-// One product of the iteration.  CTA pairs (cta_group::2) own 256 x BN tiles; two accumulators in tensor
-// memory, so that a tile's epilogue runs under the next tile's products.  A_MN / B_MN: the operand is stored
-// with the M / N index contiguous.
-template <bool SYM, bool A_MN, bool B_MN, int BN>
+// Waits until `goal` CTAs have arrived (bounded).  Called by one lane.
+__device__ __forceinline__ bool ns_grid_wait(const NsParams& p, uint32_t goal, volatile int* abort_flag) {
+  unsigned long long t0 = 0;
+  for (uint32_t spins = 0;; ++spins) {
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p.arrivals) : "memory");
+    if (v >= goal) return true;
+    __nanosleep(40);
+    if ((spins & 255u) == 255u) {
+      if (*abort_flag) return false;
+      const unsigned long long now = global_timer_ns();
+      if (t0 == 0) {
+        t0 = now;
+      } else if (now - t0 > kWaitLimitNs) {
+        *abort_flag = 1;
+        if (p.d_status) atomicOr(p.d_status, SPO_DEV_TIMEOUT);
+        return false;
+      }
+    }
+  }
+}
+
+// ---- roles.  Each walks this pair's tiles of one product; `it` and `n` run on over all products. ----
+
+template <bool SYM, int A, int B, int BN>
+__device__ __forceinline__ bool ns_produce(const CUtensorMap* a128, const CUtensorMap* a64, const CUtensorMap* b128,
+                                           const CUtensorMap* b64, int total, int tiles, int n_tiles, int k_blocks,
+                                           uint32_t base, uint32_t full0, uint32_t empty0, uint32_t rank, uint32_t& it,
+                                           volatile int* abort_flag, int32_t* d_status) {
+  using C = NsCfg<BN>;
+  for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2) {
+    const NsTile tl = ns_tile<SYM, BN>(t, tiles, n_tiles);
+    const int row = tl.i * 256 + (int)rank * NS_BM, col = tl.j * BN + (int)rank * C::b_rows;
+    for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+      const uint32_t s = it % C::stages, ph = (it / C::stages) & 1u;
+      if (!mbar_wait<20>(empty0 + 8 * s, ph ^ 1u, abort_flag, d_status)) return false;
+      const uint32_t sa = base + s * C::stage_bytes, sb = sa + C::a_bytes;
+      if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2 * C::stage_bytes);
+      const uint32_t fb = map_to_cta(full0 + 8 * s, 0);
+      if (!ns_is_mn<A>(row, kb)) {
+        tma_load_3d_pair(sa, a128, kb * 64, row, tl.b, fb);
+      } else {
+#pragma unroll
+        for (int x = 0; x < NS_BM / 64; ++x) tma_load_3d_pair(sa + x * 8192, a64, row + x * 64, kb * 64, tl.b, fb);
+      }
+#pragma unroll
+      for (int h = 0; h < C::mmas; ++h) {
+        const int c = col + h * C::n_mma;
+        if (!ns_is_mn<B>(c, kb)) {
+          tma_load_3d_pair(sb + h * C::b_bytes, C::b_rows == 64 ? b64 : b128, kb * 64, c, tl.b, fb);
+        } else {
+#pragma unroll
+          for (int x = 0; x < C::b_rows / 64; ++x)
+            tma_load_3d_pair(sb + h * C::b_bytes + x * 8192, b64, c + x * 64, kb * 64, tl.b, fb);
+        }
+      }
+    }
+  }
+  return true;
+}
+
+template <bool SYM, int A, int B, int BN>
+__device__ __forceinline__ bool ns_multiply(int total, int tiles, int n_tiles, int k_blocks, uint32_t base, uint32_t tmem_base,
+                                            uint32_t full0, uint32_t empty0, uint32_t tfull0, uint32_t tempty0, uint32_t& it,
+                                            uint32_t& n, volatile int* abort_flag, int32_t* d_status) {
+  using C = NsCfg<BN>;
+  // fp32 accumulate, fp16 A and B, M = 256 over the pair
+  constexpr uint32_t idesc0 = (1u << 4) | ((uint32_t)(C::n_mma >> 3) << 17) | (16u << 24);
+  for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2, ++n) {
+    const NsTile tl = ns_tile<SYM, BN>(t, tiles, n_tiles);
+    const uint32_t b = n % C::bufs;
+    if (!mbar_wait(tempty0 + 8 * b, ((n / C::bufs) & 1u) ^ 1u, abort_flag, d_status)) return false;
+    tc_fence_after();
+    for (int kb = 0; kb < k_blocks; ++kb, ++it) {
+      const uint32_t s = it % C::stages, ph = (it / C::stages) & 1u;
+      if (!mbar_wait(full0 + 8 * s, ph, abort_flag, d_status)) return false;
+      tc_fence_after();
+      const uint32_t sa = base + s * C::stage_bytes, sb = sa + C::a_bytes;
+      const bool a_mn = ns_is_mn<A>(tl.i * 256, kb);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t da = a_mn ? smem_desc(sa + j * 2048, 8192, 1024) : smem_desc(sa + j * 32, 16, 1024);
+#pragma unroll
+        for (int h = 0; h < C::mmas; ++h) {
+          const uint32_t sbh = sb + h * C::b_bytes;
+          const bool b_mn = ns_is_mn<B>(tl.j * BN + h * C::n_mma, kb);
+          const uint64_t db = b_mn ? smem_desc(sbh + j * 2048, 8192, 1024) : smem_desc(sbh + j * 32, 16, 1024);
+          umma_bf16(tmem_base + b * BN + h * C::n_mma, da, db, idesc0 | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16),
+                    (kb | j) != 0 ? 1u : 0u);
+        }
+      }
+      umma_commit(empty0 + 8 * s);
+    }
+    umma_commit(tfull0 + 8 * b);
+  }
+  return true;
+}
+
+// What the epilogue warps share: barriers, tensor memory, staging buffer.
+struct NsEpi {
+  uint32_t tmem_base, tfull0, tempty0, rank;
+  uint8_t* stage;
+  int quarter, half, lane;
+  volatile int* abort_flag;
+  int32_t* d_status;
+};
+template <int BN>
+__device__ __forceinline__ bool ns_tile_ready(const NsEpi& e, uint32_t n) {
+  using C = NsCfg<BN>;
+  int good = 1;
+  if (e.lane == 0) good = mbar_wait<20>(e.tfull0 + 8 * (n % C::bufs), (n / C::bufs) & 1u, e.abort_flag, e.d_status) ? 1 : 0;
+  good = __shfl_sync(0xffffffffu, good, 0);
+  tc_fence_after();
+  return good != 0;
+}
+template <int BN>
+__device__ __forceinline__ void ns_tile_done(const NsEpi& e, uint32_t n) {
+  tc_fence_before();
+  __syncwarp();
+  if (e.lane == 0) mbar_arrive_cluster(map_to_cta(e.tempty0 + 8 * (n % NsCfg<BN>::bufs), 0));
+}
+
+// A = acc / s^2, or b A + c acc (POLY); A is also kept in blocks, from which POLY reads it.  What a tile
+// reads is fetched before its products are waited for, then one step of 64 columns ahead.
+template <int BN, bool POLY>
+__device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsParams& p, int total, __half* S, float alpha, float beta,
+                                             uint32_t& n) {
+  const int lane = e.lane, rows = p.mm;
+  const int64_t ld = p.gld;
+  for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2, ++n) {
+    const NsTile tl = ns_tile<true, BN>(t, p.sym_tiles, p.sym_n);
+    const int row0 = tl.i * 256 + (int)e.rank * NS_BM + e.quarter * 32;
+    const int col_first = tl.j * BN + e.half * (BN / 2);
+    const int64_t mat = (int64_t)tl.b * rows * ld;
+    // columns left of the diagonal block (512-wide tiles of odd row blocks) are the mirror of another tile
+    const int col_begin = col_first < tl.i * 256 ? tl.i * 256 : col_first;
+    const int col_end = row0 >= rows ? col_begin : col_first + BN / 2 < rows ? col_first + BN / 2 : rows;
+    uint4 next[8];
+    auto fetch = [&](int c0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4* src = reinterpret_cast<const uint4*>(p.gram_blk + ns_block(tl.b, row0, c0 + 32 * h, rows, rows)) + lane;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) next[4 * h + q] = c0 + 32 * h < col_end ? __ldcg(src + 32 * q) : make_uint4(0u, 0u, 0u, 0u);
+      }
+    };
+    if (POLY && col_begin < col_end) fetch(col_begin);
+    if (!ns_tile_ready<BN>(e, n)) return false;
+    const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN + e.half * (BN / 2);
+#pragma unroll 1
+    for (int col0 = col_begin; col0 < col_end; col0 += 64) {
+      uint32_t v0[32], v1[32];
+      tmem_ld32_nowait(taddr + (col0 - col_first), v0);
+      tmem_ld32_nowait(taddr + (col0 - col_first) + 32, v1);
+      tmem_wait_ld(v0);
+      tmem_wait_ld(v1);
+      uint4 piece[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const uint32_t cw[4] = {next[q].x, next[q].y, next[q].z, next[q].w};
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int at = 8 * (q & 3) + 2 * k;
+          float x0 = alpha * __uint_as_float(q < 4 ? v0[at] : v1[at]), x1 = alpha * __uint_as_float(q < 4 ? v0[at + 1] : v1[at + 1]);
+          if (POLY) {
+            const float2 f = unpack_half(cw[k]);
+            x0 = fmaf(beta, f.x, x0);
+            x1 = fmaf(beta, f.y, x1);
+          }
+          o[k] = pack_half(x0, x1);
+        }
+        piece[q] = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+      if (POLY && col0 + 64 < col_end) fetch(col0 + 64);
+      if (!POLY) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (col0 + 32 * h >= col_end) continue;
+          uint4* dst = reinterpret_cast<uint4*>(p.gram_blk + ns_block(tl.b, row0, col0 + 32 * h, rows, rows)) + lane;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) dst[32 * q] = piece[4 * h + q];
+        }
+      }
+      stage_put(e.stage, lane, piece);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        int r, cc;
+        const uint4 val = stage_get(e.stage, lane, i, r, cc);
+        const int c = col0 + cc * 8;
+        // the pitch is a multiple of 8, so a piece that begins inside the row may be stored whole
+        if (row0 + r < rows && c < rows) *reinterpret_cast<uint4*>(S + mat + (int64_t)(row0 + r) * ld + c) = val;
+      }
+    }
+    ns_tile_done<BN>(e, n);
+  }
+  return true;
+}
+
+// Four columns of the last x: the result, or the weights with the step taken.  `left`: columns to the row's end.
+__device__ __forceinline__ void ns_emit(const NsParams& p, const uint4& acc, int64_t at, int left, int vec) {
+  float x[4] = {__uint_as_float(acc.x), __uint_as_float(acc.y), __uint_as_float(acc.z), __uint_as_float(acc.w)};
+  if (p.out_mode == OUT_W_BF16 || p.out_mode == OUT_W_F32) {
+    float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (p.out_mode == OUT_W_F32) {
+      const float* W = reinterpret_cast<const float*>(p.out) + at;
+      if (vec == 4) {
+        const float4 q = *reinterpret_cast<const float4*>(W);
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (k < left) w[k] = W[k];
+      }
+    } else {
+      const __nv_bfloat16* W = reinterpret_cast<const __nv_bfloat16*>(p.out) + at;
+      if (vec == 4) {
+        const uint2 q = *reinterpret_cast<const uint2*>(W);
+        w[0] = __uint_as_float(q.x << 16); w[1] = __uint_as_float(q.x & 0xFFFF0000u);
+        w[2] = __uint_as_float(q.y << 16); w[3] = __uint_as_float(q.y & 0xFFFF0000u);
+      } else if (vec == 2) {
+        const uint32_t q0 = *reinterpret_cast<const uint32_t*>(W);
+        w[0] = __uint_as_float(q0 << 16); w[1] = __uint_as_float(q0 & 0xFFFF0000u);
+        if (left > 2) {
+          const uint32_t q1 = *reinterpret_cast<const uint32_t*>(W + 2);
+          w[2] = __uint_as_float(q1 << 16); w[3] = __uint_as_float(q1 & 0xFFFF0000u);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) if (k < left) w[k] = __bfloat162float(W[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = fmaf(w[k], p.decay, -p.out_scale * x[k]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] *= p.out_scale;
+  }
+  if (p.out_mode == OUT_F32 || p.out_mode == OUT_W_F32) {
+    float* W = reinterpret_cast<float*>(p.out) + at;
+    if (vec == 4) {
+      *reinterpret_cast<float4*>(W) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (k < left) W[k] = x[k];
+    }
+  } else {
+    __nv_bfloat16* W = reinterpret_cast<__nv_bfloat16*>(p.out) + at;
+    if (vec == 4) {
+      *reinterpret_cast<uint2*>(W) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+    } else if (vec == 2) {
+      *reinterpret_cast<uint32_t*>(W) = pack_bf16(x[0], x[1]);
+      if (left > 2) *reinterpret_cast<uint32_t*>(W + 2) = pack_bf16(x[2], x[3]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (k < left) W[k] = __float2bfloat16_rn(x[k]);
+    }
+  }
+}
+
+// x = a X + acc, stored as the next X (fp32 blocks and fp16 rows), as the result, or applied to the weights.
+template <int BN, bool LAST>
+__device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsParams& p, int total, __half* hi_out, uint32_t& n) {
+  const int lane = e.lane, rows = p.m, cols = p.n;
+  const int vec = (cols & 3) == 0 ? 4 : (cols & 1) == 0 ? 2 : 1;
+  for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2, ++n) {
+    const NsTile tl = ns_tile<false, BN>(t, p.upd_tiles, p.upd_n);
+    const int row0 = tl.i * 256 + (int)e.rank * NS_BM + e.quarter * 32;
+    const int col_first = tl.j * BN + e.half * (BN / 2);
+    const int64_t mat = (int64_t)tl.b * rows * p.ld, umat = (int64_t)tl.b * rows * cols;
+    const bool skip = LAST && (p.out_mode == OUT_W_BF16 || p.out_mode == OUT_W_F32) && p.bad[tl.b] != 0;
+    const int col_end = row0 >= rows ? col_first : col_first + BN / 2 < cols ? col_first + BN / 2 : cols;
+    float4* blk = reinterpret_cast<float4*>(p.x32 + ns_block(tl.b, row0, col_first, rows, cols)) + lane;   // + 256 per 32 columns
+    float4 next[8];
+    auto fetch = [&](int step) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q) next[q] = __ldcg(blk + step * 256 + 32 * q);
+    };
+    if (col_first < col_end) fetch(0);
+    if (!ns_tile_ready<BN>(e, n)) return false;
+    const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN + e.half * (BN / 2);
+#pragma unroll 1
+    for (int step = 0; col_first + 32 * step < col_end; step += 2) {
+      uint4 piece[8];                                     // !LAST: 64 columns of fp16, one round through the staging buffer
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int col0 = col_first + 32 * (step + h);
+        if (col0 >= col_end) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) piece[4 * h + q] = make_uint4(0u, 0u, 0u, 0u);
+          continue;
+        }
+        float4 x32[8];
+        uint32_t v[32];
+        tmem_ld32(taddr + 32 * (step + h), v);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          x32[q].x = fmaf(p.a, next[q].x, __uint_as_float(v[4 * q]));
+          x32[q].y = fmaf(p.a, next[q].y, __uint_as_float(v[4 * q + 1]));
+          x32[q].z = fmaf(p.a, next[q].z, __uint_as_float(v[4 * q + 2]));
+          x32[q].w = fmaf(p.a, next[q].w, __uint_as_float(v[4 * q + 3]));
+        }
+        if (col0 + 32 < col_end) fetch(step + h + 1);
+        if constexpr (!LAST) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) blk[(step + h) * 256 + 32 * q] = x32[q];
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            piece[4 * h + q] = make_uint4(pack_half(x32[2 * q].x, x32[2 * q].y), pack_half(x32[2 * q].z, x32[2 * q].w),
+                                          pack_half(x32[2 * q + 1].x, x32[2 * q + 1].y), pack_half(x32[2 * q + 1].z, x32[2 * q + 1].w));
+        } else {
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            piece[q] = make_uint4(__float_as_uint(x32[q].x), __float_as_uint(x32[q].y), __float_as_uint(x32[q].z), __float_as_uint(x32[q].w));
+          stage_put(e.stage, lane, piece);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            int rr, cc;
+            const uint4 acc = stage_get(e.stage, lane, i, rr, cc);
+            const int r = row0 + rr, c = col0 + cc * 4;
+            if (r < rows && c < cols && !skip) ns_emit(p, acc, umat + (int64_t)r * cols + c, cols - c, vec);
+          }
+        }
+      }
+      if constexpr (!LAST) {
+        stage_put(e.stage, lane, piece);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          int r, cc;
+          const uint4 val = stage_get(e.stage, lane, i, r, cc);
+          const int c = col_first + 32 * step + cc * 8;
+          // the pitch is a multiple of 8: whole pieces; columns past the end are never read as operands
+          if (row0 + r < rows && c < cols) *reinterpret_cast<uint4*>(hi_out + mat + (int64_t)(row0 + r) * p.ld + c) = val;
+        }
+      }
+    }
+    ns_tile_done<BN>(e, n);
+  }
+  return true;
+}
+
+// All products of the iteration in one cooperative launch: 3 steps products with a grid-wide barrier after each
+// (a counter in global memory; every wait is bounded).  A launch per product cost 10 to 17 us on a single
+// tile, most of it launching, filling the pipeline and draining one epilogue.
+// CTA pairs (cta_group::2) own 256 x BN tiles.  BN = 512: two products per k-step share A, which takes the
+// L2 -> SM traffic from 64 to 48 bytes per SM and clock (64 is all there is), but fills tensor memory, so a tile's
+// epilogue is not hidden; BN = 256 and 128: two accumulators, the epilogue runs under the next tile.
+template <bool TALL, int BN>
 __global__ void __launch_bounds__(NS_THREADS, 1)
-ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const NsParams p) {
+ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsParams p) {
   using C = NsCfg<BN>;
   constexpr int S = C::stages;
   extern __shared__ uint8_t smem_raw[];
@@ -117,15 +481,17 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   const uint32_t full0 = bars, empty0 = bars + 8 * S, tfull0 = bars + 16 * S, tempty0 = tfull0 + 16;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + S * C::stage_bytes + 16 * S + 32);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* warps_done = tmem_slot + 2;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();
-  const int group = blockIdx.x / 2, n_groups = gridDim.x / 2;
-  const int total = p.batch * p.tiles;
+  const int sym_total = p.batch * p.sym_tiles, upd_total = p.batch * p.upd_tiles;
+  const int products = 3 * p.steps;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(tfull0 + 8 * b, 1); mbar_init(tempty0 + 8 * b, 2 * NS_EPI_WARPS); }
     *abort_flag = 0;
+    *warps_done = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 0) {
@@ -141,221 +507,84 @@ ns_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
   if (warp == 0) {
     if (lane == 0) {
       uint32_t it = 0;
-      bool ok = true;
-      for (int t = group; t < total && ok; t += n_groups) {
-        const NsTile tl = ns_tile<SYM, BN>(t, p);
-        const int row = tl.i * 256 + (int)rank * NS_BM, col = tl.j * BN + (int)rank * (BN / 2);
-        for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-          const uint32_t s = it % S, ph = (it / S) & 1u;
-          if (!mbar_wait<20>(empty0 + 8 * s, ph ^ 1u, abort_flag, p.d_status)) { ok = false; break; }
-          const uint32_t sa = base + s * C::stage_bytes, sb = sa + C::a_bytes;
-          if (rank == 0) mbar_expect_tx(full0 + 8 * s, 2 * C::stage_bytes);
-          const uint32_t fb = map_to_cta(full0 + 8 * s, 0);
-          if (!A_MN) {
-            tma_load_3d_pair(sa, &tmA, kb * 64, row, tl.b, fb);
-          } else {
-#pragma unroll
-            for (int x = 0; x < NS_BM / 64; ++x) tma_load_3d_pair(sa + x * 8192, &tmA, row + x * 64, kb * 64, tl.b, fb);
-          }
-          if (!B_MN) {
-            tma_load_3d_pair(sb, &tmB, kb * 64, col, tl.b, fb);
-          } else {
-#pragma unroll
-            for (int x = 0; x < BN / 128; ++x) tma_load_3d_pair(sb + x * 8192, &tmB, col + x * 64, kb * 64, tl.b, fb);
-          }
-        }
+      for (int q = 0; q < products; ++q) {
+        if (q > 0 && !ns_grid_wait(p, (uint32_t)q * gridDim.x, abort_flag)) break;
+        fence_proxy_async();                        // the operands were written by plain stores
+        const int k = q / 3, kind = q - 3 * k, x = k & 1;
+        bool ok;
+        if (kind == 0)
+          ok = ns_produce<true, TALL ? OP_MN : OP_K, TALL ? OP_MN : OP_K, BN>(
+              &maps.x128[x], &maps.x64[x], &maps.x128[x], &maps.x64[x], sym_total, p.sym_tiles, p.sym_n, p.kb_long, base, full0,
+              empty0, rank, it, abort_flag, p.d_status);
+        else if (kind == 1)
+          ok = ns_produce<true, OP_SYM, OP_SYM, BN>(&maps.gram128, &maps.gram64, &maps.gram128, &maps.gram64, sym_total,
+                                                    p.sym_tiles, p.sym_n, p.kb_short, base, full0, empty0, rank, it, abort_flag,
+                                                    p.d_status);
+        else if (TALL)
+          ok = ns_produce<false, OP_K, OP_SYM, BN>(&maps.x128[x], &maps.x64[x], &maps.poly128, &maps.poly64, upd_total,
+                                                   p.upd_tiles, p.upd_n, p.kb_short, base, full0, empty0, rank, it, abort_flag,
+                                                   p.d_status);
+        else
+          ok = ns_produce<false, OP_SYM, OP_MN, BN>(&maps.poly128, &maps.poly64, &maps.x128[x], &maps.x64[x], upd_total,
+                                                    p.upd_tiles, p.upd_n, p.kb_short, base, full0, empty0, rank, it, abort_flag,
+                                                    p.d_status);
+        if (!ok) break;
       }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      // fp32 accumulate, fp16 A and B, M = 256 over the pair, N = BN
-      constexpr uint32_t idesc = (1u << 4) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
-                                 ((uint32_t)(BN >> 3) << 17) | (16u << 24);
       uint32_t it = 0, n = 0;
-      bool ok = true;
-      for (int t = group; t < total && ok; t += n_groups, ++n) {
-        const uint32_t b = n & 1u;
-        if (!mbar_wait(tempty0 + 8 * b, ((n >> 1) & 1u) ^ 1u, abort_flag, p.d_status)) { ok = false; break; }
-        tc_fence_after();
-        for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-          const uint32_t s = it % S, ph = (it / S) & 1u;
-          if (!mbar_wait(full0 + 8 * s, ph, abort_flag, p.d_status)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t sa = base + s * C::stage_bytes, sb = sa + C::a_bytes;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint64_t da = A_MN ? smem_desc(sa + j * 2048, 8192, 1024) : smem_desc(sa + j * 32, 16, 1024);
-            const uint64_t db = B_MN ? smem_desc(sb + j * 2048, 8192, 1024) : smem_desc(sb + j * 32, 16, 1024);
-            umma_bf16(tmem_base + b * BN, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
-          }
-          umma_commit(empty0 + 8 * s);
-        }
-        if (ok) umma_commit(tfull0 + 8 * b);
+      for (int q = 0; q < products; ++q) {
+        const int kind = q % 3;
+        bool ok;
+        if (kind == 0)
+          ok = ns_multiply<true, TALL ? OP_MN : OP_K, TALL ? OP_MN : OP_K, BN>(sym_total, p.sym_tiles, p.sym_n, p.kb_long, base,
+                                                                               tmem_base, full0, empty0, tfull0, tempty0, it, n,
+                                                                               abort_flag, p.d_status);
+        else if (kind == 1)
+          ok = ns_multiply<true, OP_SYM, OP_SYM, BN>(sym_total, p.sym_tiles, p.sym_n, p.kb_short, base, tmem_base, full0, empty0,
+                                                     tfull0, tempty0, it, n, abort_flag, p.d_status);
+        else
+          ok = ns_multiply<false, TALL ? OP_K : OP_SYM, TALL ? OP_SYM : OP_MN, BN>(upd_total, p.upd_tiles, p.upd_n, p.kb_short, base,
+                                                                                   tmem_base, full0, empty0, tfull0, tempty0, it,
+                                                                                   n, abort_flag, p.d_status);
+        if (!ok) break;
       }
     }
   } else {
-    const int quarter = warp & 3, half = (warp - 2) >> 2;
-    uint8_t* stage = gen + S * C::stage_bytes + 256 + (warp - 2) * NS_STAGING;
+    NsEpi e;
+    e.tmem_base = tmem_base; e.tfull0 = tfull0; e.tempty0 = tempty0; e.rank = rank;
+    e.stage = gen + S * C::stage_bytes + 256 + (warp - 2) * NS_STAGING;
+    e.quarter = warp & 3; e.half = (warp - 2) >> 2; e.lane = lane;
+    e.abort_flag = abort_flag; e.d_status = p.d_status;
     uint32_t n = 0;
-    for (int t = group; t < total; t += n_groups, ++n) {
-      const NsTile tl = ns_tile<SYM, BN>(t, p);
-      const uint32_t b = n & 1u;
-      int good = 1;
-      if (lane == 0) good = mbar_wait<20>(tfull0 + 8 * b, (n >> 1) & 1u, abort_flag, p.d_status) ? 1 : 0;
-      good = __shfl_sync(0xffffffffu, good, 0);
-      if (!good) break;
-      tc_fence_after();
-      const int row0 = tl.i * 256 + (int)rank * NS_BM + quarter * 32;      // result row of the warp's lane 0
-      const int row = row0 + lane;
-      const int col_first = tl.j * BN + half * (BN / 2);
-      const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * BN + half * (BN / 2);
-      if (SYM) {
-        const int64_t mat = (int64_t)tl.b * p.rows * p.ld;
-        const bool mirror = tl.j >= (256 / BN) * (tl.i + 1);                // the diagonal block is computed whole
-#pragma unroll 1
-        for (int r2 = 0; r2 < BN / 2; r2 += 64) {
-          const int col0 = col_first + r2;
-          if (col0 >= p.cols) break;
-          uint4 piece[8];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int c0 = col0 + h * 32;
-            float cin[32];
-            // Cin is symmetric: its element (row, c) is read from (c, row), 32 consecutive rows per access
-            if (p.Cin) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                cin[j] = row < p.rows && c0 + j < p.cols ? __half2float(p.Cin[mat + (int64_t)(c0 + j) * p.ld + row]) : 0.0f;
-            }
-            uint32_t v[32];
-            tmem_ld32(taddr + r2 + h * 32, v);
-            uint32_t o[16];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-              float x = p.alpha * __uint_as_float(v[j]);
-              if (p.Cin) x = fmaf(p.beta, cin[j], x);
-              v[j] = __float_as_uint(x);
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) o[j] = pack_half(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-            if (mirror && row < p.rows) {
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (c0 + j < p.cols)
-                  reinterpret_cast<uint16_t*>(p.S)[mat + (int64_t)(c0 + j) * p.ld + row] =
-                      (uint16_t)((j & 1) ? o[j >> 1] >> 16 : o[j >> 1] & 0xFFFFu);
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) piece[4 * h + q] = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-          }
-          stage_put(stage, lane, piece);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            int r, cc;
-            const uint4 val = stage_get(stage, lane, i, r, cc);
-            const int c = col0 + cc * 8;
-            // the pitch is a multiple of 8, so a piece that begins inside the row may be stored whole
-            if (row0 + r < p.rows && c < p.cols) *reinterpret_cast<uint4*>(p.S + mat + (int64_t)(row0 + r) * p.ld + c) = val;
-          }
-        }
-      } else {
-        const int64_t mat = (int64_t)tl.b * p.rows * p.ld, umat = (int64_t)tl.b * p.rows * p.cols;
-        const bool vec = (p.cols & 3) == 0;
-        const bool skip = p.bad != nullptr && p.bad[tl.b] != 0;
-#pragma unroll 1
-        for (int ch = 0; ch < BN / 2; ch += 32) {
-          const int col0 = col_first + ch;
-          if (col0 >= p.cols) break;
-          uint2 xh[8], xl[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = row0 + 4 * i + (lane >> 3), c = col0 + (lane & 7) * 4;
-            xh[i] = xl[i] = make_uint2(0u, 0u);
-            if (r < p.rows && c < p.cols) {
-              xh[i] = *reinterpret_cast<const uint2*>(p.hi + mat + (int64_t)r * p.ld + c);
-              xl[i] = *reinterpret_cast<const uint2*>(p.lo + mat + (int64_t)r * p.ld + c);
-            }
-          }
-          uint32_t v[32];
-          tmem_ld32(taddr + ch, v);
-          uint4 piece[8];
-#pragma unroll
-          for (int q = 0; q < 8; ++q) piece[q] = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-          stage_put(stage, lane, piece);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            int rr, cc;
-            const uint4 acc = stage_get(stage, lane, i, rr, cc);
-            const int r = row0 + rr, c = col0 + cc * 4;
-            if (r >= p.rows || c >= p.cols) continue;
-            float x[4] = {__uint_as_float(acc.x), __uint_as_float(acc.y), __uint_as_float(acc.z), __uint_as_float(acc.w)};
-            const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&xh[i].x)),
-                         h1 = __half22float2(*reinterpret_cast<const __half2*>(&xh[i].y)),
-                         l0 = __half22float2(*reinterpret_cast<const __half2*>(&xl[i].x)),
-                         l1 = __half22float2(*reinterpret_cast<const __half2*>(&xl[i].y));
-            x[0] = fmaf(p.a, h0.x + l0.x, x[0]);
-            x[1] = fmaf(p.a, h0.y + l0.y, x[1]);
-            x[2] = fmaf(p.a, h1.x + l1.x, x[2]);
-            x[3] = fmaf(p.a, h1.y + l1.y, x[3]);
-            if (p.out_mode == OUT_PAIR) {
-              // pitch a multiple of 8: whole pieces; columns past the end are never read as operands
-              const uint2 hh = make_uint2(pack_half(x[0], x[1]), pack_half(x[2], x[3]));
-              const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&hh.x)),
-                           g1 = __half22float2(*reinterpret_cast<const __half2*>(&hh.y));
-              *reinterpret_cast<uint2*>(p.hi_out + mat + (int64_t)r * p.ld + c) = hh;
-              *reinterpret_cast<uint2*>(p.lo + mat + (int64_t)r * p.ld + c) =
-                  make_uint2(pack_half(x[0] - g0.x, x[1] - g0.y), pack_half(x[2] - g1.x, x[3] - g1.y));
-              continue;
-            }
-            const int64_t at = umat + (int64_t)r * p.cols + c;
-            if (p.out_mode == OUT_W_BF16 || p.out_mode == OUT_W_F32) {
-              if (skip) continue;
-              float w[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-              if (p.out_mode == OUT_W_F32) {
-                float* W = reinterpret_cast<float*>(p.out) + at;
-                if (vec) {
-                  const float4 q = *reinterpret_cast<const float4*>(W);
-                  w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-                } else {
-                  for (int k = 0; k < 4 && c + k < p.cols; ++k) w[k] = W[k];
-                }
-              } else {
-                const __nv_bfloat16* W = reinterpret_cast<const __nv_bfloat16*>(p.out) + at;
-                if (vec) {
-                  const uint2 q = *reinterpret_cast<const uint2*>(W);
-                  w[0] = __uint_as_float(q.x << 16); w[1] = __uint_as_float(q.x & 0xFFFF0000u);
-                  w[2] = __uint_as_float(q.y << 16); w[3] = __uint_as_float(q.y & 0xFFFF0000u);
-                } else {
-                  for (int k = 0; k < 4 && c + k < p.cols; ++k) w[k] = __bfloat162float(W[k]);
-                }
-              }
-#pragma unroll
-              for (int k = 0; k < 4; ++k) x[k] = fmaf(w[k], p.decay, -p.out_scale * x[k]);
-            } else {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) x[k] *= p.out_scale;
-            }
-            if (p.out_mode == OUT_F32 || p.out_mode == OUT_W_F32) {
-              float* W = reinterpret_cast<float*>(p.out) + at;
-              if (vec) {
-                *reinterpret_cast<float4*>(W) = make_float4(x[0], x[1], x[2], x[3]);
-              } else {
-                for (int k = 0; k < 4 && c + k < p.cols; ++k) W[k] = x[k];
-              }
-            } else {
-              __nv_bfloat16* W = reinterpret_cast<__nv_bfloat16*>(p.out) + at;
-              if (vec) {
-                *reinterpret_cast<uint2*>(W) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-              } else {
-                for (int k = 0; k < 4 && c + k < p.cols; ++k) W[k] = __float2bfloat16_rn(x[k]);
-              }
-            }
-          }
+    for (int q = 0; q < products; ++q) {
+      if (q > 0) {
+        int good = 1;
+        if (lane == 0) good = ns_grid_wait(p, (uint32_t)q * gridDim.x, abort_flag) ? 1 : 0;
+        if (!__shfl_sync(0xffffffffu, good, 0)) break;
+      }
+      const int k = q / 3, kind = q - 3 * k;
+      bool ok;
+      if (kind == 0)
+        ok = ns_store_sym<BN, false>(e, p, sym_total, p.gram, p.inv_s2, 0.0f, n);
+      else if (kind == 1)
+        ok = ns_store_sym<BN, true>(e, p, sym_total, p.poly, p.c, p.b, n);
+      else if (k < p.steps - 1)
+        ok = ns_store_update<BN, false>(e, p, upd_total, p.hi[(k + 1) & 1], n);
+      else
+        ok = ns_store_update<BN, true>(e, p, upd_total, nullptr, n);
+      if (!ok) break;
+      if (q + 1 < products) {                       // this CTA's part of the product is in memory: count it
+        // (no barrier among the warps: one that gave up must not leave the others waiting)
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          __threadfence();
+          if (atomicAdd(warps_done, 1u) % NS_EPI_WARPS == NS_EPI_WARPS - 1)
+            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.arrivals) : "memory");
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty0 + 8 * b, 0));
     }
   }
 
@@ -379,12 +608,14 @@ struct NsInput {
   float* momentum;                         // NULL: U = G
   float mu;
   int nesterov;
-  int64_t m, n, ld;                        // ld: pitch of hi / lo
+  int64_t m, n, ld;                        // ld: pitch of hi
   int blocks;                              // blocks (and norm partials) per matrix
   double* partials;                        // [batch][blocks]
   float eps, scale;
-  __half *hi, *lo;
+  __half* hi;
+  float* x32;
   int32_t *bad, *d_status;
+  uint32_t* arrivals;                      // the iteration's barrier counter, zeroed here
 };
 
 __device__ __forceinline__ float ns_load(const NsInput& p, int64_t at) {
@@ -411,6 +642,7 @@ __global__ void __launch_bounds__(256)
 ns_norm_kernel(const NsInput p) {
   const int64_t count = p.m * p.n, mat = (int64_t)blockIdx.y * count;
   double acc = 0.0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.arrivals = 0;
   if ((count & 3) == 0) {
     for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (int64_t)p.blocks * 1024) {
       float g[4], u[4];
@@ -447,7 +679,7 @@ ns_norm_kernel(const NsInput p) {
   }
 }
 
-// Momentum, and U / (|U|_F + eps) times the scale as the pair hi + lo.
+// Momentum, and U / (|U|_F + eps) times the scale, in fp32 blocks and fp16 rows.
 __global__ void __launch_bounds__(256)
 ns_split_kernel(const NsInput p) {
   const int64_t count = p.m * p.n, mat = (int64_t)blockIdx.y * count, xmat = (int64_t)blockIdx.y * p.m * p.ld;
@@ -467,45 +699,57 @@ ns_split_kernel(const NsInput p) {
     if (bad && p.d_status) atomicOr(p.d_status, SPO_DEV_NONFINITE);
   }
   const float f = bad ? 0.0f : (float)((double)p.scale / (sqrt(tot) + (double)p.eps));
-  if ((p.n & 3) == 0) {
-    const int64_t q_row = p.n >> 2, quads = count >> 2;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (int64_t)gridDim.x * 256) {
-      const int64_t r = i / q_row, c = (i - r * q_row) * 4;
-      float g[4], u[4];
-      ns_load4(p, mat + i * 4, g);
-      if (p.momentum) {
-        float4* mp = reinterpret_cast<float4*>(p.momentum + mat + i * 4);
-        const float4 q = *mp;
-        const float mo[4] = {q.x, q.y, q.z, q.w};
-        float mn[4];
+  const int64_t cbs = (p.n + 31) >> 5, tasks = ((p.m + 31) >> 5) * cbs;
+  const int lane = threadIdx.x & 31;
+  const bool quads = (p.n & 3) == 0;
+  for (int64_t task = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); task < tasks; task += (int64_t)gridDim.x * 8) {
+    const int64_t rb = task / cbs, c0 = (task - rb * cbs) * 32;
+    float* blk = p.x32 + ((int64_t)blockIdx.y * tasks + task) * 1024;
+    if (quads) {
+      // a warp takes a block of 32 x 32: eight lanes a row, four rows an access
+      const int64_t c = c0 + (lane & 7) * 4;
+#pragma unroll 4
+      for (int i = 0; i < 8; ++i) {
+        const int rr = 4 * i + (lane >> 3);
+        const int64_t r = rb * 32 + rr, at = mat + r * p.n + c;
+        float u[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (r < p.m && c < p.n && !bad) {
+          ns_load4(p, at, u);
+          if (p.momentum) {
+            float4* mp = reinterpret_cast<float4*>(p.momentum + at);
+            const float4 q = *mp;
+            const float mo[4] = {q.x, q.y, q.z, q.w};
+            float mn[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) u[k] = ns_momentum(p, g[k], mo[k], &mn[k]);
-        if (!bad) *mp = make_float4(mn[0], mn[1], mn[2], mn[3]);
-      } else {
+            for (int k = 0; k < 4; ++k) u[k] = ns_momentum(p, u[k], mo[k], &mn[k]);
+            *mp = make_float4(mn[0], mn[1], mn[2], mn[3]);
+          }
 #pragma unroll
-        for (int k = 0; k < 4; ++k) u[k] = g[k];
+          for (int k = 0; k < 4; ++k) u[k] *= f;
+        }
+        *reinterpret_cast<float4*>(blk + (lane & 7) * 128 + rr * 4) = make_float4(u[0], u[1], u[2], u[3]);
+        if (r < p.m && c < p.n)                           // the pitch is a multiple of 8: whole pieces
+          *reinterpret_cast<uint2*>(p.hi + xmat + r * p.ld + c) = make_uint2(pack_half(u[0], u[1]), pack_half(u[2], u[3]));
       }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) u[k] = bad ? 0.0f : u[k] * f;
-      const uint2 hh = make_uint2(pack_half(u[0], u[1]), pack_half(u[2], u[3]));
-      const float2 g0 = __half22float2(*reinterpret_cast<const __half2*>(&hh.x)),
-                   g1 = __half22float2(*reinterpret_cast<const __half2*>(&hh.y));
-      *reinterpret_cast<uint2*>(p.hi + xmat + r * p.ld + c) = hh;
-      *reinterpret_cast<uint2*>(p.lo + xmat + r * p.ld + c) =
-          make_uint2(pack_half(u[0] - g0.x, u[1] - g0.y), pack_half(u[2] - g1.x, u[3] - g1.y));
-    }
-  } else {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
-      const int64_t r = i / p.n, c = i - r * p.n;
-      float u = ns_load(p, mat + i), mn;
-      if (p.momentum) {
-        u = ns_momentum(p, u, p.momentum[mat + i], &mn);
-        if (!bad) p.momentum[mat + i] = mn;
+    } else {
+      // rows that do not begin on 16 bytes: a lane a column, a row an access
+      const int64_t c = c0 + lane;
+#pragma unroll 8
+      for (int rr = 0; rr < 32; ++rr) {
+        const int64_t r = rb * 32 + rr, at = mat + r * p.n + c;
+        float u = 0.0f;
+        if (r < p.m && c < p.n && !bad) {
+          u = ns_load(p, at);
+          if (p.momentum) {
+            float mn;
+            u = ns_momentum(p, u, p.momentum[at], &mn);
+            p.momentum[at] = mn;
+          }
+          u *= f;
+        }
+        blk[(lane >> 2) * 128 + rr * 4 + (lane & 3)] = u;
+        if (r < p.m && c < p.n) p.hi[xmat + r * p.ld + c] = __float2half_rn(u);
       }
-      u = bad ? 0.0f : u * f;
-      const __half hh = __float2half_rn(u);
-      p.hi[xmat + r * p.ld + c] = hh;
-      p.lo[xmat + r * p.ld + c] = __float2half_rn(u - __half2float(hh));
     }
   }
 }
@@ -513,7 +757,7 @@ ns_split_kernel(const NsInput p) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct NsWs { size_t hi[2], lo, gram, poly, partials, bad, total; int64_t ld, mm, gld; int blocks; };
+struct NsWs { size_t hi[2], x32, gram, gram_blk, poly, partials, bad, arrivals, total; int64_t ld, mm, gld; int blocks; };
 
 constexpr int kNormBlocks = 592;
 
@@ -527,11 +771,13 @@ NsWs ns_layout(int64_t m, int64_t n, int64_t batch) {
   const size_t x = (size_t)batch * m * L.ld * 2, g = (size_t)batch * L.mm * L.gld * 2;
   size_t off = 0;
   for (int i = 0; i < 2; ++i) { L.hi[i] = off; off = align_up(off + x, 256); }
-  L.lo = off;       off = align_up(off + x, 256);
+  L.x32 = off;      off = align_up(off + (size_t)batch * ceil_div(m, 32) * ceil_div(n, 32) * 4096, 256);
   L.gram = off;     off = align_up(off + g, 256);
+  L.gram_blk = off; off = align_up(off + (size_t)batch * ceil_div(L.mm, 32) * ceil_div(L.mm, 32) * 2048, 256);
   L.poly = off;     off = align_up(off + g, 256);
   L.partials = off; off = align_up(off + (size_t)batch * L.blocks * 8, 256);
   L.bad = off;      off = align_up(off + (size_t)batch * 4, 256);
+  L.arrivals = off; off = align_up(off + 4, 256);
   L.total = off;
   return L;
 }
@@ -549,52 +795,96 @@ bool make_map3(CUtensorMap* m, const void* ptr, int64_t cols, int64_t rows, int6
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-struct NsOperand { const void* ptr; int64_t cols, rows, ld; };   // as stored
-
-template <bool SYM, bool A_MN, bool B_MN, int BN>
-cudaError_t launch_ns_t(const NsOperand& A, const NsOperand& B, NsParams p, cudaStream_t st) {
-  using C = NsCfg<BN>;
-  auto kern = ns_gemm_kernel<SYM, A_MN, B_MN, BN>;
-  static std::atomic<int> ready[64];
+// CTA pairs of an instantiation that can be resident together (0 = not yet asked); one slot per device.
+template <bool TALL, int BN>
+cudaError_t ns_resident(int* out) {
+  static std::atomic<int> cached[64];
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-  if (!ready[dev].load(std::memory_order_acquire)) {
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::smem);
+  int n = cached[dev].load(std::memory_order_acquire);
+  if (n == 0) {
+    auto kern = ns_iterate_kernel<TALL, BN>;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NsCfg<BN>::smem);
     if (e != cudaSuccess) return e;
-    ready[dev].store(1, std::memory_order_release);
+    cudaLaunchConfig_t q = {};
+    q.gridDim = dim3((unsigned)(sm_count() / 2 * 2), 1, 1);
+    q.blockDim = dim3(NS_THREADS, 1, 1);
+    q.dynamicSmemBytes = NsCfg<BN>::smem;
+    cudaLaunchAttribute qa[1];
+    qa[0].id = cudaLaunchAttributeClusterDimension;
+    qa[0].val.clusterDim.x = 2;
+    qa[0].val.clusterDim.y = 1;
+    qa[0].val.clusterDim.z = 1;
+    q.attrs = qa;
+    q.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&n, kern, &q);
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaErrorLaunchOutOfResources;
+    if (n > sm_count() / 2) n = sm_count() / 2;
+    cached[dev].store(n, std::memory_order_release);
   }
-  CUtensorMap ma, mb;
-  if (!make_map3(&ma, A.ptr, A.cols, A.rows, p.batch, A.ld, A_MN ? 64 : NS_BM) ||
-      !make_map3(&mb, B.ptr, B.cols, B.rows, p.batch, B.ld, B_MN ? 64 : BN / 2))
-    return cudaErrorInvalidValue;
-  const int64_t mt = ceil_div(p.rows, 256), nt = ceil_div(p.cols, BN);
-  int64_t tiles = mt * nt;
-  if (SYM) tiles -= (256 / BN) * (mt * (mt - 1) / 2);
-  if (tiles * p.batch > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  p.m_tiles = (int)mt;
-  p.n_tiles = (int)nt;
-  p.tiles = (int)tiles;
-  const int64_t pairs = sm_count() / 2, total = tiles * p.batch;
+  *out = n;
+  return cudaSuccess;
+}
+
+int64_t sym_tile_count(int64_t mm, int bn) {
+  const int64_t mt = ceil_div(mm, 256), nt = ceil_div(mm, bn);
+  int64_t tiles = 0;
+  for (int64_t i = 0; i < mt; ++i) tiles += nt - i * 256 / bn;
+  return tiles;
+}
+
+template <bool TALL, int BN>
+cudaError_t launch_iterate_t(const NsMaps& maps, NsParams p, cudaStream_t st) {
+  int pairs = 0;
+  cudaError_t e = ns_resident<TALL, BN>(&pairs);
+  if (e != cudaSuccess) return e;
+  const int64_t sym = sym_tile_count(p.mm, BN), un = ceil_div(p.n, BN), upd = ceil_div(p.m, 256) * un;
+  const int64_t most = (sym > upd ? sym : upd) * p.batch;
+  if (most > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  p.sym_tiles = (int)sym; p.sym_n = (int)ceil_div(p.mm, BN);
+  p.upd_tiles = (int)upd; p.upd_n = (int)un;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(2 * (total < pairs ? total : pairs)), 1, 1);
+  cfg.gridDim = dim3((unsigned)(2 * (most < pairs ? most : pairs)), 1, 1);
   cfg.blockDim = dim3(NS_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = C::smem;
+  cfg.dynamicSmemBytes = NsCfg<BN>::smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = 2;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeCooperative;               // all CTAs resident, or the launch fails
+  attr[1].val.cooperative = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, ma, mb, p);
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, ns_iterate_kernel<TALL, BN>, maps, p);
 }
 
-template <bool SYM, bool A_MN, bool B_MN>
-cudaError_t launch_ns(const NsOperand& A, const NsOperand& B, const NsParams& p, cudaStream_t st) {
-  return launch_ns_t<SYM, A_MN, B_MN, 256>(A, B, p, st);
+template <int BN>
+cudaError_t launch_iterate(const NsMaps& maps, const NsParams& p, cudaStream_t st) {
+  return p.tall ? launch_iterate_t<true, BN>(maps, p, st) : launch_iterate_t<false, BN>(maps, p, st);
+}
+
+// Column width of the tiles: the one whose products take the fewest clocks by this count.  A round of tiles over
+// the pairs takes k_blocks x BN x 2 clocks of products (512 columns; narrower tiles wait for L2: measured
+// factors 1.3 and 1.6), and the last epilogue, or for 512 columns every epilogue, comes on top.
+int pick_bn(const NsParams& p) {
+  const double pairs = sm_count() / 2;
+  int best = 512;
+  double best_t = 0.0;
+  for (int bn : {512, 256, 128}) {
+    const double sym = ceil((double)sym_tile_count(p.mm, bn) * p.batch / pairs);
+    const double upd = ceil((double)ceil_div(p.m, 256) * (double)ceil_div(p.n, bn) * p.batch / pairs);
+    const double slow = bn == 512 ? 1.0 : bn == 256 ? 1.3 : 1.6;
+    const double epi = 12.0 * bn;
+    double t = slow * 2.0 * bn * (sym * (p.kb_long + p.kb_short) + upd * p.kb_short);
+    t += bn == 512 ? epi * (2.0 * sym + upd) : epi * 3.0;
+    if (best_t == 0.0 || t < best_t) { best_t = t; best = bn; }
+  }
+  return best;
 }
 
 }  // namespace
@@ -617,9 +907,10 @@ cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st) {
   const float s = (float)(1 << ex);
   in.scale = s;
   in.hi = reinterpret_cast<__half*>(ws + L.hi[0]);
-  in.lo = reinterpret_cast<__half*>(ws + L.lo);
+  in.x32 = reinterpret_cast<float*>(ws + L.x32);
   in.bad = reinterpret_cast<int32_t*>(ws + L.bad);
   in.d_status = a.d_status;
+  in.arrivals = reinterpret_cast<uint32_t*>(ws + L.arrivals);
   const dim3 grid((unsigned)L.blocks, (unsigned)a.batch);
   ns_norm_kernel<<<grid, 256, 0, st>>>(in);
   cudaError_t e = cudaGetLastError();
@@ -627,48 +918,44 @@ cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st) {
   ns_split_kernel<<<grid, 256, 0, st>>>(in);
   if ((e = cudaGetLastError()) != cudaSuccess) return e;
 
-  const bool tall = a.m > a.n;
-  const int mm = (int)L.mm;
-  __half* gram = reinterpret_cast<__half*>(ws + L.gram);
-  __half* poly = reinterpret_cast<__half*>(ws + L.poly);
-  const NsOperand og = {gram, mm, mm, L.gld}, op = {poly, mm, mm, L.gld};
-  for (int k = 0; k < pr.steps; ++k) {
-    const NsOperand ox = {ws + L.hi[k & 1], a.n, a.m, L.ld};
-    NsParams p{};                                                // A = X X^T (X^T X)
-    p.batch = a.batch; p.rows = mm; p.cols = mm;
-    p.k_blocks = (int)ceil_div(longer, 64);
-    p.S = gram; p.ld = L.gld; p.alpha = 1.0f / (s * s);
-    p.d_status = a.d_status;
-    e = tall ? launch_ns<true, true, true>(ox, ox, p, st) : launch_ns<true, false, false>(ox, ox, p, st);
-    if (e != cudaSuccess) return e;
-    p.k_blocks = (int)ceil_div(mm, 64);                          // b A + c A A
-    p.S = poly; p.alpha = pr.coef_c; p.beta = pr.coef_b; p.Cin = gram;
-    if ((e = launch_ns<true, false, false>(og, og, p, st)) != cudaSuccess) return e;
-    NsParams q{};                                                // a X + (b A + c A A) X
-    q.batch = a.batch; q.rows = (int)a.m; q.cols = (int)a.n;
-    q.k_blocks = (int)ceil_div(mm, 64);
-    q.ld = L.ld; q.a = pr.coef_a;
-    q.hi = reinterpret_cast<const __half*>(ws + L.hi[k & 1]);
-    q.lo = in.lo;
-    q.hi_out = reinterpret_cast<__half*>(ws + L.hi[(k + 1) & 1]);
-    q.out_mode = OUT_PAIR;
-    q.d_status = a.d_status;
-    if (k == pr.steps - 1) {
-      q.out = a.out;
-      if (a.update) {
-        q.out_mode = a.out_dtype == SPO_DTYPE_BF16 ? OUT_W_BF16 : OUT_W_F32;
-        q.out_scale = pr.lr * a.update_scale / s;
-        q.decay = 1.0f - pr.lr * pr.weight_decay;
-        q.bad = in.bad;
-      } else {
-        q.out_mode = a.out_dtype == SPO_DTYPE_BF16 ? OUT_BF16 : OUT_F32;
-        q.out_scale = 1.0f / s;
-      }
-    }
-    e = tall ? launch_ns<false, false, false>(ox, op, q, st) : launch_ns<false, false, true>(op, ox, q, st);
-    if (e != cudaSuccess) return e;
+  NsParams p{};
+  p.batch = a.batch; p.steps = pr.steps; p.tall = a.m > a.n;
+  p.m = (int)a.m; p.n = (int)a.n; p.mm = (int)L.mm;
+  p.ld = L.ld; p.gld = L.gld;
+  p.kb_long = (int)ceil_div(longer, 64); p.kb_short = (int)ceil_div(L.mm, 64);
+  p.hi[0] = in.hi; p.hi[1] = reinterpret_cast<__half*>(ws + L.hi[1]);
+  p.x32 = in.x32;
+  p.gram_blk = reinterpret_cast<__half*>(ws + L.gram_blk);
+  p.gram = reinterpret_cast<__half*>(ws + L.gram);
+  p.poly = reinterpret_cast<__half*>(ws + L.poly);
+  p.inv_s2 = 1.0f / (s * s);
+  p.a = pr.coef_a; p.b = pr.coef_b; p.c = pr.coef_c;
+  p.out = a.out;
+  p.bad = in.bad;
+  p.arrivals = in.arrivals;
+  p.d_status = a.d_status;
+  if (a.update) {
+    p.out_mode = a.out_dtype == SPO_DTYPE_BF16 ? OUT_W_BF16 : OUT_W_F32;
+    p.out_scale = pr.lr * a.update_scale / s;
+    p.decay = 1.0f - pr.lr * pr.weight_decay;
+  } else {
+    p.out_mode = a.out_dtype == SPO_DTYPE_BF16 ? OUT_BF16 : OUT_F32;
+    p.out_scale = 1.0f / s;
   }
-  return cudaSuccess;
+  NsMaps maps;
+  for (int x = 0; x < 2; ++x)
+    if (!make_map3(&maps.x128[x], p.hi[x], a.n, a.m, a.batch, L.ld, 128) ||
+        !make_map3(&maps.x64[x], p.hi[x], a.n, a.m, a.batch, L.ld, 64))
+      return cudaErrorInvalidValue;
+  if (!make_map3(&maps.gram128, p.gram, L.mm, L.mm, a.batch, L.gld, 128) ||
+      !make_map3(&maps.gram64, p.gram, L.mm, L.mm, a.batch, L.gld, 64) ||
+      !make_map3(&maps.poly128, p.poly, L.mm, L.mm, a.batch, L.gld, 128) ||
+      !make_map3(&maps.poly64, p.poly, L.mm, L.mm, a.batch, L.gld, 64))
+    return cudaErrorInvalidValue;
+  const int bn = pick_bn(p);
+  if (bn == 512) return launch_iterate<512>(maps, p, st);
+  if (bn == 256) return launch_iterate<256>(maps, p, st);
+  return launch_iterate<128>(maps, p, st);
 }
 
 }  // namespace spo
