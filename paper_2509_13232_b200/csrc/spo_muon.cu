@@ -35,6 +35,9 @@ constexpr int NS_BM = 128;                      // rows of A per CTA; a pair's t
 constexpr int NS_EPI_WARPS = 8;
 constexpr int NS_THREADS = 32 * (2 + NS_EPI_WARPS);
 constexpr int NS_STAGING = 4096;
+constexpr int NS_RING = 192 * 1024;             // operand stages
+constexpr int NS_BARS = 512;                    // barriers of the two kinds of product, tensor-memory address, flags
+constexpr int NS_SMEM = NS_RING + 1024 + NS_BARS + NS_EPI_WARPS * NS_STAGING;
 
 template <int BN>
 struct NsCfg {
@@ -44,11 +47,18 @@ struct NsCfg {
   static constexpr int a_bytes = NS_BM * 64 * 2;
   static constexpr int b_bytes = b_rows * 64 * 2;
   static constexpr int stage_bytes = a_bytes + mmas * b_bytes;
-  static constexpr int stages = 192 * 1024 / stage_bytes;
-  static constexpr int smem = stages * stage_bytes + 1024 + 256 + NS_EPI_WARPS * NS_STAGING;
+  static constexpr int stages = NS_RING / stage_bytes;
   static constexpr int bufs = BN > 256 ? 1 : 2;          // accumulators in tensor memory
   static constexpr int tmem_cols = bufs * BN;
+  static constexpr int bar_bytes = 16 * stages + 32;
 };
+// Barriers of one kind of product: stages full / empty, accumulators full / empty.
+struct NsBars { uint32_t full0, empty0, tfull0, tempty0; };
+template <int BN>
+__device__ __forceinline__ NsBars ns_bars(uint32_t at) {
+  constexpr int S = NsCfg<BN>::stages;
+  return {at, at + 8 * S, at + 16 * S, at + 16 * S + 16};
+}
 
 enum : int { OUT_BF16 = 1, OUT_F32 = 2, OUT_W_BF16 = 3, OUT_W_F32 = 4 };
 
@@ -149,8 +159,9 @@ __device__ __forceinline__ bool ns_grid_wait(const NsParams& p, uint32_t goal, v
 template <bool SYM, int A, int B, int BN>
 __device__ __forceinline__ bool ns_produce(const CUtensorMap* a128, const CUtensorMap* a64, const CUtensorMap* b128,
                                            const CUtensorMap* b64, int total, int tiles, int n_tiles, int k_blocks,
-                                           uint32_t base, uint32_t full0, uint32_t empty0, uint32_t rank, uint32_t& it,
+                                           uint32_t base, const NsBars& bars, uint32_t rank, uint32_t& it,
                                            volatile int* abort_flag, int32_t* d_status) {
+  const uint32_t full0 = bars.full0, empty0 = bars.empty0;
   using C = NsCfg<BN>;
   for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2) {
     const NsTile tl = ns_tile<SYM, BN>(t, tiles, n_tiles);
@@ -185,8 +196,9 @@ __device__ __forceinline__ bool ns_produce(const CUtensorMap* a128, const CUtens
 
 template <bool SYM, int A, int B, int BN>
 __device__ __forceinline__ bool ns_multiply(int total, int tiles, int n_tiles, int k_blocks, uint32_t base, uint32_t tmem_base,
-                                            uint32_t full0, uint32_t empty0, uint32_t tfull0, uint32_t tempty0, uint32_t& it,
-                                            uint32_t& n, volatile int* abort_flag, int32_t* d_status) {
+                                            const NsBars& bars, uint32_t& it, uint32_t& n, volatile int* abort_flag,
+                                            int32_t* d_status) {
+  const uint32_t full0 = bars.full0, empty0 = bars.empty0, tfull0 = bars.tfull0, tempty0 = bars.tempty0;
   using C = NsCfg<BN>;
   // fp32 accumulate, fp16 A and B, M = 256 over the pair
   constexpr uint32_t idesc0 = (1u << 4) | ((uint32_t)(C::n_mma >> 3) << 17) | (16u << 24);
@@ -222,32 +234,32 @@ __device__ __forceinline__ bool ns_multiply(int total, int tiles, int n_tiles, i
 
 // What the epilogue warps share: barriers, tensor memory, staging buffer.
 struct NsEpi {
-  uint32_t tmem_base, tfull0, tempty0, rank;
+  uint32_t tmem_base, rank;
   uint8_t* stage;
   int quarter, half, lane;
   volatile int* abort_flag;
   int32_t* d_status;
 };
 template <int BN>
-__device__ __forceinline__ bool ns_tile_ready(const NsEpi& e, uint32_t n) {
+__device__ __forceinline__ bool ns_tile_ready(const NsEpi& e, const NsBars& bars, uint32_t n) {
   using C = NsCfg<BN>;
   int good = 1;
-  if (e.lane == 0) good = mbar_wait<20>(e.tfull0 + 8 * (n % C::bufs), (n / C::bufs) & 1u, e.abort_flag, e.d_status) ? 1 : 0;
+  if (e.lane == 0) good = mbar_wait<20>(bars.tfull0 + 8 * (n % C::bufs), (n / C::bufs) & 1u, e.abort_flag, e.d_status) ? 1 : 0;
   good = __shfl_sync(0xffffffffu, good, 0);
   tc_fence_after();
   return good != 0;
 }
 template <int BN>
-__device__ __forceinline__ void ns_tile_done(const NsEpi& e, uint32_t n) {
+__device__ __forceinline__ void ns_tile_done(const NsEpi& e, const NsBars& bars, uint32_t n) {
   tc_fence_before();
   __syncwarp();
-  if (e.lane == 0) mbar_arrive_cluster(map_to_cta(e.tempty0 + 8 * (n % NsCfg<BN>::bufs), 0));
+  if (e.lane == 0) mbar_arrive_cluster(map_to_cta(bars.tempty0 + 8 * (n % NsCfg<BN>::bufs), 0));
 }
 
 // A = acc / s^2, or b A + c acc (POLY); A is also kept in blocks, from which POLY reads it.  What a tile
 // reads is fetched before its products are waited for, then one step of 64 columns ahead.
 template <int BN, bool POLY>
-__device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsParams& p, int total, __half* S, float alpha, float beta,
+__device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars, const NsParams& p, int total, __half* S, float alpha, float beta,
                                              uint32_t& n) {
   const int lane = e.lane, rows = p.mm;
   const int64_t ld = p.gld;
@@ -269,7 +281,7 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsParams& p, 
       }
     };
     if (POLY && col_begin < col_end) fetch(col_begin);
-    if (!ns_tile_ready<BN>(e, n)) return false;
+    if (!ns_tile_ready<BN>(e, bars, n)) return false;
     const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN + e.half * (BN / 2);
 #pragma unroll 1
     for (int col0 = col_begin; col0 < col_end; col0 += 64) {
@@ -316,7 +328,7 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsParams& p, 
         if (row0 + r < rows && c < rows) *reinterpret_cast<uint4*>(S + mat + (int64_t)(row0 + r) * ld + c) = val;
       }
     }
-    ns_tile_done<BN>(e, n);
+    ns_tile_done<BN>(e, bars, n);
   }
   return true;
 }
@@ -383,7 +395,7 @@ __device__ __forceinline__ void ns_emit(const NsParams& p, const uint4& acc, int
 
 // x = a X + acc, stored as the next X (fp32 blocks and fp16 rows), as the result, or applied to the weights.
 template <int BN, bool LAST>
-__device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsParams& p, int total, __half* hi_out, uint32_t& n) {
+__device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& bars, const NsParams& p, int total, __half* hi_out, uint32_t& n) {
   const int lane = e.lane, rows = p.m, cols = p.n;
   const int vec = (cols & 3) == 0 ? 4 : (cols & 1) == 0 ? 2 : 1;
   for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2, ++n) {
@@ -400,7 +412,7 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsParams& 
       for (int q = 0; q < 8; ++q) next[q] = __ldcg(blk + step * 256 + 32 * q);
     };
     if (col_first < col_end) fetch(0);
-    if (!ns_tile_ready<BN>(e, n)) return false;
+    if (!ns_tile_ready<BN>(e, bars, n)) return false;
     const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN + e.half * (BN / 2);
 #pragma unroll 1
     for (int step = 0; col_first + 32 * step < col_end; step += 2) {
@@ -436,7 +448,7 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsParams& 
           for (int q = 0; q < 8; ++q)
             piece[q] = make_uint4(__float_as_uint(x32[q].x), __float_as_uint(x32[q].y), __float_as_uint(x32[q].z), __float_as_uint(x32[q].w));
           stage_put(e.stage, lane, piece);
-#pragma unroll
+#pragma unroll 1
           for (int i = 0; i < 8; ++i) {
             int rr, cc;
             const uint4 acc = stage_get(e.stage, lane, i, rr, cc);
@@ -457,29 +469,31 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsParams& 
         }
       }
     }
-    ns_tile_done<BN>(e, n);
+    ns_tile_done<BN>(e, bars, n);
   }
   return true;
 }
 
 // All products of the iteration in one cooperative launch: 3 steps products with a grid-wide barrier after each
 // (a counter in global memory; every wait is bounded).  A launch per product cost 10 to 17 us on a single
-// tile, most of it launching, filling the pipeline and draining one epilogue.
-// CTA pairs (cta_group::2) own 256 x BN tiles.  BN = 512: two products per k-step share A, which takes the
-// L2 -> SM traffic from 64 to 48 bytes per SM and clock (64 is all there is), but fills tensor memory, so a tile's
-// epilogue is not hidden; BN = 256 and 128: two accumulators, the epilogue runs under the next tile.
-template <bool TALL, int BN>
+// tile, most of it launching, filling the pipeline and draining one epilogue; here it is 6.
+// CTA pairs (cta_group::2) own 256 x BN tiles, BS columns for the symmetric products, BU for the update.  512: two
+// products per k-step share A, which takes the L2 -> SM traffic from 64 to 48 bytes per SM and clock (64 is all there
+// is: a k-block of 256 x 256 takes 1.25 times its clocks), but fills tensor memory, so every epilogue is exposed (9 us on a
+// 4096 x 4096 matrix).  256 and 128: two accumulators, the epilogue runs under the next tile.
+template <bool TALL, int BS, int BU>
 __global__ void __launch_bounds__(NS_THREADS, 1)
 ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ NsParams p) {
-  using C = NsCfg<BN>;
-  constexpr int S = C::stages;
+  using CS = NsCfg<BS>;
+  using CU = NsCfg<BU>;
+  static_assert(CS::bar_bytes + CU::bar_bytes + 16 <= NS_BARS, "barriers");
+  constexpr int kTmemCols = CS::tmem_cols > CU::tmem_cols ? CS::tmem_cols : CU::tmem_cols;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
-  const uint32_t bars = base + S * C::stage_bytes;
-  const uint32_t full0 = bars, empty0 = bars + 8 * S, tfull0 = bars + 16 * S, tempty0 = tfull0 + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + S * C::stage_bytes + 16 * S + 32);
+  const NsBars bs = ns_bars<BS>(base + NS_RING), bu = ns_bars<BU>(base + NS_RING + CS::bar_bytes);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + NS_RING + CS::bar_bytes + CU::bar_bytes);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* warps_done = tmem_slot + 2;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -488,14 +502,20 @@ ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ N
   const int products = 3 * p.steps;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < S; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(tfull0 + 8 * b, 1); mbar_init(tempty0 + 8 * b, 2 * NS_EPI_WARPS); }
+    for (int s = 0; s < CS::stages; ++s) { mbar_init(bs.full0 + 8 * s, 1); mbar_init(bs.empty0 + 8 * s, 1); }
+    for (int s = 0; s < CU::stages; ++s) { mbar_init(bu.full0 + 8 * s, 1); mbar_init(bu.empty0 + 8 * s, 1); }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(bs.tfull0 + 8 * b, 1);
+      mbar_init(bu.tfull0 + 8 * b, 1);
+      mbar_init(bs.tempty0 + 8 * b, 2 * NS_EPI_WARPS);
+      mbar_init(bu.tempty0 + 8 * b, 2 * NS_EPI_WARPS);
+    }
     *abort_flag = 0;
     *warps_done = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 0) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(C::tmem_cols) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
@@ -504,60 +524,58 @@ ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ N
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
 
+  // The stages of both kinds of product share the ring, the accumulators tensor memory: between two products
+  // everything is drained (the barrier comes after the last epilogue).
   if (warp == 0) {
     if (lane == 0) {
-      uint32_t it = 0;
+      uint32_t its = 0, itu = 0;
       for (int q = 0; q < products; ++q) {
         if (q > 0 && !ns_grid_wait(p, (uint32_t)q * gridDim.x, abort_flag)) break;
         fence_proxy_async();                        // the operands were written by plain stores
         const int k = q / 3, kind = q - 3 * k, x = k & 1;
         bool ok;
         if (kind == 0)
-          ok = ns_produce<true, TALL ? OP_MN : OP_K, TALL ? OP_MN : OP_K, BN>(
-              &maps.x128[x], &maps.x64[x], &maps.x128[x], &maps.x64[x], sym_total, p.sym_tiles, p.sym_n, p.kb_long, base, full0,
-              empty0, rank, it, abort_flag, p.d_status);
+          ok = ns_produce<true, TALL ? OP_MN : OP_K, TALL ? OP_MN : OP_K, BS>(
+              &maps.x128[x], &maps.x64[x], &maps.x128[x], &maps.x64[x], sym_total, p.sym_tiles, p.sym_n, p.kb_long, base, bs, rank,
+              its, abort_flag, p.d_status);
         else if (kind == 1)
-          ok = ns_produce<true, OP_SYM, OP_SYM, BN>(&maps.gram128, &maps.gram64, &maps.gram128, &maps.gram64, sym_total,
-                                                    p.sym_tiles, p.sym_n, p.kb_short, base, full0, empty0, rank, it, abort_flag,
-                                                    p.d_status);
+          ok = ns_produce<true, OP_SYM, OP_SYM, BS>(&maps.gram128, &maps.gram64, &maps.gram128, &maps.gram64, sym_total,
+                                                    p.sym_tiles, p.sym_n, p.kb_short, base, bs, rank, its, abort_flag, p.d_status);
         else if (TALL)
-          ok = ns_produce<false, OP_K, OP_SYM, BN>(&maps.x128[x], &maps.x64[x], &maps.poly128, &maps.poly64, upd_total,
-                                                   p.upd_tiles, p.upd_n, p.kb_short, base, full0, empty0, rank, it, abort_flag,
-                                                   p.d_status);
+          ok = ns_produce<false, OP_K, OP_SYM, BU>(&maps.x128[x], &maps.x64[x], &maps.poly128, &maps.poly64, upd_total,
+                                                   p.upd_tiles, p.upd_n, p.kb_short, base, bu, rank, itu, abort_flag, p.d_status);
         else
-          ok = ns_produce<false, OP_SYM, OP_MN, BN>(&maps.poly128, &maps.poly64, &maps.x128[x], &maps.x64[x], upd_total,
-                                                    p.upd_tiles, p.upd_n, p.kb_short, base, full0, empty0, rank, it, abort_flag,
-                                                    p.d_status);
+          ok = ns_produce<false, OP_SYM, OP_MN, BU>(&maps.poly128, &maps.poly64, &maps.x128[x], &maps.x64[x], upd_total,
+                                                    p.upd_tiles, p.upd_n, p.kb_short, base, bu, rank, itu, abort_flag, p.d_status);
         if (!ok) break;
       }
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
-      uint32_t it = 0, n = 0;
+      uint32_t its = 0, itu = 0, ns = 0, nu = 0;
       for (int q = 0; q < products; ++q) {
         const int kind = q % 3;
         bool ok;
         if (kind == 0)
-          ok = ns_multiply<true, TALL ? OP_MN : OP_K, TALL ? OP_MN : OP_K, BN>(sym_total, p.sym_tiles, p.sym_n, p.kb_long, base,
-                                                                               tmem_base, full0, empty0, tfull0, tempty0, it, n,
-                                                                               abort_flag, p.d_status);
+          ok = ns_multiply<true, TALL ? OP_MN : OP_K, TALL ? OP_MN : OP_K, BS>(sym_total, p.sym_tiles, p.sym_n, p.kb_long, base,
+                                                                               tmem_base, bs, its, ns, abort_flag, p.d_status);
         else if (kind == 1)
-          ok = ns_multiply<true, OP_SYM, OP_SYM, BN>(sym_total, p.sym_tiles, p.sym_n, p.kb_short, base, tmem_base, full0, empty0,
-                                                     tfull0, tempty0, it, n, abort_flag, p.d_status);
+          ok = ns_multiply<true, OP_SYM, OP_SYM, BS>(sym_total, p.sym_tiles, p.sym_n, p.kb_short, base, tmem_base, bs, its, ns,
+                                                     abort_flag, p.d_status);
         else
-          ok = ns_multiply<false, TALL ? OP_K : OP_SYM, TALL ? OP_SYM : OP_MN, BN>(upd_total, p.upd_tiles, p.upd_n, p.kb_short, base,
-                                                                                   tmem_base, full0, empty0, tfull0, tempty0, it,
-                                                                                   n, abort_flag, p.d_status);
+          ok = ns_multiply<false, TALL ? OP_K : OP_SYM, TALL ? OP_SYM : OP_MN, BU>(upd_total, p.upd_tiles, p.upd_n, p.kb_short,
+                                                                                   base, tmem_base, bu, itu, nu, abort_flag,
+                                                                                   p.d_status);
         if (!ok) break;
       }
     }
   } else {
     NsEpi e;
-    e.tmem_base = tmem_base; e.tfull0 = tfull0; e.tempty0 = tempty0; e.rank = rank;
-    e.stage = gen + S * C::stage_bytes + 256 + (warp - 2) * NS_STAGING;
+    e.tmem_base = tmem_base; e.rank = rank;
+    e.stage = gen + NS_RING + NS_BARS + (warp - 2) * NS_STAGING;
     e.quarter = warp & 3; e.half = (warp - 2) >> 2; e.lane = lane;
     e.abort_flag = abort_flag; e.d_status = p.d_status;
-    uint32_t n = 0;
+    uint32_t ns = 0, nu = 0;
     for (int q = 0; q < products; ++q) {
       if (q > 0) {
         int good = 1;
@@ -567,13 +585,13 @@ ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ N
       const int k = q / 3, kind = q - 3 * k;
       bool ok;
       if (kind == 0)
-        ok = ns_store_sym<BN, false>(e, p, sym_total, p.gram, p.inv_s2, 0.0f, n);
+        ok = ns_store_sym<BS, false>(e, bs, p, sym_total, p.gram, p.inv_s2, 0.0f, ns);
       else if (kind == 1)
-        ok = ns_store_sym<BN, true>(e, p, sym_total, p.poly, p.c, p.b, n);
+        ok = ns_store_sym<BS, true>(e, bs, p, sym_total, p.poly, p.c, p.b, ns);
       else if (k < p.steps - 1)
-        ok = ns_store_update<BN, false>(e, p, upd_total, p.hi[(k + 1) & 1], n);
+        ok = ns_store_update<BU, false>(e, bu, p, upd_total, p.hi[(k + 1) & 1], nu);
       else
-        ok = ns_store_update<BN, true>(e, p, upd_total, nullptr, n);
+        ok = ns_store_update<BU, true>(e, bu, p, upd_total, nullptr, nu);
       if (!ok) break;
       if (q + 1 < products) {                       // this CTA's part of the product is in memory: count it
         // (no barrier among the warps: one that gave up must not leave the others waiting)
@@ -596,7 +614,7 @@ ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ N
   __syncthreads();
   cluster_sync_all();
   if (warp == 0)
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::tmem_cols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
 }
 
 // ---------------------------------------------------------------------------
@@ -763,9 +781,9 @@ constexpr int kNormBlocks = 592;
 
 NsWs ns_layout(int64_t m, int64_t n, int64_t batch) {
   NsWs L{};
-  L.ld = (n + 7) / 8 * 8;
+  L.ld = (n + 63) / 64 * 64;                  // rows begin on 128 bytes: a row of a TMA box is one line, not parts of two
   L.mm = m < n ? m : n;
-  L.gld = (L.mm + 7) / 8 * 8;
+  L.gld = (L.mm + 63) / 64 * 64;
   const int64_t want = ceil_div(m * n, 4096);
   L.blocks = (int)(want < kNormBlocks ? want : kNormBlocks);
   const size_t x = (size_t)batch * m * L.ld * 2, g = (size_t)batch * L.mm * L.gld * 2;
@@ -796,7 +814,7 @@ bool make_map3(CUtensorMap* m, const void* ptr, int64_t cols, int64_t rows, int6
 }
 
 // CTA pairs of an instantiation that can be resident together (0 = not yet asked); one slot per device.
-template <bool TALL, int BN>
+template <bool TALL, int BS, int BU>
 cudaError_t ns_resident(int* out) {
   static std::atomic<int> cached[64];
   int dev = 0;
@@ -805,13 +823,13 @@ cudaError_t ns_resident(int* out) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   int n = cached[dev].load(std::memory_order_acquire);
   if (n == 0) {
-    auto kern = ns_iterate_kernel<TALL, BN>;
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NsCfg<BN>::smem);
+    auto kern = ns_iterate_kernel<TALL, BS, BU>;
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, NS_SMEM);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t q = {};
     q.gridDim = dim3((unsigned)(sm_count() / 2 * 2), 1, 1);
     q.blockDim = dim3(NS_THREADS, 1, 1);
-    q.dynamicSmemBytes = NsCfg<BN>::smem;
+    q.dynamicSmemBytes = NS_SMEM;
     cudaLaunchAttribute qa[1];
     qa[0].id = cudaLaunchAttributeClusterDimension;
     qa[0].val.clusterDim.x = 2;
@@ -836,20 +854,20 @@ int64_t sym_tile_count(int64_t mm, int bn) {
   return tiles;
 }
 
-template <bool TALL, int BN>
+template <bool TALL, int BS, int BU>
 cudaError_t launch_iterate_t(const NsMaps& maps, NsParams p, cudaStream_t st) {
   int pairs = 0;
-  cudaError_t e = ns_resident<TALL, BN>(&pairs);
+  cudaError_t e = ns_resident<TALL, BS, BU>(&pairs);
   if (e != cudaSuccess) return e;
-  const int64_t sym = sym_tile_count(p.mm, BN), un = ceil_div(p.n, BN), upd = ceil_div(p.m, 256) * un;
+  const int64_t sym = sym_tile_count(p.mm, BS), un = ceil_div(p.n, BU), upd = ceil_div(p.m, 256) * un;
   const int64_t most = (sym > upd ? sym : upd) * p.batch;
   if (most > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  p.sym_tiles = (int)sym; p.sym_n = (int)ceil_div(p.mm, BN);
+  p.sym_tiles = (int)sym; p.sym_n = (int)ceil_div(p.mm, BS);
   p.upd_tiles = (int)upd; p.upd_n = (int)un;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * (most < pairs ? most : pairs)), 1, 1);
   cfg.blockDim = dim3(NS_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = NsCfg<BN>::smem;
+  cfg.dynamicSmemBytes = NS_SMEM;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -860,31 +878,26 @@ cudaError_t launch_iterate_t(const NsMaps& maps, NsParams p, cudaStream_t st) {
   attr[1].val.cooperative = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, ns_iterate_kernel<TALL, BN>, maps, p);
+  return cudaLaunchKernelEx(&cfg, ns_iterate_kernel<TALL, BS, BU>, maps, p);
 }
 
-template <int BN>
+template <int BS, int BU>
 cudaError_t launch_iterate(const NsMaps& maps, const NsParams& p, cudaStream_t st) {
-  return p.tall ? launch_iterate_t<true, BN>(maps, p, st) : launch_iterate_t<false, BN>(maps, p, st);
+  return p.tall ? launch_iterate_t<true, BS, BU>(maps, p, st) : launch_iterate_t<false, BS, BU>(maps, p, st);
 }
 
-// Column width of the tiles: the one whose products take the fewest clocks by this count.  A round of tiles over
-// the pairs takes k_blocks x BN x 2 clocks of products (512 columns; narrower tiles wait for L2: measured
-// factors 1.3 and 1.6), and the last epilogue, or for 512 columns every epilogue, comes on top.
-int pick_bn(const NsParams& p) {
+// Column widths of the tiles, by the time their products take: rounds of tiles over the pairs x k-blocks x the
+// nanoseconds of a k-block (610 / 380 / 240 for 512 / 256 / 128 columns, measured; 1.0 / 1.25 / 1.6 times the clocks of
+// its products, the narrow ones waiting for L2), and the exposed epilogues: one a round for 512, the last one for the others.
+double sym_time(const NsParams& p, int bn) {
+  const double pairs = sm_count() / 2, rounds = ceil((double)sym_tile_count(p.mm, bn) * p.batch / pairs);
+  const double kb = p.kb_long + p.kb_short;
+  return bn == 512 ? rounds * (kb * 610.0 + 2 * 9000.0) : rounds * kb * 380.0 + 2 * 5000.0;
+}
+double update_time(const NsParams& p, int bn) {
   const double pairs = sm_count() / 2;
-  int best = 512;
-  double best_t = 0.0;
-  for (int bn : {512, 256, 128}) {
-    const double sym = ceil((double)sym_tile_count(p.mm, bn) * p.batch / pairs);
-    const double upd = ceil((double)ceil_div(p.m, 256) * (double)ceil_div(p.n, bn) * p.batch / pairs);
-    const double slow = bn == 512 ? 1.0 : bn == 256 ? 1.3 : 1.6;
-    const double epi = 12.0 * bn;
-    double t = slow * 2.0 * bn * (sym * (p.kb_long + p.kb_short) + upd * p.kb_short);
-    t += bn == 512 ? epi * (2.0 * sym + upd) : epi * 3.0;
-    if (best_t == 0.0 || t < best_t) { best_t = t; best = bn; }
-  }
-  return best;
+  const double rounds = ceil((double)ceil_div(p.m, 256) * (double)ceil_div(p.n, bn) * p.batch / pairs);
+  return rounds * p.kb_short * (bn == 256 ? 380.0 : 240.0) + (bn == 256 ? 7000.0 : 4000.0);
 }
 
 }  // namespace
@@ -952,10 +965,9 @@ cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st) {
       !make_map3(&maps.poly128, p.poly, L.mm, L.mm, a.batch, L.gld, 128) ||
       !make_map3(&maps.poly64, p.poly, L.mm, L.mm, a.batch, L.gld, 64))
     return cudaErrorInvalidValue;
-  const int bn = pick_bn(p);
-  if (bn == 512) return launch_iterate<512>(maps, p, st);
-  if (bn == 256) return launch_iterate<256>(maps, p, st);
-  return launch_iterate<128>(maps, p, st);
+  const bool wide = sym_time(p, 512) < sym_time(p, 256), narrow = update_time(p, 128) < update_time(p, 256);
+  if (wide) return narrow ? launch_iterate<512, 128>(maps, p, st) : launch_iterate<512, 256>(maps, p, st);
+  return narrow ? launch_iterate<256, 128>(maps, p, st) : launch_iterate<256, 256>(maps, p, st);
 }
 
 }  // namespace spo
