@@ -266,11 +266,12 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
   for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2, ++n) {
     const NsTile tl = ns_tile<true, BN>(t, p.sym_tiles, p.sym_n);
     const int row0 = tl.i * 256 + (int)e.rank * NS_BM + e.quarter * 32;
-    const int col_first = tl.j * BN + e.half * (BN / 2);
+    // Columns left of the diagonal block (512-wide tiles of odd row blocks) are the mirror of another tile.  The
+    // two warps of a quarter take alternate steps of 64 columns, so that a narrow matrix occupies both.
+    const int tile_col = tl.j * BN;
     const int64_t mat = (int64_t)tl.b * rows * ld;
-    // columns left of the diagonal block (512-wide tiles of odd row blocks) are the mirror of another tile
-    const int col_begin = col_first < tl.i * 256 ? tl.i * 256 : col_first;
-    const int col_end = row0 >= rows ? col_begin : col_first + BN / 2 < rows ? col_first + BN / 2 : rows;
+    const int col_begin = (tile_col < tl.i * 256 ? tl.i * 256 : tile_col) + e.half * 64;
+    const int col_end = row0 >= rows ? 0 : tile_col + BN < rows ? tile_col + BN : rows;
     uint4 next[8];
     auto fetch = [&](int c0) {
 #pragma unroll
@@ -282,12 +283,12 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
     };
     if (POLY && col_begin < col_end) fetch(col_begin);
     if (!ns_tile_ready<BN>(e, bars, n)) return false;
-    const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN + e.half * (BN / 2);
+    const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN;
 #pragma unroll 1
-    for (int col0 = col_begin; col0 < col_end; col0 += 64) {
+    for (int col0 = col_begin; col0 < col_end; col0 += 128) {
       uint32_t v0[32], v1[32];
-      tmem_ld32_nowait(taddr + (col0 - col_first), v0);
-      tmem_ld32_nowait(taddr + (col0 - col_first) + 32, v1);
+      tmem_ld32_nowait(taddr + (col0 - tile_col), v0);
+      tmem_ld32_nowait(taddr + (col0 - tile_col) + 32, v1);
       tmem_wait_ld(v0);
       tmem_wait_ld(v1);
       uint4 piece[8];
@@ -308,7 +309,7 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
         }
         piece[q] = make_uint4(o[0], o[1], o[2], o[3]);
       }
-      if (POLY && col0 + 64 < col_end) fetch(col0 + 64);
+      if (POLY && col0 + 128 < col_end) fetch(col0 + 128);
       if (!POLY) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -401,21 +402,21 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
   for (int t = blockIdx.x / 2; t < total; t += gridDim.x / 2, ++n) {
     const NsTile tl = ns_tile<false, BN>(t, p.upd_tiles, p.upd_n);
     const int row0 = tl.i * 256 + (int)e.rank * NS_BM + e.quarter * 32;
-    const int col_first = tl.j * BN + e.half * (BN / 2);
+    const int col_first = tl.j * BN;                      // alternate steps of 64 columns, as above
     const int64_t mat = (int64_t)tl.b * rows * p.ld, umat = (int64_t)tl.b * rows * cols;
     const bool skip = LAST && (p.out_mode == OUT_W_BF16 || p.out_mode == OUT_W_F32) && p.bad[tl.b] != 0;
-    const int col_end = row0 >= rows ? col_first : col_first + BN / 2 < cols ? col_first + BN / 2 : cols;
+    const int col_end = row0 >= rows ? 0 : col_first + BN < cols ? col_first + BN : cols;
     float4* blk = reinterpret_cast<float4*>(p.x32 + ns_block(tl.b, row0, col_first, rows, cols)) + lane;   // + 256 per 32 columns
     float4 next[8];
     auto fetch = [&](int step) {
 #pragma unroll
       for (int q = 0; q < 8; ++q) next[q] = __ldcg(blk + step * 256 + 32 * q);
     };
-    if (col_first < col_end) fetch(0);
+    if (col_first + e.half * 64 < col_end) fetch(2 * e.half);
     if (!ns_tile_ready<BN>(e, bars, n)) return false;
-    const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN + e.half * (BN / 2);
+    const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN;
 #pragma unroll 1
-    for (int step = 0; col_first + 32 * step < col_end; step += 2) {
+    for (int step = 2 * e.half; col_first + 32 * step < col_end; step += 4) {
       uint4 piece[8];                                     // !LAST: 64 columns of fp16, one round through the staging buffer
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -435,7 +436,7 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
           x32[q].z = fmaf(p.a, next[q].z, __uint_as_float(v[4 * q + 2]));
           x32[q].w = fmaf(p.a, next[q].w, __uint_as_float(v[4 * q + 3]));
         }
-        if (col0 + 32 < col_end) fetch(step + h + 1);
+        if (h == 0 ? col0 + 32 < col_end : col0 + 96 < col_end) fetch(h == 0 ? step + 1 : step + 4);
         if constexpr (!LAST) {
 #pragma unroll
           for (int q = 0; q < 8; ++q) blk[(step + h) * 256 + 32 * q] = x32[q];
