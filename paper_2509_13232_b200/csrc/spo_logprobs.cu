@@ -9,9 +9,9 @@
 //                    split in registers, column groups of largest maximum listed on the way;
 //                    lp_merge_kernel joins the splits.
 //   few bf16 rows    (up to kLpStreamRows) lp_stream_kernel: bound by reading W once, so W is the operand
-//                    with 128 rows a tile and the token rows are the narrow one; the logits of these
-//                    few rows go to scratch (L2) and lp_rows_kernel reduces them.
-//   fp32             sgemm_kernel into a chunk of scratch, then lp_rows_kernel.
+//                    with 128 rows a tile and the token rows are the narrow one; every CTA keeps statistics
+//                    and a sorted list per token row under the stream, lp_merge_kernel joins the CTAs'.
+//   fp32             sgemm_kernel into a chunk of scratch, lp_rows_kernel, lp_merge_kernel.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -57,9 +57,38 @@ struct WarpTop {
     last_v = __shfl_sync(0xffffffffu, v, K - 1);
     last_id = __shfl_sync(0xffffffffu, id, K - 1);
   }
-  // One candidate per lane; lanes are taken in ascending order.
+  static __device__ __forceinline__ bool better(float x, int xi, float y, int yi) { return x > y || (x == y && xi < yi); }
+  // Joins a list that is sorted over the lanes (descending, empty entries -inf): the larger of entries i and 31 - i are
+  // the 32 largest of both and form a bitonic sequence, which five compare-exchanges sort.
+  __device__ __forceinline__ void merge(float x, int xi, int xa, int K, int lane) {
+    const float rx = __shfl_sync(0xffffffffu, x, 31 - lane);
+    const int ri = __shfl_sync(0xffffffffu, xi, 31 - lane), ra = __shfl_sync(0xffffffffu, xa, 31 - lane);
+    if (better(rx, ri, v, id)) { v = rx; id = ri; aux = ra; }
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) exchange(v, id, aux, s, (lane & s) == 0);
+    if (lane >= K) { v = -CUDART_INF_F; id = 0x7FFFFFFF; }
+    last_v = __shfl_sync(0xffffffffu, v, K - 1);
+    last_id = __shfl_sync(0xffffffffu, id, K - 1);
+  }
+  static __device__ __forceinline__ void exchange(float& x, int& xi, int& xa, int s, bool keep_larger) {
+    const float px = __shfl_xor_sync(0xffffffffu, x, s);
+    const int pi = __shfl_xor_sync(0xffffffffu, xi, s), pa = __shfl_xor_sync(0xffffffffu, xa, s);
+    if (keep_larger ? better(px, pi, x, xi) : better(x, xi, px, pi)) { x = px; xi = pi; xa = pa; }
+  }
+  // One candidate per lane.  A few are inserted one after the other (some 70 clocks each); many are sorted
+  // (15 compare-exchanges) and merged (6 steps), some 600 clocks whatever their number.
   __device__ __forceinline__ void offer(float x, int xi, int xa, int K, int lane) {
-    unsigned todo = __ballot_sync(0xffffffffu, beats(x, xi));
+    const bool in = beats(x, xi);
+    unsigned todo = __ballot_sync(0xffffffffu, in);
+    if (__popc(todo) > 8) {
+      if (!in) { x = -CUDART_INF_F; xi = 0x7FFFFFFF; }
+#pragma unroll
+      for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j > 0; j >>= 1) exchange(x, xi, xa, j, ((lane & j) == 0) == ((lane & k) == 0));
+      merge(x, xi, xa, K, lane);
+      return;
+    }
     while (todo) {
       const int src = __ffs(todo) - 1;
       todo &= todo - 1;
@@ -69,6 +98,11 @@ struct WarpTop {
     }
   }
 };
+
+// The launch before this one in the stream may still be running (programmatic dependent launch): wait for it to
+// have finished, and let the next launch come up behind this one.
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // (m2, l, ez) of two disjoint parts of a row, joined: m2 in log2 units, l = sum 2^(z sc2 - m2), ez = sum z 2^(...)
 __device__ __forceinline__ void join_stats(float& m2, float& l, float& ez, float m2b, float lb, float ezb) {
@@ -97,6 +131,8 @@ constexpr int kRowWarps = 8;
 __global__ void __launch_bounds__(32 * kRowWarps)
 lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int32_t V, int nseg, int part, const int32_t* __restrict__ y,
                float sc2, int K, FwdPartial* __restrict__ partials, float2* __restrict__ cand) {
+  pdl_trigger();
+  pdl_wait();
   const int64_t row = blockIdx.x / nseg;
   const int seg = (int)(blockIdx.x - row * nseg);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -156,20 +192,19 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int32_t V, int nseg, in
     partials[row * nseg + seg] = pt;
   }
   if (K > 0) {
-    for (int i = 0; i < kRowWarps * K; i += 32) {
-      const bool have = i + lane < kRowWarps * K && !(i < K && i + lane < K);   // warp 0's own list is in its registers
-      const float2 c = have ? s_top[i + lane] : make_float2(-CUDART_INF_F, __int_as_float(0x7FFFFFFF));
-      top.offer(c.x, __float_as_int(c.y), 0, K, lane);
+    for (int w = 1; w < kRowWarps; ++w) {
+      const float2 c = lane < K ? s_top[w * K + lane] : make_float2(-CUDART_INF_F, __int_as_float(0x7FFFFFFF));
+      if (__any_sync(0xffffffffu, top.beats(c.x, __float_as_int(c.y)))) top.merge(c.x, __float_as_int(c.y), 0, K, lane);
     }
     if (lane < K) cand[(row * nseg + seg) * K + lane] = make_float2(top.v, __int_as_float(top.id));
   }
 }
 
 // ---------------------------------------------------------------------------
-// One warp per token row: joins the row's partials, finishes logp / lse / entropy, and finds the
-// alternatives among the row's lists.  GROUPS: the lists hold column groups (maximum, group << 8 | slot)
-// whose 32 logits are stored in `cand`; first the K groups of largest maximum, then the K largest logits
-// in them.  Otherwise the lists hold the logits themselves, (value, id).
+// The end of every path: joins a token row's partials, finishes logp / lse / entropy, and finds the
+// alternatives among the row's lists.  WARPS warps per row.  GROUPS: the lists hold column groups (maximum, group << 8 |
+// slot) whose 32 logits are stored in `cand`; first the K groups of largest maximum, then the K largest logits
+// in them.  Otherwise the lists hold the logits themselves, (value, id), sorted.
 // ---------------------------------------------------------------------------
 struct LpOut {
   const int32_t* y;
@@ -183,29 +218,89 @@ struct LpOut {
   int32_t* d_status;
 };
 
-template <bool GROUPS>
-__global__ void __launch_bounds__(128)
+template <bool GROUPS, int WARPS>
+__global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS)
 lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part_ld, const float2* __restrict__ tops,
                 const float* __restrict__ cand, int list_len, int64_t rows, int64_t t0, const LpOut o) {
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  static_assert(WARPS == 1 || !GROUPS, "column groups are merged by one warp");
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5;
+  const int64_t row = WARPS == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
   if (row >= rows) return;
   const int64_t t = t0 + row;
+  const int K = o.K;
   // partial of list s: [s][part_ld] (GROUPS) or [row][lists]
   auto at = [&](int s) { return GROUPS ? (int64_t)s * part_ld + row : row * lists + s; };
   float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f, zt = -CUDART_INF_F;
   bool odd = false;                                 // a partial that is NaN: fmaxf would drop it
-  for (int s = lane; s < lists; s += 32) {
+  for (int s = lane + 32 * warp; s < lists; s += 32 * WARPS) {
     const FwdPartial p = partials[at(s)];
     odd |= !(p.l >= 0.0f);
     zt = p.zt > -CUDART_INF_F || p.zt != p.zt ? p.zt : zt;   // at most one list has the target
     join_stats(m2, l, ez, p.m2, p.l, p.pad);
+  }
+  WarpTop top;
+  top.init();
+  if (K > 0) {
+    if (GROUPS) {
+      const int n = lists * list_len;
+      for (int i0 = 0; i0 < n; i0 += 32) {
+        const int i = i0 + lane;
+        float x = -CUDART_INF_F;
+        int id = 0x7FFFFFFF, aux = 0;
+        if (i < n) {
+          const int s = i / list_len, k = i - s * list_len;
+          const float2 c = tops[at(s) * list_len + k];
+          x = c.x;
+          id = (int)(__float_as_uint(c.y) >> 8);
+          aux = s * list_len + (int)(__float_as_uint(c.y) & 255u);
+        }
+        top.offer(x, id, aux, K, lane);
+      }
+    } else {
+      const float2 none = make_float2(-CUDART_INF_F, __int_as_float(0x7FFFFFFF));
+      for (int s0 = warp; s0 < lists; s0 += 4 * WARPS) {          // four lists in flight
+        float2 c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          c[i] = lane < K && s0 + i * WARPS < lists ? tops[at(s0 + i * WARPS) * K + lane] : none;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (__any_sync(0xffffffffu, top.beats(c[i].x, __float_as_int(c[i].y)))) top.merge(c[i].x, __float_as_int(c[i].y), 0, K, lane);
+      }
+    }
   }
   warp_join_stats(m2, l, ez);
   odd = __any_sync(0xffffffffu, odd);
   {
     const unsigned has = __ballot_sync(0xffffffffu, zt > -CUDART_INF_F || zt != zt);
     zt = has ? __shfl_sync(0xffffffffu, zt, __ffs(has) - 1) : -CUDART_INF_F;
+  }
+  if (WARPS > 1) {                                  // warp 0 joins the others' results
+    __shared__ float4 s_stat[WARPS];
+    __shared__ int s_odd[WARPS];
+    __shared__ float2 s_top[WARPS][32];
+    if (lane == 0) { s_stat[warp] = make_float4(m2, l, ez, zt); s_odd[warp] = odd; }
+    s_top[warp][lane] = make_float2(top.v, __int_as_float(top.id));
+    __syncthreads();
+    if (warp != 0) return;
+    m2 = -CUDART_INF_F; l = 0.0f; ez = 0.0f;
+    float zw = -CUDART_INF_F;
+    if (lane < WARPS) {
+      const float4 q = s_stat[lane];
+      m2 = q.x; l = q.y; ez = q.z; zw = q.w;
+      odd |= s_odd[lane] != 0;
+    }
+    warp_join_stats(m2, l, ez);
+    odd = __any_sync(0xffffffffu, odd);
+    const unsigned has = __ballot_sync(0xffffffffu, zw > -CUDART_INF_F || zw != zw);
+    zt = has ? __shfl_sync(0xffffffffu, zw, __ffs(has) - 1) : -CUDART_INF_F;
+    if (K > 0)
+      for (int w = 1; w < WARPS; ++w) {
+        const float2 c = s_top[w][lane];
+        if (__any_sync(0xffffffffu, top.beats(c.x, __float_as_int(c.y)))) top.merge(c.x, __float_as_int(c.y), 0, K, lane);
+      }
   }
   float lse = (m2 + log2f(l)) * kLn2;
   if (odd) lse = CUDART_NAN_F;
@@ -224,28 +319,7 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part
     o.lse[t] = on ? lse : 0.0f;
     if (o.entropy) o.entropy[t] = on ? lse - o.inv_t * (ez / l) : 0.0f;
   }
-  const int K = o.K;
   if (K == 0) return;
-  WarpTop top;
-  top.init();
-  const int n = lists * list_len;
-  for (int i0 = 0; i0 < n; i0 += 32) {
-    const int i = i0 + lane;
-    float x = -CUDART_INF_F;
-    int id = 0x7FFFFFFF, aux = 0;
-    if (i < n) {
-      const int s = i / list_len, k = i - s * list_len;
-      const float2 c = tops[at(s) * list_len + k];
-      x = c.x;
-      if (GROUPS) {
-        id = (int)(__float_as_uint(c.y) >> 8);
-        aux = s * list_len + (int)(__float_as_uint(c.y) & 255u);
-      } else {
-        id = __float_as_int(c.y);
-      }
-    }
-    top.offer(x, id, aux, K, lane);
-  }
   if (GROUPS) {
     const WarpTop g = top;
     top.init();
@@ -267,50 +341,79 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part
 }
 
 // ---------------------------------------------------------------------------
-// Few bf16 token rows: Z[t][v] = h_t . w_v with W streamed once.  One CTA per SM walks tiles of `tile_h`
-// (at most 128) vocabulary rows; TMA brings 64-deep k-blocks of the tile and of all token rows, one MMA per
-// 16 of k with M = 128 vocabulary rows and N = NT token rows accumulates in tensor memory (two
-// buffers, so the store of a tile overlaps the next one's stream).  W is read once (the floor); the token rows
-// come from L2 once per tile, NT / tile_h of W's traffic.  tile_h is the smallest height that takes the
-// same number of rounds over the SMs, so that the last round is full (V = 151936 on 148 SMs: 115 rows x 9
-// rounds reads 0.8 % more than an even share, 128-row tiles would leave the ninth round nearly empty).
+// Few bf16 token rows, with W streamed once.  One CTA per SM walks tiles of `tile_h` (at most 128) vocabulary
+// rows; TMA brings 64-deep k-blocks of the tile and of all token rows, one MMA per 16 of k with M = 128 vocabulary rows
+// and N = NT token rows accumulates in tensor memory (two buffers, so a tile is reduced while the next one
+// streams).  W is read once, which is the floor (1.24 GB at d = 4096, V = 151936: 190 us at the measured copy rate); the token
+// rows come from L2 once per tile, NT / tile_h of W's traffic.  tile_h is the smallest height that takes the same number of
+// rounds over the SMs, so that the last round is full (V = 151936 on 148 SMs: 115 rows x 9 rounds reads 0.8 %
+// more than an even share, 128-row tiles would leave the ninth round nearly empty).
+// Reduction: eight warps turn the finished tile into [token][vocabulary row] in shared memory, then each takes
+// the tokens w, w + 8, ..: a lane holds four logits, the row's maximum and sums are warp reductions, lane k keeps the
+// running statistics of the warp's k-th token, and a tile whose maximum beats the token's K-th entry goes into its
+// sorted list.  Storing the logits and reducing them in further launches took 254 us where this takes 196 (one token,
+// K = 20): 80 us of launches that read 0.6 MB, most of it chains of list insertions in a few warps.
 // ---------------------------------------------------------------------------
 struct StreamParams {
   int tiles, tile_h, k_blocks;
-  int T;
+  int T, K;
   int32_t V;
-  float* Z;
-  int64_t ldz;
+  float sc2;
+  const int32_t* y;
+  FwdPartial* partials;                      // [T][gridDim.x]
+  float2* tops;                              // [T][gridDim.x][K]
   int32_t* d_status;
 };
 
-constexpr int kStreamThreads = 192;          // TMA warp, MMA warp, four epilogue warps
+constexpr int kStreamWarps = 8;              // reducing warps
+constexpr int kStreamThreads = 64 + 32 * kStreamWarps;
 constexpr int kStreamA = 128 * 64 * 2;
 template <int NT> struct StreamCfg {
   static constexpr int stage_bytes = kStreamA + NT * 128;
-  static constexpr int stages = (200 * 1024) / stage_bytes;
-  static constexpr int smem = stages * stage_bytes + 1024 + 256;
+  static constexpr int tile_bytes = NT * 128 * 4;            // logits of a tile, [token][128]
+  static constexpr int list_bytes = NT * 32 * 8;             // sorted lists, [token][32]
+  static constexpr int stages = (226 * 1024 - tile_bytes - list_bytes - 2048) / stage_bytes;
+  static constexpr int smem = stages * stage_bytes + tile_bytes + list_bytes + 1024 + 512;
   static constexpr int tmem_cols = 2 * NT < 32 ? 32 : 2 * NT;
 };
+
+// Barrier of the reducing warps; every one of them arrives, and all leave with the same answer.
+__device__ __forceinline__ bool stream_barrier(bool good) {
+  int all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.s32 p, %1, 0;\n\t"
+      "bar.red.and.pred q, 1, %2, p;\n\t"
+      "selp.b32 %0, 1, 0, q;\n\t}"
+      : "=r"(all)
+      : "r"(good ? 1 : 0), "n"(32 * kStreamWarps)
+      : "memory");
+  return all != 0;
+}
 
 template <int NT>
 __global__ void __launch_bounds__(kStreamThreads, 1)
 lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmH, const StreamParams p) {
   using C = StreamCfg<NT>;
   constexpr int S = C::stages;
+  static_assert(S >= 4 && 16 * S + 48 <= 512, "stages");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
-  const uint32_t bars = base + S * C::stage_bytes;
+  float* tile_z = reinterpret_cast<float*>(gen + S * C::stage_bytes);
+  float2* list = reinterpret_cast<float2*>(gen + S * C::stage_bytes + C::tile_bytes);
+  constexpr int kBarAt = S * C::stage_bytes + C::tile_bytes + C::list_bytes;
+  const uint32_t bars = base + kBarAt;
   const uint32_t full0 = bars, empty0 = bars + 8 * S, tfull0 = bars + 16 * S, tempty0 = tfull0 + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + S * C::stage_bytes + 16 * S + 32);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + kBarAt + 16 * S + 32);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
+  pdl_trigger();
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(tfull0 + 8 * b, 1); mbar_init(tempty0 + 8 * b, 4); }
+    for (int b = 0; b < 2; ++b) { mbar_init(tfull0 + 8 * b, 1); mbar_init(tempty0 + 8 * b, kStreamWarps); }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -363,32 +466,96 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       }
     }
   } else {
-    const int quarter = warp & 3;
+    const int quarter = warp & 3, half = (warp - 2) >> 2, w = warp - 2;
+    constexpr int PER = NT / kStreamWarps;               // tokens w, w + 8, .. of this warp; lane k < PER keeps the k-th's state
+    float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f, zt = -CUDART_INF_F, thr = -CUDART_INF_F;
+    const int my_t = w + kStreamWarps * lane;
+    const int32_t my_y = lane < PER && my_t < p.T && p.y ? p.y[my_t] : -1;
+    for (int k = 0; k < PER; ++k)
+      list[(w + kStreamWarps * k) * 32 + lane] = make_float2(-CUDART_INF_F, __int_as_float(0x7FFFFFFF));
+    __syncwarp();
     uint32_t n = 0;
     for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++n) {
       const uint32_t b = n & 1u;
       int good = 1;
       if (lane == 0) good = mbar_wait<32>(tfull0 + 8 * b, (n >> 1) & 1u, abort_flag, p.d_status) ? 1 : 0;
       good = __shfl_sync(0xffffffffu, good, 0);
-      if (!good) break;
       tc_fence_after();
-      const int r = quarter * 32 + lane;
-      const int64_t v = (int64_t)tile * p.tile_h + r;
-      const bool ok_row = r < p.tile_h && v < p.V;
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * NT;
+      if (good) {
+        constexpr int COLS = NT / 2 < 16 ? 16 : NT / 2;              // token columns per warp of a quarter
+        if (half * COLS < NT) {
 #pragma unroll 1
-      for (int c = 0; c < NT; c += 16) {
-        uint32_t x[16];
-        tmem_ld16(taddr + c, x);
-        if (ok_row) {
+          for (int c = half * COLS; c < (half + 1) * COLS; c += 16) {
+            uint32_t x[16];
+            tmem_ld16(taddr + c, x);
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (c + j < p.T) p.Z[(int64_t)(c + j) * p.ldz + v] = __uint_as_float(x[j]);
+            for (int j = 0; j < 16; ++j) tile_z[(c + j) * 128 + quarter * 32 + lane] = __uint_as_float(x[j]);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(tempty0 + 8 * b);
+      }
+      if (!stream_barrier(good != 0)) break;                          // the tile is in shared memory
+      const int v0 = tile * p.tile_h;
+      const int cols = p.V - v0 < p.tile_h ? p.V - v0 : p.tile_h;
+#pragma unroll 1
+      for (int k = 0; k < PER; ++k) {
+        const int t = w + kStreamWarps * k;
+        if (t >= p.T) break;
+        const float* z = tile_z + t * 128;
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = i * 32 + lane < cols ? z[i * 32 + lane] : -1.0e30f;
+        const int b32 = __float_as_int(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+        const int key = __reduce_max_sync(0xffffffffu, b32 ^ ((b32 >> 31) & 0x7FFFFFFF));   // floats in order as integers
+        const float mx = __int_as_float(key ^ ((key >> 31) & 0x7FFFFFFF));
+        const float mk = __shfl_sync(0xffffffffu, m2, k);
+        const float mn = fmaxf(fmaxf(mk, mx * p.sc2), -1.0e25f);
+        float s = 0.0f, u = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = fast_exp2(fmaf(x[i], p.sc2, -mn));
+          s += e;
+          u = fmaf(e, x[i], u);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          s += __shfl_xor_sync(0xffffffffu, s, o);
+          u += __shfl_xor_sync(0xffffffffu, u, o);
+        }
+        if (lane == k) {
+          const float down = fast_exp2(mk - mn);
+          l = fmaf(l, down, s);
+          ez = fmaf(ez, down, u);
+          m2 = mn;
+          if (my_y >= v0 && my_y < v0 + cols) zt = z[my_y - v0];
+        }
+        if (p.K > 0 && mx > __shfl_sync(0xffffffffu, thr, k)) {
+          float2* mine = list + t * 32 + lane;
+          WarpTop top;
+          const float2 c = *mine;
+          top.v = c.x; top.id = __float_as_int(c.y); top.aux = 0;
+          top.last_v = __shfl_sync(0xffffffffu, top.v, p.K - 1);
+          top.last_id = __shfl_sync(0xffffffffu, top.id, p.K - 1);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            top.offer(i * 32 + lane < cols ? x[i] : -CUDART_INF_F, v0 + i * 32 + lane, 0, p.K, lane);
+          *mine = make_float2(top.v, __int_as_float(top.id));
+          if (lane == k) thr = top.last_v;
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cta(tempty0 + 8 * b);
+      if (!stream_barrier(true)) break;                               // the tile has been read
+    }
+    if (lane < PER && my_t < p.T) {
+      FwdPartial pt;
+      pt.m2 = m2; pt.l = l; pt.zt = zt; pt.pad = ez;
+      p.partials[(int64_t)my_t * gridDim.x + blockIdx.x] = pt;
+    }
+    for (int k = 0; k < PER; ++k) {
+      const int t = w + kStreamWarps * k;
+      if (t < p.T && lane < p.K) p.tops[((int64_t)t * gridDim.x + blockIdx.x) * p.K + lane] = list[t * 32 + lane];
     }
   }
 
@@ -403,8 +570,19 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(C::tmem_cols) : "memory");
 }
 
+// CTAs of lp_stream_kernel, and rows of its vocabulary tiles.
+void stream_shape(int32_t V, int* grid, int* tile_h) {
+  const int sms = sm_count();
+  const int64_t rounds = ceil_div(V, (int64_t)128 * sms);
+  int h = (int)ceil_div(V, rounds * sms);
+  if (h < 8) h = 8;
+  const int64_t tiles = ceil_div(V, h);
+  *tile_h = h;
+  *grid = (int)(tiles < sms ? tiles : sms);
+}
+
 template <int NT>
-cudaError_t launch_stream_t(const LpFwd& a, float* Z, int64_t ldz, cudaStream_t st) {
+cudaError_t launch_stream_t(const LpFwd& a, FwdPartial* partials, float2* tops, cudaStream_t st) {
   using C = StreamCfg<NT>;
   static std::atomic<int> ready[64];
   int dev = 0;
@@ -416,32 +594,46 @@ cudaError_t launch_stream_t(const LpFwd& a, float* Z, int64_t ldz, cudaStream_t 
     if (e != cudaSuccess) return e;
     ready[dev].store(1, std::memory_order_release);
   }
-  const int sms = sm_count();
-  const int64_t rounds = ceil_div(a.V, (int64_t)128 * sms);
-  int h = (int)ceil_div(a.V, rounds * sms);
-  if (h < 8) h = 8;
-  CUtensorMap mW, mH;
-  if (!make_map(&mW, a.W, a.d, a.V, a.d, (uint32_t)h) || !make_map(&mH, a.H, a.d, a.T, a.ldh, NT))
-    return cudaErrorInvalidValue;
   StreamParams p{};
-  p.tile_h = h;
-  p.tiles = (int)ceil_div(a.V, h);
+  int grid = 0;
+  stream_shape(a.V, &grid, &p.tile_h);
+  CUtensorMap mW, mH;
+  if (!make_map(&mW, a.W, a.d, a.V, a.d, (uint32_t)p.tile_h) || !make_map(&mH, a.H, a.d, a.T, a.ldh, NT))
+    return cudaErrorInvalidValue;
+  p.tiles = (int)ceil_div(a.V, p.tile_h);
   p.k_blocks = (int)ceil_div(a.d, 64);
   p.T = (int)a.T;
+  p.K = a.top_k;
   p.V = a.V;
-  p.Z = Z;
-  p.ldz = ldz;
+  p.sc2 = kLog2e * a.inv_t;
+  p.y = a.y;
+  p.partials = partials;
+  p.tops = tops;
   p.d_status = a.d_status;
-  const int grid = p.tiles < sms ? p.tiles : sms;
   lp_stream_kernel<NT><<<grid, kStreamThreads, C::smem, st>>>(mW, mH, p);
   return cudaGetLastError();
 }
 
-cudaError_t launch_stream(const LpFwd& a, float* Z, int64_t ldz, cudaStream_t st) {
-  if (a.T <= 16) return launch_stream_t<16>(a, Z, ldz, st);
-  if (a.T <= 32) return launch_stream_t<32>(a, Z, ldz, st);
-  if (a.T <= 64) return launch_stream_t<64>(a, Z, ldz, st);
-  return launch_stream_t<128>(a, Z, ldz, st);
+cudaError_t launch_stream(const LpFwd& a, FwdPartial* partials, float2* tops, cudaStream_t st) {
+  if (a.T <= 16) return launch_stream_t<16>(a, partials, tops, st);
+  if (a.T <= 32) return launch_stream_t<32>(a, partials, tops, st);
+  if (a.T <= 64) return launch_stream_t<64>(a, partials, tops, st);
+  return launch_stream_t<128>(a, partials, tops, st);
+}
+
+// A launch whose kernel begins with pdl_wait(): it may come up while the launch before it still runs.
+template <typename... P, typename... A>
+cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, dim3 block, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
 }
 
 // ---------------------------------------------------------------------------
@@ -504,6 +696,7 @@ sgemm_kernel(const SgemmParams p) {
   const int64_t k_begin = (int64_t)blockIdx.z * p.k_per;
   const int64_t k_end = k_begin + p.k_per < p.K ? k_begin + p.k_per : p.K;
   float acc[4 * R][4 * R] = {};
+  pdl_trigger();
   float4 ra[LOADS], rb[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
@@ -663,14 +856,21 @@ void row_segments(int64_t rows, int32_t V, int* nseg, int* part) {
   *nseg = (int)ceil_div(V, kRowWarps * pt);
 }
 
-struct LpFwdWs { size_t z, partials, tops, cand, progress, split, total; int64_t chunk, ldz; bool stored; };
+enum : int { LP_STREAM = 0, LP_TILES = 1, LP_F32 = 2 };
+struct LpFwdWs { size_t z, partials, tops, cand, progress, total; int64_t chunk, ldz; int path; };
 
 LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype) {
   LpFwdWs L{};
-  L.stored = dtype == SPO_DTYPE_F32 || T <= kLpStreamRows;
+  L.path = dtype == SPO_DTYPE_F32 ? LP_F32 : T <= kLpStreamRows ? LP_STREAM : LP_TILES;
   size_t off = 0;
-  if (L.stored) {
-    L.chunk = dtype == SPO_DTYPE_F32 ? f32_chunk_rows(T, V) : (T > 0 ? T : 1);
+  if (L.path == LP_STREAM) {
+    L.chunk = T > 0 ? T : 1;
+    int grid, h;
+    stream_shape(V, &grid, &h);
+    L.partials = off; off = align_up(off + sizeof(FwdPartial) * (size_t)L.chunk * grid, 256);
+    L.tops = off;     off = align_up(off + sizeof(float2) * (size_t)L.chunk * grid * (top_k > 0 ? top_k : 1), 256);
+  } else if (L.path == LP_F32) {
+    L.chunk = f32_chunk_rows(T, V);
     L.ldz = pad4(V);
     // segments per row grow as the rows get fewer: the last, shorter chunk is covered by the bound below
     const int64_t segs = L.chunk * ceil_div(V, kRowWarps * 256) < (int64_t)sm_count() * 4 + L.chunk * (1 + ceil_div(V, kRowWarps * 4096))
@@ -755,35 +955,42 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
   cudaError_t e;
   for (int64_t t0 = 0; t0 < a.T; t0 += L.chunk) {
     const int64_t rows = a.T - t0 < L.chunk ? a.T - t0 : L.chunk;
-    const unsigned merge_blocks = (unsigned)ceil_div(rows, 4);
-    if (!L.stored) {
+    if (L.path == LP_TILES) {
       float* cand = reinterpret_cast<float*>(ws + L.cand);
       e = launch_lp_fwd_bf16(a, t0, rows, partials, cand, tops, reinterpret_cast<uint32_t*>(ws + L.progress), st);
+      if (e == cudaSuccess)
+        e = launch_dependent(lp_merge_kernel<true, 1>, dim3((unsigned)ceil_div(rows, 4)), dim3(128), st, partials,
+                             lp_fwd_lists(rows, a.d, a.V), rows, tops, cand, lp_list_len(a.top_k), rows, t0, o);
       if (e != cudaSuccess) return e;
-      lp_merge_kernel<true><<<merge_blocks, 128, 0, st>>>(partials, lp_fwd_lists(rows, a.d, a.V), rows, tops, cand,
-                                                          lp_list_len(a.top_k), rows, t0, o);
-      if ((e = cudaGetLastError()) != cudaSuccess) return e;
       continue;
     }
-    float* Z = reinterpret_cast<float*>(ws + L.z);
-    if (a.dtype == SPO_DTYPE_F32) {
+    int lists;
+    if (L.path == LP_STREAM) {
+      int h;
+      stream_shape(a.V, &lists, &h);
+      e = launch_stream(a, partials, tops, st);
+    } else {
+      float* Z = reinterpret_cast<float*>(ws + L.z);
       SgemmParams p{};
       p.A = (const float*)a.H + t0 * a.ldh; p.lda = a.ldh; p.M = rows;
       p.B = (const float*)a.W; p.ldb = a.d; p.N = a.V;
       p.K = a.d;
       p.C = Z; p.ldc = L.ldz;
-      e = launch_sgemm<true, true>(p, nullptr, st);
-    } else {
-      e = launch_stream(a, Z, L.ldz, st);
+      if ((e = launch_sgemm<true, true>(p, nullptr, st)) != cudaSuccess) return e;
+      int part;
+      row_segments(rows, a.V, &lists, &part);
+      e = launch_dependent(lp_rows_kernel, dim3((unsigned)(rows * lists)), dim3(32 * kRowWarps), st, Z, L.ldz, a.V, lists, part,
+                           a.y ? a.y + t0 : nullptr, kLog2e * a.inv_t, a.top_k, partials, tops);
     }
     if (e != cudaSuccess) return e;
-    int nseg, part;
-    row_segments(rows, a.V, &nseg, &part);
-    lp_rows_kernel<<<(unsigned)(rows * nseg), 32 * kRowWarps, 0, st>>>(Z, L.ldz, a.V, nseg, part, a.y ? a.y + t0 : nullptr,
-                                                                       kLog2e * a.inv_t, a.top_k, partials, tops);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
-    lp_merge_kernel<false><<<merge_blocks, 128, 0, st>>>(partials, nseg, 0, tops, nullptr, a.top_k, rows, t0, o);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    // several warps a row where a row has many lists, one where it has few
+    if (lists > 8)
+      e = launch_dependent(lp_merge_kernel<false, 8>, dim3((unsigned)rows), dim3(256), st, partials, lists, (int64_t)0, tops,
+                           nullptr, a.top_k, rows, t0, o);
+    else
+      e = launch_dependent(lp_merge_kernel<false, 1>, dim3((unsigned)ceil_div(rows, 4)), dim3(128), st, partials, lists, (int64_t)0,
+                           tops, nullptr, a.top_k, rows, t0, o);
+    if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
