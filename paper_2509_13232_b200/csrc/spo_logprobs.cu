@@ -36,8 +36,10 @@ __device__ __forceinline__ void flag(int32_t* d_status, int32_t bit) {
 
 // ---------------------------------------------------------------------------
 // K largest values of a stream, kept by one warp: lane i holds the i-th largest (value descending,
-// equal values by ascending id).  An insertion is a ballot, a population count and two shuffles.
+// equal values by ascending id).  An insertion is a ballot, a population count and a few shuffles.
 // ---------------------------------------------------------------------------
+// AUX: entries carry one more integer.
+template <bool AUX>
 struct WarpTop {
   float v;
   int id, aux;
@@ -51,7 +53,7 @@ struct WarpTop {
     const unsigned before = __ballot_sync(0xffffffffu, lane < K && (v > x || (v == x && id < xi)));
     const int pos = __popc(before);
     const float uv = __shfl_up_sync(0xffffffffu, v, 1);
-    const int ui = __shfl_up_sync(0xffffffffu, id, 1), ua = __shfl_up_sync(0xffffffffu, aux, 1);
+    const int ui = __shfl_up_sync(0xffffffffu, id, 1), ua = AUX ? __shfl_up_sync(0xffffffffu, aux, 1) : 0;
     if (lane == pos) { v = x; id = xi; aux = xa; }
     else if (lane > pos) { v = uv; id = ui; aux = ua; }
     last_v = __shfl_sync(0xffffffffu, v, K - 1);
@@ -62,7 +64,7 @@ struct WarpTop {
   // the 32 largest of both and form a bitonic sequence, which five compare-exchanges sort.
   __device__ __forceinline__ void merge(float x, int xi, int xa, int K, int lane) {
     const float rx = __shfl_sync(0xffffffffu, x, 31 - lane);
-    const int ri = __shfl_sync(0xffffffffu, xi, 31 - lane), ra = __shfl_sync(0xffffffffu, xa, 31 - lane);
+    const int ri = __shfl_sync(0xffffffffu, xi, 31 - lane), ra = AUX ? __shfl_sync(0xffffffffu, xa, 31 - lane) : 0;
     if (better(rx, ri, v, id)) { v = rx; id = ri; aux = ra; }
 #pragma unroll
     for (int s = 16; s > 0; s >>= 1) exchange(v, id, aux, s, (lane & s) == 0);
@@ -72,7 +74,7 @@ struct WarpTop {
   }
   static __device__ __forceinline__ void exchange(float& x, int& xi, int& xa, int s, bool keep_larger) {
     const float px = __shfl_xor_sync(0xffffffffu, x, s);
-    const int pi = __shfl_xor_sync(0xffffffffu, xi, s), pa = __shfl_xor_sync(0xffffffffu, xa, s);
+    const int pi = __shfl_xor_sync(0xffffffffu, xi, s), pa = AUX ? __shfl_xor_sync(0xffffffffu, xa, s) : 0;
     if (keep_larger ? better(px, pi, x, xi) : better(x, xi, px, pi)) { x = px; xi = pi; xa = pa; }
   }
   // One candidate per lane.  A few are inserted one after the other (some 70 clocks each); many are sorted
@@ -93,7 +95,7 @@ struct WarpTop {
       const int src = __ffs(todo) - 1;
       todo &= todo - 1;
       const float bx = __shfl_sync(0xffffffffu, x, src);
-      const int bi = __shfl_sync(0xffffffffu, xi, src), ba = __shfl_sync(0xffffffffu, xa, src);
+      const int bi = __shfl_sync(0xffffffffu, xi, src), ba = AUX ? __shfl_sync(0xffffffffu, xa, src) : 0;
       if (beats(bx, bi)) insert(bx, bi, ba, K, lane);
     }
   }
@@ -121,16 +123,105 @@ __device__ __forceinline__ void warp_join_stats(float& m2, float& l, float& ez) 
   }
 }
 
+// What every path ends with.
+struct LpOut {
+  const int32_t* y;
+  const uint8_t* mask;
+  float *logp, *lse, *entropy;
+  int32_t* top_ids;
+  float* top_logp;
+  float inv_t;
+  int K;
+  int32_t V;
+  int32_t* d_status;
+};
+
+// Outputs of token t from its joined statistics; the whole warp calls it, lane i < K with the i-th alternative.
+__device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, float m2, float l, float ez, float zt, bool odd, float top_v,
+                                          int top_id, int lane) {
+  float lse = (m2 + log2f(l)) * kLn2;
+  if (odd) lse = CUDART_NAN_F;
+  const bool on = o.mask == nullptr || o.mask[t] != 0;
+  if (lane == 0) {
+    if (on && !(fabsf(lse) < CUDART_INF_F)) flag(o.d_status, SPO_DEV_NONFINITE);
+    if (o.logp) {
+      const int32_t yt = o.y[t];
+      float lp = fmaf(zt, o.inv_t, -lse);
+      if (yt < 0 || yt >= o.V) {
+        lp = -CUDART_INF_F;
+        if (on) flag(o.d_status, SPO_DEV_ID_OUT_OF_RANGE);
+      }
+      o.logp[t] = on ? lp : 0.0f;
+    }
+    o.lse[t] = on ? lse : 0.0f;
+    if (o.entropy) o.entropy[t] = on ? lse - o.inv_t * (ez / l) : 0.0f;
+  }
+  if (lane < o.K) {
+    const bool found = top_v > -CUDART_INF_F;
+    o.top_ids[t * o.K + lane] = on && found ? top_id : -1;
+    o.top_logp[t * o.K + lane] = !on ? 0.0f : found ? fmaf(top_v, o.inv_t, -lse) : -CUDART_INF_F;
+  }
+}
+
+// A float as an integer of the same order (and back: the mapping is its own inverse).
+__device__ __forceinline__ int order_key(int b) { return b ^ ((b >> 31) & 0x7FFFFFFF); }
+
+// The K largest entries of sorted lists in shared memory ([list][K] of (value, id), empty entries -inf), one per lane: K
+// rounds over the lists' heads, of which a lane holds up to five.
+constexpr int kMergeLists = 160;
+__device__ __forceinline__ void merge_heads(const float2* s, int lists, int K, int lane, float* v_out, int* id_out) {
+  constexpr int H = kMergeLists / 32;
+  float hv[H];
+  int hi[H], hp[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    const int q = lane + 32 * h;
+    hp[h] = 0;
+    hv[h] = -CUDART_INF_F;
+    hi[h] = 0x7FFFFFFF;
+    if (q < lists) { const float2 c = s[q * K]; hv[h] = c.x; hi[h] = __float_as_int(c.y); }
+  }
+  float v = -CUDART_INF_F;
+  int id = 0x7FFFFFFF;
+  for (int k = 0; k < K; ++k) {
+    float bv = hv[0];
+    int bi = hi[0], bh = 0;
+#pragma unroll
+    for (int h = 1; h < H; ++h)
+      if (hv[h] > bv || (hv[h] == bv && hi[h] < bi)) { bv = hv[h]; bi = hi[h]; bh = h; }
+    const int key = order_key(__float_as_int(bv + 0.0f));            // (-0 counts as 0)
+    const int best = __reduce_max_sync(0xffffffffu, key);
+    const int best_id = __reduce_min_sync(0xffffffffu, key == best ? bi : 0x7FFFFFFF);
+    if (best_id == 0x7FFFFFFF) break;                                // the lists are exhausted
+    if (lane == k) { v = __int_as_float(order_key(best)); id = best_id; }
+    if (key == best && bi == best_id) {                              // ids are distinct: one lane
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (h == bh) {
+          const int at = ++hp[h];
+          hv[h] = -CUDART_INF_F;
+          hi[h] = 0x7FFFFFFF;
+          if (at < K) { const float2 c = s[(lane + 32 * h) * K + at]; hv[h] = c.x; hi[h] = __float_as_int(c.y); }
+        }
+    }
+  }
+  *v_out = v;
+  *id_out = id;
+}
+
 // ---------------------------------------------------------------------------
 // Statistics and alternatives of stored logit rows.  Block = (row, segment of the vocabulary); each
-// warp takes a contiguous part of `part` columns (a multiple of 256), the block joins its warps and writes one
-// partial and one sorted list.  Reads every logit once; bound by L2 or HBM.
+// warp takes a contiguous part of `part` columns, the block joins its warps and writes one partial and one
+// sorted list, or, where it has the whole row, the outputs.  Reads every logit once; bound by L2 or HBM.
 // ---------------------------------------------------------------------------
 constexpr int kRowWarps = 8;
 
 __global__ void __launch_bounds__(32 * kRowWarps)
-lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int32_t V, int nseg, int part, const int32_t* __restrict__ y,
-               float sc2, int K, FwdPartial* __restrict__ partials, float2* __restrict__ cand) {
+lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int64_t t0, const LpOut o,
+               FwdPartial* __restrict__ partials, float2* __restrict__ cand) {
+  const int32_t V = o.V;
+  const int K = o.K;
+  const float sc2 = kLog2e * o.inv_t;
   pdl_trigger();
   pdl_wait();
   const int64_t row = blockIdx.x / nseg;
@@ -140,7 +231,7 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int32_t V, int nseg, in
   const int64_t begin = ((int64_t)seg * kRowWarps + warp) * part;
   const int64_t end = begin + part < V ? begin + part : V;
   float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f;
-  WarpTop top;
+  WarpTop<false> top;
   top.init();
   for (int64_t c0 = begin; c0 < end; c0 += 256) {
     float x[8];
@@ -182,22 +273,25 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int32_t V, int nseg, in
   m2 = lane < kRowWarps ? s_m[lane] : -CUDART_INF_F;
   l = lane < kRowWarps ? s_l[lane] : 0.0f;
   ez = lane < kRowWarps ? s_e[lane] : 0.0f;
+  const bool odd = __any_sync(0xffffffffu, !(l >= 0.0f));            // a NaN, which fmaxf drops
   warp_join_stats(m2, l, ez);
+  if (odd) l = CUDART_NAN_F;
+  const int64_t lo = (int64_t)seg * kRowWarps * part, hi = lo + (int64_t)kRowWarps * part;
+  const int32_t yt = o.y ? o.y[t0 + row] : -1;
+  const float zt = yt >= lo && yt < hi && yt < V ? z[yt] : -CUDART_INF_F;
+  float tv = -CUDART_INF_F;
+  int ti = 0x7FFFFFFF;
+  if (K > 0) merge_heads(s_top, kRowWarps, K, lane, &tv, &ti);
+  if (nseg == 1) {
+    lp_finish(o, t0 + row, m2, l, ez, zt, odd, tv, ti, lane);
+    return;
+  }
   if (lane == 0) {
     FwdPartial pt;
-    pt.m2 = m2; pt.l = l; pt.pad = ez; pt.zt = -CUDART_INF_F;
-    const int64_t lo = (int64_t)seg * kRowWarps * part, hi = lo + (int64_t)kRowWarps * part;
-    const int32_t yt = y ? y[row] : -1;
-    if (yt >= lo && yt < hi && yt < V) pt.zt = z[yt];
+    pt.m2 = m2; pt.l = l; pt.pad = ez; pt.zt = zt;
     partials[row * nseg + seg] = pt;
   }
-  if (K > 0) {
-    for (int w = 1; w < kRowWarps; ++w) {
-      const float2 c = lane < K ? s_top[w * K + lane] : make_float2(-CUDART_INF_F, __int_as_float(0x7FFFFFFF));
-      if (__any_sync(0xffffffffu, top.beats(c.x, __float_as_int(c.y)))) top.merge(c.x, __float_as_int(c.y), 0, K, lane);
-    }
-    if (lane < K) cand[(row * nseg + seg) * K + lane] = make_float2(top.v, __int_as_float(top.id));
-  }
+  if (lane < K) cand[(row * nseg + seg) * K + lane] = make_float2(tv, __int_as_float(ti));
 }
 
 // ---------------------------------------------------------------------------
@@ -206,23 +300,11 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int32_t V, int nseg, in
 // slot) whose 32 logits are stored in `cand`; first the K groups of largest maximum, then the K largest logits
 // in them.  Otherwise the lists hold the logits themselves, (value, id), sorted.
 // ---------------------------------------------------------------------------
-struct LpOut {
-  const int32_t* y;
-  const uint8_t* mask;
-  float *logp, *lse, *entropy;
-  int32_t* top_ids;
-  float* top_logp;
-  float inv_t;
-  int K;
-  int32_t V;
-  int32_t* d_status;
-};
-
 template <bool GROUPS, int WARPS>
 __global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS)
 lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part_ld, const float2* __restrict__ tops,
                 const float* __restrict__ cand, int list_len, int64_t rows, int64_t t0, const LpOut o) {
-  static_assert(WARPS == 1 || !GROUPS, "column groups are merged by one warp");
+  static_assert((WARPS == 1) == GROUPS, "column groups are merged by one warp, plain lists by several");
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5;
@@ -230,98 +312,54 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part
   if (row >= rows) return;
   const int64_t t = t0 + row;
   const int K = o.K;
+  __shared__ float2 s_lists[GROUPS ? 1 : kMergeLists * kMaxTopK];
+  if (!GROUPS) {                                    // all lists into shared memory
+    for (int i = threadIdx.x; i < lists * K; i += 32 * WARPS) s_lists[i] = tops[row * lists * K + i];
+    __syncthreads();
+    if (warp != 0) return;
+  }
   // partial of list s: [s][part_ld] (GROUPS) or [row][lists]
   auto at = [&](int s) { return GROUPS ? (int64_t)s * part_ld + row : row * lists + s; };
   float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f, zt = -CUDART_INF_F;
   bool odd = false;                                 // a partial that is NaN: fmaxf would drop it
-  for (int s = lane + 32 * warp; s < lists; s += 32 * WARPS) {
+#pragma unroll 4
+  for (int s = lane; s < lists; s += 32) {
     const FwdPartial p = partials[at(s)];
     odd |= !(p.l >= 0.0f);
     zt = p.zt > -CUDART_INF_F || p.zt != p.zt ? p.zt : zt;   // at most one list has the target
     join_stats(m2, l, ez, p.m2, p.l, p.pad);
   }
-  WarpTop top;
-  top.init();
-  if (K > 0) {
-    if (GROUPS) {
-      const int n = lists * list_len;
-      for (int i0 = 0; i0 < n; i0 += 32) {
-        const int i = i0 + lane;
-        float x = -CUDART_INF_F;
-        int id = 0x7FFFFFFF, aux = 0;
-        if (i < n) {
-          const int s = i / list_len, k = i - s * list_len;
-          const float2 c = tops[at(s) * list_len + k];
-          x = c.x;
-          id = (int)(__float_as_uint(c.y) >> 8);
-          aux = s * list_len + (int)(__float_as_uint(c.y) & 255u);
-        }
-        top.offer(x, id, aux, K, lane);
-      }
-    } else {
-      const float2 none = make_float2(-CUDART_INF_F, __int_as_float(0x7FFFFFFF));
-      for (int s0 = warp; s0 < lists; s0 += 4 * WARPS) {          // four lists in flight
-        float2 c[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          c[i] = lane < K && s0 + i * WARPS < lists ? tops[at(s0 + i * WARPS) * K + lane] : none;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (__any_sync(0xffffffffu, top.beats(c[i].x, __float_as_int(c[i].y)))) top.merge(c[i].x, __float_as_int(c[i].y), 0, K, lane);
-      }
-    }
-  }
   warp_join_stats(m2, l, ez);
   odd = __any_sync(0xffffffffu, odd);
-  {
-    const unsigned has = __ballot_sync(0xffffffffu, zt > -CUDART_INF_F || zt != zt);
-    zt = has ? __shfl_sync(0xffffffffu, zt, __ffs(has) - 1) : -CUDART_INF_F;
-  }
-  if (WARPS > 1) {                                  // warp 0 joins the others' results
-    __shared__ float4 s_stat[WARPS];
-    __shared__ int s_odd[WARPS];
-    __shared__ float2 s_top[WARPS][32];
-    if (lane == 0) { s_stat[warp] = make_float4(m2, l, ez, zt); s_odd[warp] = odd; }
-    s_top[warp][lane] = make_float2(top.v, __int_as_float(top.id));
-    __syncthreads();
-    if (warp != 0) return;
-    m2 = -CUDART_INF_F; l = 0.0f; ez = 0.0f;
-    float zw = -CUDART_INF_F;
-    if (lane < WARPS) {
-      const float4 q = s_stat[lane];
-      m2 = q.x; l = q.y; ez = q.z; zw = q.w;
-      odd |= s_odd[lane] != 0;
-    }
-    warp_join_stats(m2, l, ez);
-    odd = __any_sync(0xffffffffu, odd);
-    const unsigned has = __ballot_sync(0xffffffffu, zw > -CUDART_INF_F || zw != zw);
-    zt = has ? __shfl_sync(0xffffffffu, zw, __ffs(has) - 1) : -CUDART_INF_F;
-    if (K > 0)
-      for (int w = 1; w < WARPS; ++w) {
-        const float2 c = s_top[w][lane];
-        if (__any_sync(0xffffffffu, top.beats(c.x, __float_as_int(c.y)))) top.merge(c.x, __float_as_int(c.y), 0, K, lane);
+  const unsigned has = __ballot_sync(0xffffffffu, zt > -CUDART_INF_F || zt != zt);
+  zt = has ? __shfl_sync(0xffffffffu, zt, __ffs(has) - 1) : -CUDART_INF_F;
+  float tv = -CUDART_INF_F;
+  int ti = 0x7FFFFFFF;
+  if (!GROUPS) {
+    if (K > 0) merge_heads(s_lists, lists, K, lane, &tv, &ti);
+  } else if (K > 0) {
+    WarpTop<true> g;
+    g.init();
+    const int n = lists * list_len;
+    for (int i0 = 0; i0 < n; i0 += 128) {           // four accesses in flight
+      float2 c[4];
+      int ax[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + 32 * u + lane;
+        c[u] = make_float2(-CUDART_INF_F, __uint_as_float(0xFFFFFF00u));
+        ax[u] = 0;
+        if (i < n) {
+          const int s = i / list_len, k = i - s * list_len;
+          c[u] = tops[at(s) * list_len + k];
+          ax[u] = s * list_len;
+        }
       }
-  }
-  float lse = (m2 + log2f(l)) * kLn2;
-  if (odd) lse = CUDART_NAN_F;
-  const bool on = o.mask == nullptr || o.mask[t] != 0;
-  if (lane == 0) {
-    if (on && !(fabsf(lse) < CUDART_INF_F)) flag(o.d_status, SPO_DEV_NONFINITE);
-    if (o.logp) {
-      const int32_t yt = o.y[t];
-      float lp = fmaf(zt, o.inv_t, -lse);
-      if (yt < 0 || yt >= o.V) {
-        lp = -CUDART_INF_F;
-        if (on) flag(o.d_status, SPO_DEV_ID_OUT_OF_RANGE);
-      }
-      o.logp[t] = on ? lp : 0.0f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        g.offer(c[u].x, (int)(__float_as_uint(c[u].y) >> 8), ax[u] + (int)(__float_as_uint(c[u].y) & 255u), K, lane);
     }
-    o.lse[t] = on ? lse : 0.0f;
-    if (o.entropy) o.entropy[t] = on ? lse - o.inv_t * (ez / l) : 0.0f;
-  }
-  if (K == 0) return;
-  if (GROUPS) {
-    const WarpTop g = top;
+    WarpTop<false> top;
     top.init();
     for (int k = 0; k < K; ++k) {
       const float gm = __shfl_sync(0xffffffffu, g.v, k);
@@ -332,12 +370,10 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part
       const float x = cand[(at(s) * list_len + slot) * 32 + lane];
       top.offer(id < o.V ? x : -CUDART_INF_F, id, 0, K, lane);
     }
+    tv = top.v;
+    ti = top.id;
   }
-  if (lane < K) {
-    const bool found = top.v > -CUDART_INF_F;
-    o.top_ids[t * K + lane] = on && found ? top.id : -1;
-    o.top_logp[t * K + lane] = !on ? 0.0f : found ? fmaf(top.v, o.inv_t, -lse) : -CUDART_INF_F;
-  }
+  lp_finish(o, t, m2, l, ez, zt, odd, tv, ti, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -509,8 +545,7 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = i * 32 + lane < cols ? z[i * 32 + lane] : -1.0e30f;
         const int b32 = __float_as_int(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-        const int key = __reduce_max_sync(0xffffffffu, b32 ^ ((b32 >> 31) & 0x7FFFFFFF));   // floats in order as integers
-        const float mx = __int_as_float(key ^ ((key >> 31) & 0x7FFFFFFF));
+        const float mx = __int_as_float(order_key(__reduce_max_sync(0xffffffffu, order_key(b32))));
         const float mk = __shfl_sync(0xffffffffu, m2, k);
         const float mn = fmaxf(fmaxf(mk, mx * p.sc2), -1.0e25f);
         float s = 0.0f, u = 0.0f;
@@ -534,7 +569,7 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
         }
         if (p.K > 0 && mx > __shfl_sync(0xffffffffu, thr, k)) {
           float2* mine = list + t * 32 + lane;
-          WarpTop top;
+          WarpTop<false> top;
           const float2 c = *mine;
           top.v = c.x; top.id = __float_as_int(c.y); top.aux = 0;
           top.last_v = __shfl_sync(0xffffffffu, top.v, p.K - 1);
@@ -572,7 +607,7 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 
 // CTAs of lp_stream_kernel, and rows of its vocabulary tiles.
 void stream_shape(int32_t V, int* grid, int* tile_h) {
-  const int sms = sm_count();
+  const int sms = sm_count() < kMergeLists ? sm_count() : kMergeLists;
   const int64_t rounds = ceil_div(V, (int64_t)128 * sms);
   int h = (int)ceil_div(V, rounds * sms);
   if (h < 8) h = 8;
@@ -847,11 +882,14 @@ int64_t f32_chunk_rows(int64_t T, int32_t V) {
   return rows < T ? rows : (T > 0 ? T : 1);
 }
 
-// Segments of the vocabulary a stored row is reduced in: enough blocks to fill the GPU when the rows are few.
+// Segments of the vocabulary a stored row is reduced in: enough blocks to fill the GPU when the rows are few, at most as
+// many as one block merges; a warp's part is a multiple of 32 columns.
 void row_segments(int64_t rows, int32_t V, int* nseg, int* part) {
-  const int64_t want = ceil_div((int64_t)sm_count() * 4, rows);      // segments per row
-  int64_t pt = ceil_div(ceil_div(V, kRowWarps * want), 256) * 256;
-  if (pt > 4096) pt = 4096;
+  int64_t want = ceil_div((int64_t)sm_count() * 4, rows);            // segments per row
+  if (want > kMergeLists) want = kMergeLists;
+  int64_t pt = ceil_div(ceil_div(V, kRowWarps * want), 32) * 32;
+  if (want > 1 && pt < 256) pt = 256;                                // no shorter than one step of the loop
+  if (pt > 4096 && ceil_div(V, kRowWarps * 4096) <= kMergeLists) pt = 4096;
   *part = (int)pt;
   *nseg = (int)ceil_div(V, kRowWarps * pt);
 }
@@ -872,10 +910,8 @@ LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype)
   } else if (L.path == LP_F32) {
     L.chunk = f32_chunk_rows(T, V);
     L.ldz = pad4(V);
-    // segments per row grow as the rows get fewer: the last, shorter chunk is covered by the bound below
-    const int64_t segs = L.chunk * ceil_div(V, kRowWarps * 256) < (int64_t)sm_count() * 4 + L.chunk * (1 + ceil_div(V, kRowWarps * 4096))
-                             ? L.chunk * ceil_div(V, kRowWarps * 256)
-                             : (int64_t)sm_count() * 4 + L.chunk * (1 + ceil_div(V, kRowWarps * 4096));
+    // rows x segments: `want` segments a row come to at most 4 SMs' worth + rows, longer rows to one per 32 k columns
+    const int64_t segs = (int64_t)sm_count() * 4 + L.chunk * (1 + ceil_div(V, kRowWarps * 4096));
     L.z = off;        off = align_up(off + (size_t)L.chunk * L.ldz * 4, 256);
     L.partials = off; off = align_up(off + sizeof(FwdPartial) * (size_t)segs, 256);
     L.tops = off;     off = align_up(off + sizeof(float2) * (size_t)segs * (top_k > 0 ? top_k : 1), 256);
@@ -979,17 +1015,13 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
       if ((e = launch_sgemm<true, true>(p, nullptr, st)) != cudaSuccess) return e;
       int part;
       row_segments(rows, a.V, &lists, &part);
-      e = launch_dependent(lp_rows_kernel, dim3((unsigned)(rows * lists)), dim3(32 * kRowWarps), st, Z, L.ldz, a.V, lists, part,
-                           a.y ? a.y + t0 : nullptr, kLog2e * a.inv_t, a.top_k, partials, tops);
+      e = launch_dependent(lp_rows_kernel, dim3((unsigned)(rows * lists)), dim3(32 * kRowWarps), st, Z, L.ldz, lists, part, t0, o,
+                           partials, tops);
+      if (e == cudaSuccess && lists == 1) continue;
     }
     if (e != cudaSuccess) return e;
-    // several warps a row where a row has many lists, one where it has few
-    if (lists > 8)
-      e = launch_dependent(lp_merge_kernel<false, 8>, dim3((unsigned)rows), dim3(256), st, partials, lists, (int64_t)0, tops,
-                           nullptr, a.top_k, rows, t0, o);
-    else
-      e = launch_dependent(lp_merge_kernel<false, 1>, dim3((unsigned)ceil_div(rows, 4)), dim3(128), st, partials, lists, (int64_t)0,
-                           tops, nullptr, a.top_k, rows, t0, o);
+    e = launch_dependent(lp_merge_kernel<false, 8>, dim3((unsigned)rows), dim3(256), st, partials, lists, (int64_t)0, tops, nullptr,
+                         a.top_k, rows, t0, o);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
