@@ -531,7 +531,7 @@ int32_t spo_loss_stats(const float* logp, const float* logp_old, const uint8_t* 
  *   y           device in  [T] int32, optional together with logp (both NULL: no target)
  *   mask        device in  [T] uint8, optional: rows with mask 0 give logp = lse = entropy = 0, ids -1,
  *               top_logp 0, whatever their H and y hold (NaN included), and set no status bit
- *   inv_temperature   > 0, finite
+ *   inv_temperature   1e-4 .. 1e4
  *   top_k       0 .. SPO_MAX_TOP_K, at most V
  *   logp, lse   device out [T] fp32;  entropy  device out [T] fp32, optional
  *   top_ids     device out [T][top_k] int32;  top_logp  device out [T][top_k] fp32 (NULL when top_k = 0)

@@ -624,7 +624,7 @@ int32_t spo_loss_stats(const float* logp, const float* logp_old, const uint8_t* 
 static int32_t check_lp_shape(int32_t dtype, int64_t T, int64_t ldH, int32_t d, int32_t V, float inv_t) {
   if (dtype != SPO_DTYPE_F32 && dtype != SPO_DTYPE_BF16) return SPO_ERR_UNSUPPORTED_DTYPE;
   if (T < 0 || d < 1 || V < 1 || ldH < d) return SPO_ERR_INVALID_ARG;
-  if (!(inv_t > 0.0f) || !(inv_t < 3.0e38f)) return SPO_ERR_INVALID_ARG;
+  if (!(inv_t >= 1.0e-4f) || !(inv_t <= 1.0e4f)) return SPO_ERR_INVALID_ARG;
   if (T >= ((int64_t)1 << 31) - 256 || V >= (1 << 29)) return SPO_ERR_BAD_SHAPE;
   const int lanes = dtype == SPO_DTYPE_BF16 ? 8 : 4;               // elements per 16 bytes
   if ((d % (dtype == SPO_DTYPE_BF16 ? 64 : 4)) != 0 || (ldH % lanes) != 0) return SPO_ERR_BAD_SHAPE;

@@ -9,8 +9,9 @@
 //                    split in registers, column groups of largest maximum listed on the way;
 //                    lp_merge_kernel joins the splits.
 //   few bf16 rows    (up to kLpStreamRows) lp_stream_kernel: bound by reading W once, so W is the operand
-//                    with 128 rows a tile and the token rows are the narrow one; every CTA keeps statistics
-//                    and a sorted list per token row under the stream, lp_merge_kernel joins the CTAs'.
+//                    with 128 rows a tile and the token rows are the narrow one; every CTA keeps the token
+//                    rows' statistics under the stream, and where alternatives are wanted the logits of these few
+//                    rows go to scratch with the maximum of every 64; lp_pick_kernel finishes.
 //   fp32             sgemm_kernel into a chunk of scratch, lp_rows_kernel, lp_merge_kernel.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -29,77 +30,155 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.69314718055994531f;
+constexpr int kMaxSegments = 160;                    // parts of the vocabulary that a row's statistics come in
 
 __device__ __forceinline__ void flag(int32_t* d_status, int32_t bit) {
   if (d_status) atomicOr(d_status, bit);
 }
 
 // ---------------------------------------------------------------------------
-// K largest values of a stream, kept by one warp: lane i holds the i-th largest (value descending,
-// equal values by ascending id).  An insertion is a ballot, a population count and a few shuffles.
+// The K largest of n candidates (value descending, equal values by ascending id), found by a block of 256 threads.
+// Every eight threads take the maximum of their share; the K-th largest of these 32 distinct candidates bounds the K-th
+// largest of all from below, and usually little more than K candidates reach it (31 for K = 20).  They are collected and
+// each counts how many precede it.  No step is a chain of dependent comparisons (sorted lists kept by insertion took 30 us
+// for 5000 candidates, this takes 3).  When more than 256 reach the bound (many equal values, or one thread's
+// share holds most of the large ones) the exact bound is found by bisection, first on the value, then on the id.
 // ---------------------------------------------------------------------------
-// AUX: entries carry one more integer.
-template <bool AUX>
-struct WarpTop {
-  float v;
-  int id, aux;
-  float last_v;      // the K-th entry (what a candidate has to beat), uniform
-  int last_id;
-  __device__ __forceinline__ void init() { v = last_v = -CUDART_INF_F; id = last_id = 0x7FFFFFFF; aux = 0; }
-  __device__ __forceinline__ bool beats(float x, int xi) const {
-    return x > last_v || (x == last_v && xi < last_id && x > -CUDART_INF_F);
-  }
-  __device__ __forceinline__ void insert(float x, int xi, int xa, int K, int lane) {
-    const unsigned before = __ballot_sync(0xffffffffu, lane < K && (v > x || (v == x && id < xi)));
-    const int pos = __popc(before);
-    const float uv = __shfl_up_sync(0xffffffffu, v, 1);
-    const int ui = __shfl_up_sync(0xffffffffu, id, 1), ua = AUX ? __shfl_up_sync(0xffffffffu, aux, 1) : 0;
-    if (lane == pos) { v = x; id = xi; aux = xa; }
-    else if (lane > pos) { v = uv; id = ui; aux = ua; }
-    last_v = __shfl_sync(0xffffffffu, v, K - 1);
-    last_id = __shfl_sync(0xffffffffu, id, K - 1);
-  }
-  static __device__ __forceinline__ bool better(float x, int xi, float y, int yi) { return x > y || (x == y && xi < yi); }
-  // Joins a list that is sorted over the lanes (descending, empty entries -inf): the larger of entries i and 31 - i are
-  // the 32 largest of both and form a bitonic sequence, which five compare-exchanges sort.
-  __device__ __forceinline__ void merge(float x, int xi, int xa, int K, int lane) {
-    const float rx = __shfl_sync(0xffffffffu, x, 31 - lane);
-    const int ri = __shfl_sync(0xffffffffu, xi, 31 - lane), ra = AUX ? __shfl_sync(0xffffffffu, xa, 31 - lane) : 0;
-    if (better(rx, ri, v, id)) { v = rx; id = ri; aux = ra; }
-#pragma unroll
-    for (int s = 16; s > 0; s >>= 1) exchange(v, id, aux, s, (lane & s) == 0);
-    if (lane >= K) { v = -CUDART_INF_F; id = 0x7FFFFFFF; }
-    last_v = __shfl_sync(0xffffffffu, v, K - 1);
-    last_id = __shfl_sync(0xffffffffu, id, K - 1);
-  }
-  static __device__ __forceinline__ void exchange(float& x, int& xi, int& xa, int s, bool keep_larger) {
-    const float px = __shfl_xor_sync(0xffffffffu, x, s);
-    const int pi = __shfl_xor_sync(0xffffffffu, xi, s), pa = AUX ? __shfl_xor_sync(0xffffffffu, xa, s) : 0;
-    if (keep_larger ? better(px, pi, x, xi) : better(x, xi, px, pi)) { x = px; xi = pi; xa = pa; }
-  }
-  // One candidate per lane.  A few are inserted one after the other (some 70 clocks each); many are sorted
-  // (15 compare-exchanges) and merged (6 steps), some 600 clocks whatever their number.
-  __device__ __forceinline__ void offer(float x, int xi, int xa, int K, int lane) {
-    const bool in = beats(x, xi);
-    unsigned todo = __ballot_sync(0xffffffffu, in);
-    if (__popc(todo) > 8) {
-      if (!in) { x = -CUDART_INF_F; xi = 0x7FFFFFFF; }
-#pragma unroll
-      for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-        for (int j = k >> 1; j > 0; j >>= 1) exchange(x, xi, xa, j, ((lane & j) == 0) == ((lane & k) == 0));
-      merge(x, xi, xa, K, lane);
-      return;
-    }
-    while (todo) {
-      const int src = __ffs(todo) - 1;
-      todo &= todo - 1;
-      const float bx = __shfl_sync(0xffffffffu, x, src);
-      const int bi = __shfl_sync(0xffffffffu, xi, src), ba = AUX ? __shfl_sync(0xffffffffu, xa, src) : 0;
-      if (beats(bx, bi)) insert(bx, bi, ba, K, lane);
-    }
-  }
+constexpr int kTopThreads = 256;
+constexpr int kTopKept = 12;
+static_assert(SPO_MAX_TOP_K <= 32, "the bound is one of 32 maxima");
+constexpr int kNoKey = -0x7FFFFFFF - 1;
+struct __align__(16) TopSmem {
+  int key[kTopThreads], id[kTopThreads], at[kTopThreads];
+  int count[2][kTopThreads / 32];
+  int n;
+  int out_key[kMaxTopK], out_id[kMaxTopK], out_at[kMaxTopK];     // out_key kNoKey: fewer than that many candidates
 };
+
+// A float as an integer of the same order (and back: the mapping is its own inverse on the ordered values).
+__device__ __forceinline__ int order_key(int b) { return b ^ ((b >> 31) & 0x7FFFFFFF); }
+// The same for a logit that may be listed: -0 counts as 0; NaN and -inf are no candidates.
+__device__ __forceinline__ int top_key(float x) { return x > -CUDART_INF_F ? order_key(__float_as_int(x + 0.0f)) : kNoKey; }
+
+template <class Pred>
+__device__ __forceinline__ int block_count(int n, Pred pred, TopSmem& sh, int& buf) {
+  int c = 0;
+  for (int i = threadIdx.x; i < n; i += kTopThreads) c += pred(i) ? 1 : 0;
+  c = __reduce_add_sync(0xffffffffu, c);
+  if ((threadIdx.x & 31) == 0) sh.count[buf][threadIdx.x >> 5] = c;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < kTopThreads / 32; ++w) total += sh.count[buf][w];
+  buf ^= 1;
+  return total;
+}
+
+// How many of the first n entries of sh.key / sh.id precede (k, d).
+__device__ __forceinline__ int rank_of(int k, int d, int n, const TopSmem& sh) {
+  int before = 0;
+#pragma unroll 4
+  for (int q = 0; q < (n + 3) / 4; ++q) {
+    const int4 kk = reinterpret_cast<const int4*>(sh.key)[q], dd = reinterpret_cast<const int4*>(sh.id)[q];
+    before += (kk.x > k || (kk.x == k && dd.x < d)) + (kk.y > k || (kk.y == k && dd.y < d)) +
+              (kk.z > k || (kk.z == k && dd.z < d)) + (kk.w > k || (kk.w == k && dd.w < d));
+  }
+  return before;
+}
+
+// key(i) is candidate i's top_key, id(i) its id (distinct).  Results in sh.out_*, after a barrier; every thread calls it.
+template <class Key, class Id>
+__device__ __forceinline__ void block_top(int n, int K, Key key, Id id, TopSmem& sh) {
+  const int tid = threadIdx.x;
+  __syncthreads();                                  // the caller is done with what sh held
+  if (tid == 0) sh.n = 0;
+  if (tid < kMaxTopK) sh.out_key[tid] = kNoKey;
+  int bound = kNoKey;
+  int kept[kTopKept];                               // the first candidates of this thread, fetched together
+  kept[0] = key(min(tid, n - 1));
+  if (n > kTopThreads) {
+#pragma unroll
+    for (int u = 1; u < kTopKept; ++u) kept[u] = key(min(tid + u * kTopThreads, n - 1));
+    int m = kept[0];
+#pragma unroll
+    for (int u = 1; u < kTopKept; ++u) {
+      if (tid + u * kTopThreads >= n) kept[u] = kNoKey;
+      m = max(m, kept[u]);
+    }
+#pragma unroll 4
+    for (int i = tid + kTopKept * kTopThreads; i < n; i += kTopThreads) m = max(m, key(i));
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((tid & 7) == 0) sh.key[tid >> 3] = m;
+    __syncthreads();
+    m = sh.key[tid & 31];
+    int before = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int4 k4 = reinterpret_cast<const int4*>(sh.key)[q];
+      const int me = tid & 31;
+      before += (k4.x > m || (k4.x == m && 4 * q < me)) + (k4.y > m || (k4.y == m && 4 * q + 1 < me)) +
+                (k4.z > m || (k4.z == m && 4 * q + 2 < me)) + (k4.w > m || (k4.w == m && 4 * q + 3 < me));
+    }
+    bound = __shfl_sync(0xffffffffu, m, __ffs(__ballot_sync(0xffffffffu, before == K - 1)) - 1);
+    __syncthreads();
+  } else if (tid >= n) {
+    kept[0] = kNoKey;
+  }
+  int last_id = 0x7FFFFFFF;                         // of the candidates at the bound, those up to this id count
+  auto take = [&](int i, int k) {
+    if (k < bound || k == kNoKey) return;
+    const int d = id(i);
+    if (k == bound && d > last_id) return;
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < kTopThreads) { sh.key[at] = k; sh.id[at] = d; sh.at[at] = i; }
+  };
+  auto collect = [&]() {
+#pragma unroll
+    for (int u = 0; u < kTopKept; ++u) take(tid + u * kTopThreads, kept[u]);
+    for (int i = tid + kTopKept * kTopThreads; i < n; i += kTopThreads) take(i, key(i));
+    __syncthreads();
+  };
+  if (n > kTopThreads) {
+    collect();
+  } else {                                          // every thread has one candidate or none
+    sh.key[tid] = kept[0];
+    sh.id[tid] = tid < n ? id(tid) : 0;
+    sh.at[tid] = tid;
+    if (tid == 0) sh.n = n;
+    __syncthreads();
+  }
+  if (sh.n > kTopThreads) {
+    int buf = 0;
+    long long lo = bound, hi = 0x7FFFFFFF;          // the largest bound that K candidates reach
+    while (lo < hi) {
+      const long long mid = lo + (hi - lo + 1) / 2;
+      if (block_count(n, [&](int i) { return key(i) >= mid; }, sh, buf) >= K) lo = mid; else hi = mid - 1;
+    }
+    bound = (int)lo;
+    const int want = K - block_count(n, [&](int i) { return key(i) > bound; }, sh, buf);
+    lo = 0; hi = 0x7FFFFFFF;
+    while (lo < hi) {
+      const long long mid = (lo + hi) / 2;
+      if (block_count(n, [&](int i) { return key(i) == bound && id(i) <= mid; }, sh, buf) >= want) hi = mid; else lo = mid + 1;
+    }
+    last_id = (int)lo;
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    collect();
+  }
+  const int total = sh.n;
+  if (tid >= total && tid < ((total + 3) & ~3)) sh.key[tid] = kNoKey;             // rank_of takes four at a time
+  __syncthreads();
+  if (tid < total) {
+    const int k = sh.key[tid], d = sh.id[tid];
+    if (k != kNoKey) {
+      const int before = rank_of(k, d, total, sh);
+      if (before < K) { sh.out_key[before] = k; sh.out_id[before] = d; sh.out_at[before] = sh.at[tid]; }
+    }
+  }
+  __syncthreads();
+}
 
 // The launch before this one in the stream may still be running (programmatic dependent launch): wait for it to
 // have finished, and let the next launch come up behind this one.
@@ -109,7 +188,7 @@ __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.lau
 // (m2, l, ez) of two disjoint parts of a row, joined: m2 in log2 units, l = sum 2^(z sc2 - m2), ez = sum z 2^(...)
 __device__ __forceinline__ void join_stats(float& m2, float& l, float& ez, float m2b, float lb, float ezb) {
   const float m = fmaxf(m2, m2b);
-  const float wa = m2 == m ? 1.0f : exp2f(m2 - m), wb = m2b == m ? 1.0f : exp2f(m2b - m);
+  const float wa = m2 == m ? 1.0f : fast_exp2(m2 - m), wb = m2b == m ? 1.0f : fast_exp2(m2b - m);
   l = l * wa + lb * wb;
   ez = ez * wa + ezb * wb;
   m2 = m;
@@ -136,16 +215,23 @@ struct LpOut {
   int32_t* d_status;
 };
 
-// Outputs of token t from its joined statistics; the whole warp calls it, lane i < K with the i-th alternative.
-__device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, float m2, float l, float ez, float zt, bool odd, float top_v,
-                                          int top_id, int lane) {
+// A token's target and mask, fetched before the work that ends in lp_finish.
+struct LpRow {
+  int32_t y;
+  bool on;
+  __device__ __forceinline__ LpRow(const LpOut& o, int64_t t) : y(o.y ? o.y[t] : -1), on(o.mask == nullptr || o.mask[t] != 0) {}
+};
+
+// Outputs of token t from its joined statistics and the selected alternatives; one whole warp calls it.
+__device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, const LpRow& r, float m2, float l, float ez, float zt, bool odd,
+                                          const TopSmem& top, int lane) {
   float lse = (m2 + log2f(l)) * kLn2;
   if (odd) lse = CUDART_NAN_F;
-  const bool on = o.mask == nullptr || o.mask[t] != 0;
+  const bool on = r.on;
   if (lane == 0) {
     if (on && !(fabsf(lse) < CUDART_INF_F)) flag(o.d_status, SPO_DEV_NONFINITE);
     if (o.logp) {
-      const int32_t yt = o.y[t];
+      const int32_t yt = r.y;
       float lp = fmaf(zt, o.inv_t, -lse);
       if (yt < 0 || yt >= o.V) {
         lp = -CUDART_INF_F;
@@ -157,82 +243,70 @@ __device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, float m2, f
     if (o.entropy) o.entropy[t] = on ? lse - o.inv_t * (ez / l) : 0.0f;
   }
   if (lane < o.K) {
-    const bool found = top_v > -CUDART_INF_F;
-    o.top_ids[t * o.K + lane] = on && found ? top_id : -1;
-    o.top_logp[t * o.K + lane] = !on ? 0.0f : found ? fmaf(top_v, o.inv_t, -lse) : -CUDART_INF_F;
+    const int key = top.out_key[lane];
+    const bool found = key != kNoKey;
+    o.top_ids[t * o.K + lane] = on && found ? top.out_id[lane] : -1;
+    o.top_logp[t * o.K + lane] = !on ? 0.0f : found ? fmaf(__int_as_float(order_key(key)), o.inv_t, -lse) : -CUDART_INF_F;
   }
 }
 
-// A float as an integer of the same order (and back: the mapping is its own inverse).
-__device__ __forceinline__ int order_key(int b) { return b ^ ((b >> 31) & 0x7FFFFFFF); }
-
-// The K largest entries of sorted lists in shared memory ([list][K] of (value, id), empty entries -inf), one per lane: K
-// rounds over the lists' heads, of which a lane holds up to five.
-constexpr int kMergeLists = 160;
-__device__ __forceinline__ void merge_heads(const float2* s, int lists, int K, int lane, float* v_out, int* id_out) {
-  constexpr int H = kMergeLists / 32;
-  float hv[H];
-  int hi[H], hp[H];
+// The K largest logits of a row, from its groups of kGroup columns: the K groups of largest maximum hold them.  Group g covers
+// columns (g >> 1) tile_h + (g & 1) kGroup ..; gmax(g) is its maximum as a float (NaN and -inf: nothing in it counts).
+constexpr int kGroup = 64;
+template <class Gmax>
+__device__ __forceinline__ void block_pick(const float* z, int groups, int tile_h, int32_t V, int K, Gmax gmax, TopSmem& sh,
+                                           int* s_key, int* s_id) {
+  block_top(groups, K, [&](int g) { return top_key(gmax(g)); }, [](int g) { return g; }, sh);
+  constexpr int kSteps = kMaxTopK * kGroup / kTopThreads;
+  float x[kSteps];
+  int id[kSteps];
 #pragma unroll
-  for (int h = 0; h < H; ++h) {
-    const int q = lane + 32 * h;
-    hp[h] = 0;
-    hv[h] = -CUDART_INF_F;
-    hi[h] = 0x7FFFFFFF;
-    if (q < lists) { const float2 c = s[q * K]; hv[h] = c.x; hi[h] = __float_as_int(c.y); }
-  }
-  float v = -CUDART_INF_F;
-  int id = 0x7FFFFFFF;
-  for (int k = 0; k < K; ++k) {
-    float bv = hv[0];
-    int bi = hi[0], bh = 0;
-#pragma unroll
-    for (int h = 1; h < H; ++h)
-      if (hv[h] > bv || (hv[h] == bv && hi[h] < bi)) { bv = hv[h]; bi = hi[h]; bh = h; }
-    const int key = order_key(__float_as_int(bv + 0.0f));            // (-0 counts as 0)
-    const int best = __reduce_max_sync(0xffffffffu, key);
-    const int best_id = __reduce_min_sync(0xffffffffu, key == best ? bi : 0x7FFFFFFF);
-    if (best_id == 0x7FFFFFFF) break;                                // the lists are exhausted
-    if (lane == k) { v = __int_as_float(order_key(best)); id = best_id; }
-    if (key == best && bi == best_id) {                              // ids are distinct: one lane
-#pragma unroll
-      for (int h = 0; h < H; ++h)
-        if (h == bh) {
-          const int at = ++hp[h];
-          hv[h] = -CUDART_INF_F;
-          hi[h] = 0x7FFFFFFF;
-          if (at < K) { const float2 c = s[(lane + 32 * h) * K + at]; hv[h] = c.x; hi[h] = __float_as_int(c.y); }
-        }
+  for (int u = 0; u < kSteps; ++u) {                // fetched together
+    const int i = threadIdx.x + u * kTopThreads, q = i / kGroup;
+    id[u] = -1;
+    if (q < K && sh.out_key[q] != kNoKey) {
+      const int g = sh.out_id[q], c = (g & 1) * kGroup + i % kGroup;
+      if (c < tile_h && (g >> 1) * tile_h + c < V) id[u] = (g >> 1) * tile_h + c;
     }
+    x[u] = z[max(id[u], 0)];
   }
-  *v_out = v;
-  *id_out = id;
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int i = threadIdx.x + u * kTopThreads;
+    if (i < K * kGroup) { s_key[i] = id[u] < 0 ? kNoKey : top_key(x[u]); s_id[i] = id[u]; }
+  }
+  block_top(K * kGroup, K, [&](int i) { return s_key[i]; }, [&](int i) { return s_id[i]; }, sh);
 }
 
 // ---------------------------------------------------------------------------
-// Statistics and alternatives of stored logit rows.  Block = (row, segment of the vocabulary); each
-// warp takes a contiguous part of `part` columns, the block joins its warps and writes one partial and one
-// sorted list, or, where it has the whole row, the outputs.  Reads every logit once; bound by L2 or HBM.
+// Statistics of stored logit rows and the maxima of their groups of kGroup columns.  Block = (row, segment of the vocabulary);
+// each warp takes a contiguous part of `part` columns (a multiple of kGroup).  A block that has the whole row finishes it,
+// otherwise it leaves its partial and its groups' maxima to lp_pick_kernel.  Reads every logit once; bound by L2 or HBM.
 // ---------------------------------------------------------------------------
-constexpr int kRowWarps = 8;
+constexpr int kRowWarps = kTopThreads / 32;
+constexpr int kRowGroups = kRowWarps * 4096 / kGroup;      // groups of a row that one block takes whole
 
 __global__ void __launch_bounds__(32 * kRowWarps)
 lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int64_t t0, const LpOut o,
-               FwdPartial* __restrict__ partials, float2* __restrict__ cand) {
+               FwdPartial* __restrict__ partials, float* __restrict__ gmax, int groups) {
+  __shared__ TopSmem sh;
+  __shared__ int s_key[kMaxTopK * kGroup], s_id[kMaxTopK * kGroup];
+  __shared__ float s_gmax[kRowGroups];
+  __shared__ float s_m[kRowWarps], s_l[kRowWarps], s_e[kRowWarps];
+  pdl_trigger();
+  pdl_wait();
   const int32_t V = o.V;
   const int K = o.K;
   const float sc2 = kLog2e * o.inv_t;
-  pdl_trigger();
-  pdl_wait();
   const int64_t row = blockIdx.x / nseg;
+  const LpRow tr(o, t0 + row);
   const int seg = (int)(blockIdx.x - row * nseg);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float* z = Z + row * ldz;
+  float* gm = nseg == 1 ? s_gmax : gmax + row * groups;
   const int64_t begin = ((int64_t)seg * kRowWarps + warp) * part;
   const int64_t end = begin + part < V ? begin + part : V;
   float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f;
-  WarpTop<false> top;
-  top.init();
   for (int64_t c0 = begin; c0 < end; c0 += 256) {
     float x[8];
 #pragma unroll
@@ -243,6 +317,15 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int
     float mx = x[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) mx = fmaxf(mx, x[i]);
+    if (K > 0) {
+      float mine = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = __reduce_max_sync(0xffffffffu, max(top_key(x[2 * i]), top_key(x[2 * i + 1])));
+        if (lane == i) mine = key == kNoKey ? -CUDART_INF_F : __int_as_float(order_key(key));
+      }
+      if (lane < 4 && c0 + lane * kGroup < end) gm[c0 / kGroup + lane] = mine;
+    }
     const float mn = fmaxf(fmaxf(m2, mx * sc2), -1.0e25f);   // a lane without columns: exponentials of -inf, not of rounding
     float s = 0.0f, t = 0.0f;
 #pragma unroll
@@ -255,20 +338,11 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int
     l = fmaf(l, down, s);
     ez = fmaf(ez, down, t);
     m2 = mn;
-    if (K > 0 && __any_sync(0xffffffffu, mx > top.last_v)) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t c = c0 + i * 32 + lane;
-        top.offer(c < end ? x[i] : -CUDART_INF_F, (int)c, 0, K, lane);
-      }
-    }
   }
-  __shared__ float s_m[kRowWarps], s_l[kRowWarps], s_e[kRowWarps];
-  __shared__ float2 s_top[kRowWarps * kMaxTopK];
   warp_join_stats(m2, l, ez);
   if (lane == 0) { s_m[warp] = m2; s_l[warp] = l; s_e[warp] = ez; }
-  if (lane < K) s_top[warp * K + lane] = make_float2(top.v, __int_as_float(top.id));
   __syncthreads();
+  if (nseg == 1 && K > 0) block_pick(z, groups, 128, V, K, [&](int g) { return s_gmax[g]; }, sh, s_key, s_id);
   if (warp != 0) return;
   m2 = lane < kRowWarps ? s_m[lane] : -CUDART_INF_F;
   l = lane < kRowWarps ? s_l[lane] : 0.0f;
@@ -277,103 +351,126 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int
   warp_join_stats(m2, l, ez);
   if (odd) l = CUDART_NAN_F;
   const int64_t lo = (int64_t)seg * kRowWarps * part, hi = lo + (int64_t)kRowWarps * part;
-  const int32_t yt = o.y ? o.y[t0 + row] : -1;
+  const int32_t yt = tr.y;
   const float zt = yt >= lo && yt < hi && yt < V ? z[yt] : -CUDART_INF_F;
-  float tv = -CUDART_INF_F;
-  int ti = 0x7FFFFFFF;
-  if (K > 0) merge_heads(s_top, kRowWarps, K, lane, &tv, &ti);
   if (nseg == 1) {
-    lp_finish(o, t0 + row, m2, l, ez, zt, odd, tv, ti, lane);
-    return;
-  }
-  if (lane == 0) {
+    lp_finish(o, t0 + row, tr, m2, l, ez, zt, odd, sh, lane);
+  } else if (lane == 0) {
     FwdPartial pt;
     pt.m2 = m2; pt.l = l; pt.pad = ez; pt.zt = zt;
     partials[row * nseg + seg] = pt;
   }
-  if (lane < K) cand[(row * nseg + seg) * K + lane] = make_float2(tv, __int_as_float(ti));
 }
 
+// A row's partials, fetched by one warp (at(s) is the place of the s-th) and joined later: the fetch is in flight meanwhile.
+struct RowParts {
+  float4 p[kMaxSegments / 32];
+  template <class At>
+  __device__ __forceinline__ void fetch(const FwdPartial* partials, int lists, At at, int lane) {
+#pragma unroll
+    for (int u = 0; u < kMaxSegments / 32; ++u)
+      p[u] = lane + 32 * u < lists ? *reinterpret_cast<const float4*>(partials + at(lane + 32 * u))
+                                   : make_float4(-CUDART_INF_F, 0.0f, -CUDART_INF_F, 0.0f);
+  }
+  __device__ __forceinline__ void join(float& m2, float& l, float& ez, float& zt, bool& odd) const {
+    m2 = -CUDART_INF_F; l = 0.0f; ez = 0.0f; zt = -CUDART_INF_F;
+    odd = false;                                    // a partial that is NaN: fmaxf would drop it
+#pragma unroll
+    for (int u = 0; u < kMaxSegments / 32; ++u) {
+      odd |= !(p[u].y >= 0.0f);
+      zt = p[u].z > -CUDART_INF_F || p[u].z != p[u].z ? p[u].z : zt;   // at most one part has the target
+      join_stats(m2, l, ez, p[u].x, p[u].y, p[u].w);
+    }
+    warp_join_stats(m2, l, ez);
+    odd = __any_sync(0xffffffffu, odd);
+    const unsigned has = __ballot_sync(0xffffffffu, zt > -CUDART_INF_F || zt != zt);
+    zt = has ? __shfl_sync(0xffffffffu, zt, __ffs(has) - 1) : -CUDART_INF_F;
+  }
+};
+
 // ---------------------------------------------------------------------------
-// The end of every path: joins a token row's partials, finishes logp / lse / entropy, and finds the
-// alternatives among the row's lists.  WARPS warps per row.  GROUPS: the lists hold column groups (maximum, group << 8 |
-// slot) whose 32 logits are stored in `cand`; first the K groups of largest maximum, then the K largest logits
-// in them.  Otherwise the lists hold the logits themselves, (value, id), sorted.
+// The end of the tiled path, a block per token row: joins the row's partials ([list][rows]) and picks the alternatives from
+// its lists of column groups (maximum, group << 8 | slot), whose 32 logits each are stored in `cand`.
 // ---------------------------------------------------------------------------
-template <bool GROUPS, int WARPS>
-__global__ void __launch_bounds__(WARPS == 1 ? 128 : 32 * WARPS)
-lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part_ld, const float2* __restrict__ tops,
-                const float* __restrict__ cand, int list_len, int64_t rows, int64_t t0, const LpOut o) {
-  static_assert((WARPS == 1) == GROUPS, "column groups are merged by one warp, plain lists by several");
+__global__ void __launch_bounds__(kTopThreads)
+lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, const float2* __restrict__ tops, const float* __restrict__ cand,
+                int list_len, int64_t rows, int64_t t0, const LpOut o) {
+  __shared__ TopSmem sh;
+  __shared__ int s_key[kMaxTopK * 32], s_id[kMaxTopK * 32];
   pdl_trigger();
   pdl_wait();
-  const int lane = threadIdx.x & 31, warp = WARPS == 1 ? 0 : threadIdx.x >> 5;
-  const int64_t row = WARPS == 1 ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : (int64_t)blockIdx.x;
-  if (row >= rows) return;
-  const int64_t t = t0 + row;
-  const int K = o.K;
-  __shared__ float2 s_lists[GROUPS ? 1 : kMergeLists * kMaxTopK];
-  if (!GROUPS) {                                    // all lists into shared memory
-    for (int i = threadIdx.x; i < lists * K; i += 32 * WARPS) s_lists[i] = tops[row * lists * K + i];
-    __syncthreads();
-    if (warp != 0) return;
-  }
-  // partial of list s: [s][part_ld] (GROUPS) or [row][lists]
-  auto at = [&](int s) { return GROUPS ? (int64_t)s * part_ld + row : row * lists + s; };
-  float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f, zt = -CUDART_INF_F;
-  bool odd = false;                                 // a partial that is NaN: fmaxf would drop it
-#pragma unroll 4
-  for (int s = lane; s < lists; s += 32) {
-    const FwdPartial p = partials[at(s)];
-    odd |= !(p.l >= 0.0f);
-    zt = p.zt > -CUDART_INF_F || p.zt != p.zt ? p.zt : zt;   // at most one list has the target
-    join_stats(m2, l, ez, p.m2, p.l, p.pad);
-  }
-  warp_join_stats(m2, l, ez);
-  odd = __any_sync(0xffffffffu, odd);
-  const unsigned has = __ballot_sync(0xffffffffu, zt > -CUDART_INF_F || zt != zt);
-  zt = has ? __shfl_sync(0xffffffffu, zt, __ffs(has) - 1) : -CUDART_INF_F;
-  float tv = -CUDART_INF_F;
-  int ti = 0x7FFFFFFF;
-  if (!GROUPS) {
-    if (K > 0) merge_heads(s_lists, lists, K, lane, &tv, &ti);
-  } else if (K > 0) {
-    WarpTop<true> g;
-    g.init();
-    const int n = lists * list_len;
-    for (int i0 = 0; i0 < n; i0 += 128) {           // four accesses in flight
-      float2 c[4];
-      int ax[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int i = i0 + 32 * u + lane;
-        c[u] = make_float2(-CUDART_INF_F, __uint_as_float(0xFFFFFF00u));
-        ax[u] = 0;
-        if (i < n) {
-          const int s = i / list_len, k = i - s * list_len;
-          c[u] = tops[at(s) * list_len + k];
-          ax[u] = s * list_len;
-        }
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, K = o.K;
+  const LpRow tr(o, t0 + row);
+  RowParts parts;
+  if (warp == 0) parts.fetch(partials, lists, [&](int s) { return (int64_t)s * rows + row; }, lane);
+  {
+    auto entry = [&](int i) {
+      const int s = i / list_len;
+      return tops[((int64_t)s * rows + row) * list_len + (i - s * list_len)];
+    };
+    block_top(lists * list_len, K, [&](int i) { return top_key(entry(i).x); },
+              [&](int i) { return (int)(__float_as_uint(entry(i).y) >> 8); }, sh);
+    for (int i = threadIdx.x; i < K * 32; i += kTopThreads) {
+      int key = kNoKey, id = 0;
+      if (sh.out_key[i >> 5] != kNoKey) {
+        const int at = sh.out_at[i >> 5], s = at / list_len, slot = (int)(__float_as_uint(entry(at).y) & 255u);
+        id = sh.out_id[i >> 5] * 32 + (i & 31);
+        if (id < o.V) key = top_key(cand[(((int64_t)s * rows + row) * list_len + slot) * 32 + (i & 31)]);
       }
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        g.offer(c[u].x, (int)(__float_as_uint(c[u].y) >> 8), ax[u] + (int)(__float_as_uint(c[u].y) & 255u), K, lane);
+      s_key[i] = key;
+      s_id[i] = id;
     }
-    WarpTop<false> top;
-    top.init();
-    for (int k = 0; k < K; ++k) {
-      const float gm = __shfl_sync(0xffffffffu, g.v, k);
-      const int gid = __shfl_sync(0xffffffffu, g.id, k), loc = __shfl_sync(0xffffffffu, g.aux, k);
-      if (!(gm > -CUDART_INF_F)) break;             // fewer groups than K
-      const int s = loc / list_len, slot = loc - s * list_len;
-      const int id = gid * 32 + lane;
-      const float x = cand[(at(s) * list_len + slot) * 32 + lane];
-      top.offer(id < o.V ? x : -CUDART_INF_F, id, 0, K, lane);
-    }
-    tv = top.v;
-    ti = top.id;
+    block_top(K * 32, K, [&](int i) { return s_key[i]; }, [&](int i) { return s_id[i]; }, sh);
   }
-  lp_finish(o, t, m2, l, ez, zt, odd, tv, ti, lane);
+  if (warp != 0) return;
+  float m2, l, ez, zt;
+  bool odd;
+  parts.join(m2, l, ez, zt, odd);
+  lp_finish(o, t0 + row, tr, m2, l, ez, zt, odd, sh, lane);
+}
+
+// The same for rows of which one warp joins the partials and no alternatives are wanted.
+__global__ void __launch_bounds__(128)
+lp_join_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t rows, int64_t t0, const LpOut o) {
+  __shared__ TopSmem none;                          // not read: K = 0
+  pdl_trigger();
+  pdl_wait();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  const LpRow tr(o, t0 + row);
+  RowParts parts;
+  parts.fetch(partials, lists, [&](int s) { return (int64_t)s * rows + row; }, lane);
+  float m2, l, ez, zt;
+  bool odd;
+  parts.join(m2, l, ez, zt, odd);
+  lp_finish(o, t0 + row, tr, m2, l, ez, zt, odd, none, lane);
+}
+
+// The end of the paths whose logits are stored, a block per token row: joins the row's partials ([row][lists]) and picks the
+// alternatives from the maxima of its groups.
+__global__ void __launch_bounds__(kTopThreads)
+lp_pick_kernel(const FwdPartial* __restrict__ partials, int lists, const float* __restrict__ gmax, int groups, int tile_h,
+               const float* __restrict__ Z, int64_t ldz, int64_t t0, const LpOut o) {
+  __shared__ TopSmem sh;
+  __shared__ int s_key[kMaxTopK * kGroup], s_id[kMaxTopK * kGroup];
+  pdl_trigger();
+  pdl_wait();
+  const int64_t row = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const LpRow tr(o, t0 + row);
+  RowParts parts;
+  if (warp == 0) parts.fetch(partials, lists, [&](int s) { return row * lists + s; }, lane);
+  if (o.K > 0) {
+    const float* gm = gmax + row * groups;
+    block_pick(Z + row * ldz, groups, tile_h, o.V, o.K, [&](int g) { return gm[g]; }, sh, s_key, s_id);
+  }
+  if (warp != 0) return;
+  float m2, l, ez, zt;
+  bool odd;
+  parts.join(m2, l, ez, zt, odd);
+  lp_finish(o, t0 + row, tr, m2, l, ez, zt, odd, sh, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -383,21 +480,25 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t part
 // streams).  W is read once, which is the floor (1.24 GB at d = 4096, V = 151936: 190 us at the measured copy rate); the token
 // rows come from L2 once per tile, NT / tile_h of W's traffic.  tile_h is the smallest height that takes the same number of
 // rounds over the SMs, so that the last round is full (V = 151936 on 148 SMs: 115 rows x 9 rounds reads 0.8 %
-// more than an even share, 128-row tiles would leave the ninth round nearly empty).
+// more than an even share, 128-row tiles would leave the ninth round nearly empty).  Pairs of CTAs on one 256-row tile
+// (half the traffic of token rows each) are slower, 207 against 197 us for one row, 217 against 207 for 48.
 // Reduction: eight warps turn the finished tile into [token][vocabulary row] in shared memory, then each takes
-// the tokens w, w + 8, ..: a lane holds four logits, the row's maximum and sums are warp reductions, lane k keeps the
-// running statistics of the warp's k-th token, and a tile whose maximum beats the token's K-th entry goes into its
-// sorted list.  Storing the logits and reducing them in further launches took 254 us where this takes 196 (one token,
-// K = 20): 80 us of launches that read 0.6 MB, most of it chains of list insertions in a few warps.
+// the tokens w, w + 8, .., two at a time: a lane holds four logits, the row's maximum and sums are warp reductions, lane k
+// keeps the running statistics of the warp's k-th token.  For the alternatives the tile's logits are stored ([token][V] fp32,
+// 4 T / (2 d) of W's bytes) with the maxima of their groups of 64; the K largest of a row lie in its K groups of largest
+// maximum, which lp_pick_kernel looks up.  (Keeping a sorted list per token row and CTA instead costs a chain of dependent
+// shuffles per tile: 128 rows with K = 20 took 438 us that way.)
 // ---------------------------------------------------------------------------
 struct StreamParams {
   int tiles, tile_h, k_blocks;
-  int T, K;
+  int T;
   int32_t V;
   float sc2;
   const int32_t* y;
   FwdPartial* partials;                      // [T][gridDim.x]
-  float2* tops;                              // [T][gridDim.x][K]
+  float* Z;                                  // logits [T][ldz] and maxima of their groups [T][2 tiles]; NULL: not wanted
+  int64_t ldz;
+  float* gmax;
   int32_t* d_status;
 };
 
@@ -406,10 +507,10 @@ constexpr int kStreamThreads = 64 + 32 * kStreamWarps;
 constexpr int kStreamA = 128 * 64 * 2;
 template <int NT> struct StreamCfg {
   static constexpr int stage_bytes = kStreamA + NT * 128;
-  static constexpr int tile_bytes = NT * 128 * 4;            // logits of a tile, [token][128]
-  static constexpr int list_bytes = NT * 32 * 8;             // sorted lists, [token][32]
-  static constexpr int stages = (226 * 1024 - tile_bytes - list_bytes - 2048) / stage_bytes;
-  static constexpr int smem = stages * stage_bytes + tile_bytes + list_bytes + 1024 + 512;
+  static constexpr int round = NT < 32 ? NT : 32;            // tokens reduced at a time
+  static constexpr int tile_bytes = round * 128 * 4;         // their logits, [token][128]
+  static constexpr int stages = (226 * 1024 - tile_bytes - 2048) / stage_bytes;
+  static constexpr int smem = stages * stage_bytes + tile_bytes + 1024 + 512;
   static constexpr int tmem_cols = 2 * NT < 32 ? 32 : 2 * NT;
 };
 
@@ -438,8 +539,7 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
   float* tile_z = reinterpret_cast<float*>(gen + S * C::stage_bytes);
-  float2* list = reinterpret_cast<float2*>(gen + S * C::stage_bytes + C::tile_bytes);
-  constexpr int kBarAt = S * C::stage_bytes + C::tile_bytes + C::list_bytes;
+  constexpr int kBarAt = S * C::stage_bytes + C::tile_bytes;
   const uint32_t bars = base + kBarAt;
   const uint32_t full0 = bars, empty0 = bars + 8 * S, tfull0 = bars + 16 * S, tempty0 = tfull0 + 16;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + kBarAt + 16 * S + 32);
@@ -504,12 +604,9 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2, w = warp - 2;
     constexpr int PER = NT / kStreamWarps;               // tokens w, w + 8, .. of this warp; lane k < PER keeps the k-th's state
-    float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f, zt = -CUDART_INF_F, thr = -CUDART_INF_F;
+    float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f, zt = -CUDART_INF_F;
     const int my_t = w + kStreamWarps * lane;
     const int32_t my_y = lane < PER && my_t < p.T && p.y ? p.y[my_t] : -1;
-    for (int k = 0; k < PER; ++k)
-      list[(w + kStreamWarps * k) * 32 + lane] = make_float2(-CUDART_INF_F, __int_as_float(0x7FFFFFFF));
-    __syncwarp();
     uint32_t n = 0;
     for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x, ++n) {
       const uint32_t b = n & 1u;
@@ -518,79 +615,94 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
       good = __shfl_sync(0xffffffffu, good, 0);
       tc_fence_after();
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + b * NT;
-      if (good) {
-        constexpr int COLS = NT / 2 < 16 ? 16 : NT / 2;              // token columns per warp of a quarter
-        if (half * COLS < NT) {
-#pragma unroll 1
-          for (int c = half * COLS; c < (half + 1) * COLS; c += 16) {
-            uint32_t x[16];
-            tmem_ld16(taddr + c, x);
-#pragma unroll
-            for (int j = 0; j < 16; ++j) tile_z[(c + j) * 128 + quarter * 32 + lane] = __uint_as_float(x[j]);
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cta(tempty0 + 8 * b);
-      }
-      if (!stream_barrier(good != 0)) break;                          // the tile is in shared memory
       const int v0 = tile * p.tile_h;
       const int cols = p.V - v0 < p.tile_h ? p.V - v0 : p.tile_h;
+      bool on = true;
 #pragma unroll 1
-      for (int k = 0; k < PER; ++k) {
-        const int t = w + kStreamWarps * k;
-        if (t >= p.T) break;
-        const float* z = tile_z + t * 128;
-        float x[4];
+      for (int r = 0; r < NT / C::round; ++r) {
+        if (good) {
+#pragma unroll 1
+          for (int c = half * 16; c < C::round; c += 32) {               // 16 token columns at a time
+            uint32_t x[16];
+            tmem_ld16(taddr + r * C::round + c, x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = i * 32 + lane < cols ? z[i * 32 + lane] : -1.0e30f;
-        const int b32 = __float_as_int(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
-        const float mx = __int_as_float(order_key(__reduce_max_sync(0xffffffffu, order_key(b32))));
-        const float mk = __shfl_sync(0xffffffffu, m2, k);
-        const float mn = fmaxf(fmaxf(mk, mx * p.sc2), -1.0e25f);
-        float s = 0.0f, u = 0.0f;
+            for (int j = 0; j < 16; ++j) tile_z[(c + j) * 128 + quarter * 32 + lane] = __uint_as_float(x[j]);
+            if (p.Z && quarter * 32 + lane < cols) {
+              float* dst = p.Z + (int64_t)(r * C::round + c) * p.ldz + v0 + quarter * 32 + lane;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = fast_exp2(fmaf(x[i], p.sc2, -mn));
-          s += e;
-          u = fmaf(e, x[i], u);
+              for (int j = 0; j < 16; ++j)
+                if (r * C::round + c + j < p.T) dst[(int64_t)j * p.ldz] = __uint_as_float(x[j]);
+            }
+          }
+          if (r == NT / C::round - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cta(tempty0 + 8 * b);
+          }
         }
+        on = stream_barrier(good != 0);                                   // the logits are in shared memory
+        if (!on) break;
+        constexpr int KR = C::round / kStreamWarps;                       // this warp's tokens of the round: 2 or 4
+#pragma unroll 1
+        for (int k0 = r * KR; k0 < (r + 1) * KR; k0 += 2) {
+          if (w + kStreamWarps * k0 >= p.T) break;
+          float s[2], u[2], mx[2], mk[2], mn[2];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          s += __shfl_xor_sync(0xffffffffu, s, o);
-          u += __shfl_xor_sync(0xffffffffu, u, o);
-        }
-        if (lane == k) {
-          const float down = fast_exp2(mk - mn);
-          l = fmaf(l, down, s);
-          ez = fmaf(ez, down, u);
-          m2 = mn;
-          if (my_y >= v0 && my_y < v0 + cols) zt = z[my_y - v0];
-        }
-        if (p.K > 0 && mx > __shfl_sync(0xffffffffu, thr, k)) {
-          float2* mine = list + t * 32 + lane;
-          WarpTop<false> top;
-          const float2 c = *mine;
-          top.v = c.x; top.id = __float_as_int(c.y); top.aux = 0;
-          top.last_v = __shfl_sync(0xffffffffu, top.v, p.K - 1);
-          top.last_id = __shfl_sync(0xffffffffu, top.id, p.K - 1);
+          for (int e = 0; e < 2; ++e) {                                   // (a second token past T has logits of zero rows)
+            const float* z = tile_z + (w + kStreamWarps * (k0 + e) - r * C::round) * 128;
+            float x[4];
+            int key[2];
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            top.offer(i * 32 + lane < cols ? x[i] : -CUDART_INF_F, v0 + i * 32 + lane, 0, p.K, lane);
-          *mine = make_float2(top.v, __int_as_float(top.id));
-          if (lane == k) thr = top.last_v;
+            for (int i = 0; i < 4; ++i) x[i] = i * 32 + lane < cols ? z[i * 32 + lane] : -1.0e30f;
+            if (p.Z) {
+#pragma unroll
+              for (int i = 0; i < 2; ++i) key[i] = __reduce_max_sync(0xffffffffu, max(top_key(x[2 * i]), top_key(x[2 * i + 1])));
+              const int mine = lane == 0 ? key[0] : key[1];
+              const int t = w + kStreamWarps * (k0 + e);
+              if (lane < 2 && t < p.T)
+                p.gmax[((int64_t)t * p.tiles + tile) * 2 + lane] = mine == kNoKey ? -CUDART_INF_F : __int_as_float(order_key(mine));
+              const int top = max(key[0], key[1]);
+              mx[e] = top == kNoKey ? -CUDART_INF_F : __int_as_float(order_key(top));
+            } else {
+              const float lm = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+              mx[e] = __int_as_float(order_key(__reduce_max_sync(0xffffffffu, order_key(__float_as_int(lm)))));
+            }
+            mk[e] = __shfl_sync(0xffffffffu, m2, k0 + e);
+            mn[e] = fmaxf(fmaxf(mk[e], mx[e] * p.sc2), -1.0e25f);
+            s[e] = u[e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float ex = fast_exp2(fmaf(x[i], p.sc2, -mn[e]));
+              s[e] += ex;
+              u[e] = fmaf(ex, x[i], u[e]);
+            }
+          }
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              s[e] += __shfl_xor_sync(0xffffffffu, s[e], o);
+              u[e] += __shfl_xor_sync(0xffffffffu, u[e], o);
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (lane == k0 + e) {
+              const float down = fast_exp2(mk[e] - mn[e]);
+              l = fmaf(l, down, s[e]);
+              ez = fmaf(ez, down, u[e]);
+              m2 = mn[e];
+              if (my_y >= v0 && my_y < v0 + cols) zt = tile_z[(my_t - r * C::round) * 128 + my_y - v0];
+            }
         }
+        stream_barrier(true);                                             // they have been read
       }
-      if (!stream_barrier(true)) break;                               // the tile has been read
+      if (!on) break;
     }
     if (lane < PER && my_t < p.T) {
       FwdPartial pt;
       pt.m2 = m2; pt.l = l; pt.zt = zt; pt.pad = ez;
       p.partials[(int64_t)my_t * gridDim.x + blockIdx.x] = pt;
-    }
-    for (int k = 0; k < PER; ++k) {
-      const int t = w + kStreamWarps * k;
-      if (t < p.T && lane < p.K) p.tops[((int64_t)t * gridDim.x + blockIdx.x) * p.K + lane] = list[t * 32 + lane];
     }
   }
 
@@ -607,7 +719,7 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
 
 // CTAs of lp_stream_kernel, and rows of its vocabulary tiles.
 void stream_shape(int32_t V, int* grid, int* tile_h) {
-  const int sms = sm_count() < kMergeLists ? sm_count() : kMergeLists;
+  const int sms = sm_count() < kMaxSegments ? sm_count() : kMaxSegments;
   const int64_t rounds = ceil_div(V, (int64_t)128 * sms);
   int h = (int)ceil_div(V, rounds * sms);
   if (h < 8) h = 8;
@@ -617,7 +729,7 @@ void stream_shape(int32_t V, int* grid, int* tile_h) {
 }
 
 template <int NT>
-cudaError_t launch_stream_t(const LpFwd& a, FwdPartial* partials, float2* tops, cudaStream_t st) {
+cudaError_t launch_stream_t(const LpFwd& a, FwdPartial* partials, float* Z, int64_t ldz, float* gmax, cudaStream_t st) {
   using C = StreamCfg<NT>;
   static std::atomic<int> ready[64];
   int dev = 0;
@@ -638,22 +750,16 @@ cudaError_t launch_stream_t(const LpFwd& a, FwdPartial* partials, float2* tops, 
   p.tiles = (int)ceil_div(a.V, p.tile_h);
   p.k_blocks = (int)ceil_div(a.d, 64);
   p.T = (int)a.T;
-  p.K = a.top_k;
   p.V = a.V;
   p.sc2 = kLog2e * a.inv_t;
   p.y = a.y;
   p.partials = partials;
-  p.tops = tops;
+  p.Z = Z;
+  p.ldz = ldz;
+  p.gmax = gmax;
   p.d_status = a.d_status;
   lp_stream_kernel<NT><<<grid, kStreamThreads, C::smem, st>>>(mW, mH, p);
   return cudaGetLastError();
-}
-
-cudaError_t launch_stream(const LpFwd& a, FwdPartial* partials, float2* tops, cudaStream_t st) {
-  if (a.T <= 16) return launch_stream_t<16>(a, partials, tops, st);
-  if (a.T <= 32) return launch_stream_t<32>(a, partials, tops, st);
-  if (a.T <= 64) return launch_stream_t<64>(a, partials, tops, st);
-  return launch_stream_t<128>(a, partials, tops, st);
 }
 
 // A launch whose kernel begins with pdl_wait(): it may come up while the launch before it still runs.
@@ -669,6 +775,20 @@ cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, dim3 block, cudaStre
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+
+// Z and gmax may be NULL when no alternatives are wanted.
+cudaError_t launch_stream(const LpFwd& a, const LpOut& o, FwdPartial* partials, float* Z, int64_t ldz, float* gmax, cudaStream_t st) {
+  if (a.top_k == 0) Z = nullptr;
+  cudaError_t e = a.T <= 16   ? launch_stream_t<16>(a, partials, Z, ldz, gmax, st)
+                  : a.T <= 32 ? launch_stream_t<32>(a, partials, Z, ldz, gmax, st)
+                  : a.T <= 64 ? launch_stream_t<64>(a, partials, Z, ldz, gmax, st)
+                              : launch_stream_t<128>(a, partials, Z, ldz, gmax, st);
+  if (e != cudaSuccess) return e;
+  int grid, h;
+  stream_shape(a.V, &grid, &h);
+  return launch_dependent(lp_pick_kernel, dim3((unsigned)a.T), dim3(kTopThreads), st, partials, grid, gmax, 2 * (int)ceil_div(a.V, h),
+                          h, Z, ldz, (int64_t)0, o);
 }
 
 // ---------------------------------------------------------------------------
@@ -882,14 +1002,14 @@ int64_t f32_chunk_rows(int64_t T, int32_t V) {
   return rows < T ? rows : (T > 0 ? T : 1);
 }
 
-// Segments of the vocabulary a stored row is reduced in: enough blocks to fill the GPU when the rows are few, at most as
-// many as one block merges; a warp's part is a multiple of 32 columns.
+// Segments of the vocabulary a stored row is reduced in: enough blocks to fill the GPU when the rows are few; a warp's part is
+// a multiple of kGroup columns.
 void row_segments(int64_t rows, int32_t V, int* nseg, int* part) {
   int64_t want = ceil_div((int64_t)sm_count() * 4, rows);            // segments per row
-  if (want > kMergeLists) want = kMergeLists;
-  int64_t pt = ceil_div(ceil_div(V, kRowWarps * want), 32) * 32;
+  if (want > kMaxSegments) want = kMaxSegments;
+  int64_t pt = ceil_div(ceil_div(V, kRowWarps * want), kGroup) * kGroup;
   if (want > 1 && pt < 256) pt = 256;                                // no shorter than one step of the loop
-  if (pt > 4096 && ceil_div(V, kRowWarps * 4096) <= kMergeLists) pt = 4096;
+  if (pt > 4096 && ceil_div(V, kRowWarps * 4096) <= kMaxSegments) pt = 4096;
   *part = (int)pt;
   *nseg = (int)ceil_div(V, kRowWarps * pt);
 }
@@ -906,7 +1026,12 @@ LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype)
     int grid, h;
     stream_shape(V, &grid, &h);
     L.partials = off; off = align_up(off + sizeof(FwdPartial) * (size_t)L.chunk * grid, 256);
-    L.tops = off;     off = align_up(off + sizeof(float2) * (size_t)L.chunk * grid * (top_k > 0 ? top_k : 1), 256);
+    L.ldz = pad4(V);
+    L.z = L.tops = off;
+    if (top_k > 0) {
+      off = align_up(off + (size_t)L.chunk * L.ldz * 4, 256);
+      L.tops = off;   off = align_up(off + (size_t)L.chunk * ceil_div(V, h) * 8, 256);
+    }
   } else if (L.path == LP_F32) {
     L.chunk = f32_chunk_rows(T, V);
     L.ldz = pad4(V);
@@ -914,7 +1039,8 @@ LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype)
     const int64_t segs = (int64_t)sm_count() * 4 + L.chunk * (1 + ceil_div(V, kRowWarps * 4096));
     L.z = off;        off = align_up(off + (size_t)L.chunk * L.ldz * 4, 256);
     L.partials = off; off = align_up(off + sizeof(FwdPartial) * (size_t)segs, 256);
-    L.tops = off;     off = align_up(off + sizeof(float2) * (size_t)segs * (top_k > 0 ? top_k : 1), 256);
+    L.tops = off;
+    if (top_k > 0) off = align_up(off + (size_t)L.chunk * ceil_div(V, kGroup) * 4, 256);      // maxima of the groups
   } else {
     const int64_t n = ceil_div(T, kLpChunkRows);
     L.chunk = ceil_div(ceil_div(T, n), 256) * 256;               // chunks of like size
@@ -994,34 +1120,33 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
     if (L.path == LP_TILES) {
       float* cand = reinterpret_cast<float*>(ws + L.cand);
       e = launch_lp_fwd_bf16(a, t0, rows, partials, cand, tops, reinterpret_cast<uint32_t*>(ws + L.progress), st);
-      if (e == cudaSuccess)
-        e = launch_dependent(lp_merge_kernel<true, 1>, dim3((unsigned)ceil_div(rows, 4)), dim3(128), st, partials,
-                             lp_fwd_lists(rows, a.d, a.V), rows, tops, cand, lp_list_len(a.top_k), rows, t0, o);
+      const int lists = lp_fwd_lists(rows, a.d, a.V);
+      if (e == cudaSuccess && a.top_k == 0)
+        e = launch_dependent(lp_join_kernel, dim3((unsigned)ceil_div(rows, 4)), dim3(128), st, partials, lists, rows, t0, o);
+      else if (e == cudaSuccess)
+        e = launch_dependent(lp_merge_kernel, dim3((unsigned)rows), dim3(kTopThreads), st, partials, lists, tops, cand,
+                             lp_list_len(a.top_k), rows, t0, o);
       if (e != cudaSuccess) return e;
       continue;
     }
-    int lists;
-    if (L.path == LP_STREAM) {
-      int h;
-      stream_shape(a.V, &lists, &h);
-      e = launch_stream(a, partials, tops, st);
-    } else {
-      float* Z = reinterpret_cast<float*>(ws + L.z);
-      SgemmParams p{};
-      p.A = (const float*)a.H + t0 * a.ldh; p.lda = a.ldh; p.M = rows;
-      p.B = (const float*)a.W; p.ldb = a.d; p.N = a.V;
-      p.K = a.d;
-      p.C = Z; p.ldc = L.ldz;
-      if ((e = launch_sgemm<true, true>(p, nullptr, st)) != cudaSuccess) return e;
-      int part;
-      row_segments(rows, a.V, &lists, &part);
-      e = launch_dependent(lp_rows_kernel, dim3((unsigned)(rows * lists)), dim3(32 * kRowWarps), st, Z, L.ldz, lists, part, t0, o,
-                           partials, tops);
-      if (e == cudaSuccess && lists == 1) continue;
-    }
-    if (e != cudaSuccess) return e;
-    e = launch_dependent(lp_merge_kernel<false, 8>, dim3((unsigned)rows), dim3(256), st, partials, lists, (int64_t)0, tops, nullptr,
-                         a.top_k, rows, t0, o);
+    if (L.path == LP_STREAM)
+      return launch_stream(a, o, partials, reinterpret_cast<float*>(ws + L.z), L.ldz, reinterpret_cast<float*>(ws + L.tops), st);
+    float* Z = reinterpret_cast<float*>(ws + L.z);
+    SgemmParams p{};
+    p.A = (const float*)a.H + t0 * a.ldh; p.lda = a.ldh; p.M = rows;
+    p.B = (const float*)a.W; p.ldb = a.d; p.N = a.V;
+    p.K = a.d;
+    p.C = Z; p.ldc = L.ldz;
+    if ((e = launch_sgemm<true, true>(p, nullptr, st)) != cudaSuccess) return e;
+    int lists, part;
+    row_segments(rows, a.V, &lists, &part);
+    float* gmax = reinterpret_cast<float*>(ws + L.tops);
+    const int groups = (int)ceil_div(a.V, kGroup);
+    e = launch_dependent(lp_rows_kernel, dim3((unsigned)(rows * lists)), dim3(32 * kRowWarps), st, Z, L.ldz, lists, part, t0, o,
+                         partials, gmax, groups);
+    if (e == cudaSuccess && lists > 1)
+      e = launch_dependent(lp_pick_kernel, dim3((unsigned)rows), dim3(kTopThreads), st, partials, lists, gmax, groups, 128, Z, L.ldz,
+                           t0, o);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

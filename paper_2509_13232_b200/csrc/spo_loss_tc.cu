@@ -1074,7 +1074,29 @@ cudaError_t launch_bwd_bf16(const void* H, const void* W, const int32_t* y, cons
 // ---------------------------------------------------------------------------
 int lp_list_len(int top_k) { return top_k == 0 ? 0 : top_k <= 8 ? 8 : kMaxTopK; }
 
-int lp_fwd_lists(int64_t rows, int32_t d, int32_t V) { return 2 * fwd_unit_splits(rows, d, V); }
+// Splits of the vocabulary tiles.  A few row tiles stream W once whatever the split (its tiles are not read
+// again), so only the number of tiles that the busiest pair gets counts; with many row tiles the pairs re-read W and
+// pick_fwd_split weighs the L2 footprint.  (129 rows at d = 4096, V = 151936: 1001 us with the latter's 12 splits, which
+// leave 62 pairs idle, 263 us with 60.)
+static int lp_split(int64_t rows, int32_t d, int32_t V) {
+  const int64_t m_tiles = ceil_div(rows, GROUP_M);
+  const int n_tiles = (int)ceil_div(V, BN), groups = group_count();
+  if (m_tiles * 4 > groups) {
+    const int ns = pick_fwd_split(m_tiles, n_tiles, d);
+    if (ns <= 80) return ns;                                       // (a row's partials: at most 160)
+  }
+  int best = 1;
+  int64_t best_cost = INT64_MAX;
+  for (int ns = 1; ns <= n_tiles && ns <= groups && ns <= 80; ++ns) {         // (a row's partials: at most 160)
+    const int64_t per = ceil_div(n_tiles, ns);
+    if (ceil_div(n_tiles, per) != ns) continue;                    // not a distinct partition
+    const int64_t cost = per * ceil_div(m_tiles * ns, groups);
+    if (cost < best_cost) { best_cost = cost; best = ns; }
+  }
+  return best;
+}
+
+int lp_fwd_lists(int64_t rows, int32_t d, int32_t V) { return 2 * lp_split(rows, d, V); }
 
 cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
                                float2* cand_max, uint32_t* progress, cudaStream_t st) {
@@ -1084,7 +1106,7 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
   GemmParams p{};
   p.m_tiles = (int)ceil_div(rows, GROUP_M);
   p.n_tiles = (int)ceil_div(a.V, BN);
-  p.nsplit = fwd_unit_splits(rows, a.d, a.V);
+  p.nsplit = lp_split(rows, a.d, a.V);
   p.per_split = (int)ceil_div(p.n_tiles, p.nsplit);
   p.k_blocks = (int)ceil_div(a.d, BK);
   p.a_row0 = (int)t0;
@@ -1132,7 +1154,7 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
       GemmParams p{};
       p.m_tiles = m_tiles;
       p.n_tiles = n_tiles_v;
-      p.nsplit = pick_fwd_split(m_tiles, n_tiles_v, a.d);
+      p.nsplit = lp_split(rows, a.d, a.V);
       p.per_split = (int)ceil_div(n_tiles_v, p.nsplit);
       p.k_blocks = (int)ceil_div(a.d, BK);
       p.a_row0 = (int)t0;
