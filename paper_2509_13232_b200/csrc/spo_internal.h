@@ -264,8 +264,11 @@ int lp_list_len(int top_k);               // column groups listed per row, vocab
 int lp_fwd_lists(int64_t rows, int32_t d, int32_t V);   // lists (and partials) per row of a launch over `rows` rows
 cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
                                float2* cand_max, uint32_t* progress, cudaStream_t st);
+int lp_dh_splits(int64_t rows, int32_t d, int32_t V);    // parts of dH's contraction over the vocabulary
 cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_rows, int64_t ldg, float* partial,
-                               void* h_clean, uint32_t* progress, cudaStream_t st);
+                               void* h_clean, float* split, uint32_t* progress, cudaStream_t st);
+// out[i] = sum over `parts` of src[part][i] in order, n elements (a multiple of 4) of type out_dtype
+cudaError_t launch_sum_parts(const float* src, int parts, int64_t n, void* out, int32_t out_dtype, cudaStream_t st);
 // out[i][:] = H[t0 + i][:] (bf16, row pitch ldh), or zeros where mask[t0 + i] is 0
 cudaError_t launch_clean_rows(const void* H, int64_t ldh, const uint8_t* mask, int64_t t0, int64_t rows, int32_t d,
                               void* out, cudaStream_t st);

@@ -987,6 +987,21 @@ clean_rows_kernel(const uint4* __restrict__ H, int64_t ld_vec, const uint8_t* __
   }
 }
 
+template <bool BF16>
+__global__ void __launch_bounds__(256)
+sum_parts_kernel(const float4* __restrict__ src, int parts, int64_t quads, void* __restrict__ out) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (int64_t)gridDim.x * 256) {
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+    for (int z = 0; z < parts; ++z) {
+      const float4 x = src[z * quads + i];
+      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+    }
+    if (BF16) reinterpret_cast<uint2*>(out)[i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+    else reinterpret_cast<float4*>(out)[i] = s;
+  }
+}
+
 // ---------------------------------------------------------------------------
 // scratch
 // ---------------------------------------------------------------------------
@@ -1079,6 +1094,16 @@ LpBwdWs lp_bwd_layout(int64_t T, int32_t d, int32_t V, int32_t dtype) {
     L.progress = off; off = align_up(off + kProgressBytes, 256);
     L.partial = off;
     if (T > L.chunk) off = align_up(off + (size_t)V * d * 4, 256);
+    L.split = off;                                               // parts of dH, of a full chunk or of the last one
+    size_t parts = 0;
+    const int64_t t_eff = T > 0 ? T : 1, first = t_eff < L.chunk ? t_eff : L.chunk,
+                  last = t_eff - (ceil_div(t_eff, L.chunk) - 1) * L.chunk;
+    for (int64_t rows : {first, last}) {
+      const int s = lp_dh_splits(rows, d, V);
+      const size_t x = s > 1 ? (size_t)s * rows * d * 4 : 0;
+      if (x > parts) parts = x;
+    }
+    off = align_up(off + parts, 256);
   }
   L.total = off;
   return L;
@@ -1105,6 +1130,16 @@ cudaError_t launch_clean_rows(const void* H, int64_t ldh, const uint8_t* mask, i
   if (blocks > (int64_t)sm_count() * 16) blocks = (int64_t)sm_count() * 16;
   clean_rows_kernel<<<(unsigned)blocks, 256, 0, st>>>(reinterpret_cast<const uint4*>(H), ldh / 8, mask, t0, rows, d / 8,
                                                       reinterpret_cast<uint4*>(out));
+  return cudaGetLastError();
+}
+
+cudaError_t launch_sum_parts(const float* src, int parts, int64_t n, void* out, int32_t out_dtype, cudaStream_t st) {
+  int64_t blocks = ceil_div(n / 4, 256);
+  if (blocks > (int64_t)sm_count() * 8) blocks = (int64_t)sm_count() * 8;
+  if (out_dtype == SPO_DTYPE_BF16)
+    sum_parts_kernel<true><<<(unsigned)blocks, 256, 0, st>>>(reinterpret_cast<const float4*>(src), parts, n / 4, out);
+  else
+    sum_parts_kernel<false><<<(unsigned)blocks, 256, 0, st>>>(reinterpret_cast<const float4*>(src), parts, n / 4, out);
   return cudaGetLastError();
 }
 
@@ -1158,7 +1193,7 @@ cudaError_t lp_backward(const LpBwd& a, char* ws, cudaStream_t st) {
   const LpBwdWs L = lp_bwd_layout(a.T, a.d, a.V, a.dtype);
   if (a.dtype == SPO_DTYPE_BF16)
     return launch_lp_bwd_bf16(a, reinterpret_cast<__nv_bfloat16*>(ws + L.g), L.chunk, L.ldg,
-                              reinterpret_cast<float*>(ws + L.partial), ws + L.h_clean,
+                              reinterpret_cast<float*>(ws + L.partial), ws + L.h_clean, reinterpret_cast<float*>(ws + L.split),
                               reinterpret_cast<uint32_t*>(ws + L.progress), st);
   float* Z = reinterpret_cast<float*>(ws + L.g);
   float* split = reinterpret_cast<float*>(ws + L.split);

@@ -135,6 +135,8 @@ struct GemmParams {
   const float *ent, *g_logp, *g_lse, *g_ent; // G: entropy and upstream gradients per row (g_lse, g_ent + ent optional)
   float inv_t;                               // G: 1 / temperature
   const float* partial;                      // DW: fp32 sum of the earlier chunks, added before the rounding; NULL = none
+  int k_splits, k_per;                       // DH: the contraction cut into k_splits parts of k_per k-blocks, each with an
+                                             // fp32 result of its own in `out`, [part][rows_valid][ldo]
 };
 
 // g = c_t (1[v = y_t] - 2^(z log2e - lse_t log2e)) for 32 consecutive columns, packed to bf16.
@@ -251,7 +253,7 @@ __device__ __forceinline__ Unit unit_of(int u, const GemmParams& p) {
 // softmax; the list is kept sorted in registers by LP compare-exchanges that the warp skips when none of its
 // rows has a group above its last entry, and a listed group's 32 logits are stored once, when it enters.
 // (A list of the logits themselves would be touched by nearly every group of 32 rows x 32 columns, in a
-// scan of every logit.)  G: general upstream gradients.  DW: bf16 result.
+// scan of every logit.)  G: general upstream gradients.  DW: bf16 result.  DH: the contraction split along k.
 template <int MODE, bool ENT = false, int LP = -1>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmParams p) {
@@ -272,7 +274,8 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_ctarank();                    // 0 = leader of the pair
   const int group = blockIdx.x / CG, n_groups = gridDim.x / CG;
-  const int total_units = p.m_tiles * p.nsplit;
+  constexpr bool KS = MODE == MODE_DH && LP >= 0;             // units are (tile, part of the contraction)
+  const int total_units = p.m_tiles * p.nsplit * (KS ? p.k_splits : 1);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
@@ -308,11 +311,12 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     int ok = 1;
     const bool paced = (rank == 0) && p.progress != nullptr;
     for (int u = group; u < total_units; u += n_groups) {
-      const Unit un = unit_of(u, p);
+      const Unit un = unit_of(KS ? u / p.k_splits : u, p);
+      const int kb0 = KS ? (u % p.k_splits) * p.k_per : 0, kb1 = KS ? min(kb0 + p.k_per, p.k_blocks) : p.k_blocks;
       const int row_base = un.m_tile * GROUP_M + (int)rank * BM;       // this CTA's rows of the tile
       for (int n = un.n_begin; n < un.n_end; ++n) {
         const int col_base = n * BN + (int)rank * BSUB_ROWS;           // this CTA's columns of half 0
-        for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+        for (int kb = kb0; kb < kb1; ++kb, ++it) {
           if (paced && lane == 0 && ok) {
             *pace_mine = it;
             for (int tries = 0; tries < kHoldTries && it > *pace_limit; ++tries) __nanosleep(64);
@@ -358,11 +362,12 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       uint32_t it = 0, tile = 0;
       bool ok = true;
       for (int u = group; u < total_units && ok; u += n_groups) {
-        const Unit un = unit_of(u, p);
+        const Unit un = unit_of(KS ? u / p.k_splits : u, p);
+        const int kb0 = KS ? (u % p.k_splits) * p.k_per : 0, kb1 = KS ? min(kb0 + p.k_per, p.k_blocks) : p.k_blocks;
         for (int n = un.n_begin; n < un.n_end && ok; ++n, ++tile) {
           if (!mbar_wait(tempty, (tile & 1u) ^ 1u, abort_flag, p.d_status)) { ok = false; break; }
           tc_fence_after();
-          for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+          for (int kb = kb0; kb < kb1; ++kb, ++it) {
             const uint32_t s = it % STAGES, ph = (it / STAGES) & 1u;
             if (!mbar_wait(full0 + 8 * s, ph, abort_flag, p.d_status)) { ok = false; break; }
             tc_fence_after();
@@ -374,7 +379,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               for (int h = 0; h < 2; ++h) {
                 const uint32_t sbh = sb + h * BSUB_BYTES;
                 const uint64_t db = B_MN ? smem_desc(sbh + j * 2048, 8192, 1024) : smem_desc(sbh + j * 32, 16, 1024);
-                umma_bf16(tmem_base + h * HALF_N, da, db, idesc, (kb | j) != 0 ? 1u : 0u);
+                umma_bf16(tmem_base + h * HALF_N, da, db, idesc, ((kb - kb0) | j) != 0 ? 1u : 0u);
               }
             }
             umma_commit(empty0 + 8 * s);
@@ -395,7 +400,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     uint32_t tile = 0;
     bool ok = true;
     for (int u = group; u < total_units && ok; u += n_groups) {
-      const Unit un = unit_of(u, p);
+      const Unit un = unit_of(KS ? u / p.k_splits : u, p);
       const int64_t grow = p.out_row0 + (int64_t)un.m_tile * GROUP_M + row;   // global output row of this lane
       const int64_t grow_warp0 = grow - lane;                                  // ... and of the warp's first lane
       const bool row_ok = grow < p.rows_valid;
@@ -644,7 +649,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           }
         } else {
           // fp32 outputs: 32 columns (128 bytes per row) per staging round; dW may accumulate
-          float* obase = reinterpret_cast<float*>(p.out) + grow_warp0 * p.ldo;
+          float* obase = reinterpret_cast<float*>(p.out) + grow_warp0 * p.ldo + (KS ? (u % p.k_splits) * p.rows_valid * p.ldo : 0);
 #pragma unroll 1
           for (int ch = 0; ch < HALF_N / 32; ++ch) {
             const int col0 = col_half + ch * 32;
@@ -847,7 +852,7 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmPa
   int max_groups = 0;
   cudaError_t e0 = resident_groups<MODE, ENT, LP>(&max_groups);
   if (e0 != cudaSuccess) return e0;
-  const int units = p_in.m_tiles * p_in.nsplit;
+  const int units = p_in.m_tiles * p_in.nsplit * (MODE == MODE_DH && LP >= 0 ? p_in.k_splits : 1);
   if (units <= 0) return cudaSuccess;
   GemmParams p = p_in;
   // k-blocks a pair may run ahead of the slowest one.  E / FWD / G sweep short tiles (d / 64 k-blocks) and
@@ -1098,6 +1103,10 @@ static int lp_split(int64_t rows, int32_t d, int32_t V) {
 
 int lp_fwd_lists(int64_t rows, int32_t d, int32_t V) { return 2 * lp_split(rows, d, V); }
 
+// With one or two row tiles the pairs share nothing but those rows, which stay in L2: no pacing, and no launch that
+// zeroes its counters (2 us of some 25).
+static bool lp_paced(int64_t rows) { return rows > 2 * GROUP_M; }
+
 cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
                                float2* cand_max, uint32_t* progress, cudaStream_t st) {
   CUtensorMap ma, mb;
@@ -1124,6 +1133,7 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
   p.cand_ld = rows;
   const int list = lp_list_len(a.top_k);
   const bool ent = a.entropy != nullptr;
+  if (!lp_paced(rows)) progress = nullptr;
   if (list == 0) return ent ? launch_gemm<MODE_FWD, true, 0>(ma, mb, p, progress, st)
                             : launch_gemm<MODE_FWD, false, 0>(ma, mb, p, progress, st);
   if (list == 8) return ent ? launch_gemm<MODE_FWD, true, 8>(ma, mb, p, progress, st)
@@ -1132,19 +1142,38 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
              : launch_gemm<MODE_FWD, false, kMaxTopK>(ma, mb, p, progress, st);
 }
 
+// Parts that dH's contraction over the vocabulary is cut into when its tiles leave pairs idle: the one that minimises
+// the k-blocks of a part (0.61 us each) plus the writing and summing of the parts' fp32 results (8 bytes per element at 4 TB/s,
+// and a launch).  203 rows, d = 1024, V = 32000: 2 tiles, 286 us in one part, 22 us in 25 and their sum.
+int lp_dh_splits(int64_t rows, int32_t d, int32_t V) {
+  const int64_t units = ceil_div(rows, GROUP_M) * ceil_div(d, BN);
+  const int k_blocks = (int)ceil_div(V, BK), most = (int)(group_count() / units);
+  int best = 1;
+  double best_t = 0.61 * k_blocks;
+  for (int s = 2; s <= most && s <= k_blocks; ++s) {
+    const int per = (int)ceil_div(k_blocks, s);
+    if ((int)ceil_div(k_blocks, per) != s) continue;
+    const double t = 0.61 * per + 4.0 + s * (double)rows * d * 2.0e-6;
+    if (t < best_t) { best_t = t; best = s; }
+  }
+  return best;
+}
+
 // bf16 backward for general upstream gradients, chunk by chunk as launch_bwd_bf16: the chunk's logit
 // gradient, dH = G W, dW (+)= G^T H.  A bf16 dW over several chunks is summed in fp32 (`partial`) and
 // rounded once, in the last chunk's epilogue.
 cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_rows, int64_t ldg, float* partial,
-                               void* h_clean, uint32_t* progress, cudaStream_t st) {
+                               void* h_clean, float* split, uint32_t* progress, cudaStream_t st) {
   CUtensorMap mH_k, mW_k, mW_mn, mH_mn;
   if (!make_map(&mH_k, a.H, a.d, a.T, a.ldh, kBoxA) || !make_map(&mW_k, a.W, a.d, a.V, a.d, kBoxB) ||
       !make_map(&mW_mn, a.W, a.d, a.V, a.d, 64))
     return cudaErrorInvalidValue;
   const int n_tiles_v = (int)ceil_div(a.V, BN), tiles_v = (int)ceil_div(a.V, GROUP_M);
+  uint32_t* const all_progress = progress;
   cudaError_t e;
   for (int64_t t0 = 0; t0 < a.T; t0 += chunk_rows) {
     const int64_t rows = (a.T - t0) < chunk_rows ? (a.T - t0) : chunk_rows;
+    progress = lp_paced(rows) ? all_progress : nullptr;
     const int m_tiles = (int)ceil_div(rows, GROUP_M);
     const bool last = t0 + rows >= a.T;
     CUtensorMap mG_k, mG_mn;
@@ -1168,9 +1197,28 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
       p.d_status = a.d_status;
       if ((e = launch_gemm<MODE_G, false, 0>(mH_k, mW_k, p, progress, st)) != cudaSuccess) return e;
     }
-    if ((e = launch_dh(mG_k, mW_mn, t0, rows, a.T, a.d, a.V, a.dH, a.dH_dtype, nullptr, progress, a.d_status, st)) !=
-        cudaSuccess)
-      return e;
+    const int k_splits = lp_dh_splits(rows, a.d, a.V);
+    if (k_splits == 1) {
+      e = launch_dh(mG_k, mW_mn, t0, rows, a.T, a.d, a.V, a.dH, a.dH_dtype, nullptr, progress, a.d_status, st);
+    } else {
+      GemmParams p{};
+      p.m_tiles = m_tiles;
+      p.n_tiles = (int)ceil_div(a.d, BN);
+      p.nsplit = p.n_tiles;
+      p.per_split = 1;
+      p.k_blocks = (int)ceil_div(a.V, BK);
+      p.k_splits = k_splits;
+      p.k_per = (int)ceil_div(p.k_blocks, k_splits);
+      p.rows_valid = rows;
+      p.cols_valid = a.d;
+      p.out = split; p.ldo = a.d;
+      p.d_status = a.d_status;
+      e = launch_gemm<MODE_DH, false, 0>(mG_k, mW_mn, p, progress, st);
+      if (e == cudaSuccess)
+        e = launch_sum_parts(split, k_splits, rows * a.d, (char*)a.dH + t0 * a.d * (a.dH_dtype == SPO_DTYPE_BF16 ? 2 : 4),
+                             a.dH_dtype, st);
+    }
+    if (e != cudaSuccess) return e;
     // The gradient of a masked row is zero, but zero times a NaN in that row of H is not: with a mask the
     // dW contraction reads a copy of the chunk's rows in which the masked ones are zero.
     int64_t h_row0 = t0;
