@@ -795,14 +795,24 @@ cudaError_t launch_stream(const LpFwd& a, const LpOut& o, FwdPartial* partials, 
 // fp32 matrix product on the fp32 pipes: C[m][n] (+)= sum_k A(m,k) B(n,k).  A_K / B_K: the operand is
 // contiguous along k, else along m / n.  Tiles of TILE x TILE x 16, 256 threads, TILE/16 squared results a
 // thread; the next k-block is fetched into registers while this one is multiplied.  gridDim.z splits k:
-// each split writes its own C (stride M * ldc) and sum_splits_kernel adds them in a fixed order.
+// each split writes its own C (stride M * ldc) and sum_splits_kernel adds them in a fixed order.  GRAD: the results are
+// logits, and their gradient is stored in their place (the formula of g_values_lp, with log p in nats).
 // ---------------------------------------------------------------------------
+struct GradParams {
+  const int32_t* y;                 // all by row of C
+  const uint8_t* mask;
+  const float *lse, *ent, *g_logp, *g_lse, *g_ent;
+  float inv_t;
+  int32_t V;
+  int32_t* d_status;
+};
 struct SgemmParams {
   const float *A, *B;
   int64_t lda, ldb, ldc, M, N, K, k_per;
   float* C;
   int accumulate;
   const uint8_t* b_mask;            // k rows whose B is taken as zero where the mask is 0 (B contiguous along n)
+  GradParams grad;
 };
 
 template <int TILE, bool KC>
@@ -840,7 +850,7 @@ __device__ __forceinline__ void sg_store(float (*s)[TILE + 4], int idx, float4 v
   }
 }
 
-template <int TILE, bool A_K, bool B_K>
+template <int TILE, bool A_K, bool B_K, bool GRAD>
 __global__ void __launch_bounds__(256)
 sgemm_kernel(const SgemmParams p) {
   constexpr int R = TILE / 64;                       // groups of four rows (columns) per thread, 64 apart
@@ -852,6 +862,7 @@ sgemm_kernel(const SgemmParams p) {
   const int64_t k_end = k_begin + p.k_per < p.K ? k_begin + p.k_per : p.K;
   float acc[4 * R][4 * R] = {};
   pdl_trigger();
+  pdl_wait();
   float4 ra[LOADS], rb[LOADS];
 #pragma unroll
   for (int i = 0; i < LOADS; ++i) {
@@ -892,35 +903,70 @@ sgemm_kernel(const SgemmParams p) {
   for (int i = 0; i < 4 * R; ++i) {
     const int64_t m = m0 + ty * 4 + (i & 3) + 64 * (i >> 2);
     if (m >= p.M) continue;
+    bool live = true;
+    float a = 0.0f, b = 0.0f, tgt = 0.0f, ls = 0.0f;
+    int32_t yt = -1;
+    if (GRAD) {
+      const GradParams& g = p.grad;
+      live = g.mask == nullptr || g.mask[m] != 0;
+      float gl = g.g_logp ? g.g_logp[m] : 0.0f;
+      yt = g.y ? g.y[m] : -1;
+      if (g.g_logp && (yt < 0 || yt >= g.V)) {               // no such target: its log-prob is the constant -inf
+        if (live && blockIdx.y == 0 && tx == 0) flag(g.d_status, SPO_DEV_ID_OUT_OF_RANGE);
+        gl = 0.0f;
+      }
+      const float ge = g.g_ent ? g.g_ent[m] : 0.0f, gs = g.g_lse ? g.g_lse[m] : 0.0f;
+      a = g.inv_t * (gs - gl - (g.g_ent ? ge * g.ent[m] : 0.0f));
+      b = -g.inv_t * ge;
+      tgt = g.inv_t * gl;
+      ls = g.lse[m];
+    }
 #pragma unroll
     for (int j = 0; j < 4 * R; ++j) {
       const int64_t n = n0 + tx * 4 + (j & 3) + 64 * (j >> 2);
       if (n >= p.N) continue;
       float* dst = C + m * p.ldc + n;
-      *dst = p.accumulate ? *dst + acc[i][j] : acc[i][j];
+      if (GRAD) {
+        float v = 0.0f;
+        if (live) {
+          const float u = fmaf(acc[i][j], p.grad.inv_t, -ls);
+          v = expf(u) * fmaf(b, u, a);
+          if (n == yt) v += tgt;
+        }
+        *dst = v;
+      } else {
+        *dst = p.accumulate ? *dst + acc[i][j] : acc[i][j];
+      }
     }
   }
 }
 
+// out[i] (+)= sum of the splits' results, in order; blockIdx.y selects one of two sums.
+struct SplitSum { const float* parts; int splits; int64_t n; float* out; int accumulate; };
 __global__ void __launch_bounds__(256)
-sum_splits_kernel(const float* __restrict__ parts, int splits, int64_t n, float* __restrict__ out, int accumulate) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    float s = accumulate ? out[i] : 0.0f;
-    for (int z = 0; z < splits; ++z) s += parts[(int64_t)z * n + i];
-    out[i] = s;
+sum_splits_kernel(const SplitSum s0, const SplitSum s1) {
+  pdl_trigger();
+  pdl_wait();
+  const SplitSum& s = blockIdx.y == 0 ? s0 : s1;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < s.n; i += (int64_t)gridDim.x * 256) {
+    float x = s.accumulate ? s.out[i] : 0.0f;
+#pragma unroll 4
+    for (int z = 0; z < s.splits; ++z) x += s.parts[(int64_t)z * s.n + i];
+    s.out[i] = x;
   }
 }
 
 constexpr int kSplitBlocks = 444;                              // blocks that a split of k fills the GPU with
 constexpr size_t kSplitBytes = (size_t)kSplitBlocks * 128 * 128 * 4;   // room for all splits' results together
 
-template <bool A_K, bool B_K>
-cudaError_t launch_sgemm(SgemmParams p, float* split_ws, cudaStream_t st) {
+// `sum` (NULL: k is not split): receives what is left to be summed, n = 0 for nothing.  `first`: the first launch of a call.
+template <bool A_K, bool B_K, bool GRAD = false>
+cudaError_t launch_sgemm(SgemmParams p, bool first, float* split_ws, SplitSum* sum, cudaStream_t st) {
   const int64_t big = ceil_div(p.M, 128) * ceil_div(p.N, 128);
   const int tile = big >= sm_count() ? 128 : 64;               // 64: four times the blocks where 128 leaves SMs idle
   const int64_t bm = ceil_div(p.M, tile), bn = ceil_div(p.N, tile);
   int64_t splits = 1;
-  if (split_ws && p.ldc == p.N && bm * bn < 2 * sm_count()) {
+  if (sum && p.ldc == p.N && bm * bn < 2 * sm_count()) {
     splits = kSplitBlocks / (bm * bn);
     const int64_t most = ceil_div(p.K, 128);                   // at least 8 k-blocks a split
     if (splits > most) splits = most;
@@ -930,50 +976,15 @@ cudaError_t launch_sgemm(SgemmParams p, float* split_ws, cudaStream_t st) {
   p.k_per = ceil_div(ceil_div(p.K, 16), splits) * 16;
   splits = ceil_div(p.K, p.k_per);
   if (bn > 65535 || splits > 65535) return cudaErrorInvalidConfiguration;
-  float* out = p.C;
-  const int accumulate = p.accumulate;
+  if (sum) *sum = SplitSum{split_ws, (int)splits, splits > 1 ? p.M * p.N : 0, p.C, p.accumulate};
   if (splits > 1) { p.C = split_ws; p.accumulate = 0; }
   const dim3 grid((unsigned)bm, (unsigned)bn, (unsigned)splits);
-  if (tile == 128) sgemm_kernel<128, A_K, B_K><<<grid, 256, 0, st>>>(p);
-  else sgemm_kernel<64, A_K, B_K><<<grid, 256, 0, st>>>(p);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || splits == 1) return e;
-  const int64_t n = p.M * p.N;
-  int64_t blocks = ceil_div(n, 256);
-  if (blocks > (int64_t)sm_count() * 8) blocks = (int64_t)sm_count() * 8;
-  sum_splits_kernel<<<(unsigned)blocks, 256, 0, st>>>(split_ws, (int)splits, n, out, accumulate);
-  return cudaGetLastError();
-}
-
-// fp32 logits to their gradient, in place (the formula of g_values_lp, with log p in nats).
-__global__ void __launch_bounds__(256)
-lp_g_f32_kernel(float* __restrict__ Z, int64_t ldz, int nseg, int32_t V, int64_t t0, const int32_t* __restrict__ y,
-                const uint8_t* __restrict__ mask, const float* __restrict__ lse, const float* __restrict__ ent,
-                const float* __restrict__ g_logp, const float* __restrict__ g_lse, const float* __restrict__ g_ent,
-                float inv_t, int32_t* d_status) {
-  const int64_t row = blockIdx.x / nseg;
-  const int seg = (int)(blockIdx.x - row * nseg);
-  const int64_t t = t0 + row;
-  float* z = Z + row * ldz;
-  const bool live = mask == nullptr || mask[t] != 0;
-  float gl = g_logp ? g_logp[t] : 0.0f;
-  const int32_t yt = y ? y[t] : -1;
-  if (g_logp && (yt < 0 || yt >= V)) {
-    if (live && seg == 0 && threadIdx.x == 0) flag(d_status, SPO_DEV_ID_OUT_OF_RANGE);
-    gl = 0.0f;
+  auto kern = tile == 128 ? sgemm_kernel<128, A_K, B_K, GRAD> : sgemm_kernel<64, A_K, B_K, GRAD>;
+  if (first) {
+    kern<<<grid, 256, 0, st>>>(p);
+    return cudaGetLastError();
   }
-  const float ge = g_ent ? g_ent[t] : 0.0f, gs = g_lse ? g_lse[t] : 0.0f;
-  const float a = inv_t * (gs - gl - (g_ent ? ge * ent[t] : 0.0f)), b = -inv_t * ge, tgt = inv_t * gl, ls = lse[t];
-  const int64_t lo = (int64_t)seg * 4096, hi = lo + 4096 < V ? lo + 4096 : V;
-  for (int64_t v = lo + threadIdx.x; v < hi; v += 256) {
-    float g = 0.0f;
-    if (live) {
-      const float u = fmaf(z[v], inv_t, -ls);
-      g = expf(u) * fmaf(b, u, a);
-      if (v == yt) g += tgt;
-    }
-    z[v] = g;
-  }
+  return launch_dependent(kern, grid, dim3(256), st, p);
 }
 
 __global__ void __launch_bounds__(256)
@@ -1084,7 +1095,7 @@ LpBwdWs lp_bwd_layout(int64_t T, int32_t d, int32_t V, int32_t dtype) {
     L.chunk = f32_chunk_rows(T, V);
     L.ldg = pad4(V);
     L.g = off;     off = align_up(off + (size_t)L.chunk * L.ldg * 4, 256);
-    L.split = off; off = align_up(off + kSplitBytes, 256);
+    L.split = off; off = align_up(off + 2 * kSplitBytes, 256);           // of dH and of dW
   } else {
     const BwdWs b = bwd_ws_layout(T, d, V);
     L.chunk = b.chunk_rows;
@@ -1172,7 +1183,7 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
     p.B = (const float*)a.W; p.ldb = a.d; p.N = a.V;
     p.K = a.d;
     p.C = Z; p.ldc = L.ldz;
-    if ((e = launch_sgemm<true, true>(p, nullptr, st)) != cudaSuccess) return e;
+    if ((e = launch_sgemm<true, true>(p, t0 == 0, nullptr, nullptr, st)) != cudaSuccess) return e;
     int lists, part;
     row_segments(rows, a.V, &lists, &part);
     float* gmax = reinterpret_cast<float*>(ws + L.tops);
@@ -1206,24 +1217,38 @@ cudaError_t lp_backward(const LpBwd& a, char* ws, cudaStream_t st) {
     p.B = (const float*)a.W; p.ldb = a.d; p.N = a.V;
     p.K = a.d;
     p.C = Z; p.ldc = L.ldg;
-    if ((e = launch_sgemm<true, true>(p, nullptr, st)) != cudaSuccess) return e;
-    const int nseg = (int)ceil_div(a.V, 4096);
-    lp_g_f32_kernel<<<(unsigned)(rows * nseg), 256, 0, st>>>(Z, L.ldg, nseg, a.V, t0, a.y, a.mask, a.lse, a.ent, a.g_logp,
-                                                             a.g_lse, a.g_ent, a.inv_t, a.d_status);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    GradParams& g = p.grad;
+    g.y = a.y ? a.y + t0 : nullptr;
+    g.mask = a.mask ? a.mask + t0 : nullptr;
+    g.lse = a.lse + t0;
+    g.ent = a.ent ? a.ent + t0 : nullptr;
+    g.g_logp = a.g_logp ? a.g_logp + t0 : nullptr;
+    g.g_lse = a.g_lse ? a.g_lse + t0 : nullptr;
+    g.g_ent = a.g_ent ? a.g_ent + t0 : nullptr;
+    g.inv_t = a.inv_t;
+    g.V = a.V;
+    g.d_status = a.d_status;
+    if ((e = launch_sgemm<true, true, true>(p, t0 == 0, nullptr, nullptr, st)) != cudaSuccess) return e;
+    SplitSum sums[2];
     SgemmParams q{};                                           // dH = G W
     q.A = Z; q.lda = L.ldg; q.M = rows;
     q.B = (const float*)a.W; q.ldb = a.d; q.N = a.d;
     q.K = a.V;
     q.C = (float*)a.dH + t0 * a.d; q.ldc = a.d;
-    if ((e = launch_sgemm<true, false>(q, split, st)) != cudaSuccess) return e;
+    if ((e = launch_sgemm<true, false>(q, false, split, &sums[0], st)) != cudaSuccess) return e;
     SgemmParams r{};                                           // dW (+)= G^T H
     r.A = Z; r.lda = L.ldg; r.M = a.V;
     r.B = H; r.ldb = a.ldh; r.N = a.d;
     r.K = rows;
     r.C = (float*)a.dW; r.ldc = a.d; r.accumulate = (a.accumulate || t0 > 0) ? 1 : 0;
     r.b_mask = a.mask ? a.mask + t0 : nullptr;
-    if ((e = launch_sgemm<false, false>(r, split, st)) != cudaSuccess) return e;
+    if ((e = launch_sgemm<false, false>(r, false, split + kSplitBytes / 4, &sums[1], st)) != cudaSuccess) return e;
+    const int64_t n = sums[0].n > sums[1].n ? sums[0].n : sums[1].n;
+    if (n > 0) {
+      int64_t blocks = ceil_div(n, 256);
+      if (blocks > (int64_t)sm_count() * 8) blocks = (int64_t)sm_count() * 8;
+      if ((e = launch_dependent(sum_splits_kernel, dim3((unsigned)blocks, 2), dim3(256), st, sums[0], sums[1])) != cudaSuccess) return e;
+    }
   }
   return cudaSuccess;
 }
