@@ -373,90 +373,111 @@ def spo_loss_bwd_rows(H, W, y, lse, coef, grad_loss, rows, n_active, dH, dW, dW_
 MAX_TOP_K = 20
 
 
-def _need(name, t, dtype, shape, optional=False):
-    """Checks one tensor argument: its type, shape, layout and device (the current one)."""
-    import torch
-    if t is None:
-        if optional:
-            return
-        raise ValueError("%s is required" % name)
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
-        raise TypeError("%s must be a %s tensor, got %s" % (name, dtype, getattr(t, "dtype", type(t))))
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
-    _on_current_device(name, t)
+class _Args:
+    """Checks of one call's tensors: type, shape, layout and device (the current one).  The methods return addresses."""
 
+    __slots__ = ("torch", "device")
 
-def _on_current_device(name, t):
-    import torch
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise ValueError("%s must be on the current CUDA device, is on %s" % (name, t.device))
+    def __init__(self):
+        import torch
+        self.torch = torch
+        self.device = torch.cuda.current_device()
 
+    def here(self, name, t):
+        if t.get_device() != self.device:
+            raise ValueError("%s must be on the current CUDA device, is on %s" % (name, t.device))
 
-def _hidden_rows(H, W):
-    """Checks H [T, d] (rows contiguous, any row pitch) against W [V, d]; returns (T, d, V, row pitch of H)."""
-    import torch
-    if not isinstance(H, torch.Tensor) or not isinstance(W, torch.Tensor) or H.dim() != 2 or W.dim() != 2:
-        raise ValueError("H and W must be matrices")
-    (T, d), V = H.shape, W.shape[0]
-    _need("W", W, H.dtype, (V, d))
-    _on_current_device("H", H)
-    if T > 0 and d > 1 and H.stride(1) != 1:
-        raise ValueError("the rows of H must be contiguous")
-    ld = H.stride(0) if T > 1 else max(d, 1)
-    if ld < d:
-        raise ValueError("the rows of H overlap")
-    return T, d, V, ld
+    def need(self, name, t, dtype, shape):
+        try:                                    # the call that is right pays one pass over the conditions
+            if (dtype is None or t.dtype is dtype) and t.shape == shape and t.is_contiguous() and t.get_device() == self.device:
+                return t.data_ptr()
+        except AttributeError:
+            pass
+        if not isinstance(t, self.torch.Tensor):
+            raise TypeError("%s must be a tensor, got %s" % (name, type(t).__name__))
+        if dtype is not None and t.dtype is not dtype:
+            raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+        if t.shape != shape:
+            raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+        self.here(name, t)
+        return t.data_ptr()
 
+    def may(self, name, t, dtype, shape):
+        if t is None:
+            return None
+        return self.need(name, t, dtype, shape)
 
-def _scratch(ws):
-    import torch
-    if not isinstance(ws, torch.Tensor) or not ws.is_contiguous():
-        raise ValueError("ws must be a contiguous tensor")
-    _on_current_device("ws", ws)
-    return _ptr(ws), ws.numel() * ws.element_size()
+    def rows(self, H, W):
+        """H [T, d] (rows contiguous, any row pitch) against W [V, d]: (T, d, V, row pitch of H)."""
+        if not isinstance(H, self.torch.Tensor) or not isinstance(W, self.torch.Tensor) or H.dim() != 2 or W.dim() != 2:
+            raise ValueError("H and W must be matrices")
+        (T, d), V = H.shape, W.shape[0]
+        self.need("W", W, H.dtype, (V, d))
+        self.here("H", H)
+        if T > 0 and d > 1 and H.stride(1) != 1:
+            raise ValueError("the rows of H must be contiguous")
+        ld = H.stride(0) if T > 1 else max(d, 1)
+        if ld < d:
+            raise ValueError("the rows of H overlap")
+        return T, d, V, ld
+
+    def scratch(self, ws):
+        if not isinstance(ws, self.torch.Tensor) or not ws.is_contiguous():
+            raise ValueError("ws must be a contiguous tensor")
+        self.here("ws", ws)
+        return ws.data_ptr(), ws.numel() * ws.element_size()
+
+    def status(self, d_status):
+        if d_status is None:
+            return None
+        if not isinstance(d_status, self.torch.Tensor) or d_status.dtype is not self.torch.int32 or d_status.numel() < 1:
+            raise TypeError("d_status must be an int32 tensor")
+        self.here("d_status", d_status)
+        return d_status.data_ptr()
+
+    def stream(self):
+        raw = getattr(self.torch._C, "_cuda_getCurrentRawStream", None)      # without building a Stream object: 3 us
+        return raw(self.device) if raw else self.torch.cuda.current_stream().cuda_stream
 
 
 def spo_logprobs(H, W, y, mask, logp, lse, entropy, top_ids, top_logp, ws, d_status, inv_temperature=1.0):
     """Log-probabilities of the tokens y under softmax(inv_temperature * H W^T), with log-sum-exp and, where the
     tensors are given, entropy and the top_ids.shape[1] most likely alternatives.  H may be a slice of a wider buffer
     (rows contiguous); y and logp may both be None."""
-    import torch
-    T, d, V, ld = _hidden_rows(H, W)
+    c = _Args()
+    f32, i32 = c.torch.float32, c.torch.int32
+    T, d, V, ld = c.rows(H, W)
     K = 0 if top_ids is None else top_ids.shape[-1]
-    _need("y", y, torch.int32, (T,), optional=True)
-    _need("mask", mask, torch.uint8, (T,), optional=True)
-    _need("logp", logp, torch.float32, (T,), optional=True)
-    _need("lse", lse, torch.float32, (T,))
-    _need("entropy", entropy, torch.float32, (T,), optional=True)
-    _need("top_ids", top_ids, torch.int32, (T, K), optional=True)
-    _need("top_logp", top_logp, torch.float32, (T, K), optional=K == 0)
-    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
-    w, n = _scratch(ws)
-    _check(lib().spo_logprobs(_ptr(H), ld, _ptr(W), _dtype_code(W), _ptr(y), _ptr(mask), T, d, V, c_float(inv_temperature),
-                              K, _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(top_ids), _ptr(top_logp), w, n,
-                              _ptr(d_status), _stream()), "spo_logprobs")
+    if K == 0:
+        top_ids = top_logp = None
+    elif top_logp is None:
+        raise ValueError("top_logp is required with top_ids")
+    row = (T,)
+    w, n = c.scratch(ws)
+    rc = lib().spo_logprobs(
+        H.data_ptr(), ld, W.data_ptr(), _dtype_code(W), c.may("y", y, i32, row), c.may("mask", mask, c.torch.uint8, row), T, d, V,
+        inv_temperature, K, c.may("logp", logp, f32, row), c.need("lse", lse, f32, row), c.may("entropy", entropy, f32, row),
+        c.may("top_ids", top_ids, i32, (T, K)), c.may("top_logp", top_logp, f32, (T, K)), w, n, c.status(d_status), c.stream())
+    _check(rc, "spo_logprobs")
 
 
 def spo_logprobs_bwd(H, W, y, mask, lse, entropy, g_logp, g_lse, g_entropy, dH, dW, dW_accumulate, ws, d_status,
                      inv_temperature=1.0):
     """Gradients dH, dW of spo_logprobs for upstream gradients of logp, lse and entropy (None = zero)."""
-    import torch
-    T, d, V, ld = _hidden_rows(H, W)
-    for name, t in (("lse", lse), ("entropy", entropy), ("g_logp", g_logp), ("g_lse", g_lse), ("g_entropy", g_entropy)):
-        _need(name, t, torch.float32, (T,), optional=name != "lse")
-    _need("y", y, torch.int32, (T,), optional=True)
-    _need("mask", mask, torch.uint8, (T,), optional=True)
-    _need("dH", dH, dH.dtype, (T, d))
-    _need("dW", dW, dW.dtype, (V, d))
-    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
-    w, n = _scratch(ws)
-    _check(lib().spo_logprobs_bwd(_ptr(H), ld, _ptr(W), _dtype_code(W), _ptr(y), _ptr(mask), _ptr(lse), _ptr(entropy),
-                                  _ptr(g_logp), _ptr(g_lse), _ptr(g_entropy), T, d, V, c_float(inv_temperature),
-                                  _ptr(dH), _dtype_code(dH), _ptr(dW), _dtype_code(dW), int(dW_accumulate), w, n,
-                                  _ptr(d_status), _stream()), "spo_logprobs_bwd")
+    c = _Args()
+    f32 = c.torch.float32
+    T, d, V, ld = c.rows(H, W)
+    row = (T,)
+    w, n = c.scratch(ws)
+    rc = lib().spo_logprobs_bwd(
+        H.data_ptr(), ld, W.data_ptr(), _dtype_code(W), c.may("y", y, c.torch.int32, row), c.may("mask", mask, c.torch.uint8, row),
+        c.need("lse", lse, f32, row), c.may("entropy", entropy, f32, row), c.may("g_logp", g_logp, f32, row),
+        c.may("g_lse", g_lse, f32, row), c.may("g_entropy", g_entropy, f32, row), T, d, V, inv_temperature,
+        c.need("dH", dH, None, (T, d)), _dtype_code(dH), c.need("dW", dW, None, (V, d)), _dtype_code(dW), int(dW_accumulate), w, n,
+        c.status(d_status), c.stream())
+    _check(rc, "spo_logprobs_bwd")
 
 
 def default_muon_params(**overrides) -> SpoMuonParams:
@@ -477,24 +498,20 @@ def _matrices(G):
 
 def spo_orthogonalize(G, out, ws, params, d_status):
     """out = the Newton-Schulz orthogonalisation of the matrix (or of each matrix of the batch) G."""
-    import torch
+    c = _Args()
     b, m, n = _matrices(G)
-    _need("G", G, G.dtype, G.shape)
-    _need("out", out, out.dtype, G.shape)
-    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
-    w, nb = _scratch(ws)
-    _check(lib().spo_orthogonalize(_ptr(G), _dtype_code(G), b, m, n, _ptr(out), _dtype_code(out), w, nb,
-                                   ctypes.byref(params), _ptr(d_status), _stream()), "spo_orthogonalize")
+    w, nb = c.scratch(ws)
+    rc = lib().spo_orthogonalize(c.need("G", G, None, G.shape), _dtype_code(G), b, m, n, c.need("out", out, None, G.shape),
+                                 _dtype_code(out), w, nb, ctypes.byref(params), c.status(d_status), c.stream())
+    _check(rc, "spo_orthogonalize")
 
 
 def spo_muon_update(W, momentum, G, ws, params, d_status):
     """One Muon step of W (in place) for the gradient G, with the fp32 momentum buffer (in place)."""
-    import torch
+    c = _Args()
     b, m, n = _matrices(G)
-    _need("G", G, G.dtype, G.shape)
-    _need("W", W, W.dtype, G.shape)
-    _need("momentum", momentum, torch.float32, G.shape)
-    _need("d_status", d_status, torch.int32, d_status.shape if d_status is not None else (), optional=True)
-    w, nb = _scratch(ws)
-    _check(lib().spo_muon_update(_ptr(W), _dtype_code(W), _ptr(momentum), _ptr(G), _dtype_code(G), b, m, n, w, nb,
-                                 ctypes.byref(params), _ptr(d_status), _stream()), "spo_muon_update")
+    w, nb = c.scratch(ws)
+    rc = lib().spo_muon_update(c.need("W", W, None, G.shape), _dtype_code(W), c.need("momentum", momentum, c.torch.float32, G.shape),
+                               c.need("G", G, None, G.shape), _dtype_code(G), b, m, n, w, nb, ctypes.byref(params),
+                               c.status(d_status), c.stream())
+    _check(rc, "spo_muon_update")
