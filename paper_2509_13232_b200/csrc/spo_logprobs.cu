@@ -251,10 +251,10 @@ __device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, const LpRow
 }
 
 // The K largest logits of a row, from its groups of kGroup columns: the K groups of largest maximum hold them.  Group g covers
-// columns (g >> 1) tile_h + (g & 1) kGroup ..; gmax(g) is its maximum as a float (NaN and -inf: nothing in it counts).
+// columns (g >> 1) tile_h + (g & 1) kGroup .., stored from z[(g >> 1) pitch + (g & 1) kGroup] on; gmax(g) is its maximum as a float (NaN and -inf: nothing in it counts).
 constexpr int kGroup = 64;
 template <class Gmax>
-__device__ __forceinline__ void block_pick(const float* z, int groups, int tile_h, int32_t V, int K, Gmax gmax, TopSmem& sh,
+__device__ __forceinline__ void block_pick(const float* z, int64_t pitch, int groups, int tile_h, int32_t V, int K, Gmax gmax, TopSmem& sh,
                                            int* s_key, int* s_id) {
   block_top(groups, K, [&](int g) { return top_key(gmax(g)); }, [](int g) { return g; }, sh);
   constexpr int kSteps = kMaxTopK * kGroup / kTopThreads;
@@ -262,13 +262,17 @@ __device__ __forceinline__ void block_pick(const float* z, int groups, int tile_
   int id[kSteps];
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {                // fetched together
+    int64_t at = 0;
     const int i = threadIdx.x + u * kTopThreads, q = i / kGroup;
     id[u] = -1;
     if (q < K && sh.out_key[q] != kNoKey) {
       const int g = sh.out_id[q], c = (g & 1) * kGroup + i % kGroup;
-      if (c < tile_h && (g >> 1) * tile_h + c < V) id[u] = (g >> 1) * tile_h + c;
+      if (c < tile_h && (g >> 1) * tile_h + c < V) {
+        id[u] = (g >> 1) * tile_h + c;
+        at = (int64_t)(g >> 1) * pitch + c;
+      }
     }
-    x[u] = z[max(id[u], 0)];
+    x[u] = z[at];
   }
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
@@ -342,7 +346,7 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int
   warp_join_stats(m2, l, ez);
   if (lane == 0) { s_m[warp] = m2; s_l[warp] = l; s_e[warp] = ez; }
   __syncthreads();
-  if (nseg == 1 && K > 0) block_pick(z, groups, 128, V, K, [&](int g) { return s_gmax[g]; }, sh, s_key, s_id);
+  if (nseg == 1 && K > 0) block_pick(z, 128, groups, 128, V, K, [&](int g) { return s_gmax[g]; }, sh, s_key, s_id);
   if (warp != 0) return;
   m2 = lane < kRowWarps ? s_m[lane] : -CUDART_INF_F;
   l = lane < kRowWarps ? s_l[lane] : 0.0f;
@@ -452,7 +456,7 @@ lp_join_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t rows,
 // alternatives from the maxima of its groups.
 __global__ void __launch_bounds__(kTopThreads)
 lp_pick_kernel(const FwdPartial* __restrict__ partials, int lists, const float* __restrict__ gmax, int groups, int tile_h,
-               const float* __restrict__ Z, int64_t ldz, int64_t t0, const LpOut o) {
+               const float* __restrict__ Z, int64_t ldz, int64_t pitch, int64_t t0, const LpOut o) {
   __shared__ TopSmem sh;
   __shared__ int s_key[kMaxTopK * kGroup], s_id[kMaxTopK * kGroup];
   pdl_trigger();
@@ -464,7 +468,7 @@ lp_pick_kernel(const FwdPartial* __restrict__ partials, int lists, const float* 
   if (warp == 0) parts.fetch(partials, lists, [&](int s) { return row * lists + s; }, lane);
   if (o.K > 0) {
     const float* gm = gmax + row * groups;
-    block_pick(Z + row * ldz, groups, tile_h, o.V, o.K, [&](int g) { return gm[g]; }, sh, s_key, s_id);
+    block_pick(Z + row * ldz, pitch, groups, tile_h, o.V, o.K, [&](int g) { return gm[g]; }, sh, s_key, s_id);
   }
   if (warp != 0) return;
   float m2, l, ez, zt;
@@ -484,8 +488,8 @@ lp_pick_kernel(const FwdPartial* __restrict__ partials, int lists, const float* 
 // (half the traffic of token rows each) are slower, 207 against 197 us for one row, 217 against 207 for 48.
 // Reduction: eight warps turn the finished tile into [token][vocabulary row] in shared memory, then each takes
 // the tokens w, w + 8, .., two at a time: a lane holds four logits, the row's maximum and sums are warp reductions, lane k
-// keeps the running statistics of the warp's k-th token.  For the alternatives the tile's logits are stored ([token][V] fp32,
-// 4 T / (2 d) of W's bytes) with the maxima of their groups of 64; the K largest of a row lie in its K groups of largest
+// keeps the running statistics of the warp's k-th token.  For the alternatives the tile's logits are stored ([tile][token][128]
+// fp32, 4 T / (2 d) of W's bytes) with the maxima of their groups of 64; the K largest of a row lie in its K groups of largest
 // maximum, which lp_pick_kernel looks up.  (Keeping a sorted list per token row and CTA instead costs a chain of dependent
 // shuffles per tile: 128 rows with K = 20 took 438 us that way.)
 // ---------------------------------------------------------------------------
@@ -496,8 +500,7 @@ struct StreamParams {
   float sc2;
   const int32_t* y;
   FwdPartial* partials;                      // [T][gridDim.x]
-  float* Z;                                  // logits [T][ldz] and maxima of their groups [T][2 tiles]; NULL: not wanted
-  int64_t ldz;
+  float* Z;                                  // logits [tiles][T][128] and maxima of their groups [T][2 tiles]; NULL: not wanted
   float* gmax;
   int32_t* d_status;
 };
@@ -507,11 +510,11 @@ constexpr int kStreamThreads = 64 + 32 * kStreamWarps;
 constexpr int kStreamA = 128 * 64 * 2;
 template <int NT> struct StreamCfg {
   static constexpr int stage_bytes = kStreamA + NT * 128;
-  static constexpr int round = NT < 32 ? NT : 32;            // tokens reduced at a time
+  static constexpr int round = NT % 32 != 0 ? 16 : 32;       // tokens reduced at a time
   static constexpr int tile_bytes = round * 128 * 4;         // their logits, [token][128]
   static constexpr int stages = (226 * 1024 - tile_bytes - 2048) / stage_bytes;
   static constexpr int smem = stages * stage_bytes + tile_bytes + 1024 + 512;
-  static constexpr int tmem_cols = 2 * NT < 32 ? 32 : 2 * NT;
+  static constexpr int tmem_cols = NT <= 16 ? 32 : NT <= 32 ? 64 : NT <= 64 ? 128 : 256;
 };
 
 // Barrier of the reducing warps; every one of them arrives, and all leave with the same answer.
@@ -627,11 +630,11 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
             tmem_ld16(taddr + r * C::round + c, x);
 #pragma unroll
             for (int j = 0; j < 16; ++j) tile_z[(c + j) * 128 + quarter * 32 + lane] = __uint_as_float(x[j]);
-            if (p.Z && quarter * 32 + lane < cols) {
-              float* dst = p.Z + (int64_t)(r * C::round + c) * p.ldz + v0 + quarter * 32 + lane;
+            if (p.Z) {                                                    // whole lines, past the tile's last row too
+              float* dst = p.Z + ((int64_t)tile * p.T + r * C::round + c) * 128 + quarter * 32 + lane;
 #pragma unroll
               for (int j = 0; j < 16; ++j)
-                if (r * C::round + c + j < p.T) dst[(int64_t)j * p.ldz] = __uint_as_float(x[j]);
+                if (r * C::round + c + j < p.T) dst[j * 128] = __uint_as_float(x[j]);
             }
           }
           if (r == NT / C::round - 1) {
@@ -729,7 +732,7 @@ void stream_shape(int32_t V, int* grid, int* tile_h) {
 }
 
 template <int NT>
-cudaError_t launch_stream_t(const LpFwd& a, FwdPartial* partials, float* Z, int64_t ldz, float* gmax, cudaStream_t st) {
+cudaError_t launch_stream_t(const LpFwd& a, FwdPartial* partials, float* Z, float* gmax, cudaStream_t st) {
   using C = StreamCfg<NT>;
   static std::atomic<int> ready[64];
   int dev = 0;
@@ -755,7 +758,6 @@ cudaError_t launch_stream_t(const LpFwd& a, FwdPartial* partials, float* Z, int6
   p.y = a.y;
   p.partials = partials;
   p.Z = Z;
-  p.ldz = ldz;
   p.gmax = gmax;
   p.d_status = a.d_status;
   lp_stream_kernel<NT><<<grid, kStreamThreads, C::smem, st>>>(mW, mH, p);
@@ -778,17 +780,19 @@ cudaError_t launch_dependent(void (*kern)(P...), dim3 grid, dim3 block, cudaStre
 }
 
 // Z and gmax may be NULL when no alternatives are wanted.
-cudaError_t launch_stream(const LpFwd& a, const LpOut& o, FwdPartial* partials, float* Z, int64_t ldz, float* gmax, cudaStream_t st) {
+cudaError_t launch_stream(const LpFwd& a, const LpOut& o, FwdPartial* partials, float* Z, float* gmax, cudaStream_t st) {
   if (a.top_k == 0) Z = nullptr;
-  cudaError_t e = a.T <= 16   ? launch_stream_t<16>(a, partials, Z, ldz, gmax, st)
-                  : a.T <= 32 ? launch_stream_t<32>(a, partials, Z, ldz, gmax, st)
-                  : a.T <= 64 ? launch_stream_t<64>(a, partials, Z, ldz, gmax, st)
-                              : launch_stream_t<128>(a, partials, Z, ldz, gmax, st);
+  cudaError_t e = a.T <= 16   ? launch_stream_t<16>(a, partials, Z, gmax, st)
+                  : a.T <= 32 ? launch_stream_t<32>(a, partials, Z, gmax, st)
+                  : a.T <= 48 ? launch_stream_t<48>(a, partials, Z, gmax, st)
+                  : a.T <= 64 ? launch_stream_t<64>(a, partials, Z, gmax, st)
+                  : a.T <= 96 ? launch_stream_t<96>(a, partials, Z, gmax, st)
+                              : launch_stream_t<128>(a, partials, Z, gmax, st);
   if (e != cudaSuccess) return e;
   int grid, h;
   stream_shape(a.V, &grid, &h);
   return launch_dependent(lp_pick_kernel, dim3((unsigned)a.T), dim3(kTopThreads), st, partials, grid, gmax, 2 * (int)ceil_div(a.V, h),
-                          h, Z, ldz, (int64_t)0, o);
+                          h, Z, (int64_t)128, a.T * 128, (int64_t)0, o);
 }
 
 // ---------------------------------------------------------------------------
@@ -1052,7 +1056,7 @@ LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype)
     int grid, h;
     stream_shape(V, &grid, &h);
     L.partials = off; off = align_up(off + sizeof(FwdPartial) * (size_t)L.chunk * grid, 256);
-    L.ldz = pad4(V);
+    L.ldz = ceil_div(V, h) * 128;                                // a tile's logits on whole lines, behind one another
     L.z = L.tops = off;
     if (top_k > 0) {
       off = align_up(off + (size_t)L.chunk * L.ldz * 4, 256);
@@ -1176,7 +1180,7 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
       continue;
     }
     if (L.path == LP_STREAM)
-      return launch_stream(a, o, partials, reinterpret_cast<float*>(ws + L.z), L.ldz, reinterpret_cast<float*>(ws + L.tops), st);
+      return launch_stream(a, o, partials, reinterpret_cast<float*>(ws + L.z), reinterpret_cast<float*>(ws + L.tops), st);
     float* Z = reinterpret_cast<float*>(ws + L.z);
     SgemmParams p{};
     p.A = (const float*)a.H + t0 * a.ldh; p.lda = a.ldh; p.M = rows;
@@ -1192,7 +1196,7 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
                          partials, gmax, groups);
     if (e == cudaSuccess && lists > 1)
       e = launch_dependent(lp_pick_kernel, dim3((unsigned)rows), dim3(kTopThreads), st, partials, lists, gmax, groups, 128, Z, L.ldz,
-                           t0, o);
+                           (int64_t)128, t0, o);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
