@@ -1021,7 +1021,7 @@ sum_parts_kernel(const float4* __restrict__ src, int parts, int64_t quads, void*
 // scratch
 // ---------------------------------------------------------------------------
 constexpr int64_t kLpChunkRows = 18944;              // bf16 token rows per contraction launch: bounds the lists' scratch
-constexpr size_t kLpLogitBytes = (size_t)512 << 20;  // stored fp32 logits of one chunk of rows (fp32 path)
+constexpr size_t kLpLogitBytes = (size_t)256 << 20;  // stored fp32 logits of one chunk of rows (fp32 path)
 
 int64_t pad4(int64_t v) { return (v + 3) / 4 * 4; }
 
