@@ -37,8 +37,8 @@ __device__ __forceinline__ void flag(int32_t* d_status, int32_t bit) {
 }
 
 // ---------------------------------------------------------------------------
-// The K largest of n candidates (value descending, equal values by ascending id), found by a block of 256 threads.
-// Every eight threads take the maximum of their share; the K-th largest of these 32 distinct candidates bounds the K-th
+// The K largest of n candidates (value descending, equal values by ascending id), found by a block of TH threads.
+// Every TH / 32 threads take the maximum of their share; the K-th largest of these 32 distinct candidates bounds the K-th
 // largest of all from below, and usually little more than K candidates reach it (31 for K = 20).  They are collected and
 // each counts how many precede it.  No step is a chain of dependent comparisons (sorted lists kept by insertion took 30 us
 // for 5000 candidates, this takes 3).  When more than 256 reach the bound (many equal values, or one thread's
@@ -46,11 +46,14 @@ __device__ __forceinline__ void flag(int32_t* d_status, int32_t bit) {
 // ---------------------------------------------------------------------------
 constexpr int kTopThreads = 256;
 constexpr int kTopKept = 12;
+constexpr int kTopFew = 48;
+constexpr int kTopRoom = 256;             // candidates that are ranked
 static_assert(SPO_MAX_TOP_K <= 32, "the bound is one of 32 maxima");
 constexpr int kNoKey = -0x7FFFFFFF - 1;
+template <int TH>
 struct __align__(16) TopSmem {
-  int key[kTopThreads], id[kTopThreads], at[kTopThreads];
-  int count[2][kTopThreads / 32];
+  int key[kTopRoom], id[kTopRoom], at[kTopRoom];
+  int count[2][TH / 32];
   int n;
   int out_key[kMaxTopK], out_id[kMaxTopK], out_at[kMaxTopK];     // out_key kNoKey: fewer than that many candidates
 };
@@ -60,22 +63,23 @@ __device__ __forceinline__ int order_key(int b) { return b ^ ((b >> 31) & 0x7FFF
 // The same for a logit that may be listed: -0 counts as 0; NaN and -inf are no candidates.
 __device__ __forceinline__ int top_key(float x) { return x > -CUDART_INF_F ? order_key(__float_as_int(x + 0.0f)) : kNoKey; }
 
-template <class Pred>
-__device__ __forceinline__ int block_count(int n, Pred pred, TopSmem& sh, int& buf) {
+template <int TH, class Pred>
+__device__ __forceinline__ int block_count(int n, Pred pred, TopSmem<TH>& sh, int& buf) {
   int c = 0;
-  for (int i = threadIdx.x; i < n; i += kTopThreads) c += pred(i) ? 1 : 0;
+  for (int i = threadIdx.x; i < n; i += TH) c += pred(i) ? 1 : 0;
   c = __reduce_add_sync(0xffffffffu, c);
   if ((threadIdx.x & 31) == 0) sh.count[buf][threadIdx.x >> 5] = c;
   __syncthreads();
   int total = 0;
 #pragma unroll
-  for (int w = 0; w < kTopThreads / 32; ++w) total += sh.count[buf][w];
+  for (int w = 0; w < TH / 32; ++w) total += sh.count[buf][w];
   buf ^= 1;
   return total;
 }
 
 // How many of the first n entries of sh.key / sh.id precede (k, d).
-__device__ __forceinline__ int rank_of(int k, int d, int n, const TopSmem& sh) {
+template <int TH>
+__device__ __forceinline__ int rank_of(int k, int d, int n, const TopSmem<TH>& sh) {
   int before = 0;
 #pragma unroll 4
   for (int q = 0; q < (n + 3) / 4; ++q) {
@@ -87,8 +91,8 @@ __device__ __forceinline__ int rank_of(int k, int d, int n, const TopSmem& sh) {
 }
 
 // key(i) is candidate i's top_key, id(i) its id (distinct).  Results in sh.out_*, after a barrier; every thread calls it.
-template <class Key, class Id>
-__device__ __forceinline__ void block_top(int n, int K, Key key, Id id, TopSmem& sh) {
+template <int TH, class Key, class Id>
+__device__ __forceinline__ void block_top(int n, int K, Key key, Id id, TopSmem<TH>& sh) {
   const int tid = threadIdx.x;
   __syncthreads();                                  // the caller is done with what sh held
   if (tid == 0) sh.n = 0;
@@ -96,34 +100,33 @@ __device__ __forceinline__ void block_top(int n, int K, Key key, Id id, TopSmem&
   int bound = kNoKey;
   int kept[kTopKept];                               // the first candidates of this thread, fetched together
   kept[0] = key(min(tid, n - 1));
-  if (n > kTopThreads) {
-#pragma unroll
-    for (int u = 1; u < kTopKept; ++u) kept[u] = key(min(tid + u * kTopThreads, n - 1));
+  if (tid >= n) kept[0] = kNoKey;
+  if (n > kTopFew) {
     int m = kept[0];
+    if (n > TH) {
 #pragma unroll
-    for (int u = 1; u < kTopKept; ++u) {
-      if (tid + u * kTopThreads >= n) kept[u] = kNoKey;
-      m = max(m, kept[u]);
-    }
+      for (int u = 1; u < kTopKept; ++u) kept[u] = key(min(tid + u * TH, n - 1));
+#pragma unroll
+      for (int u = 1; u < kTopKept; ++u) {
+        if (tid + u * TH >= n) kept[u] = kNoKey;
+        m = max(m, kept[u]);
+      }
 #pragma unroll 4
-    for (int i = tid + kTopKept * kTopThreads; i < n; i += kTopThreads) m = max(m, key(i));
-#pragma unroll
-    for (int o = 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if ((tid & 7) == 0) sh.key[tid >> 3] = m;
+      for (int i = tid + kTopKept * TH; i < n; i += TH) m = max(m, key(i));
+    }
+    sh.key[tid] = m;
     __syncthreads();
-    m = sh.key[tid & 31];
+    const int lane = tid & 31;
+#pragma unroll
+    for (int w = 0; w < TH / 32; ++w) m = max(m, sh.key[w * 32 + lane]);     // of the threads of this lane
     int before = 0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int4 k4 = reinterpret_cast<const int4*>(sh.key)[q];
-      const int me = tid & 31;
-      before += (k4.x > m || (k4.x == m && 4 * q < me)) + (k4.y > m || (k4.y == m && 4 * q + 1 < me)) +
-                (k4.z > m || (k4.z == m && 4 * q + 2 < me)) + (k4.w > m || (k4.w == m && 4 * q + 3 < me));
+    for (int q = 0; q < 32; ++q) {
+      const int other = __shfl_sync(0xffffffffu, m, q);
+      before += other > m || (other == m && q < lane);
     }
     bound = __shfl_sync(0xffffffffu, m, __ffs(__ballot_sync(0xffffffffu, before == K - 1)) - 1);
     __syncthreads();
-  } else if (tid >= n) {
-    kept[0] = kNoKey;
   }
   int last_id = 0x7FFFFFFF;                         // of the candidates at the bound, those up to this id count
   auto take = [&](int i, int k) {
@@ -131,24 +134,27 @@ __device__ __forceinline__ void block_top(int n, int K, Key key, Id id, TopSmem&
     const int d = id(i);
     if (k == bound && d > last_id) return;
     const int at = atomicAdd(&sh.n, 1);
-    if (at < kTopThreads) { sh.key[at] = k; sh.id[at] = d; sh.at[at] = i; }
+    if (at < kTopRoom) { sh.key[at] = k; sh.id[at] = d; sh.at[at] = i; }
   };
   auto collect = [&]() {
+    take(tid, kept[0]);
+    if (n > TH) {
 #pragma unroll
-    for (int u = 0; u < kTopKept; ++u) take(tid + u * kTopThreads, kept[u]);
-    for (int i = tid + kTopKept * kTopThreads; i < n; i += kTopThreads) take(i, key(i));
+      for (int u = 1; u < kTopKept; ++u) take(tid + u * TH, kept[u]);
+    }
+    for (int i = tid + kTopKept * TH; i < n; i += TH) take(i, key(i));
     __syncthreads();
   };
-  if (n > kTopThreads) {
+  if (n > kTopFew) {
     collect();
-  } else {                                          // every thread has one candidate or none
+  } else {                                          // so few that ranking all is less than looking for a bound
     sh.key[tid] = kept[0];
     sh.id[tid] = tid < n ? id(tid) : 0;
     sh.at[tid] = tid;
     if (tid == 0) sh.n = n;
     __syncthreads();
   }
-  if (sh.n > kTopThreads) {
+  if (sh.n > kTopRoom) {
     int buf = 0;
     long long lo = bound, hi = 0x7FFFFFFF;          // the largest bound that K candidates reach
     while (lo < hi) {
@@ -168,14 +174,13 @@ __device__ __forceinline__ void block_top(int n, int K, Key key, Id id, TopSmem&
     collect();
   }
   const int total = sh.n;
-  if (tid >= total && tid < ((total + 3) & ~3)) sh.key[tid] = kNoKey;             // rank_of takes four at a time
+  if (tid < 4 && total + tid < ((total + 3) & ~3)) sh.key[total + tid] = kNoKey;      // rank_of takes four at a time
   __syncthreads();
-  if (tid < total) {
-    const int k = sh.key[tid], d = sh.id[tid];
-    if (k != kNoKey) {
-      const int before = rank_of(k, d, total, sh);
-      if (before < K) { sh.out_key[before] = k; sh.out_id[before] = d; sh.out_at[before] = sh.at[tid]; }
-    }
+  for (int c = tid; c < total; c += TH) {
+    const int k = sh.key[c], d = sh.id[c];
+    if (k == kNoKey) continue;
+    const int before = rank_of(k, d, total, sh);
+    if (before < K) { sh.out_key[before] = k; sh.out_id[before] = d; sh.out_at[before] = sh.at[c]; }
   }
   __syncthreads();
 }
@@ -223,8 +228,9 @@ struct LpRow {
 };
 
 // Outputs of token t from its joined statistics and the selected alternatives; one whole warp calls it.
+template <int TH>
 __device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, const LpRow& r, float m2, float l, float ez, float zt, bool odd,
-                                          const TopSmem& top, int lane) {
+                                          const TopSmem<TH>& top, int lane) {
   float lse = (m2 + log2f(l)) * kLn2;
   if (odd) lse = CUDART_NAN_F;
   const bool on = r.on;
@@ -254,7 +260,7 @@ __device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, const LpRow
 // columns (g >> 1) tile_h + (g & 1) kGroup .., stored from z[(g >> 1) pitch + (g & 1) kGroup] on; gmax(g) is its maximum as a float (NaN and -inf: nothing in it counts).
 constexpr int kGroup = 64;
 template <class Gmax>
-__device__ __forceinline__ void block_pick(const float* z, int64_t pitch, int groups, int tile_h, int32_t V, int K, Gmax gmax, TopSmem& sh,
+__device__ __forceinline__ void block_pick(const float* z, int64_t pitch, int groups, int tile_h, int32_t V, int K, Gmax gmax, TopSmem<kTopThreads>& sh,
                                            int* s_key, int* s_id) {
   block_top(groups, K, [&](int g) { return top_key(gmax(g)); }, [](int g) { return g; }, sh);
   constexpr int kSteps = kMaxTopK * kGroup / kTopThreads;
@@ -293,7 +299,7 @@ constexpr int kRowGroups = kRowWarps * 4096 / kGroup;      // groups of a row th
 __global__ void __launch_bounds__(32 * kRowWarps)
 lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int64_t t0, const LpOut o,
                FwdPartial* __restrict__ partials, float* __restrict__ gmax, int groups) {
-  __shared__ TopSmem sh;
+  __shared__ TopSmem<kTopThreads> sh;
   __shared__ int s_key[kMaxTopK * kGroup], s_id[kMaxTopK * kGroup];
   __shared__ float s_gmax[kRowGroups];
   __shared__ float s_m[kRowWarps], s_l[kRowWarps], s_e[kRowWarps];
@@ -396,10 +402,12 @@ struct RowParts {
 // The end of the tiled path, a block per token row: joins the row's partials ([list][rows]) and picks the alternatives from
 // its lists of column groups (maximum, group << 8 | slot), whose 32 logits each are stored in `cand`.
 // ---------------------------------------------------------------------------
-__global__ void __launch_bounds__(kTopThreads)
+constexpr int kMergeThreads = 128;        // half of what the others use: many rows with a hundred or two entries each
+template <int LIST>
+__global__ void __launch_bounds__(kMergeThreads)
 lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, const float2* __restrict__ tops, const float* __restrict__ cand,
-                int list_len, int64_t rows, int64_t t0, const LpOut o) {
-  __shared__ TopSmem sh;
+                int64_t rows, int64_t t0, const LpOut o) {
+  __shared__ TopSmem<kMergeThreads> sh;
   __shared__ int s_key[kMaxTopK * 32], s_id[kMaxTopK * 32];
   pdl_trigger();
   pdl_wait();
@@ -409,18 +417,20 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, const float2
   RowParts parts;
   if (warp == 0) parts.fetch(partials, lists, [&](int s) { return (int64_t)s * rows + row; }, lane);
   {
+    // All lists' first entries, then their second ones, ..: the shares that give the bound are alike that way (list by list,
+    // a share would hold the same few places of every list).
     auto entry = [&](int i) {
-      const int s = i / list_len;
-      return tops[((int64_t)s * rows + row) * list_len + (i - s * list_len)];
+      const int k = i / lists;
+      return tops[((int64_t)(i - k * lists) * rows + row) * LIST + k];
     };
-    block_top(lists * list_len, K, [&](int i) { return top_key(entry(i).x); },
+    block_top(lists * LIST, K, [&](int i) { return top_key(entry(i).x); },
               [&](int i) { return (int)(__float_as_uint(entry(i).y) >> 8); }, sh);
-    for (int i = threadIdx.x; i < K * 32; i += kTopThreads) {
+    for (int i = threadIdx.x; i < K * 32; i += kMergeThreads) {
       int key = kNoKey, id = 0;
       if (sh.out_key[i >> 5] != kNoKey) {
-        const int at = sh.out_at[i >> 5], s = at / list_len, slot = (int)(__float_as_uint(entry(at).y) & 255u);
+        const int at = sh.out_at[i >> 5], s = at % lists, slot = (int)(__float_as_uint(entry(at).y) & 255u);
         id = sh.out_id[i >> 5] * 32 + (i & 31);
-        if (id < o.V) key = top_key(cand[(((int64_t)s * rows + row) * list_len + slot) * 32 + (i & 31)]);
+        if (id < o.V) key = top_key(cand[(((int64_t)s * rows + row) * LIST + slot) * 32 + (i & 31)]);
       }
       s_key[i] = key;
       s_id[i] = id;
@@ -437,7 +447,7 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, const float2
 // The same for rows of which one warp joins the partials and no alternatives are wanted.
 __global__ void __launch_bounds__(128)
 lp_join_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t rows, int64_t t0, const LpOut o) {
-  __shared__ TopSmem none;                          // not read: K = 0
+  __shared__ TopSmem<32> none;                          // not read: K = 0
   pdl_trigger();
   pdl_wait();
   const int lane = threadIdx.x & 31;
@@ -457,7 +467,7 @@ lp_join_kernel(const FwdPartial* __restrict__ partials, int lists, int64_t rows,
 __global__ void __launch_bounds__(kTopThreads)
 lp_pick_kernel(const FwdPartial* __restrict__ partials, int lists, const float* __restrict__ gmax, int groups, int tile_h,
                const float* __restrict__ Z, int64_t ldz, int64_t pitch, int64_t t0, const LpOut o) {
-  __shared__ TopSmem sh;
+  __shared__ TopSmem<kTopThreads> sh;
   __shared__ int s_key[kMaxTopK * kGroup], s_id[kMaxTopK * kGroup];
   pdl_trigger();
   pdl_wait();
@@ -1174,8 +1184,8 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
       if (e == cudaSuccess && a.top_k == 0)
         e = launch_dependent(lp_join_kernel, dim3((unsigned)ceil_div(rows, 4)), dim3(128), st, partials, lists, rows, t0, o);
       else if (e == cudaSuccess)
-        e = launch_dependent(lp_merge_kernel, dim3((unsigned)rows), dim3(kTopThreads), st, partials, lists, tops, cand,
-                             lp_list_len(a.top_k), rows, t0, o);
+        e = launch_dependent(lp_list_len(a.top_k) == 8 ? lp_merge_kernel<8> : lp_merge_kernel<kMaxTopK>, dim3((unsigned)rows),
+                             dim3(kMergeThreads), st, partials, lists, tops, cand, rows, t0, o);
       if (e != cudaSuccess) return e;
       continue;
     }

@@ -65,6 +65,9 @@ constexpr int A_BYTES = BM * BK * 2;                 // 16 KB
 constexpr int BSUB_ROWS = HALF_N / CG;               // B columns per CTA per half (128)
 constexpr int BSUB_BYTES = BSUB_ROWS * BK * 2;       // 16 KB
 constexpr int STAGE_BYTES = A_BYTES + 2 * BSUB_BYTES;  // 48 KB
+constexpr int RING_BYTES = STAGES * STAGE_BYTES;
+constexpr int kWideStages = STAGES;
+constexpr int kNarrowStages = RING_BYTES / (A_BYTES + BSUB_BYTES);   // 256-column tiles
 constexpr int EPI_WARPS = 8;
 constexpr int PACER_WARP = 2 + EPI_WARPS;              // last warp: keeps the pairs' loads close together in time
 constexpr int NUM_THREADS = 32 * (3 + EPI_WARPS);
@@ -254,21 +257,30 @@ __device__ __forceinline__ Unit unit_of(int u, const GemmParams& p) {
 // rows has a group above its last entry, and a listed group's 32 logits are stored once, when it enters.
 // (A list of the logits themselves would be touched by nearly every group of 32 rows x 32 columns, in a
 // scan of every logit.)  G: general upstream gradients.  DW: bf16 result.  DH: the contraction split along k.
-template <int MODE, bool ENT = false, int LP = -1>
+// NARROW (log-probability operators): tiles of 256 x 256 with two accumulators and six stages, so that a tile's epilogue
+// runs under the next one's products, for contractions too short to carry it otherwise (see lp_narrow).
+template <int MODE, bool ENT = false, int LP = -1, bool NARROW = false>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
 spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmParams p) {
   constexpr bool A_MN = (MODE == MODE_DW);
   constexpr bool B_MN = (MODE == MODE_DH || MODE == MODE_DW);
+  constexpr int MMAS = NARROW ? 1 : 2;                        // products of 256 columns per k-step
+  constexpr int BN = MMAS * HALF_N;                           // columns of a tile
+  constexpr int EPI_N = BN / 2;                               // columns of an epilogue warp
+  constexpr int BUFS = NARROW ? 2 : 1;                        // accumulators
+  constexpr int STAGE_BYTES = A_BYTES + MMAS * BSUB_BYTES;
+  constexpr int STAGES = NARROW ? kNarrowStages : kWideStages;
+  static_assert(STAGES * STAGE_BYTES == RING_BYTES && 16 * STAGES + 80 <= 256, "shared memory");
 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - raw);
   const uint32_t bars = base + STAGES * STAGE_BYTES;
-  const uint32_t full0 = bars, empty0 = bars + 8 * STAGES, tfull = bars + 16 * STAGES, tempty = tfull + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + STAGES * STAGE_BYTES + 16 * STAGES + 16);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + STAGES * STAGE_BYTES + 16 * STAGES + 24);
-  volatile uint32_t* pace_mine = reinterpret_cast<volatile uint32_t*>(gen + STAGES * STAGE_BYTES + 16 * STAGES + 32);
+  const uint32_t full0 = bars, empty0 = bars + 8 * STAGES, tfull0 = bars + 16 * STAGES, tempty0 = tfull0 + 8 * BUFS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(gen + RING_BYTES + 16 * STAGES + 16 * BUFS);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(gen + RING_BYTES + 16 * STAGES + 16 * BUFS + 8);
+  volatile uint32_t* pace_mine = reinterpret_cast<volatile uint32_t*>(gen + RING_BYTES + 16 * STAGES + 16 * BUFS + 16);
   volatile uint32_t* pace_limit = pace_mine + 1;   // k-blocks this pair's producer may have issued (pacer -> producer)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -279,8 +291,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
-    mbar_init(tfull, 1);
-    mbar_init(tempty, EPI_WARPS * CG);
+    for (int b = 0; b < BUFS; ++b) { mbar_init(tfull0 + 8 * b, 1); mbar_init(tempty0 + 8 * b, EPI_WARPS * CG); }
     *abort_flag = 0;
     *pace_mine = 0;
     *pace_limit = p.progress ? (uint32_t)p.window : 0xFFFFFFFFu;
@@ -337,7 +348,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                   tma_load_2d(sa + b * 8192, &tmA, row_base + b * 64, p.a_row0 + kb * BK, fb);
               }
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
+              for (int h = 0; h < MMAS; ++h) {
                 const uint32_t sbh = sb + h * BSUB_BYTES;
                 const int col = col_base + h * HALF_N;
                 if (!B_MN) {
@@ -365,7 +376,8 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const Unit un = unit_of(KS ? u / p.k_splits : u, p);
         const int kb0 = KS ? (u % p.k_splits) * p.k_per : 0, kb1 = KS ? min(kb0 + p.k_per, p.k_blocks) : p.k_blocks;
         for (int n = un.n_begin; n < un.n_end && ok; ++n, ++tile) {
-          if (!mbar_wait(tempty, (tile & 1u) ^ 1u, abort_flag, p.d_status)) { ok = false; break; }
+          const uint32_t buf = tile % BUFS;
+          if (!mbar_wait(tempty0 + 8 * buf, ((tile / BUFS) & 1u) ^ 1u, abort_flag, p.d_status)) { ok = false; break; }
           tc_fence_after();
           for (int kb = kb0; kb < kb1; ++kb, ++it) {
             const uint32_t s = it % STAGES, ph = (it / STAGES) & 1u;
@@ -376,27 +388,26 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             for (int j = 0; j < BK / 16; ++j) {
               const uint64_t da = A_MN ? smem_desc(sa + j * 2048, 8192, 1024) : smem_desc(sa + j * 32, 16, 1024);
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
+              for (int h = 0; h < MMAS; ++h) {
                 const uint32_t sbh = sb + h * BSUB_BYTES;
                 const uint64_t db = B_MN ? smem_desc(sbh + j * 2048, 8192, 1024) : smem_desc(sbh + j * 32, 16, 1024);
-                umma_bf16(tmem_base + h * HALF_N, da, db, idesc, ((kb - kb0) | j) != 0 ? 1u : 0u);
+                umma_bf16(tmem_base + (buf + h) * HALF_N, da, db, idesc, ((kb - kb0) | j) != 0 ? 1u : 0u);
               }
             }
             umma_commit(empty0 + 8 * s);
           }
-          if (ok) umma_commit(tfull);
+          if (ok) umma_commit(tfull0 + 8 * buf);
         }
       }
     }
   } else if (warp < 2 + EPI_WARPS) {
     // ------------------------------------------------------------------ epilogue (warps 2..9)
     const int quarter = warp & 3;                            // tensor-memory lanes this warp may read
-    const int half = (warp - 2) >> 2;                        // which 256-column half of the tile
+    const int half = (warp - 2) >> 2;                        // which half of the tile's columns
     const int row = (int)rank * BM + quarter * 32 + lane;    // row of the pair's tile
     const int warp_row0 = (int)rank * BM + quarter * 32;     // tile row of the warp's first lane
-    uint8_t* stage = gen + STAGES * STAGE_BYTES + 256 + (warp - 2) * STAGING_BYTES;
-    const uint32_t tempty_leader = map_to_cta(tempty, 0);
-    const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * HALF_N;
+    uint8_t* stage = gen + RING_BYTES + 256 + (warp - 2) * STAGING_BYTES;
+    const uint32_t tempty_leader = map_to_cta(tempty0, 0);
     uint32_t tile = 0;
     bool ok = true;
     for (int u = group; u < total_units && ok; u += n_groups) {
@@ -454,15 +465,17 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       for (int n = un.n_begin; n < un.n_end && ok; ++n, ++tile) {
         {                                   // one lane polls (with backoff); the warp reconverges on the outcome
           int good = 1;
-          if (lane == 0) good = mbar_wait<kEpilogueSleepNs>(tfull, tile & 1u, abort_flag, p.d_status) ? 1 : 0;
+          if (lane == 0)
+            good = mbar_wait<kEpilogueSleepNs>(tfull0 + 8 * (tile % BUFS), (tile / BUFS) & 1u, abort_flag, p.d_status) ? 1 : 0;
           good = __shfl_sync(0xffffffffu, good, 0);
           if (!good) { ok = false; break; }
         }
         tc_fence_after();
-        const int col_half = n * BN + half * HALF_N;
+        const int col_half = n * BN + half * EPI_N;
+        const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (tile % BUFS) * HALF_N + half * EPI_N;
         if (MODE == MODE_FWD) {
 #pragma unroll 1
-          for (int ch = 0; ch < HALF_N / 32; ++ch) {
+          for (int ch = 0; ch < EPI_N / 32; ++ch) {
             const int col0 = col_half + ch * 32;
             if (col0 >= p.cols_valid) break;                           // nothing valid further right
             uint32_t v[32];
@@ -538,7 +551,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           __nv_bfloat16* obase = p.G + ((int64_t)(un.m_tile - p.m_tile0) * GROUP_M + warp_row0) * p.ldg;
           const float neg = -m2;
 #pragma unroll 1
-          for (int r2 = 0; r2 < HALF_N / 64; ++r2) {
+          for (int r2 = 0; r2 < EPI_N / 64; ++r2) {
             const int col0 = col_half + r2 * 64;
             uint4 piece[8];
             if (col0 < p.cols_valid) {
@@ -607,7 +620,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               : reinterpret_cast<__nv_bfloat16*>(p.out) + grow_warp0 * p.ldo;
           const int64_t ld = MODE == MODE_G ? p.ldg : p.ldo;
 #pragma unroll 1
-          for (int r2 = 0; r2 < HALF_N / 64; ++r2) {
+          for (int r2 = 0; r2 < EPI_N / 64; ++r2) {
             const int col0 = col_half + r2 * 64;
             if (MODE != MODE_G && col0 >= p.cols_valid) break;
             uint32_t v0[32], v1[32];
@@ -651,7 +664,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
           // fp32 outputs: 32 columns (128 bytes per row) per staging round; dW may accumulate
           float* obase = reinterpret_cast<float*>(p.out) + grow_warp0 * p.ldo + (KS ? (u % p.k_splits) * p.rows_valid * p.ldo : 0);
 #pragma unroll 1
-          for (int ch = 0; ch < HALF_N / 32; ++ch) {
+          for (int ch = 0; ch < EPI_N / 32; ++ch) {
             const int col0 = col_half + ch * 32;
             if (col0 >= p.cols_valid) break;
             uint32_t v[32];
@@ -721,7 +734,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(tempty_leader);
+        if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * (tile % BUFS));
       }
       if ((MODE == MODE_FWD || MODE == MODE_E) && ok && row_ok) {
         FwdPartial part;
@@ -814,7 +827,7 @@ int group_count() { return sm_count() / CG; }
 // CTA pairs of this instantiation that can be resident together on a device (0 = not yet asked).
 // The kernel is persistent and its pairs pace one another, so a grid must not exceed it.  One slot
 // per device, filled once; concurrent first calls compute the same value (atomic stores).
-template <int MODE, bool ENT, int LP>
+template <int MODE, bool ENT, int LP, bool NARROW>
 cudaError_t resident_groups(int* out) {
   static std::atomic<int> cached[64];
   int dev = 0;
@@ -823,7 +836,7 @@ cudaError_t resident_groups(int* out) {
   if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   int n = cached[dev].load(std::memory_order_acquire);
   if (n == 0) {
-    e = cudaFuncSetAttribute(spo_gemm_kernel<MODE, ENT, LP>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+    e = cudaFuncSetAttribute(spo_gemm_kernel<MODE, ENT, LP, NARROW>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t q = {};
     q.gridDim = dim3(group_count() * CG, 1, 1);
@@ -836,7 +849,7 @@ cudaError_t resident_groups(int* out) {
     qa[0].val.clusterDim.z = 1;
     q.attrs = qa;
     q.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(&n, spo_gemm_kernel<MODE, ENT, LP>, &q);
+    e = cudaOccupancyMaxActiveClusters(&n, spo_gemm_kernel<MODE, ENT, LP, NARROW>, &q);
     if (e != cudaSuccess) return e;
     if (n < 1) return cudaErrorLaunchOutOfResources;
     if (n > group_count()) n = group_count();
@@ -846,11 +859,11 @@ cudaError_t resident_groups(int* out) {
   return cudaSuccess;
 }
 
-template <int MODE, bool ENT = false, int LP = -1>
+template <int MODE, bool ENT = false, int LP = -1, bool NARROW = false>
 cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmParams& p_in, uint32_t* progress,
                         cudaStream_t st) {
   int max_groups = 0;
-  cudaError_t e0 = resident_groups<MODE, ENT, LP>(&max_groups);
+  cudaError_t e0 = resident_groups<MODE, ENT, LP, NARROW>(&max_groups);
   if (e0 != cudaSuccess) return e0;
   const int units = p_in.m_tiles * p_in.nsplit * (MODE == MODE_DH && LP >= 0 ? p_in.k_splits : 1);
   if (units <= 0) return cudaSuccess;
@@ -878,7 +891,7 @@ cudaError_t launch_gemm(const CUtensorMap& a, const CUtensorMap& b, const GemmPa
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, spo_gemm_kernel<MODE, ENT, LP>, a, b, p);
+  return cudaLaunchKernelEx(&cfg, spo_gemm_kernel<MODE, ENT, LP, NARROW>, a, b, p);
 }
 
 // Operand box heights (rows per TMA box) for K-major operands.
@@ -1079,20 +1092,23 @@ cudaError_t launch_bwd_bf16(const void* H, const void* W, const int32_t* y, cons
 // ---------------------------------------------------------------------------
 int lp_list_len(int top_k) { return top_k == 0 ? 0 : top_k <= 8 ? 8 : kMaxTopK; }
 
-// Splits of the vocabulary tiles.  A few row tiles stream W once whatever the split (its tiles are not read
+#ifndef SPO_TUNE_LP_NARROW
+#define SPO_TUNE_LP_NARROW 1024
+#endif
+// Splits of the vocabulary tiles of `bn` columns.  A few row tiles stream W once whatever the split (its tiles are not read
 // again), so only the number of tiles that the busiest pair gets counts; with many row tiles the pairs re-read W and
 // pick_fwd_split weighs the L2 footprint.  (129 rows at d = 4096, V = 151936: 1001 us with the latter's 12 splits, which
 // leave 62 pairs idle, 263 us with 60.)
-static int lp_split(int64_t rows, int32_t d, int32_t V) {
+static int lp_split(int64_t rows, int32_t d, int32_t V, int bn) {
   const int64_t m_tiles = ceil_div(rows, GROUP_M);
-  const int n_tiles = (int)ceil_div(V, BN), groups = group_count();
+  const int n_tiles = (int)ceil_div(V, bn), groups = group_count();
   if (m_tiles * 4 > groups) {
     const int ns = pick_fwd_split(m_tiles, n_tiles, d);
     if (ns <= 80) return ns;                                       // (a row's partials: at most 160)
   }
   int best = 1;
   int64_t best_cost = INT64_MAX;
-  for (int ns = 1; ns <= n_tiles && ns <= groups && ns <= 80; ++ns) {         // (a row's partials: at most 160)
+  for (int ns = 1; ns <= n_tiles && ns <= groups && ns <= 80; ++ns) {
     const int64_t per = ceil_div(n_tiles, ns);
     if (ceil_div(n_tiles, per) != ns) continue;                    // not a distinct partition
     const int64_t cost = per * ceil_div(m_tiles * ns, groups);
@@ -1101,11 +1117,29 @@ static int lp_split(int64_t rows, int32_t d, int32_t V) {
   return best;
 }
 
-int lp_fwd_lists(int64_t rows, int32_t d, int32_t V) { return 2 * lp_split(rows, d, V); }
+// Tiles of 256 columns instead of 512 for a contraction of `k` products: an epilogue of a 512-column tile takes 5 us
+// (statistics) to 10 us (stored gradient), its products k / 64 x 0.61 us.  Up to k = 1024 hiding the epilogue is worth the
+// narrow tile's third more operand traffic: forward of 3000 rows at V = 32000, d = 512 120 us wide, 90 narrow; d = 1024
+// 170 / 157; forward and backward of 1531 rows at V = 151936, d = 1024 366 / 368 and 1133 / 1109; d = 2048 677 / 724 and 2110 / 2230.
+static bool lp_narrow(int64_t k) { return k <= SPO_TUNE_LP_NARROW; }
+static int lp_tile_cols(int64_t k) { return lp_narrow(k) ? HALF_N : BN; }
+
+int lp_fwd_lists(int64_t rows, int32_t d, int32_t V) { return 2 * lp_split(rows, d, V, lp_tile_cols(d)); }
 
 // With one or two row tiles the pairs share nothing but those rows, which stay in L2: no pacing, and no launch that
 // zeroes its counters (2 us of some 25).
 static bool lp_paced(int64_t rows) { return rows > 2 * GROUP_M; }
+
+template <bool NARROW>
+static cudaError_t launch_lp_fwd(int list, bool ent, const CUtensorMap& ma, const CUtensorMap& mb, const GemmParams& p,
+                                 uint32_t* progress, cudaStream_t st) {
+  if (list == 0) return ent ? launch_gemm<MODE_FWD, true, 0, NARROW>(ma, mb, p, progress, st)
+                            : launch_gemm<MODE_FWD, false, 0, NARROW>(ma, mb, p, progress, st);
+  if (list == 8) return ent ? launch_gemm<MODE_FWD, true, 8, NARROW>(ma, mb, p, progress, st)
+                            : launch_gemm<MODE_FWD, false, 8, NARROW>(ma, mb, p, progress, st);
+  return ent ? launch_gemm<MODE_FWD, true, kMaxTopK, NARROW>(ma, mb, p, progress, st)
+             : launch_gemm<MODE_FWD, false, kMaxTopK, NARROW>(ma, mb, p, progress, st);
+}
 
 cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
                                float2* cand_max, uint32_t* progress, cudaStream_t st) {
@@ -1114,8 +1148,8 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
     return cudaErrorInvalidValue;
   GemmParams p{};
   p.m_tiles = (int)ceil_div(rows, GROUP_M);
-  p.n_tiles = (int)ceil_div(a.V, BN);
-  p.nsplit = lp_split(rows, a.d, a.V);
+  p.n_tiles = (int)ceil_div(a.V, lp_tile_cols(a.d));
+  p.nsplit = lp_split(rows, a.d, a.V, lp_tile_cols(a.d));
   p.per_split = (int)ceil_div(p.n_tiles, p.nsplit);
   p.k_blocks = (int)ceil_div(a.d, BK);
   p.a_row0 = (int)t0;
@@ -1134,12 +1168,8 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
   const int list = lp_list_len(a.top_k);
   const bool ent = a.entropy != nullptr;
   if (!lp_paced(rows)) progress = nullptr;
-  if (list == 0) return ent ? launch_gemm<MODE_FWD, true, 0>(ma, mb, p, progress, st)
-                            : launch_gemm<MODE_FWD, false, 0>(ma, mb, p, progress, st);
-  if (list == 8) return ent ? launch_gemm<MODE_FWD, true, 8>(ma, mb, p, progress, st)
-                            : launch_gemm<MODE_FWD, false, 8>(ma, mb, p, progress, st);
-  return ent ? launch_gemm<MODE_FWD, true, kMaxTopK>(ma, mb, p, progress, st)
-             : launch_gemm<MODE_FWD, false, kMaxTopK>(ma, mb, p, progress, st);
+  return lp_narrow(a.d) ? launch_lp_fwd<true>(list, ent, ma, mb, p, progress, st)
+                        : launch_lp_fwd<false>(list, ent, ma, mb, p, progress, st);
 }
 
 // Parts that dH's contraction over the vocabulary is cut into when its tiles leave pairs idle: the one that minimises
@@ -1168,7 +1198,7 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
   if (!make_map(&mH_k, a.H, a.d, a.T, a.ldh, kBoxA) || !make_map(&mW_k, a.W, a.d, a.V, a.d, kBoxB) ||
       !make_map(&mW_mn, a.W, a.d, a.V, a.d, 64))
     return cudaErrorInvalidValue;
-  const int n_tiles_v = (int)ceil_div(a.V, BN), tiles_v = (int)ceil_div(a.V, GROUP_M);
+  const int tiles_v = (int)ceil_div(a.V, GROUP_M);
   uint32_t* const all_progress = progress;
   cudaError_t e;
   for (int64_t t0 = 0; t0 < a.T; t0 += chunk_rows) {
@@ -1182,9 +1212,9 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
     {
       GemmParams p{};
       p.m_tiles = m_tiles;
-      p.n_tiles = n_tiles_v;
-      p.nsplit = lp_split(rows, a.d, a.V);
-      p.per_split = (int)ceil_div(n_tiles_v, p.nsplit);
+      p.n_tiles = (int)ceil_div(a.V, lp_tile_cols(a.d));
+      p.nsplit = lp_split(rows, a.d, a.V, lp_tile_cols(a.d));
+      p.per_split = (int)ceil_div(p.n_tiles, p.nsplit);
       p.k_blocks = (int)ceil_div(a.d, BK);
       p.a_row0 = (int)t0;
       p.rows_valid = a.T;
@@ -1195,7 +1225,9 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
       p.inv_t = a.inv_t; p.sc2 = kLog2e * a.inv_t;
       p.G = G; p.ldg = ldg;
       p.d_status = a.d_status;
-      if ((e = launch_gemm<MODE_G, false, 0>(mH_k, mW_k, p, progress, st)) != cudaSuccess) return e;
+      e = lp_narrow(a.d) ? launch_gemm<MODE_G, false, 0, true>(mH_k, mW_k, p, progress, st)
+                         : launch_gemm<MODE_G, false, 0, false>(mH_k, mW_k, p, progress, st);
+      if (e != cudaSuccess) return e;
     }
     const int k_splits = lp_dh_splits(rows, a.d, a.V);
     if (k_splits == 1) {
@@ -1237,7 +1269,7 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
     } else {
       GemmParams p{};
       p.m_tiles = tiles_v;
-      p.n_tiles = (int)ceil_div(a.d, BN);
+      p.n_tiles = (int)ceil_div(a.d, lp_tile_cols(rows));
       p.nsplit = p.n_tiles;
       p.per_split = 1;
       p.k_blocks = (int)ceil_div(rows, BK);
@@ -1247,7 +1279,8 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
       p.out = a.dW; p.out_bf16 = 1; p.ldo = a.d; p.accumulate = a.accumulate;
       p.partial = t0 > 0 ? partial : nullptr;
       p.d_status = a.d_status;
-      e = launch_gemm<MODE_DW, false, 0>(mG_mn, mH_mn, p, progress, st);
+      e = lp_narrow(rows) ? launch_gemm<MODE_DW, false, 0, true>(mG_mn, mH_mn, p, progress, st)
+                          : launch_gemm<MODE_DW, false, 0, false>(mG_mn, mH_mn, p, progress, st);
     }
     if (e != cudaSuccess) return e;
   }
