@@ -257,13 +257,15 @@ __device__ __forceinline__ void lp_finish(const LpOut& o, int64_t t, const LpRow
 }
 
 // The K largest logits of a row, from its groups of kGroup columns: the K groups of largest maximum hold them.  Group g covers
-// columns (g >> 1) tile_h + (g & 1) kGroup .., stored from z[(g >> 1) pitch + (g & 1) kGroup] on; gmax(g) is its maximum as a float (NaN and -inf: nothing in it counts).
+// columns (g >> h) tile_h + (g & h) kGroup .., stored from z[(g >> h) pitch + (g & h) kGroup] on, where h = 1 for tiles of
+// more than kGroup columns (two groups a tile) and 0 for others; gmax(g) is its maximum as a float (NaN and -inf: nothing in it counts).
 constexpr int kGroup = 64;
 template <class Gmax>
 __device__ __forceinline__ void block_pick(const float* z, int64_t pitch, int groups, int tile_h, int32_t V, int K, Gmax gmax, TopSmem<kTopThreads>& sh,
                                            int* s_key, int* s_id) {
   block_top(groups, K, [&](int g) { return top_key(gmax(g)); }, [](int g) { return g; }, sh);
   constexpr int kSteps = kMaxTopK * kGroup / kTopThreads;
+  const int h = tile_h > kGroup ? 1 : 0;
   float x[kSteps];
   int id[kSteps];
 #pragma unroll
@@ -272,10 +274,10 @@ __device__ __forceinline__ void block_pick(const float* z, int64_t pitch, int gr
     const int i = threadIdx.x + u * kTopThreads, q = i / kGroup;
     id[u] = -1;
     if (q < K && sh.out_key[q] != kNoKey) {
-      const int g = sh.out_id[q], c = (g & 1) * kGroup + i % kGroup;
-      if (c < tile_h && (g >> 1) * tile_h + c < V) {
-        id[u] = (g >> 1) * tile_h + c;
-        at = (int64_t)(g >> 1) * pitch + c;
+      const int g = sh.out_id[q], c = (g & h) * kGroup + i % kGroup;
+      if (c < tile_h && (g >> h) * tile_h + c < V) {
+        id[u] = (g >> h) * tile_h + c;
+        at = (int64_t)(g >> h) * pitch + c;
       }
     }
     x[u] = z[at];
@@ -283,7 +285,8 @@ __device__ __forceinline__ void block_pick(const float* z, int64_t pitch, int gr
 #pragma unroll
   for (int u = 0; u < kSteps; ++u) {
     const int i = threadIdx.x + u * kTopThreads;
-    if (i < K * kGroup) { s_key[i] = id[u] < 0 ? kNoKey : top_key(x[u]); s_id[i] = id[u]; }
+    const int to = (i % kGroup) * K + i / kGroup;   // the groups' first columns, then their second ones, .. (shares alike)
+    if (i < K * kGroup) { s_key[to] = id[u] < 0 ? kNoKey : top_key(x[u]); s_id[to] = id[u]; }
   }
   block_top(K * kGroup, K, [&](int i) { return s_key[i]; }, [&](int i) { return s_id[i]; }, sh);
 }
@@ -432,8 +435,8 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, const float2
         id = sh.out_id[i >> 5] * 32 + (i & 31);
         if (id < o.V) key = top_key(cand[(((int64_t)s * rows + row) * LIST + slot) * 32 + (i & 31)]);
       }
-      s_key[i] = key;
-      s_id[i] = id;
+      s_key[(i & 31) * K + (i >> 5)] = key;
+      s_id[(i & 31) * K + (i >> 5)] = id;
     }
     block_top(K * 32, K, [&](int i) { return s_key[i]; }, [&](int i) { return s_id[i]; }, sh);
   }
@@ -510,7 +513,7 @@ struct StreamParams {
   float sc2;
   const int32_t* y;
   FwdPartial* partials;                      // [T][gridDim.x]
-  float* Z;                                  // logits [tiles][T][128] and maxima of their groups [T][2 tiles]; NULL: not wanted
+  float* Z;                                  // logits [tiles][T][128] and maxima of their groups [T][tiles x 1 or 2]; NULL: not wanted
   float* gmax;
   int32_t* d_status;
 };
@@ -616,6 +619,7 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
     }
   } else {
     const int quarter = warp & 3, half = (warp - 2) >> 2, w = warp - 2;
+    const int per_tile = p.tile_h > kGroup ? 2 : 1;      // groups of columns
     constexpr int PER = NT / kStreamWarps;               // tokens w, w + 8, .. of this warp; lane k < PER keeps the k-th's state
     float m2 = -CUDART_INF_F, l = 0.0f, ez = 0.0f, zt = -CUDART_INF_F;
     const int my_t = w + kStreamWarps * lane;
@@ -672,8 +676,8 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
               for (int i = 0; i < 2; ++i) key[i] = __reduce_max_sync(0xffffffffu, max(top_key(x[2 * i]), top_key(x[2 * i + 1])));
               const int mine = lane == 0 ? key[0] : key[1];
               const int t = w + kStreamWarps * (k0 + e);
-              if (lane < 2 && t < p.T)
-                p.gmax[((int64_t)t * p.tiles + tile) * 2 + lane] = mine == kNoKey ? -CUDART_INF_F : __int_as_float(order_key(mine));
+              if (lane < per_tile && t < p.T)
+                p.gmax[((int64_t)t * p.tiles + tile) * per_tile + lane] = mine == kNoKey ? -CUDART_INF_F : __int_as_float(order_key(mine));
               const int top = max(key[0], key[1]);
               mx[e] = top == kNoKey ? -CUDART_INF_F : __int_as_float(order_key(top));
             } else {
@@ -801,14 +805,13 @@ cudaError_t launch_stream(const LpFwd& a, const LpOut& o, FwdPartial* partials, 
   if (e != cudaSuccess) return e;
   int grid, h;
   stream_shape(a.V, &grid, &h);
-  return launch_dependent(lp_pick_kernel, dim3((unsigned)a.T), dim3(kTopThreads), st, partials, grid, gmax, 2 * (int)ceil_div(a.V, h),
+  return launch_dependent(lp_pick_kernel, dim3((unsigned)a.T), dim3(kTopThreads), st, partials, grid, gmax, (h > kGroup ? 2 : 1) * (int)ceil_div(a.V, h),
                           h, Z, (int64_t)128, a.T * 128, (int64_t)0, o);
 }
 
 // ---------------------------------------------------------------------------
 // fp32 matrix product on the fp32 pipes: C[m][n] (+)= sum_k A(m,k) B(n,k).  A_K / B_K: the operand is
-// contiguous along k, else along m / n.  Tiles of TILE x TILE x 16, 256 threads, TILE/16 squared results a
-// thread; the next k-block is fetched into registers while this one is multiplied.  gridDim.z splits k:
+// contiguous along k, else along m / n.  Tiles of TILE x TILE x 16, PT x PT results a thread; the next k-block is fetched into registers while this one is multiplied.  gridDim.z splits k:
 // each split writes its own C (stride M * ldc) and sum_splits_kernel adds them in a fixed order.  GRAD: the results are
 // logits, and their gradient is stored in their place (the formula of g_values_lp, with log p in nats).
 // ---------------------------------------------------------------------------
@@ -829,93 +832,124 @@ struct SgemmParams {
   GradParams grad;
 };
 
-template <int TILE, bool KC>
-__device__ __forceinline__ float4 sg_fetch(const float* X, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int64_t k_end,
-                                           int idx, const uint8_t* kmask) {
-  float4 r = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (KC) {
-    const int64_t m = row0 + (idx >> 2), k = k0 + (idx & 3) * 4;
-    if (m < rows && k < k_end) {
-      const float* s = X + m * ld + k;
-      if (k + 3 < k_end) return *reinterpret_cast<const float4*>(s);
-      r.x = s[0];
-      if (k + 1 < k_end) r.y = s[1];
-      if (k + 2 < k_end) r.z = s[2];
-    }
-  } else {
-    const int64_t k = k0 + idx / (TILE / 4), m = row0 + (idx % (TILE / 4)) * 4;
-    if (k < k_end && m < rows && (kmask == nullptr || kmask[k] != 0)) {
-      const float* s = X + k * ld + m;
-      if (m + 3 < rows) return *reinterpret_cast<const float4*>(s);
-      r.x = s[0];
-      if (m + 1 < rows) r.y = s[1];
-      if (m + 2 < rows) r.z = s[2];
+// One thread's share of an operand's k-blocks: where its float4s come from, advanced block by block.
+template <int TILE, bool KC, int LOADS, int THREADS>
+struct SgOperand {
+  const float* at[LOADS];
+  int k[LOADS], live[LOADS];        // k within a block; KC: whether the row exists, else how many of the four columns do
+  int64_t step, ld;
+  __device__ __forceinline__ void init(const float* X, int64_t ld_, int64_t row0, int64_t rows, int64_t k0) {
+    ld = ld_;
+    step = KC ? 16 : 16 * ld;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int idx = threadIdx.x + i * THREADS;
+      const int64_t m = row0 + (KC ? idx >> 2 : (idx % (TILE / 4)) * 4);
+      k[i] = KC ? (idx & 3) * 4 : idx / (TILE / 4);
+      live[i] = KC ? (m < rows ? 1 : 0) : m + 3 < rows ? 4 : m < rows ? (int)(rows - m) : 0;
+      at[i] = live[i] ? (KC ? X + m * ld + k0 + k[i] : X + (k0 + k[i]) * ld + m) : X;
     }
   }
+  // The block whose first k is k0 (left = k_end - k0 > 0), then on to the next.
+  __device__ __forceinline__ void fetch(float4 (&r)[LOADS], int64_t k0, int64_t left, const uint8_t* kmask) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      r[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      const int n = KC ? (live[i] == 0 || left <= k[i] ? 0 : left - k[i] >= 4 ? 4 : (int)(left - k[i]))
+                       : (left <= k[i] || (kmask != nullptr && kmask[k0 + k[i]] == 0) ? 0 : live[i]);
+      if (n == 4) {
+        r[i] = *reinterpret_cast<const float4*>(at[i]);
+      } else if (n > 0) {
+        r[i].x = at[i][0];
+        if (n > 1) r[i].y = at[i][1];
+        if (n > 2) r[i].z = at[i][2];
+      }
+      at[i] += step;
+    }
+  }
+  __device__ __forceinline__ void store(float (*s)[TILE + 4], const float4 (&r)[LOADS]) const {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int idx = threadIdx.x + i * THREADS;
+      if (KC) {
+        const int m = idx >> 2, kk = (idx & 3) * 4;
+        s[kk][m] = r[i].x; s[kk + 1][m] = r[i].y; s[kk + 2][m] = r[i].z; s[kk + 3][m] = r[i].w;
+      } else {
+        *reinterpret_cast<float4*>(&s[idx / (TILE / 4)][(idx % (TILE / 4)) * 4]) = r[i];
+      }
+    }
+  }
+};
+// Two fused multiply-adds in one instruction: (x0, x1) += a (b0, b1), each rounded like fmaf.
+__device__ __forceinline__ void ffma2(uint64_t& acc, uint64_t a, uint64_t b) {
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b));
+}
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
   return r;
 }
-template <int TILE, bool KC>
-__device__ __forceinline__ void sg_store(float (*s)[TILE + 4], int idx, float4 v) {
-  if (KC) {
-    const int m = idx >> 2, k = (idx & 3) * 4;
-    s[k][m] = v.x; s[k + 1][m] = v.y; s[k + 2][m] = v.z; s[k + 3][m] = v.w;
-  } else {
-    *reinterpret_cast<float4*>(&s[idx / (TILE / 4)][(idx % (TILE / 4)) * 4]) = v;
-  }
-}
 
-template <int TILE, bool A_K, bool B_K, bool GRAD>
-__global__ void __launch_bounds__(256)
+template <int TILE, int PT, bool A_K, bool B_K, bool GRAD>
+__global__ void __launch_bounds__((TILE / PT) * (TILE / PT), TILE == 128 ? 2 : 4)
 sgemm_kernel(const SgemmParams p) {
-  constexpr int R = TILE / 64;                       // groups of four rows (columns) per thread, 64 apart
-  constexpr int LOADS = TILE * 16 / 4 / 256;
+  constexpr int R = PT / 4;                          // groups of four rows (columns) per thread, APART apart
+  constexpr int APART = TILE / R;
+  constexpr int SIDE = TILE / PT, THREADS = SIDE * SIDE;
+  constexpr int LOADS = TILE * 16 / 4 / THREADS;
   __shared__ __align__(16) float As[2][16][TILE + 4], Bs[2][16][TILE + 4];
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int tx = threadIdx.x % SIDE, ty = threadIdx.x / SIDE;
   const int64_t m0 = (int64_t)blockIdx.x * TILE, n0 = (int64_t)blockIdx.y * TILE;
   const int64_t k_begin = (int64_t)blockIdx.z * p.k_per;
   const int64_t k_end = k_begin + p.k_per < p.K ? k_begin + p.k_per : p.K;
-  float acc[4 * R][4 * R] = {};
+  uint64_t acc2[4 * R][2 * R] = {};                  // pairs of neighbouring columns
   pdl_trigger();
   pdl_wait();
+  SgOperand<TILE, A_K, LOADS, THREADS> oa;
+  SgOperand<TILE, B_K, LOADS, THREADS> ob;
+  oa.init(p.A, p.lda, m0, p.M, k_begin);
+  ob.init(p.B, p.ldb, n0, p.N, k_begin);
   float4 ra[LOADS], rb[LOADS];
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    ra[i] = sg_fetch<TILE, A_K>(p.A, p.lda, m0, p.M, k_begin, k_end, threadIdx.x + i * 256, nullptr);
-    rb[i] = sg_fetch<TILE, B_K>(p.B, p.ldb, n0, p.N, k_begin, k_end, threadIdx.x + i * 256, p.b_mask);
-  }
+  oa.fetch(ra, k_begin, k_end - k_begin, nullptr);
+  ob.fetch(rb, k_begin, k_end - k_begin, p.b_mask);
   int buf = 0;
   for (int64_t k0 = k_begin; k0 < k_end; k0 += 16, buf ^= 1) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      sg_store<TILE, A_K>(As[buf], threadIdx.x + i * 256, ra[i]);
-      sg_store<TILE, B_K>(Bs[buf], threadIdx.x + i * 256, rb[i]);
-    }
+    oa.store(As[buf], ra);
+    ob.store(Bs[buf], rb);
     __syncthreads();
     if (k0 + 16 < k_end) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        ra[i] = sg_fetch<TILE, A_K>(p.A, p.lda, m0, p.M, k0 + 16, k_end, threadIdx.x + i * 256, nullptr);
-        rb[i] = sg_fetch<TILE, B_K>(p.B, p.ldb, n0, p.N, k0 + 16, k_end, threadIdx.x + i * 256, p.b_mask);
-      }
+      oa.fetch(ra, k0 + 16, k_end - k0 - 16, nullptr);
+      ob.fetch(rb, k0 + 16, k_end - k0 - 16, p.b_mask);
     }
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
-      float a[4 * R], b[4 * R];
+      float a[4 * R];
+      uint64_t b[2 * R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        *reinterpret_cast<float4*>(a + 4 * r) = *reinterpret_cast<const float4*>(&As[buf][k][ty * 4 + 64 * r]);
-        *reinterpret_cast<float4*>(b + 4 * r) = *reinterpret_cast<const float4*>(&Bs[buf][k][tx * 4 + 64 * r]);
+        *reinterpret_cast<float4*>(a + 4 * r) = *reinterpret_cast<const float4*>(&As[buf][k][ty * 4 + APART * r]);
+        const ulonglong2 bb = *reinterpret_cast<const ulonglong2*>(&Bs[buf][k][tx * 4 + APART * r]);
+        b[2 * r] = bb.x;
+        b[2 * r + 1] = bb.y;
       }
 #pragma unroll
-      for (int i = 0; i < 4 * R; ++i)
+      for (int i = 0; i < 4 * R; ++i) {
+        const uint64_t aa = pair(a[i], a[i]);
 #pragma unroll
-        for (int j = 0; j < 4 * R; ++j) acc[i][j] = fmaf(a[i], b[j], acc[i][j]);
+        for (int j = 0; j < 2 * R; ++j) ffma2(acc2[i][j], aa, b[j]);
+      }
     }
   }
+  float acc[4 * R][4 * R];
+#pragma unroll
+  for (int i = 0; i < 4 * R; ++i)
+#pragma unroll
+    for (int j = 0; j < 2 * R; ++j)
+      asm("mov.b64 {%0, %1}, %2;" : "=f"(acc[i][2 * j]), "=f"(acc[i][2 * j + 1]) : "l"(acc2[i][j]));
   float* C = p.C + (int64_t)blockIdx.z * p.M * p.ldc;
 #pragma unroll
   for (int i = 0; i < 4 * R; ++i) {
-    const int64_t m = m0 + ty * 4 + (i & 3) + 64 * (i >> 2);
+    const int64_t m = m0 + ty * 4 + (i & 3) + APART * (i >> 2);
     if (m >= p.M) continue;
     bool live = true;
     float a = 0.0f, b = 0.0f, tgt = 0.0f, ls = 0.0f;
@@ -937,7 +971,7 @@ sgemm_kernel(const SgemmParams p) {
     }
 #pragma unroll
     for (int j = 0; j < 4 * R; ++j) {
-      const int64_t n = n0 + tx * 4 + (j & 3) + 64 * (j >> 2);
+      const int64_t n = n0 + tx * 4 + (j & 3) + APART * (j >> 2);
       if (n >= p.N) continue;
       float* dst = C + m * p.ldc + n;
       if (GRAD) {
@@ -993,12 +1027,18 @@ cudaError_t launch_sgemm(SgemmParams p, bool first, float* split_ws, SplitSum* s
   if (sum) *sum = SplitSum{split_ws, (int)splits, splits > 1 ? p.M * p.N : 0, p.C, p.accumulate};
   if (splits > 1) { p.C = split_ws; p.accumulate = 0; }
   const dim3 grid((unsigned)bm, (unsigned)bn, (unsigned)splits);
-  auto kern = tile == 128 ? sgemm_kernel<128, A_K, B_K, GRAD> : sgemm_kernel<64, A_K, B_K, GRAD>;
+  // 64-wide tiles: 8 x 8 results a thread (half the shared-memory reads per product) when the blocks fill the GPU,
+  // 4 x 4 and four times the threads when they do not and a block's own latency counts
+  const bool fat = tile == 128 || bm * bn * splits >= sm_count();
+  auto kern = tile == 128 ? sgemm_kernel<128, 8, A_K, B_K, GRAD>
+              : fat       ? sgemm_kernel<64, 8, A_K, B_K, GRAD>
+                          : sgemm_kernel<64, 4, A_K, B_K, GRAD>;
+  const dim3 block(tile == 64 && fat ? 64 : 256);
   if (first) {
-    kern<<<grid, 256, 0, st>>>(p);
+    kern<<<grid, block, 0, st>>>(p);
     return cudaGetLastError();
   }
-  return launch_dependent(kern, grid, dim3(256), st, p);
+  return launch_dependent(kern, grid, block, st, p);
 }
 
 __global__ void __launch_bounds__(256)
