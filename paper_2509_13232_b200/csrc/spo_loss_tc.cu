@@ -1174,7 +1174,7 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
 
 // Parts that dH's contraction over the vocabulary is cut into when its tiles leave pairs idle: the one that minimises
 // the k-blocks of a part (0.61 us each) plus the writing and summing of the parts' fp32 results (8 bytes per element at 4 TB/s,
-// and a launch).  203 rows, d = 1024, V = 32000: 2 tiles, 286 us in one part, 22 us in 25 and their sum.
+// and a launch).  203 rows, d = 1024, V = 32000: 2 tiles, 286 us in one part, 26 + 4 us in 25 parts and their sum.
 int lp_dh_splits(int64_t rows, int32_t d, int32_t V) {
   const int64_t units = ceil_div(rows, GROUP_M) * ceil_div(d, BN);
   const int k_blocks = (int)ceil_div(V, BK), most = (int)(group_count() / units);
