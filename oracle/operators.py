@@ -87,7 +87,7 @@ def muon_update(w, momentum, g, lr, mu, weight_decay=0.0, nesterov=True, mode=0,
 
 def newton_schulz_rounded(g, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7):
     """The same iteration with fp16 roundings where the library documents them (iterate as a pair of fp16 numbers scaled
-    by a power of two, the Gram matrix and the polynomial once each), everything else in 64 bits: what those roundings
+    by a power of two, the Gram matrix and the polynomial once each, the latter's diagonal not at all), everything else in 64 bits: what those roundings
     alone do to a given input, which is what a tolerance has to allow for."""
     a, b, c = coefficients
     x = np.asarray(g, np.float64)
@@ -101,5 +101,7 @@ def newton_schulz_rounded(g, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7):
         hi = half(x)
         pair = hi + half(x - hi)
         q = half(hi @ hi.T / s**2)
-        x = a * pair + half(b * q + c * (q @ q)) @ hi
+        poly = b * q + c * (q @ q)
+        diagonal = np.diag(poly)
+        x = (a + diagonal)[:, None] * pair + half(poly - np.diag(diagonal)) @ hi
     return (x.T if tall else x) / s

@@ -267,10 +267,34 @@ int lp_fwd_lists(int64_t rows, int32_t d, int32_t V);   // lists (and partials) 
 cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
                                float2* cand_max, uint32_t* progress, cudaStream_t st);
 int lp_dh_splits(int64_t rows, int32_t d, int32_t V);    // parts of dH's contraction over the vocabulary
-cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_rows, int64_t ldg, float* partial,
-                               void* h_clean, float* split, uint32_t* progress, cudaStream_t st);
-// out[i] = sum over `parts` of src[part][i] in order, n elements (a multiple of 4) of type out_dtype
-cudaError_t launch_sum_parts(const float* src, int parts, int64_t n, void* out, int32_t out_dtype, cudaStream_t st);
+// The target entry of a token's logit gradient is by far its largest, and what rounding it to bf16 takes off does not
+// average out over the few tokens of a vocabulary row.  So the gradient launch keeps that rest (by token of the chunk), and it
+// is added in fp32: rest W[y] to the token's dH, the sum of rest H over a target's tokens to the target's row of dW.
+struct TargetRest {
+  const int32_t* y;                       // all by token of the chunk
+  const uint8_t* mask;
+  float* rest;                            // NULL: the log-prob has no upstream gradient, nothing is kept
+  int32_t* slot;                          // [V] of a vocabulary row that is some token's target: the first such token
+  float* rows;                            // [token][d], of first tokens: the sum of rest H over all of the target's tokens
+};
+struct LpBwdScratch {
+  __nv_bfloat16* g;
+  int64_t chunk, ldg;                     // token rows and pitch of g
+  float* partial;
+  void* h_clean;
+  float* split;
+  float* rest;
+  int32_t* slot;
+  float* rest_rows;
+  uint32_t* progress;
+};
+cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream_t st);
+// Both of these after the chunk's gradient; either may be left out (parts = 0, rest.rest = NULL).
+//   dH[t] = sum over `parts` of src[part][t] in order, plus rest W[y] (bf16 [V, d]); rows x d of type dh_dtype
+//   the targets' rows of rest H: into rest.rows and rest.slot, or added to dw (fp32 [V, d]) if that is not NULL
+cudaError_t launch_lp_rest(const float* src, int parts, int64_t rows, int32_t d, int32_t V, void* dh, int32_t dh_dtype,
+                           const void* W, const void* H, int64_t ldh, const TargetRest& rest, bool targets, float* dw,
+                           cudaStream_t st);
 // out[i][:] = H[t0 + i][:] (bf16, row pitch ldh), or zeros where mask[t0 + i] is 0
 cudaError_t launch_clean_rows(const void* H, int64_t ldh, const uint8_t* mask, int64_t t0, int64_t rows, int32_t d,
                               void* out, cudaStream_t st);

@@ -1053,19 +1053,113 @@ clean_rows_kernel(const uint4* __restrict__ H, int64_t ld_vec, const uint8_t* __
   }
 }
 
+// What follows the logit gradient of a chunk in bf16 (see TargetRest).  The first `sum_blocks` blocks add the parts of dH and
+// the tokens' rests; each of the others has a token, and if no earlier token has its target, sums rest H over all that do,
+// in their order.  Finding them is a scan of the chunk's targets by every block: 19,000 tokens take 9 rounds of 2048, and
+// nothing has to be sorted or counted first.
+struct RestParams {
+  const float4* src;
+  int parts, sum_blocks;
+  uint32_t quads, row_quads;               // float4s of dH, and of a row
+  void* dh;
+  const uint2* W;
+  const __nv_bfloat16* H;
+  int64_t ldh;
+  int32_t rows, d, V;
+  TargetRest r;
+  float* dw;
+};
+__device__ __forceinline__ int32_t rest_target(const RestParams& p, int32_t t) {
+  const int32_t y = p.r.y[t];
+  return y >= 0 && y < p.V && (p.r.mask == nullptr || p.r.mask[t] != 0) ? y : -1;
+}
+
 template <bool BF16>
 __global__ void __launch_bounds__(256)
-sum_parts_kernel(const float4* __restrict__ src, int parts, int64_t quads, void* __restrict__ out) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (int64_t)gridDim.x * 256) {
-    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+lp_rest_kernel(const RestParams p) {
+  if ((int)blockIdx.x < p.sum_blocks) {
+    for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < p.quads; i += (uint32_t)p.sum_blocks * 256u) {
+      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
-    for (int z = 0; z < parts; ++z) {
-      const float4 x = src[z * quads + i];
-      s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+      for (int z = 0; z < p.parts; ++z) {
+        const float4 x = p.src[(int64_t)z * p.quads + i];
+        s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+      }
+      if (p.r.rest) {
+        const uint32_t t = i / p.row_quads;
+        const int32_t y = rest_target(p, (int32_t)t);
+        const float r = y >= 0 ? p.r.rest[t] : 0.0f;
+        if (r != 0.0f) {
+          const uint2 w = __ldg(p.W + (int64_t)y * p.row_quads + (i - t * p.row_quads));
+          s.x = fmaf(r, __uint_as_float(w.x << 16), s.x);
+          s.y = fmaf(r, __uint_as_float(w.x & 0xFFFF0000u), s.y);
+          s.z = fmaf(r, __uint_as_float(w.y << 16), s.z);
+          s.w = fmaf(r, __uint_as_float(w.y & 0xFFFF0000u), s.w);
+        }
+      }
+      if (BF16) reinterpret_cast<uint2*>(p.dh)[i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
+      else reinterpret_cast<float4*>(p.dh)[i] = s;
     }
-    if (BF16) reinterpret_cast<uint2*>(out)[i] = make_uint2(pack_bf16(s.x, s.y), pack_bf16(s.z, s.w));
-    else reinterpret_cast<float4*>(out)[i] = s;
+    return;
   }
+  __shared__ uint32_t found[64];
+  const int32_t t = (int32_t)blockIdx.x - p.sum_blocks;
+  const int32_t y = rest_target(p, t);
+  if (y < 0) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int32_t c0 = 0; c0 < p.d; c0 += 2048) {
+    const int32_t c = c0 + (int32_t)threadIdx.x * 8;
+    float acc[8] = {};
+    for (int32_t t0 = 0; t0 < p.rows; t0 += 2048) {
+      int32_t ys[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int32_t i = t0 + k * 256 + (int32_t)threadIdx.x;
+        ys[k] = i < p.rows ? __ldg(p.r.y + i) : -1;
+      }
+      bool any = false, earlier = false;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int32_t i = t0 + k * 256 + (int32_t)threadIdx.x;
+        const bool hit = ys[k] == y && (p.r.mask == nullptr || p.r.mask[i] != 0);
+        earlier = earlier || (hit && i < t);
+        any = any || hit;
+        const uint32_t b = __ballot_sync(0xffffffffu, hit);
+        if (lane == 0) found[k * 8 + warp] = b;
+      }
+      if (__syncthreads_or(earlier)) return;
+      if (__syncthreads_or(any)) {
+        for (int q = 0; q < 64; ++q) {
+          for (uint32_t b = found[q]; b != 0; b &= b - 1) {
+            const int32_t i = t0 + q * 32 + __ffs(b) - 1;
+            const float r = p.r.rest[i];
+            if (r == 0.0f || c >= p.d) continue;
+            const uint4 h = __ldg(reinterpret_cast<const uint4*>(p.H + (int64_t)i * p.ldh + c));
+            const uint32_t x[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              acc[2 * k] = fmaf(r, __uint_as_float(x[k] << 16), acc[2 * k]);
+              acc[2 * k + 1] = fmaf(r, __uint_as_float(x[k] & 0xFFFF0000u), acc[2 * k + 1]);
+            }
+          }
+        }
+        __syncthreads();
+      }
+    }
+    if (c < p.d) {
+      float4* dst = reinterpret_cast<float4*>(p.dw ? p.dw + (int64_t)y * p.d + c : p.r.rows + (int64_t)t * p.d + c);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float4 v = make_float4(acc[4 * h], acc[4 * h + 1], acc[4 * h + 2], acc[4 * h + 3]);
+        if (p.dw) {
+          const float4 o = dst[h];
+          v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        }
+        dst[h] = v;
+      }
+    }
+  }
+  if (p.dw == nullptr && threadIdx.x == 0) p.r.slot[y] = t;
 }
 
 // ---------------------------------------------------------------------------
@@ -1141,7 +1235,7 @@ LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype)
   return L;
 }
 
-struct LpBwdWs { size_t g, h_clean, partial, progress, split, total; int64_t chunk, ldg; };
+struct LpBwdWs { size_t g, h_clean, partial, progress, split, rest, slot, rest_rows, total; int64_t chunk, ldg; };
 
 LpBwdWs lp_bwd_layout(int64_t T, int32_t d, int32_t V, int32_t dtype) {
   LpBwdWs L{};
@@ -1170,6 +1264,9 @@ LpBwdWs lp_bwd_layout(int64_t T, int32_t d, int32_t V, int32_t dtype) {
       if (x > parts) parts = x;
     }
     off = align_up(off + parts, 256);
+    L.rest = off;      off = align_up(off + (size_t)first * 4, 256);
+    L.slot = off;      off = align_up(off + (size_t)V * 4, 256);
+    L.rest_rows = off; off = align_up(off + (size_t)first * d * 4, 256);
   }
   L.total = off;
   return L;
@@ -1199,13 +1296,28 @@ cudaError_t launch_clean_rows(const void* H, int64_t ldh, const uint8_t* mask, i
   return cudaGetLastError();
 }
 
-cudaError_t launch_sum_parts(const float* src, int parts, int64_t n, void* out, int32_t out_dtype, cudaStream_t st) {
-  int64_t blocks = ceil_div(n / 4, 256);
-  if (blocks > (int64_t)sm_count() * 8) blocks = (int64_t)sm_count() * 8;
-  if (out_dtype == SPO_DTYPE_BF16)
-    sum_parts_kernel<true><<<(unsigned)blocks, 256, 0, st>>>(reinterpret_cast<const float4*>(src), parts, n / 4, out);
-  else
-    sum_parts_kernel<false><<<(unsigned)blocks, 256, 0, st>>>(reinterpret_cast<const float4*>(src), parts, n / 4, out);
+cudaError_t launch_lp_rest(const float* src, int parts, int64_t rows, int32_t d, int32_t V, void* dh, int32_t dh_dtype,
+                           const void* W, const void* H, int64_t ldh, const TargetRest& rest, bool targets, float* dw,
+                           cudaStream_t st) {
+  RestParams p{};
+  p.src = reinterpret_cast<const float4*>(src);
+  p.parts = parts;
+  if (parts > 0) {
+    p.quads = (uint32_t)(rows * d / 4);
+    const int64_t blocks = ceil_div(p.quads, 256), most = (int64_t)sm_count() * 8;
+    p.sum_blocks = (int)(blocks < most ? blocks : most);
+  }
+  p.row_quads = (uint32_t)d / 4;
+  p.dh = dh;
+  p.W = reinterpret_cast<const uint2*>(W);
+  p.H = reinterpret_cast<const __nv_bfloat16*>(H); p.ldh = ldh;
+  p.rows = (int32_t)rows; p.d = d; p.V = V;
+  p.r = rest;
+  p.dw = dw;
+  const int64_t blocks = p.sum_blocks + (targets && rest.rest ? rows : 0);
+  if (blocks == 0) return cudaSuccess;
+  if (dh_dtype == SPO_DTYPE_BF16) lp_rest_kernel<true><<<(unsigned)blocks, 256, 0, st>>>(p);
+  else lp_rest_kernel<false><<<(unsigned)blocks, 256, 0, st>>>(p);
   return cudaGetLastError();
 }
 
@@ -1257,10 +1369,19 @@ cudaError_t lp_backward(const LpBwd& a, char* ws, cudaStream_t st) {
   const size_t dw_bytes = (size_t)a.V * a.d * (a.dW_dtype == SPO_DTYPE_BF16 ? 2 : 4);
   if (a.T == 0) return a.accumulate ? cudaSuccess : cudaMemsetAsync(a.dW, 0, dw_bytes, st);
   const LpBwdWs L = lp_bwd_layout(a.T, a.d, a.V, a.dtype);
-  if (a.dtype == SPO_DTYPE_BF16)
-    return launch_lp_bwd_bf16(a, reinterpret_cast<__nv_bfloat16*>(ws + L.g), L.chunk, L.ldg,
-                              reinterpret_cast<float*>(ws + L.partial), ws + L.h_clean, reinterpret_cast<float*>(ws + L.split),
-                              reinterpret_cast<uint32_t*>(ws + L.progress), st);
+  if (a.dtype == SPO_DTYPE_BF16) {
+    LpBwdScratch w{};
+    w.g = reinterpret_cast<__nv_bfloat16*>(ws + L.g);
+    w.chunk = L.chunk; w.ldg = L.ldg;
+    w.partial = reinterpret_cast<float*>(ws + L.partial);
+    w.h_clean = ws + L.h_clean;
+    w.split = reinterpret_cast<float*>(ws + L.split);
+    w.rest = reinterpret_cast<float*>(ws + L.rest);
+    w.slot = reinterpret_cast<int32_t*>(ws + L.slot);
+    w.rest_rows = reinterpret_cast<float*>(ws + L.rest_rows);
+    w.progress = reinterpret_cast<uint32_t*>(ws + L.progress);
+    return launch_lp_bwd_bf16(a, w, st);
+  }
   float* Z = reinterpret_cast<float*>(ws + L.g);
   float* split = reinterpret_cast<float*>(ws + L.split);
   cudaError_t e;

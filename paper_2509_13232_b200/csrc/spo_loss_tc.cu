@@ -140,6 +140,9 @@ struct GemmParams {
   const float* partial;                      // DW: fp32 sum of the earlier chunks, added before the rounding; NULL = none
   int k_splits, k_per;                       // DH: the contraction cut into k_splits parts of k_per k-blocks, each with an
                                              // fp32 result of its own in `out`, [part][rows_valid][ldo]
+  TargetRest rest;                           // G: rest is stored;  DH (one part), DW: it is added to the result
+  int n_rest;                                // DH: V;  DW: tokens of the chunk
+  const __nv_bfloat16* w_rows;               // DH: W, [vocabulary row][ldo]
 };
 
 // g = c_t (1[v = y_t] - 2^(z log2e - lse_t log2e)) for 32 consecutive columns, packed to bf16.
@@ -172,7 +175,7 @@ __device__ __forceinline__ void g_values(const uint32_t (&v)[32], int col0, floa
 // Gradient of a row's logits for upstream gradients of its log-prob, log-sum-exp and entropy:
 // with u = log2 p = z sc2 - lse2, g = 2^u (a + b u) + tgt 1[v = y_t] (a, b, tgt: see the row setup), packed to bf16.
 __device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, bool live, float sc2, float lse2, float a,
-                                            float b, float tgt, int yt, int cols_valid, uint4* out4) {
+                                            float b, float tgt, int yt, int cols_valid, uint4* out4, float* rest) {
   float g[32];
   if (live) {
 #pragma unroll
@@ -183,7 +186,13 @@ __device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, b
     if (yt >= col0 && yt < col0 + 32) {
       const int jj = yt - col0;
 #pragma unroll
-      for (int j = 0; j < 32; ++j) if (j == jj) g[j] += tgt;
+      float t = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) if (j == jj) { g[j] += tgt; t = g[j]; }
+      if (rest) {                                  // what the rounding takes off the target's entry (see TargetRest)
+        const float r = t - __bfloat162float(__float2bfloat16_rn(t));
+        *rest = isfinite(r) ? r : 0.0f;
+      }
     }
     if (col0 + 32 > cols_valid) {
 #pragma unroll
@@ -197,6 +206,32 @@ __device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, b
   for (int q = 0; q < 4; ++q)
     out4[q] = make_uint4(pack_bf16(g[8 * q + 0], g[8 * q + 1]), pack_bf16(g[8 * q + 2], g[8 * q + 3]),
                          pack_bf16(g[8 * q + 4], g[8 * q + 5]), pack_bf16(g[8 * q + 6], g[8 * q + 7]));
+}
+
+// v += r x the row's 32 values from `row` on, of which the first `cols` exist (a multiple of 8)
+__device__ __forceinline__ void add_row(uint32_t (&v)[32], const __nv_bfloat16* row, float r, int cols) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    if (8 * q >= cols) break;
+    const uint4 w = __ldg(reinterpret_cast<const uint4*>(row) + q);
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      v[8 * q + 2 * k] = __float_as_uint(fmaf(r, __uint_as_float(x[k] << 16), __uint_as_float(v[8 * q + 2 * k])));
+      v[8 * q + 2 * k + 1] = __float_as_uint(fmaf(r, __uint_as_float(x[k] & 0xFFFF0000u), __uint_as_float(v[8 * q + 2 * k + 1])));
+    }
+  }
+}
+__device__ __forceinline__ void add_row(uint32_t (&v)[32], const float* row, int cols) {
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    if (4 * q >= cols) break;
+    const float4 w = __ldg(reinterpret_cast<const float4*>(row) + q);
+    v[4 * q] = __float_as_uint(__uint_as_float(v[4 * q]) + w.x);
+    v[4 * q + 1] = __float_as_uint(__uint_as_float(v[4 * q + 1]) + w.y);
+    v[4 * q + 2] = __float_as_uint(__uint_as_float(v[4 * q + 2]) + w.z);
+    v[4 * q + 3] = __float_as_uint(__uint_as_float(v[4 * q + 3]) + w.w);
+  }
 }
 
 // Two floats to a bf16 pair, infinities replaced by the largest finite value (stored exponentials
@@ -446,6 +481,24 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         gb = -p.inv_t * ge * 0.69314718055994531f;
         lse2 = p.lse[grow] * kLog2e;
       }
+      float* const rest_at = MODE == MODE_G && LP >= 0 && p.rest.rest ? p.rest.rest + (grow - p.out_row0) : nullptr;
+      float rest = 0.0f;                                                   // DH, DW with LP: what the row's targets are
+      const __nv_bfloat16* rest_w = nullptr;                               // still owed (see TargetRest)
+      const float* rest_sum = nullptr;
+      if (MODE == MODE_DH && LP >= 0 && p.rest.rest && row_ok) {
+        const int32_t yy = p.rest.y[grow];
+        if (yy >= 0 && yy < p.n_rest && (p.rest.mask == nullptr || p.rest.mask[grow] != 0)) {
+          rest = p.rest.rest[grow];
+          rest_w = p.w_rows + (int64_t)yy * p.ldo;
+        }
+      }
+      if (MODE == MODE_DW && LP >= 0 && p.rest.rest && row_ok) {
+        // rows that are nobody's target have no slot: theirs is whatever the scratch held, and then does not lead
+        // to a token with this target
+        const int32_t s = p.rest.slot[grow];
+        if (s >= 0 && s < p.n_rest && p.rest.y[s] == grow && (p.rest.mask == nullptr || p.rest.mask[s] != 0))
+          rest_sum = p.rest.rows + (int64_t)s * p.ldo;
+      }
       float rs = 1.0f;                                                     // DH: factor of this lane's output row
       if (MODE == MODE_FWD || MODE == MODE_G || MODE == MODE_E) {
         if (row_ok && (LP < 0 || p.y)) yt = p.y[grow];
@@ -631,8 +684,8 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             uint4 piece[8];
             if (MODE == MODE_G) {
               if (LP >= 0) {
-                g_values_lp(v0, col0, live, p.sc2, lse2, ga, gb, gt, yt, p.cols_valid, piece);
-                g_values_lp(v1, col0 + 32, live, p.sc2, lse2, ga, gb, gt, yt, p.cols_valid, piece + 4);
+                g_values_lp(v0, col0, live, p.sc2, lse2, ga, gb, gt, yt, p.cols_valid, piece, rest_at);
+                g_values_lp(v1, col0 + 32, live, p.sc2, lse2, ga, gb, gt, yt, p.cols_valid, piece + 4, rest_at);
               } else {
                 g_values(v0, col0, c, lse2, yt, p.cols_valid, piece);
                 g_values(v1, col0 + 32, c, lse2, yt, p.cols_valid, piece + 4);
@@ -644,6 +697,14 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                   v0[j] = __float_as_uint(rs == 0.0f ? 0.0f : __uint_as_float(v0[j]) * rs);
                   v1[j] = __float_as_uint(rs == 0.0f ? 0.0f : __uint_as_float(v1[j]) * rs);
                 }
+              }
+              if (MODE == MODE_DH && LP >= 0 && rest != 0.0f) {
+                add_row(v0, rest_w + col0, rest, p.cols_valid - col0);
+                add_row(v1, rest_w + col0 + 32, rest, p.cols_valid - col0 - 32);
+              }
+              if (MODE == MODE_DW && LP >= 0 && rest_sum) {
+                add_row(v0, rest_sum + col0, p.cols_valid - col0);
+                add_row(v1, rest_sum + col0 + 32, p.cols_valid - col0 - 32);
               }
               bf16_values(v0, piece);
               bf16_values(v1, piece + 4);
@@ -673,6 +734,8 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 #pragma unroll
               for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(rs == 0.0f ? 0.0f : __uint_as_float(v[j]) * rs);
             }
+            if (MODE == MODE_DH && LP >= 0 && rest != 0.0f) add_row(v, rest_w + col0, rest, p.cols_valid - col0);
+            if (MODE == MODE_DW && LP >= 0 && rest_sum) add_row(v, rest_sum + col0, p.cols_valid - col0);
             uint4 piece[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) piece[q] = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
@@ -1192,8 +1255,10 @@ int lp_dh_splits(int64_t rows, int32_t d, int32_t V) {
 // bf16 backward for general upstream gradients, chunk by chunk as launch_bwd_bf16: the chunk's logit
 // gradient, dH = G W, dW (+)= G^T H.  A bf16 dW over several chunks is summed in fp32 (`partial`) and
 // rounded once, in the last chunk's epilogue.
-cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_rows, int64_t ldg, float* partial,
-                               void* h_clean, float* split, uint32_t* progress, cudaStream_t st) {
+cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream_t st) {
+  __nv_bfloat16* const G = w.g;
+  const int64_t chunk_rows = w.chunk, ldg = w.ldg;
+  uint32_t* progress = w.progress;
   CUtensorMap mH_k, mW_k, mW_mn, mH_mn;
   if (!make_map(&mH_k, a.H, a.d, a.T, a.ldh, kBoxA) || !make_map(&mW_k, a.W, a.d, a.V, a.d, kBoxB) ||
       !make_map(&mW_mn, a.W, a.d, a.V, a.d, 64))
@@ -1204,8 +1269,14 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
   for (int64_t t0 = 0; t0 < a.T; t0 += chunk_rows) {
     const int64_t rows = (a.T - t0) < chunk_rows ? (a.T - t0) : chunk_rows;
     progress = lp_paced(rows) ? all_progress : nullptr;
+    const bool rounded = a.dW_dtype == SPO_DTYPE_BF16 && t0 + rows >= a.T;       // dW's final rounding is this chunk's
+    TargetRest rest{};
+    if (a.g_logp) {
+      rest.y = a.y + t0;
+      rest.mask = a.mask ? a.mask + t0 : nullptr;
+      rest.rest = w.rest; rest.slot = w.slot; rest.rows = w.rest_rows;
+    }
     const int m_tiles = (int)ceil_div(rows, GROUP_M);
-    const bool last = t0 + rows >= a.T;
     CUtensorMap mG_k, mG_mn;
     if (!make_map(&mG_k, G, a.V, rows, ldg, kBoxA) || !make_map(&mG_mn, G, a.V, rows, ldg, 64))
       return cudaErrorInvalidValue;
@@ -1224,15 +1295,16 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
       p.g_logp = a.g_logp; p.g_lse = a.g_lse; p.g_ent = a.g_ent;
       p.inv_t = a.inv_t; p.sc2 = kLog2e * a.inv_t;
       p.G = G; p.ldg = ldg;
+      p.rest = rest;
       p.d_status = a.d_status;
       e = lp_narrow(a.d) ? launch_gemm<MODE_G, false, 0, true>(mH_k, mW_k, p, progress, st)
                          : launch_gemm<MODE_G, false, 0, false>(mH_k, mW_k, p, progress, st);
       if (e != cudaSuccess) return e;
     }
     const int k_splits = lp_dh_splits(rows, a.d, a.V);
-    if (k_splits == 1) {
-      e = launch_dh(mG_k, mW_mn, t0, rows, a.T, a.d, a.V, a.dH, a.dH_dtype, nullptr, progress, a.d_status, st);
-    } else {
+    const int64_t dh_bytes = a.dH_dtype == SPO_DTYPE_BF16 ? 2 : 4;
+    void* const dH = (char*)a.dH + t0 * a.d * dh_bytes;
+    {
       GemmParams p{};
       p.m_tiles = m_tiles;
       p.n_tiles = (int)ceil_div(a.d, BN);
@@ -1243,29 +1315,37 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
       p.k_per = (int)ceil_div(p.k_blocks, k_splits);
       p.rows_valid = rows;
       p.cols_valid = a.d;
-      p.out = split; p.ldo = a.d;
+      p.ldo = a.d;
       p.d_status = a.d_status;
+      if (k_splits == 1) {
+        p.out = dH; p.out_bf16 = a.dH_dtype == SPO_DTYPE_BF16;
+        p.rest = rest; p.n_rest = a.V; p.w_rows = reinterpret_cast<const __nv_bfloat16*>(a.W);
+      } else {
+        p.out = w.split;
+      }
       e = launch_gemm<MODE_DH, false, 0>(mG_k, mW_mn, p, progress, st);
-      if (e == cudaSuccess)
-        e = launch_sum_parts(split, k_splits, rows * a.d, (char*)a.dH + t0 * a.d * (a.dH_dtype == SPO_DTYPE_BF16 ? 2 : 4),
-                             a.dH_dtype, st);
+      if (e != cudaSuccess) return e;
     }
+    const __nv_bfloat16* const H = reinterpret_cast<const __nv_bfloat16*>(a.H) + t0 * a.ldh;
+    e = launch_lp_rest(w.split, k_splits == 1 ? 0 : k_splits, rows, a.d, a.V, dH, a.dH_dtype, a.W, H, a.ldh, rest, rounded,
+                       nullptr, st);
     if (e != cudaSuccess) return e;
     // The gradient of a masked row is zero, but zero times a NaN in that row of H is not: with a mask the
     // dW contraction reads a copy of the chunk's rows in which the masked ones are zero.
     int64_t h_row0 = t0;
     if (a.mask) {
-      if ((e = launch_clean_rows(a.H, a.ldh, a.mask, t0, rows, a.d, h_clean, st)) != cudaSuccess) return e;
+      if ((e = launch_clean_rows(a.H, a.ldh, a.mask, t0, rows, a.d, w.h_clean, st)) != cudaSuccess) return e;
       h_row0 = 0;
-      if (!make_map(&mH_mn, h_clean, a.d, rows, a.d, 64)) return cudaErrorInvalidValue;
+      if (!make_map(&mH_mn, w.h_clean, a.d, rows, a.d, 64)) return cudaErrorInvalidValue;
     } else if (!make_map(&mH_mn, a.H, a.d, a.T, a.ldh, 64)) {
       return cudaErrorInvalidValue;
     }
-    if (a.dW_dtype == SPO_DTYPE_F32) {
-      e = launch_dw(mG_mn, mH_mn, h_row0, rows, a.d, a.V, (float*)a.dW, (a.accumulate || t0 > 0) ? 1 : 0, 0, tiles_v,
-                    progress, a.d_status, st);
-    } else if (!last) {
-      e = launch_dw(mG_mn, mH_mn, h_row0, rows, a.d, a.V, partial, t0 > 0 ? 1 : 0, 0, tiles_v, progress, a.d_status, st);
+    if (!rounded) {
+      float* const sum = a.dW_dtype == SPO_DTYPE_F32 ? (float*)a.dW : w.partial;
+      const bool add = t0 > 0 || (a.dW_dtype == SPO_DTYPE_F32 && a.accumulate);
+      e = launch_dw(mG_mn, mH_mn, h_row0, rows, a.d, a.V, sum, add ? 1 : 0, 0, tiles_v, progress, a.d_status, st);
+      if (e == cudaSuccess)
+        e = launch_lp_rest(nullptr, 0, rows, a.d, a.V, nullptr, a.dH_dtype, a.W, H, a.ldh, rest, true, sum, st);
     } else {
       GemmParams p{};
       p.m_tiles = tiles_v;
@@ -1277,7 +1357,8 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, __nv_bfloat16* G, int64_t chunk_r
       p.rows_valid = a.V;
       p.cols_valid = a.d;
       p.out = a.dW; p.out_bf16 = 1; p.ldo = a.d; p.accumulate = a.accumulate;
-      p.partial = t0 > 0 ? partial : nullptr;
+      p.partial = t0 > 0 ? w.partial : nullptr;
+      p.rest = rest; p.n_rest = (int)rows;
       p.d_status = a.d_status;
       e = lp_narrow(rows) ? launch_gemm<MODE_DW, false, 0, true>(mG_mn, mH_mn, p, progress, st)
                           : launch_gemm<MODE_DW, false, 0, false>(mG_mn, mH_mn, p, progress, st);

@@ -10,7 +10,9 @@
 // puts the entries of an orthogonal matrix near one.  Errors against 64 bits for a 512 x 512 update of rank 16
 // under no noise: this 4e-4, fp16 alone 4e-2, bf16 alone 0.33 (a full-rank Gaussian: 1.5e-3, 1.3e-3, 1.1e-2).  fp16 rather than bf16 because everything
 // here is bounded by about 10 in magnitude and fp16 has 8 times finer steps.  A and b A + c A A are rounded
-// to fp16 once each; all sums are fp32.
+// to fp16 once each, but for the diagonal of the latter: near convergence it is -2.7 and the rest almost nothing,
+// so it stays in fp32 and multiplies X in fp32 (19 x 183: error of the iteration 8e-4; rounded with the rest 1.7e-3).
+// All sums are fp32.
 //
 // Work.  A and A A are symmetric: only the blocks on and above the diagonal are computed and stored (a block below
 // it is read as the transposed operand of its mirror image), 3 m^2 n + m^3 operations a step for m <= n instead of 4 m^2 n + 2 m^3.  Five steps of a 4096 x 4096
@@ -37,7 +39,8 @@ constexpr int NS_THREADS = 32 * (2 + NS_EPI_WARPS);
 constexpr int NS_STAGING = 4096;
 constexpr int NS_RING = 192 * 1024;             // operand stages
 constexpr int NS_BARS = 512;                    // barriers of the two kinds of product, tensor-memory address, flags
-constexpr int NS_SMEM = NS_RING + 1024 + NS_BARS + NS_EPI_WARPS * NS_STAGING;
+constexpr int NS_FACTORS = 128;                 // a warp's 32 row factors
+constexpr int NS_SMEM = NS_RING + 1024 + NS_BARS + NS_EPI_WARPS * (NS_STAGING + NS_FACTORS);
 
 template <int BN>
 struct NsCfg {
@@ -73,6 +76,7 @@ struct NsParams {
   __half *hi[2], *gram, *poly;                 // X in fp16 (two, written in turn), A, b A + c A A; row-major
   float* x32;                                  // X in fp32, in blocks of 32 x 32 (see ns_block)
   __half* gram_blk;                            // A once more, in blocks
+  float* diag;                                 // [batch][mm] the diagonal of b A + c A A (zero in poly)
   float inv_s2, a, b, c;
   int out_mode;
   void* out;                                   // result or weights, pitch n
@@ -236,6 +240,7 @@ __device__ __forceinline__ bool ns_multiply(int total, int tiles, int n_tiles, i
 struct NsEpi {
   uint32_t tmem_base, rank;
   uint8_t* stage;
+  volatile float* factor;                      // wide: this lane's row's, in the update
   int quarter, half, lane;
   volatile int* abort_flag;
   int32_t* d_status;
@@ -256,8 +261,8 @@ __device__ __forceinline__ void ns_tile_done(const NsEpi& e, const NsBars& bars,
   if (e.lane == 0) mbar_arrive_cluster(map_to_cta(bars.tempty0 + 8 * (n % NsCfg<BN>::bufs), 0));
 }
 
-// A = acc / s^2, or b A + c acc (POLY); A is also kept in blocks, from which POLY reads it.  What a tile
-// reads is fetched before its products are waited for, then one step of 64 columns ahead.
+// A = acc / s^2, or b A + c acc (POLY); A is also kept in blocks, from which POLY reads it.  POLY keeps the diagonal
+// apart, in fp32, and leaves zeros in its place: see the numbers above.  What a tile reads is fetched before its products are waited for, then one step of 64 columns ahead.
 template <int BN, bool POLY>
 __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars, const NsParams& p, int total, __half* S, float alpha, float beta,
                                              uint32_t& n) {
@@ -329,6 +334,20 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
         if (row0 + r < rows && c < rows) *reinterpret_cast<uint4*>(S + mat + (int64_t)(row0 + r) * ld + c) = val;
       }
     }
+    // The diagonal, by the warp that has just stored its block of 32 x 32 (apart from the loop above, whose registers are all taken).
+    if (POLY && row0 >= col_begin && row0 < col_end && ((row0 - col_begin) & 127) < 64) {
+      uint32_t v[32];
+      tmem_ld32(taddr + (row0 - tile_col), v);
+      float acc = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) acc = k == lane ? __uint_as_float(v[k]) : acc;
+      __syncwarp();
+      if (row0 + lane < rows) {
+        const __half x = __ldcg(p.gram_blk + ns_block(tl.b, row0, row0, rows, rows) + (lane >> 3) * 256 + lane * 8 + (lane & 7));
+        p.diag[(int64_t)tl.b * rows + row0 + lane] = fmaf(beta, __half2float(x), alpha * acc);
+        S[mat + (int64_t)(row0 + lane) * (ld + 1)] = __float2half_rn(0.0f);
+      }
+    }
     ns_tile_done<BN>(e, bars, n);
   }
   return true;
@@ -394,8 +413,8 @@ __device__ __forceinline__ void ns_emit(const NsParams& p, const uint4& acc, int
   }
 }
 
-// x = a X + acc, stored as the next X (fp32 blocks and fp16 rows), as the result, or applied to the weights.
-template <int BN, bool LAST>
+// x = (a + diagonal) X + acc (the diagonal's entry of the row, TALL: of the column), stored as the next X (fp32 blocks and fp16 rows), as the result, or applied to the weights.
+template <bool TALL, int BN, bool LAST>
 __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& bars, const NsParams& p, int total, __half* hi_out, uint32_t& n) {
   const int lane = e.lane, rows = p.m, cols = p.n;
   const int vec = (cols & 3) == 0 ? 4 : (cols & 1) == 0 ? 2 : 1;
@@ -407,10 +426,15 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
     const bool skip = LAST && (p.out_mode == OUT_W_BF16 || p.out_mode == OUT_W_F32) && p.bad[tl.b] != 0;
     const int col_end = row0 >= rows ? 0 : col_first + BN < cols ? col_first + BN : cols;
     float4* blk = reinterpret_cast<float4*>(p.x32 + ns_block(tl.b, row0, col_first, rows, cols)) + lane;   // + 256 per 32 columns
+    const float* diag = p.diag + (int64_t)tl.b * p.mm;
+    if (!TALL) *e.factor = row0 + lane < rows ? p.a + __ldcg(diag + row0 + lane) : 0.0f;   // (a register too many: 20 spills)
     float4 next[8];
+    float next_a = 0.0f;                                  // TALL: of column `lane` of the step
     auto fetch = [&](int step) {
 #pragma unroll
       for (int q = 0; q < 8; ++q) next[q] = __ldcg(blk + step * 256 + 32 * q);
+      const int c = col_first + 32 * step + lane;
+      if (TALL) next_a = c < cols ? p.a + __ldcg(diag + c) : 0.0f;
     };
     if (col_first + e.half * 64 < col_end) fetch(2 * e.half);
     if (!ns_tile_ready<BN>(e, bars, n)) return false;
@@ -429,12 +453,14 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
         float4 x32[8];
         uint32_t v[32];
         tmem_ld32(taddr + 32 * (step + h), v);
+        const float row_a = TALL ? 0.0f : *e.factor;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-          x32[q].x = fmaf(p.a, next[q].x, __uint_as_float(v[4 * q]));
-          x32[q].y = fmaf(p.a, next[q].y, __uint_as_float(v[4 * q + 1]));
-          x32[q].z = fmaf(p.a, next[q].z, __uint_as_float(v[4 * q + 2]));
-          x32[q].w = fmaf(p.a, next[q].w, __uint_as_float(v[4 * q + 3]));
+          auto factor = [&](int c) { return TALL ? __shfl_sync(0xffffffffu, next_a, c) : row_a; };
+          x32[q].x = fmaf(factor(4 * q), next[q].x, __uint_as_float(v[4 * q]));
+          x32[q].y = fmaf(factor(4 * q + 1), next[q].y, __uint_as_float(v[4 * q + 1]));
+          x32[q].z = fmaf(factor(4 * q + 2), next[q].z, __uint_as_float(v[4 * q + 2]));
+          x32[q].w = fmaf(factor(4 * q + 3), next[q].w, __uint_as_float(v[4 * q + 3]));
         }
         if (h == 0 ? col0 + 32 < col_end : col0 + 96 < col_end) fetch(h == 0 ? step + 1 : step + 4);
         if constexpr (!LAST) {
@@ -574,6 +600,7 @@ ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ N
     NsEpi e;
     e.tmem_base = tmem_base; e.rank = rank;
     e.stage = gen + NS_RING + NS_BARS + (warp - 2) * NS_STAGING;
+    e.factor = reinterpret_cast<float*>(gen + NS_RING + NS_BARS + NS_EPI_WARPS * NS_STAGING + (warp - 2) * NS_FACTORS) + lane;
     e.quarter = warp & 3; e.half = (warp - 2) >> 2; e.lane = lane;
     e.abort_flag = abort_flag; e.d_status = p.d_status;
     uint32_t ns = 0, nu = 0;
@@ -590,9 +617,9 @@ ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ N
       else if (kind == 1)
         ok = ns_store_sym<BS, true>(e, bs, p, sym_total, p.poly, p.c, p.b, ns);
       else if (k < p.steps - 1)
-        ok = ns_store_update<BU, false>(e, bu, p, upd_total, p.hi[(k + 1) & 1], nu);
+        ok = ns_store_update<TALL, BU, false>(e, bu, p, upd_total, p.hi[(k + 1) & 1], nu);
       else
-        ok = ns_store_update<BU, true>(e, bu, p, upd_total, nullptr, nu);
+        ok = ns_store_update<TALL, BU, true>(e, bu, p, upd_total, nullptr, nu);
       if (!ok) break;
       if (q + 1 < products) {                       // this CTA's part of the product is in memory: count it
         // (no barrier among the warps: one that gave up must not leave the others waiting)
@@ -776,7 +803,7 @@ ns_split_kernel(const NsInput p) {
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-struct NsWs { size_t hi[2], x32, gram, gram_blk, poly, partials, bad, arrivals, total; int64_t ld, mm, gld; int blocks; };
+struct NsWs { size_t hi[2], x32, gram, gram_blk, poly, diag, partials, bad, arrivals, total; int64_t ld, mm, gld; int blocks; };
 
 constexpr int kNormBlocks = 592;
 
@@ -794,6 +821,7 @@ NsWs ns_layout(int64_t m, int64_t n, int64_t batch) {
   L.gram = off;     off = align_up(off + g, 256);
   L.gram_blk = off; off = align_up(off + (size_t)batch * ceil_div(L.mm, 32) * ceil_div(L.mm, 32) * 2048, 256);
   L.poly = off;     off = align_up(off + g, 256);
+  L.diag = off;     off = align_up(off + (size_t)batch * L.mm * 4, 256);
   L.partials = off; off = align_up(off + (size_t)batch * L.blocks * 8, 256);
   L.bad = off;      off = align_up(off + (size_t)batch * 4, 256);
   L.arrivals = off; off = align_up(off + 4, 256);
@@ -942,6 +970,7 @@ cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st) {
   p.gram_blk = reinterpret_cast<__half*>(ws + L.gram_blk);
   p.gram = reinterpret_cast<__half*>(ws + L.gram);
   p.poly = reinterpret_cast<__half*>(ws + L.poly);
+  p.diag = reinterpret_cast<float*>(ws + L.diag);
   p.inv_s2 = 1.0f / (s * s);
   p.a = pr.coef_a; p.b = pr.coef_b; p.c = pr.coef_c;
   p.out = a.out;

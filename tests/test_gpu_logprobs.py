@@ -312,6 +312,51 @@ def test_backward_of_bad_targets_and_of_no_rows(bf16):
         assert st == 0 and np.all(dw == (0 if init is None else 1))
 
 
+@pytest.mark.parametrize("T,d,V,targets,masked,dh32,dw32,acc", [
+    (1, 64, 1000, 1, False, False, False, False),
+    (1, 2112, 600, 1, False, True, True, False),
+    (5, 128, 3000, 2, False, True, False, True),
+    (40, 64, 900, 7, True, False, True, True),
+    (300, 192, 520, 1, False, True, True, False),          # one target for all
+    (2500, 64, 300, 40, True, True, False, False),
+    (9700, 64, 260, 3, True, True, True, False),           # more rows than one chunk
+    (9700, 64, 260, 260, False, False, False, True),
+])
+def test_the_targets_entry_is_not_rounded(T, d, V, targets, masked, dh32, dw32, acc):
+    """Upstream gradients that put every target's entry half way between two bf16 numbers: its term keeps 32 bits, so only
+    the other entries' roundings are left, whose terms carry p."""
+    h, w, y, rng = make(T + V, T, d, V, w_std=0.02)
+    y = rng.integers(0, targets, T).astype(np.int32) * (V // targets)
+    mask = (rng.random(T) < 0.7).astype(np.uint8) if masked else None
+    if masked:
+        mask[0] = 1
+    fwd = O.logprobs(h, w, y, None, 1.0)
+    gl = ((1 + 2.0**-8) / -np.expm1(fwd["logp"])).astype(np.float32)
+    on = np.ones(T) if mask is None else (mask != 0).astype(np.float64)
+    init = rng.standard_normal((V, d)).astype(np.float32) if acc else None
+    if acc and not dw32:
+        init = np.round(init * 16) / 16                    # exact in bf16
+    dh, dw, _ = O.logprobs_backward(h, w, y, mask, fwd["lse"], None, gl, None, None, 1.0)
+    got_dh, got_dw, st = call_bwd(h, w, y, mask, fwd["lse"], None, gl, None, None, 1.0, dh32=dh32, dw32=dw32, dw_init=init)
+    assert st == 0
+    _, tol, _ = tolerances(h, w, 1.0, fwd)
+    p = np.exp(h.astype(np.float64) @ w.T.astype(np.float64) - fwd["lse"].astype(np.float64)[:, None]) * (gl * on)[:, None]
+    slack = (2 * tol + 2.0**-20) * p                       # of a term in p, as elsewhere, and its rounding to bf16
+    slack = slack + 2.0**-8 * p * (np.arange(V)[None, :] != y[:, None])
+    slack[np.arange(T), y] += 2.0**-22 * gl * on           # the target's entry: rounded to 32 bits twice
+    size = p.copy()
+    size[np.arange(T), y] += gl * on
+    aw, ah = np.abs(w).astype(np.float64), np.abs(h).astype(np.float64)
+    bound_h = slack @ aw + (V + 64) * 2.0**-24 * (size @ aw) + (0 if dh32 else 2.0**-8) * np.abs(dh)
+    bound_w = slack.T @ ah + (T + 64) * 2.0**-24 * (size.T @ ah)
+    if acc:
+        dw = dw + init
+        bound_w = bound_w + 2.0**-23 * (np.abs(dw) + np.abs(init))
+    bound_w = bound_w + (0 if dw32 else 2.0**-8) * np.abs(dw)
+    assert np.all(np.abs(got_dh - dh) <= bound_h)
+    assert np.all(np.abs(got_dw - dw) <= bound_w)
+
+
 def test_gradients_match_differences_of_the_forward():
     """Central differences of the library's own fp32 forward along a random direction of H and of W."""
     T, d, V, inv_t = 12, 32, 50, 0.8
