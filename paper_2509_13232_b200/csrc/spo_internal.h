@@ -269,13 +269,14 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
 int lp_dh_splits(int64_t rows, int32_t d, int32_t V);    // parts of dH's contraction over the vocabulary
 // The target entry of a token's logit gradient is by far its largest, and what rounding it to bf16 takes off does not
 // average out over the few tokens of a vocabulary row.  So the gradient launch keeps that rest (by token of the chunk), and it
-// is added in fp32: rest W[y] to the token's dH, the sum of rest H over a target's tokens to the target's row of dW.
+// is added in fp32: rest W[y] to the token's dH, the sum of rest H over a target's tokens to the target's row of dW (that sum
+// as bf16: it is 2^-8 of the term at most, so its own rounding is 2^-16 of it).
 struct TargetRest {
   const int32_t* y;                       // all by token of the chunk
   const uint8_t* mask;
   float* rest;                            // NULL: the log-prob has no upstream gradient, nothing is kept
-  int32_t* slot;                          // [V] of a vocabulary row that is some token's target: the first such token
-  float* rows;                            // [token][d], of first tokens: the sum of rest H over all of the target's tokens
+  int32_t* slot;                          // [V] the first token that has this target, or -1 (cleared by the gradient launch)
+  __nv_bfloat16* rows;                    // [token][d], of first tokens: the sum of rest H over all of the target's tokens
 };
 struct LpBwdScratch {
   __nv_bfloat16* g;
@@ -285,7 +286,7 @@ struct LpBwdScratch {
   float* split;
   float* rest;
   int32_t* slot;
-  float* rest_rows;
+  __nv_bfloat16* rest_rows;
   uint32_t* progress;
 };
 cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream_t st);

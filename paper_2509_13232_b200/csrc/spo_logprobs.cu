@@ -1147,15 +1147,17 @@ lp_rest_kernel(const RestParams p) {
       }
     }
     if (c < p.d) {
-      float4* dst = reinterpret_cast<float4*>(p.dw ? p.dw + (int64_t)y * p.d + c : p.r.rows + (int64_t)t * p.d + c);
+      if (p.dw) {
+        float4* dst = reinterpret_cast<float4*>(p.dw + (int64_t)y * p.d + c);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float4 v = make_float4(acc[4 * h], acc[4 * h + 1], acc[4 * h + 2], acc[4 * h + 3]);
-        if (p.dw) {
-          const float4 o = dst[h];
-          v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        for (int h = 0; h < 2; ++h) {
+          float4 v = dst[h];
+          v.x += acc[4 * h]; v.y += acc[4 * h + 1]; v.z += acc[4 * h + 2]; v.w += acc[4 * h + 3];
+          dst[h] = v;
         }
-        dst[h] = v;
+      } else {
+        *reinterpret_cast<uint4*>(p.r.rows + (int64_t)t * p.d + c) =
+            make_uint4(pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3]), pack_bf16(acc[4], acc[5]), pack_bf16(acc[6], acc[7]));
       }
     }
   }
@@ -1266,7 +1268,7 @@ LpBwdWs lp_bwd_layout(int64_t T, int32_t d, int32_t V, int32_t dtype) {
     off = align_up(off + parts, 256);
     L.rest = off;      off = align_up(off + (size_t)first * 4, 256);
     L.slot = off;      off = align_up(off + (size_t)V * 4, 256);
-    L.rest_rows = off; off = align_up(off + (size_t)first * d * 4, 256);
+    L.rest_rows = off; off = align_up(off + (size_t)first * d * 2, 256);
   }
   L.total = off;
   return L;
@@ -1378,7 +1380,7 @@ cudaError_t lp_backward(const LpBwd& a, char* ws, cudaStream_t st) {
     w.split = reinterpret_cast<float*>(ws + L.split);
     w.rest = reinterpret_cast<float*>(ws + L.rest);
     w.slot = reinterpret_cast<int32_t*>(ws + L.slot);
-    w.rest_rows = reinterpret_cast<float*>(ws + L.rest_rows);
+    w.rest_rows = reinterpret_cast<__nv_bfloat16*>(ws + L.rest_rows);
     w.progress = reinterpret_cast<uint32_t*>(ws + L.progress);
     return launch_lp_bwd_bf16(a, w, st);
   }

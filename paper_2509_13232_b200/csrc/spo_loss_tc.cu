@@ -141,7 +141,7 @@ struct GemmParams {
   int k_splits, k_per;                       // DH: the contraction cut into k_splits parts of k_per k-blocks, each with an
                                              // fp32 result of its own in `out`, [part][rows_valid][ldo]
   TargetRest rest;                           // G: rest is stored;  DH (one part), DW: it is added to the result
-  int n_rest;                                // DH: V;  DW: tokens of the chunk
+  int n_rest;                                // DH: V
   const __nv_bfloat16* w_rows;               // DH: W, [vocabulary row][ldo]
 };
 
@@ -208,29 +208,16 @@ __device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, b
                          pack_bf16(g[8 * q + 4], g[8 * q + 5]), pack_bf16(g[8 * q + 6], g[8 * q + 7]));
 }
 
-// v += r x the row's 32 values from `row` on, of which the first `cols` exist (a multiple of 8)
-__device__ __forceinline__ void add_row(uint32_t (&v)[32], const __nv_bfloat16* row, float r, int cols) {
+// v += r x the 32 bf16 values of `row`
+__device__ __forceinline__ void add_row(uint32_t (&v)[32], const uint4 (&row)[4], float r) {
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    if (8 * q >= cols) break;
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(row) + q);
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+    const uint32_t x[4] = {row[q].x, row[q].y, row[q].z, row[q].w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       v[8 * q + 2 * k] = __float_as_uint(fmaf(r, __uint_as_float(x[k] << 16), __uint_as_float(v[8 * q + 2 * k])));
       v[8 * q + 2 * k + 1] = __float_as_uint(fmaf(r, __uint_as_float(x[k] & 0xFFFF0000u), __uint_as_float(v[8 * q + 2 * k + 1])));
     }
-  }
-}
-__device__ __forceinline__ void add_row(uint32_t (&v)[32], const float* row, int cols) {
-#pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    if (4 * q >= cols) break;
-    const float4 w = __ldg(reinterpret_cast<const float4*>(row) + q);
-    v[4 * q] = __float_as_uint(__uint_as_float(v[4 * q]) + w.x);
-    v[4 * q + 1] = __float_as_uint(__uint_as_float(v[4 * q + 1]) + w.y);
-    v[4 * q + 2] = __float_as_uint(__uint_as_float(v[4 * q + 2]) + w.z);
-    v[4 * q + 3] = __float_as_uint(__uint_as_float(v[4 * q + 3]) + w.w);
   }
 }
 
@@ -324,6 +311,9 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
   constexpr bool KS = MODE == MODE_DH && LP >= 0;             // units are (tile, part of the contraction)
   const int total_units = p.m_tiles * p.nsplit * (KS ? p.k_splits : 1);
 
+  if (MODE == MODE_G && LP >= 0 && p.rest.rest) {
+    for (int i = blockIdx.x * NUM_THREADS + threadIdx.x; i < p.cols_valid; i += gridDim.x * NUM_THREADS) p.rest.slot[i] = -1;
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { mbar_init(full0 + 8 * s, 1); mbar_init(empty0 + 8 * s, 1); }
     for (int b = 0; b < BUFS; ++b) { mbar_init(tfull0 + 8 * b, 1); mbar_init(tempty0 + 8 * b, EPI_WARPS * CG); }
@@ -445,6 +435,12 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
     const uint32_t tempty_leader = map_to_cta(tempty0, 0);
     uint32_t tile = 0;
     bool ok = true;
+    auto slot_of = [&](int unit) {                       // DW with LP: of this lane's row in a unit
+      if (MODE != MODE_DW || LP < 0 || p.rest.rest == nullptr || unit >= total_units) return -1;
+      const int64_t r = p.out_row0 + (int64_t)unit_of(unit, p).m_tile * GROUP_M + row;
+      return r < p.rows_valid ? p.rest.slot[r] : -1;
+    };
+    int32_t slot_next = slot_of(group);
     for (int u = group; u < total_units && ok; u += n_groups) {
       const Unit un = unit_of(KS ? u / p.k_splits : u, p);
       const int64_t grow = p.out_row0 + (int64_t)un.m_tile * GROUP_M + row;   // global output row of this lane
@@ -482,23 +478,37 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         lse2 = p.lse[grow] * kLog2e;
       }
       float* const rest_at = MODE == MODE_G && LP >= 0 && p.rest.rest ? p.rest.rest + (grow - p.out_row0) : nullptr;
-      float rest = 0.0f;                                                   // DH, DW with LP: what the row's targets are
-      const __nv_bfloat16* rest_w = nullptr;                               // still owed (see TargetRest)
-      const float* rest_sum = nullptr;
-      if (MODE == MODE_DH && LP >= 0 && p.rest.rest && row_ok) {
+      // DH, DW with LP: what the row's targets are still owed (see TargetRest), `owed` times a bf16 row, which is fetched one
+      // step of 64 columns ahead, the first one before the tile's products are waited for
+      constexpr bool OWED = (MODE == MODE_DH || MODE == MODE_DW) && LP >= 0;
+      float owed = 0.0f;
+      const uint4* owed_row = nullptr;
+      uint4 owed0[4], owed1[4];
+      if (MODE == MODE_DH && OWED && p.rest.rest && row_ok) {
         const int32_t yy = p.rest.y[grow];
         if (yy >= 0 && yy < p.n_rest && (p.rest.mask == nullptr || p.rest.mask[grow] != 0)) {
-          rest = p.rest.rest[grow];
-          rest_w = p.w_rows + (int64_t)yy * p.ldo;
+          owed = p.rest.rest[grow];
+          owed_row = reinterpret_cast<const uint4*>(p.w_rows + (int64_t)yy * p.ldo);
         }
       }
-      if (MODE == MODE_DW && LP >= 0 && p.rest.rest && row_ok) {
-        // rows that are nobody's target have no slot: theirs is whatever the scratch held, and then does not lead
-        // to a token with this target
-        const int32_t s = p.rest.slot[grow];
-        if (s >= 0 && s < p.n_rest && p.rest.y[s] == grow && (p.rest.mask == nullptr || p.rest.mask[s] != 0))
-          rest_sum = p.rest.rows + (int64_t)s * p.ldo;
+      if (MODE == MODE_DW && OWED) {
+        const int32_t s = slot_next;
+        slot_next = slot_of(u + n_groups);
+        if (s >= 0) {
+          owed = 1.0f;
+          owed_row = reinterpret_cast<const uint4*>(p.rest.rows + (int64_t)s * p.ldo);
+        }
       }
+      const bool any_owed = OWED && __any_sync(0xffffffffu, owed != 0.0f);
+      auto fetch_owed = [&](int col0) {
+        if (!OWED) return;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const bool on = owed != 0.0f && col0 < p.cols_valid;
+          owed0[q] = on ? __ldg(owed_row + col0 / 8 + q) : make_uint4(0u, 0u, 0u, 0u);
+          owed1[q] = on && col0 + 32 < p.cols_valid ? __ldg(owed_row + col0 / 8 + 4 + q) : make_uint4(0u, 0u, 0u, 0u);
+        }
+      };
       float rs = 1.0f;                                                     // DH: factor of this lane's output row
       if (MODE == MODE_FWD || MODE == MODE_G || MODE == MODE_E) {
         if (row_ok && (LP < 0 || p.y)) yt = p.y[grow];
@@ -516,6 +526,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       }
       if (MODE == MODE_DH && p.rowscale && row_ok) rs = p.rowscale[grow];
       for (int n = un.n_begin; n < un.n_end && ok; ++n, ++tile) {
+        if (OWED && any_owed) fetch_owed(n * BN + half * EPI_N);
         {                                   // one lane polls (with backoff); the warp reconverges on the outcome
           int good = 1;
           if (lane == 0)
@@ -698,13 +709,10 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                   v1[j] = __float_as_uint(rs == 0.0f ? 0.0f : __uint_as_float(v1[j]) * rs);
                 }
               }
-              if (MODE == MODE_DH && LP >= 0 && rest != 0.0f) {
-                add_row(v0, rest_w + col0, rest, p.cols_valid - col0);
-                add_row(v1, rest_w + col0 + 32, rest, p.cols_valid - col0 - 32);
-              }
-              if (MODE == MODE_DW && LP >= 0 && rest_sum) {
-                add_row(v0, rest_sum + col0, p.cols_valid - col0);
-                add_row(v1, rest_sum + col0 + 32, p.cols_valid - col0 - 32);
+              if (OWED && any_owed) {
+                add_row(v0, owed0, owed);
+                add_row(v1, owed1, owed);
+                if (r2 + 1 < EPI_N / 64) fetch_owed(col0 + 64);
               }
               bf16_values(v0, piece);
               bf16_values(v1, piece + 4);
@@ -734,8 +742,14 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
 #pragma unroll
               for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(rs == 0.0f ? 0.0f : __uint_as_float(v[j]) * rs);
             }
-            if (MODE == MODE_DH && LP >= 0 && rest != 0.0f) add_row(v, rest_w + col0, rest, p.cols_valid - col0);
-            if (MODE == MODE_DW && LP >= 0 && rest_sum) add_row(v, rest_sum + col0, p.cols_valid - col0);
+            if (OWED && any_owed) {
+              if (ch & 1) {
+                add_row(v, owed1, owed);
+                if (ch + 1 < EPI_N / 32) fetch_owed(col0 + 32);
+              } else {
+                add_row(v, owed0, owed);
+              }
+            }
             uint4 piece[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) piece[q] = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
@@ -1358,7 +1372,7 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream
       p.cols_valid = a.d;
       p.out = a.dW; p.out_bf16 = 1; p.ldo = a.d; p.accumulate = a.accumulate;
       p.partial = t0 > 0 ? w.partial : nullptr;
-      p.rest = rest; p.n_rest = (int)rows;
+      p.rest = rest;
       p.d_status = a.d_status;
       e = lp_narrow(rows) ? launch_gemm<MODE_DW, false, 0, true>(mG_mn, mH_mn, p, progress, st)
                           : launch_gemm<MODE_DW, false, 0, false>(mG_mn, mH_mn, p, progress, st);

@@ -286,9 +286,22 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
         for (int q = 0; q < 4; ++q) next[4 * h + q] = c0 + 32 * h < col_end ? __ldcg(src + 32 * q) : make_uint4(0u, 0u, 0u, 0u);
       }
     };
+    // The warp that has the block of 32 x 32 on the diagonal: lane's own column.
+    const bool own = POLY && row0 >= col_begin && row0 < col_end && ((row0 - col_begin) & 127) < 64;
+    float d = 0.0f;
+    if (own && row0 + lane < rows)
+      d = beta * __half2float(__ldcg(p.gram_blk + ns_block(tl.b, row0, row0, rows, rows) + (lane >> 3) * 256 + lane * 8 + (lane & 7)));
     if (POLY && col_begin < col_end) fetch(col_begin);
     if (!ns_tile_ready<BN>(e, bars, n)) return false;
     const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN;
+    if (own) {
+      uint32_t v[32];
+      tmem_ld32(taddr + (row0 - tile_col), v);
+      float acc = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 32; ++k) acc = k == lane ? __uint_as_float(v[k]) : acc;
+      if (row0 + lane < rows) p.diag[(int64_t)tl.b * rows + row0 + lane] = fmaf(alpha, acc, d);
+    }
 #pragma unroll 1
     for (int col0 = col_begin; col0 < col_end; col0 += 128) {
       uint32_t v0[32], v1[32];
@@ -328,24 +341,18 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         int r, cc;
-        const uint4 val = stage_get(e.stage, lane, i, r, cc);
+        uint4 val = stage_get(e.stage, lane, i, r, cc);
         const int c = col0 + cc * 8;
+        if (POLY && own && (unsigned)(row0 - col0) < 64u) {
+          const int at = row0 + r - c;                    // column of the piece on the diagonal
+          const uint32_t keep = at & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+          if (at >> 1 == 0) val.x &= keep;
+          if (at >> 1 == 1) val.y &= keep;
+          if (at >> 1 == 2) val.z &= keep;
+          if (at >> 1 == 3) val.w &= keep;
+        }
         // the pitch is a multiple of 8, so a piece that begins inside the row may be stored whole
         if (row0 + r < rows && c < rows) *reinterpret_cast<uint4*>(S + mat + (int64_t)(row0 + r) * ld + c) = val;
-      }
-    }
-    // The diagonal, by the warp that has just stored its block of 32 x 32 (apart from the loop above, whose registers are all taken).
-    if (POLY && row0 >= col_begin && row0 < col_end && ((row0 - col_begin) & 127) < 64) {
-      uint32_t v[32];
-      tmem_ld32(taddr + (row0 - tile_col), v);
-      float acc = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 32; ++k) acc = k == lane ? __uint_as_float(v[k]) : acc;
-      __syncwarp();
-      if (row0 + lane < rows) {
-        const __half x = __ldcg(p.gram_blk + ns_block(tl.b, row0, row0, rows, rows) + (lane >> 3) * 256 + lane * 8 + (lane & 7));
-        p.diag[(int64_t)tl.b * rows + row0 + lane] = fmaf(beta, __half2float(x), alpha * acc);
-        S[mat + (int64_t)(row0 + lane) * (ld + 1)] = __float2half_rn(0.0f);
       }
     }
     ns_tile_done<BN>(e, bars, n);

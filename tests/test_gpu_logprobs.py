@@ -349,6 +349,8 @@ def test_the_targets_entry_is_not_rounded(T, d, V, targets, masked, dh32, dw32, 
     aw, ah = np.abs(w).astype(np.float64), np.abs(h).astype(np.float64)
     bound_h = slack @ aw + (V + 64) * 2.0**-24 * (size @ aw) + (0 if dh32 else 2.0**-8) * np.abs(dh)
     bound_w = slack.T @ ah + (T + 64) * 2.0**-24 * (size.T @ ah)
+    if not dw32:                                           # the rest of the target's term (2^-8 of it) goes through bf16
+        bound_w = bound_w + 2.0**-16 * (size.T @ ah)
     if acc:
         dw = dw + init
         bound_w = bound_w + 2.0**-23 * (np.abs(dw) + np.abs(init))
