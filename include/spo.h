@@ -558,7 +558,8 @@ int32_t spo_logprobs(const void* H, int64_t ldH, const void* W, int32_t dtype, c
  *   mask        rows with mask 0 have dH = 0 and add nothing to dW, whatever their H holds
  *   dH          device out [T][d];  dW  device out [V][d], overwritten or (dW_accumulate) added to.  Types:
  *               bf16 H / W: dH and dW bf16 or fp32 each; fp32 H / W: both fp32.  A bf16 dW is summed over all
- *               tokens in fp32 and rounded once.
+ *               tokens in fp32 and rounded once.  For the products dz is rounded to bf16, but for the target's
+ *               entry, by far the largest of its row, whose rounding is put back in fp32.
  *   ws          device scratch, spo_workspace_bytes(SPO_WS_LOGPROBS_BWD, T, d, V, 0, 0, 0) bytes: a chunk of dz (a few
  *               thousand rows by V, bf16; fp32 for fp32 inputs), never all of it
  * A target outside [0,V) contributes nothing through g_logp and sets SPO_DEV_ID_OUT_OF_RANGE (unless masked).
@@ -579,7 +580,7 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
  *   M <- momentum M + G;  U = G + momentum M (nesterov) or M;
  *   W <- (1 - lr weight_decay) W - lr scale X,  scale = 1 (SPO_MUON_SCALE_NONE), sqrt(max(1, m/n))
  *   (SPO_MUON_SCALE_SPECTRAL) or 0.2 sqrt(max(m, n)) (SPO_MUON_SCALE_RMS).
- * Iterates are pairs of fp16 numbers (22 bits), products fp16 with fp32 sums; the Frobenius norm is summed in
+ * Iterates are kept in fp32; the products' operands are fp16 with fp32 sums; the Frobenius norm is summed in
  * fp64 in a fixed order, so results repeat bit for bit.
  *
  *   G         device in  [batch][m][n], fp32 or bf16 (dtype)

@@ -86,7 +86,7 @@ def muon_update(w, momentum, g, lr, mu, weight_decay=0.0, nesterov=True, mode=0,
 
 
 def newton_schulz_rounded(g, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7):
-    """The same iteration with fp16 roundings where the library documents them (iterate as a pair of fp16 numbers scaled
+    """The same iteration with fp16 roundings where the library documents them (iterate at 22 bits or more, its fp16 part the operand, scaled
     by a power of two, the Gram matrix and the polynomial once each, the latter's diagonal not at all), everything else in 64 bits: what those roundings
     alone do to a given input, which is what a tolerance has to allow for."""
     a, b, c = coefficients

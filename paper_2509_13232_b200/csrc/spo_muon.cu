@@ -8,15 +8,16 @@
 // every rounding made in X while they are small.  So X is held twice, in fp32 for the term a X and in fp16
 // for the products, whose spectrum is small where X's is; both times s = 2^round(log2 sqrt(max(m, n))), which
 // puts the entries of an orthogonal matrix near one.  Errors against 64 bits for a 512 x 512 update of rank 16
-// under no noise: this 4e-4, fp16 alone 4e-2, bf16 alone 0.33 (a full-rank Gaussian: 1.5e-3, 1.3e-3, 1.1e-2).  fp16 rather than bf16 because everything
-// here is bounded by about 10 in magnitude and fp16 has 8 times finer steps.  A and b A + c A A are rounded
+// under no noise: this 8e-4, fp16 alone 4e-2, bf16 alone 0.33 (a full-rank Gaussian: 8e-4, 1.3e-3, 1.1e-2).  fp16
+// rather than bf16 because everything here is bounded by about 10 in magnitude and fp16 has 8 times finer steps.  A and b A + c A A are rounded
 // to fp16 once each, but for the diagonal of the latter: near convergence it is -2.7 and the rest almost nothing,
 // so it stays in fp32 and multiplies X in fp32 (19 x 183: error of the iteration 8e-4; rounded with the rest 1.7e-3).
+// That costs about a microsecond in each of a step's last two products (4 x 1000 x 2730: 575 us, 550 without).
 // All sums are fp32.
 //
 // Work.  A and A A are symmetric: only the blocks on and above the diagonal are computed and stored (a block below
-// it is read as the transposed operand of its mirror image), 3 m^2 n + m^3 operations a step for m <= n instead of 4 m^2 n + 2 m^3.  Five steps of a 4096 x 4096
-// matrix are 1.37 TFLOP: tensor-bound from a few hundred rows on, launch-bound below.
+// it is read as the transposed operand of its mirror image), 3 m^2 n + m^3 operations a step for m <= n instead of
+// 4 m^2 n + 2 m^3.  Five steps of a 4096 x 4096 matrix are 1.37 TFLOP: tensor-bound from a few hundred rows on, launch-bound below.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -262,7 +263,8 @@ __device__ __forceinline__ void ns_tile_done(const NsEpi& e, const NsBars& bars,
 }
 
 // A = acc / s^2, or b A + c acc (POLY); A is also kept in blocks, from which POLY reads it.  POLY keeps the diagonal
-// apart, in fp32, and leaves zeros in its place: see the numbers above.  What a tile reads is fetched before its products are waited for, then one step of 64 columns ahead.
+// apart, in fp32, and leaves zeros in its place: see the numbers above.  What a tile reads is fetched before its
+// products are waited for, then one step of 64 columns ahead.
 template <int BN, bool POLY>
 __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars, const NsParams& p, int total, __half* S, float alpha, float beta,
                                              uint32_t& n) {
@@ -290,7 +292,8 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
     const bool own = POLY && row0 >= col_begin && row0 < col_end && ((row0 - col_begin) & 127) < 64;
     float d = 0.0f;
     if (own && row0 + lane < rows)
-      d = beta * __half2float(__ldcg(p.gram_blk + ns_block(tl.b, row0, row0, rows, rows) + (lane >> 3) * 256 + lane * 8 + (lane & 7)));
+      d = beta * __half2float(__ldcg(p.gram_blk + ns_block(tl.b, row0, row0, rows, rows) + (lane >> 3) * 256 + lane * 8 +
+                                     (lane & 7)));
     if (POLY && col_begin < col_end) fetch(col_begin);
     if (!ns_tile_ready<BN>(e, bars, n)) return false;
     const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN;
@@ -420,7 +423,8 @@ __device__ __forceinline__ void ns_emit(const NsParams& p, const uint4& acc, int
   }
 }
 
-// x = (a + diagonal) X + acc (the diagonal's entry of the row, TALL: of the column), stored as the next X (fp32 blocks and fp16 rows), as the result, or applied to the weights.
+// x = (a + diagonal) X + acc (the diagonal's entry of the row, TALL: of the column), stored as the next X (fp32 blocks
+// and fp16 rows), as the result, or applied to the weights.
 template <bool TALL, int BN, bool LAST>
 __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& bars, const NsParams& p, int total, __half* hi_out, uint32_t& n) {
   const int lane = e.lane, rows = p.m, cols = p.n;
@@ -434,7 +438,8 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
     const int col_end = row0 >= rows ? 0 : col_first + BN < cols ? col_first + BN : cols;
     float4* blk = reinterpret_cast<float4*>(p.x32 + ns_block(tl.b, row0, col_first, rows, cols)) + lane;   // + 256 per 32 columns
     const float* diag = p.diag + (int64_t)tl.b * p.mm;
-    if (!TALL) *e.factor = row0 + lane < rows ? p.a + __ldcg(diag + row0 + lane) : 0.0f;   // (a register too many: 20 spills)
+    // (through shared memory: kept in a register, it brought spills, 115 us for 110 on 128 x 512)
+    if (!TALL) *e.factor = row0 + lane < rows ? p.a + __ldcg(diag + row0 + lane) : 0.0f;
     float4 next[8];
     float next_a = 0.0f;                                  // TALL: of column `lane` of the step
     auto fetch = [&](int step) {
