@@ -930,10 +930,11 @@ cudaError_t launch_iterate(const NsMaps& maps, const NsParams& p, cudaStream_t s
 // Column widths of the tiles, by the time their products take: rounds of tiles over the pairs x k-blocks x the
 // nanoseconds of a k-block (610 / 380 / 240 for 512 / 256 / 128 columns, measured; 1.0 / 1.25 / 1.6 times the clocks of
 // its products, the narrow ones waiting for L2), and the exposed epilogues: one a round for 512, the last one for the others.
+// 128 for the symmetric products pays where 256 leaves pairs idle: 512 x 2048 174 us (256: 190), 1000 x 2730 273 (290).
 double sym_time(const NsParams& p, int bn) {
   const double pairs = sm_count() / 2, rounds = ceil((double)sym_tile_count(p.mm, bn) * p.batch / pairs);
   const double kb = p.kb_long + p.kb_short;
-  return bn == 512 ? rounds * (kb * 610.0 + 2 * 9000.0) : rounds * kb * 380.0 + 2 * 5000.0;
+  return bn == 512 ? rounds * (kb * 610.0 + 2 * 9000.0) : bn == 256 ? rounds * kb * 380.0 + 2 * 5000.0 : rounds * kb * 240.0 + 2 * 4000.0;
 }
 double update_time(const NsParams& p, int bn) {
   const double pairs = sm_count() / 2;
@@ -1007,8 +1008,10 @@ cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st) {
       !make_map3(&maps.poly128, p.poly, L.mm, L.mm, a.batch, L.gld, 128) ||
       !make_map3(&maps.poly64, p.poly, L.mm, L.mm, a.batch, L.gld, 64))
     return cudaErrorInvalidValue;
-  const bool wide = sym_time(p, 512) < sym_time(p, 256), narrow = update_time(p, 128) < update_time(p, 256);
-  if (wide) return narrow ? launch_iterate<512, 128>(maps, p, st) : launch_iterate<512, 256>(maps, p, st);
+  const double t512 = sym_time(p, 512), t256 = sym_time(p, 256), t128 = sym_time(p, 128);
+  const bool narrow = update_time(p, 128) < update_time(p, 256);
+  if (t512 < t256 && t512 < t128) return narrow ? launch_iterate<512, 128>(maps, p, st) : launch_iterate<512, 256>(maps, p, st);
+  if (t128 < t256) return narrow ? launch_iterate<128, 128>(maps, p, st) : launch_iterate<128, 256>(maps, p, st);
   return narrow ? launch_iterate<256, 128>(maps, p, st) : launch_iterate<256, 256>(maps, p, st);
 }
 
