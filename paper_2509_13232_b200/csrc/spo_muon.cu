@@ -12,7 +12,6 @@
 // rather than bf16 because everything here is bounded by about 10 in magnitude and fp16 has 8 times finer steps.  A and b A + c A A are rounded
 // to fp16 once each, but for the diagonal of the latter: near convergence it is -2.7 and the rest almost nothing,
 // so it stays in fp32 and multiplies X in fp32 (19 x 183: error of the iteration 8e-4; rounded with the rest 1.7e-3).
-// That costs about a microsecond in each of a step's last two products (4 x 1000 x 2730: 575 us, 550 without).
 // All sums are fp32.
 //
 // Work.  A and A A are symmetric: only the blocks on and above the diagonal are computed and stored (a block below
@@ -40,8 +39,7 @@ constexpr int NS_THREADS = 32 * (2 + NS_EPI_WARPS);
 constexpr int NS_STAGING = 4096;
 constexpr int NS_RING = 192 * 1024;             // operand stages
 constexpr int NS_BARS = 512;                    // barriers of the two kinds of product, tensor-memory address, flags
-constexpr int NS_FACTORS = 128;                 // a warp's 32 row factors
-constexpr int NS_SMEM = NS_RING + 1024 + NS_BARS + NS_EPI_WARPS * (NS_STAGING + NS_FACTORS);
+constexpr int NS_SMEM = NS_RING + 1024 + NS_BARS + NS_EPI_WARPS * NS_STAGING;
 
 template <int BN>
 struct NsCfg {
@@ -237,11 +235,13 @@ __device__ __forceinline__ bool ns_multiply(int total, int tiles, int n_tiles, i
   return true;
 }
 
+// Epilogues.  On small matrices a product lasts as long as its code takes to arrive: each of them runs once between two
+// barriers, so the 32-column steps are loops that are not unrolled (unrolled in pairs: 128 x 512 106 us for 96, four
+// 1000 x 2730 568 for 540).
 // What the epilogue warps share: barriers, tensor memory, staging buffer.
 struct NsEpi {
   uint32_t tmem_base, rank;
   uint8_t* stage;
-  volatile float* factor;                      // wide: this lane's row's, in the update
   int quarter, half, lane;
   volatile int* abort_flag;
   int32_t* d_status;
@@ -279,81 +279,65 @@ __device__ __forceinline__ bool ns_store_sym(const NsEpi& e, const NsBars& bars,
     const int64_t mat = (int64_t)tl.b * rows * ld;
     const int col_begin = (tile_col < tl.i * 256 ? tl.i * 256 : tile_col) + e.half * 64;
     const int col_end = row0 >= rows ? 0 : tile_col + BN < rows ? tile_col + BN : rows;
-    uint4 next[8];
+    uint4 next[4];
     auto fetch = [&](int c0) {
+      const uint4* src = reinterpret_cast<const uint4*>(p.gram_blk + ns_block(tl.b, row0, c0, rows, rows)) + lane;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint4* src = reinterpret_cast<const uint4*>(p.gram_blk + ns_block(tl.b, row0, c0 + 32 * h, rows, rows)) + lane;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) next[4 * h + q] = c0 + 32 * h < col_end ? __ldcg(src + 32 * q) : make_uint4(0u, 0u, 0u, 0u);
-      }
+      for (int q = 0; q < 4; ++q) next[q] = __ldcg(src + 32 * q);
     };
-    // The warp that has the block of 32 x 32 on the diagonal: lane's own column.
-    const bool own = POLY && row0 >= col_begin && row0 < col_end && ((row0 - col_begin) & 127) < 64;
-    float d = 0.0f;
-    if (own && row0 + lane < rows)
-      d = beta * __half2float(__ldcg(p.gram_blk + ns_block(tl.b, row0, row0, rows, rows) + (lane >> 3) * 256 + lane * 8 +
-                                     (lane & 7)));
     if (POLY && col_begin < col_end) fetch(col_begin);
     if (!ns_tile_ready<BN>(e, bars, n)) return false;
     const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN;
-    if (own) {
-      uint32_t v[32];
-      tmem_ld32(taddr + (row0 - tile_col), v);
-      float acc = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 32; ++k) acc = k == lane ? __uint_as_float(v[k]) : acc;
-      if (row0 + lane < rows) p.diag[(int64_t)tl.b * rows + row0 + lane] = fmaf(alpha, acc, d);
-    }
 #pragma unroll 1
     for (int col0 = col_begin; col0 < col_end; col0 += 128) {
-      uint32_t v0[32], v1[32];
-      tmem_ld32_nowait(taddr + (col0 - tile_col), v0);
-      tmem_ld32_nowait(taddr + (col0 - tile_col) + 32, v1);
-      tmem_wait_ld(v0);
-      tmem_wait_ld(v1);
-      uint4 piece[8];
+      __syncwarp();                                       // earlier read-backs of the staging buffer are done
+#pragma unroll 1
+      for (int h = 0; h < 2 && col0 + 32 * h < col_end; ++h) {
+        const int c0 = col0 + 32 * h;
+        uint32_t v[32];
+        float x[32];
+        tmem_ld32(taddr + (c0 - tile_col), v);
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        const uint32_t cw[4] = {next[q].x, next[q].y, next[q].z, next[q].w};
-        uint32_t o[4];
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t cw[4] = {next[q].x, next[q].y, next[q].z, next[q].w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int at = 8 * (q & 3) + 2 * k;
-          float x0 = alpha * __uint_as_float(q < 4 ? v0[at] : v1[at]), x1 = alpha * __uint_as_float(q < 4 ? v0[at + 1] : v1[at + 1]);
-          if (POLY) {
-            const float2 f = unpack_half(cw[k]);
-            x0 = fmaf(beta, f.x, x0);
-            x1 = fmaf(beta, f.y, x1);
+          for (int k = 0; k < 4; ++k) {
+            const int at = 8 * q + 2 * k;
+            x[at] = alpha * __uint_as_float(v[at]);
+            x[at + 1] = alpha * __uint_as_float(v[at + 1]);
+            if (POLY) {
+              const float2 f = unpack_half(cw[k]);
+              x[at] = fmaf(beta, f.x, x[at]);
+              x[at + 1] = fmaf(beta, f.y, x[at + 1]);
+            }
           }
-          o[k] = pack_half(x0, x1);
         }
-        piece[q] = make_uint4(o[0], o[1], o[2], o[3]);
-      }
-      if (POLY && col0 + 128 < col_end) fetch(col0 + 128);
-      if (!POLY) {
+        if (POLY && h == 0 && c0 + 32 < col_end) fetch(c0 + 32);
+        if (POLY && h == 1 && c0 + 96 < col_end) fetch(c0 + 96);
+        if (POLY && c0 == row0) {                         // the block on the diagonal: lane's own column
+          float d = 0.0f;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (col0 + 32 * h >= col_end) continue;
-          uint4* dst = reinterpret_cast<uint4*>(p.gram_blk + ns_block(tl.b, row0, col0 + 32 * h, rows, rows)) + lane;
+          for (int k = 0; k < 32; ++k) {
+            d = k == lane ? x[k] : d;
+            x[k] = k == lane ? 0.0f : x[k];
+          }
+          if (row0 + lane < rows) p.diag[(int64_t)tl.b * rows + row0 + lane] = d;
+        }
+        uint4* dst = reinterpret_cast<uint4*>(p.gram_blk + ns_block(tl.b, row0, c0, rows, rows)) + lane;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) dst[32 * q] = piece[4 * h + q];
+        for (int q = 0; q < 4; ++q) {
+          const uint4 piece = make_uint4(pack_half(x[8 * q], x[8 * q + 1]), pack_half(x[8 * q + 2], x[8 * q + 3]),
+                                         pack_half(x[8 * q + 4], x[8 * q + 5]), pack_half(x[8 * q + 6], x[8 * q + 7]));
+          if (!POLY) dst[32 * q] = piece;
+          stage_put_piece(e.stage, lane, 4 * h + q, piece);
         }
       }
-      stage_put(e.stage, lane, piece);
+      __syncwarp();
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         int r, cc;
-        uint4 val = stage_get(e.stage, lane, i, r, cc);
+        const uint4 val = stage_get(e.stage, lane, i, r, cc);
         const int c = col0 + cc * 8;
-        if (POLY && own && (unsigned)(row0 - col0) < 64u) {
-          const int at = row0 + r - c;                    // column of the piece on the diagonal
-          const uint32_t keep = at & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-          if (at >> 1 == 0) val.x &= keep;
-          if (at >> 1 == 1) val.y &= keep;
-          if (at >> 1 == 2) val.z &= keep;
-          if (at >> 1 == 3) val.w &= keep;
-        }
         // the pitch is a multiple of 8, so a piece that begins inside the row may be stored whole
         if (row0 + r < rows && c < rows) *reinterpret_cast<uint4*>(S + mat + (int64_t)(row0 + r) * ld + c) = val;
       }
@@ -438,8 +422,7 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
     const int col_end = row0 >= rows ? 0 : col_first + BN < cols ? col_first + BN : cols;
     float4* blk = reinterpret_cast<float4*>(p.x32 + ns_block(tl.b, row0, col_first, rows, cols)) + lane;   // + 256 per 32 columns
     const float* diag = p.diag + (int64_t)tl.b * p.mm;
-    // (through shared memory: kept in a register, it brought spills, 115 us for 110 on 128 x 512)
-    if (!TALL) *e.factor = row0 + lane < rows ? p.a + __ldcg(diag + row0 + lane) : 0.0f;
+    const float row_a = TALL || row0 + lane >= rows ? 0.0f : p.a + __ldcg(diag + row0 + lane);
     float4 next[8];
     float next_a = 0.0f;                                  // TALL: of column `lane` of the step
     auto fetch = [&](int step) {
@@ -453,19 +436,13 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
     const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN;
 #pragma unroll 1
     for (int step = 2 * e.half; col_first + 32 * step < col_end; step += 4) {
-      uint4 piece[8];                                     // !LAST: 64 columns of fp16, one round through the staging buffer
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      if (!LAST) __syncwarp();                            // earlier read-backs of the staging buffer are done
+#pragma unroll 1
+      for (int h = 0; h < 2 && col_first + 32 * (step + h) < col_end; ++h) {
         const int col0 = col_first + 32 * (step + h);
-        if (col0 >= col_end) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) piece[4 * h + q] = make_uint4(0u, 0u, 0u, 0u);
-          continue;
-        }
         float4 x32[8];
         uint32_t v[32];
         tmem_ld32(taddr + 32 * (step + h), v);
-        const float row_a = TALL ? 0.0f : *e.factor;
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
           auto factor = [&](int c) { return TALL ? __shfl_sync(0xffffffffu, next_a, c) : row_a; };
@@ -480,9 +457,11 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
           for (int q = 0; q < 8; ++q) blk[(step + h) * 256 + 32 * q] = x32[q];
 #pragma unroll
           for (int q = 0; q < 4; ++q)
-            piece[4 * h + q] = make_uint4(pack_half(x32[2 * q].x, x32[2 * q].y), pack_half(x32[2 * q].z, x32[2 * q].w),
-                                          pack_half(x32[2 * q + 1].x, x32[2 * q + 1].y), pack_half(x32[2 * q + 1].z, x32[2 * q + 1].w));
+            stage_put_piece(e.stage, lane, 4 * h + q,
+                            make_uint4(pack_half(x32[2 * q].x, x32[2 * q].y), pack_half(x32[2 * q].z, x32[2 * q].w),
+                                       pack_half(x32[2 * q + 1].x, x32[2 * q + 1].y), pack_half(x32[2 * q + 1].z, x32[2 * q + 1].w)));
         } else {
+          uint4 piece[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q)
             piece[q] = make_uint4(__float_as_uint(x32[q].x), __float_as_uint(x32[q].y), __float_as_uint(x32[q].z), __float_as_uint(x32[q].w));
@@ -497,7 +476,7 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
         }
       }
       if constexpr (!LAST) {
-        stage_put(e.stage, lane, piece);
+        __syncwarp();
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           int r, cc;
@@ -612,7 +591,6 @@ ns_iterate_kernel(const __grid_constant__ NsMaps maps, const __grid_constant__ N
     NsEpi e;
     e.tmem_base = tmem_base; e.rank = rank;
     e.stage = gen + NS_RING + NS_BARS + (warp - 2) * NS_STAGING;
-    e.factor = reinterpret_cast<float*>(gen + NS_RING + NS_BARS + NS_EPI_WARPS * NS_STAGING + (warp - 2) * NS_FACTORS) + lane;
     e.quarter = warp & 3; e.half = (warp - 2) >> 2; e.lane = lane;
     e.abort_flag = abort_flag; e.d_status = p.d_status;
     uint32_t ns = 0, nu = 0;

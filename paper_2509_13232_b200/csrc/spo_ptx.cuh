@@ -163,6 +163,10 @@ __device__ __forceinline__ void stage_put(uint8_t* stage, int lane, const uint4 
     *reinterpret_cast<uint4*>(stage + lane * 128 + ((c ^ (lane & 7)) << 4)) = piece[c];
   __syncwarp();
 }
+// One of the eight pieces of a lane's row; __syncwarp() before the first (earlier read-backs are done) and behind the last.
+__device__ __forceinline__ void stage_put_piece(uint8_t* stage, int lane, int c, const uint4& piece) {
+  *reinterpret_cast<uint4*>(stage + lane * 128 + ((c ^ (lane & 7)) << 4)) = piece;
+}
 // Read-back i (0..7): lanes 8j..8j+7 fetch the eight pieces of row 4i + j, so one warp-wide global
 // access covers four whole 128-byte rows.
 __device__ __forceinline__ uint4 stage_get(const uint8_t* stage, int lane, int i, int& r, int& c) {
