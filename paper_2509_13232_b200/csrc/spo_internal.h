@@ -290,15 +290,13 @@ struct LpBwdScratch {
   uint32_t* progress;
 };
 cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream_t st);
-// Both of these after the chunk's gradient; either may be left out (parts = 0, rest.rest = NULL).
+// What lies between a chunk's gradient and its dW; each part may be left out (parts = 0, rest.rest or clean = NULL).
 //   dH[t] = sum over `parts` of src[part][t] in order, plus rest W[y] (bf16 [V, d]); rows x d of type dh_dtype
 //   the targets' rows of rest H: into rest.rows and rest.slot, or added to dw (fp32 [V, d]) if that is not NULL
+//   clean[t] = H[t], or zeros where mask[t] is 0 (bf16 [rows, d])
 cudaError_t launch_lp_rest(const float* src, int parts, int64_t rows, int32_t d, int32_t V, void* dh, int32_t dh_dtype,
                            const void* W, const void* H, int64_t ldh, const TargetRest& rest, bool targets, float* dw,
-                           cudaStream_t st);
-// out[i][:] = H[t0 + i][:] (bf16, row pitch ldh), or zeros where mask[t0 + i] is 0
-cudaError_t launch_clean_rows(const void* H, int64_t ldh, const uint8_t* mask, int64_t t0, int64_t rows, int32_t d,
-                              void* out, cudaStream_t st);
+                           const uint8_t* mask, void* clean, cudaStream_t st);
 size_t lp_fwd_ws_bytes(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype);
 size_t lp_bwd_ws_bytes(int64_t T, int32_t d, int32_t V, int32_t dtype);
 cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st);

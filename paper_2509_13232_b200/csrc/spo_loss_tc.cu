@@ -1342,13 +1342,12 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream
     }
     const __nv_bfloat16* const H = reinterpret_cast<const __nv_bfloat16*>(a.H) + t0 * a.ldh;
     e = launch_lp_rest(w.split, k_splits == 1 ? 0 : k_splits, rows, a.d, a.V, dH, a.dH_dtype, a.W, H, a.ldh, rest, rounded,
-                       nullptr, st);
+                       nullptr, a.mask ? a.mask + t0 : nullptr, a.mask ? w.h_clean : nullptr, st);
     if (e != cudaSuccess) return e;
     // The gradient of a masked row is zero, but zero times a NaN in that row of H is not: with a mask the
     // dW contraction reads a copy of the chunk's rows in which the masked ones are zero.
     int64_t h_row0 = t0;
     if (a.mask) {
-      if ((e = launch_clean_rows(a.H, a.ldh, a.mask, t0, rows, a.d, w.h_clean, st)) != cudaSuccess) return e;
       h_row0 = 0;
       if (!make_map(&mH_mn, w.h_clean, a.d, rows, a.d, 64)) return cudaErrorInvalidValue;
     } else if (!make_map(&mH_mn, a.H, a.d, a.T, a.ldh, 64)) {
@@ -1359,7 +1358,8 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream
       const bool add = t0 > 0 || (a.dW_dtype == SPO_DTYPE_F32 && a.accumulate);
       e = launch_dw(mG_mn, mH_mn, h_row0, rows, a.d, a.V, sum, add ? 1 : 0, 0, tiles_v, progress, a.d_status, st);
       if (e == cudaSuccess)
-        e = launch_lp_rest(nullptr, 0, rows, a.d, a.V, nullptr, a.dH_dtype, a.W, H, a.ldh, rest, true, sum, st);
+        e = launch_lp_rest(nullptr, 0, rows, a.d, a.V, nullptr, a.dH_dtype, a.W, H, a.ldh, rest, true, sum,
+                           nullptr, nullptr, st);
     } else {
       GemmParams p{};
       p.m_tiles = tiles_v;
