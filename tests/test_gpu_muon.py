@@ -74,6 +74,47 @@ def test_orthogonalize(b, m, n, bf16):
     check(got, g, bf16)
 
 
+def iterate64(g, rounded):
+    """oracle.operators.newton_schulz and newton_schulz_rounded for a batch, in 64 bits on the GPU: the sizes at which wide tiles
+    are chosen take the CPU minutes."""
+    import torch
+    a, b, c = O.NS_COEFFICIENTS
+    x = torch.from_numpy(g).cuda().double()
+    tall = x.shape[1] > x.shape[2]
+    x = x.transpose(1, 2).contiguous() if tall else x
+    s = 2.0 ** np.round(np.log2(np.sqrt(x.shape[2])))
+    x = x / (torch.linalg.vector_norm(x, dim=(1, 2), keepdim=True) + 1e-7) * s
+    half = (lambda z: z.half().double()) if rounded else (lambda z: z)
+    for _ in range(5):
+        hi = half(x)
+        q = half(hi @ hi.transpose(1, 2) / s**2)
+        poly = b * q + c * (q @ q)
+        d = torch.diagonal(poly, dim1=1, dim2=2).unsqueeze(2).clone()
+        torch.diagonal(poly, dim1=1, dim2=2).zero_()
+        x = (a + d) * x + half(poly) @ hi
+    x = x / s
+    return x.transpose(1, 2) if tall else x
+
+
+# one for each pair of tile widths (symmetric products, update) and orientation
+@pytest.mark.parametrize("b,m,n", [(24, 130, 8200), (80, 2056, 130), (74, 130, 1040), (74, 1040, 130), (24, 260, 2056),
+                                   (74, 2600, 130), (12, 1000, 2600), (12, 2600, 1000), (1, 3026, 3762), (2, 3738, 2428),
+                                   (4, 1000, 2730)])
+def test_large_batches_and_matrices(b, m, n):
+    import torch
+    rng = np.random.default_rng(b + m)
+    k = min(b, 3)
+    g = np.concatenate([gradient(rng, k, m, n, 40) + 3e-4 * rng.standard_normal((k, m, n)).astype(np.float32)] * -(-b // k))[:b]
+    got, st = orthogonalize(g)
+    assert st == 0
+    want, rounded = iterate64(g[:k], False), iterate64(g[:k], True)
+    norm = torch.linalg.vector_norm(want, dim=(1, 2))
+    allowed = 2 * torch.linalg.vector_norm(rounded - want, dim=(1, 2)) + 2.0**-19 * norm
+    assert bool((torch.linalg.vector_norm(torch.from_numpy(got[:k]).cuda().double() - want, dim=(1, 2)) <= allowed).all())
+    for i in range(k, b):                                 # the same matrix again, on other tiles: the same bits
+        assert np.array_equal(got[i], got[i % k])
+
+
 @pytest.mark.parametrize("m,n,rank", [(256, 320, 1), (320, 256, 8), (512, 512, 40)])
 def test_low_rank_updates_keep_their_rank(m, n, rank):
     """The case in which a rounding of the iterate is amplified most: directions that are exactly zero."""
