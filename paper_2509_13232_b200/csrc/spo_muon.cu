@@ -9,14 +9,15 @@
 // for the products, whose spectrum is small where X's is; both times s = 2^round(log2 sqrt(max(m, n))), which
 // puts the entries of an orthogonal matrix near one.  Errors against 64 bits for a 512 x 512 update of rank 16
 // under no noise: this 8e-4, fp16 alone 4e-2, bf16 alone 0.33 (a full-rank Gaussian: 8e-4, 1.3e-3, 1.1e-2).  fp16
-// rather than bf16 because everything here is bounded by about 10 in magnitude and fp16 has 8 times finer steps.  A and b A + c A A are rounded
-// to fp16 once each, but for the diagonal of the latter: near convergence it is -2.7 and the rest almost nothing,
-// so it stays in fp32 and multiplies X in fp32 (19 x 183: error of the iteration 8e-4; rounded with the rest 1.7e-3).
-// All sums are fp32.
+// rather than bf16 because everything here is bounded by about 10 in magnitude and fp16 has 8 times finer steps.
+// A and b A + c A A are rounded to fp16 once each, but for the diagonal of the latter: near convergence it is -2.7 and
+// the rest almost nothing, so it stays in fp32 and multiplies X in fp32 (19 x 183: error of the iteration 8e-4; rounded
+// with the rest 1.7e-3).  All sums are fp32.
 //
-// Work.  A and A A are symmetric: only the blocks on and above the diagonal are computed and stored (a block below
-// it is read as the transposed operand of its mirror image), 3 m^2 n + m^3 operations a step for m <= n instead of
-// 4 m^2 n + 2 m^3.  Five steps of a 4096 x 4096 matrix are 1.37 TFLOP: tensor-bound from a few hundred rows on, launch-bound below.
+// Work.  A and A A are symmetric: only the blocks on and above the diagonal are computed and stored (a block below it
+// is read as the transposed operand of its mirror image), 3 m^2 n + m^3 operations a step for m <= n instead of
+// 4 m^2 n + 2 m^3.  Five steps of a 4096 x 4096 matrix are 1.37 TFLOP: tensor-bound from a few hundred rows on,
+// launch-bound below.
 #include <cuda.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
