@@ -431,6 +431,40 @@ def test_other_stream_graph_replay_and_two_calls_at_once():
         assert torch.equal(got, ref)
 
 
+@pytest.mark.parametrize("T", [37, 300])
+def test_captured_backward_with_other_targets_at_each_replay(T):
+    """What a call keeps in its scratch by target (rows, slots) is its own: replays with new targets, masks and gradients
+    give the bits of fresh calls on scratch full of ones."""
+    import torch
+    from paper_2509_13232_b200 import binding as B
+    d, V = 128, 700
+    h, w, y, rng = make(31, T, d, V)
+    H, W = torch.from_numpy(h).cuda().bfloat16(), torch.from_numpy(w).cuda().bfloat16()
+    lse = torch.from_numpy(O.logprobs(h, w, y, None, 1.0)["lse"].astype(np.float32)).cuda()
+    st = torch.zeros(4, dtype=torch.int32, device="cuda")
+    n = B.spo_workspace_bytes(B.WS_LOGPROBS_BWD, T=T, d=d, V=V)
+    ws, fresh = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(n, dtype=torch.uint8, device="cuda")
+    Y, M = torch.zeros(T, dtype=torch.int32, device="cuda"), torch.ones(T, dtype=torch.uint8, device="cuda")
+    gl = torch.ones(T, device="cuda")
+    dH, dW, dH1, dW1 = (torch.empty_like(x) for x in (H, W, H, W))
+    call = lambda a, b, s: B.spo_logprobs_bwd(H, W, Y, M, lse, None, gl, None, None, a, b, 0, s, st)  # noqa: E731
+    call(dH, dW, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(dH, dW, ws)
+    for k, targets in enumerate((V, 5, 1, V)):
+        Y.copy_(torch.from_numpy(rng.integers(0, targets, T).astype(np.int32)))
+        M.copy_(torch.from_numpy((rng.random(T) < 0.6 + 0.1 * k).astype(np.uint8)))
+        gl.copy_(torch.from_numpy(rng.standard_normal(T).astype(np.float32)))
+        dH.fill_(float("nan")), dW.fill_(float("nan"))
+        g.replay()
+        fresh.fill_(0xFF)
+        call(dH1, dW1, fresh)
+        torch.cuda.synchronize()
+        assert torch.equal(dH, dH1) and torch.equal(dW, dW1) and int(st[0]) == 0
+
+
 def test_old_log_probs_agree_with_the_loss_calls():
     """spo_logprobs feeds logp_old of the loss: with the same weights every ratio is one."""
     import torch
