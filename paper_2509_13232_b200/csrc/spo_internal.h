@@ -227,6 +227,10 @@ cudaError_t launch_scatter_rows(const void* dH_act, const int32_t* rows, int64_t
 
 // ---- log-probability operators ---------------------------------------------
 constexpr int kMaxTopK = SPO_MAX_TOP_K;
+// Logits of -inf (banned tokens) have p = 0 and add nothing to a sum, which 0 x inf and inf - inf would not say:
+constexpr float kMaxFloor = -1.0e25f;     // least running maximum (log2 units): exponentials of -inf are then 0, not NaN
+constexpr float kFarBelow = -1.0e30f;     // stands for such a logit in e z (its e is 0): far below the floor at any temperature
+constexpr float kNoChance = -1.0e4f;      // stands for its log2 p, or log p, in p log p (2^-10000 is 0)
 // bf16: up to this many token rows the vocabulary streams past them (d = 4096, V = 151936: 128 rows 240 us so, 129 rows in
 // tiles 272 us; d = 1024, V = 32000: 33 and 38 us).
 constexpr int kLpStreamRows = 128;

@@ -326,7 +326,7 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t c = c0 + i * 32 + lane;
-      x[i] = c < end ? z[c] : -1.0e30f;            // far below any logit: its exponential is zero, and zero times it too
+      x[i] = c < end ? z[c] : -CUDART_INF_F;
     }
     float mx = x[0];
 #pragma unroll
@@ -340,13 +340,13 @@ lp_rows_kernel(const float* __restrict__ Z, int64_t ldz, int nseg, int part, int
       }
       if (lane < 4 && c0 + lane * kGroup < end) gm[c0 / kGroup + lane] = mine;
     }
-    const float mn = fmaxf(fmaxf(m2, mx * sc2), -1.0e25f);   // a lane without columns: exponentials of -inf, not of rounding
+    const float mn = fmaxf(fmaxf(m2, mx * sc2), kMaxFloor);  // a lane without columns: exponentials of -inf, not of rounding
     float s = 0.0f, t = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float e = fast_exp2(fmaf(x[i], sc2, -mn));
       s += e;
-      t = fmaf(e, x[i], t);
+      t = fmaf(e, fmaxf(x[i], kFarBelow), t);
     }
     const float down = fast_exp2(m2 - mn);
     l = fmaf(l, down, s);
@@ -671,7 +671,7 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
             float x[4];
             int key[2];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = i * 32 + lane < cols ? z[i * 32 + lane] : -1.0e30f;
+            for (int i = 0; i < 4; ++i) x[i] = i * 32 + lane < cols ? z[i * 32 + lane] : -CUDART_INF_F;
             if (p.Z) {
 #pragma unroll
               for (int i = 0; i < 2; ++i) key[i] = __reduce_max_sync(0xffffffffu, max(top_key(x[2 * i]), top_key(x[2 * i + 1])));
@@ -686,13 +686,13 @@ lp_stream_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant_
               mx[e] = __int_as_float(order_key(__reduce_max_sync(0xffffffffu, order_key(__float_as_int(lm)))));
             }
             mk[e] = __shfl_sync(0xffffffffu, m2, k0 + e);
-            mn[e] = fmaxf(fmaxf(mk[e], mx[e] * p.sc2), -1.0e25f);
+            mn[e] = fmaxf(fmaxf(mk[e], mx[e] * p.sc2), kMaxFloor);
             s[e] = u[e] = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float ex = fast_exp2(fmaf(x[i], p.sc2, -mn[e]));
               s[e] += ex;
-              u[e] = fmaf(ex, x[i], u[e]);
+              u[e] = fmaf(ex, fmaxf(x[i], kFarBelow), u[e]);
             }
           }
 #pragma unroll
@@ -979,7 +979,7 @@ sgemm_kernel(const SgemmParams p) {
         float v = 0.0f;
         if (live) {
           const float u = fmaf(acc[i][j], p.grad.inv_t, -ls);
-          v = expf(u) * fmaf(b, u, a);
+          v = expf(u) * fmaf(b, fmaxf(u, kNoChance), a);
           if (n == yt) v += tgt;
         }
         *dst = v;

@@ -174,6 +174,7 @@ __device__ __forceinline__ void g_values(const uint32_t (&v)[32], int col0, floa
 
 // Gradient of a row's logits for upstream gradients of its log-prob, log-sum-exp and entropy:
 // with u = log2 p = z sc2 - lse2, g = 2^u (a + b u) + tgt 1[v = y_t] (a, b, tgt: see the row setup), packed to bf16.
+// p log p is zero where p is: kNoChance stands for u there (a logit of -inf gives 0 x inf otherwise; a NaN still comes through 2^u).
 __device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, bool live, float sc2, float lse2, float a,
                                             float b, float tgt, int yt, int cols_valid, uint4* out4, float* rest) {
   float g[32];
@@ -181,7 +182,7 @@ __device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, b
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
       const float u = fmaf(__uint_as_float(v[j]), sc2, -lse2);
-      g[j] = fast_exp2(u) * fmaf(b, u, a);
+      g[j] = fast_exp2(u) * fmaf(b, fmaxf(u, kNoChance), a);
     }
     if (yt >= col0 && yt < col0 + 32) {
       const int jj = yt - col0;
@@ -545,8 +546,9 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             uint32_t v[32];
             tmem_ld32(taddr + ch * 32, v);
             if (col0 + 32 > p.cols_valid) {                            // ragged last chunk of the vocabulary
-              // (with ENT a large finite value instead of -inf: its e is 0 either way and 0 * z stays 0)
-              const float fill = ENT ? -1.0e30f : -CUDART_INF_F;
+              // (with ENT a large finite value instead of -inf: its e is 0 either way and 0 * z stays 0.  LP takes -inf, which no
+              // logit of a banned token is below, so that the lists are right among those too)
+              const float fill = ENT && LP < 0 ? -1.0e30f : -CUDART_INF_F;
 #pragma unroll
               for (int j = 0; j < 32; ++j)
                 if (col0 + j >= p.cols_valid) v[j] = __float_as_uint(fill);
@@ -585,7 +587,8 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 }
               }
             }
-            const float mn = fmaxf(m2, fmaxf(mx0, mx1) * sc2);
+            float mn = fmaxf(m2, fmaxf(mx0, mx1) * sc2);
+            if (LP >= 0) mn = fmaxf(mn, kMaxFloor);
             const float neg = -mn;
             float s0 = 0.0f, s1 = 0.0f, t0 = 0.0f, t1 = 0.0f;
 #pragma unroll
@@ -595,8 +598,9 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
               s0 += e0;
               s1 += e1;
               if (ENT) {
-                t0 = fmaf(e0, __uint_as_float(v[j]), t0);
-                t1 = fmaf(e1, __uint_as_float(v[j + 1]), t1);
+                const float z0 = __uint_as_float(v[j]), z1 = __uint_as_float(v[j + 1]);
+                t0 = fmaf(e0, LP >= 0 ? fmaxf(z0, kFarBelow) : z0, t0);
+                t1 = fmaf(e1, LP >= 0 ? fmaxf(z1, kFarBelow) : z1, t1);
               }
             }
             const float down = fast_exp2(m2 - mn);
