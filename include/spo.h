@@ -590,7 +590,7 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
  *   W         device in/out [batch][m][n], fp32 or bf16;  momentum  device in/out [batch][m][n] fp32
  *   ws        device scratch, spo_workspace_bytes(SPO_WS_MUON, m, n, 0, 0, batch, 0) bytes
  * A matrix whose U holds a NaN or an infinity sets SPO_DEV_NONFINITE; its out is zero, its W and momentum are
- * left as they were (the other matrices of the batch are not affected).  A zero U gives X = 0.
+ * left as they were (the other matrices of the batch are not affected).  A zero U gives X = 0, whatever eps.
  * Limits: 1 <= m, n < 2^24, min(m, n) <= 65536, 0 <= batch <= 65535.
  */
 #define SPO_MUON_SCALE_NONE      0

@@ -735,7 +735,13 @@ ns_split_kernel(const NsInput p) {
     p.bad[blockIdx.y] = bad;
     if (bad && p.d_status) atomicOr(p.d_status, SPO_DEV_NONFINITE);
   }
-  const float f = bad ? 0.0f : (float)((double)p.scale / (sqrt(tot) + (double)p.eps));
+  // scale / (|U|_F + eps) may be past fp32's range (a zero matrix with a tiny eps), or so small that fp32 has few bits left:
+  // multiplied in two steps then, the second an exact power of two (1 otherwise), U f up being at most the scale.
+  double factor = bad ? 0.0 : (double)p.scale / (sqrt(tot) + (double)p.eps);
+  float up = 1.0f;
+  if (factor > 0x1p100) { factor *= 0x1p-64; up = 0x1p64f; }
+  else if (factor < 0x1p-100) { factor *= 0x1p64; up = 0x1p-64f; }
+  const float f = (float)factor;
   const int64_t cbs = (p.n + 31) >> 5, tasks = ((p.m + 31) >> 5) * cbs;
   const int lane = threadIdx.x & 31;
   const bool quads = (p.n & 3) == 0;
@@ -762,7 +768,7 @@ ns_split_kernel(const NsInput p) {
             *mp = make_float4(mn[0], mn[1], mn[2], mn[3]);
           }
 #pragma unroll
-          for (int k = 0; k < 4; ++k) u[k] *= f;
+          for (int k = 0; k < 4; ++k) u[k] = u[k] * f * up;
         }
         *reinterpret_cast<float4*>(blk + (lane & 7) * 128 + rr * 4) = make_float4(u[0], u[1], u[2], u[3]);
         if (r < p.m && c < p.n)                           // the pitch is a multiple of 8: whole pieces
@@ -782,7 +788,7 @@ ns_split_kernel(const NsInput p) {
             u = ns_momentum(p, u, p.momentum[at], &mn);
             p.momentum[at] = mn;
           }
-          u *= f;
+          u = u * f * up;
         }
         blk[(lane >> 2) * 128 + rr * 4 + (lane & 3)] = u;
         if (r < p.m && c < p.n) p.hi[xmat + r * p.ld + c] = __float2half_rn(u);
