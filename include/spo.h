@@ -591,6 +591,8 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
  *   ws        device scratch, spo_workspace_bytes(SPO_WS_MUON, m, n, 0, 0, batch, 0) bytes
  * A matrix whose U holds a NaN or an infinity sets SPO_DEV_NONFINITE; its out is zero, its W and momentum are
  * left as they were (the other matrices of the batch are not affected).  A zero U gives X = 0, whatever eps.
+ * The default coefficients keep every singular value of X below 1.3.  Others may let X grow past fp16 (65504), in which case
+ * the result, or W, holds NaN or infinities: SPO_DEV_NONFINITE is set, and nothing is taken back.
  * Limits: 1 <= m, n < 2^24, min(m, n) <= 65536, 0 <= batch <= 65535.
  */
 #define SPO_MUON_SCALE_NONE      0

@@ -409,7 +409,8 @@ __device__ __forceinline__ void ns_emit(const NsParams& p, const uint4& acc, int
 }
 
 // x = (a + diagonal) X + acc (the diagonal's entry of the row, TALL: of the column), stored as the next X (fp32 blocks
-// and fp16 rows), as the result, or applied to the weights.
+// and fp16 rows), as the result, or applied to the weights.  The last x is looked at for NaN and infinities: whatever
+// overflows on the way (coefficients under which X grows without bound) ends in one, as inf - inf or inf x 0 at the latest.
 template <bool TALL, int BN, bool LAST>
 __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& bars, const NsParams& p, int total, __half* hi_out, uint32_t& n) {
   const int lane = e.lane, rows = p.m, cols = p.n;
@@ -432,6 +433,7 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
       const int c = col_first + 32 * step + lane;
       if (TALL) next_a = c < cols ? p.a + __ldcg(diag + c) : 0.0f;
     };
+    float odd = 0.0f;                                     // LAST: NaN once an x is not finite
     if (col_first + e.half * 64 < col_end) fetch(2 * e.half);
     if (!ns_tile_ready<BN>(e, bars, n)) return false;
     const uint32_t taddr = e.tmem_base + ((uint32_t)(e.quarter * 32) << 16) + (n % NsCfg<BN>::bufs) * BN;
@@ -464,8 +466,10 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
         } else {
           uint4 piece[8];
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
+          for (int q = 0; q < 8; ++q) {
             piece[q] = make_uint4(__float_as_uint(x32[q].x), __float_as_uint(x32[q].y), __float_as_uint(x32[q].z), __float_as_uint(x32[q].w));
+            odd = fmaf(x32[q].x, 0.0f, fmaf(x32[q].y, 0.0f, fmaf(x32[q].z, 0.0f, fmaf(x32[q].w, 0.0f, odd))));
+          }
           stage_put(e.stage, lane, piece);
 #pragma unroll 1
           for (int i = 0; i < 8; ++i) {
@@ -488,6 +492,7 @@ __device__ __forceinline__ bool ns_store_update(const NsEpi& e, const NsBars& ba
         }
       }
     }
+    if (LAST && odd != odd && p.d_status) atomicOr(p.d_status, SPO_DEV_NONFINITE);
     ns_tile_done<BN>(e, bars, n);
   }
   return true;

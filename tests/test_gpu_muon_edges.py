@@ -1,4 +1,5 @@
-"""Newton-Schulz updates at the ends of the range: zero matrices and the smallest epsilons, entries near the ends of fp32."""
+"""Newton-Schulz updates at the ends of the range: zero matrices and the smallest epsilons, entries near the ends of fp32, and
+coefficients under which the iteration has no bound."""
 
 import numpy as np
 import pytest
@@ -43,3 +44,28 @@ def test_the_ends_of_the_range(m, n, size, eps):
     want, rounded = O.newton_schulz(g[0], eps=eps32), O.newton_schulz_rounded(g[0], eps=eps32)
     norm = np.linalg.norm(want)
     assert np.linalg.norm(got[0] - want) <= 2 * np.linalg.norm(rounded - want) + 2.0**-19 * norm
+
+
+@pytest.mark.parametrize("m,n", [(60, 90), (500, 300), (1, 1)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_an_iteration_without_bound_is_reported(m, n, bf16):
+    import torch
+    from paper_2509_13232_b200 import binding as B
+    g = gradient(np.random.default_rng(n), 1, m, n)
+    got, st = orthogonalize(g, out_bf16=bf16, coef_a=90.0, coef_b=50.0, coef_c=50.0, steps=12)
+    assert not np.all(np.isfinite(got)) and st == B.DEV_NONFINITE
+    W = torch.zeros(m, n, device="cuda").to(torch.bfloat16 if bf16 else torch.float32)
+    ws, k = workspace(m, n, 1)
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    p = B.default_muon_params(coef_a=90.0, coef_b=50.0, coef_c=50.0, steps=12)
+    B.spo_muon_update(W, torch.zeros(m, n, device="cuda"), torch.from_numpy(g[0]).cuda(), ws[:k], p, status)
+    torch.cuda.synchronize()
+    assert int(status[0]) == B.DEV_NONFINITE
+
+
+def test_a_large_but_finite_result_is_not_reported():
+    g = gradient(np.random.default_rng(0), 1, 60, 90)
+    got, st = orthogonalize(g, coef_a=90.0, coef_b=0.0, coef_c=0.0, steps=2)        # X = 8100 U / |U|: no other term
+    assert st == 0
+    want = 8100.0 * g[0] / (np.linalg.norm(g[0].astype(np.float64)) + float(np.float32(1e-7)))
+    np.testing.assert_allclose(got[0], want, rtol=2.0**-20)                          # six roundings to 32 bits
