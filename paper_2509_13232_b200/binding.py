@@ -449,17 +449,19 @@ def spo_logprobs(H, W, y, mask, logp, lse, entropy, top_ids, top_logp, ws, d_sta
     c = _Args()
     f32, i32 = c.torch.float32, c.torch.int32
     T, d, V, ld = c.rows(H, W)
-    K = 0 if top_ids is None else top_ids.shape[-1]
-    if K == 0:
-        top_ids = top_logp = None
-    elif top_logp is None:
-        raise ValueError("top_logp is required with top_ids")
-    row = (T,)
+    if (top_ids is None) != (top_logp is None):
+        raise ValueError("top_ids and top_logp come together")
+    K, row = 0, (T,)
+    if top_ids is not None:
+        if not isinstance(top_ids, c.torch.Tensor) or top_ids.dim() != 2:
+            raise TypeError("top_ids must be a tensor [T, K]")
+        K = top_ids.shape[1]
+    ids, ids_logp = c.may("top_ids", top_ids, i32, (T, K)), c.may("top_logp", top_logp, f32, (T, K))
     w, n = c.scratch(ws)
     rc = lib().spo_logprobs(
         H.data_ptr(), ld, W.data_ptr(), _dtype_code(W), c.may("y", y, i32, row), c.may("mask", mask, c.torch.uint8, row), T, d, V,
         inv_temperature, K, c.may("logp", logp, f32, row), c.need("lse", lse, f32, row), c.may("entropy", entropy, f32, row),
-        c.may("top_ids", top_ids, i32, (T, K)), c.may("top_logp", top_logp, f32, (T, K)), w, n, c.status(d_status), c.stream())
+        ids, ids_logp, w, n, c.status(d_status), c.stream())
     _check(rc, "spo_logprobs")
 
 
