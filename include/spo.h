@@ -535,7 +535,8 @@ int32_t spo_loss_stats(const float* logp, const float* logp_old, const uint8_t* 
  *   top_k       0 .. SPO_MAX_TOP_K, at most V
  *   logp, lse   device out [T] fp32;  entropy  device out [T] fp32, optional
  *   top_ids     device out [T][top_k] int32;  top_logp  device out [T][top_k] fp32 (NULL when top_k = 0)
- *   ws          device scratch, spo_workspace_bytes(SPO_WS_LOGPROBS, T, d, V, 0, top_k, 0) bytes
+ *   ws          device scratch, spo_workspace_bytes(SPO_WS_LOGPROBS, T, d, V, 0, top_k, 0) bytes; a buffer of the size
+ *               named for T rows serves every call of at most T rows (same d, V and top_k)
  * A target outside [0,V) gives logp = -inf and SPO_DEV_ID_OUT_OF_RANGE; a row whose lse is not finite sets
  * SPO_DEV_NONFINITE.  A logit of -inf (a banned token) has probability zero: it adds nothing to lse and entropy, and its
  * own log-prob is -inf.  Logits that are NaN or -inf are never listed; where fewer than top_k are left the
@@ -562,7 +563,7 @@ int32_t spo_logprobs(const void* H, int64_t ldH, const void* W, int32_t dtype, c
  *               tokens in fp32 and rounded once.  For the products dz is rounded to bf16, but for the target's
  *               entry, by far the largest of its row, whose rounding is put back in fp32.
  *   ws          device scratch, spo_workspace_bytes(SPO_WS_LOGPROBS_BWD, T, d, V, 0, 0, 0) bytes: a chunk of dz (a few
- *               thousand rows by V, bf16; fp32 for fp32 inputs), never all of it
+ *               thousand rows by V, bf16; fp32 for fp32 inputs), never all of it; it serves shorter calls too
  * A target outside [0,V) contributes nothing through g_logp and sets SPO_DEV_ID_OUT_OF_RANGE (unless masked).
  * A token whose logit is -inf has dz = 0 (but for a target's g_logp).
  * T = 0 zeroes dW (unless accumulating).

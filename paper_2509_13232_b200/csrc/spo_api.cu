@@ -790,8 +790,8 @@ size_t spo_workspace_bytes(int32_t which, int64_t T, int32_t d, int32_t V, int64
     }
     case SPO_WS_LOGPROBS: {             /* B = top_k; enough for either element type */
       if (T < 0 || V < 1 || d < 1 || B < 0 || B > SPO_MAX_TOP_K) return 0;
-      const size_t f32 = lp_fwd_ws_bytes(T, d, V, B, SPO_DTYPE_F32);
-      const size_t bf16 = (d % 64) == 0 ? lp_fwd_ws_bytes(T, d, V, B, SPO_DTYPE_BF16) : 0;
+      const size_t f32 = lp_fwd_ws_bound(T, d, V, B, SPO_DTYPE_F32);
+      const size_t bf16 = (d % 64) == 0 ? lp_fwd_ws_bound(T, d, V, B, SPO_DTYPE_BF16) : 0;
       return bf16 > f32 ? bf16 : f32;
     }
     case SPO_WS_LOGPROBS_BWD: {

@@ -268,9 +268,11 @@ struct LpBwd {
 };
 int lp_list_len(int top_k);               // column groups listed per row, vocabulary split and column half
 int lp_fwd_lists(int64_t rows, int32_t d, int32_t V);   // lists (and partials) per row of a launch over `rows` rows
+int lp_fwd_slots(int lists, int32_t d, int32_t V, int top_k);   // groups whose logits a list has room for: no more than there are
 cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPartial* partials, float* cand,
                                float2* cand_max, uint32_t* progress, cudaStream_t st);
 int lp_dh_splits(int64_t rows, int32_t d, int32_t V);    // parts of dH's contraction over the vocabulary
+size_t lp_dh_split_bytes(int64_t rows, int32_t d);       // their results, of a launch over up to `rows` rows
 // The target entry of a token's logit gradient is by far its largest, and what rounding it to bf16 takes off does not
 // average out over the few tokens of a vocabulary row.  So the gradient launch keeps that rest (by token of the chunk), and it
 // is added in fp32: rest W[y] to the token's dH, the sum of rest H over a target's tokens to the target's row of dW (that sum
@@ -301,7 +303,8 @@ cudaError_t launch_lp_bwd_bf16(const LpBwd& a, const LpBwdScratch& w, cudaStream
 cudaError_t launch_lp_rest(const float* src, int parts, int64_t rows, int32_t d, int32_t V, void* dh, int32_t dh_dtype,
                            const void* W, const void* H, int64_t ldh, const TargetRest& rest, bool targets, float* dw,
                            const uint8_t* mask, void* clean, cudaStream_t st);
-size_t lp_fwd_ws_bytes(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype);
+size_t lp_fwd_ws_bytes(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype);         // what a call of T rows uses
+size_t lp_fwd_ws_bound(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype);         // enough for every call of up to T rows
 size_t lp_bwd_ws_bytes(int64_t T, int32_t d, int32_t V, int32_t dtype);
 cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st);
 cudaError_t lp_backward(const LpBwd& a, char* ws, cudaStream_t st);

@@ -410,7 +410,7 @@ constexpr int kMergeThreads = 128;        // half of what the others use: many r
 template <int LIST>
 __global__ void __launch_bounds__(kMergeThreads)
 lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, const float2* __restrict__ tops, const float* __restrict__ cand,
-                int64_t rows, int64_t t0, const LpOut o) {
+                int slots, int64_t rows, int64_t t0, const LpOut o) {
   __shared__ TopSmem<kMergeThreads> sh;
   __shared__ int s_key[kMaxTopK * 32], s_id[kMaxTopK * 32];
   pdl_trigger();
@@ -434,7 +434,7 @@ lp_merge_kernel(const FwdPartial* __restrict__ partials, int lists, const float2
       if (sh.out_key[i >> 5] != kNoKey) {
         const int at = sh.out_at[i >> 5], s = at % lists, slot = (int)(__float_as_uint(entry(at).y) & 255u);
         id = sh.out_id[i >> 5] * 32 + (i & 31);
-        if (id < o.V) key = top_key(cand[(((int64_t)s * rows + row) * LIST + slot) * 32 + (i & 31)]);
+        if (id < o.V) key = top_key(cand[(((int64_t)s * rows + row) * slots + slot) * 32 + (i & 31)]);
       }
       s_key[(i & 31) * K + (i >> 5)] = key;
       s_id[(i & 31) * K + (i >> 5)] = id;
@@ -1198,6 +1198,20 @@ void row_segments(int64_t rows, int32_t V, int* nseg, int* part) {
 enum : int { LP_STREAM = 0, LP_TILES = 1, LP_F32 = 2 };
 struct LpFwdWs { size_t z, partials, tops, cand, progress, total; int64_t chunk, ldz; int path; };
 
+struct LpLists { size_t rl, rs; };        // rows x lists, rows x lists x slots of one launch of the tiled path
+LpLists lp_lists(int64_t rows, int32_t d, int32_t V, int top_k) {
+  const int lists = lp_fwd_lists(rows, d, V);
+  return {(size_t)rows * lists, (size_t)rows * lists * lp_fwd_slots(lists, d, V, top_k)};
+}
+void lp_lists_layout(LpFwdWs& L, size_t rl, size_t rs, int top_k) {
+  size_t off = 0;
+  L.progress = off; off = align_up(off + kProgressBytes, 256);
+  L.partials = off; off = align_up(off + sizeof(FwdPartial) * rl, 256);
+  L.tops = off;     off = align_up(off + sizeof(float2) * rl * lp_list_len(top_k), 256);
+  L.cand = off;     off = align_up(off + (size_t)128 * rs, 256);
+  L.total = off;
+}
+
 LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype) {
   LpFwdWs L{};
   L.path = dtype == SPO_DTYPE_F32 ? LP_F32 : T <= kLpStreamRows ? LP_STREAM : LP_TILES;
@@ -1225,17 +1239,15 @@ LpFwdWs lp_fwd_layout(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype)
   } else {
     const int64_t n = ceil_div(T, kLpChunkRows);
     L.chunk = ceil_div(ceil_div(T, n), 256) * 256;               // chunks of like size
-    size_t rl = 0;                                               // rows x lists, the largest of a full and of the last chunk
+    size_t rl = 0, rs = 0;                                       // rows x lists, and x slots: the largest of a full and of the last chunk
     const int64_t first = T < L.chunk ? T : L.chunk, last = T - (ceil_div(T, L.chunk) - 1) * L.chunk;
     for (int64_t rows : {first, last}) {
-      const size_t x = (size_t)rows * lp_fwd_lists(rows, d, V);
-      if (x > rl) rl = x;
+      const LpLists x = lp_lists(rows, d, V, top_k);
+      if (x.rl > rl) rl = x.rl;
+      if (x.rs > rs) rs = x.rs;
     }
-    const int len = lp_list_len(top_k);
-    L.progress = off; off = align_up(off + kProgressBytes, 256);
-    L.partials = off; off = align_up(off + sizeof(FwdPartial) * rl, 256);
-    L.tops = off;     off = align_up(off + sizeof(float2) * rl * len, 256);
-    L.cand = off;     off = align_up(off + (size_t)128 * rl * len, 256);
+    lp_lists_layout(L, rl, rs, top_k);
+    return L;
   }
   L.total = off;
   return L;
@@ -1260,16 +1272,8 @@ LpBwdWs lp_bwd_layout(int64_t T, int32_t d, int32_t V, int32_t dtype) {
     L.progress = off; off = align_up(off + kProgressBytes, 256);
     L.partial = off;
     if (T > L.chunk) off = align_up(off + (size_t)V * d * 4, 256);
-    L.split = off;                                               // parts of dH, of a full chunk or of the last one
-    size_t parts = 0;
-    const int64_t t_eff = T > 0 ? T : 1, first = t_eff < L.chunk ? t_eff : L.chunk,
-                  last = t_eff - (ceil_div(t_eff, L.chunk) - 1) * L.chunk;
-    for (int64_t rows : {first, last}) {
-      const int s = lp_dh_splits(rows, d, V);
-      const size_t x = s > 1 ? (size_t)s * rows * d * 4 : 0;
-      if (x > parts) parts = x;
-    }
-    off = align_up(off + parts, 256);
+    const int64_t t_eff = T > 0 ? T : 1, first = t_eff < L.chunk ? t_eff : L.chunk;
+    L.split = off; off = align_up(off + lp_dh_split_bytes(first, d), 256);
     L.rest = off;      off = align_up(off + (size_t)first * 4, 256);
     L.slot = off;      off = align_up(off + (size_t)V * 4, 256);
     L.rest_rows = off; off = align_up(off + (size_t)first * d * 2, 256);
@@ -1290,6 +1294,22 @@ LpOut out_of(const LpFwd& a) {
 
 size_t lp_fwd_ws_bytes(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype) {
   return lp_fwd_layout(T, d, V, top_k, dtype).total;
+}
+// The tiled path's lists are not monotone in the rows (d = 4096, V = 151936, K = 20: 3840 rows take 693 MB, 8192 take 403: the
+// fewer the row tiles, the finer the vocabulary is split), so the bound takes every number of row tiles that a launch can have.
+size_t lp_fwd_ws_bound(int64_t T, int32_t d, int32_t V, int top_k, int32_t dtype) {
+  if (dtype == SPO_DTYPE_F32 || T <= kLpStreamRows) return lp_fwd_layout(T, d, V, top_k, dtype).total;   // these grow with the rows
+  size_t rl = 0, rs = 0;
+  for (int64_t rows = 256; rows < kLpChunkRows + 256; rows += 256) {
+    const LpLists x = lp_lists(rows < T ? rows : T, d, V, top_k);    // (full row tiles: the splits depend on their number alone)
+    if (x.rl > rl) rl = x.rl;
+    if (x.rs > rs) rs = x.rs;
+    if (rows >= T) break;
+  }
+  LpFwdWs L{};
+  lp_lists_layout(L, rl, rs, top_k);
+  const size_t few = lp_fwd_layout(kLpStreamRows, d, V, top_k, dtype).total;
+  return L.total > few ? L.total : few;
 }
 size_t lp_bwd_ws_bytes(int64_t T, int32_t d, int32_t V, int32_t dtype) { return lp_bwd_layout(T, d, V, dtype).total; }
 
@@ -1342,7 +1362,7 @@ cudaError_t lp_forward(const LpFwd& a, char* ws, cudaStream_t st) {
         e = launch_dependent(lp_join_kernel, dim3((unsigned)ceil_div(rows, 4)), dim3(128), st, partials, lists, rows, t0, o);
       else if (e == cudaSuccess)
         e = launch_dependent(lp_list_len(a.top_k) == 8 ? lp_merge_kernel<8> : lp_merge_kernel<kMaxTopK>, dim3((unsigned)rows),
-                             dim3(kMergeThreads), st, partials, lists, tops, cand, rows, t0, o);
+                             dim3(kMergeThreads), st, partials, lists, tops, cand, lp_fwd_slots(lists, a.d, a.V, a.top_k), rows, t0, o);
       if (e != cudaSuccess) return e;
       continue;
     }

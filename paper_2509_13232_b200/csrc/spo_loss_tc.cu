@@ -130,10 +130,10 @@ struct GemmParams {
   int window;
   // Log-probability operators (template argument LP >= 0)
   float sc2;                                 // FWD / G: log2(e) / temperature
-  float* cand;                               // FWD: logits of the listed column groups, [list][cand_ld][top_k][32]
-  float2* cand_max;                          // FWD: (group maximum, group and slot) of the listed groups, [list][cand_ld][top_k]
+  float* cand;                               // FWD: logits of the listed column groups, [list][cand_ld][cand_slots][32]
+  float2* cand_max;                          // FWD: (group maximum, group and slot) of the listed groups, [list][cand_ld][LP]
   int64_t cand_ld;                           // rows between two lists
-  int top_k;
+  int cand_slots;                            // places of a list: LP, or as many groups as its columns have
   const uint8_t* mask;                       // G: rows with mask 0 get g = 0
   const float *ent, *g_logp, *g_lse, *g_ent; // G: entropy and upstream gradients per row (g_lse, g_ent + ent optional)
   float inv_t;                               // G: 1 / temperature
@@ -457,7 +457,10 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       uint32_t top_p[LIST];                                                // ... and (group << 8 | slot)
       if (MODE == MODE_FWD && LP > 0) {
 #pragma unroll
-        for (int i = 0; i < LIST; ++i) { top_v[i] = -CUDART_INF_F; top_p[i] = 0xFFFFFF00u | (uint32_t)i; }
+        for (int i = 0; i < LIST; ++i) {                                 // (slots are taken from the end: 0, 1, ..)
+          top_v[i] = -CUDART_INF_F;
+          top_p[i] = 0xFFFFFF00u | (uint32_t)(LIST - 1 - i);
+        }
       }
       const float sc2 = (MODE == MODE_FWD && LP >= 0) ? p.sc2 : kLog2e;
       bool live = false;                                                   // G with LP: coefficients of g
@@ -579,7 +582,7 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
                 }
                 if (enters) {
                   float4* dst = reinterpret_cast<float4*>(
-                      p.cand + (((int64_t)((u % p.nsplit) * 2 + half) * p.cand_ld + (grow - p.part_row0)) * LIST + slot) * 32);
+                      p.cand + (((int64_t)((u % p.nsplit) * 2 + half) * p.cand_ld + (grow - p.part_row0)) * p.cand_slots + slot) * 32);
 #pragma unroll
                   for (int q = 0; q < 8; ++q)
                     dst[q] = make_float4(__uint_as_float(v[4 * q]), __uint_as_float(v[4 * q + 1]),
@@ -1206,6 +1209,11 @@ static bool lp_narrow(int64_t k) { return k <= SPO_TUNE_LP_NARROW; }
 static int lp_tile_cols(int64_t k) { return lp_narrow(k) ? HALF_N : BN; }
 
 int lp_fwd_lists(int64_t rows, int32_t d, int32_t V) { return 2 * lp_split(rows, d, V, lp_tile_cols(d)); }
+int lp_fwd_slots(int lists, int32_t d, int32_t V, int top_k) {
+  const int bn = lp_tile_cols(d), len = lp_list_len(top_k);
+  const int64_t groups = ceil_div(ceil_div(V, bn), lists / 2) * (bn / 2 / 32);    // of a split's column half
+  return len < groups ? len : (int)groups;
+}
 
 // With one or two row tiles the pairs share nothing but those rows, which stay in L2: no pacing, and no launch that
 // zeroes its counters (2 us of some 25).
@@ -1246,6 +1254,7 @@ cudaError_t launch_lp_fwd_bf16(const LpFwd& a, int64_t t0, int64_t rows, FwdPart
   p.cand = cand;
   p.cand_max = cand_max;
   p.cand_ld = rows;
+  p.cand_slots = lp_fwd_slots(2 * p.nsplit, a.d, a.V, a.top_k);
   const int list = lp_list_len(a.top_k);
   const bool ent = a.entropy != nullptr;
   if (!lp_paced(rows)) progress = nullptr;
@@ -1268,6 +1277,15 @@ int lp_dh_splits(int64_t rows, int32_t d, int32_t V) {
     if (t < best_t) { best_t = t; best = s; }
   }
   return best;
+}
+
+// Room for those parts, for a launch over any number of rows up to `rows`: s parts take at most the pairs, s x row tiles x
+// column tiles <= pairs, so neither more than pairs / column tiles of them nor more than a tile for each pair.
+size_t lp_dh_split_bytes(int64_t rows, int32_t d) {
+  const int64_t cols = ceil_div(d, BN), most = group_count() / cols;
+  if (most < 2) return 0;
+  const int64_t by_rows = most * rows * d, by_tiles = group_count() * (int64_t)GROUP_M * BN;
+  return (size_t)(by_rows < by_tiles ? by_rows : by_tiles) * 4;
 }
 
 // bf16 backward for general upstream gradients, chunk by chunk as launch_bwd_bf16: the chunk's logit
