@@ -186,7 +186,6 @@ __device__ __forceinline__ void g_values_lp(const uint32_t (&v)[32], int col0, b
     }
     if (yt >= col0 && yt < col0 + 32) {
       const int jj = yt - col0;
-#pragma unroll
       float t = 0.0f;
 #pragma unroll
       for (int j = 0; j < 32; ++j) if (j == jj) { g[j] += tgt; t = g[j]; }
@@ -505,12 +504,13 @@ spo_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
       }
       const bool any_owed = OWED && __any_sync(0xffffffffu, owed != 0.0f);
       auto fetch_owed = [&](int col0) {
-        if (!OWED) return;
+        if constexpr (OWED) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const bool on = owed != 0.0f && col0 < p.cols_valid;
-          owed0[q] = on ? __ldg(owed_row + col0 / 8 + q) : make_uint4(0u, 0u, 0u, 0u);
-          owed1[q] = on && col0 + 32 < p.cols_valid ? __ldg(owed_row + col0 / 8 + 4 + q) : make_uint4(0u, 0u, 0u, 0u);
+          for (int q = 0; q < 4; ++q) {
+            const bool on = owed != 0.0f && col0 < p.cols_valid;
+            owed0[q] = on ? __ldg(owed_row + col0 / 8 + q) : make_uint4(0u, 0u, 0u, 0u);
+            owed1[q] = on && col0 + 32 < p.cols_valid ? __ldg(owed_row + col0 / 8 + 4 + q) : make_uint4(0u, 0u, 0u, 0u);
+          }
         }
       };
       float rs = 1.0f;                                                     // DH: factor of this lane's output row
