@@ -595,6 +595,10 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
  * The default coefficients keep every singular value of X below 1.3.  Others may let X grow past fp16 (65504), in which case
  * the result, or W, holds NaN or infinities: SPO_DEV_NONFINITE is set, and nothing is taken back.
  * Limits: 1 <= m, n < 2^24, min(m, n) <= 65536, 0 <= batch <= 65535.
+ * The scratch is what takes memory: 8 bytes an element of the batch, and 6 for each element of a min(m, n) square (5.1 GB
+ * for a vocabulary matrix of 151936 x 4096, beside W, momentum and G).
+ * More than one tile of work is one cooperative launch of clusters, which Nsight Compute (2025.2) does not replay: a program
+ * profiled with it does not get past such a call, so leave the call out of what is profiled.
  */
 #define SPO_MUON_SCALE_NONE      0
 #define SPO_MUON_SCALE_SPECTRAL  1

@@ -908,7 +908,7 @@ cudaError_t launch_iterate_t(const NsMaps& maps, NsParams p, cudaStream_t st) {
   attr[1].id = cudaLaunchAttributeCooperative;               // all CTAs resident, or the launch fails
   attr[1].val.cooperative = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 2;
+  cfg.numAttrs = most > 1 ? 2 : 1;                           // (the CTAs of a single pair, a cluster, always are)
   return cudaLaunchKernelEx(&cfg, ns_iterate_kernel<TALL, BS, BU>, maps, p);
 }
 
