@@ -564,6 +564,7 @@ int32_t spo_logprobs(const void* H, int64_t ldH, const void* W, int32_t dtype, c
  *               entry, by far the largest of its row, whose rounding is put back in fp32.
  *   ws          device scratch, spo_workspace_bytes(SPO_WS_LOGPROBS_BWD, T, d, V, 0, 0, 0) bytes: a chunk of dz (a few
  *               thousand rows by V, bf16; fp32 for fp32 inputs), never all of it; it serves shorter calls too
+ * dH and dW share no memory with H, W or each other (SPO_ERR_INVALID_ARG).
  * A target outside [0,V) contributes nothing through g_logp and sets SPO_DEV_ID_OUT_OF_RANGE (unless masked).
  * A token whose logit is -inf has dz = 0 (but for a target's g_logp).
  * T = 0 zeroes dW (unless accumulating).

@@ -656,6 +656,12 @@ int32_t spo_logprobs(const void* H, int64_t ldH, const void* W, int32_t dtype, c
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);
 }
 
+// Whether two ranges of bytes share any.
+static bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+
 int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtype, const int32_t* y, const uint8_t* mask,
                          const float* lse, const float* entropy, const float* g_logp, const float* g_lse,
                          const float* g_entropy, int64_t T, int32_t d, int32_t V, float inv_temperature, void* dH,
@@ -671,6 +677,12 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
   if (!aligned16(H) || !aligned16(W) || !aligned16(y) || !aligned16(lse) || !aligned16(entropy) || !aligned16(g_logp) ||
       !aligned16(g_lse) || !aligned16(g_entropy) || !aligned16(dH) || !aligned16(dW) || !aligned16(ws))
     return SPO_ERR_BAD_ALIGNMENT;
+  if (T > 0) {                        // H and W are read again after the first rows of dH and dW have been written
+    const int64_t in = dtype == SPO_DTYPE_BF16 ? 2 : 4, h = ((T - 1) * ldH + d) * in, w = (int64_t)V * d * in;
+    const int64_t dh = T * d * (dH_dtype == SPO_DTYPE_BF16 ? 2 : 4), dw = (int64_t)V * d * (dW_dtype == SPO_DTYPE_BF16 ? 2 : 4);
+    if (overlap(dH, dh, H, h) || overlap(dH, dh, W, w) || overlap(dW, dw, H, h) || overlap(dW, dw, W, w) || overlap(dH, dh, dW, dw))
+      return SPO_ERR_INVALID_ARG;
+  }
   if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
   if (T > 0 && ws_bytes < lp_bwd_ws_bytes(T, d, V, dtype)) return SPO_ERR_WORKSPACE_TOO_SMALL;
   LpBwd a{};
