@@ -86,9 +86,9 @@ def muon_update(w, momentum, g, lr, mu, weight_decay=0.0, nesterov=True, mode=0,
 
 
 def newton_schulz_rounded(g, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7):
-    """The same iteration with fp16 roundings where the library documents them (iterate at 22 bits or more, its fp16 part the operand, scaled
-    by a power of two, the Gram matrix and the polynomial once each, the latter's diagonal not at all), everything else in 64 bits: what those roundings
-    alone do to a given input, which is what a tolerance has to allow for."""
+    """The same iteration with fp16 roundings where the library documents them (the iterate where it is an operand, scaled by a
+    power of two, but not in the term a X; the Gram matrix and the polynomial once each, the latter's diagonal not at all), everything
+    else in 64 bits: what those roundings alone do to a given input, which is what a tolerance has to allow for."""
     a, b, c = coefficients
     x = np.asarray(g, np.float64)
     tall = x.shape[0] > x.shape[1]
@@ -99,9 +99,8 @@ def newton_schulz_rounded(g, steps=5, coefficients=NS_COEFFICIENTS, eps=1e-7):
     x = x / (np.linalg.norm(x) + eps) * s
     for _ in range(steps):
         hi = half(x)
-        pair = hi + half(x - hi)
         q = half(hi @ hi.T / s**2)
         poly = b * q + c * (q @ q)
         diagonal = np.diag(poly)
-        x = (a + diagonal)[:, None] * pair + half(poly - np.diag(diagonal)) @ hi
+        x = (a + diagonal)[:, None] * x + half(poly - np.diag(diagonal)) @ hi
     return (x.T if tall else x) / s
