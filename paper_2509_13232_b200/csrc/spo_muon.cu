@@ -917,19 +917,27 @@ cudaError_t launch_iterate(const NsMaps& maps, const NsParams& p, cudaStream_t s
   return p.tall ? launch_iterate_t<true, BS, BU>(maps, p, st) : launch_iterate_t<false, BS, BU>(maps, p, st);
 }
 
-// Column widths of the tiles, by the time their products take: rounds of tiles over the pairs x k-blocks x the
-// nanoseconds of a k-block (610 / 380 / 240 for 512 / 256 / 128 columns, measured; 1.0 / 1.25 / 1.6 times the clocks of
-// its products, the narrow ones waiting for L2), and the exposed epilogues: one a round for 512, the last one for the others.
-// 128 for the symmetric products pays where 256 leaves pairs idle: 512 x 2048 174 us (256: 190), 1000 x 2730 273 (290).
+// Column widths of the tiles.  128 instead of 256 where that takes no more rounds over the pairs: more pairs have work and an
+// epilogue is shorter (us; symmetric products 128 against 256 columns, update 256: 512 x 2048 179 / 193, 1000 x 2730 240 / 254, 2048 x 2048
+// 291 / 298; update 128 against 256, symmetric 128: 128 x 512 104 / 116, 512 x 2048 169 / 179, 3 x 4000 x 300 248 / 271).  With one
+// round more they lose by what their operands cost in traffic (symmetric: 16 x 1024 x 1024 718 / 593, 4 x 1000 x 2730 514 / 436,
+// 80 x 2056 x 130 863 / 803; update: 1000 x 2730 265 / 240, 2 x 1500 x 1500 298 / 271, 2048 x 2048 334 / 291).
+int64_t rounds_of(int64_t tiles) { return ceil_div(tiles, sm_count() / 2); }
+bool narrow_symmetric(const NsParams& p) {
+  return rounds_of(sym_tile_count(p.mm, 128) * p.batch) <= rounds_of(sym_tile_count(p.mm, 256) * p.batch);
+}
+bool narrow_update(const NsParams& p) {
+  const int64_t rows = ceil_div(p.m, 256) * p.batch;
+  return rounds_of(rows * ceil_div(p.n, 128)) <= rounds_of(rows * ceil_div(p.n, 256));
+}
+// 512 or 256 for the other symmetric products: rounds of tiles x k-blocks x the nanoseconds of a k-block (610 and 380: 1.0 and
+// 1.25 times the clocks of its products, the narrower one waiting for L2) and the exposed epilogues, one a round for 512, the
+// last one for 256.  An ordering, not a time: barriers, fills and fences are left out.  512 against 256: 4096 x 4096 1217 and
+// 1352 us, 12 x 1000 x 2600 905 / 993; 4 x 1000 x 2730 529 / 436, 16 x 1024 x 1024 688 / 593, 2048 x 8192 930 / 715.
 double sym_time(const NsParams& p, int bn) {
   const double pairs = sm_count() / 2, rounds = ceil((double)sym_tile_count(p.mm, bn) * p.batch / pairs);
   const double kb = p.kb_long + p.kb_short;
-  return bn == 512 ? rounds * (kb * 610.0 + 2 * 9000.0) : bn == 256 ? rounds * kb * 380.0 + 2 * 5000.0 : rounds * kb * 240.0 + 2 * 4000.0;
-}
-double update_time(const NsParams& p, int bn) {
-  const double pairs = sm_count() / 2;
-  const double rounds = ceil((double)ceil_div(p.m, 256) * (double)ceil_div(p.n, bn) * p.batch / pairs);
-  return rounds * p.kb_short * (bn == 256 ? 380.0 : 240.0) + (bn == 256 ? 7000.0 : 4000.0);
+  return bn == 512 ? rounds * (kb * 610.0 + 2 * 9000.0) : rounds * kb * 380.0 + 2 * 5000.0;
 }
 
 }  // namespace
@@ -998,11 +1006,13 @@ cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st) {
       !make_map3(&maps.poly128, p.poly, L.mm, L.mm, a.batch, L.gld, 128) ||
       !make_map3(&maps.poly64, p.poly, L.mm, L.mm, a.batch, L.gld, 64))
     return cudaErrorInvalidValue;
-  const double t512 = sym_time(p, 512), t256 = sym_time(p, 256), t128 = sym_time(p, 128);
-  const bool narrow = update_time(p, 128) < update_time(p, 256);
-  if (t512 < t256 && t512 < t128) return narrow ? launch_iterate<512, 128>(maps, p, st) : launch_iterate<512, 256>(maps, p, st);
-  if (t128 < t256) return narrow ? launch_iterate<128, 128>(maps, p, st) : launch_iterate<128, 256>(maps, p, st);
-  return narrow ? launch_iterate<256, 128>(maps, p, st) : launch_iterate<256, 256>(maps, p, st);
+  // (Where the update is narrow and the symmetric products are not, these are one round of 256 columns, and 512 never less: the
+  // update has as many tiles at least, and for two rounds of 256 to hold the 128-column ones too there have to be few of them.)
+  const bool narrow = narrow_update(p);
+  if (narrow_symmetric(p)) return narrow ? launch_iterate<128, 128>(maps, p, st) : launch_iterate<128, 256>(maps, p, st);
+  if (narrow) return launch_iterate<256, 128>(maps, p, st);
+  if (sym_time(p, 512) < sym_time(p, 256)) return launch_iterate<512, 256>(maps, p, st);
+  return launch_iterate<256, 256>(maps, p, st);
 }
 
 }  // namespace spo
