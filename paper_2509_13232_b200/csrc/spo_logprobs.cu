@@ -1044,8 +1044,10 @@ cudaError_t launch_sgemm(SgemmParams p, bool first, float* split_ws, SplitSum* s
 
 // What follows the logit gradient of a chunk in bf16 (see TargetRest).  The first `sum_blocks` blocks add the parts of dH and
 // the tokens' rests; each of the others has a token, and if no earlier token has its target, sums rest H over all that do,
-// in their order.  Finding them is a scan of the chunk's targets by every block: 19,000 tokens take 9 rounds of 2048, and
-// nothing has to be sorted or counted first.  The last `clean_blocks` blocks copy H with zeros in the masked rows: their
+// in their order.  Finding them is a scan of the chunk's targets by every block: 9472 tokens, the most there are, take 5 rounds of
+// 2048, and nothing has to be sorted or counted first.  A target's tokens follow one another in its block, so common targets cost: with
+// uniform ones, Zipf's and one for all the backward takes 86, 92 and 190 us for 203 rows (d = 1024, V = 32000), 25.9, 27.1 and 34.0 ms
+// for 9472 (d = 4096, V = 151936).  The last `clean_blocks` blocks copy H with zeros in the masked rows: their
 // gradient is zero, but zero times a NaN is not.  203 rows, d = 1024: 8.5 us, 13 as two launches.
 struct RestParams {
   const float4* src;
