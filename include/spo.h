@@ -584,8 +584,9 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
  *   M <- momentum M + G;  U = G + momentum M (nesterov) or M;
  *   W <- (1 - lr weight_decay) W - lr scale X,  scale = 1 (SPO_MUON_SCALE_NONE), sqrt(max(1, m/n))
  *   (SPO_MUON_SCALE_SPECTRAL) or 0.2 sqrt(max(m, n)) (SPO_MUON_SCALE_RMS).
- * Iterates are kept in fp32; the products' operands are fp16 with fp32 sums; the Frobenius norm is summed in
- * fp64 in a fixed order, so results repeat bit for bit.
+ * Iterates are kept in fp32; the products' operands are fp16 with fp32 sums, whatever the types of G, W and out: a result is off by
+ * about 1e-3 of its norm (matrices of two or three rows: up to 4e-3).  The Frobenius norm is summed in fp64 in a fixed order, so
+ * results repeat bit for bit.
  *
  *   G         device in  [batch][m][n], fp32 or bf16 (dtype)
  *   out       device out [batch][m][n], fp32 or bf16; may be G itself when the types agree

@@ -656,10 +656,11 @@ int32_t spo_logprobs(const void* H, int64_t ldH, const void* W, int32_t dtype, c
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);
 }
 
-// Whether two ranges of bytes share any.
-static bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+// Whether two ranges of bytes share any (in 128 bits: no pitch that a caller may name makes the sums wrap).
+typedef unsigned __int128 wide_t;
+static bool overlap(const void* a, wide_t a_bytes, const void* b, wide_t b_bytes) {
+  const wide_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + b_bytes && y < x + a_bytes;
 }
 
 int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtype, const int32_t* y, const uint8_t* mask,
@@ -678,8 +679,8 @@ int32_t spo_logprobs_bwd(const void* H, int64_t ldH, const void* W, int32_t dtyp
       !aligned16(g_lse) || !aligned16(g_entropy) || !aligned16(dH) || !aligned16(dW) || !aligned16(ws))
     return SPO_ERR_BAD_ALIGNMENT;
   if (T > 0) {                        // H and W are read again after the first rows of dH and dW have been written
-    const int64_t in = dtype == SPO_DTYPE_BF16 ? 2 : 4, h = ((T - 1) * ldH + d) * in, w = (int64_t)V * d * in;
-    const int64_t dh = T * d * (dH_dtype == SPO_DTYPE_BF16 ? 2 : 4), dw = (int64_t)V * d * (dW_dtype == SPO_DTYPE_BF16 ? 2 : 4);
+    const wide_t in = dtype == SPO_DTYPE_BF16 ? 2 : 4, h = ((wide_t)(T - 1) * ldH + d) * in, w = (wide_t)V * d * in;
+    const wide_t dh = (wide_t)T * d * (dH_dtype == SPO_DTYPE_BF16 ? 2 : 4), dw = (wide_t)V * d * (dW_dtype == SPO_DTYPE_BF16 ? 2 : 4);
     if (overlap(dH, dh, H, h) || overlap(dH, dh, W, w) || overlap(dW, dw, H, h) || overlap(dW, dw, W, w) || overlap(dH, dh, dW, dw))
       return SPO_ERR_INVALID_ARG;
   }

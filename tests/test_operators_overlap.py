@@ -26,7 +26,8 @@ def call(lib, h=H, w=W, dh=DH, dw=DW, dht=1, dwt=1, ld=D, rows=T):
 
 @pytest.mark.parametrize("bad", [
     dict(dh=H), dict(dh=H + 0x3F0), dict(dh=H - 0x3F0), dict(dh=W), dict(dh=W + 0x31F0), dict(dw=W), dict(dw=W - 0x31F0), dict(dw=H),
-    dict(dh=DW), dict(dw=DH + 0x3F0), dict(dh=H - 0x7F0, dht=0), dict(dw=W - 0x63F0, dwt=0), dict(dh=H + 0xB00, ld=256)])
+    dict(dh=DW), dict(dw=DH + 0x3F0), dict(dh=H - 0x7F0, dht=0), dict(dw=W - 0x63F0, dwt=0), dict(dh=H + 0xB00, ld=256),
+    dict(dh=H + (1 << 50), ld=1 << 62)])
 def test_shared_memory_is_refused(lib, bad):
     assert call(lib, **bad) == B.ERR_INVALID_ARG
 
