@@ -82,6 +82,8 @@ extern "C" {
 #define SPO_WS_LOGPROBS       9
 #define SPO_WS_LOGPROBS_BWD  10
 #define SPO_WS_MUON          11   /* T = rows m, d = columns n, B = matrices */
+#define SPO_WS_LAYERNORM_BWD 12
+#define SPO_WS_GRAD_NORM     13
 
 /*
  * Hyper-parameters.  Defaults (spo_default_params) are the values the paper prints:
@@ -622,6 +624,140 @@ int32_t spo_orthogonalize(const void* G, int32_t G_dtype, int32_t batch, int64_t
 int32_t spo_muon_update(void* W, int32_t W_dtype, float* momentum, const void* G, int32_t G_dtype,
                         int32_t batch, int64_t m, int64_t n, void* ws, size_t ws_bytes,
                         const spo_muon_params* params, int32_t* d_status, void* stream);
+
+/*
+ * Layer norm and RMS norm of hidden states, the step that makes the H of the loss and log-probability calls (and, with dH, takes their
+ * gradient back to the residual stream).  Per row t:
+ *   h = x, or x + residual rounded to the type of x;   mu = mean_j h (SPO_NORM_LAYER) or 0 (SPO_NORM_RMS);
+ *   rstd = 1 / sqrt( mean_j (h_j - mu)^2 + eps );      y_j = (h_j - mu) rstd weight_j + bias_j.
+ * Statistics in fp32, the squares about the mean; y is rounded once.
+ *
+ *   x         device in  [T] rows of d elements, fp32 or bf16 (dtype), row pitch ldx >= d elements: the last-token rows of a padded
+ *             batch need no copy
+ *   residual  device in  [T][d], type of x, optional;   h  device out [T][d], type of x: required with residual and only then.
+ *             h may be x (ldx = d) or residual
+ *   weight, bias   device in [d], fp32 or bf16 (w_dtype), each optional (NULL: 1 and 0)
+ *   mask      device in  [T] uint8, optional: rows with mask 0 give y = h = mean = rstd = 0, whatever they hold (NaN included), and set
+ *             no status bit
+ *   eps       > 0
+ *   y         device out [T][d], fp32 or bf16 (y_dtype); may be x (ldx = d) where the types agree and there is no residual
+ *   mean      device out [T] fp32, optional, SPO_NORM_LAYER only;   rstd  device out [T] fp32, optional
+ * A row whose mean square is not finite sets SPO_DEV_NONFINITE; its y is what the formula gives.
+ * Any d up to SPO_NORM_MAX_D: rows that begin on 16 bytes (d and ldx multiples of 8 in bf16, of 4 in fp32) are read fastest.  T = 0 is
+ * allowed and launches nothing.
+ */
+#define SPO_NORM_LAYER  0
+#define SPO_NORM_RMS    1
+#define SPO_NORM_MAX_D  1048576
+int32_t spo_layernorm_fwd(const void* x, int64_t ldx, const void* residual, int32_t dtype, const void* weight, const void* bias,
+                          int32_t w_dtype, const uint8_t* mask, int64_t T, int32_t d, float eps, int32_t kind,
+                          void* y, int32_t y_dtype, void* h, float* mean, float* rstd, int32_t* d_status, void* stream);
+
+/*
+ * Gradients of spo_layernorm_fwd.  With xh = (h - mu) rstd and a_j = weight_j dy_j:
+ *   dx = rstd ( a - mean_j a [SPO_NORM_LAYER] - xh mean_j(a xh) ) + dh,    dweight (+)= sum_t dy xh,    dbias (+)= sum_t dy.
+ * dx is the gradient of h, so of x and of residual alike; dh is what reaches h past the norm (the residual stream).
+ *
+ *   dy        device in  [T][d], fp32 or bf16 (dy_dtype)
+ *   x         device in  the rows that were normalised (x of the forward call, or its h), row pitch ldx, dtype
+ *   mean, rstd   device in [T] fp32, the forward's (mean: SPO_NORM_LAYER only)
+ *   dh        device in  [T][d], type of x, optional
+ *   mask      rows with mask 0 give dx = 0 and add nothing to dweight and dbias, whatever they hold
+ *   dx        device out [T][d], type of x; may be dy (where the types agree), dh or x (ldx = d)
+ *   dweight, dbias   device out [d], fp32 or bf16 (dw_dtype), each optional; overwritten, or added to when dw_accumulate != 0.  Summed
+ *             over all rows in fp32, in an order that depends on T, d and the device alone: results repeat bit for bit
+ *   ws        device scratch, spo_workspace_bytes(SPO_WS_LAYERNORM_BWD, T, d, 0, 0, 0, 0) bytes; it serves shorter calls too.  Optional
+ *             where neither dweight nor dbias is wanted
+ * T = 0 zeroes dweight and dbias (unless accumulating).
+ */
+int32_t spo_layernorm_bwd(const void* dy, int32_t dy_dtype, const void* x, int64_t ldx, int32_t dtype, const void* weight,
+                          int32_t w_dtype, const uint8_t* mask, const float* mean, const float* rstd, const void* dh,
+                          int64_t T, int32_t d, int32_t kind, void* dx, void* dweight, void* dbias, int32_t dw_dtype,
+                          int32_t dw_accumulate, void* ws, size_t ws_bytes, int32_t* d_status, void* stream);
+
+/*
+ * Global norm of many gradients and the factor that clips them (Algorithm 1, "update the policy parameters"; the paper leaves the
+ * optimiser open): with s = grad_scale (1 / loss scale; 1),
+ *   norm = |s| sqrt( sum over all tensors and elements of g^2 ),   factor = s min(1, max_norm / norm)    (max_norm <= 0: factor = s).
+ * Sums in fp64 over shares of a few squares in fp32, in a fixed order: results repeat bit for bit.
+ *
+ *   grads   host in [n_grads], read before the call returns; each g is a device pointer to n elements (n = 0 is allowed), aligned
+ *           to its element (16 bytes is fastest)
+ *   out     device out [4] fp32 = (norm, factor, 1 if norm is finite else 0, 0).  factor is NaN where norm is not finite:
+ *           spo_adamw_update then takes no step.  Such a norm sets SPO_DEV_NONFINITE
+ *   ws      device scratch, spo_workspace_bytes(SPO_WS_GRAD_NORM, ...) bytes (the same for all calls)
+ * Up to 1200 tensors are one launch (and one small one behind it).
+ */
+typedef struct spo_grad_tensor {
+  const void* g;
+  int64_t     n;
+  int32_t     dtype;
+  int32_t     reserved;
+} spo_grad_tensor;
+int32_t spo_grad_norm(const spo_grad_tensor* grads /* host */, int32_t n_grads, float max_norm, float grad_scale, float* out,
+                      void* ws, size_t ws_bytes, int32_t* d_status, void* stream);
+
+/*
+ * One AdamW step over many tensors (the vocabulary matrix with the loss's dW, norms, biases: what spo_muon_update is not used on).
+ * With t the number of this step, f = *d_scale, lr_k = lr lr_scale and decay_k = weight_decay decay_scale of the tensor, per element:
+ *   g~ = f g;   m <- beta1 m + (1 - beta1) g~;   v <- beta2 v + (1 - beta2) g~^2;
+ *   w <- w - lr_k ( (m / (1 - beta1^t)) / ( sqrt(v / (1 - beta2^t)) + eps ) + decay_k w );   copy <- w rounded to bf16.
+ * m and v are formed by individually rounded fp32 operations (every product and sum above; 1 - beta rounded to fp32 first).  bf16
+ * weights are rounded to nearest after each step: at small lr they need fp32 weights with a bf16 copy to move at all.
+ *
+ *   tensors    host in [n_tensors], read before the call returns.  Device pointers, aligned to their elements (16 bytes is fastest):
+ *     w        in/out [n], fp32 or bf16 (w_dtype);   g  in [n], fp32 or bf16 (g_dtype);   copy  out [n] bf16, optional
+ *     state_bits 32:  m, v  in/out [n] fp32;  m_scale = v_scale = NULL
+ *     state_bits 8:   m  in/out [n] int8, v  in/out [n] uint8;  m_scale, v_scale  in/out [ceil(n / 256)] fp32.  Elements 256 i ..
+ *              256 i + 255 share scale i:  m = s sgn(c) (c/127)^2,  v = s (c/255)^4.  The new scale is the largest new magnitude of the
+ *              block (at least 2^-100 for m, 2^-90 for v); a new code is the number of borders (j - 1/2)^2, j = 1 .. 127 (v: (j - 1/2)^4,
+ *              j = 1 .. 255, as fp32), at or below the magnitude times the fp32 quotient 127^2 / s (255^4 / s); v > 0 takes code 1 at
+ *              least.  Zeroed codes and scales are the start.  The update of w uses m and v before they are rounded to codes
+ *     lr_scale, decay_scale   1 for the call's own
+ *   No two tensors may share memory that is written, nor a gradient with what is written.
+ *   d_scale    device in [1] fp32, optional (1): spo_grad_norm's out + 1
+ *   d_lr       device in [1] fp32, optional: replaces params->lr (a captured step whose rate changes)
+ *   d_step     device in/out [2] int32 (steps taken, 0), optional: t is one more than d_step[0], and the call leaves it so (calls
+ *              that share it run one after the other).  NULL: t = params->step
+ * An element whose g~ is not finite or above 2^60 in magnitude keeps its w, m and v (in 8 bits up to the rounding to the block's new scale)
+ * and sets SPO_DEV_NONFINITE.  A factor or rate that is not finite sets it too, and then the step is neither taken nor counted.
+ * Up to 400 tensors are one launch.  Tensors without elements are allowed; a call without any launches nothing and counts no step.
+ */
+#define SPO_ADAMW_BLOCK 256
+typedef struct spo_adamw_tensor {
+  void*       w;
+  const void* g;
+  void*       m;
+  void*       v;
+  float*      m_scale;
+  float*      v_scale;
+  void*       copy;
+  int64_t     n;
+  int32_t     w_dtype;
+  int32_t     g_dtype;
+  int32_t     state_bits;   /* 8 or 32 */
+  float       lr_scale;
+  float       decay_scale;
+  int32_t     reserved;
+} spo_adamw_tensor;
+typedef struct spo_adamw_params {
+  float   lr;             /* 1e-6 */
+  float   beta1;          /* 0.9, in [0, 1) */
+  float   beta2;          /* 0.999, in [0, 1) */
+  float   eps;            /* 1e-8, > 0 */
+  float   weight_decay;   /* 0 */
+  int32_t step;           /* 1, >= 1: the step that is taken, where d_step is NULL */
+} spo_adamw_params;
+int32_t spo_default_adamw_params(spo_adamw_params* p /* host, out */);
+int32_t spo_adamw_update(const spo_adamw_tensor* tensors /* host */, int32_t n_tensors, const float* d_scale, const float* d_lr,
+                         int32_t* d_step, const spo_adamw_params* params, int32_t* d_status, void* stream);
+
+/*
+ * Values of 8-bit states, for inspection or for going on in 32 bits: m_out[i], v_out[i] fp32 from the codes and scales of
+ * spo_adamw_update.  m with m_scale and m_out, or v with v_scale and v_out, may be NULL together.
+ */
+int32_t spo_adamw_decode(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n,
+                         float* m_out, float* v_out, void* stream);
 
 /* Scratch size in bytes for one call of the selected entry point (host only, no CUDA call
  * except a device-property query).  Arguments that the selected call does not use are ignored. */

@@ -22,16 +22,19 @@ DEV_ID_OUT_OF_RANGE, DEV_NONFINITE, DEV_UNIFORMS_EXHAUSTED, DEV_TIMEOUT, DEV_ZER
 DTYPE_F32, DTYPE_BF16 = 0, 1
 (WS_SAMPLE, WS_ADVANTAGES, WS_LOSS_FWD, WS_LOSS_BWD, WS_UPDATE_REPEATS, WS_ACTIVE_ROWS, WS_LOSS_BWD_ROWS,
  WS_LOSS_FWD_BWD, WS_LOSS_FWD_BWD_ROWS, WS_LOGPROBS, WS_LOGPROBS_BWD,
- WS_MUON) = range(12)
+ WS_MUON, WS_LAYERNORM_BWD, WS_GRAD_NORM) = range(14)
 AGG_TOKEN_MEAN, AGG_SEQ_MEAN = 0, 1
 SUR_PPO_CLIP, SUR_CISPO, SUR_GSPO = 0, 1, 2
 MUON_SCALE_NONE, MUON_SCALE_SPECTRAL, MUON_SCALE_RMS = 0, 1, 2
+NORM_LAYER, NORM_RMS = 0, 1
+ADAMW_BLOCK = 256                # elements of an 8-bit state that share a scale
 
 EXPORTS = [
     "spo_default_params", "spo_tracker_init", "spo_sample_prompts", "spo_advantages",
     "spo_advantages_static", "spo_advantages_apply", "spo_advantages_update",
     "spo_tracker_update", "spo_tracker_update_repeats", "spo_loss_fwd", "spo_loss_bwd", "spo_loss_fwd_bwd", "spo_loss_fwd_bwd_slabs", "spo_dw_slab_rows", "spo_loss_fwd_bwd_scatter", "spo_loss_stats", "spo_loss_mask_rows", "spo_loss_fwd_bwd_rows", "spo_loss_active_rows", "spo_loss_bwd_rows",
     "spo_logprobs", "spo_logprobs_bwd", "spo_default_muon_params", "spo_orthogonalize", "spo_muon_update",
+    "spo_layernorm_fwd", "spo_layernorm_bwd", "spo_grad_norm", "spo_default_adamw_params", "spo_adamw_update", "spo_adamw_decode",
     "spo_workspace_bytes",
     "spo_status_string", "spo_last_cuda_error", "spo_version", "spo_selftest_bounded_wait",
 ]
@@ -52,6 +55,24 @@ class SpoMuonParams(Structure):
         ("lr", c_float), ("momentum", c_float), ("weight_decay", c_float), ("eps", c_float),
         ("coef_a", c_float), ("coef_b", c_float), ("coef_c", c_float),
         ("steps", c_int32), ("nesterov", c_int32), ("scale_mode", c_int32),
+    ]
+
+
+class SpoAdamwParams(Structure):
+    _fields_ = [
+        ("lr", c_float), ("beta1", c_float), ("beta2", c_float), ("eps", c_float), ("weight_decay", c_float), ("step", c_int32),
+    ]
+
+
+class SpoGradTensor(Structure):
+    _fields_ = [("g", c_void_p), ("n", c_int64), ("dtype", c_int32), ("reserved", c_int32)]
+
+
+class SpoAdamwTensor(Structure):
+    _fields_ = [
+        ("w", c_void_p), ("g", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
+        ("copy", c_void_p), ("n", c_int64), ("w_dtype", c_int32), ("g_dtype", c_int32), ("state_bits", c_int32),
+        ("lr_scale", c_float), ("decay_scale", c_float), ("reserved", c_int32),
     ]
 
 
@@ -139,6 +160,16 @@ def lib():
                                         c_void_p, c_size_t, PM, c_void_p, c_void_p]
         L.spo_muon_update.argtypes = [c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_int32, c_int64, c_int64,
                                       c_void_p, c_size_t, PM, c_void_p, c_void_p]
+        L.spo_layernorm_fwd.argtypes = [c_void_p, c_int64, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_int32,
+                                        c_float, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.spo_layernorm_bwd.argtypes = [c_void_p, c_int32, c_void_p, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                        c_void_p, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32,
+                                        c_void_p, c_size_t, c_void_p, c_void_p]
+        L.spo_grad_norm.argtypes = [c_void_p, c_int32, c_float, c_float, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
+        PA = POINTER(SpoAdamwParams)
+        L.spo_default_adamw_params.argtypes = [PA]
+        L.spo_adamw_update.argtypes = [c_void_p, c_int32, c_void_p, c_void_p, c_void_p, PA, c_void_p, c_void_p]
+        L.spo_adamw_decode.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
         L.spo_selftest_bounded_wait.argtypes = [ctypes.c_uint32, c_void_p, c_void_p, c_void_p]
         L.spo_workspace_bytes.argtypes = [c_int32, c_int64, c_int32, c_int32, c_int64, c_int32, c_int32]
         L.spo_workspace_bytes.restype = c_size_t
@@ -517,3 +548,204 @@ def spo_muon_update(W, momentum, G, ws, params, d_status):
                                c.need("G", G, None, G.shape), _dtype_code(G), b, m, n, w, nb, ctypes.byref(params),
                                c.status(d_status), c.stream())
     _check(rc, "spo_muon_update")
+
+
+def _hidden_rows(c, name, t):
+    """(T, d, row pitch) of a matrix [T, d] whose rows are contiguous, at any pitch."""
+    if not isinstance(t, c.torch.Tensor) or t.dim() != 2:
+        raise ValueError("%s must be a matrix [T, d]" % name)
+    c.here(name, t)
+    T, d = t.shape
+    if T > 0 and d > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % name)
+    ld = t.stride(0) if T > 1 else max(d, 1)
+    if ld < d:
+        raise ValueError("the rows of %s overlap" % name)
+    return T, d, ld
+
+
+def _vectors(c, first, second, names, d, default):
+    """(address, address, type code) of two optional vectors [d] of one type."""
+    dtype = first.dtype if first is not None else second.dtype if second is not None else None
+    code = default if dtype is None else DTYPE_BF16 if dtype is c.torch.bfloat16 else DTYPE_F32 if dtype is c.torch.float32 else None
+    if code is None:
+        raise TypeError("%s must be float32 or bfloat16, got %s" % (names[0], dtype))
+    return c.may(names[0], first, dtype, (d,)), c.may(names[1], second, dtype, (d,)), code
+
+
+def spo_layernorm_fwd(x, residual, weight, bias, mask, y, h, mean, rstd, d_status, eps=1e-6, kind=NORM_LAYER):
+    """y = the layer norm (kind=NORM_RMS: the RMS norm) of the rows of x, or of h = x + residual where both tensors are given.  x may be
+    a slice of a wider buffer (rows contiguous); weight, bias, mask, mean and rstd may be None."""
+    c = _Args()
+    f32 = c.torch.float32
+    T, d, ld = _hidden_rows(c, "x", x)
+    w, b, w_code = _vectors(c, weight, bias, ("weight", "bias"), d, DTYPE_F32)
+    full, row = (T, d), (T,)
+    rc = lib().spo_layernorm_fwd(
+        x.data_ptr(), ld, c.may("residual", residual, x.dtype, full), _dtype_code(x), w, b, w_code,
+        c.may("mask", mask, c.torch.uint8, row), T, d, eps, kind, c.need("y", y, None, full), _dtype_code(y),
+        c.may("h", h, x.dtype, full), c.may("mean", mean, f32, row), c.may("rstd", rstd, f32, row), c.status(d_status), c.stream())
+    _check(rc, "spo_layernorm_fwd")
+
+
+def spo_layernorm_bwd(dy, x, weight, mask, mean, rstd, dh, dx, dw, db, dw_accumulate, ws, d_status, kind=NORM_LAYER):
+    """Gradients dx, dw, db of spo_layernorm_fwd: x are the rows that were normalised (the forward's h where it had a residual), dh
+    what reaches them past the norm.  weight, mask, dh, dw and db may be None, and ws where dw and db are."""
+    c = _Args()
+    f32 = c.torch.float32
+    T, d, ld = _hidden_rows(c, "x", x)
+    w, _, w_code = _vectors(c, weight, None, ("weight", ""), d, DTYPE_F32)
+    pw, pb, dw_code = _vectors(c, dw, db, ("dw", "db"), d, DTYPE_F32)
+    full, row = (T, d), (T,)
+    scratch, n = (None, 0) if ws is None else c.scratch(ws)
+    rc = lib().spo_layernorm_bwd(
+        c.need("dy", dy, None, full), _dtype_code(dy), x.data_ptr(), ld, _dtype_code(x), w, w_code,
+        c.may("mask", mask, c.torch.uint8, row), c.may("mean", mean, f32, row), c.need("rstd", rstd, f32, row),
+        c.may("dh", dh, x.dtype, full), T, d, kind, c.need("dx", dx, x.dtype, full), pw, pb, dw_code, int(dw_accumulate), scratch, n,
+        c.status(d_status), c.stream())
+    _check(rc, "spo_layernorm_bwd")
+
+
+class TensorList:
+    """The table of one spo_grad_norm or spo_adamw_update: the addresses of tensors that stay alive with it.  Made once, used in every
+    step while the tensors keep their memory."""
+
+    __slots__ = ("table", "address", "count", "device", "tensors")
+
+    def __init__(self, table, device, tensors):
+        self.table, self.address, self.count, self.device, self.tensors = table, ctypes.addressof(table), len(tensors), device, tensors
+
+    def here(self, c):
+        if self.count and self.device != c.device:
+            raise ValueError("the tensors of the list must be on the current CUDA device, are on cuda:%d" % self.device)
+
+
+def _one_device(torch, tensors):
+    """Checks every (name, tensor): on one CUDA device and contiguous; its number (-1: no tensors)."""
+    device = -1
+    for name, t in tensors:
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a tensor, got %s" % (name, type(t).__name__))
+        if not t.is_cuda or device not in (-1, t.get_device()):
+            raise ValueError("the tensors of a list must be on one CUDA device, %s is on %s" % (name, t.device))
+        if not t.is_contiguous():
+            raise ValueError("%s must be contiguous" % name)
+        device = t.get_device()
+    return device
+
+
+def grad_list(grads) -> TensorList:
+    """The table of the gradients (contiguous fp32 or bf16 tensors of any shape) that spo_grad_norm reads."""
+    import torch
+    grads = list(grads)
+    device = _one_device(torch, [("grads[%d]" % i, g) for i, g in enumerate(grads)])
+    table = (SpoGradTensor * max(len(grads), 1))()
+    for q, g in zip(table, grads):
+        q.g, q.n, q.dtype = g.data_ptr(), g.numel(), _dtype_code(g)
+    return TensorList(table, device, grads)
+
+
+def spo_grad_norm(grads, out, ws, d_status, max_norm=0.0, grad_scale=1.0):
+    """out[0] = the norm of all gradients of the list (times |grad_scale|), out[1] = the factor that clips them to max_norm (0: no
+    clipping) and scales them, out[2] = 1 where the norm is finite."""
+    c = _Args()
+    grads.here(c)
+    w, n = c.scratch(ws)
+    rc = lib().spo_grad_norm(grads.address, grads.count, max_norm, grad_scale, c.need("out", out, c.torch.float32, (4,)), w, n,
+                             c.status(d_status), c.stream())
+    _check(rc, "spo_grad_norm")
+
+
+def default_adamw_params(**overrides) -> SpoAdamwParams:
+    p = SpoAdamwParams()
+    _check(lib().spo_default_adamw_params(ctypes.byref(p)), "spo_default_adamw_params")
+    for k, v in overrides.items():
+        setattr(p, k, v)
+    return p
+
+
+def adamw_list(weights, grads, m, v, m_scale=None, v_scale=None, copies=None, lr_scale=None, decay_scale=None) -> TensorList:
+    """The table of one spo_adamw_update: lists of tensors, one entry for each weight.  States are fp32 (32 bits) or int8 / uint8
+    (8 bits, with scales of ceil(n / ADAMW_BLOCK) fp32 elements; None for a 32-bit entry); copies are bf16 or None; lr_scale and
+    decay_scale are numbers (default 1)."""
+    import torch
+    weights = list(weights)
+    k = len(weights)
+    f32, bf16 = torch.float32, torch.bfloat16
+
+    def column(name, values, fill=None):
+        values = [fill] * k if values is None else list(values)
+        if len(values) != k:
+            raise ValueError("%s has %d entries for %d weights" % (name, len(values), k))
+        return values
+
+    columns = [("weights", weights)] + [(name, column(name, x)) for name, x in (
+        ("grads", list(grads)), ("m", list(m)), ("v", list(v)), ("m_scale", m_scale), ("v_scale", v_scale), ("copies", copies))]
+    rates, decays = column("lr_scale", lr_scale, 1.0), column("decay_scale", decay_scale, 1.0)
+    device = _one_device(torch, [("%s[%d]" % (name, i), t) for name, x in columns for i, t in enumerate(x)
+                                 if t is not None or name in ("weights", "grads", "m", "v")])
+    table = (SpoAdamwTensor * max(k, 1))()
+    spans = []                                      # (first byte, byte behind the last, written)
+
+    def cover(t, written):
+        if t is not None and t.numel():
+            spans.append((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), written))
+        return None if t is None else t.data_ptr()
+
+    for i, (w, g, mi, vi, ms, vs, copy) in enumerate(zip(*[x for _, x in columns])):
+        n, q = w.numel(), table[i]
+        if g.shape != w.shape:
+            raise ValueError("grads[%d] must have shape %s, got %s" % (i, tuple(w.shape), tuple(g.shape)))
+        for name, t in (("m", mi), ("v", vi), ("copies", copy)):
+            if t is not None and t.numel() != n:
+                raise ValueError("%s[%d] must have %d elements, has %d" % (name, i, n, t.numel()))
+        if (mi.dtype, vi.dtype) == (f32, f32):
+            q.state_bits = 32
+            if ms is not None or vs is not None:
+                raise ValueError("m_scale[%d] and v_scale[%d] belong to 8-bit states" % (i, i))
+        elif (mi.dtype, vi.dtype) == (torch.int8, torch.uint8):
+            q.state_bits = 8
+            for name, t in (("m_scale", ms), ("v_scale", vs)):
+                if t is None or t.dtype != f32 or t.numel() != -(-n // ADAMW_BLOCK):
+                    raise ValueError("%s[%d] must be a float32 tensor of %d elements" % (name, i, -(-n // ADAMW_BLOCK)))
+        else:
+            raise TypeError("m[%d] and v[%d] must be float32, or int8 and uint8" % (i, i))
+        if copy is not None and copy.dtype != bf16:
+            raise TypeError("copies[%d] must be bfloat16" % i)
+        q.w, q.g, q.m, q.v = cover(w, True), cover(g, False), cover(mi, True), cover(vi, True)
+        q.m_scale, q.v_scale, q.copy = cover(ms, True), cover(vs, True), cover(copy, True)
+        q.n, q.w_dtype, q.g_dtype = n, _dtype_code(w), _dtype_code(g)
+        q.lr_scale, q.decay_scale = rates[i], decays[i]
+    read = written = 0
+    for begin, end, out in sorted(spans):
+        if begin < written or (out and begin < read):
+            raise ValueError("tensors of the list share memory that is written (the same tensor twice?)")
+        read, written = max(read, end), max(written, end if out else 0)
+    return TensorList(table, device, list(zip(*[x for _, x in columns])))
+
+
+def spo_adamw_update(tensors, d_scale, d_step, d_lr, params, d_status):
+    """One AdamW step over the tensors of the list: weights, states and copies in place.  d_scale [1] (spo_grad_norm's out[1:2]) multiplies
+    the gradients; d_step [2] int32 counts the steps on the device (None: params.step is the step); d_lr [1] replaces params.lr."""
+    c = _Args()
+    f32 = c.torch.float32
+    tensors.here(c)
+    rc = lib().spo_adamw_update(tensors.address, tensors.count, c.may("d_scale", d_scale, f32, (1,)), c.may("d_lr", d_lr, f32, (1,)),
+                                c.may("d_step", d_step, c.torch.int32, (2,)), ctypes.byref(params), c.status(d_status), c.stream())
+    _check(rc, "spo_adamw_update")
+
+
+def spo_adamw_decode(m, m_scale, v, v_scale, m_out, v_out):
+    """The fp32 values of 8-bit states; m, m_scale and m_out, or v, v_scale and v_out, may be None together."""
+    c = _Args()
+    t = m if m is not None else v
+    if not isinstance(t, c.torch.Tensor):
+        raise TypeError("m or v must be a tensor")
+    f32, shape, blocks = c.torch.float32, t.shape, (-(-t.numel() // ADAMW_BLOCK),)
+    if (m is None) != (m_out is None) or (v is None) != (v_out is None):
+        raise ValueError("m and m_out, v and v_out come together")
+    rc = lib().spo_adamw_decode(
+        c.may("m", m, c.torch.int8, shape), None if m is None else c.need("m_scale", m_scale, f32, blocks),
+        c.may("v", v, c.torch.uint8, shape), None if v is None else c.need("v_scale", v_scale, f32, blocks), t.numel(),
+        c.may("m_out", m_out, f32, shape), c.may("v_out", v_out, f32, shape), c.stream())
+    _check(rc, "spo_adamw_decode")

@@ -10,7 +10,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libspo.so")
-SOURCES = ["spo_api.cu", "spo_small.cu", "spo_loss_common.cu", "spo_loss_tc.cu", "spo_logprobs.cu", "spo_muon.cu"]
+SOURCES = ["spo_api.cu", "spo_small.cu", "spo_loss_common.cu", "spo_loss_tc.cu", "spo_logprobs.cu", "spo_muon.cu",
+           "spo_layernorm.cu", "spo_adamw.cu"]
 HEADERS = [os.path.join(CSRC, "spo_internal.h"), os.path.join(CSRC, "spo_ptx.cuh"), os.path.join(ROOT, "include", "spo.h")]
 
 

@@ -768,6 +768,165 @@ int32_t spo_muon_update(void* W, int32_t W_dtype, float* momentum, const void* G
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);
 }
 
+static bool float_type(int32_t t) { return t == SPO_DTYPE_F32 || t == SPO_DTYPE_BF16; }
+static size_t float_size(int32_t t) { return t == SPO_DTYPE_BF16 ? 2 : 4; }
+
+static int32_t check_norm_shape(int64_t T, int32_t d, int64_t ldx, int32_t kind) {
+  if (T < 0 || d < 1 || ldx < d || (kind != SPO_NORM_LAYER && kind != SPO_NORM_RMS)) return SPO_ERR_INVALID_ARG;
+  if (T >= ((int64_t)1 << 31) - 256 || d > SPO_NORM_MAX_D) return SPO_ERR_BAD_SHAPE;
+  return SPO_OK;
+}
+
+// An output may be an input only as a whole, element for element.
+static bool clash(const void* out, wide_t out_bytes, const void* in, wide_t in_bytes, bool same_layout) {
+  return out && in && overlap(out, out_bytes, in, in_bytes) && !(same_layout && out == in);
+}
+
+int32_t spo_layernorm_fwd(const void* x, int64_t ldx, const void* residual, int32_t dtype, const void* weight, const void* bias,
+                          int32_t w_dtype, const uint8_t* mask, int64_t T, int32_t d, float eps, int32_t kind, void* y,
+                          int32_t y_dtype, void* h, float* mean, float* rstd, int32_t* d_status, void* stream) {
+  if (!float_type(dtype) || !float_type(w_dtype) || !float_type(y_dtype)) return SPO_ERR_UNSUPPORTED_DTYPE;
+  const int32_t rc = check_norm_shape(T, d, ldx, kind);
+  if (rc != SPO_OK) return rc;
+  if (!(eps > 0.0f) || !(eps < 3.0e38f) || (residual == nullptr) != (h == nullptr)) return SPO_ERR_INVALID_ARG;
+  if (mean && kind != SPO_NORM_LAYER) return SPO_ERR_INVALID_ARG;
+  if (T > 0 && (!x || !y)) return SPO_ERR_INVALID_ARG;
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(bias) || !aligned16(y) || !aligned16(h) ||
+      !aligned16(mean) || !aligned16(rstd))
+    return SPO_ERR_BAD_ALIGNMENT;
+  if (T > 0) {
+    const wide_t bx = ((wide_t)(T - 1) * ldx + d) * float_size(dtype), row = (wide_t)T * d, bh = row * float_size(dtype);
+    const wide_t by = row * float_size(y_dtype), bw = (wide_t)d * float_size(w_dtype), bt = (wide_t)T * 4;
+    const bool packed = ldx == d || T == 1;
+    if (clash(y, by, x, bx, packed && dtype == y_dtype && !residual) || clash(y, by, residual, bh, false) || clash(y, by, h, bh, false) ||
+        clash(h, bh, x, bx, packed) || clash(h, bh, residual, bh, true))
+      return SPO_ERR_INVALID_ARG;
+    const struct { const void* p; wide_t n; } out[4] = {{y, by}, {h, bh}, {mean, bt}, {rstd, bt}}, in[5] = {{weight, bw}, {bias, bw}, {mask, (wide_t)T}, {x, bx}, {residual, bh}};
+    for (int i = 0; i < 4; ++i) {
+      for (int k = 0; k < (i < 2 ? 3 : 5); ++k)
+        if (clash(out[i].p, out[i].n, in[k].p, in[k].n, false)) return SPO_ERR_INVALID_ARG;
+      for (int k = i + 1; k < 4; ++k)
+        if (clash(out[i].p, out[i].n, out[k].p, out[k].n, false)) return SPO_ERR_INVALID_ARG;
+    }
+  }
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  LayerNormFwd a{};
+  a.x = x; a.residual = residual; a.weight = weight; a.bias = bias; a.mask = mask; a.ldx = ldx; a.T = T; a.d = d; a.dtype = dtype;
+  a.w_dtype = w_dtype; a.y_dtype = y_dtype; a.kind = kind; a.eps = eps; a.y = y; a.h = h; a.mean = mean; a.rstd = rstd;
+  a.d_status = d_status;
+  cudaError_t e = launch_layernorm_fwd(a, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
+int32_t spo_layernorm_bwd(const void* dy, int32_t dy_dtype, const void* x, int64_t ldx, int32_t dtype, const void* weight,
+                          int32_t w_dtype, const uint8_t* mask, const float* mean, const float* rstd, const void* dh, int64_t T,
+                          int32_t d, int32_t kind, void* dx, void* dweight, void* dbias, int32_t dw_dtype, int32_t dw_accumulate,
+                          void* ws, size_t ws_bytes, int32_t* d_status, void* stream) {
+  (void)d_status;                       // nothing of this call is found on the device; the argument is that of the other calls
+  if (!float_type(dtype) || !float_type(dy_dtype) || !float_type(w_dtype) || !float_type(dw_dtype)) return SPO_ERR_UNSUPPORTED_DTYPE;
+  const int32_t rc = check_norm_shape(T, d, ldx, kind);
+  if (rc != SPO_OK) return rc;
+  const bool sums = dweight || dbias;
+  if ((mean == nullptr) != (kind == SPO_NORM_RMS) && (T > 0 || mean)) return SPO_ERR_INVALID_ARG;
+  if (T > 0 && (!dy || !x || !rstd || !dx || (sums && !ws))) return SPO_ERR_INVALID_ARG;
+  if (!aligned16(dy) || !aligned16(x) || !aligned16(weight) || !aligned16(mean) || !aligned16(rstd) || !aligned16(dh) ||
+      !aligned16(dx) || !aligned16(dweight) || !aligned16(dbias) || !aligned16(ws))
+    return SPO_ERR_BAD_ALIGNMENT;
+  const wide_t bd = (wide_t)d * float_size(dw_dtype);
+  if (clash(dweight, bd, dbias, bd, false)) return SPO_ERR_INVALID_ARG;
+  if (T > 0) {
+    const wide_t bx = ((wide_t)(T - 1) * ldx + d) * float_size(dtype), row = (wide_t)T * d, bh = row * float_size(dtype);
+    const wide_t by = row * float_size(dy_dtype), bw = (wide_t)d * float_size(w_dtype), bt = (wide_t)T * 4;
+    const bool packed = ldx == d || T == 1;
+    if (clash(dx, bh, dy, by, dtype == dy_dtype) || clash(dx, bh, dh, bh, true) || clash(dx, bh, x, bx, packed)) return SPO_ERR_INVALID_ARG;
+    const struct { const void* p; wide_t n; } out[3] = {{dx, bh}, {dweight, bd}, {dbias, bd}},
+        in[8] = {{weight, bw}, {mask, (wide_t)T}, {mean, bt}, {rstd, bt}, {dx, bh}, {dy, by}, {dh, bh}, {x, bx}};
+    for (int i = 0; i < 3; ++i)
+      for (int k = 0; k < (i == 0 ? 4 : 8); ++k)
+        if (clash(out[i].p, out[i].n, in[k].p, in[k].n, false)) return SPO_ERR_INVALID_ARG;
+  }
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  if (T > 0 && sums && ws_bytes < layernorm_bwd_ws_bytes(T, d)) return SPO_ERR_WORKSPACE_TOO_SMALL;
+  LayerNormBwd a{};
+  a.dy = dy; a.x = x; a.weight = weight; a.dh = dh; a.mask = mask; a.mean = mean; a.rstd = rstd; a.ldx = ldx; a.T = T; a.d = d;
+  a.dtype = dtype; a.dy_dtype = dy_dtype; a.w_dtype = w_dtype; a.dw_dtype = dw_dtype; a.dw_accumulate = dw_accumulate; a.kind = kind;
+  a.dx = dx; a.dw = dweight; a.db = dbias;
+  cudaError_t e = launch_layernorm_bwd(a, (char*)ws, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
+static constexpr int64_t kElementsMost = (int64_t)1 << 33;         // of one tensor: chunk numbers of a launch fit 32 bits
+
+int32_t spo_grad_norm(const spo_grad_tensor* grads, int32_t n_grads, float max_norm, float grad_scale, float* out, void* ws,
+                      size_t ws_bytes, int32_t* d_status, void* stream) {
+  const float big = 3.0e38f;
+  if (n_grads < 0 || (n_grads > 0 && !grads) || !out || !ws) return SPO_ERR_INVALID_ARG;
+  if (!(max_norm > -big && max_norm < big) || !(grad_scale > -big && grad_scale < big)) return SPO_ERR_INVALID_ARG;
+  for (int i = 0; i < n_grads; ++i) {
+    const spo_grad_tensor& q = grads[i];
+    if (!float_type(q.dtype)) return SPO_ERR_UNSUPPORTED_DTYPE;
+    if (q.n < 0 || (q.n > 0 && !q.g)) return SPO_ERR_INVALID_ARG;
+    if (q.n > kElementsMost) return SPO_ERR_BAD_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(q.g) & (float_size(q.dtype) - 1)) != 0) return SPO_ERR_BAD_ALIGNMENT;
+  }
+  if (!aligned16(ws) || (reinterpret_cast<uintptr_t>(out) & 15) != 0) return SPO_ERR_BAD_ALIGNMENT;
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  if (ws_bytes < grad_norm_ws_bytes()) return SPO_ERR_WORKSPACE_TOO_SMALL;
+  cudaError_t e = launch_grad_norm(grads, n_grads, max_norm, grad_scale, out, (char*)ws, d_status, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
+int32_t spo_default_adamw_params(spo_adamw_params* p) {
+  if (!p) return SPO_ERR_INVALID_ARG;
+  p->lr = 1e-6f;
+  p->beta1 = 0.9f;
+  p->beta2 = 0.999f;
+  p->eps = 1e-8f;
+  p->weight_decay = 0.0f;
+  p->step = 1;
+  return SPO_OK;
+}
+
+int32_t spo_adamw_update(const spo_adamw_tensor* tensors, int32_t n_tensors, const float* d_scale, const float* d_lr, int32_t* d_step,
+                         const spo_adamw_params* params, int32_t* d_status, void* stream) {
+  const float big = 3.0e38f;
+  if (!params || n_tensors < 0 || (n_tensors > 0 && !tensors)) return SPO_ERR_INVALID_ARG;
+  if (!(params->lr > -big && params->lr < big) || !(params->weight_decay > -big && params->weight_decay < big)) return SPO_ERR_INVALID_ARG;
+  for (float b : {params->beta1, params->beta2})
+    if (!(b >= 0.0f) || !(b < 1.0f)) return SPO_ERR_INVALID_ARG;
+  if (!(params->eps > 0.0f) || !(params->eps < big) || params->step < 1) return SPO_ERR_INVALID_ARG;
+  for (int i = 0; i < n_tensors; ++i) {
+    const spo_adamw_tensor& q = tensors[i];
+    if (!float_type(q.w_dtype) || !float_type(q.g_dtype) || (q.state_bits != 8 && q.state_bits != 32)) return SPO_ERR_UNSUPPORTED_DTYPE;
+    if (q.n < 0 || (q.n > 0 && (!q.w || !q.g || !q.m || !q.v))) return SPO_ERR_INVALID_ARG;
+    if (q.n > 0 && ((q.m_scale != nullptr) != (q.state_bits == 8) || (q.v_scale != nullptr) != (q.state_bits == 8))) return SPO_ERR_INVALID_ARG;
+    if (!(q.lr_scale > -big && q.lr_scale < big) || !(q.decay_scale > -big && q.decay_scale < big)) return SPO_ERR_INVALID_ARG;
+    if (q.n > kElementsMost) return SPO_ERR_BAD_SHAPE;
+    const uintptr_t state = q.state_bits == 32 ? 3 : 0;
+    if ((reinterpret_cast<uintptr_t>(q.w) & (float_size(q.w_dtype) - 1)) || (reinterpret_cast<uintptr_t>(q.g) & (float_size(q.g_dtype) - 1)) ||
+        (reinterpret_cast<uintptr_t>(q.copy) & 1) || ((reinterpret_cast<uintptr_t>(q.m) | reinterpret_cast<uintptr_t>(q.v)) & state) ||
+        ((reinterpret_cast<uintptr_t>(q.m_scale) | reinterpret_cast<uintptr_t>(q.v_scale)) & 3))
+      return SPO_ERR_BAD_ALIGNMENT;
+  }
+  if (((reinterpret_cast<uintptr_t>(d_scale) | reinterpret_cast<uintptr_t>(d_lr) | reinterpret_cast<uintptr_t>(d_step)) & 3) != 0)
+    return SPO_ERR_BAD_ALIGNMENT;
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  cudaError_t e = launch_adamw(tensors, n_tensors, d_scale, d_lr, d_step, *params, d_status, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
+int32_t spo_adamw_decode(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n, float* m_out,
+                         float* v_out, void* stream) {
+  if (n < 0) return SPO_ERR_INVALID_ARG;
+  if (n > 0 && ((m != nullptr) != (m_out != nullptr) || (v != nullptr) != (v_out != nullptr) || (m && !m_scale) || (v && !v_scale)))
+    return SPO_ERR_INVALID_ARG;
+  for (const float* p : {m_scale, v_scale, (const float*)m_out, (const float*)v_out})
+    if ((reinterpret_cast<uintptr_t>(p) & 3) != 0) return SPO_ERR_BAD_ALIGNMENT;
+  if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
+  cudaError_t e = launch_adamw_decode(m, m_scale, v, v_scale, n, m_out, v_out, (cudaStream_t)stream);
+  return e == cudaSuccess ? SPO_OK : cuda_fail(e);
+}
+
 size_t spo_workspace_bytes(int32_t which, int64_t T, int32_t d, int32_t V, int64_t N, int32_t B, int32_t M) {
   switch (which) {
     case SPO_WS_SAMPLE:
@@ -818,6 +977,11 @@ size_t spo_workspace_bytes(int32_t which, int64_t T, int32_t d, int32_t V, int64
     case SPO_WS_MUON:                   /* T = rows, d = columns, B = matrices */
       if (!muon_shape_ok(B, T, d)) return 0;
       return muon_ws_bytes(T, d, B);
+    case SPO_WS_LAYERNORM_BWD:
+      if (T < 0 || d < 1 || d > SPO_NORM_MAX_D) return 0;
+      return layernorm_bwd_ws_bytes(T, d);
+    case SPO_WS_GRAD_NORM:
+      return grad_norm_ws_bytes();
     default:
       return 0;
   }

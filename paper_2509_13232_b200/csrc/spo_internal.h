@@ -326,6 +326,38 @@ struct MuonArgs {
 size_t muon_ws_bytes(int64_t m, int64_t n, int64_t batch);
 cudaError_t muon_run(const MuonArgs& a, char* ws, cudaStream_t st);
 
+// ---- norms of the hidden states ----------------------------------------------
+struct LayerNormFwd {
+  const void *x, *residual, *weight, *bias;
+  const uint8_t* mask;
+  int64_t ldx, T;
+  int32_t d, dtype, w_dtype, y_dtype, kind;
+  float eps;
+  void *y, *h;
+  float *mean, *rstd;
+  int32_t* d_status;
+};
+struct LayerNormBwd {
+  const void *dy, *x, *weight, *dh;
+  const uint8_t* mask;
+  const float *mean, *rstd;
+  int64_t ldx, T;
+  int32_t d, dtype, dy_dtype, w_dtype, dw_dtype, dw_accumulate, kind;
+  void *dx, *dw, *db;
+};
+size_t layernorm_bwd_ws_bytes(int64_t T, int32_t d);
+cudaError_t launch_layernorm_fwd(const LayerNormFwd& a, cudaStream_t st);
+cudaError_t launch_layernorm_bwd(const LayerNormBwd& a, char* ws, cudaStream_t st);
+
+// ---- gradient norm and AdamW ----------------------------------------------------
+size_t grad_norm_ws_bytes();
+cudaError_t launch_grad_norm(const spo_grad_tensor* grads, int count, float max_norm, float scale, float* out, char* ws,
+                             int32_t* d_status, cudaStream_t st);
+cudaError_t launch_adamw(const spo_adamw_tensor* tensors, int count, const float* d_scale, const float* d_lr, int32_t* d_step,
+                         const spo_adamw_params& p, int32_t* d_status, cudaStream_t st);
+cudaError_t launch_adamw_decode(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n, float* m_out,
+                                float* v_out, cudaStream_t st);
+
 cudaError_t launch_bounded_wait_probe(int32_t* d_status, uint32_t limit_us, int32_t* reached_end, cudaStream_t st);
 
 }  // namespace spo
