@@ -744,7 +744,7 @@ typedef struct spo_adamw_params {
   float   lr;             /* 1e-6 */
   float   beta1;          /* 0.9, in [0, 1) */
   float   beta2;          /* 0.999, in [0, 1) */
-  float   eps;            /* 1e-8, > 0 */
+  float   eps;            /* 1e-8, at least 2^-100 */
   float   weight_decay;   /* 0 */
   int32_t step;           /* 1, >= 1: the step that is taken, where d_step is NULL */
 } spo_adamw_params;

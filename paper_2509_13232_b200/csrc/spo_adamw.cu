@@ -193,9 +193,13 @@ cudaError_t norm_launch(const spo_grad_tensor* grads, int from, int to, double* 
 // ---------------------------------------------------------------------------
 // AdamW
 // ---------------------------------------------------------------------------
-constexpr int kStepThreads = 256;
-constexpr int kStepChunk = 2048;                    // elements that a block takes at a time: a warp takes one block of an 8-bit state
-constexpr int kStepBlocksPerSm = 4;
+// A block is one warp: it shares nothing with others, and an SM starts the next one as soon as one is done.
+constexpr int kStepChunk = 256;                     // elements that a warp takes at a time, a block of an 8-bit state
+constexpr int kStepBlocksPerSm = 24;
+// Chunks in a row that a warp takes: enough for its start to be paid (the constants, the first inputs) and, in 8 bits, for the inputs that
+// are fetched ahead; few enough for kRounds rounds of warps over the GPU.  155 million elements: 8 bits 479 us (bf16 weights 323) with
+// up to 16 and 516 (369) with up to 6, 32 bits 694 us and 682; 11 million in 8 bits: 37 us with one round, 30 with three.
+constexpr int kSpanMost8 = 16, kSpanMost32 = 6, kRounds = 3;
 constexpr int kTensorsMost = 400;                   // tensors per launch, 80 bytes each
 constexpr int kTensorsFew = 12;
 
@@ -219,9 +223,11 @@ static_assert(sizeof(Tensor) == 80, "two tables have to fit the parameters of a 
 struct StepScalars {
   const float *d_scale, *d_lr;
   int32_t* d_step;
-  double log_b1, log_b2;
+  float log_b1, log_b2;                             // -inf for 0, whose powers are then 0
   float lr, b1, b1c, b2, b2c, eps;
+  float one;                                        // 1: a product and a sum that must not become one multiply-add go through it
   float rate, root;                                 // lr-free 1/(1 - b1^t) and 1/sqrt(1 - b2^t), where the host knows t
+  uint32_t span;
   int32_t advance;                                  // the last launch of a call counts the step
   int32_t* d_status;
 };
@@ -233,237 +239,454 @@ struct StepTable {
   uint32_t chunks;
 };
 
-struct Rates {                                      // of one launch, in shared memory
-  float f, lr, rate, root;
+// What a launch reads from the device, as issued, and the constants that come of it.
+struct Rates {
+  float f, lr;
+  int32_t taken;
+  float rate;
+  bool ready, fine;
 };
 
-// One element: m and v become the new moments; returns the new weight.  A gradient that is not usable changes nothing.
-__device__ __forceinline__ float step_element(float w, float g, float& m, float& v, const StepScalars& a, float step, float root,
-                                              float pull, bool& bad) {
-  const float g2 = __fmul_rn(g, g);
-  if (!(g2 <= kSquareMost)) {
-    bad = true;
-    return w;
-  }
-  m = __fadd_rn(__fmul_rn(m, a.b1), __fmul_rn(g, a.b1c));
-  v = __fadd_rn(__fmul_rn(v, a.b2), __fmul_rn(g2, a.b2c));
-  float s;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(s) : "f"(v));
-  const float u = __fdividef(m, fmaf(s, root, a.eps));
-  return w - fmaf(step, u, pull * w);
+// Two fp32 operations in one instruction, each rounded by itself.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
 }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z, u;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 u, x, y, z;\n\tmov.b64 {%0, %1}, u;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return fma2(b, make_float2(-1.0f, -1.0f), a); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Approximate root and reciprocal (relative error below 2^-22); arguments and results below 2^-126 count as zero, but for full_sqrt.
+__device__ __forceinline__ float near_sqrt(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float full_sqrt(float x) {
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float near_inverse(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float2 near_sqrt2(float2 x) { return make_float2(near_sqrt(x.x), near_sqrt(x.y)); }
 
 __device__ __forceinline__ float warp_max(float v) {          // of magnitudes: their bit patterns are in order
   return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(v)));
 }
 
-__device__ __forceinline__ float decode_m(int c, float unit) { return __fmul_rn((float)(c * abs(c)), unit); }
-__device__ __forceinline__ float decode_v(uint32_t c, float unit) {
-  const float q = (float)(c * c);
-  return __fmul_rn(__fmul_rn(q, q), unit);
+// Constants of the packed operations, as pairs in shared memory: each is read where it is used (two at a time), because as many pairs as
+// there are would take half of the registers.
+enum { kCb1, kCb1c, kCb2, kCb2c, kCone, kCf, kCbyte, kCbyte128, kCwhole, kCminus, kCeps, kCroot, kConstants };
+__device__ __forceinline__ void pair_of(const float2* c, float2& a, float2& b) {       // c[0] and c[1], 16 bytes aligned
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(a.x), "=f"(a.y), "=f"(b.x), "=f"(b.y) : "r"((uint32_t)__cvta_generic_to_shared(c)));
+}
+
+// The four bytes of a word as floats: a byte is the low end of the mantissa of 2^23.
+constexpr float kByteBase = 8388608.0f;
+__device__ __forceinline__ float byte_float(uint32_t w, int k) { return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7540 + k)); }
+__device__ __forceinline__ float2 decode_m2(uint32_t w, int k, float unit, float2 byte128 = both(-(kByteBase + 128.0f))) {
+  const float2 c = add2(make_float2(byte_float(w ^ 0x80808080u, k), byte_float(w ^ 0x80808080u, k + 1)), byte128);   // codes k and k + 1
+  return mul2(make_float2(c.x * fabsf(c.x), c.y * fabsf(c.y)), both(unit));            // (c |c| is exact)
+}
+__device__ __forceinline__ float2 decode_v2(uint32_t w, int k, float unit, float2 byte = both(-kByteBase)) {
+  float2 c = add2(make_float2(byte_float(w, k), byte_float(w, k + 1)), byte);
+  c = mul2(c, c);
+  return mul2(mul2(c, c), both(unit));
 }
 __device__ __forceinline__ float unit_m(float scale) { return __fmul_rn(scale, (float)(1.0 / 16129.0)); }
 __device__ __forceinline__ float unit_v(float scale) { return __fmul_rn(scale, (float)(1.0 / 4228250625.0)); }
 
-// Codes: the estimate from the approximate root is the count of borders or one beside it, and the comparison with the borders next
-// to it says which.
-__device__ __forceinline__ int encode_m(float m, float to_unit) {
+// Codes.  Adding 1.5 x 2^23 to the root of a scaled magnitude rounds it to a whole number and leaves that, in two's complement, in the low
+// bits.  The approximate root does for a code unless it lies within kNear of a border (its error is below 2^-22 of it, 6e-5 at 255)
+// or belongs to a v that might take code 0; one warp in thirty has such an element, and forms its codes by the comparison with the
+// borders: the root, enlarged by more than its error, rounds to the count of borders or one more, and the border below,
+// (c - 1/2)^2 (exact) or that squared (rounded once, as the borders are), says which.
+constexpr float kWhole = 12582912.0f, kEnlarge = 1.0f + 0x1p-20f, kNear = 0x1p-13f;
+__device__ __forceinline__ uint32_t low_bytes(float2 a, float2 b) {
+  const uint32_t lo = __byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040);
+  const uint32_t hi = __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040);
+  return __byte_perm(lo, hi, 0x5410);
+}
+__device__ __forceinline__ float encode_m(float m, float to_unit) {                     // in the low bits
   const float y = __fmul_rn(fabsf(m), to_unit);
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(y));
-  float c = rintf(r);
-  const float below = fmaf(c, c, 0.25f) - c, above = fmaf(c, c, 0.25f) + c;      // (c - 1/2)^2 and (c + 1/2)^2, exact
-  if (c > 0.0f && y < below) c -= 1.0f;
-  if (y >= above) c += 1.0f;
-  return (int)copysignf(c, m);
+  float c = rintf(near_sqrt(y) * kEnlarge);
+  const float h = c - 0.5f;                                                             // (-1/2 where c is 0: its square counts as negative)
+  if (y < h * fabsf(h)) c -= 1.0f;
+  return copysignf(c, m) + kWhole;
 }
-__device__ __forceinline__ uint32_t encode_v(float v, float to_unit) {
+__device__ __forceinline__ float encode_v(float v, float to_unit) {
   const float y = __fmul_rn(v, to_unit);
-  float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(y));
-  asm("sqrt.approx.f32 %0, %0;" : "+f"(r));
-  float c = rintf(r);
-  const float below = fmaf(c, c, 0.25f) - c, above = fmaf(c, c, 0.25f) + c;      // their squares are rounded once, as the borders are
-  if (c > 0.0f && y < __fmul_rn(below, below)) c -= 1.0f;
-  if (y >= __fmul_rn(above, above)) c += 1.0f;
+  float c = fmaxf(rintf(near_sqrt(near_sqrt(y)) * kEnlarge), 1.0f);
+  const float h = c - 0.5f, b = h * h;
+  if (y < __fmul_rn(b, b)) c -= 1.0f;
   if (v > 0.0f) c = fmaxf(c, 1.0f);
-  return (uint32_t)c;
+  return c + kWhole;
+}
+__device__ __forceinline__ float2 encode_m2(float2 m, float to_unit) { return make_float2(encode_m(m.x, to_unit), encode_m(m.y, to_unit)); }
+__device__ __forceinline__ float2 encode_v2(float2 v, float to_unit) { return make_float2(encode_v(v.x, to_unit), encode_v(v.y, to_unit)); }
+
+// Four consecutive elements, aligned, as they are in memory.  Loads of a step are issued where they are written, all of them before the
+// first one is waited for: left to the compiler, those of the weights come after the moments' arithmetic, and their latency is paid
+// apart (8 bits: 388 and 516 us).
+template <bool IS16>
+struct Raw4 {
+  uint32_t x[IS16 ? 2 : 4];
+};
+__device__ __forceinline__ void issue(const void* p, Raw4<true>& r) {
+  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.x[0]), "=r"(r.x[1]) : "l"(p));
+}
+__device__ __forceinline__ void issue(const void* p, Raw4<false>& r) {
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x[0]), "=r"(r.x[1]), "=r"(r.x[2]), "=r"(r.x[3]) : "l"(p));
+}
+__device__ __forceinline__ void issue(const void* p, uint32_t& x) { asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(x) : "l"(p)); }
+__device__ __forceinline__ void issue(const int32_t* p, int32_t& x) { asm volatile("ld.global.s32 %0, [%1];" : "=r"(x) : "l"(p)); }
+__device__ __forceinline__ void issue(const float* p, float& x) { asm volatile("ld.global.f32 %0, [%1];" : "=f"(x) : "l"(p)); }
+template <bool IS16>
+__device__ __forceinline__ float2 pair_in(const Raw4<IS16>& r, int p) {                // elements 2 p and 2 p + 1
+  if constexpr (IS16) return make_float2(low_bf16(r.x[p]), high_bf16(r.x[p]));
+  else return make_float2(__uint_as_float(r.x[2 * p]), __uint_as_float(r.x[2 * p + 1]));
+}
+__device__ __forceinline__ void store4(void* p, bool is16, const float* f) {
+  if (is16) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
+    *static_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  } else {
+    *static_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+  }
 }
 
-// Four consecutive elements, of which `left` exist (4 or more: all); `vec`: they are aligned.
-__device__ __forceinline__ void load4(const void* p, bool is16, int64_t e, int64_t left, bool vec, float* f) {
-  if (vec && left >= 4) {
-    if (is16) {
-      const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + e);
-      f[0] = low_bf16(q.x); f[1] = high_bf16(q.x); f[2] = low_bf16(q.y); f[3] = high_bf16(q.y);
-    } else {
-      const float4 q = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + e);
-      f[0] = q.x; f[1] = q.y; f[2] = q.z; f[3] = q.w;
-    }
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    f[k] = k < left ? (is16 ? low_bf16(static_cast<const uint16_t*>(p)[e + k]) : static_cast<const float*>(p)[e + k]) : 0.0f;
-}
-__device__ __forceinline__ void store4(void* p, bool is16, int64_t e, int64_t left, bool vec, const float* f) {
-  if (vec && left >= 4) {
-    if (is16) {
-      const __nv_bfloat162 a = __floats2bfloat162_rn(f[0], f[1]), b = __floats2bfloat162_rn(f[2], f[3]);
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + e) =
-          make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-    } else {
-      *reinterpret_cast<float4*>(static_cast<float*>(p) + e) = make_float4(f[0], f[1], f[2], f[3]);
-    }
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (k < left) {
-      if (is16) static_cast<__nv_bfloat16*>(p)[e + k] = __float2bfloat16_rn(f[k]);
-      else static_cast<float*>(p)[e + k] = f[k];
-    }
-}
-__device__ __forceinline__ uint32_t load4_codes(const void* p, int64_t e, int64_t left, bool vec) {
-  const uint8_t* c = static_cast<const uint8_t*>(p) + e;
-  if (vec && left >= 4) return *reinterpret_cast<const uint32_t*>(c);
-  uint32_t q = 0;
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (k < left) q |= (uint32_t)c[k] << (8 * k);
-  return q;
-}
-__device__ __forceinline__ void store4_codes(void* p, int64_t e, int64_t left, bool vec, uint32_t q) {
-  uint8_t* c = static_cast<uint8_t*>(p) + e;
-  if (vec && left >= 4) {
-    *reinterpret_cast<uint32_t*>(c) = q;
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (k < left) c[k] = (uint8_t)(q >> (8 * k));
+// Element e of an array whose elements have `bytes` bytes.
+__device__ __forceinline__ char* at_element(const void* p, int bytes, int64_t e) {
+  return const_cast<char*>(static_cast<const char*>(p)) + e * bytes;
 }
 
-// A warp's 256 elements from `base` on: a lane has elements 4 lane .. + 3 and 128 + 4 lane .. + 3.
+// What a lane reads of 256 elements: 4 lane .. + 3 and 128 + 4 lane .. + 3.
 template <bool W16, bool G16, bool EIGHT>
-__device__ __forceinline__ void step_warp(const Tensor& t, int64_t base, const StepScalars& a, const Rates& s, bool& bad) {
-  const int lane = threadIdx.x & 31;
-  const bool vec = t.kind & kAligned;
-  float w[8], g[8], m[8], v[8];
+struct Inputs {
+  Raw4<G16> g[2];
+  Raw4<W16> w[2];
+  Raw4<false> m[EIGHT ? 1 : 2], v[EIGHT ? 1 : 2];
   uint32_t cm[2], cv[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t e = base + 128 * h + 4 * lane, left = t.n - e;
-    load4(t.g, G16, e, left, vec, g + 4 * h);
-    load4(t.w, W16, e, left, vec, w + 4 * h);
-    if (EIGHT) {
-      cm[h] = load4_codes(t.m, e, left, vec);
-      cv[h] = load4_codes(t.v, e, left, vec);
-    } else {
-      load4(t.m, false, e, left, vec, m + 4 * h);
-      load4(t.v, false, e, left, vec, v + 4 * h);
-    }
-  }
-  if (EIGHT) {
-    const float um = unit_m(t.m_scale[base >> 8]), uv = unit_v(t.v_scale[base >> 8]);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      m[k] = decode_m((int)(int8_t)(cm[k >> 2] >> (8 * (k & 3))), um);
-      v[k] = decode_v((cv[k >> 2] >> (8 * (k & 3))) & 0xffu, uv);
-    }
-  }
-  const float lr = s.lr * t.lr_scale, step = lr * s.rate, pull = lr * t.decay;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) w[k] = step_element(w[k], __fmul_rn(g[k], s.f), m[k], v[k], a, step, s.root, pull, bad);
-  if (EIGHT) {
-    float top_m = kMFloor, top_v = kVFloor;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      top_m = fmaxf(top_m, fabsf(m[k]));
-      top_v = fmaxf(top_v, v[k]);
-    }
-    top_m = warp_max(top_m);
-    top_v = warp_max(top_v);
-    const float to_m = __fdiv_rn(16129.0f, top_m), to_v = __fdiv_rn(4228250625.0f, top_v);
+  float m_scale, v_scale;
+  __device__ __forceinline__ void fetch(const Tensor& t, int64_t base) {
+    constexpr int kW = W16 ? 2 : 4, kG = G16 ? 2 : 4;
+    const int64_t e = base + 4 * (threadIdx.x & 31);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      cm[h] = cv[h] = 0u;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        cm[h] |= ((uint32_t)encode_m(m[4 * h + k], to_m) & 0xffu) << (8 * k);
-        cv[h] |= encode_v(v[4 * h + k], to_v) << (8 * k);
+      issue(at_element(t.g, kG, e) + 128 * h * kG, g[h]);
+      if constexpr (EIGHT) {
+        issue(at_element(t.m, 1, e) + 128 * h, cm[h]);
+        issue(at_element(t.v, 1, e) + 128 * h, cv[h]);
+      } else {
+        issue(at_element(t.m, 4, e) + 512 * h, m[h]);
+        issue(at_element(t.v, 4, e) + 512 * h, v[h]);
       }
     }
+    if constexpr (EIGHT) {
+      issue(t.m_scale + (base >> 8), m_scale);
+      issue(t.v_scale + (base >> 8), v_scale);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) issue(at_element(t.w, kW, e) + 128 * h * kW, w[h]);
+  }
+};
+
+// A warp's 256 elements from `base` on, whole and aligned, as four pairs a lane.
+// Returns false, with nothing written, where a gradient may not be usable: v stays below 2^96 where all are, because (1 - b2) g~^2 is at
+// least 2^-24 times g~^2.
+template <bool W16, bool G16, bool EIGHT>
+__device__ __forceinline__ bool step_warp(const Tensor& t, int64_t base, const Inputs<W16, G16, EIGHT>& in, const float2* consts, float step,
+                                          float pull) {
+  const int lane = threadIdx.x & 31;
+  const int64_t e = base + 4 * lane;
+  constexpr int kW = W16 ? 2 : 4, kS = EIGHT ? 1 : 4;
+  float2 m[4], v[4];
+  uint32_t cm[2], cv[2];
+  if constexpr (EIGHT) {
+    const float um = unit_m(in.m_scale), uv = unit_v(in.v_scale);
+    float2 byte, byte128;
+    pair_of(consts + kCbyte, byte, byte128);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      m[p] = decode_m2(in.cm[p >> 1], 2 * (p & 1), um, byte128);
+      v[p] = decode_v2(in.cv[p >> 1], 2 * (p & 1), uv, byte);
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      m[p] = pair_in(in.m[p >> 1], p & 1);
+      v[p] = pair_in(in.v[p >> 1], p & 1);
+    }
+  }
+  float top_m = kMFloor;
+  uint32_t top_v = __float_as_uint(kVFloor);                  // as bits: a NaN is above all numbers
+  {
+    float2 one, f, b1, b1c, b2, b2c;
+    pair_of(consts + kCone, one, f);
+    pair_of(consts + kCb1, b1, b1c);
+    pair_of(consts + kCb2, b2, b2c);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const float2 gs = mul2(pair_in(in.g[p >> 1], p & 1), f);
+      m[p] = fma2(mul2(m[p], b1), one, mul2(gs, b1c));
+      v[p] = fma2(mul2(v[p], b2), one, mul2(mul2(gs, gs), b2c));
+      if (EIGHT) top_m = fmaxf(top_m, fmaxf(fabsf(m[p].x), fabsf(m[p].y)));
+      top_v = max(top_v, max(__float_as_uint(v[p].x), __float_as_uint(v[p].y)));
+    }
+  }
+  if (EIGHT) {
+    top_m = warp_max(top_m);
+    top_v = __reduce_max_sync(0xffffffffu, top_v);
+    if (top_v >= __float_as_uint(0x1p96f)) return false;
+  } else {
+    if (__any_sync(0xffffffffu, top_v >= __float_as_uint(0x1p96f))) return false;
+  }
+  float2 w[4], eps, root_unit;
+  pair_of(consts + kCeps, eps, root_unit);
+  if (EIGHT) {
+    const float scale_v = __uint_as_float(top_v);
+    const float to_m = __fdiv_rn(16129.0f, top_m), to_v = __fdiv_rn(4228250625.0f, scale_v);
+    root_unit = both(root_unit.x * (near_sqrt(scale_v) * (1.0f / 65025.0f)));       // of the root of the scaled v
+    float2 whole, minus;
+    pair_of(consts + kCwhole, whole, minus);
+    float far = 0.0f, low = 1.0f;                             // the largest distance from a whole number, the lowest root of a v
+    float2 tm[2], tv[2];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const float2 y = mul2(v[p], both(to_v)), root = near_sqrt2(y);
+      const float2 d = fma2(root, root_unit, eps);
+      const float2 u = mul2(m[p], make_float2(near_inverse(d.x), near_inverse(d.y)));
+      const float2 w0 = pair_in(in.w[p >> 1], p & 1);
+      w[p] = add2(w0, fma2(both(step), u, mul2(both(pull), w0)));
+      const float2 z = mul2(m[p], both(to_m)), rv = near_sqrt2(root);
+      const float2 rm = make_float2(copysignf(near_sqrt(fabsf(z.x)), z.x), copysignf(near_sqrt(fabsf(z.y)), z.y));
+      tm[p & 1] = add2(rm, whole);
+      tv[p & 1] = add2(rv, whole);
+      const float2 fm = sub2(rm, add2(tm[p & 1], minus)), fv = sub2(rv, add2(tv[p & 1], minus));
+      far = fmaxf(fmaxf(far, fabsf(fm.x)), fabsf(fm.y));
+      far = fmaxf(fmaxf(far, fabsf(fv.x)), fabsf(fv.y));
+      low = fminf(fminf(low, rv.x), rv.y);
+      if (p & 1) {
+        cm[p >> 1] = low_bytes(tm[0], tm[1]);
+        cv[p >> 1] = low_bytes(tv[0], tv[1]);
+      }
+    }
+    if (__any_sync(0xffffffffu, far > 0.5f - kNear || low < 0.5f + kNear)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        cm[h] = low_bytes(encode_m2(m[2 * h], to_m), encode_m2(m[2 * h + 1], to_m));
+        cv[h] = low_bytes(encode_v2(v[2 * h], to_v), encode_v2(v[2 * h + 1], to_v));
+      }
+    }
+    if (lane == 0) {
+      t.m_scale[base >> 8] = top_m;
+      t.v_scale[base >> 8] = scale_v;
+    }
+  } else {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const float2 d = fma2(make_float2(full_sqrt(v[p].x), full_sqrt(v[p].y)), root_unit, eps);
+      const float2 u = mul2(m[p], make_float2(near_inverse(d.x), near_inverse(d.y)));
+      const float2 w0 = pair_in(in.w[p >> 1], p & 1);
+      w[p] = add2(w0, fma2(both(step), u, mul2(both(pull), w0)));
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    store4(at_element(t.w, kW, e) + 128 * h * kW, W16, &w[2 * h].x);
+    if (t.copy) store4(t.copy + e + 128 * h, true, &w[2 * h].x);
+    if (EIGHT) {
+      *reinterpret_cast<uint32_t*>(at_element(t.m, 1, e) + 128 * h) = cm[h];
+      *reinterpret_cast<uint32_t*>(at_element(t.v, 1, e) + 128 * h) = cv[h];
+    } else {
+      store4(at_element(t.m, kS, e) + 128 * h * kS, false, &m[2 * h].x);
+      store4(at_element(t.v, kS, e) + 128 * h * kS, false, &v[2 * h].x);
+    }
+  }
+  return true;
+}
+
+// The same for any 256 elements or the rest of a tensor, element by element (lane, lane + 32, ...): unaligned tensors, ends, and gradients
+// that are not usable, whose elements keep their moments and weight.  Returns whether there was one.  Nothing is held from one
+// element to the next, and the moments are formed twice where their largest has to be known first: a call, or arrays, would cost the
+// loop above its registers.
+__device__ __forceinline__ bool step_warp_any(const Tensor& t, int64_t base, const float2* consts, float step, float pull) {
+  const int lane = threadIdx.x & 31;
+  const bool w16 = t.kind & kW16, g16 = t.kind & kG16, eight = t.kind & kEight;
+  const int64_t end = t.n - base < 256 ? t.n : base + 256;
+  float um = 0.0f, uv = 0.0f, to_m = 0.0f, to_v = 0.0f;
+  bool kept = false;
+  auto moments = [&](int64_t e, float& m, float& v) {           // whether the gradient was usable
+    const float g = __fmul_rn(g16 ? low_bf16(static_cast<const uint16_t*>(t.g)[e]) : static_cast<const float*>(t.g)[e], consts[kCf].x);
+    m = eight ? decode_m2(static_cast<const uint8_t*>(t.m)[e], 0, um).x : static_cast<const float*>(t.m)[e];
+    v = eight ? decode_v2(static_cast<const uint8_t*>(t.v)[e], 0, uv).x : static_cast<const float*>(t.v)[e];
+    const float g2 = __fmul_rn(g, g);
+    if (!(g2 <= kSquareMost)) return false;
+    m = __fadd_rn(__fmul_rn(m, consts[kCb1].x), __fmul_rn(g, consts[kCb1c].x));
+    v = __fadd_rn(__fmul_rn(v, consts[kCb2].x), __fmul_rn(g2, consts[kCb2c].x));
+    return true;
+  };
+  if (eight) {
+    um = unit_m(t.m_scale[base >> 8]);
+    uv = unit_v(t.v_scale[base >> 8]);
+    float top_m = kMFloor, top_v = kVFloor, m, v;
+#pragma unroll 1
+    for (int64_t e = base + lane; e < end; e += 32) {
+      moments(e, m, v);
+      top_m = fmaxf(top_m, fabsf(m));
+      top_v = fmaxf(top_v, v);
+    }
+    __syncwarp();
+    top_m = warp_max(top_m);
+    top_v = warp_max(top_v);
+    to_m = __fdiv_rn(16129.0f, top_m);
+    to_v = __fdiv_rn(4228250625.0f, top_v);
     if (lane == 0) {
       t.m_scale[base >> 8] = top_m;
       t.v_scale[base >> 8] = top_v;
     }
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t e = base + 128 * h + 4 * lane, left = t.n - e;
-    store4(t.w, W16, e, left, vec, w + 4 * h);
-    if (t.copy) store4(t.copy, true, e, left, vec, w + 4 * h);
-    if (EIGHT) {
-      store4_codes(t.m, e, left, vec, cm[h]);
-      store4_codes(t.v, e, left, vec, cv[h]);
+#pragma unroll 1
+  for (int64_t e = base + lane; e < end; e += 32) {
+    float m, v;
+    const bool usable = moments(e, m, v);
+    const float w0 = w16 ? low_bf16(static_cast<const uint16_t*>(t.w)[e]) : static_cast<const float*>(t.w)[e];
+    const float u = m * near_inverse(fmaf(full_sqrt(v), consts[kCroot].x, consts[kCeps].x));
+    const float w = usable ? w0 + fmaf(step, u, pull * w0) : w0;
+    kept |= !usable;
+    if (eight) {
+      static_cast<uint8_t*>(t.m)[e] = (uint8_t)__float_as_uint(encode_m(m, to_m));
+      static_cast<uint8_t*>(t.v)[e] = (uint8_t)__float_as_uint(encode_v(v, to_v));
     } else {
-      store4(t.m, false, e, left, vec, m + 4 * h);
-      store4(t.v, false, e, left, vec, v + 4 * h);
+      static_cast<float*>(t.m)[e] = m;
+      static_cast<float*>(t.v)[e] = v;
     }
+    if (w16) static_cast<__nv_bfloat16*>(t.w)[e] = __float2bfloat16_rn(w);
+    else static_cast<float*>(t.w)[e] = w;
+    if (t.copy) t.copy[e] = __float2bfloat16_rn(w);
   }
+  __syncwarp();
+  return kept;
 }
 
-template <int N>
-__global__ void __launch_bounds__(kStepThreads, kStepBlocksPerSm) adamw_kernel(const __grid_constant__ StepTable<N> tab,
-                                                                              const __grid_constant__ StepScalars a) {
-  __shared__ Rates s_rates;
-  if (threadIdx.x == 0) {
-    Rates r;
-    r.f = a.d_scale ? *a.d_scale : 1.0f;
-    r.lr = a.d_lr ? *a.d_lr : a.lr;
-    r.rate = a.rate;
-    r.root = a.root;
-    if (a.d_step) {
-      const int32_t taken = *a.d_step;
-      const double t = (double)(taken < 0 ? 0 : taken) + 1.0;
-      r.rate = (float)(-1.0 / expm1(t * a.log_b1));
-      r.root = (float)rsqrt(-expm1(t * a.log_b2));
-    }
-    s_rates = r;
+// The constants of a launch, in shared memory; whether the step is taken at all.
+__device__ __forceinline__ void make_constants(float2* consts, const StepScalars& a, Rates& s) {
+  float root = a.root;
+  s.rate = a.rate;
+  if (a.d_step) {
+    const float t = (float)max(s.taken, 0) + 1.0f;
+    s.rate = -1.0f / expm1f(t * a.log_b1);
+    root = rsqrtf(-expm1f(t * a.log_b2));
   }
-  __syncthreads();
-  const Rates s = s_rates;
-  if (!(fabsf(s.f) < INFINITY) || !(fabsf(s.lr) < INFINITY)) {       // the step is not taken, and not counted
+  if (threadIdx.x == 0) {
+    consts[kCf] = both(s.f); consts[kCroot] = both(root);
+    consts[kCb1] = both(a.b1); consts[kCb1c] = both(a.b1c); consts[kCb2] = both(a.b2); consts[kCb2c] = both(a.b2c);
+    consts[kCone] = both(a.one); consts[kCeps] = both(a.eps);
+    consts[kCbyte] = both(-kByteBase); consts[kCbyte128] = both(-(kByteBase + 128.0f));
+    consts[kCwhole] = both(kWhole); consts[kCminus] = both(-kWhole);
+  }
+  __syncwarp();
+  s.ready = true;
+  s.fine = fabsf(s.f) < INFINITY && fabsf(s.lr) < INFINITY;
+}
+
+// A warp's share, `chunks` chunks from `base` on, as far as they are whole.  Returns the chunks (a bit each) that are left
+// for step_warp_any: it is kept out of this loop, whose registers its call would cost.
+template <bool W16, bool G16, bool EIGHT>
+__device__ __forceinline__ uint32_t step_span(const Tensor& t, int64_t base, int chunks, float2* consts, const StepScalars& a, Rates& s) {
+  const int64_t whole = t.n - base >= 256 ? (t.n - base - 256) / kStepChunk + 1 : 0;
+  const int n = whole < chunks ? (int)whole : chunks;
+  const uint32_t left = ((1u << chunks) - 1) & ~((1u << n) - 1);
+  if (n == 0) return left;
+  Inputs<W16, G16, EIGHT> in;
+  in.fetch(t, base);
+  if (!s.ready) make_constants(consts, a, s);
+  if (!s.fine) return 0;
+  const float lr = s.lr * t.lr_scale, step = -lr * s.rate, pull = -lr * t.decay;
+  uint32_t again = 0;
+#pragma unroll 1
+  for (int c = 0; c < n; ++c, base += kStepChunk) {
+    if (EIGHT) {                             // the next chunk's inputs are on their way while this one is worked on
+      Inputs<W16, G16, EIGHT> next = in;
+      if (c + 1 < n) next.fetch(t, base + kStepChunk);
+      if (!step_warp<W16, G16, EIGHT>(t, base, in, consts, step, pull)) again |= 1u << c;
+      in = next;
+    } else {
+      if (!step_warp<W16, G16, EIGHT>(t, base, in, consts, step, pull)) again |= 1u << c;
+      if (c + 1 < n) in.fetch(t, base + kStepChunk);
+    }
+  }
+  return left | again;
+}
+
+// Many more blocks than fit at once, each with a few chunks in a row, come out ahead of as many as fit that walk through all of it: the SMs
+// do not run at one pace (32-bit states, 155 million elements: 644 us and 732 us).
+template <int N>
+__global__ void __launch_bounds__(32, kStepBlocksPerSm) adamw_kernel(const __grid_constant__ StepTable<N> tab,
+                                                                     const __grid_constant__ StepScalars a) {
+  __shared__ __align__(16) float2 s_const[kConstants];
+  Rates s;
+  s.f = 1.0f;
+  s.lr = a.lr;
+  s.taken = 0;
+  if (a.d_scale) issue(a.d_scale, s.f);
+  if (a.d_lr) issue(a.d_lr, s.lr);
+  if (a.d_step) issue(a.d_step, s.taken);
+  s.ready = false;
+  bool bad = false;
+  uint32_t chunk = blockIdx.x * a.span;
+  const uint32_t end = min(chunk + a.span, tab.chunks);
+  for (int i = find_tensor(tab, chunk); chunk < end; ++i) {
+    const Tensor& t = tab.t[i];
+    const uint32_t stop = min(end, i + 1 < tab.count ? tab.t[i + 1].first : tab.chunks);
+    const int64_t base = (int64_t)(chunk - t.first) * kStepChunk;
+    const int here = (int)(stop - chunk);
+    uint32_t left = (1u << here) - 1;
+    switch (t.kind) {
+      case kAligned: left = step_span<false, false, false>(t, base, here, s_const, a, s); break;
+      case kAligned | kW16: left = step_span<true, false, false>(t, base, here, s_const, a, s); break;
+      case kAligned | kG16: left = step_span<false, true, false>(t, base, here, s_const, a, s); break;
+      case kAligned | kW16 | kG16: left = step_span<true, true, false>(t, base, here, s_const, a, s); break;
+      case kAligned | kEight: left = step_span<false, false, true>(t, base, here, s_const, a, s); break;
+      case kAligned | kEight | kW16: left = step_span<true, false, true>(t, base, here, s_const, a, s); break;
+      case kAligned | kEight | kG16: left = step_span<false, true, true>(t, base, here, s_const, a, s); break;
+      case kAligned | kEight | kW16 | kG16: left = step_span<true, true, true>(t, base, here, s_const, a, s); break;
+      default: break;                                         // unaligned: all of them are left
+    }
+    if (!s.ready) make_constants(s_const, a, s);
+    if (!s.fine) break;
+    const float lr = s.lr * t.lr_scale;
+    for (; left; left &= left - 1)
+      bad |= step_warp_any(t, base + (int64_t)(__ffs(left) - 1) * kStepChunk, s_const, -lr * s.rate, -lr * t.decay);
+    chunk = stop;
+  }
+  if (!s.fine) {                                              // the step is not taken, and not counted
     if (blockIdx.x == 0 && threadIdx.x == 0) flag(a.d_status, SPO_DEV_NONFINITE);
     return;
   }
-  bool bad = false;
-  int i = find_tensor(tab, blockIdx.x);
-  for (uint64_t chunk = blockIdx.x; chunk < tab.chunks; chunk += gridDim.x) {
-    while (i + 1 < tab.count && tab.t[i + 1].first <= chunk) ++i;
-    const Tensor& t = tab.t[i];
-    const int64_t base = (int64_t)(chunk - t.first) * kStepChunk + (threadIdx.x >> 5) * 256;
-    if (base >= t.n) continue;
-    switch (t.kind & (kW16 | kG16 | kEight)) {
-      case 0: step_warp<false, false, false>(t, base, a, s, bad); break;
-      case kW16: step_warp<true, false, false>(t, base, a, s, bad); break;
-      case kG16: step_warp<false, true, false>(t, base, a, s, bad); break;
-      case kW16 | kG16: step_warp<true, true, false>(t, base, a, s, bad); break;
-      case kEight: step_warp<false, false, true>(t, base, a, s, bad); break;
-      case kEight | kW16: step_warp<true, false, true>(t, base, a, s, bad); break;
-      case kEight | kG16: step_warp<false, true, true>(t, base, a, s, bad); break;
-      default: step_warp<true, true, true>(t, base, a, s, bad); break;
-    }
-  }
   if (bad) flag(a.d_status, SPO_DEV_NONFINITE);
-  if (a.d_step && a.advance && threadIdx.x == 0) {
-    // every block has read the counter before it arrives here; the last one to arrive moves it
-    const int arrived = atomicAdd(a.d_step + 1, 1);
-    if (arrived == (int)gridDim.x - 1) {
-      a.d_step[1] = 0;
-      if (a.d_step[0] < 0x7fffffff) a.d_step[0] = (a.d_step[0] < 0 ? 0 : a.d_step[0]) + 1;
-    }
+  // every block has read the counter before it arrives here; the last one to arrive moves it
+  if (a.d_step && a.advance && threadIdx.x == 0 && atomicAdd(a.d_step + 1, 1) == (int)gridDim.x - 1) {
+    a.d_step[1] = 0;
+    if (s.taken < 0x7fffffff) a.d_step[0] = (s.taken < 0 ? 0 : s.taken) + 1;
   }
 }
 
@@ -471,7 +694,7 @@ template <int N>
 cudaError_t step_launch(const spo_adamw_tensor* tensors, int from, int to, StepScalars a, const spo_adamw_params& p, cudaStream_t st) {
   StepTable<N> tab;
   tab.count = 0;
-  uint64_t chunks = 0;
+  uint64_t chunks = 0, eight = 0;
   for (int i = from; i < to; ++i) {
     const spo_adamw_tensor& q = tensors[i];
     if (q.n == 0) continue;
@@ -483,34 +706,49 @@ cudaError_t step_launch(const spo_adamw_tensor* tensors, int from, int to, StepS
     t.kind = (q.w_dtype == SPO_DTYPE_BF16 ? kW16 : 0) | (q.g_dtype == SPO_DTYPE_BF16 ? kG16 : 0) |
              (q.state_bits == 8 ? kEight : 0) | ((at & 15) == 0 ? kAligned : 0);
     chunks += (uint64_t)ceil_div(q.n, kStepChunk);
+    if (q.state_bits == 8) eight += (uint64_t)ceil_div(q.n, kStepChunk);
   }
   tab.chunks = (uint32_t)chunks;
   if (chunks == 0) return cudaSuccess;
-  const int64_t most = (int64_t)sm_count() * kStepBlocksPerSm;
-  adamw_kernel<N><<<(unsigned)((int64_t)chunks < most ? (int64_t)chunks : most), kStepThreads, 0, st>>>(tab, a);
+  const uint64_t at_once = (uint64_t)sm_count() * kStepBlocksPerSm, span = chunks / (at_once * kRounds);
+  const uint64_t most = 2 * eight > chunks ? kSpanMost8 : kSpanMost32;
+  a.span = (uint32_t)(chunks <= at_once ? 1 : span < 2 ? 2 : span > most ? most : span);
+  adamw_kernel<N><<<(unsigned)ceil_div((int64_t)chunks, a.span), 32, 0, st>>>(tab, a);
   return cudaGetLastError();
 }
 
-// Values of 8-bit states: four of each a thread.
-__global__ void __launch_bounds__(256) adamw_decode_kernel(const int8_t* __restrict__ m, const float* __restrict__ m_scale,
+// Values of 8-bit states: a warp takes the 256 elements of a block, a lane elements 4 lane .. + 3 and 128 + 4 lane .. + 3 (or, where they are
+// not aligned or end, every 32nd).
+__global__ void __launch_bounds__(256) adamw_decode_kernel(const uint8_t* __restrict__ m, const float* __restrict__ m_scale,
                                                            const uint8_t* __restrict__ v, const float* __restrict__ v_scale, int64_t n,
-                                                           bool vec, float* __restrict__ m_out, float* __restrict__ v_out) {
-  for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; e < n; e += (int64_t)gridDim.x * 1024) {
-    const int64_t left = n - e;
-    float f[4];
-    if (m) {
-      const uint32_t c = load4_codes(m, e, left, vec);
-      const float unit = unit_m(m_scale[e >> 8]);
+                                                           bool aligned, float* __restrict__ m_out, float* __restrict__ v_out) {
+  const int lane = threadIdx.x & 31;
+  for (int64_t base = ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)) * 256; base < n; base += (int64_t)gridDim.x * 2048) {
+    const float um = m ? unit_m(m_scale[base >> 8]) : 0.0f, uv = v ? unit_v(v_scale[base >> 8]) : 0.0f;
+    if (aligned && n - base >= 256) {
+      const int64_t e = base + 4 * lane;
+      uint32_t cm[2] = {0, 0}, cv[2] = {0, 0};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) f[k] = decode_m((int)(int8_t)(c >> (8 * k)), unit);
-      store4(m_out, false, e, left, vec, f);
-    }
-    if (v) {
-      const uint32_t c = load4_codes(v, e, left, vec);
-      const float unit = unit_v(v_scale[e >> 8]);
+      for (int h = 0; h < 2; ++h) {
+        if (m) cm[h] = *reinterpret_cast<const uint32_t*>(m + e + 128 * h);
+        if (v) cv[h] = *reinterpret_cast<const uint32_t*>(v + e + 128 * h);
+      }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) f[k] = decode_v((c >> (8 * k)) & 0xffu, unit);
-      store4(v_out, false, e, left, vec, f);
+      for (int h = 0; h < 2; ++h) {
+        if (m) {
+          const float2 f[2] = {decode_m2(cm[h], 0, um), decode_m2(cm[h], 2, um)};
+          store4(m_out + e + 128 * h, false, &f[0].x);
+        }
+        if (v) {
+          const float2 f[2] = {decode_v2(cv[h], 0, uv), decode_v2(cv[h], 2, uv)};
+          store4(v_out + e + 128 * h, false, &f[0].x);
+        }
+      }
+    } else {
+      for (int64_t e = base + lane; e < n && e < base + 256; e += 32) {
+        if (m) m_out[e] = decode_m2(m[e], 0, um).x;
+        if (v) v_out[e] = decode_v2(v[e], 0, uv).x;
+      }
     }
   }
 }
@@ -551,12 +789,12 @@ cudaError_t launch_adamw(const spo_adamw_tensor* tensors, int count, const float
   StepScalars a{};
   a.d_scale = d_scale; a.d_lr = d_lr; a.d_step = d_step; a.d_status = d_status;
   const double b1 = p.beta1, b2 = p.beta2, t = p.step;
-  a.log_b1 = log(b1);                               // -inf for 0, whose powers are then 0
-  a.log_b2 = log(b2);
-  a.lr = p.lr; a.eps = p.eps;
+  a.log_b1 = (float)log(b1);
+  a.log_b2 = (float)log(b2);
+  a.lr = p.lr; a.eps = p.eps; a.one = 1.0f;
   a.b1 = p.beta1; a.b1c = (float)(1.0 - b1); a.b2 = p.beta2; a.b2c = (float)(1.0 - b2);
-  a.rate = (float)(-1.0 / expm1(t * a.log_b1));
-  a.root = (float)(1.0 / sqrt(-expm1(t * a.log_b2)));
+  a.rate = (float)(-1.0 / expm1(t * log(b1)));
+  a.root = (float)(1.0 / sqrt(-expm1(t * log(b2))));
   // the launches of a call, the last of which counts the step: those that hold an element
   int end = count;
   while (end > 0 && tensors[end - 1].n == 0) --end;
@@ -576,8 +814,9 @@ cudaError_t launch_adamw_decode(const int8_t* m, const float* m_scale, const uin
   if (n == 0 || (!m && !v)) return cudaSuccess;
   uintptr_t at = 0;
   for (const void* x : {(const void*)m, (const void*)v, (const void*)m_out, (const void*)v_out}) at |= reinterpret_cast<uintptr_t>(x);
-  const int64_t need = ceil_div(n, 1024), most = (int64_t)sm_count() * 8 * 4;
-  adamw_decode_kernel<<<(unsigned)(need < most ? need : most), 256, 0, st>>>(m, m_scale, v, v_scale, n, (at & 15) == 0, m_out, v_out);
+  const int64_t need = ceil_div(n, 2048), most = 0x7fffffff;
+  adamw_decode_kernel<<<(unsigned)(need < most ? need : most), 256, 0, st>>>(reinterpret_cast<const uint8_t*>(m), m_scale, v, v_scale, n, (at & 15) == 0,
+                                                                             m_out, v_out);
   return cudaGetLastError();
 }
 

@@ -894,7 +894,7 @@ int32_t spo_adamw_update(const spo_adamw_tensor* tensors, int32_t n_tensors, con
   if (!(params->lr > -big && params->lr < big) || !(params->weight_decay > -big && params->weight_decay < big)) return SPO_ERR_INVALID_ARG;
   for (float b : {params->beta1, params->beta2})
     if (!(b >= 0.0f) || !(b < 1.0f)) return SPO_ERR_INVALID_ARG;
-  if (!(params->eps > 0.0f) || !(params->eps < big) || params->step < 1) return SPO_ERR_INVALID_ARG;
+  if (!(params->eps >= 0x1p-100f) || !(params->eps < big) || params->step < 1) return SPO_ERR_INVALID_ARG;
   for (int i = 0; i < n_tensors; ++i) {
     const spo_adamw_tensor& q = tensors[i];
     if (!float_type(q.w_dtype) || !float_type(q.g_dtype) || (q.state_bits != 8 && q.state_bits != 32)) return SPO_ERR_UNSUPPORTED_DTYPE;
