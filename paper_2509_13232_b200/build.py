@@ -12,7 +12,8 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libspo.so")
 SOURCES = ["spo_api.cu", "spo_small.cu", "spo_loss_common.cu", "spo_loss_tc.cu", "spo_logprobs.cu", "spo_muon.cu",
            "spo_layernorm.cu", "spo_adamw.cu"]
-HEADERS = [os.path.join(CSRC, "spo_internal.h"), os.path.join(CSRC, "spo_ptx.cuh"), os.path.join(ROOT, "include", "spo.h")]
+HEADERS = [os.path.join(CSRC, "spo_internal.h"), os.path.join(CSRC, "spo_ptx.cuh"), os.path.join(CSRC, "spo_vec.cuh"),
+           os.path.join(ROOT, "include", "spo.h")]
 
 
 def nvcc_path() -> str:

@@ -11,7 +11,10 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "spo_internal.h"
+#include "spo_vec.cuh"
 
 namespace spo {
 namespace {
@@ -46,17 +49,46 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
   return r;
 }
 
+// The same for rows that are read once: they leave the L1 cache to the weights, which every row wants again (24 000 rows of 4096 with a
+// residual: 155 and 12X us).
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> stream_pack(const T* p) {
+  Pack<T, V> r;
+  constexpr int kBytes = Pack<T, V>::kBytes;
+  if constexpr (kBytes >= 16) {
+#pragma unroll
+    for (int i = 0; i < kBytes / 16; ++i)
+      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(r.w[4 * i]), "=r"(r.w[4 * i + 1]), "=r"(r.w[4 * i + 2]), "=r"(r.w[4 * i + 3])
+                   : "l"(reinterpret_cast<const char*>(p) + 16 * i));
+  } else if constexpr (kBytes == 8) {
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
+  } else {
+    r = load_pack<T, V>(p);
+  }
+  return r;
+}
+
 template <typename T, int V>
 __device__ __forceinline__ void zero_pack(Pack<T, V>& r) {
 #pragma unroll
   for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) r.w[i] = 0u;
 }
 
+// Element k from its bits (for 16-bit types in the low half); the element was 0.
+template <typename T, int V>
+__device__ __forceinline__ void put_element(Pack<T, V>& r, int k, uint32_t bits) {
+  if constexpr (sizeof(T) == 4) r.w[k] = bits;
+  else r.w[k >> 1] |= bits << (16 * (k & 1));
+}
+
 template <typename T, int V>
 __device__ __forceinline__ float element(const Pack<T, V>& r, int k) {
   if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[k]);
-  return __uint_as_float((k & 1) ? (r.w[k >> 1] & 0xffff0000u) : (r.w[k >> 1] << 16));
+  return (k & 1) ? high_bf16(r.w[k >> 1]) : low_bf16(r.w[k >> 1]);
 }
+template <typename T, int V>
+__device__ __forceinline__ float2 pair_of(const Pack<T, V>& r, int p) { return make_float2(element(r, 2 * p), element(r, 2 * p + 1)); }
 
 template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> round_pack(const float* f) {
@@ -109,6 +141,8 @@ __device__ __forceinline__ void load_weights(const void* p, int bf16, int64_t c,
   }
 }
 
+__host__ __device__ __forceinline__ constexpr int align16(int n) { return (n + 15) & ~15; }
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -129,123 +163,317 @@ struct FwdParams {
   const void *x, *residual, *weight, *bias;
   const uint8_t* mask;
   int64_t ldx, T;
-  int32_t d, w_bf16;
+  int32_t d, w_bf16, y_bf16;
   float eps;
   void *y, *h;
   float *mean, *rstd;
   int32_t* d_status;
 };
 
-constexpr int kFwdThreads = 256;          // of a block whose groups are smaller than that
+// Chunks.  A thread holds NV chunks of V elements (16 bytes) of a row: chunk i * threads + thread, so that a warp's accesses are
+// contiguous.  Where rows do not begin on 16 bytes (SHIFT), chunk c has the columns V c - shift + (0 .. V - 1), shift = (t d) mod V: in the
+// tensors without a pitch it then lies on 16 bytes again, but for the columns that the first and last chunk do not have, which are
+// moved one by one.
+template <typename T, int V, bool SHIFT>
+__device__ __forceinline__ Pack<T, V> load_chunk(const T* row, int j, int d) {            // columns j .. of a row
+  if constexpr (SHIFT) {
+    if (j < 0 || j + V > d) {
+      Pack<T, V> r;
+      zero_pack(r);
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (j + k >= 0 && j + k < d) put_element<T, V>(r, k, load_pack<T, 1>(row + j + k).w[0]);
+      return r;
+    }
+  }
+  return stream_pack<T, V>(row + j);
+}
+template <typename T, int V, bool SHIFT>
+__device__ __forceinline__ void store_chunk(T* row, int j, int d, const Pack<T, V>& r) {
+  if constexpr (SHIFT) {
+    if (j < 0 || j + V > d) {
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        if (j + k >= 0 && j + k < d) {
+          Pack<T, 1> one;
+          if constexpr (sizeof(T) == 4) one.w[0] = r.w[k];
+          else one.w[0] = (k & 1) ? r.w[k >> 1] >> 16 : r.w[k >> 1];
+          store_pack(row + j + k, one);
+        }
+      return;
+    }
+  }
+  store_pack(row + j, r);
+}
+// Whether all of a chunk's columns are in the row; otherwise which.
+template <int V, bool SHIFT>
+__device__ __forceinline__ bool is_whole(int j, int d) { return !SHIFT || (j >= 0 && j + V <= d); }
+__device__ __forceinline__ bool has_column(int j, int k, int d) { return j + k >= 0 && j + k < d; }
 
-// A group of `group` threads (a power of two, 32 or more) per row, NV chunks of V elements per thread: chunk i of a thread is the
-// row's chunk i * group + thread, so a warp's accesses are contiguous.  Mean and squared deviations are formed about each warp's
-// own mean (two passes over registers) and merged over the warps pairwise-exactly, M2 = sum M2_w + n_w (mu_w - mu)^2: the accuracy
-// of two passes with one barrier.
-template <typename X, typename Y, int V, int NV, bool CENTER>
-__global__ void __launch_bounds__(1024) ln_fwd_kernel(FwdParams a, int group) {
-  __shared__ float s_mean[32], s_m2[32], s_cnt[32];
-  const int lane = threadIdx.x & 31, g = threadIdx.x / group, tid = threadIdx.x - g * group;
-  const int64_t t = (int64_t)blockIdx.x * (blockDim.x / group) + g;
-  const bool here = t < a.T, live = here && (!a.mask || a.mask[t] != 0);
-  float f[NV * V];
-  int count = 0;
-  float sum = 0.0f;
+// Rows with another shift than the tensors without a pitch: through shared memory, as they are in memory, and out again by column.
+// Called by all threads of the row's group; the barrier is the caller's.
+template <typename T, int V, int NV>
+__device__ __forceinline__ void stage_row(const T* row, int shift, int d, T* s_row, int tid, int threads) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int64_t c = (int64_t)(i * group + tid) * V;
-    const bool in = live && c < a.d;
-    Pack<X, V> p, r;
-    zero_pack(p);
-    zero_pack(r);
-    if (in) {
-      p = load_pack<X, V>(static_cast<const X*>(a.x) + t * a.ldx + c);
-      if (a.residual) r = load_pack<X, V>(static_cast<const X*>(a.residual) + t * a.d + c);
-    }
-#pragma unroll
-    for (int k = 0; k < V; ++k) f[i * V + k] = element(p, k);
-    if (a.residual && here && c < a.d) {
-#pragma unroll
-      for (int k = 0; k < V; ++k) f[i * V + k] += element(r, k);
-      const Pack<X, V> q = round_pack<X, V>(f + i * V);
-      store_pack(static_cast<X*>(a.h) + t * a.d + c, q);
-#pragma unroll
-      for (int k = 0; k < V; ++k) f[i * V + k] = element(q, k);
-    }
-    if (CENTER) {
-      count += __popc(__ballot_sync(0xffffffffu, in)) * V;
-#pragma unroll
-      for (int k = 0; k < V; ++k) sum += f[i * V + k];
-    }
+  for (int i = 0; i <= NV; ++i) {                     // (another shift may have one chunk more)
+    const int j = (i * threads + tid) * V - shift;
+    if (j < d) store_pack(s_row + j + shift, load_chunk<T, V, true>(row, j, d));
   }
-  float mu = 0.0f;
-  if (CENTER) {
-    sum = warp_sum(sum);
-    mu = count ? sum / (float)count : 0.0f;
+}
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> staged_chunk(const T* s_row, int shift, int j, int d) {
+  Pack<T, V> r;
+  zero_pack(r);
+  if (is_whole<V, true>(j, d)) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) put_element<T, V>(r, k, load_pack<T, 1>(s_row + j + k + shift).w[0]);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (has_column(j, k, d)) put_element<T, V>(r, k, load_pack<T, 1>(s_row + j + k + shift).w[0]);
   }
-  float m2 = 0.0f;
+  return r;
+}
+
+// V values to fp32 or bf16 rows.
+template <int V, bool SHIFT>
+__device__ __forceinline__ void store_values(void* base, bool bf16, int64_t row, int j, int d, const float* f) {
+  if (bf16) store_chunk<__nv_bfloat16, V, SHIFT>(static_cast<__nv_bfloat16*>(base) + row, j, d, round_pack<__nv_bfloat16, V>(f));
+  else store_chunk<float, V, SHIFT>(static_cast<float*>(base) + row, j, d, round_pack<float, V>(f));
+}
+
+// Weight and bias by column in shared memory (SHIFT, where a chunk's columns are not aligned in them): one place in V + 1 is left out, so
+// that threads V columns apart do not meet on a bank.
+template <int V>
+__device__ __forceinline__ int spread(int j) { return j + j / V; }
+
+// Mean and squared deviations of a row from those of its warps, each about a point near its own mean: M2 = sum M2_w + n_w (near_w - mu)^2,
+// up to the square of what a point is off its warp's mean by, some 2^-23 of it.  The accuracy of two passes, with one barrier.
+struct WarpStats { float sum, m2, near, count; };
+
+constexpr int kFwdBlocks = 6;
+constexpr int kSpreadMost = 8192;         // longest row whose weights are kept in shared memory
+
+template <typename X, int NV, int MOST, bool SHIFT, bool CENTER, bool RES>
+__global__ void __launch_bounds__(MOST, MOST == 128 ? (RES ? 5 : kFwdBlocks) : 1) ln_fwd_kernel(FwdParams a, int span) {
+  constexpr int V = 16 / (int)sizeof(X), P = V / 2;
+  // The row stays in registers as fp32 values, or as it is in memory: with both inputs of the next row on their way there is no room for
+  // the values (their loads would be put off; 24 000 rows of 4096 with a residual: 155 and 12X us).
+  constexpr bool PACKED = RES && sizeof(X) == 2;
+  __shared__ WarpStats s_stats[2][32];
+  extern __shared__ __align__(16) char s_raw[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
+  const int d = a.d;
+  const float inv_d = 1.0f / (float)d;
+  const int64_t t0 = (int64_t)blockIdx.x * span;
+  const int rows = (int)(a.T - t0 < span ? a.T - t0 : span);
+  const uint32_t live_rows = __ballot_sync(0xffffffffu, lane < rows && (!a.mask || a.mask[t0 + (lane < rows ? lane : 0)] != 0));
+  const bool staged = SHIFT && a.ldx % V != d % V && a.T > 1;
+  const bool spread_out = SHIFT && d <= kSpreadMost;
+  float2* const s_wb = reinterpret_cast<float2*>(s_raw);
+  X* const s_row = reinterpret_cast<X*>(s_raw + (spread_out ? align16(8 * (spread<V>(d) + 1)) : 0));
+
+  Pack<X, V> next[NV], pr[RES ? NV : 1];
+  auto shift_of = [&](int64_t t) { return SHIFT ? (int)((t * d) % V) : 0; };
+  auto column = [&](int shift, int i) { return (i * threads + tid) * V - shift; };
+  auto fetch = [&](int r) {                            // the row's inputs, in flight while another one is worked on
+    if (!(live_rows >> r & 1)) return;
+    const int64_t t = t0 + r;
+    const int shift = shift_of(t);
+    const X *const x = static_cast<const X*>(a.x) + t * a.ldx, *const res = static_cast<const X*>(a.residual) + t * d;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    if (!CENTER || (int64_t)(i * group + tid) * V < a.d) {      // (beyond the row f is 0)
+    for (int i = 0; i < NV; ++i) {
+      const int j = column(shift, i);
+      if (j >= d) continue;
+      if (!staged) next[i] = load_chunk<X, V, SHIFT>(x, j, d);
+      if (RES) pr[i] = load_chunk<X, V, SHIFT>(res, j, d);
+    }
+  };
+  fetch(0);
+  int count = 0;                                       // columns of this warp; where rows are shifted it is counted in each
+  if (CENTER && !SHIFT) {
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const float c = f[i * V + k] - mu;
-        m2 = fmaf(c, c, m2);
+    for (int i = 0; i < NV; ++i) count += column(0, i) < d ? V : 0;
+    count = __reduce_add_sync(0xffffffffu, count);
+  }
+  if (spread_out) {
+    for (int j = tid * V; j < d; j += threads * V) {
+      float w[V], b[V];
+      if (j + V <= d) {
+        load_weights<V>(a.weight, a.w_bf16, j, 1.0f, w);
+        load_weights<V>(a.bias, a.w_bf16, j, 0.0f, b);
+#pragma unroll
+        for (int k = 0; k < V; ++k) s_wb[spread<V>(j) + k] = make_float2(w[k], b[k]);
+      } else {
+        for (int k = 0; j + k < d; ++k) {
+          load_weights<1>(a.weight, a.w_bf16, j + k, 1.0f, w);
+          load_weights<1>(a.bias, a.w_bf16, j + k, 0.0f, b);
+          s_wb[spread<V>(j) + k] = make_float2(w[0], b[0]);
+        }
       }
-    }
-  }
-  m2 = warp_sum(m2);
-  if (group > 32) {
-    if (lane == 0) {
-      s_m2[threadIdx.x >> 5] = m2;
-      if (CENTER) { s_mean[threadIdx.x >> 5] = mu; s_cnt[threadIdx.x >> 5] = (float)count; }
     }
     __syncthreads();
-    const int w0 = g * (group >> 5), nw = group >> 5;
-    m2 = 0.0f;
+  }
+#pragma unroll 1
+  for (int r = 0; r < rows; ++r) {
+    const int64_t t = t0 + r;
+    const int shift = shift_of(t);
+    X* const h = static_cast<X*>(a.h) + t * d;
+    if (!(live_rows >> r & 1)) {                       // (all threads of the block: the bits are the same in every warp)
+      float zero[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) zero[k] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int j = column(shift, i);
+        if (j >= d) continue;
+        store_values<V, SHIFT>(a.y, a.y_bf16, t * d, j, d, zero);
+        if (RES) store_chunk<X, V, SHIFT>(h, j, d, round_pack<X, V>(zero));
+      }
+      if (tid == 0) {
+        if (CENTER && a.mean) a.mean[t] = 0.0f;
+        if (a.rstd) a.rstd[t] = 0.0f;
+      }
+      if (r + 1 < rows) fetch(r + 1);
+      continue;
+    }
+    if (staged) {
+      const int own = (int)((t * a.ldx) % V);
+      stage_row<X, V, NV>(static_cast<const X*>(a.x) + t * a.ldx, own, d, s_row, tid, threads);
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int j = column(shift, i);
+        if (j < d) next[i] = staged_chunk<X, V>(s_row, own, j, d);
+      }
+    }
+    float2 f[PACKED ? 1 : NV * P] = {}, part = both(0.0f);
+    Pack<X, V> now[PACKED ? NV : 1] = {};
+    auto value = [&](int i, int p) {
+      if constexpr (PACKED) return pair_of(now[i], p);
+      else return f[i * P + p];
+    };
+    if (CENTER && SHIFT) count = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = column(shift, i);
+      if (j < d) {
+        if (RES) {
+          float2 both_in[P];
+#pragma unroll
+          for (int p = 0; p < P; ++p) both_in[p] = add2(pair_of(next[i], p), pair_of(pr[i], p));
+          next[i] = round_pack<X, V>(&both_in[0].x);
+          store_chunk<X, V, SHIFT>(h, j, d, next[i]);
+        }
+        if constexpr (PACKED) now[i] = next[i];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          if constexpr (!PACKED) f[i * P + p] = pair_of(next[i], p);
+          if (CENTER) part = add2(part, value(i, p));                                   // (0 where there is no column)
+        }
+        if (CENTER && SHIFT) count += min(j + V, d) - max(j, 0);
+      } else {
+        if constexpr (PACKED) zero_pack(now[i]);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+          if constexpr (!PACKED) f[i * P + p] = both(0.0f);
+      }
+    }
+    if (r + 1 < rows) fetch(r + 1);
+    float sum = 0.0f, mu = 0.0f;
     if (CENTER) {
-      float all = 0.0f;
-      for (int w = 0; w < nw; ++w) all = fmaf(s_cnt[w0 + w], s_mean[w0 + w], all);
-      mu = all / (float)a.d;
-      for (int w = 0; w < nw; ++w) {
-        const float c = s_mean[w0 + w] - mu;
-        m2 += fmaf(s_cnt[w0 + w] * c, c, s_m2[w0 + w]);
+      sum = warp_sum(part.x + part.y);
+      if (SHIFT) count = __reduce_add_sync(0xffffffffu, count);
+      mu = count ? __fdividef(sum, (float)count) : 0.0f;      // any point near the mean serves to measure the deviations from
+    }
+    part = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = column(shift, i);
+      if (CENTER && j >= d) continue;
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        float2 c = CENTER ? add2(value(i, p), both(-mu)) : value(i, p);
+        if (CENTER && !is_whole<V, SHIFT>(j, d)) {
+          if (!has_column(j, 2 * p, d)) c.x = 0.0f;
+          if (!has_column(j, 2 * p + 1, d)) c.y = 0.0f;
+        }
+        part = fma2(c, c, part);
+      }
+    }
+    float m2 = warp_sum(part.x + part.y);
+    if (warps > 1) {
+      WarpStats* const st = s_stats[r & 1];
+      if (lane == 0) st[warp] = WarpStats{sum, m2, mu, (float)count};
+      __syncthreads();
+      m2 = 0.0f;
+      if (CENTER) {
+        sum = 0.0f;
+        for (int w = 0; w < warps; ++w) sum += st[w].sum;
+        mu = sum * inv_d;
+        for (int w = 0; w < warps; ++w) {
+          const float c = st[w].near - mu;
+          m2 += fmaf(st[w].count * c, c, st[w].m2);
+        }
+      } else {
+        for (int w = 0; w < warps; ++w) m2 += st[w].m2;
       }
     } else {
-      for (int w = 0; w < nw; ++w) m2 += s_m2[w0 + w];
+      if (CENTER) {
+        const float c = sum * inv_d - mu;
+        mu = sum * inv_d;
+        m2 = fmaf((float)count * c, c, m2);
+      }
+      if (staged) __syncwarp();
     }
-  }
-  if (!here) return;
-  const float var = m2 / (float)a.d;
-  const float rstd = live ? 1.0f / sqrtf(var + a.eps) : 0.0f;
-  if (tid == 0) {
-    if (CENTER && a.mean) a.mean[t] = live ? mu : 0.0f;
-    if (a.rstd) a.rstd[t] = rstd;
-    if (live && !(var < INFINITY)) flag(a.d_status, SPO_DEV_NONFINITE);
-  }
+    const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps), drop = -mu * rstd;
+    if (tid == 0) {
+      if (CENTER && a.mean) a.mean[t] = mu;
+      if (a.rstd) a.rstd[t] = rstd;
+      if (!(var < INFINITY)) flag(a.d_status, SPO_DEV_NONFINITE);
+    }
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int64_t c = (int64_t)(i * group + tid) * V;
-    if (c < a.d) {
-      float w[V], b[V];
-      load_weights<V>(a.weight, a.w_bf16, c, 1.0f, w);
-      load_weights<V>(a.bias, a.w_bf16, c, 0.0f, b);
+    for (int i = 0; i < NV; ++i) {
+      const int j = column(shift, i);
+      if (j >= d) continue;
+      float2 w[P], b[P];
+      if (!SHIFT) {
+        load_weights<V>(a.weight, a.w_bf16, j, 1.0f, &w[0].x);
+        load_weights<V>(a.bias, a.w_bf16, j, 0.0f, &b[0].x);
+      } else if (spread_out && is_whole<V, SHIFT>(j, d)) {
+        const int at = spread<V>(j), first = V - j % V;  // V columns from j on: a place is skipped behind the first multiple of V
 #pragma unroll
-      for (int k = 0; k < V; ++k) w[k] = live ? fmaf((f[i * V + k] - mu) * rstd, w[k], b[k]) : 0.0f;
-      store_pack(static_cast<Y*>(a.y) + t * a.d + c, round_pack<Y, V>(w));
+        for (int p = 0; p < P; ++p) {
+          const float2 q0 = s_wb[at + 2 * p + (2 * p >= first)], q1 = s_wb[at + 2 * p + 1 + (2 * p + 1 >= first)];
+          w[p] = make_float2(q0.x, q1.x);
+          b[p] = make_float2(q0.y, q1.y);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const int c = has_column(j, k, d) ? j + k : 0;
+          load_weights<1>(a.weight, a.w_bf16, c, 1.0f, &w[0].x + k);
+          load_weights<1>(a.bias, a.w_bf16, c, 0.0f, &b[0].x + k);
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const float2 xh = CENTER ? fma2(value(i, p), both(rstd), both(drop)) : mul2(value(i, p), both(rstd));
+        w[p] = fma2(xh, w[p], b[p]);
+      }
+      store_values<V, SHIFT>(a.y, a.y_bf16, t * d, j, d, &w[0].x);
     }
   }
 }
 
 // Rows longer than a block's registers hold: the row is read again for each of the three passes.
-template <typename X, typename Y, bool CENTER>
+template <typename X, bool CENTER>
 __global__ void __launch_bounds__(1024) ln_fwd_long_kernel(FwdParams a) {
   __shared__ float s_part[32];
   const int64_t t = blockIdx.x;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
   const bool live = !a.mask || a.mask[t] != 0;
   const X* row = static_cast<const X*>(a.x) + t * a.ldx;
-  Y* y = static_cast<Y*>(a.y) + t * a.d;
   if (a.residual) {
     const X* r = static_cast<const X*>(a.residual) + t * a.d;
     X* h = static_cast<X*>(a.h) + t * a.d;
@@ -292,7 +520,7 @@ __global__ void __launch_bounds__(1024) ln_fwd_long_kernel(FwdParams a) {
       load_weights<1>(a.bias, a.w_bf16, c, 0.0f, &b);
       v = fmaf((element(load_pack<X, 1>(row + c), 0) - mu) * rstd, w, b);
     }
-    store_pack(y + c, round_pack<Y, 1>(&v));
+    store_values<1, false>(a.y, a.y_bf16, t * a.d, c, a.d, &v);
   }
 }
 
@@ -303,30 +531,52 @@ int group_of(int64_t chunks, int nv) {
   return (int)(g > 2048 ? 2048 : g);
 }
 
-template <typename X, typename Y, int V, int NV, bool CENTER>
-cudaError_t run_fwd(const FwdParams& a, cudaStream_t st) {
-  const int group = group_of(ceil_div(a.d, V), NV);
-  const int threads = group > kFwdThreads ? group : kFwdThreads;
-  ln_fwd_kernel<X, Y, V, NV, CENTER><<<(unsigned)ceil_div(a.T, threads / group), threads, 0, st>>>(a, group);
+constexpr int kFwdThreadsPerSm = 640;     // that fit with their registers
+constexpr int kFwdSpanMost = 4, kFwdSpanShift = 12, kFwdRounds = 3;
+
+template <typename X, int NV, int MOST, bool SHIFT, bool CENTER, bool RES>
+cudaError_t run_fwd(const FwdParams& a, int64_t chunks, cudaStream_t st) {
+  constexpr int V = 16 / (int)sizeof(X);
+  const auto kernel = ln_fwd_kernel<X, NV, MOST, SHIFT, CENTER, RES>;
+  const int threads = (int)align_up((size_t)ceil_div(chunks, NV), 32);
+  const int64_t at_once = (int64_t)sm_count() * (threads >= kFwdThreadsPerSm ? 1 : kFwdThreadsPerSm / threads);
+  int64_t span = a.T / (at_once * kFwdRounds);
+  const int64_t most = SHIFT ? kFwdSpanShift : kFwdSpanMost;
+  span = span < 1 ? 1 : span > most ? most : span;
+  int smem = 0;
+  if (SHIFT) {
+    if (a.d <= kSpreadMost) smem += align16(8 * (a.d + a.d / V + 1));
+    if (a.T > 1 && a.ldx % V != a.d % V) smem += align16((int)sizeof(X) * (a.d + 2 * V));
+    if (smem > 32 * 1024) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+      if (e != cudaSuccess) return e;
+    }
+  }
+  kernel<<<(unsigned)ceil_div(a.T, span), threads, smem, st>>>(a, (int)span);
   return cudaGetLastError();
 }
 
-template <typename X, typename Y, bool CENTER>
+template <typename X, bool CENTER, bool RES>
 cudaError_t pick_fwd(const FwdParams& a, cudaStream_t st) {
-  constexpr int V = 16 / (int)sizeof(X), kMost = 32 / V;          // 32 elements a thread at most
-  const bool aligned = a.d % V == 0 && (a.T == 1 || a.ldx % V == 0);
-  if (aligned && ceil_div(a.d, V) <= 1024 * kMost) {
-    const int64_t chunks = a.d / V;
-    if (chunks <= 32) return run_fwd<X, Y, V, 1, CENTER>(a, st);
-    if (chunks <= 256 * kMost / 2) return run_fwd<X, Y, V, kMost / 2, CENTER>(a, st);
-    return run_fwd<X, Y, V, kMost, CENTER>(a, st);
+  constexpr int V = 16 / (int)sizeof(X);
+  const bool shift = !(a.d % V == 0 && (a.T == 1 || a.ldx % V == 0));
+  const int64_t chunks = shift ? ceil_div(a.d + V - 1, V) : a.d / V;
+  if (chunks > 4 * 1024) {
+    ln_fwd_long_kernel<X, CENTER><<<(unsigned)a.T, 1024, 0, st>>>(a);
+    return cudaGetLastError();
   }
-  if (!aligned && a.d <= 1024 * 32) {
-    if (a.d <= 256 * 8) return run_fwd<X, Y, 1, 8, CENTER>(a, st);
-    return run_fwd<X, Y, 1, 32, CENTER>(a, st);
-  }
-  ln_fwd_long_kernel<X, Y, CENTER><<<(unsigned)a.T, 1024, 0, st>>>(a);
-  return cudaGetLastError();
+  // One warp with one chunk a thread for short rows; up to 128 threads with four chunks, whose registers leave room for five blocks an SM;
+  // then as many threads as two chunks (at last four) a thread need.  Where there are fewer rows than SMs, as many threads as there
+  // are chunks: one row of 4096 takes 2.9 us so and 3.4 on 128 threads.
+  auto form = [&](auto sh) {
+    constexpr bool S = decltype(sh)::value;
+    if (chunks <= 32) return run_fwd<X, 1, 128, S, CENTER, RES>(a, chunks, st);
+    if (chunks <= 1024 && a.T <= sm_count()) return run_fwd<X, 1, 1024, S, CENTER, RES>(a, chunks, st);
+    if (chunks <= 4 * 128) return run_fwd<X, 4, 128, S, CENTER, RES>(a, chunks, st);
+    if (chunks <= 2 * 1024) return run_fwd<X, 2, 1024, S, CENTER, RES>(a, chunks, st);
+    return run_fwd<X, 4, 1024, S, CENTER, RES>(a, chunks, st);
+  };
+  return shift ? form(std::true_type{}) : form(std::false_type{});
 }
 
 // ---------------------------------------------------------------------------
@@ -640,14 +890,15 @@ cudaError_t launch_layernorm_fwd(const LayerNormFwd& q, cudaStream_t st) {
   FwdParams a{};
   a.x = q.x; a.residual = q.residual; a.weight = q.weight; a.bias = q.bias; a.mask = q.mask; a.ldx = q.ldx; a.T = q.T; a.d = q.d;
   a.w_bf16 = q.w_dtype == SPO_DTYPE_BF16; a.eps = q.eps; a.y = q.y; a.h = q.h; a.mean = q.mean; a.rstd = q.rstd; a.d_status = q.d_status;
-  using bf = __nv_bfloat16;
-  const bool x16 = q.dtype == SPO_DTYPE_BF16, y16 = q.y_dtype == SPO_DTYPE_BF16;
-  if (q.kind == SPO_NORM_LAYER) {
-    if (x16) return y16 ? pick_fwd<bf, bf, true>(a, st) : pick_fwd<bf, float, true>(a, st);
-    return y16 ? pick_fwd<float, bf, true>(a, st) : pick_fwd<float, float, true>(a, st);
-  }
-  if (x16) return y16 ? pick_fwd<bf, bf, false>(a, st) : pick_fwd<bf, float, false>(a, st);
-  return y16 ? pick_fwd<float, bf, false>(a, st) : pick_fwd<float, float, false>(a, st);
+  a.y_bf16 = q.y_dtype == SPO_DTYPE_BF16;
+  auto typed = [&](auto center, auto res) {
+    constexpr bool C = decltype(center)::value, R = decltype(res)::value;
+    return q.dtype == SPO_DTYPE_BF16 ? pick_fwd<__nv_bfloat16, C, R>(a, st) : pick_fwd<float, C, R>(a, st);
+  };
+  using yes = std::true_type;
+  using no = std::false_type;
+  if (q.kind == SPO_NORM_LAYER) return q.residual ? typed(yes{}, yes{}) : typed(yes{}, no{});
+  return q.residual ? typed(no{}, yes{}) : typed(no{}, no{});
 }
 
 cudaError_t launch_layernorm_bwd(const LayerNormBwd& q, char* ws, cudaStream_t st) {
