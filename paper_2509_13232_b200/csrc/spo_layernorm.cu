@@ -49,23 +49,13 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T* p) {
   return r;
 }
 
-// The same for rows that are read once: they leave the L1 cache to the weights, which every row wants again (24 000 rows of 4096 with a
-// residual: 155 and 12X us).
+// The same for rows that are read once: issued where it is written, and past the L1 cache.
 template <typename T, int V>
 __device__ __forceinline__ Pack<T, V> stream_pack(const T* p) {
+  static_assert(Pack<T, V>::kBytes == 16, "rows are read by 16 bytes");
   Pack<T, V> r;
-  constexpr int kBytes = Pack<T, V>::kBytes;
-  if constexpr (kBytes >= 16) {
-#pragma unroll
-    for (int i = 0; i < kBytes / 16; ++i)
-      asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(r.w[4 * i]), "=r"(r.w[4 * i + 1]), "=r"(r.w[4 * i + 2]), "=r"(r.w[4 * i + 3])
-                   : "l"(reinterpret_cast<const char*>(p) + 16 * i));
-  } else if constexpr (kBytes == 8) {
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.w[0]), "=r"(r.w[1]) : "l"(p));
-  } else {
-    r = load_pack<T, V>(p);
-  }
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "l"(p));
   return r;
 }
 
@@ -170,31 +160,22 @@ struct FwdParams {
   int32_t* d_status;
 };
 
-// Chunks.  A thread holds NV chunks of V elements (16 bytes) of a row: chunk i * threads + thread, so that a warp's accesses are
+// Chunks.  A thread holds NV chunks of V elements (16 bytes) of a row: chunk c = i * threads + thread, so that a warp's accesses are
 // contiguous.  Where rows do not begin on 16 bytes (SHIFT), chunk c has the columns V c - shift + (0 .. V - 1), shift = (t d) mod V: in the
-// tensors without a pitch it then lies on 16 bytes again, but for the columns that the first and last chunk do not have, which are
-// moved one by one.
-template <typename T, int V, bool SHIFT>
-__device__ __forceinline__ Pack<T, V> load_chunk(const T* row, int j, int d) {            // columns j .. of a row
-  if constexpr (SHIFT) {
-    if (j < 0 || j + V > d) {
-      Pack<T, V> r;
-      zero_pack(r);
-#pragma unroll
-      for (int k = 0; k < V; ++k)
-        if (j + k >= 0 && j + k < d) put_element<T, V>(r, k, load_pack<T, 1>(row + j + k).w[0]);
-      return r;
-    }
-  }
-  return stream_pack<T, V>(row + j);
-}
+// tensors without a pitch it then lies on 16 bytes again.  The first and the last chunk of such a row have columns that are the
+// neighbouring rows': they are read along (not behind the end of the last row), count as zeros, and are not written.  A block takes
+// rows of one shift only, so that its threads' columns stay the same.
+template <int V, bool SHIFT>
+__device__ __forceinline__ bool is_whole(int j, int d) { return !SHIFT || (j >= 0 && j + V <= d); }
+__device__ __forceinline__ bool has_column(int j, int k, int d) { return j + k >= 0 && j + k < d; }
+
 template <typename T, int V, bool SHIFT>
 __device__ __forceinline__ void store_chunk(T* row, int j, int d, const Pack<T, V>& r) {
   if constexpr (SHIFT) {
-    if (j < 0 || j + V > d) {
+    if (!is_whole<V, SHIFT>(j, d)) {
 #pragma unroll
       for (int k = 0; k < V; ++k)
-        if (j + k >= 0 && j + k < d) {
+        if (has_column(j, k, d)) {
           Pack<T, 1> one;
           if constexpr (sizeof(T) == 4) one.w[0] = r.w[k];
           else one.w[0] = (k & 1) ? r.w[k >> 1] >> 16 : r.w[k >> 1];
@@ -205,36 +186,6 @@ __device__ __forceinline__ void store_chunk(T* row, int j, int d, const Pack<T, 
   }
   store_pack(row + j, r);
 }
-// Whether all of a chunk's columns are in the row; otherwise which.
-template <int V, bool SHIFT>
-__device__ __forceinline__ bool is_whole(int j, int d) { return !SHIFT || (j >= 0 && j + V <= d); }
-__device__ __forceinline__ bool has_column(int j, int k, int d) { return j + k >= 0 && j + k < d; }
-
-// Rows with another shift than the tensors without a pitch: through shared memory, as they are in memory, and out again by column.
-// Called by all threads of the row's group; the barrier is the caller's.
-template <typename T, int V, int NV>
-__device__ __forceinline__ void stage_row(const T* row, int shift, int d, T* s_row, int tid, int threads) {
-#pragma unroll
-  for (int i = 0; i <= NV; ++i) {                     // (another shift may have one chunk more)
-    const int j = (i * threads + tid) * V - shift;
-    if (j < d) store_pack(s_row + j + shift, load_chunk<T, V, true>(row, j, d));
-  }
-}
-template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> staged_chunk(const T* s_row, int shift, int j, int d) {
-  Pack<T, V> r;
-  zero_pack(r);
-  if (is_whole<V, true>(j, d)) {
-#pragma unroll
-    for (int k = 0; k < V; ++k) put_element<T, V>(r, k, load_pack<T, 1>(s_row + j + k + shift).w[0]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < V; ++k)
-      if (has_column(j, k, d)) put_element<T, V>(r, k, load_pack<T, 1>(s_row + j + k + shift).w[0]);
-  }
-  return r;
-}
-
 // V values to fp32 or bf16 rows.
 template <int V, bool SHIFT>
 __device__ __forceinline__ void store_values(void* base, bool bf16, int64_t row, int j, int d, const float* f) {
@@ -242,82 +193,198 @@ __device__ __forceinline__ void store_values(void* base, bool bf16, int64_t row,
   else store_chunk<float, V, SHIFT>(static_cast<float*>(base) + row, j, d, round_pack<float, V>(f));
 }
 
-// Weight and bias by column in shared memory (SHIFT, where a chunk's columns are not aligned in them): one place in V + 1 is left out, so
-// that threads V columns apart do not meet on a bank.
+// Rows come through a ring in shared memory: a thread copies its own chunks there, one or two rows ahead, and reads them itself, so that
+// rows on their way take no registers and no barrier.
+// The first `bytes` come from memory, the rest are zeros.
+__device__ __forceinline__ void copy16(void* s, const void* g, int bytes = 16) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(s)), "l"(g), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy8(void* s, const void* g, int bytes = 8) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(s)), "l"(g), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the newest `newer` groups of this thread's copies have arrived.
+__device__ __forceinline__ void copies_arrived(int newer) {
+  if (newer >= 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else if (newer == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+template <typename T, int V, bool SHIFT>
+__device__ __forceinline__ void copy_chunk(char* s, const T* row, int j, int end) {
+  constexpr int kSize = V * (int)sizeof(T);
+  const int there = SHIFT ? min(end - j, V) * (int)sizeof(T) : kSize;           // bytes up to the end of the tensor
+  if constexpr (kSize == 8) {
+    copy8(s, row + j, there);
+  } else {
+#pragma unroll
+    for (int o = 0; o < kSize; o += 16) {
+      const int left = max(min(there - o, 16), 0);
+      copy16(s + o, reinterpret_cast<const char*>(row + j) + (left > 0 ? o : 0), left);
+    }
+  }
+}
+// Elements from the beginning of row t to the end of the tensor, behind which nothing is read.
+__device__ __forceinline__ int end_of(int64_t T, int64_t t, int64_t ld, int d) {
+  const int64_t n = (T - 1 - t) * ld + d;
+  return n < (1 << 30) ? (int)n : 1 << 30;
+}
+// The first and the last chunk of a row, as far as they are this thread's and have columns of a neighbouring row; otherwise -1.
 template <int V>
-__device__ __forceinline__ int spread(int j) { return j + j / V; }
+__device__ __forceinline__ int2 edge_chunks(int shift, int d, int tid, int threads) {
+  const int last = (d + shift - 1) / V;
+  return make_int2(tid == 0 && shift > 0 ? 0 : -1, last % threads == tid && (d + shift) % V != 0 && (last > 0 || shift == 0) ? last : -1);
+}
+// Zeros for the columns of a copied chunk that are not the row's.
+template <typename T, int V>
+__device__ __forceinline__ void blank(char* s, int j, int d) {
+#pragma unroll 1
+  for (int k = 0; k < V; ++k) {
+    Pack<T, 1> zero;
+    zero.w[0] = 0;
+    if (!has_column(j, k, d)) store_pack(reinterpret_cast<T*>(s) + k, zero);
+  }
+}
+// Columns j .. of a row that lies at s_row with its own shift.
+template <typename T, int V>
+__device__ __forceinline__ Pack<T, V> staged_chunk(const T* s_row, int j, int d) {
+  Pack<T, V> r;
+  zero_pack(r);
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+    if (has_column(j, k, d)) put_element<T, V>(r, k, load_pack<T, 1>(s_row + j + k).w[0]);
+  return r;
+}
+
+// A vector of weights (or biases) in shared memory as fp32, by chunk: quarter q of chunk c at q held + c.
+template <int V>
+__device__ __forceinline__ void spread_weights(float4* s, const void* p, int bf16, float none, int held, int c, int j, int d) {
+  float w[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    w[k] = 0.0f;
+    if (has_column(j, k, d)) load_weights<1>(p, bf16, j + k, none, w + k);
+  }
+#pragma unroll
+  for (int q = 0; q < V / 4; ++q) s[q * held + c] = make_float4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+}
+template <int V>
+__device__ __forceinline__ void chunk_weights(const float4* s, int held, int c, float2* w) {
+#pragma unroll
+  for (int q = 0; q < V / 4; ++q) {
+    const float4 v = s[q * held + c];
+    w[2 * q] = make_float2(v.x, v.y);
+    w[2 * q + 1] = make_float2(v.z, v.w);
+  }
+}
+
+constexpr int kRowMost = 16384;           // elements of a row that a block's registers hold
+constexpr int kSharedMost = 228 * 1024;   // of an SM, for the blocks that run on it,
+constexpr int kSharedOwn = 2304;          // with what each of them has besides its ring and weights
+
+int shifts_of(int32_t d, int v) {         // shifts that rows of d elements have
+  int n = 1;
+  while (n < v && (int64_t)n * d % v != 0) n *= 2;
+  return n;
+}
+// Chunks a thread holds in the backward pass: one in a single warp, or 32 elements on up to 128 threads, or 16.
+int row_form(int64_t chunks, int v) { return chunks <= 32 ? 1 : chunks * v <= 32 * 128 ? 32 / v : 16 / v; }
+int row_threads(int64_t chunks, int nv) { return (int)align_up((size_t)ceil_div(chunks, nv), 32); }
+// Blocks on an SM and rows in the ring: three rows where as many blocks still fit as the registers allow, two otherwise, and for the longest
+// rows one.
+struct RowPlan { int per_sm, stages; };
+RowPlan plan_rows(int per_sm, int fixed, int stage) {
+  RowPlan p{per_sm, 3};
+  auto fits = [&] { return p.per_sm * (fixed + p.stages * stage + kSharedOwn) <= kSharedMost; };
+  while (p.stages > 2 && !fits()) --p.stages;
+  while (p.per_sm > 1 && !fits()) --p.per_sm;
+  while (p.stages > 1 && !fits()) --p.stages;
+  if (p.stages == 2 && p.per_sm * (fixed + 3 * stage + kSharedOwn) <= kSharedMost) p.stages = 3;
+  return p;
+}
+template <class Kernel>
+cudaError_t allow_shared(Kernel kernel, int bytes) {
+  return bytes <= 32 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
 
 // Mean and squared deviations of a row from those of its warps, each about a point near its own mean: M2 = sum M2_w + n_w (near_w - mu)^2,
 // up to the square of what a point is off its warp's mean by, some 2^-23 of it.  The accuracy of two passes, with one barrier.
 struct WarpStats { float sum, m2, near, count; };
 
-constexpr int kFwdBlocks = 6;
-constexpr int kSpreadMost = 8192;         // longest row whose weights are kept in shared memory
+// From each warp's to the row's: mu becomes the mean, m2 the squared deviations from it.  (Also the barrier between the row's reads of the
+// ring and the copies that follow.)
+template <bool CENTER, int WARPS>
+__device__ __forceinline__ void merge_warps(WarpStats* st, int lane, int warp, int warps, float sum, float& m2, float& mu, int count,
+                                            float inv_d) {
+  if (warps == 1) {
+    if (CENTER) {
+      const float c = sum * inv_d - mu;
+      mu = sum * inv_d;
+      m2 = fmaf((float)count * c, c, m2);
+    }
+    __syncwarp();
+    return;
+  }
+  if (lane == 0) st[warp] = WarpStats{sum, m2, mu, (float)count};
+  __syncthreads();
+  m2 = 0.0f;
+  sum = 0.0f;
+  if (CENTER) {
+#pragma unroll 4
+    for (int w = 0; w < warps; ++w) sum += st[w].sum;
+    mu = sum * inv_d;
+  }
+#pragma unroll 4
+  for (int w = 0; w < warps; ++w) {
+    const WarpStats q = st[w];
+    if (CENTER) {
+      const float c = q.near - mu;
+      m2 += fmaf(q.count * c, c, q.m2);
+    } else {
+      m2 += q.m2;
+    }
+  }
+}
 
-template <typename X, int NV, int MOST, bool SHIFT, bool CENTER, bool RES>
-__global__ void __launch_bounds__(MOST, MOST == 128 ? (RES ? 5 : kFwdBlocks) : 1) ln_fwd_kernel(FwdParams a, int span) {
+// Rows that begin on 16 bytes.  A block takes `span` rows in a row; the next row's inputs are on their way to registers while one is worked
+// on.  (Through the ring 5 to 15 % slower: 24 000 rows of 4096 with a residual 125 and 132 us, without 72 and 77.)
+template <typename X, int NV, int MOST, int LEAST, bool CENTER, bool RES>
+__global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int span) {
   constexpr int V = 16 / (int)sizeof(X), P = V / 2;
   // The row stays in registers as fp32 values, or as it is in memory: with both inputs of the next row on their way there is no room for
-  // the values (their loads would be put off; 24 000 rows of 4096 with a residual: 155 and 12X us).
+  // the values (their loads would be put off; 24 000 rows of 4096 with a residual: 155 and 125 us).
   constexpr bool PACKED = RES && sizeof(X) == 2;
   __shared__ WarpStats s_stats[2][32];
-  extern __shared__ __align__(16) char s_raw[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const int d = a.d;
   const float inv_d = 1.0f / (float)d;
   const int64_t t0 = (int64_t)blockIdx.x * span;
   const int rows = (int)(a.T - t0 < span ? a.T - t0 : span);
   const uint32_t live_rows = __ballot_sync(0xffffffffu, lane < rows && (!a.mask || a.mask[t0 + (lane < rows ? lane : 0)] != 0));
-  const bool staged = SHIFT && a.ldx % V != d % V && a.T > 1;
-  const bool spread_out = SHIFT && d <= kSpreadMost;
-  float2* const s_wb = reinterpret_cast<float2*>(s_raw);
-  X* const s_row = reinterpret_cast<X*>(s_raw + (spread_out ? align16(8 * (spread<V>(d) + 1)) : 0));
-
   Pack<X, V> next[NV], pr[RES ? NV : 1];
-  auto shift_of = [&](int64_t t) { return SHIFT ? (int)((t * d) % V) : 0; };
-  auto column = [&](int shift, int i) { return (i * threads + tid) * V - shift; };
-  auto fetch = [&](int r) {                            // the row's inputs, in flight while another one is worked on
+  auto column = [&](int i) { return (i * threads + tid) * V; };
+  auto fetch = [&](int r) {
     if (!(live_rows >> r & 1)) return;
     const int64_t t = t0 + r;
-    const int shift = shift_of(t);
     const X *const x = static_cast<const X*>(a.x) + t * a.ldx, *const res = static_cast<const X*>(a.residual) + t * d;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = column(shift, i);
+      const int j = column(i);
       if (j >= d) continue;
-      if (!staged) next[i] = load_chunk<X, V, SHIFT>(x, j, d);
-      if (RES) pr[i] = load_chunk<X, V, SHIFT>(res, j, d);
+      next[i] = stream_pack<X, V>(x + j);
+      if (RES) pr[i] = stream_pack<X, V>(res + j);
     }
   };
   fetch(0);
-  int count = 0;                                       // columns of this warp; where rows are shifted it is counted in each
-  if (CENTER && !SHIFT) {
+  int count = 0;                                       // columns of this warp
+  if (CENTER) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) count += column(0, i) < d ? V : 0;
+    for (int i = 0; i < NV; ++i) count += column(i) < d ? V : 0;
     count = __reduce_add_sync(0xffffffffu, count);
   }
-  if (spread_out) {
-    for (int j = tid * V; j < d; j += threads * V) {
-      float w[V], b[V];
-      if (j + V <= d) {
-        load_weights<V>(a.weight, a.w_bf16, j, 1.0f, w);
-        load_weights<V>(a.bias, a.w_bf16, j, 0.0f, b);
-#pragma unroll
-        for (int k = 0; k < V; ++k) s_wb[spread<V>(j) + k] = make_float2(w[k], b[k]);
-      } else {
-        for (int k = 0; j + k < d; ++k) {
-          load_weights<1>(a.weight, a.w_bf16, j + k, 1.0f, w);
-          load_weights<1>(a.bias, a.w_bf16, j + k, 0.0f, b);
-          s_wb[spread<V>(j) + k] = make_float2(w[0], b[0]);
-        }
-      }
-    }
-    __syncthreads();
-  }
+  const float inv_count = count ? 1.0f / (float)count : 0.0f;
 #pragma unroll 1
   for (int r = 0; r < rows; ++r) {
     const int64_t t = t0 + r;
-    const int shift = shift_of(t);
     X* const h = static_cast<X*>(a.h) + t * d;
     if (!(live_rows >> r & 1)) {                       // (all threads of the block: the bits are the same in every warp)
       float zero[V];
@@ -325,10 +392,10 @@ __global__ void __launch_bounds__(MOST, MOST == 128 ? (RES ? 5 : kFwdBlocks) : 1
       for (int k = 0; k < V; ++k) zero[k] = 0.0f;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int j = column(shift, i);
+        const int j = column(i);
         if (j >= d) continue;
-        store_values<V, SHIFT>(a.y, a.y_bf16, t * d, j, d, zero);
-        if (RES) store_chunk<X, V, SHIFT>(h, j, d, round_pack<X, V>(zero));
+        store_values<V, false>(a.y, a.y_bf16, t * d, j, d, zero);
+        if (RES) store_pack(h + j, round_pack<X, V>(zero));
       }
       if (tid == 0) {
         if (CENTER && a.mean) a.mean[t] = 0.0f;
@@ -337,41 +404,29 @@ __global__ void __launch_bounds__(MOST, MOST == 128 ? (RES ? 5 : kFwdBlocks) : 1
       if (r + 1 < rows) fetch(r + 1);
       continue;
     }
-    if (staged) {
-      const int own = (int)((t * a.ldx) % V);
-      stage_row<X, V, NV>(static_cast<const X*>(a.x) + t * a.ldx, own, d, s_row, tid, threads);
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int j = column(shift, i);
-        if (j < d) next[i] = staged_chunk<X, V>(s_row, own, j, d);
-      }
-    }
     float2 f[PACKED ? 1 : NV * P] = {}, part = both(0.0f);
     Pack<X, V> now[PACKED ? NV : 1] = {};
     auto value = [&](int i, int p) {
       if constexpr (PACKED) return pair_of(now[i], p);
       else return f[i * P + p];
     };
-    if (CENTER && SHIFT) count = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = column(shift, i);
+      const int j = column(i);
       if (j < d) {
         if (RES) {
-          float2 both_in[P];
+          float2 sums[P];
 #pragma unroll
-          for (int p = 0; p < P; ++p) both_in[p] = add2(pair_of(next[i], p), pair_of(pr[i], p));
-          next[i] = round_pack<X, V>(&both_in[0].x);
-          store_chunk<X, V, SHIFT>(h, j, d, next[i]);
+          for (int p = 0; p < P; ++p) sums[p] = add2(pair_of(next[i], p), pair_of(pr[i], p));
+          next[i] = round_pack<X, V>(&sums[0].x);
+          store_pack(h + j, next[i]);
         }
         if constexpr (PACKED) now[i] = next[i];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           if constexpr (!PACKED) f[i * P + p] = pair_of(next[i], p);
-          if (CENTER) part = add2(part, value(i, p));                                   // (0 where there is no column)
+          if (CENTER) part = add2(part, value(i, p));
         }
-        if (CENTER && SHIFT) count += min(j + V, d) - max(j, 0);
       } else {
         if constexpr (PACKED) zero_pack(now[i]);
 #pragma unroll
@@ -383,17 +438,172 @@ __global__ void __launch_bounds__(MOST, MOST == 128 ? (RES ? 5 : kFwdBlocks) : 1
     float sum = 0.0f, mu = 0.0f;
     if (CENTER) {
       sum = warp_sum(part.x + part.y);
-      if (SHIFT) count = __reduce_add_sync(0xffffffffu, count);
-      mu = count ? __fdividef(sum, (float)count) : 0.0f;      // any point near the mean serves to measure the deviations from
+      mu = sum * inv_count;                            // any point near the mean serves to measure the deviations from
     }
     part = both(0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = column(shift, i);
+      if (CENTER && column(i) >= d) continue;
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const float2 c = CENTER ? add2(value(i, p), both(-mu)) : value(i, p);
+        part = fma2(c, c, part);
+      }
+    }
+    float m2 = warp_sum(part.x + part.y);
+    merge_warps<CENTER, MOST / 32>(s_stats[r & 1], lane, warp, warps, sum, m2, mu, count, inv_d);
+    const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
+    if (tid == 0) {
+      if (CENTER && a.mean) a.mean[t] = mu;
+      if (a.rstd) a.rstd[t] = rstd;
+      if (!(var < INFINITY)) flag(a.d_status, SPO_DEV_NONFINITE);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = column(i);
+      if (j >= d) continue;
+      float2 w[P], b[P];
+      load_weights<V>(a.weight, a.w_bf16, j, 1.0f, &w[0].x);
+      if (a.bias) load_weights<V>(a.bias, a.w_bf16, j, 0.0f, &b[0].x);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        const float2 xh = mul2(CENTER ? add2(value(i, p), both(-mu)) : value(i, p), both(rstd));
+        w[p] = a.bias ? fma2(xh, w[p], b[p]) : mul2(xh, w[p]);
+      }
+      store_values<V, false>(a.y, a.y_bf16, t * d, j, d, &w[0].x);
+    }
+  }
+}
+
+// Rows that do not begin on 16 bytes, through the ring.  A block takes `span` rows of one shift; x rows of another shift than y's (`staged`)
+// are copied by their own chunks and read by column after a barrier.
+template <typename X, int NV, int MOST, int LEAST, bool CENTER, bool RES>
+__global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, int span, int stages, int shifts) {
+  constexpr int V = 16 / (int)sizeof(X), P = V / 2;
+  constexpr bool SHIFT = true;
+  __shared__ WarpStats s_stats[2][32];
+  extern __shared__ __align__(16) char s_raw[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
+  const int d = a.d, held = threads * NV;
+  const float inv_d = 1.0f / (float)d;
+  // rows first + k step, k < rows
+  const int64_t first = blockIdx.x % shifts + (int64_t)shifts * span * (blockIdx.x / shifts);
+  const int step = shifts;
+  const int64_t reach = (a.T - first + step - 1) / step;
+  const int rows = reach < 0 ? 0 : (int)(reach < span ? reach : span);
+  const uint32_t live_rows = __ballot_sync(0xffffffffu, lane < rows && (!a.mask || a.mask[first + (int64_t)(lane < rows ? lane : 0) * step] != 0));
+  const int shift = (int)((first * d) % V);
+  const bool staged = a.ldx % V != d % V && a.T > 1;
+  const int2 edges = edge_chunks<V>(shift, d, tid, threads);
+  float4* const s_w = reinterpret_cast<float4*>(s_raw);
+  float4* const s_b = s_w + V / 4 * held;
+  const int fixed = held * V * 4 * (a.bias ? 2 : 1), x_bytes = held * 16 + 16;
+  const int stage = x_bytes + (RES ? held * 16 : 0);
+  auto column = [&](int i) { return (i * threads + tid) * V - shift; };
+  auto fetch = [&](int r, int slot) {
+    if (r < rows && (live_rows >> r & 1)) {
+      const int64_t t = first + (int64_t)r * step;
+      char* const s = s_raw + fixed + slot * stage;
+      const X *const x = static_cast<const X*>(a.x) + t * a.ldx, *const res = static_cast<const X*>(a.residual) + t * d;
+      const int own = staged ? (int)((t * a.ldx) % V) : shift;
+      const int end_x = end_of(a.T, t, a.ldx, d), end = end_of(a.T, t, d, d);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = i * threads + tid, j = c * V - shift, jx = c * V - own;
+        if (jx < d) copy_chunk<X, V, SHIFT>(s + c * 16, x, jx, end_x);
+        if (RES && j < d) copy_chunk<X, V, SHIFT>(s + x_bytes + c * 16, res, j, end);
+      }
+    }
+    copies_issued();
+  };
+  for (int k = 0; k < stages - 1; ++k) fetch(k, k);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = i * threads + tid;
+    spread_weights<V>(s_w, a.weight, a.w_bf16, 1.0f, held, c, column(i), d);
+    if (a.bias) spread_weights<V>(s_b, a.bias, a.w_bf16, 0.0f, held, c, column(i), d);
+  }
+  int count = 0;                                       // columns of this warp
+  if (CENTER) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (column(i) < d) count += min(column(i) + V, d) - max(column(i), 0);
+    count = __reduce_add_sync(0xffffffffu, count);
+  }
+  const float inv_count = count ? 1.0f / (float)count : 0.0f;
+  int slot = 0;
+#pragma unroll 1
+  for (int k = 0; k < rows; ++k) {
+    const int64_t t = first + (int64_t)k * step;
+    char* const s = s_raw + fixed + slot * stage;
+    fetch(k + stages - 1, slot == 0 ? stages - 1 : slot - 1);
+    slot = slot + 1 == stages ? 0 : slot + 1;
+    X* const h = static_cast<X*>(a.h) + t * d;
+    copies_arrived(stages - 1);
+    if (!(live_rows >> k & 1)) {                       // (all threads of the block: the bits are the same in every warp)
+      float zero[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) zero[e] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int j = column(i);
+        if (j >= d) continue;
+        store_values<V, SHIFT>(a.y, a.y_bf16, t * d, j, d, zero);
+        if (RES) store_chunk<X, V, SHIFT>(h, j, d, round_pack<X, V>(zero));
+      }
+      if (tid == 0) {
+        if (CENTER && a.mean) a.mean[t] = 0.0f;
+        if (a.rstd) a.rstd[t] = 0.0f;
+      }
+      continue;
+    }
+    if (staged) __syncthreads();
+    for (int e = 0; e < 2; ++e) {
+      const int c = e == 0 ? edges.x : edges.y;
+      if (c < 0) continue;
+      if (!staged) blank<X, V>(s + c * 16, c * V - shift, d);
+      if (RES) blank<X, V>(s + x_bytes + c * 16, c * V - shift, d);
+    }
+    const X* const s_own = reinterpret_cast<const X*>(s) + (staged ? (int)((t * a.ldx) % V) : 0);
+    float2 f[NV * P], part = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * threads + tid, j = column(i);
+      if (j < d) {
+        Pack<X, V> q;
+        if (staged) q = staged_chunk<X, V>(s_own, j, d);
+        else q = load_pack<X, V>(reinterpret_cast<const X*>(s + c * 16));
+        if (RES) {
+          const Pack<X, V> pr = load_pack<X, V>(reinterpret_cast<const X*>(s + x_bytes + c * 16));
+          float2 sums[P];
+#pragma unroll
+          for (int p = 0; p < P; ++p) sums[p] = add2(pair_of(q, p), pair_of(pr, p));
+          q = round_pack<X, V>(&sums[0].x);
+          store_chunk<X, V, SHIFT>(h, j, d, q);
+        }
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          f[i * P + p] = pair_of(q, p);
+          if (CENTER) part = add2(part, f[i * P + p]);
+        }
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) f[i * P + p] = both(0.0f);
+      }
+    }
+    float sum = 0.0f, mu = 0.0f;
+    if (CENTER) {
+      sum = warp_sum(part.x + part.y);
+      mu = sum * inv_count;                            // any point near the mean serves to measure the deviations from
+    }
+    part = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = column(i);
       if (CENTER && j >= d) continue;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        float2 c = CENTER ? add2(value(i, p), both(-mu)) : value(i, p);
+        float2 c = CENTER ? add2(f[i * P + p], both(-mu)) : f[i * P + p];
         if (CENTER && !is_whole<V, SHIFT>(j, d)) {
           if (!has_column(j, 2 * p, d)) c.x = 0.0f;
           if (!has_column(j, 2 * p + 1, d)) c.y = 0.0f;
@@ -402,31 +612,8 @@ __global__ void __launch_bounds__(MOST, MOST == 128 ? (RES ? 5 : kFwdBlocks) : 1
       }
     }
     float m2 = warp_sum(part.x + part.y);
-    if (warps > 1) {
-      WarpStats* const st = s_stats[r & 1];
-      if (lane == 0) st[warp] = WarpStats{sum, m2, mu, (float)count};
-      __syncthreads();
-      m2 = 0.0f;
-      if (CENTER) {
-        sum = 0.0f;
-        for (int w = 0; w < warps; ++w) sum += st[w].sum;
-        mu = sum * inv_d;
-        for (int w = 0; w < warps; ++w) {
-          const float c = st[w].near - mu;
-          m2 += fmaf(st[w].count * c, c, st[w].m2);
-        }
-      } else {
-        for (int w = 0; w < warps; ++w) m2 += st[w].m2;
-      }
-    } else {
-      if (CENTER) {
-        const float c = sum * inv_d - mu;
-        mu = sum * inv_d;
-        m2 = fmaf((float)count * c, c, m2);
-      }
-      if (staged) __syncwarp();
-    }
-    const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps), drop = -mu * rstd;
+    merge_warps<CENTER, MOST / 32>(s_stats[k & 1], lane, warp, warps, sum, m2, mu, count, inv_d);
+    const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
     if (tid == 0) {
       if (CENTER && a.mean) a.mean[t] = mu;
       if (a.rstd) a.rstd[t] = rstd;
@@ -434,36 +621,20 @@ __global__ void __launch_bounds__(MOST, MOST == 128 ? (RES ? 5 : kFwdBlocks) : 1
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = column(shift, i);
+      const int j = column(i);
       if (j >= d) continue;
       float2 w[P], b[P];
-      if (!SHIFT) {
-        load_weights<V>(a.weight, a.w_bf16, j, 1.0f, &w[0].x);
-        load_weights<V>(a.bias, a.w_bf16, j, 0.0f, &b[0].x);
-      } else if (spread_out && is_whole<V, SHIFT>(j, d)) {
-        const int at = spread<V>(j), first = V - j % V;  // V columns from j on: a place is skipped behind the first multiple of V
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const float2 q0 = s_wb[at + 2 * p + (2 * p >= first)], q1 = s_wb[at + 2 * p + 1 + (2 * p + 1 >= first)];
-          w[p] = make_float2(q0.x, q1.x);
-          b[p] = make_float2(q0.y, q1.y);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const int c = has_column(j, k, d) ? j + k : 0;
-          load_weights<1>(a.weight, a.w_bf16, c, 1.0f, &w[0].x + k);
-          load_weights<1>(a.bias, a.w_bf16, c, 0.0f, &b[0].x + k);
-        }
-      }
+      chunk_weights<V>(s_w, held, i * threads + tid, w);
+      if (a.bias) chunk_weights<V>(s_b, held, i * threads + tid, b);
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        const float2 xh = CENTER ? fma2(value(i, p), both(rstd), both(drop)) : mul2(value(i, p), both(rstd));
-        w[p] = fma2(xh, w[p], b[p]);
+        const float2 xh = mul2(CENTER ? add2(f[i * P + p], both(-mu)) : f[i * P + p], both(rstd));
+        w[p] = a.bias ? fma2(xh, w[p], b[p]) : mul2(xh, w[p]);
       }
       store_values<V, SHIFT>(a.y, a.y_bf16, t * d, j, d, &w[0].x);
     }
   }
+  copies_arrived(0);
 }
 
 // Rows longer than a block's registers hold: the row is read again for each of the three passes.
@@ -524,35 +695,29 @@ __global__ void __launch_bounds__(1024) ln_fwd_long_kernel(FwdParams a) {
   }
 }
 
-// Threads per row: chunks of V elements, NV a thread.
-int group_of(int64_t chunks, int nv) {
-  int64_t g = 32;
-  while (g * nv < chunks) g *= 2;
-  return (int)(g > 2048 ? 2048 : g);
+constexpr int kFwdSpan = 4, kFwdSpanShift = 16, kFwdRounds = 3;
+int fwd_span(int64_t T, int per_sm, int most) {        // rows of a block, as long as kFwdRounds rounds of blocks are left
+  const int64_t span = T / ((int64_t)sm_count() * per_sm * kFwdRounds);
+  return (int)(span < 1 ? 1 : span > most ? most : span);
 }
 
-constexpr int kFwdThreadsPerSm = 640;     // that fit with their registers
-constexpr int kFwdSpanMost = 4, kFwdSpanShift = 12, kFwdRounds = 3;
-
-template <typename X, int NV, int MOST, bool SHIFT, bool CENTER, bool RES>
-cudaError_t run_fwd(const FwdParams& a, int64_t chunks, cudaStream_t st) {
+template <typename X, int NV, int MOST, int LEAST, bool CENTER, bool RES>
+cudaError_t run_fwd(const FwdParams& a, int64_t chunks, bool shift, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(X);
-  const auto kernel = ln_fwd_kernel<X, NV, MOST, SHIFT, CENTER, RES>;
-  const int threads = (int)align_up((size_t)ceil_div(chunks, NV), 32);
-  const int64_t at_once = (int64_t)sm_count() * (threads >= kFwdThreadsPerSm ? 1 : kFwdThreadsPerSm / threads);
-  int64_t span = a.T / (at_once * kFwdRounds);
-  const int64_t most = SHIFT ? kFwdSpanShift : kFwdSpanMost;
-  span = span < 1 ? 1 : span > most ? most : span;
-  int smem = 0;
-  if (SHIFT) {
-    if (a.d <= kSpreadMost) smem += align16(8 * (a.d + a.d / V + 1));
-    if (a.T > 1 && a.ldx % V != a.d % V) smem += align16((int)sizeof(X) * (a.d + 2 * V));
-    if (smem > 32 * 1024) {
-      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      if (e != cudaSuccess) return e;
-    }
+  const int threads = row_threads(chunks, NV), held = threads * NV;
+  const int by_registers = LEAST * MOST / threads > 32 ? 32 : LEAST * MOST / threads > 1 ? LEAST * MOST / threads : 1;
+  if (!shift) {
+    const int span = fwd_span(a.T, by_registers, kFwdSpan);
+    ln_fwd_kernel<X, NV, MOST, LEAST, CENTER, RES><<<(unsigned)ceil_div(a.T, span), threads, 0, st>>>(a, span);
+    return cudaGetLastError();
   }
-  kernel<<<(unsigned)ceil_div(a.T, span), threads, smem, st>>>(a, (int)span);
+  const auto kernel = ln_fwd_shift_kernel<X, NV, MOST, LEAST, CENTER, RES>;
+  const int fixed = held * V * 4 * (a.bias ? 2 : 1), stage = held * 16 + 16 + (RES ? held * 16 : 0);
+  const RowPlan p = plan_rows(by_registers, fixed, stage);
+  const int shifts = shifts_of(a.d, V), span = fwd_span(a.T, p.per_sm, kFwdSpanShift), smem = fixed + p.stages * stage;
+  const cudaError_t e = allow_shared(kernel, smem);
+  if (e != cudaSuccess) return e;
+  kernel<<<(unsigned)(ceil_div(a.T, (int64_t)span * shifts) * shifts), threads, smem, st>>>(a, span, p.stages, shifts);
   return cudaGetLastError();
 }
 
@@ -560,23 +725,17 @@ template <typename X, bool CENTER, bool RES>
 cudaError_t pick_fwd(const FwdParams& a, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(X);
   const bool shift = !(a.d % V == 0 && (a.T == 1 || a.ldx % V == 0));
-  const int64_t chunks = shift ? ceil_div(a.d + V - 1, V) : a.d / V;
-  if (chunks > 4 * 1024) {
+  const int64_t chunks = ceil_div(shift ? a.d + V - 1 : a.d, V);
+  const int nv = chunks <= 32 ? 1 : chunks <= 4 * 128 ? 4 : 16 / V, threads = row_threads(chunks, nv), held = threads * nv;
+  if (a.d > kRowMost || threads > 1024 || (shift && held * (V * 8 + 32) + 16 + kSharedOwn > kSharedMost)) {
     ln_fwd_long_kernel<X, CENTER><<<(unsigned)a.T, 1024, 0, st>>>(a);
     return cudaGetLastError();
   }
-  // One warp with one chunk a thread for short rows; up to 128 threads with four chunks, whose registers leave room for five blocks an SM;
-  // then as many threads as two chunks (at last four) a thread need.  Where there are fewer rows than SMs, as many threads as there
-  // are chunks: one row of 4096 takes 2.9 us so and 3.4 on 128 threads.
-  auto form = [&](auto sh) {
-    constexpr bool S = decltype(sh)::value;
-    if (chunks <= 32) return run_fwd<X, 1, 128, S, CENTER, RES>(a, chunks, st);
-    if (chunks <= 1024 && a.T <= sm_count()) return run_fwd<X, 1, 1024, S, CENTER, RES>(a, chunks, st);
-    if (chunks <= 4 * 128) return run_fwd<X, 4, 128, S, CENTER, RES>(a, chunks, st);
-    if (chunks <= 2 * 1024) return run_fwd<X, 2, 1024, S, CENTER, RES>(a, chunks, st);
-    return run_fwd<X, 4, 1024, S, CENTER, RES>(a, chunks, st);
-  };
-  return shift ? form(std::true_type{}) : form(std::false_type{});
+  // Where there are fewer rows than SMs, as many threads as there are chunks: one row of 4096 takes 2.7 us so and 3.4 on 128 threads.
+  if (chunks <= 32) return run_fwd<X, 1, 32, 20, CENTER, RES>(a, chunks, shift, st);
+  if (chunks <= 1024 && a.T <= sm_count()) return run_fwd<X, 1, 1024, 1, CENTER, RES>(a, chunks, shift, st);
+  if (chunks <= 4 * 128) return run_fwd<X, 4, 128, 5, CENTER, RES>(a, chunks, shift, st);
+  return run_fwd<X, 16 / V, 1024, 1, CENTER, RES>(a, chunks, shift, st);
 }
 
 // ---------------------------------------------------------------------------
@@ -587,157 +746,230 @@ struct BwdParams {
   const uint8_t* mask;
   const float *mean, *rstd;
   int64_t ldx, T;
-  int32_t d, w_bf16;
+  int32_t d, w_bf16, dy_bf16;
   void* dx;
   float* partial;                // [blocks][want][d]: dw, then db
   int want_dw, want_db;
 };
 
-// A group of threads per row as in the forward pass, and a thread keeps its columns for all rows that its group walks through
-// (rows g, g + groups of the grid, ...): weights and the sums of dw and db stay in registers.  The next row is loaded before the
-// current one is reduced.  Both row means take one barrier.  At the end the groups of a block add up in shared memory, in order,
-// and each block leaves one partial row of dw and db.
-template <typename X, typename DY, int V, int NV, bool CENTER>
-__global__ void __launch_bounds__(1024) ln_bwd_kernel(BwdParams a, int group) {
-  constexpr int E = V * NV;
-  __shared__ float2 s_sum[2][32];
-  extern __shared__ float s_cols[];                     // [groups - 1][2][d], where a block has several groups
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = threadIdx.x / group, tid = threadIdx.x - g * group;
-  const int groups = blockDim.x / group;
-  const int64_t step = (int64_t)gridDim.x * groups;
-  float w[E], dw[E], db[E];
+// V sums to a partial row of d of them, which begins on 16 bytes only where d is a multiple of 4.
+template <int V, bool SHIFT>
+__device__ __forceinline__ void store_partial(float* row, int j, int d, const float* f) {
+  if constexpr (SHIFT) {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int64_t c = (int64_t)(i * group + tid) * V;
-    if (c < a.d) {
-      load_weights<V>(a.weight, a.w_bf16, c, 1.0f, w + i * V);
-    } else {
-#pragma unroll
-      for (int k = 0; k < V; ++k) w[i * V + k] = 0.0f;
-    }
+    for (int k = 0; k < V; ++k)
+      if (has_column(j, k, d)) row[j + k] = f[k];
+  } else {
+    store_pack(row + j, round_pack<float, V>(f));
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.0f;
+}
 
-  Pack<X, V> px[NV], ph[NV];
-  Pack<DY, V> py[NV];
-  float mu = 0.0f, rstd = 0.0f;
-  bool live = false;
-  auto fetch = [&](int64_t t) {
-    live = t < a.T && (!a.mask || a.mask[t] != 0);
-    rstd = live ? a.rstd[t] : 0.0f;
-    mu = CENTER && live ? a.mean[t] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(i * group + tid) * V;
-      zero_pack(px[i]);
-      zero_pack(py[i]);
-      zero_pack(ph[i]);
-      if (live && c < a.d) {
-        px[i] = load_pack<X, V>(static_cast<const X*>(a.x) + t * a.ldx + c);
-        py[i] = load_pack<DY, V>(static_cast<const DY*>(a.dy) + t * a.d + c);
-        if (a.dh) ph[i] = load_pack<X, V>(static_cast<const X*>(a.dh) + t * a.d + c);
-      }
-    }
+// A block walks through rows b, b + blocks, ... (shifted ones: the number of blocks is a multiple of that of shifts); its threads keep
+// their columns for all of them, so the sums of dw and db stay in registers, and each block leaves one partial row of both.  A row is
+// read twice from shared memory, for the two row means and for dx.  Columns that are not a shifted row's are zeros of x, dy and w, which
+// add nothing.
+// Bytes of the ring and the weights of a block: `held` chunks.
+struct BwdShared {
+  int weights, x, dy, dh, stage;
+};
+__host__ __device__ __forceinline__ BwdShared bwd_shared(int held, int v, int dy_size, bool dh, bool shift) {
+  BwdShared b;
+  b.weights = held * v * 4;
+  b.x = held * 16 + (shift ? 16 : 0);
+  b.dy = align16(held * v * dy_size);
+  b.dh = dh ? held * 16 : 0;
+  b.stage = b.x + b.dy + b.dh;
+  return b;
+}
+
+template <typename X, int NV, int MOST, int LEAST, bool SHIFT, bool CENTER, bool DB>
+__global__ void __launch_bounds__(MOST, LEAST) ln_bwd_kernel(BwdParams a, int stages) {
+  constexpr int V = 16 / (int)sizeof(X), P = V / 2;
+  __shared__ float2 s_sum[2][32];
+  extern __shared__ __align__(16) char s_raw[];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
+  const int d = a.d, held = threads * NV, dy_size = a.dy_bf16 ? 2 : 4;
+  const BwdShared at = bwd_shared(held, V, dy_size, a.dh != nullptr, SHIFT);
+  float4* const s_w = reinterpret_cast<float4*>(s_raw);
+  char* const s_ring = s_raw + at.weights;
+  const int64_t first = blockIdx.x, step = gridDim.x;
+  const int shift = SHIFT ? (int)((first * d) % V) : 0;
+  const bool staged = SHIFT && a.ldx % V != d % V && a.T > 1;
+  const int2 edges = edge_chunks<V>(shift, d, tid, threads);
+  auto column = [&](int i) { return (i * threads + tid) * V - shift; };
+
+  // a row's mask byte (0 behind the last row), looked at a row later: a comparison here would wait for it
+  auto mask_of = [&](int64_t t) -> uint32_t {
+    uint32_t m = t < a.T;
+    if (a.mask && t < a.T) asm volatile("ld.global.u8 %0, [%1];" : "=r"(m) : "l"(a.mask + t));
+    return m;
   };
-  const float inv_d = 1.0f / (float)a.d;
-  int buf = 0;
-  int64_t t = (int64_t)blockIdx.x * groups + g;
-  fetch(t);
-  for (int64_t first = (int64_t)blockIdx.x * groups; first < a.T; first += step, t += step, buf ^= 1) {
-    float xh[E], dy[E];
-    Pack<X, V> h[NV];
-    const float r = rstd;
-    float s1 = 0.0f, s2 = 0.0f;
+  auto fetch = [&](int64_t t, bool live, int slot) {
+    if (live) {
+      char* const s = s_ring + slot * at.stage;
+      const X *const x = static_cast<const X*>(a.x) + t * a.ldx, *const dh = static_cast<const X*>(a.dh) + t * d;
+      const int own = staged ? (int)((t * a.ldx) % V) : shift;
+      const int end_x = SHIFT ? end_of(a.T, t, a.ldx, d) : 0, end = SHIFT ? end_of(a.T, t, d, d) : 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      h[i] = ph[i];
-#pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const int e = i * V + k;
-        xh[e] = (element(px[i], k) - mu) * r;
-        dy[e] = element(py[i], k);
+      for (int i = 0; i < NV; ++i) {
+        const int c = i * threads + tid, j = c * V - shift, jx = c * V - own;
+        if (jx < d) copy_chunk<X, V, SHIFT>(s + c * 16, x, jx, end_x);
+        if (j >= d) continue;
+        if (a.dy_bf16) copy_chunk<__nv_bfloat16, V, SHIFT>(s + at.x + c * V * 2, static_cast<const __nv_bfloat16*>(a.dy) + t * d, j, end);
+        else copy_chunk<float, V, SHIFT>(s + at.x + c * V * 4, static_cast<const float*>(a.dy) + t * d, j, end);
+        if (a.dh) copy_chunk<X, V, SHIFT>(s + at.x + at.dy + c * 16, dh, j, end);
       }
     }
+    copies_issued();
+  };
+  // the first rows on their way, then the weights
+  uint32_t live_bits = 0;                               // bit i: row i from the current one on
+  for (int k = 0; k < stages - 1; ++k) {
+    const bool live = mask_of(first + k * step) != 0;
+    live_bits |= (uint32_t)live << k;
+    fetch(first + k * step, live, k);
+  }
+  uint32_t mask_next = mask_of(first + (stages - 1) * step);
+  float r_next = first < a.T ? a.rstd[first] : 0.0f, mu_next = CENTER && first < a.T ? a.mean[first] : 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      dw[e] = fmaf(dy[e], xh[e], dw[e]);
-      db[e] += dy[e];
-      dy[e] *= w[e];
-      s1 = fmaf(dy[e], xh[e], s1);
-      if (CENTER) s2 += dy[e];
+  for (int i = 0; i < NV; ++i) spread_weights<V>(s_w, a.weight, a.w_bf16, 1.0f, held, i * threads + tid, column(i), d);
+  float2 dw[NV * P], db[DB ? NV * P : 1];
+#pragma unroll
+  for (int e = 0; e < NV * P; ++e) {
+    dw[e] = both(0.0f);
+    if constexpr (DB) db[e] = both(0.0f);
+  }
+  const float inv_d = 1.0f / (float)d;
+  int slot = 0, buf = 0;
+#pragma unroll 1
+  for (int64_t t = first; t < a.T; t += step, buf ^= 1) {
+    const int64_t ahead = t + (stages - 1) * step;
+    const bool live_ahead = mask_next != 0;
+    live_bits |= (uint32_t)live_ahead << (stages - 1);
+    fetch(ahead, live_ahead, slot == 0 ? stages - 1 : slot - 1);
+    mask_next = mask_of(ahead + step);
+    const float r = r_next, mu = mu_next;
+    if (t + step < a.T) {
+      r_next = a.rstd[t + step];
+      if (CENTER) mu_next = a.mean[t + step];
     }
-    fetch(t + step);
-    s1 = warp_sum(s1);
-    if (CENTER) s2 = warp_sum(s2);
-    if (group > 32) {
+    const bool live = live_bits & 1;
+    live_bits >>= 1;
+    char* const s = s_ring + slot * at.stage;
+    slot = slot + 1 == stages ? 0 : slot + 1;
+    X* const out = static_cast<X*>(a.dx) + t * d;
+    copies_arrived(stages - 1);
+    if (!live) {                                        // (the same for all threads of the block)
+      Pack<X, V> zero;
+      zero_pack(zero);
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (column(i) < d) store_chunk<X, V, SHIFT>(out, column(i), d, zero);
+      continue;
+    }
+    if (SHIFT) {
+      if (staged) __syncthreads();
+      for (int e = 0; e < 2; ++e) {
+        const int c = e == 0 ? edges.x : edges.y, j = c * V - shift;
+        if (c < 0) continue;
+        if (!staged) blank<X, V>(s + c * 16, j, d);
+        if (a.dy_bf16) blank<__nv_bfloat16, V>(s + at.x + c * V * 2, j, d);
+        else blank<float, V>(s + at.x + c * V * 4, j, d);
+      }
+    }
+    const X* const s_own = reinterpret_cast<const X*>(s) + (staged ? (int)((t * a.ldx) % V) : 0);
+    auto normalised = [&](int i, float2* xh) {          // of chunk i
+      const int c = i * threads + tid;
+      Pack<X, V> px;
+      if (SHIFT && staged) px = staged_chunk<X, V>(s_own, column(i), d);
+      else px = load_pack<X, V>(reinterpret_cast<const X*>(s + c * 16));
+#pragma unroll
+      for (int p = 0; p < P; ++p) xh[p] = mul2(CENTER ? add2(pair_of(px, p), both(-mu)) : pair_of(px, p), both(r));
+    };
+    auto gradient = [&](int i, float2* g) {
+      const int c = i * threads + tid;
+      if (a.dy_bf16) {
+        const Pack<__nv_bfloat16, V> q = load_pack<__nv_bfloat16, V>(reinterpret_cast<const __nv_bfloat16*>(s + at.x) + c * V);
+#pragma unroll
+        for (int p = 0; p < P; ++p) g[p] = pair_of(q, p);
+      } else {
+        const Pack<float, V> q = load_pack<float, V>(reinterpret_cast<const float*>(s + at.x) + c * V);
+#pragma unroll
+        for (int p = 0; p < P; ++p) g[p] = pair_of(q, p);
+      }
+    };
+    auto weights = [&](int i, float2* w) { chunk_weights<V>(s_w, held, i * threads + tid, w); };
+    float2 p1 = both(0.0f), p2 = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (column(i) >= d) continue;
+      float2 xh[P], g[P], w[P];
+      normalised(i, xh);
+      gradient(i, g);
+      weights(i, w);
+#pragma unroll
+      for (int p = 0; p < P; ++p) {
+        dw[i * P + p] = fma2(g[p], xh[p], dw[i * P + p]);
+        if constexpr (DB) db[i * P + p] = add2(db[i * P + p], g[p]);
+        const float2 up = mul2(g[p], w[p]);
+        p1 = fma2(up, xh[p], p1);
+        if (CENTER) p2 = add2(p2, up);
+      }
+    }
+    float s1 = warp_sum(p1.x + p1.y), s2 = CENTER ? warp_sum(p2.x + p2.y) : 0.0f;
+    if (warps > 1) {
       if (lane == 0) s_sum[buf][warp] = make_float2(s1, s2);
       __syncthreads();
       s1 = s2 = 0.0f;
-      const int w0 = g * (group >> 5);
-      for (int q = 0; q < (group >> 5); ++q) {
-        const float2 v = s_sum[buf][w0 + q];
+      for (int q = 0; q < warps; ++q) {
+        const float2 v = s_sum[buf][q];
         s1 += v.x;
         if (CENTER) s2 += v.y;
       }
     }
-    s1 *= inv_d;
-    s2 *= inv_d;
-    if (t < a.T) {
+    s1 *= -inv_d;
+    s2 *= -inv_d;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int64_t c = (int64_t)(i * group + tid) * V;
-        if (c < a.d) {
-          float o[V];
+    for (int i = 0; i < NV; ++i) {
+      const int j = column(i);
+      if (j >= d) continue;
+      float2 xh[P], g[P], w[P];
+      normalised(i, xh);
+      gradient(i, g);
+      weights(i, w);
+      Pack<X, V> ph;
+      zero_pack(ph);
+      if (a.dh) ph = load_pack<X, V>(reinterpret_cast<const X*>(s + at.x + at.dy) + (i * threads + tid) * V);
 #pragma unroll
-          for (int k = 0; k < V; ++k) {
-            const int e = i * V + k;
-            o[k] = fmaf(r, CENTER ? fmaf(-xh[e], s1, dy[e] - s2) : fmaf(-xh[e], s1, dy[e]), element(h[i], k));
-          }
-          store_pack(static_cast<X*>(a.dx) + t * a.d + c, round_pack<X, V>(o));
-        }
+      for (int p = 0; p < P; ++p) {
+        const float2 up = CENTER ? fma2(g[p], w[p], both(s2)) : mul2(g[p], w[p]);
+        w[p] = fma2(fma2(xh[p], both(s1), up), both(r), pair_of(ph, p));
       }
+      store_chunk<X, V, SHIFT>(out, j, d, round_pack<X, V>(&w[0].x));
     }
+    if (staged) __syncthreads();                        // others read these chunks of x: they are overwritten in the next round
   }
+  copies_arrived(0);
   if (!a.partial) return;
   pdl_release();
-  if (g > 0) {
+  float* const row = a.partial + (int64_t)blockIdx.x * (a.want_dw + a.want_db) * d;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(i * group + tid) * V;
-      if (c < a.d) {
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          s_cols[(int64_t)(2 * (g - 1)) * a.d + c + k] = dw[i * V + k];
-          s_cols[(int64_t)(2 * (g - 1) + 1) * a.d + c + k] = db[i * V + k];
-        }
-      }
-    }
-  }
-  if (groups > 1) __syncthreads();
-  if (g == 0) {
-    const int want = a.want_dw + a.want_db;
-    float* row = a.partial + (int64_t)blockIdx.x * want * a.d;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int64_t c = (int64_t)(i * group + tid) * V;
-      if (c < a.d) {
-        for (int q = 0; q < groups - 1; ++q) {
-#pragma unroll
-          for (int k = 0; k < V; ++k) {
-            dw[i * V + k] += s_cols[(int64_t)(2 * q) * a.d + c + k];
-            db[i * V + k] += s_cols[(int64_t)(2 * q + 1) * a.d + c + k];
-          }
-        }
-        if (a.want_dw) store_pack(row + c, round_pack<float, V>(dw + i * V));
-        if (a.want_db) store_pack(row + (int64_t)a.want_dw * a.d + c, round_pack<float, V>(db + i * V));
-      }
+  for (int i = 0; i < NV; ++i) {
+    const int j = column(i);
+    if (j >= d) continue;
+    float* const both_rows[2] = {a.want_dw ? row : nullptr, a.want_db ? row + (int64_t)a.want_dw * d : nullptr};
+    if (both_rows[0]) store_partial<V, SHIFT>(both_rows[0], j, d, &dw[i * P].x);
+    if constexpr (DB) {
+      if (both_rows[1]) store_partial<V, SHIFT>(both_rows[1], j, d, &db[i * P].x);
     }
   }
 }
 
 // Rows longer than a block's registers hold: one block per row finds the two means and writes dx ...
-template <typename X, typename DY, bool CENTER>
+__device__ __forceinline__ float one_gradient(const BwdParams& a, int64_t at) {
+  return a.dy_bf16 ? element(load_pack<__nv_bfloat16, 1>(static_cast<const __nv_bfloat16*>(a.dy) + at), 0) : static_cast<const float*>(a.dy)[at];
+}
+template <typename X, bool CENTER>
 __global__ void __launch_bounds__(1024) ln_bwd_long_rows_kernel(BwdParams a) {
   __shared__ float2 s_sum[32];
   const int64_t t = blockIdx.x;
@@ -745,7 +977,6 @@ __global__ void __launch_bounds__(1024) ln_bwd_long_rows_kernel(BwdParams a) {
   const bool live = !a.mask || a.mask[t] != 0;
   const X* x = static_cast<const X*>(a.x) + t * a.ldx;
   const X* dh = a.dh ? static_cast<const X*>(a.dh) + t * a.d : nullptr;
-  const DY* dy = static_cast<const DY*>(a.dy) + t * a.d;
   X* dx = static_cast<X*>(a.dx) + t * a.d;
   const float r = live ? a.rstd[t] : 0.0f, mu = CENTER && live ? a.mean[t] : 0.0f;
   float s1 = 0.0f, s2 = 0.0f;
@@ -753,7 +984,7 @@ __global__ void __launch_bounds__(1024) ln_bwd_long_rows_kernel(BwdParams a) {
     for (int64_t c = threadIdx.x; c < a.d; c += blockDim.x) {
       float w;
       load_weights<1>(a.weight, a.w_bf16, c, 1.0f, &w);
-      const float up = w * element(load_pack<DY, 1>(dy + c), 0);
+      const float up = w * one_gradient(a, t * a.d + c);
       s1 = fmaf(up, (element(load_pack<X, 1>(x + c), 0) - mu) * r, s1);
       s2 += up;
     }
@@ -774,7 +1005,7 @@ __global__ void __launch_bounds__(1024) ln_bwd_long_rows_kernel(BwdParams a) {
       float w;
       load_weights<1>(a.weight, a.w_bf16, c, 1.0f, &w);
       const float xh = (element(load_pack<X, 1>(x + c), 0) - mu) * r;
-      o = r * fmaf(-xh, s1, w * element(load_pack<DY, 1>(dy + c), 0) - s2);
+      o = r * fmaf(-xh, s1, w * one_gradient(a, t * a.d + c) - s2);
       if (dh) o += element(load_pack<X, 1>(dh + c), 0);
     }
     store_pack(dx + c, round_pack<X, 1>(&o));
@@ -782,14 +1013,14 @@ __global__ void __launch_bounds__(1024) ln_bwd_long_rows_kernel(BwdParams a) {
 }
 
 // ... and before that (dx may take dy's place) blocks of 256 columns by a share of the rows sum dw and db.
-template <typename X, typename DY, bool CENTER>
+template <typename X, bool CENTER>
 __global__ void __launch_bounds__(256) ln_bwd_long_cols_kernel(BwdParams a) {
   const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (c >= a.d) return;
   float dw = 0.0f, db = 0.0f;
   for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
     if (a.mask && a.mask[t] == 0) continue;
-    const float dy = element(load_pack<DY, 1>(static_cast<const DY*>(a.dy) + t * a.d + c), 0);
+    const float dy = one_gradient(a, t * a.d + c);
     const float x = element(load_pack<X, 1>(static_cast<const X*>(a.x) + t * a.ldx + c), 0);
     dw = fmaf(dy, (x - (CENTER ? a.mean[t] : 0.0f)) * a.rstd[t], dw);
     db += dy;
@@ -828,61 +1059,69 @@ __global__ void __launch_bounds__(256) ln_bwd_columns_kernel(const float* __rest
   }
 }
 
-// The launch of a backward pass; a function of d and T alone, so that the scratch can be sized by it.
-constexpr int kLongRows = 16384;           // elements of a row that a block's registers hold
-struct BwdPlan {
-  int v, nv, group, threads, blocks;       // v = 0: the long form; blocks then is the number of row shares
-};
-BwdPlan bwd_plan(int64_t T, int32_t d, int v) {
-  BwdPlan p{};
-  if (d > kLongRows) {
-    p.blocks = (int)(T < 64 ? T : 64);
-    return p;
+// The launch of a backward pass.  The number of blocks is at most bwd_blocks_most(), so that the scratch can be sized by d and T alone.
+int bwd_per_sm(int threads) { return threads == 32 ? 16 : threads <= 128 ? 512 / threads : threads <= 1024 ? 1024 / threads : 1; }
+int64_t bwd_blocks_most(int64_t T, int32_t d) {
+  int64_t most = T < 64 ? T : 64;          // of rows that take the long form
+  if (d > kRowMost) return most;
+  for (int v : {4, 8}) {                   // rows of fp32 and of bf16; shifted rows may have a chunk more
+    for (int64_t chunks : {ceil_div(d, v), ceil_div(d + v - 1, v)}) {
+      const int64_t n = (int64_t)sm_count() * bwd_per_sm(row_threads(chunks, row_form(chunks, v)));
+      most = n > most ? n : most;
+    }
   }
-  p.v = v;
-  p.nv = (d <= 8192 ? 8 : 16) / v;
-  p.group = group_of(ceil_div(d, v), p.nv);
-  p.threads = p.group > 256 ? p.group : 256;
-  const int64_t most = (int64_t)sm_count() * (1024 / p.threads), need = ceil_div(T, p.threads / p.group);
-  p.blocks = (int)(need < most ? need : most);
-  return p;
+  const int64_t rows = (T + 7) / 8 * 8;    // shifted rows: blocks are a multiple of the shifts, up to eight
+  return rows < most ? rows : most;
 }
 
-template <typename X, typename DY, int V, int NV, bool CENTER>
-cudaError_t run_bwd(const BwdParams& a, const BwdPlan& p, cudaStream_t st) {
-  const int smem = a.partial ? (p.threads / p.group - 1) * 2 * a.d * (int)sizeof(float) : 0;      // below 16 KB: groups are as long as rows
-  ln_bwd_kernel<X, DY, V, NV, CENTER><<<p.blocks, p.threads, smem, st>>>(a, p.group);
+template <typename X, int NV, int MOST, int LEAST, bool SHIFT, bool CENTER, bool DB>
+cudaError_t run_bwd(const BwdParams& a, int64_t chunks, int* blocks, cudaStream_t st) {
+  constexpr int V = 16 / (int)sizeof(X);
+  const auto kernel = ln_bwd_kernel<X, NV, MOST, LEAST, SHIFT, CENTER, DB>;
+  const int threads = row_threads(chunks, NV);
+  const BwdShared at = bwd_shared(threads * NV, V, a.dy_bf16 ? 2 : 4, a.dh != nullptr, SHIFT);
+  const RowPlan p = plan_rows(bwd_per_sm(threads), at.weights, at.stage);
+  const int shifts = SHIFT ? shifts_of(a.d, V) : 1;
+  const int64_t most = (int64_t)sm_count() * p.per_sm / shifts * shifts, rows = (a.T + shifts - 1) / shifts * shifts;
+  *blocks = (int)(rows < most ? rows : most);
+  const int smem = at.weights + p.stages * at.stage;
+  const cudaError_t e = allow_shared(kernel, smem);
+  if (e != cudaSuccess) return e;
+  kernel<<<*blocks, threads, smem, st>>>(a, p.stages);
   return cudaGetLastError();
 }
 
-template <typename X, typename DY, bool CENTER>
-cudaError_t pick_bwd(const BwdParams& a, const BwdPlan& p, cudaStream_t st) {
-  if (p.v == 0) {
+template <typename X, bool CENTER, bool DB>
+cudaError_t pick_bwd(const BwdParams& a, int* blocks, cudaStream_t st) {
+  constexpr int V = 16 / (int)sizeof(X);
+  const bool shift = !(a.d % V == 0 && (a.T == 1 || a.ldx % V == 0));
+  const int64_t chunks = ceil_div(shift ? a.d + V - 1 : a.d, V);
+  const int nv = row_form(chunks, V), threads = row_threads(chunks, nv);
+  const BwdShared at = bwd_shared(threads * nv, V, a.dy_bf16 ? 2 : 4, a.dh != nullptr, shift);
+  if (a.d > kRowMost || threads > 1024 || at.weights + at.stage + kSharedOwn > kSharedMost) {
+    *blocks = (int)(a.T < 64 ? a.T : 64);
     cudaError_t e = cudaSuccess;
     if (a.partial) {
-      ln_bwd_long_cols_kernel<X, DY, CENTER><<<dim3((unsigned)ceil_div(a.d, 256), p.blocks), 256, 0, st>>>(a);
+      ln_bwd_long_cols_kernel<X, CENTER><<<dim3((unsigned)ceil_div(a.d, 256), *blocks), 256, 0, st>>>(a);
       if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
-    ln_bwd_long_rows_kernel<X, DY, CENTER><<<(unsigned)a.T, 1024, 0, st>>>(a);
+    ln_bwd_long_rows_kernel<X, CENTER><<<(unsigned)a.T, 1024, 0, st>>>(a);
     return cudaGetLastError();
   }
-  constexpr int V = 16 / (int)sizeof(X);
-  const bool two = p.nv * p.v > 8;
-  if (p.v == 1) return two ? run_bwd<X, DY, 1, 16, CENTER>(a, p, st) : run_bwd<X, DY, 1, 8, CENTER>(a, p, st);
-  return two ? run_bwd<X, DY, V, 16 / V, CENTER>(a, p, st) : run_bwd<X, DY, V, 8 / V, CENTER>(a, p, st);
+  auto form = [&](auto sh) {
+    constexpr bool S = decltype(sh)::value;
+    if (nv == 1 && chunks <= 32) return run_bwd<X, 1, 32, 16, S, CENTER, DB>(a, chunks, blocks, st);
+    if (nv == 32 / V) return run_bwd<X, 32 / V, 128, 4, S, CENTER, DB>(a, chunks, blocks, st);
+    return run_bwd<X, 16 / V, 1024, 1, S, CENTER, DB>(a, chunks, blocks, st);
+  };
+  return shift ? form(std::true_type{}) : form(std::false_type{});
 }
 
 }  // namespace
 
 size_t layernorm_bwd_ws_bytes(int64_t T, int32_t d) {
   if (T < 1) return 256;
-  size_t most = 0;
-  for (int v : {8, 4, 1}) {                // aligned bf16, aligned fp32, any other rows
-    const BwdPlan p = bwd_plan(T, d, v);
-    const size_t n = (size_t)p.blocks * 2 * (size_t)d * sizeof(float);
-    if (n > most) most = n;
-  }
-  return align_up(most, 256);
+  return align_up((size_t)bwd_blocks_most(T, d) * 2 * (size_t)d * sizeof(float), 256);
 }
 
 cudaError_t launch_layernorm_fwd(const LayerNormFwd& q, cudaStream_t st) {
@@ -909,23 +1148,20 @@ cudaError_t launch_layernorm_bwd(const LayerNormBwd& q, char* ws, cudaStream_t s
       if (o && !q.dw_accumulate && (e = cudaMemsetAsync(o, 0, (size_t)q.d * size, st)) != cudaSuccess) return e;
     return e;
   }
-  const int v = 16 / (q.dtype == SPO_DTYPE_BF16 ? 2 : 4);
-  const bool aligned = q.d % v == 0 && (q.T == 1 || q.ldx % v == 0);
-  const BwdPlan p = bwd_plan(q.T, q.d, aligned ? v : 1);
   BwdParams a{};
   a.dy = q.dy; a.x = q.x; a.weight = q.weight; a.dh = q.dh; a.mask = q.mask; a.mean = q.mean; a.rstd = q.rstd; a.ldx = q.ldx;
-  a.T = q.T; a.d = q.d; a.w_bf16 = q.w_dtype == SPO_DTYPE_BF16; a.dx = q.dx;
+  a.T = q.T; a.d = q.d; a.w_bf16 = q.w_dtype == SPO_DTYPE_BF16; a.dy_bf16 = q.dy_dtype == SPO_DTYPE_BF16; a.dx = q.dx;
   a.want_dw = q.dw != nullptr; a.want_db = q.db != nullptr;
   a.partial = a.want_dw || a.want_db ? reinterpret_cast<float*>(ws) : nullptr;
-  using bf = __nv_bfloat16;
-  const bool x16 = q.dtype == SPO_DTYPE_BF16, y16 = q.dy_dtype == SPO_DTYPE_BF16;
-  if (q.kind == SPO_NORM_LAYER) {
-    if (x16) e = y16 ? pick_bwd<bf, bf, true>(a, p, st) : pick_bwd<bf, float, true>(a, p, st);
-    else e = y16 ? pick_bwd<float, bf, true>(a, p, st) : pick_bwd<float, float, true>(a, p, st);
-  } else {
-    if (x16) e = y16 ? pick_bwd<bf, bf, false>(a, p, st) : pick_bwd<bf, float, false>(a, p, st);
-    else e = y16 ? pick_bwd<float, bf, false>(a, p, st) : pick_bwd<float, float, false>(a, p, st);
-  }
+  int blocks = 0;
+  auto typed = [&](auto center, auto bias) {
+    constexpr bool C = decltype(center)::value, D = decltype(bias)::value;
+    return q.dtype == SPO_DTYPE_BF16 ? pick_bwd<__nv_bfloat16, C, D>(a, &blocks, st) : pick_bwd<float, C, D>(a, &blocks, st);
+  };
+  using yes = std::true_type;
+  using no = std::false_type;
+  if (q.kind == SPO_NORM_LAYER) e = q.db ? typed(yes{}, yes{}) : typed(yes{}, no{});
+  else e = q.db ? typed(no{}, yes{}) : typed(no{}, no{});
   if (e != cudaSuccess || !a.partial) return e;
   const int64_t width = (int64_t)(a.want_dw + a.want_db) * q.d;
   cudaLaunchConfig_t cfg{};
@@ -934,10 +1170,10 @@ cudaError_t launch_layernorm_bwd(const LayerNormBwd& q, char* ws, cudaStream_t s
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = p.v ? 1 : 0;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, ln_bwd_columns_kernel, (const float*)a.partial, p.blocks, width, q.d, q.dw, q.db,
+  return cudaLaunchKernelEx(&cfg, ln_bwd_columns_kernel, (const float*)a.partial, blocks, width, q.d, q.dw, q.db,
                             (int)(q.dw_dtype == SPO_DTYPE_BF16), (int)q.dw_accumulate);
 }
 
