@@ -256,13 +256,17 @@ __device__ __forceinline__ Pack<T, V> staged_chunk(const T* s_row, int j, int d)
 }
 
 // A vector of weights (or biases) in shared memory as fp32, by chunk: quarter q of chunk c at q held + c.
-template <int V>
+template <int V, bool SHIFT>
 __device__ __forceinline__ void spread_weights(float4* s, const void* p, int bf16, float none, int held, int c, int j, int d) {
   float w[V];
+  if (!SHIFT && j < d) {
+    load_weights<V>(p, bf16, j, none, w);
+  } else {
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    w[k] = 0.0f;
-    if (has_column(j, k, d)) load_weights<1>(p, bf16, j + k, none, w + k);
+    for (int k = 0; k < V; ++k) {
+      w[k] = 0.0f;
+      if (has_column(j, k, d)) load_weights<1>(p, bf16, j + k, none, w + k);
+    }
   }
 #pragma unroll
   for (int q = 0; q < V / 4; ++q) s[q * held + c] = make_float4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
@@ -286,8 +290,9 @@ int shifts_of(int32_t d, int v) {         // shifts that rows of d elements have
   while (n < v && (int64_t)n * d % v != 0) n *= 2;
   return n;
 }
-// Chunks a thread holds in the backward pass: one in a single warp, or 32 elements on up to 128 threads, or 16.
-int row_form(int64_t chunks, int v) { return chunks <= 32 ? 1 : chunks * v <= 32 * 128 ? 32 / v : 16 / v; }
+// Chunks a thread holds in the backward pass: one in a single warp, otherwise 16 elements; of shifted bf16 rows on up to 128 threads 32
+// (24 000 rows: of 2730 164 us so and 190 with 16, of 4096 with residual and fp32 gradients 187 and 154).
+int row_form(int64_t chunks, int v, bool shift) { return chunks <= 32 ? 1 : shift && v == 8 && chunks * v <= 32 * 128 ? 32 / v : 16 / v; }
 int row_threads(int64_t chunks, int nv) { return (int)align_up((size_t)ceil_div(chunks, nv), 32); }
 // Blocks on an SM and rows in the ring: three rows where as many blocks still fit as the registers allow, two otherwise, and for the longest
 // rows one.
@@ -303,7 +308,8 @@ RowPlan plan_rows(int per_sm, int fixed, int stage) {
 }
 template <class Kernel>
 cudaError_t allow_shared(Kernel kernel, int bytes) {
-  return bytes <= 32 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  return e != cudaSuccess || bytes <= 32 * 1024 ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 // Mean and squared deviations of a row from those of its warps, each about a point near its own mean: M2 = sum M2_w + n_w (near_w - mu)^2,
@@ -520,8 +526,8 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = i * threads + tid;
-    spread_weights<V>(s_w, a.weight, a.w_bf16, 1.0f, held, c, column(i), d);
-    if (a.bias) spread_weights<V>(s_b, a.bias, a.w_bf16, 0.0f, held, c, column(i), d);
+    spread_weights<V, true>(s_w, a.weight, a.w_bf16, 1.0f, held, c, column(i), d);
+    if (a.bias) spread_weights<V, true>(s_b, a.bias, a.w_bf16, 0.0f, held, c, column(i), d);
   }
   int count = 0;                                       // columns of this warp
   if (CENTER) {
@@ -696,8 +702,9 @@ __global__ void __launch_bounds__(1024) ln_fwd_long_kernel(FwdParams a) {
 }
 
 constexpr int kFwdSpan = 4, kFwdSpanShift = 16, kFwdRounds = 3;
-int fwd_span(int64_t T, int per_sm, int most) {        // rows of a block, as long as kFwdRounds rounds of blocks are left
-  const int64_t span = T / ((int64_t)sm_count() * per_sm * kFwdRounds);
+// Rows of a block: as many as leave so many rounds of blocks over the GPU, or one round of a short batch.
+int fwd_span(int64_t T, int per_sm, int rounds, int most) {
+  const int64_t at_once = (int64_t)sm_count() * per_sm, span = T <= rounds * at_once ? ceil_div(T, at_once) : T / (rounds * at_once);
   return (int)(span < 1 ? 1 : span > most ? most : span);
 }
 
@@ -707,14 +714,14 @@ cudaError_t run_fwd(const FwdParams& a, int64_t chunks, bool shift, cudaStream_t
   const int threads = row_threads(chunks, NV), held = threads * NV;
   const int by_registers = LEAST * MOST / threads > 32 ? 32 : LEAST * MOST / threads > 1 ? LEAST * MOST / threads : 1;
   if (!shift) {
-    const int span = fwd_span(a.T, by_registers, kFwdSpan);
+    const int span = fwd_span(a.T, by_registers, kFwdRounds, kFwdSpan);
     ln_fwd_kernel<X, NV, MOST, LEAST, CENTER, RES><<<(unsigned)ceil_div(a.T, span), threads, 0, st>>>(a, span);
     return cudaGetLastError();
   }
   const auto kernel = ln_fwd_shift_kernel<X, NV, MOST, LEAST, CENTER, RES>;
   const int fixed = held * V * 4 * (a.bias ? 2 : 1), stage = held * 16 + 16 + (RES ? held * 16 : 0);
   const RowPlan p = plan_rows(by_registers, fixed, stage);
-  const int shifts = shifts_of(a.d, V), span = fwd_span(a.T, p.per_sm, kFwdSpanShift), smem = fixed + p.stages * stage;
+  const int shifts = shifts_of(a.d, V), span = fwd_span(a.T, p.per_sm, kFwdRounds, kFwdSpanShift), smem = fixed + p.stages * stage;
   const cudaError_t e = allow_shared(kernel, smem);
   if (e != cudaSuccess) return e;
   kernel<<<(unsigned)(ceil_div(a.T, (int64_t)span * shifts) * shifts), threads, smem, st>>>(a, span, p.stages, shifts);
@@ -832,7 +839,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_bwd_kernel(BwdParams a, int st
   uint32_t mask_next = mask_of(first + (stages - 1) * step);
   float r_next = first < a.T ? a.rstd[first] : 0.0f, mu_next = CENTER && first < a.T ? a.mean[first] : 0.0f;
 #pragma unroll
-  for (int i = 0; i < NV; ++i) spread_weights<V>(s_w, a.weight, a.w_bf16, 1.0f, held, i * threads + tid, column(i), d);
+  for (int i = 0; i < NV; ++i) spread_weights<V, SHIFT>(s_w, a.weight, a.w_bf16, 1.0f, held, i * threads + tid, column(i), d);
   float2 dw[NV * P], db[DB ? NV * P : 1];
 #pragma unroll
   for (int e = 0; e < NV * P; ++e) {
@@ -916,34 +923,53 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_bwd_kernel(BwdParams a, int st
         if (CENTER) p2 = add2(p2, up);
       }
     }
-    float s1 = warp_sum(p1.x + p1.y), s2 = CENTER ? warp_sum(p2.x + p2.y) : 0.0f;
+    float s1 = p1.x + p1.y, s2 = p2.x + p2.y;
+    if (CENTER) {
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const float2 v = add2(make_float2(s1, s2), make_float2(__shfl_xor_sync(0xffffffffu, s1, o), __shfl_xor_sync(0xffffffffu, s2, o)));
+        s1 = v.x;
+        s2 = v.y;
+      }
+    } else {
+      s1 = warp_sum(s1);
+    }
     if (warps > 1) {
       if (lane == 0) s_sum[buf][warp] = make_float2(s1, s2);
       __syncthreads();
       s1 = s2 = 0.0f;
+#pragma unroll 4
       for (int q = 0; q < warps; ++q) {
         const float2 v = s_sum[buf][q];
         s1 += v.x;
         if (CENTER) s2 += v.y;
       }
     }
-    s1 *= -inv_d;
-    s2 *= -inv_d;
+    // dx = r (up - mean up - xh mean(up xh)) + dh = (w r) g + along x + level + dh
+    const float along = -inv_d * s1 * r * r, level = CENTER ? -fmaf(along, mu, inv_d * s2 * r) : 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = column(i);
+      const int c = i * threads + tid, j = column(i);
       if (j >= d) continue;
-      float2 xh[P], g[P], w[P];
-      normalised(i, xh);
+      float2 g[P], w[P];
+      Pack<X, V> px;
+      if (SHIFT && staged) px = staged_chunk<X, V>(s_own, j, d);
+      else px = load_pack<X, V>(reinterpret_cast<const X*>(s + c * 16));
       gradient(i, g);
       weights(i, w);
-      Pack<X, V> ph;
-      zero_pack(ph);
-      if (a.dh) ph = load_pack<X, V>(reinterpret_cast<const X*>(s + at.x + at.dy) + (i * threads + tid) * V);
+      if (a.dh) {
+        const Pack<X, V> ph = load_pack<X, V>(reinterpret_cast<const X*>(s + at.x + at.dy) + c * V);
 #pragma unroll
-      for (int p = 0; p < P; ++p) {
-        const float2 up = CENTER ? fma2(g[p], w[p], both(s2)) : mul2(g[p], w[p]);
-        w[p] = fma2(fma2(xh[p], both(s1), up), both(r), pair_of(ph, p));
+        for (int p = 0; p < P; ++p) {
+          const float2 rest = CENTER ? add2(pair_of(ph, p), both(level)) : pair_of(ph, p);
+          w[p] = fma2(mul2(w[p], both(r)), g[p], fma2(pair_of(px, p), both(along), rest));
+        }
+      } else {
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+          const float2 rest = CENTER ? fma2(pair_of(px, p), both(along), both(level)) : mul2(pair_of(px, p), both(along));
+          w[p] = fma2(mul2(w[p], both(r)), g[p], rest);
+        }
       }
       store_chunk<X, V, SHIFT>(out, j, d, round_pack<X, V>(&w[0].x));
     }
@@ -1030,23 +1056,22 @@ __global__ void __launch_bounds__(256) ln_bwd_long_cols_kernel(BwdParams a) {
   if (a.want_db) row[(int64_t)a.want_dw * a.d + c] = db;
 }
 
-// dw and db from the blocks' partial rows, in their order: 32 columns a block, eight warps that take every eighth partial row each.
-__global__ void __launch_bounds__(256) ln_bwd_columns_kernel(const float* __restrict__ partial, int parts, int64_t width, int32_t d,
-                                                             void* dw, void* db, int bf16, int accumulate) {
-  __shared__ float s_sum[8][32];
+// dw and db from the blocks' partial rows, in their order: 32 columns a block, and as many warps as leave each some four rows.
+__global__ void __launch_bounds__(1024) ln_bwd_columns_kernel(const float* __restrict__ partial, int parts, int64_t width, int32_t d, void* dw,
+                                                              void* db, int bf16, int accumulate) {
+  __shared__ float s_sum[32][32];
   pdl_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int64_t j = (int64_t)blockIdx.x * 32 + lane;
   float sum = 0.0f;
   if (j < width) {
 #pragma unroll 8
-    for (int p = warp; p < parts; p += 8) sum += partial[(int64_t)p * width + j];
+    for (int p = warp; p < parts; p += warps) sum += partial[(int64_t)p * width + j];
   }
   s_sum[warp][lane] = sum;
   __syncthreads();
   if (warp != 0 || j >= width) return;
-#pragma unroll
-  for (int q = 1; q < 8; ++q) sum += s_sum[q][lane];
+  for (int q = 1; q < warps; ++q) sum += s_sum[q][lane];
   void* out = dw && j < d ? dw : db;
   const int64_t at = j < d ? j : j - d;
   if (bf16) {
@@ -1060,13 +1085,14 @@ __global__ void __launch_bounds__(256) ln_bwd_columns_kernel(const float* __rest
 }
 
 // The launch of a backward pass.  The number of blocks is at most bwd_blocks_most(), so that the scratch can be sized by d and T alone.
-int bwd_per_sm(int threads) { return threads == 32 ? 16 : threads <= 128 ? 512 / threads : threads <= 1024 ? 1024 / threads : 1; }
+int bwd_per_sm(int threads) { return threads <= 512 ? 512 / threads : 1; }
 int64_t bwd_blocks_most(int64_t T, int32_t d) {
   int64_t most = T < 64 ? T : 64;          // of rows that take the long form
   if (d > kRowMost) return most;
   for (int v : {4, 8}) {                   // rows of fp32 and of bf16; shifted rows may have a chunk more
-    for (int64_t chunks : {ceil_div(d, v), ceil_div(d + v - 1, v)}) {
-      const int64_t n = (int64_t)sm_count() * bwd_per_sm(row_threads(chunks, row_form(chunks, v)));
+    for (bool shift : {false, true}) {
+      const int64_t chunks = ceil_div(shift ? d + v - 1 : d, v);
+      const int64_t n = (int64_t)sm_count() * bwd_per_sm(row_threads(chunks, row_form(chunks, v, shift)));
       most = n > most ? n : most;
     }
   }
@@ -1096,7 +1122,7 @@ cudaError_t pick_bwd(const BwdParams& a, int* blocks, cudaStream_t st) {
   constexpr int V = 16 / (int)sizeof(X);
   const bool shift = !(a.d % V == 0 && (a.T == 1 || a.ldx % V == 0));
   const int64_t chunks = ceil_div(shift ? a.d + V - 1 : a.d, V);
-  const int nv = row_form(chunks, V), threads = row_threads(chunks, nv);
+  const int nv = row_form(chunks, V, shift), threads = row_threads(chunks, nv);
   const BwdShared at = bwd_shared(threads * nv, V, a.dy_bf16 ? 2 : 4, a.dh != nullptr, shift);
   if (a.d > kRowMost || threads > 1024 || at.weights + at.stage + kSharedOwn > kSharedMost) {
     *blocks = (int)(a.T < 64 ? a.T : 64);
@@ -1110,8 +1136,12 @@ cudaError_t pick_bwd(const BwdParams& a, int* blocks, cudaStream_t st) {
   }
   auto form = [&](auto sh) {
     constexpr bool S = decltype(sh)::value;
-    if (nv == 1 && chunks <= 32) return run_bwd<X, 1, 32, 16, S, CENTER, DB>(a, chunks, blocks, st);
-    if (nv == 32 / V) return run_bwd<X, 32 / V, 128, 4, S, CENTER, DB>(a, chunks, blocks, st);
+    if (chunks <= 32) return run_bwd<X, 1, 32, 16, S, CENTER, DB>(a, chunks, blocks, st);
+    if constexpr (S && V == 8) {
+      if (nv == 32 / V) return run_bwd<X, 32 / V, 128, 4, S, CENTER, DB>(a, chunks, blocks, st);
+    }
+    if (threads <= 256) return run_bwd<X, 16 / V, 256, 2, S, CENTER, DB>(a, chunks, blocks, st);
+    if (threads <= 512) return run_bwd<X, 16 / V, 512, 1, S, CENTER, DB>(a, chunks, blocks, st);
     return run_bwd<X, 16 / V, 1024, 1, S, CENTER, DB>(a, chunks, blocks, st);
   };
   return shift ? form(std::true_type{}) : form(std::false_type{});
@@ -1166,7 +1196,7 @@ cudaError_t launch_layernorm_bwd(const LayerNormBwd& q, char* ws, cudaStream_t s
   const int64_t width = (int64_t)(a.want_dw + a.want_db) * q.d;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)ceil_div(width, 32));
-  cfg.blockDim = dim3(256);
+  cfg.blockDim = dim3(32u * (unsigned)(blocks >= 128 ? 32 : ceil_div(blocks, 4)));
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
