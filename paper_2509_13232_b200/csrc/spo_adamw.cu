@@ -33,9 +33,9 @@ __device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.lau
 // ---------------------------------------------------------------------------
 // gradient norm
 // ---------------------------------------------------------------------------
-constexpr int kNormThreads = 256;
-constexpr int kNormChunk = 8192;                    // elements that a block takes at a time
-constexpr int kNormBlocksPerSm = 8;
+constexpr int kNormThreads = 128, kFinishThreads = 512;
+constexpr int kNormChunk = 4096;                    // elements that a block takes at a time
+constexpr int kNormBlocksPerSm = 32;                // more than fit at once: the SMs do not run at one pace
 constexpr int kGradsMost = 1200;                    // tensors per launch: 24 bytes each, of the 32764 bytes that parameters may have
 constexpr int kGradsFew = 40;
 
@@ -62,18 +62,26 @@ __device__ __forceinline__ int find_tensor(const Table& tab, uint64_t chunk) {
   return lo;
 }
 
-// Squares of one thread's share are summed in fp32; where that sum leaves the range in which this loses nothing it is formed again
-// in fp64.
-template <int N>
+// The sum of a few squares as an fp32 sum and what its roundings (and, but for bf16 values, the products') took off: good to 2^-44, so that
+// the norm and the factor do not depend on the order of the terms once they are rounded to fp32.  Where the sum leaves the range in
+// which this holds it is formed again in fp64 (whose conversions would be the bound of the whole if every value took them).
+template <bool BF16, int N>
 __device__ __forceinline__ double sum_squares(const float (&f)[N]) {
-  float s = 0.0f;
+  float2 s = both(0.0f), rest = both(0.0f);
 #pragma unroll
-  for (int k = 0; k < N; ++k) s = fmaf(f[k], f[k], s);
-  if (s > 0x1p-80f && s < INFINITY) return (double)s;
+  for (int k = 0; k < N; k += 2) {
+    const float2 x = make_float2(f[k], k + 1 < N ? f[k + 1] : 0.0f), p = mul2(x, x), t = add2(s, p), back = sub2(t, s);
+    float2 off = add2(sub2(s, sub2(t, back)), sub2(p, back));
+    if (!BF16) off = add2(off, fma2(x, x, make_float2(-p.x, -p.y)));
+    rest = add2(rest, off);
+    s = t;
+  }
+  const float least = N > 1 ? fminf(s.x, s.y) : s.x, most = fmaxf(s.x, s.y);
+  if (least > 0x1p-60f && most < INFINITY) return ((double)s.x + (double)s.y) + (double)(rest.x + rest.y);
   float any = 0.0f;
 #pragma unroll
   for (int k = 0; k < N; ++k) any = fmaxf(any, fabsf(f[k]));
-  if (s == 0.0f && any == 0.0f) return 0.0;         // (a NaN is in s)
+  if (s.x == 0.0f && s.y == 0.0f && any == 0.0f) return 0.0;      // (a NaN is in them)
   double d = 0.0;
 #pragma unroll
   for (int k = 0; k < N; ++k) d = fma((double)f[k], (double)f[k], d);
@@ -123,27 +131,33 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
         uint4 q[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) q[k] = __ldcs(p + k * kNormThreads);
+        float f[32];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const float f[8] = {low_bf16(q[k].x), high_bf16(q[k].x), low_bf16(q[k].y), high_bf16(q[k].y),
-                              low_bf16(q[k].z), high_bf16(q[k].z), low_bf16(q[k].w), high_bf16(q[k].w)};
-          sum += sum_squares(f);
+          const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            f[8 * k + 2 * i] = low_bf16(w[i]);
+            f[8 * k + 2 * i + 1] = high_bf16(w[i]);
+          }
         }
+        sum += sum_squares<true>(f);
       } else if (whole) {
         const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(g) + base) + threadIdx.x;
         float4 q[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) q[k] = __ldcs(p + k * kNormThreads);
+        float f[32];
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-          const float f[8] = {q[k].x, q[k].y, q[k].z, q[k].w, q[k + 1].x, q[k + 1].y, q[k + 1].z, q[k + 1].w};
-          sum += sum_squares(f);
+        for (int k = 0; k < 8; ++k) {
+          f[4 * k] = q[k].x; f[4 * k + 1] = q[k].y; f[4 * k + 2] = q[k].z; f[4 * k + 3] = q[k].w;
         }
+        sum += sum_squares<false>(f);
       } else {
         const int64_t end = n - base < kNormChunk ? n : base + kNormChunk;
         for (int64_t e = base + threadIdx.x; e < end; e += kNormThreads) {
           const float f[1] = {bf16 ? low_bf16(static_cast<const uint16_t*>(g)[e]) : static_cast<const float*>(g)[e]};
-          sum += sum_squares(f);
+          sum += sum_squares<false>(f);
         }
       }
     }
@@ -159,13 +173,13 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
   }
 }
 
-__global__ void __launch_bounds__(kNormThreads) grad_norm_finish_kernel(const double* partial, int parts, float max_norm, float scale,
+__global__ void __launch_bounds__(kFinishThreads) grad_norm_finish_kernel(const double* partial, int parts, float max_norm, float scale,
                                                                         float* out, int32_t* d_status) {
-  __shared__ double s_part[kNormThreads / 32];
+  __shared__ double s_part[kFinishThreads / 32];
   pdl_wait();
   double sum = 0.0;
 #pragma unroll 4
-  for (int p = threadIdx.x; p < parts; p += kNormThreads) sum += partial[p];
+  for (int p = threadIdx.x; p < parts; p += kFinishThreads) sum += partial[p];
   sum = block_sum(sum, s_part);
   if (threadIdx.x == 0) finish_norm(sum, max_norm, scale, out, d_status);
 }
@@ -199,7 +213,7 @@ constexpr int kStepBlocksPerSm = 24;
 // up to 16 and 516 (369) with up to 6, 32 bits 694 us and 682; 11 million in 8 bits: 37 us with one round, 30 with three.
 constexpr int kSpanMost8 = 16, kSpanMost32 = 6, kRounds = 3;
 constexpr int kTensorsMost = 400;                   // tensors per launch, 80 bytes each
-constexpr int kTensorsFew = 12;
+constexpr int kTensorsSome = 136, kTensorsFew = 12;  // smaller tables for shorter lists: what a launch costs the host grows with them
 
 constexpr float kMFloor = 0x1p-100f, kVFloor = 0x1p-90f;     // least scales: 1 / scale and scale / 255^4 are normal numbers
 constexpr float kSquareMost = 0x1p120f;                      // of a scaled gradient: beyond it (or NaN) the element is left out
@@ -319,9 +333,8 @@ __device__ __forceinline__ float encode_v(float v, float to_unit) {
 __device__ __forceinline__ float2 encode_m2(float2 m, float to_unit) { return make_float2(encode_m(m.x, to_unit), encode_m(m.y, to_unit)); }
 __device__ __forceinline__ float2 encode_v2(float2 v, float to_unit) { return make_float2(encode_v(v.x, to_unit), encode_v(v.y, to_unit)); }
 
-// Four consecutive elements, aligned, as they are in memory.  Loads of a step are issued where they are written, all of them before the
-// first one is waited for: left to the compiler, those of the weights come after the moments' arithmetic, and their latency is paid
-// apart (8 bits: 388 and 516 us).
+// Four consecutive elements, aligned, as they are in memory.  The loads of a chunk are issued where they are written, all of them before the
+// first one is waited for, and past the L1 cache: nothing is read twice.
 template <bool IS16>
 struct Raw4 {
   uint32_t x[IS16 ? 2 : 4];
@@ -750,7 +763,7 @@ cudaError_t launch_grad_norm(const spo_grad_tensor* grads, int count, float max_
   if (have == 1) return cudaSuccess;               // the one block has written the results
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(1);
-  cfg.blockDim = dim3(kNormThreads);
+  cfg.blockDim = dim3(kFinishThreads);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -777,8 +790,9 @@ cudaError_t launch_adamw(const spo_adamw_tensor* tensors, int count, const float
   for (int from = 0; from < end;) {
     const int left = end - from, take = left < kTensorsMost ? left : kTensorsMost;
     a.advance = take == left;
-    const cudaError_t e = take <= kTensorsFew ? step_launch<kTensorsFew>(tensors, from, from + take, a, p, st)
-                                              : step_launch<kTensorsMost>(tensors, from, from + take, a, p, st);
+    const cudaError_t e = take <= kTensorsFew    ? step_launch<kTensorsFew>(tensors, from, from + take, a, p, st)
+                          : take <= kTensorsSome ? step_launch<kTensorsSome>(tensors, from, from + take, a, p, st)
+                                                 : step_launch<kTensorsMost>(tensors, from, from + take, a, p, st);
     if (e != cudaSuccess) return e;
     from += take;
   }

@@ -449,3 +449,17 @@ def test_the_tables_refuse():
     with pytest.raises(ValueError):
         B.spo_adamw_decode(x(dt=torch.int8), x(3), None, None, x(), None)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_norm_and_factor_are_rounded_once(bf16):
+    """The codes of 8-bit states hang on the factor's last bit, so it is the definition's: rounded from a sum that is good to 2^-44."""
+    import torch
+    for seed in range(20):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        n = int(10 ** (2 + seed / 4))
+        x = (torch.randn(n, generator=g, device="cuda") * torch.exp(2 * torch.randn(n, generator=g, device="cuda"))).to(torch.bfloat16 if bf16 else torch.float32)
+        (norm, factor, _, _), _ = run_norm([x[:n // 3], x[n // 3:]], 1.0)
+        want = float(x.double().square().sum().sqrt())
+        assert norm == float(F(want)) and factor == float(F(min(1.0, 1.0 / want)))

@@ -397,3 +397,26 @@ def test_the_binding_refuses():
         with pytest.raises(err):
             B.spo_layernorm_bwd(**{**back, **bad})
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("d,pad", [(4096, 0), (1000, 0), (2730, 0), (1365, 3), (8192, 0)])
+def test_masked_rows_between_others(d, pad):
+    """A masked row takes no part in its block's exchange of partial sums; the rows around it come out as in a batch without it, bit
+    for bit, however the masked ones lie."""
+    import torch
+    from paper_2509_13232_b200 import binding as B
+    T = 6000
+    c = case(d, T, d, O.LAYER, True, True, True, pad=pad)
+    dy, dh = grads(1, c, False, True)
+    whole, back = run_fwd(c), run_bwd(c, dy, dh)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d)
+    for pattern in (torch.arange(T, device="cuda") % 2, torch.arange(T, device="cuda") // 4 % 2, torch.rand(T, generator=g, device="cuda") < 0.5):
+        c["mask"] = pattern.to(torch.uint8)
+        on = c["mask"] != 0
+        for _ in range(3):
+            got = run_fwd(c)
+            assert torch.equal(got["y"][on], whole["y"][on]) and torch.equal(got["rstd"][on], whole["rstd"][on]) and got["status"] == 0
+            assert float(got["y"][~on].abs().sum()) == 0
+            b = run_bwd(c, dy, dh, mean=back["mean"], rstd=back["rstd"])
+            assert torch.equal(b["dx"][on], back["dx"][on]) and float(b["dx"][~on].abs().sum()) == 0
