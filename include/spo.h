@@ -668,7 +668,7 @@ int32_t spo_layernorm_fwd(const void* x, int64_t ldx, const void* residual, int3
  *             over all rows in fp32, in an order that depends on T, d and the device alone: results repeat bit for bit
  *   ws        device scratch, spo_workspace_bytes(SPO_WS_LAYERNORM_BWD, T, d, 0, 0, 0, 0) bytes; it serves shorter calls too.  Optional
  *             where neither dweight nor dbias is wanted
- * T = 0 zeroes dweight and dbias (unless accumulating).
+ * T = 0 zeroes dweight and dbias (unless accumulating).  The call sets no status bit: what is not finite goes where the formula takes it.
  */
 int32_t spo_layernorm_bwd(const void* dy, int32_t dy_dtype, const void* x, int64_t ldx, int32_t dtype, const void* weight,
                           int32_t w_dtype, const uint8_t* mask, const float* mean, const float* rstd, const void* dh,
@@ -686,7 +686,8 @@ int32_t spo_layernorm_bwd(const void* dy, int32_t dy_dtype, const void* x, int64
  *           to its element (16 bytes is fastest)
  *   out     device out [4] fp32 = (norm, factor, 1 if norm is finite else 0, 0).  factor is NaN where norm is not finite:
  *           spo_adamw_update then takes no step.  Such a norm sets SPO_DEV_NONFINITE
- *   ws      device scratch, spo_workspace_bytes(SPO_WS_GRAD_NORM, ...) bytes (the same for all calls)
+ *   ws      device scratch, spo_workspace_bytes(SPO_WS_GRAD_NORM, ...) bytes (the same for all calls); neither it nor out may lie in a
+ *           gradient
  * Up to 1200 tensors are one launch (and one small one behind it).
  */
 typedef struct spo_grad_tensor {
@@ -755,7 +756,7 @@ int32_t spo_adamw_update(const spo_adamw_tensor* tensors /* host */, int32_t n_t
 
 /*
  * Values of 8-bit states, for inspection or for going on in 32 bits: m_out[i], v_out[i] fp32 from the codes and scales of
- * spo_adamw_update.  m with m_scale and m_out, or v with v_scale and v_out, may be NULL together.
+ * spo_adamw_update.  m with m_scale and m_out, or v with v_scale and v_out, may be NULL together.  The outputs share memory with nothing.
  */
 int32_t spo_adamw_decode(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n,
                          float* m_out, float* v_out, void* stream);

@@ -870,6 +870,11 @@ int32_t spo_grad_norm(const spo_grad_tensor* grads, int32_t n_grads, float max_n
     if ((reinterpret_cast<uintptr_t>(q.g) & (float_size(q.dtype) - 1)) != 0) return SPO_ERR_BAD_ALIGNMENT;
   }
   if (!aligned16(ws) || (reinterpret_cast<uintptr_t>(out) & 15) != 0) return SPO_ERR_BAD_ALIGNMENT;
+  if (overlap(out, 16, ws, ws_bytes)) return SPO_ERR_INVALID_ARG;
+  for (int i = 0; i < n_grads; ++i) {
+    const wide_t bytes = (wide_t)grads[i].n * float_size(grads[i].dtype);
+    if (grads[i].n > 0 && (overlap(out, 16, grads[i].g, bytes) || overlap(ws, ws_bytes, grads[i].g, bytes))) return SPO_ERR_INVALID_ARG;
+  }
   if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
   if (ws_bytes < grad_norm_ws_bytes()) return SPO_ERR_WORKSPACE_TOO_SMALL;
   cudaError_t e = launch_grad_norm(grads, n_grads, max_norm, grad_scale, out, (char*)ws, d_status, (cudaStream_t)stream);
@@ -922,6 +927,12 @@ int32_t spo_adamw_decode(const int8_t* m, const float* m_scale, const uint8_t* v
     return SPO_ERR_INVALID_ARG;
   for (const float* p : {m_scale, v_scale, (const float*)m_out, (const float*)v_out})
     if ((reinterpret_cast<uintptr_t>(p) & 3) != 0) return SPO_ERR_BAD_ALIGNMENT;
+  const wide_t codes = (wide_t)n, values = codes * 4, scales = (codes + SPO_ADAMW_BLOCK - 1) / SPO_ADAMW_BLOCK * 4;
+  for (const float* out : {m ? m_out : nullptr, v ? v_out : nullptr})
+    if (clash(out, values, m, codes, false) || clash(out, values, v, codes, false) || clash(out, values, m_scale, scales, false) ||
+        clash(out, values, v_scale, scales, false))
+      return SPO_ERR_INVALID_ARG;
+  if (m && v && clash(m_out, values, v_out, values, false)) return SPO_ERR_INVALID_ARG;
   if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
   cudaError_t e = launch_adamw_decode(m, m_scale, v, v_scale, n, m_out, v_out, (cudaStream_t)stream);
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);

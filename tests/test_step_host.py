@@ -248,6 +248,16 @@ def test_decode_refuses(lib, no_gpu):
         assert no_gpu(d(**good))
 
 
+def test_results_share_memory_with_nothing(lib, no_gpu):
+    assert norm(lib, out=at(0, 192)) == B.ERR_INVALID_ARG and norm(lib, ws=at(0, 192)) == B.ERR_INVALID_ARG
+    assert norm(lib, ws=at(1)) == B.ERR_INVALID_ARG
+    assert no_gpu(norm(lib, out=at(0, 208), ws=at(3))) and no_gpu(norm(lib, n=0, out=at(0)))
+    d = lambda m=at(0), ms=at(1), v=at(2), vs=at(3), n=300, mo=at(4), vo=at(5): lib.spo_adamw_decode(m, ms, v, vs, n, mo, vo, None)  # noqa: E731
+    for bad in (dict(mo=at(0)), dict(mo=at(0, 296)), dict(mo=at(2)), dict(vo=at(1, 4)), dict(vo=at(3)), dict(vo=at(4, 1196)), dict(vo=at(0, 196))):
+        assert d(**bad) == B.ERR_INVALID_ARG
+    assert no_gpu(d(mo=at(0, 300))) and no_gpu(d(vo=at(4, 1200))) and no_gpu(d(n=0, mo=at(0)))
+
+
 def test_scratch_sizes_of_the_step():
     size = B.spo_workspace_bytes
     for d in (1, 7, 64, 1000, 4096, 8192, 8200, 16384, 20000, 1 << 20):
