@@ -679,8 +679,7 @@ int32_t spo_layernorm_bwd(const void* dy, int32_t dy_dtype, const void* x, int64
  * Global norm of many gradients and the factor that clips them (Algorithm 1, "update the policy parameters"; the paper leaves the
  * optimiser open): with s = grad_scale (1 / loss scale; 1),
  *   norm = |s| sqrt( sum over all tensors and elements of g^2 ),   factor = s min(1, max_norm / norm)    (max_norm <= 0: factor = s).
- * Sums of a few squares to 2^-44 of themselves, these in fp64 in a fixed order: results repeat bit for bit, and are the exact norm and
- * factor rounded once (up to a near tie).
+ * Summed in fp64 in a fixed order: results repeat bit for bit, and are the exact norm and factor rounded once (up to a near tie).
  *
  *   grads   host in [n_grads], read before the call returns; each g is a device pointer to n elements (n = 0 is allowed), aligned
  *           to its element (16 bytes is fastest)

@@ -62,29 +62,35 @@ __device__ __forceinline__ int find_tensor(const Table& tab, uint64_t chunk) {
   return lo;
 }
 
-// The sum of a few squares as an fp32 sum and what its roundings (and, but for bf16 values, the products') took off: good to 2^-44, so that
-// the norm and the factor do not depend on the order of the terms once they are rounded to fp32.  Where the sum leaves the range in
-// which this holds it is formed again in fp64 (whose conversions would be the bound of the whole if every value took them).
+// The sum of the squares of a few values in fp64, whose products of fp32 values are exact, so that the norm and the factor do not depend on
+// the order of the terms once they are rounded to fp32.  The conversion instructions would be the bound of the whole: |x| 2^-128 is put
+// together from the bits instead, as if x were a normal number.  A zero then counts as 2^-127 and an infinity as 2^128; a sum that this
+// could change, or that holds one, is formed again from converted values.
+__device__ __forceinline__ double wide_normal(uint32_t w) { return __hiloint2double((int)((w >> 3 & 0x0fffffffu) | 0x30000000u), (int)(w << 29)); }
+__device__ __forceinline__ double wide_low(uint32_t w) { return __hiloint2double((int)((w << 13 & 0x0fffe000u) | 0x30000000u), 0); }
+__device__ __forceinline__ double wide_high(uint32_t w) { return __hiloint2double((int)((w >> 3 & 0x0fffe000u) | 0x30000000u), 0); }
 template <bool BF16, int N>
-__device__ __forceinline__ double sum_squares(const float (&f)[N]) {
-  float2 s = both(0.0f), rest = both(0.0f);
+__device__ __forceinline__ double sum_squares(const uint32_t (&w)[N]) {
+  double s[2] = {0.0, 0.0};
 #pragma unroll
-  for (int k = 0; k < N; k += 2) {
-    const float2 x = make_float2(f[k], k + 1 < N ? f[k + 1] : 0.0f), p = mul2(x, x), t = add2(s, p), back = sub2(t, s);
-    float2 off = add2(sub2(s, sub2(t, back)), sub2(p, back));
-    if (!BF16) off = add2(off, fma2(x, x, make_float2(-p.x, -p.y)));
-    rest = add2(rest, off);
-    s = t;
+  for (int k = 0; k < N; ++k) {
+    const double x = BF16 ? wide_low(w[k]) : wide_normal(w[k]);
+    s[k & 1] = fma(x, x, s[k & 1]);
+    if (BF16) s[k & 1] = fma(wide_high(w[k]), wide_high(w[k]), s[k & 1]);
   }
-  const float least = N > 1 ? fminf(s.x, s.y) : s.x, most = fmaxf(s.x, s.y);
-  if (least > 0x1p-60f && most < INFINITY) return ((double)s.x + (double)s.y) + (double)(rest.x + rest.y);
-  float any = 0.0f;
+  const double sum = s[0] + s[1];
+  if (sum > 0x1p-446 && sum < 1.0) return sum * 0x1p256;
+  uint32_t any = 0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) any = fmaxf(any, fabsf(f[k]));
-  if (s.x == 0.0f && s.y == 0.0f && any == 0.0f) return 0.0;      // (a NaN is in them)
+  for (int k = 0; k < N; ++k) any |= w[k];
+  if ((any & (BF16 ? 0x7fff7fffu : 0x7fffffffu)) == 0) return 0.0;
   double d = 0.0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) d = fma((double)f[k], (double)f[k], d);
+  for (int k = 0; k < N; ++k) {
+    const double x = BF16 ? low_bf16(w[k]) : __uint_as_float(w[k]);
+    d = fma(x, x, d);
+    if (BF16) d = fma((double)high_bf16(w[k]), (double)high_bf16(w[k]), d);
+  }
   return d;
 }
 
@@ -131,33 +137,28 @@ __global__ void __launch_bounds__(kNormThreads) grad_norm_kernel(const __grid_co
         uint4 q[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) q[k] = __ldcs(p + k * kNormThreads);
-        float f[32];
+        uint32_t w[16];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint32_t w[4] = {q[k].x, q[k].y, q[k].z, q[k].w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            f[8 * k + 2 * i] = low_bf16(w[i]);
-            f[8 * k + 2 * i + 1] = high_bf16(w[i]);
-          }
+          w[4 * k] = q[k].x; w[4 * k + 1] = q[k].y; w[4 * k + 2] = q[k].z; w[4 * k + 3] = q[k].w;
         }
-        sum += sum_squares<true>(f);
+        sum += sum_squares<true>(w);
       } else if (whole) {
-        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(g) + base) + threadIdx.x;
-        float4 q[8];
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(g) + base) + threadIdx.x;
+        uint4 q[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) q[k] = __ldcs(p + k * kNormThreads);
-        float f[32];
+        uint32_t w[32];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          f[4 * k] = q[k].x; f[4 * k + 1] = q[k].y; f[4 * k + 2] = q[k].z; f[4 * k + 3] = q[k].w;
+          w[4 * k] = q[k].x; w[4 * k + 1] = q[k].y; w[4 * k + 2] = q[k].z; w[4 * k + 3] = q[k].w;
         }
-        sum += sum_squares<false>(f);
+        sum += sum_squares<false>(w);
       } else {
         const int64_t end = n - base < kNormChunk ? n : base + kNormChunk;
         for (int64_t e = base + threadIdx.x; e < end; e += kNormThreads) {
-          const float f[1] = {bf16 ? low_bf16(static_cast<const uint16_t*>(g)[e]) : static_cast<const float*>(g)[e]};
-          sum += sum_squares<false>(f);
+          const uint32_t w[1] = {bf16 ? (uint32_t)static_cast<const uint16_t*>(g)[e] << 16 : static_cast<const uint32_t*>(g)[e]};
+          sum += sum_squares<false>(w);
         }
       }
     }

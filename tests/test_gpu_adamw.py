@@ -7,6 +7,8 @@ and its own rounding u.  A weight moves by  step m / (sqrt(v) root + eps) + pull
 the weight's own rounding is u (fp32) or 2^-8 (bf16) of its value.
 """
 
+import math
+
 import numpy as np
 import pytest
 
@@ -453,7 +455,7 @@ def test_the_tables_refuse():
 
 @pytest.mark.parametrize("bf16", [False, True])
 def test_norm_and_factor_are_rounded_once(bf16):
-    """The codes of 8-bit states hang on the factor's last bit, so it is the definition's: rounded from a sum that is good to 2^-44."""
+    """The codes of 8-bit states hang on the factor's last bit, so it is the definition's: rounded once from a sum in 64 bits."""
     import torch
     for seed in range(20):
         g = torch.Generator(device="cuda")
@@ -463,3 +465,34 @@ def test_norm_and_factor_are_rounded_once(bf16):
         (norm, factor, _, _), _ = run_norm([x[:n // 3], x[n // 3:]], 1.0)
         want = float(x.double().square().sum().sqrt())
         assert norm == float(F(want)) and factor == float(F(min(1.0, 1.0 / want)))
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_norm_of_zeros_and_few_extremes(bf16, offset):
+    """Chunks of zeros (of both signs) with single values from the whole range, aligned and not, and infinities and NaN anywhere in one.
+    All squares are exact in 64 bits and few, so the norm is the exact one rounded once; below fp32's normal numbers, to its grid."""
+    import torch
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    least = 2.0**-133 if bf16 else 2.0**-149
+    n = 3 * 4096 + 17
+    base = torch.zeros(n + 1, device="cuda", dtype=dtype)
+    x = base[offset:offset + n]
+    x[1::3] = -0.0
+    assert run_norm([x], 1.0)[0] == [0.0, 1.0, 1.0, 0.0]
+    for value in (least, 3 * least, 2.0**-126, 2.0**-112, 2.0**-95, 2.0**-90, 2.0**-50, 1.0, 2.0**62, 2.0**100, 1.75 * 2.0**127):
+        for places in ((0,), (4095,), (n - 1,), (7, 8, 4096, n - 2)):
+            x.zero_()
+            x[list(places)] = value
+            want = value * math.sqrt(len(places))
+            norm, factor, fine, _ = run_norm([x], 1.0)[0]
+            if want < 3.4e38:
+                assert norm == float(F(want)) and factor == float(F(min(1.0, 1.0 / want))) and fine == 1.0
+            else:
+                assert norm == math.inf and math.isnan(factor) and fine == 0.0
+    for value in (math.inf, -math.inf, math.nan):
+        for place in (0, 5000, n - 1):
+            x.fill_(0.5)
+            x[place] = value
+            norm, factor, fine, _ = run_norm([x], 1.0)[0]
+            assert not norm < math.inf and math.isnan(factor) and fine == 0.0
