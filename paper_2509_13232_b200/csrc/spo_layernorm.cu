@@ -68,13 +68,6 @@ __device__ __forceinline__ void zero_pack(Pack<T, V>& r) {
   for (int i = 0; i < (int)(sizeof(r.w) / 4); ++i) r.w[i] = 0u;
 }
 
-// Element k from its bits (for 16-bit types in the low half); the element was 0.
-template <typename T, int V>
-__device__ __forceinline__ void put_element(Pack<T, V>& r, int k, uint32_t bits) {
-  if constexpr (sizeof(T) == 4) r.w[k] = bits;
-  else r.w[k >> 1] |= bits << (16 * (k & 1));
-}
-
 template <typename T, int V>
 __device__ __forceinline__ float element(const Pack<T, V>& r, int k) {
   if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[k]);
@@ -247,14 +240,33 @@ __device__ __forceinline__ void blank(char* s, int j, int d) {
     if (!has_column(j, k, d)) store_pack(reinterpret_cast<T*>(s) + k, zero);
   }
 }
-// Columns j .. of a row that lies at s_row with its own shift.
+// Columns j .. of a row that lies in shared memory with its own shift, from the two aligned chunks that hold them: up to a chunk in front
+// of the row and one behind it are read, and count as zeros.
 template <typename T, int V>
-__device__ __forceinline__ Pack<T, V> staged_chunk(const T* s_row, int j, int d) {
-  Pack<T, V> r;
-  zero_pack(r);
+__device__ __forceinline__ Pack<T, V> staged_chunk(const char* s, int own, int j, int d) {
+  const int at = (own + j) * (int)sizeof(T), words = at >> 2 & 3, bits = 8 * (at & 3);          // (the same for all of a row)
+  const uint4* const p = reinterpret_cast<const uint4*>(s) + (at >> 4);
+  const uint4 lo = p[0], hi = p[1];
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  if (words & 2) {
 #pragma unroll
-  for (int k = 0; k < V; ++k)
-    if (has_column(j, k, d)) put_element<T, V>(r, k, load_pack<T, 1>(s_row + j + k).w[0]);
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  }
+  if (words & 1) {
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  }
+  Pack<T, V> r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r.w[i] = __funnelshift_r(w[i], w[i + 1], bits);
+  if (!is_whole<V, true>(j, d)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      constexpr int kEach = 4 / (int)sizeof(T);
+      if (!has_column(j, i * kEach, d)) r.w[i] &= kEach == 2 ? 0xffff0000u : 0u;
+      if (kEach == 2 && !has_column(j, 2 * i + 1, d)) r.w[i] &= 0x0000ffffu;
+    }
+  }
   return r;
 }
 
@@ -574,14 +586,14 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
       if (!staged) blank<X, V>(s + c * 16, c * V - shift, d);
       if (RES) blank<X, V>(s + x_bytes + c * 16, c * V - shift, d);
     }
-    const X* const s_own = reinterpret_cast<const X*>(s) + (staged ? (int)((t * a.ldx) % V) : 0);
+    const int own = staged ? (int)((t * a.ldx) % V) : 0;
     float2 f[NV * P], part = both(0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = i * threads + tid, j = column(i);
       if (j < d) {
         Pack<X, V> q;
-        if (staged) q = staged_chunk<X, V>(s_own, j, d);
+        if (staged) q = staged_chunk<X, V>(s, own, j, d);
         else q = load_pack<X, V>(reinterpret_cast<const X*>(s + c * 16));
         if (RES) {
           const Pack<X, V> pr = load_pack<X, V>(reinterpret_cast<const X*>(s + x_bytes + c * 16));
@@ -889,11 +901,11 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_bwd_kernel(BwdParams a, int st
         else blank<float, V>(s + at.x + c * V * 4, j, d);
       }
     }
-    const X* const s_own = reinterpret_cast<const X*>(s) + (staged ? (int)((t * a.ldx) % V) : 0);
+    const int own = staged ? (int)((t * a.ldx) % V) : 0;
     auto normalised = [&](int i, float2* xh) {          // of chunk i
       const int c = i * threads + tid;
       Pack<X, V> px;
-      if (SHIFT && staged) px = staged_chunk<X, V>(s_own, column(i), d);
+      if (SHIFT && staged) px = staged_chunk<X, V>(s, own, column(i), d);
       else px = load_pack<X, V>(reinterpret_cast<const X*>(s + c * 16));
 #pragma unroll
       for (int p = 0; p < P; ++p) xh[p] = mul2(CENTER ? add2(pair_of(px, p), both(-mu)) : pair_of(px, p), both(r));
@@ -959,7 +971,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_bwd_kernel(BwdParams a, int st
       if (j >= d) continue;
       float2 g[P], w[P];
       Pack<X, V> px;
-      if (SHIFT && staged) px = staged_chunk<X, V>(s_own, j, d);
+      if (SHIFT && staged) px = staged_chunk<X, V>(s, own, j, d);
       else px = load_pack<X, V>(reinterpret_cast<const X*>(s + c * 16));
       gradient(i, g);
       weights(i, w);
