@@ -271,20 +271,53 @@ __device__ __forceinline__ Pack<T, V> staged_chunk(const char* s, int own, int j
 }
 
 // A vector of weights (or biases) in shared memory as fp32, by chunk: quarter q of chunk c at q held + c.
-template <int V, bool SHIFT>
-__device__ __forceinline__ void spread_weights(float4* s, const void* p, int bf16, float none, int held, int c, int j, int d) {
-  float w[V];
-  if (!SHIFT && j < d) {
-    load_weights<V>(p, bf16, j, none, w);
-  } else {
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      w[k] = 0.0f;
-      if (has_column(j, k, d)) load_weights<1>(p, bf16, j + k, none, w + k);
-    }
-  }
+template <int V>
+__device__ __forceinline__ void spread_quarters(float4* s, int held, int c, const float* w) {
 #pragma unroll
   for (int q = 0; q < V / 4; ++q) s[q * held + c] = make_float4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+}
+template <int V>
+__device__ __forceinline__ void spread_weights(float4* s, const void* p, int bf16, int held, int c, int d) {
+  float w[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) w[k] = 0.0f;
+  if (c * V < d) load_weights<V>(p, bf16, c * V, 1.0f, w);
+  spread_quarters<V>(s, held, c, w);
+}
+// The same for all chunks of a thread of a shifted row: every load is on its way before the first one is waited for
+// (2003 rows of 2730 with a bias: 14.8 us so and 16.4 chunk by chunk).
+template <typename W, int V, int NV>
+__device__ __forceinline__ void spread_shifted(float4* s, const W* p, int held, int shift, int d, int tid, int threads) {
+  Pack<W, 1> q[NV * V];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int k = 0; k < V; ++k) q[i * V + k] = load_pack<W, 1>(p + min(max((i * threads + tid) * V - shift + k, 0), d - 1));
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = i * threads + tid, j = c * V - shift;
+    float w[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) w[k] = has_column(j, k, d) ? element(q[i * V + k], 0) : 0.0f;
+    spread_quarters<V>(s, held, c, w);
+  }
+}
+template <int V, int NV>
+__device__ __forceinline__ void spread_shifted(float4* s, const void* p, int bf16, int held, int shift, int d, int tid, int threads) {
+  if (!p) {                                            // no weight: 1
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = i * threads + tid;
+      float w[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) w[k] = has_column(c * V - shift, k, d) ? 1.0f : 0.0f;
+      spread_quarters<V>(s, held, c, w);
+    }
+  } else if (bf16) {
+    spread_shifted<__nv_bfloat16, V, NV>(s, static_cast<const __nv_bfloat16*>(p), held, shift, d, tid, threads);
+  } else {
+    spread_shifted<float, V, NV>(s, static_cast<const float*>(p), held, shift, d, tid, threads);
+  }
 }
 template <int V>
 __device__ __forceinline__ void chunk_weights(const float4* s, int held, int c, float2* w) {
@@ -539,12 +572,8 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
     copies_issued();
   };
   for (int k = 0; k < stages - 1; ++k) fetch(k, k);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int c = i * threads + tid;
-    spread_weights<V, true>(s_w, a.weight, a.w_bf16, 1.0f, held, c, column(i), d);
-    if (a.bias) spread_weights<V, true>(s_b, a.bias, a.w_bf16, 0.0f, held, c, column(i), d);
-  }
+  spread_shifted<V, NV>(s_w, a.weight, a.w_bf16, held, shift, d, tid, threads);
+  if (a.bias) spread_shifted<V, NV>(s_b, a.bias, a.w_bf16, held, shift, d, tid, threads);
   int count = 0;                                       // columns of this warp
   if (CENTER) {
 #pragma unroll
@@ -855,8 +884,12 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_bwd_kernel(BwdParams a, int st
   }
   uint32_t mask_next = mask_of(first + (stages - 1) * step);
   float r_next = first < a.T ? a.rstd[first] : 0.0f, mu_next = CENTER && first < a.T ? a.mean[first] : 0.0f;
+  if constexpr (SHIFT) {
+    spread_shifted<V, NV>(s_w, a.weight, a.w_bf16, held, shift, d, tid, threads);
+  } else {
 #pragma unroll
-  for (int i = 0; i < NV; ++i) spread_weights<V, SHIFT>(s_w, a.weight, a.w_bf16, 1.0f, held, i * threads + tid, column(i), d);
+    for (int i = 0; i < NV; ++i) spread_weights<V>(s_w, a.weight, a.w_bf16, held, i * threads + tid, d);
+  }
   float2 dw[NV * P], db[DB ? NV * P : 1];
 #pragma unroll
   for (int e = 0; e < NV * P; ++e) {
