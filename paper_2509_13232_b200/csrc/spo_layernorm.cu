@@ -14,6 +14,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "spo_internal.h"
@@ -354,9 +355,18 @@ RowPlan plan_rows(int per_sm, int fixed, int stage) {
   if (p.stages == 2 && p.per_sm * (fixed + 3 * stage + kSharedOwn) <= kSharedMost) p.stages = 3;
   return p;
 }
+// What a kernel may ask for belongs to the kernel, not to the call: the most that any plan asks for, once on each device, so that a call with
+// less does not lower it between another thread's permission and its launch.
 template <class Kernel>
-cudaError_t allow_shared(Kernel kernel, int bytes) {
-  return bytes <= 32 * 1024 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+cudaError_t allow_shared(Kernel kernel, std::atomic<int> (&ready)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (ready[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedMost - kSharedOwn);
+  if (e == cudaSuccess) ready[dev].store(1, std::memory_order_release);
+  return e;
 }
 
 // Mean and squared deviations of a row from those of its warps, each about a point near its own mean: M2 = sum M2_w + n_w (near_w - mu)^2,
@@ -768,7 +778,8 @@ cudaError_t run_fwd(const FwdParams& a, int64_t chunks, bool shift, cudaStream_t
   const int fixed = held * V * 4 * (a.bias ? 2 : 1), stage = held * 16 + 16 + (RES ? held * 16 : 0);
   const RowPlan p = plan_rows(by_registers, fixed, stage);
   const int shifts = shifts_of(a.d, V), span = fwd_span(a.T, p.per_sm, kFwdRounds, kFwdSpanShift), smem = fixed + p.stages * stage;
-  const cudaError_t e = allow_shared(kernel, smem);
+  static std::atomic<int> ready[64];
+  const cudaError_t e = allow_shared(kernel, ready);
   if (e != cudaSuccess) return e;
   kernel<<<(unsigned)(ceil_div(a.T, (int64_t)span * shifts) * shifts), threads, smem, st>>>(a, span, p.stages, shifts);
   return cudaGetLastError();
@@ -1162,7 +1173,8 @@ cudaError_t run_bwd(const BwdParams& a, int64_t chunks, int* blocks, cudaStream_
   const int64_t most = (int64_t)sm_count() * p.per_sm / shifts * shifts, rows = (a.T + shifts - 1) / shifts * shifts;
   *blocks = (int)(rows < most ? rows : most);
   const int smem = at.weights + p.stages * at.stage;
-  const cudaError_t e = allow_shared(kernel, smem);
+  static std::atomic<int> ready[64];
+  const cudaError_t e = allow_shared(kernel, ready);
   if (e != cudaSuccess) return e;
   kernel<<<*blocks, threads, smem, st>>>(a, p.stages);
   return cudaGetLastError();
