@@ -369,43 +369,77 @@ cudaError_t allow_shared(Kernel kernel, std::atomic<int> (&ready)[64]) {
   return e;
 }
 
-// Mean and squared deviations of a row from those of its warps, each about a point near its own mean: M2 = sum M2_w + n_w (near_w - mu)^2,
-// up to the square of what a point is off its warp's mean by, some 2^-23 of it.  The accuracy of two passes, with one barrier.
-struct WarpStats { float sum, m2, near, count; };
+// Mean and squared deviations of a row from sums over its warps, each about a point of its own:  with S_w = sum (x - near_w)^2 and
+// E_w = sum (x - near_w),  mu = sum (n_w near_w + E_w) / d,  and with c = near_w - mu  M2 = sum S_w + c (2 E_w + n_w c),  exactly, whatever the points.
+// near_w is the mean of the threads' first chunks, one of NV equal parts of the warp's columns and so at most sqrt(NV - 1) deviations off its mean:
+// S_w is at most NV times the squares about that, and the differences lose two bits at the worst, as two passes with two barriers would not.
+// (Without E_w what near_w is rounded by counts where the columns of different warps have different means: fp32 rows with a mean of 1000
+// deviations had the variance off by 1e-4.)  A point that is not finite gives way to zero, so that the mean is that of the formula.
+struct __align__(16) WarpStats { float near, count, squares, off; };
+__device__ __forceinline__ float point_near(float mean) { return fabsf(mean) < INFINITY ? mean : 0.0f; }
 
-// From each warp's to the row's: mu becomes the mean, m2 the squared deviations from it.  (Also the barrier between the row's reads of the
-// ring and the copies that follow.)
-template <bool CENTER>
-__device__ __forceinline__ void merge_warps(WarpStats* st, int lane, int warp, int warps, float sum, float& m2, float& mu, int count,
-                                            float inv_d) {
+// The sums of a and of b over a warp, by as many exchanges as of one: a's in lanes 0 to 15, b's in lanes 16 to 31.
+__device__ __forceinline__ float warp_sums(float a, float b, int lane) {
+  const bool high = lane & 16;
+  float v = high ? b : a;
+  v += __shfl_xor_sync(0xffffffffu, high ? a : b, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// From each warp's to the row's: mu, the point of this warp, becomes the mean (of CENTER), and the squared deviations from it are returned.
+// squares, off: the thread's own shares of S_w and E_w;  the counts are in st.  A lane takes a warp's (10 000 rows of 8192 of layer norm: 97 us
+// so, 132 where every thread goes through all warps); EACH: every thread all of them (24 000 aligned rows of 4096 of RMS norm, four warps each:
+// 70 us so, 77 by lanes).  (Also the barrier between the row's reads of the ring and the copies that follow.)
+template <bool CENTER, int NV, bool EACH>
+__device__ __forceinline__ float merge_warps(WarpStats* st, int lane, int warp, int warps, int d, float squares, float off, float& mu, float inv_d) {
+  static_assert(!CENTER || !EACH, "the mean is summed by lanes");
+  auto about = [&](const WarpStats& q) {
+    const float c = q.near - mu;
+    return fmaf(c, fmaf(q.count, c, 2.0f * q.off), q.squares);
+  };
   if (warps == 1) {
-    if (CENTER) {
-      const float c = sum * inv_d - mu;
-      mu = sum * inv_d;
-      m2 = fmaf((float)count * c, c, m2);
-    }
     __syncwarp();
-    return;
+    if (!CENTER || NV == 1) return warp_sum(squares);  // (about the mean already)
+    const float v = warp_sums(squares, off, lane);
+    const WarpStats q{mu, (float)d, __shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16)};
+    mu = fmaf(q.near, q.count, q.off) * inv_d;
+    return about(q);
   }
-  if (lane == 0) st[warp] = WarpStats{sum, m2, mu, (float)count};
-  __syncthreads();
-  m2 = 0.0f;
-  sum = 0.0f;
   if (CENTER) {
-#pragma unroll 4
-    for (int w = 0; w < warps; ++w) sum += st[w].sum;
-    mu = sum * inv_d;
-  }
-#pragma unroll 4
-  for (int w = 0; w < warps; ++w) {
-    const WarpStats q = st[w];
-    if (CENTER) {
-      const float c = q.near - mu;
-      m2 += fmaf(q.count * c, c, q.m2);
-    } else {
-      m2 += q.m2;
+    const float v = warp_sums(squares, off, lane);
+    if (lane == 0) {
+      st[warp].near = mu;
+      st[warp].squares = v;
     }
+    if (lane == 16) st[warp].off = v;
+  } else {
+    const float v = warp_sum(squares);
+    if (lane == 0) st[warp].squares = v;
   }
+  __syncthreads();
+  float m2 = 0.0f;
+  if (EACH) {
+#pragma unroll 4
+    for (int w = 0; w < warps; ++w) m2 += st[w].squares;
+    return m2;
+  }
+  const int lanes = 1 << (32 - __clz(warps - 1)), w = lane & (lanes - 1);            // warps, up to a power of two
+  if (CENTER) {
+    WarpStats q{0.0f, 0.0f, 0.0f, 0.0f};
+    if (w < warps) q = st[w];
+    float sum = fmaf(q.near, q.count, q.off);
+#pragma unroll 1
+    for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    mu = sum * inv_d;
+    m2 = about(q);                                     // (of a lane without a warp zero, but where mu is not finite)
+  } else if (w < warps) {
+    m2 = st[w].squares;
+  }
+#pragma unroll 1
+  for (int o = 1; o < lanes; o <<= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+  return m2;
 }
 
 // Rows that begin on 16 bytes.  A block takes `span` rows in a row; the next row's inputs are on their way to registers while one is worked
@@ -416,6 +450,9 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
   // The row stays in registers as fp32 values, or as it is in memory: with both inputs of the next row on their way there is no room for
   // the values (their loads would be put off; 24 000 rows of 4096 with a residual: 155 and 125 us).
   constexpr bool PACKED = RES && sizeof(X) == 2;
+  // fp32 rows with a residual take up the registers of four blocks of 256 threads: one sum at a time (12 000 rows of 4096: 159 us so, 172 in
+  // pairs, with spills).
+  constexpr bool TIGHT = RES && CENTER && sizeof(X) == 4;
   __shared__ WarpStats s_stats[2][32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
   const int d = a.d;
@@ -438,13 +475,15 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
     }
   };
   fetch(0);
-  int count = 0;                                       // columns of this warp
+  int columns = 0, firsts = 0;                         // columns of this warp, and those in its threads' first chunks
   if (CENTER) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) count += column(i) < d ? V : 0;
-    count = __reduce_add_sync(0xffffffffu, count);
+    for (int i = 0; i < NV; ++i) columns += column(i) < d ? V : 0;
+    columns = __reduce_add_sync(0xffffffffu, columns);
+    firsts = __reduce_add_sync(0xffffffffu, column(0) < d ? V : 0);
   }
-  const float inv_count = count ? 1.0f / (float)count : 0.0f;
+  if (CENTER && lane == 0) s_stats[0][warp].count = s_stats[1][warp].count = (float)columns;
+  const float inv_firsts = firsts ? 1.0f / (float)firsts : 0.0f;
   int buf = 0;
 #pragma unroll 1
   for (int r = 0; r < rows; ++r) {
@@ -489,7 +528,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           if constexpr (!PACKED) f[i * P + p] = pair_of(next[i], p);
-          if (CENTER) part = add2(part, value(i, p));
+          if (CENTER && i == 0) part = add2(part, value(i, p));
         }
       } else {
         if constexpr (PACKED) zero_pack(now[i]);
@@ -499,23 +538,25 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
       }
     }
     if (r + 1 < rows) fetch(r + 1);
-    float sum = 0.0f, mu = 0.0f;
-    if (CENTER) {
-      sum = warp_sum(part.x + part.y);
-      mu = sum * inv_count;                            // any point near the mean serves to measure the deviations from
-    }
+    float mu = CENTER ? point_near(warp_sum(part.x + part.y) * inv_firsts) : 0.0f;
     part = both(0.0f);
+    float2 off = both(0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (CENTER && column(i) >= d) continue;
 #pragma unroll
       for (int p = 0; p < P; ++p) {
         const float2 c = CENTER ? add2(value(i, p), both(-mu)) : value(i, p);
-        part = fma2(c, c, part);
+        if constexpr (TIGHT) {
+          part.x = fmaf(c.x, c.x, fmaf(c.y, c.y, part.x));
+          off.x += c.x + c.y;
+        } else {
+          part = fma2(c, c, part);
+          if (CENTER) off = add2(off, c);
+        }
       }
     }
-    float m2 = warp_sum(part.x + part.y);
-    merge_warps<CENTER>(s_stats[buf], lane, warp, warps, sum, m2, mu, count, inv_d);
+    const float m2 = merge_warps<CENTER, NV, !CENTER && MOST <= 128>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
     buf ^= 1;                                          // (of rows that are not masked: two barriers lie between two uses of a buffer)
     const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
     if (tid == 0) {
@@ -584,14 +625,18 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
   for (int k = 0; k < stages - 1; ++k) fetch(k, k);
   spread_shifted<V, NV>(s_w, a.weight, a.w_bf16, held, shift, d, tid, threads);
   if (a.bias) spread_shifted<V, NV>(s_b, a.bias, a.w_bf16, held, shift, d, tid, threads);
-  int count = 0;                                       // columns of this warp
+  int columns = 0, firsts = 0;                         // columns of this warp, and those in its threads' first chunks
   if (CENTER) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-      if (column(i) < d) count += min(column(i) + V, d) - max(column(i), 0);
-    count = __reduce_add_sync(0xffffffffu, count);
+    for (int i = 0; i < NV; ++i) {
+      if (column(i) < d) columns += min(column(i) + V, d) - max(column(i), 0);
+      if (i == 0) firsts = columns;
+    }
+    columns = __reduce_add_sync(0xffffffffu, columns);
+    firsts = __reduce_add_sync(0xffffffffu, firsts);
   }
-  const float inv_count = count ? 1.0f / (float)count : 0.0f;
+  if (CENTER && lane == 0) s_stats[0][warp].count = s_stats[1][warp].count = (float)columns;
+  const float inv_firsts = firsts ? 1.0f / (float)firsts : 0.0f;
   int slot = 0, buf = 0;
 #pragma unroll 1
   for (int k = 0; k < rows; ++k) {
@@ -645,19 +690,16 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           f[i * P + p] = pair_of(q, p);
-          if (CENTER) part = add2(part, f[i * P + p]);
+          if (CENTER && i == 0) part = add2(part, f[i * P + p]);
         }
       } else {
 #pragma unroll
         for (int p = 0; p < P; ++p) f[i * P + p] = both(0.0f);
       }
     }
-    float sum = 0.0f, mu = 0.0f;
-    if (CENTER) {
-      sum = warp_sum(part.x + part.y);
-      mu = sum * inv_count;                            // any point near the mean serves to measure the deviations from
-    }
+    float mu = CENTER ? point_near(warp_sum(part.x + part.y) * inv_firsts) : 0.0f;
     part = both(0.0f);
+    float2 off = both(0.0f);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int j = column(i);
@@ -670,10 +712,10 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
           if (!has_column(j, 2 * p + 1, d)) c.y = 0.0f;
         }
         part = fma2(c, c, part);
+        if (CENTER) off = add2(off, c);
       }
     }
-    float m2 = warp_sum(part.x + part.y);
-    merge_warps<CENTER>(s_stats[buf], lane, warp, warps, sum, m2, mu, count, inv_d);
+    const float m2 = merge_warps<CENTER, NV, false>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
     buf ^= 1;
     const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
     if (tid == 0) {
