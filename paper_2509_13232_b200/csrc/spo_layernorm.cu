@@ -1049,31 +1049,25 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_bwd_kernel(BwdParams a, int st
       }
       buf ^= 1;                                         // (of rows that are not masked: two barriers lie between two uses of a buffer)
     }
-    // dx = r (up - mean up - xh mean(up xh)) + dh = (w r) g + along x + level + dh
-    const float along = -inv_d * s1 * r * r, level = CENTER ? -fmaf(along, mu, inv_d * s2 * r) : 0.0f;
+    // dx = r (up - mean up - xh mean(up xh)) + dh
+    const float c1 = -inv_d * s1, c2 = -inv_d * s2;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = i * threads + tid, j = column(i);
       if (j >= d) continue;
-      float2 g[P], w[P];
-      Pack<X, V> px;
-      if (SHIFT && staged) px = staged_chunk<X, V>(s, own, j, d);
-      else px = load_pack<X, V>(reinterpret_cast<const X*>(s + c * 16));
+      float2 xh[P], g[P], w[P];
+      normalised(i, xh);
       gradient(i, g);
       weights(i, w);
+#pragma unroll
+      for (int p = 0; p < P; ++p) w[p] = fma2(xh[p], both(c1), CENTER ? fma2(g[p], w[p], both(c2)) : mul2(g[p], w[p]));
       if (a.dh) {
         const Pack<X, V> ph = load_pack<X, V>(reinterpret_cast<const X*>(s + at.x + at.dy) + c * V);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const float2 rest = CENTER ? add2(pair_of(ph, p), both(level)) : pair_of(ph, p);
-          w[p] = fma2(mul2(w[p], both(r)), g[p], fma2(pair_of(px, p), both(along), rest));
-        }
+        for (int p = 0; p < P; ++p) w[p] = fma2(w[p], both(r), pair_of(ph, p));
       } else {
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-          const float2 rest = CENTER ? fma2(pair_of(px, p), both(along), both(level)) : mul2(pair_of(px, p), both(along));
-          w[p] = fma2(mul2(w[p], both(r)), g[p], rest);
-        }
+        for (int p = 0; p < P; ++p) w[p] = mul2(w[p], both(r));
       }
       store_chunk<X, V, SHIFT>(out, j, d, round_pack<X, V>(&w[0].x));
     }
