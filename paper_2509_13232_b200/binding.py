@@ -608,12 +608,14 @@ def spo_layernorm_bwd(dy, x, weight, mask, mean, rstd, dh, dx, dw, db, dw_accumu
 
 class TensorList:
     """The table of one spo_grad_norm or spo_adamw_update: the addresses of tensors that stay alive with it.  Made once, used in every
-    step while the tensors keep their memory."""
+    step while the tensors keep their memory.  A tensor that is given other memory (p.data = ...) needs another list: this one holds the
+    memory that its addresses lie in, and goes on with that."""
 
-    __slots__ = ("table", "address", "count", "device", "tensors")
+    __slots__ = ("table", "address", "count", "device", "tensors", "memory")
 
-    def __init__(self, table, device, tensors):
+    def __init__(self, table, device, tensors, memory):
         self.table, self.address, self.count, self.device, self.tensors = table, ctypes.addressof(table), len(tensors), device, tensors
+        self.memory = [t.untyped_storage() for t in memory if t is not None]
 
     def here(self, c):
         if self.count and self.device != c.device:
@@ -642,7 +644,7 @@ def grad_list(grads) -> TensorList:
     table = (SpoGradTensor * max(len(grads), 1))()
     for q, g in zip(table, grads):
         q.g, q.n, q.dtype = g.data_ptr(), g.numel(), _dtype_code(g)
-    return TensorList(table, device, grads)
+    return TensorList(table, device, grads, grads)
 
 
 def spo_grad_norm(grads, out, ws, d_status, max_norm=0.0, grad_scale=1.0):
@@ -721,7 +723,7 @@ def adamw_list(weights, grads, m, v, m_scale=None, v_scale=None, copies=None, lr
         if begin < written or (out and begin < read):
             raise ValueError("tensors of the list share memory that is written (the same tensor twice?)")
         read, written = max(read, end), max(written, end if out else 0)
-    return TensorList(table, device, list(zip(*[x for _, x in columns])))
+    return TensorList(table, device, list(zip(*[x for _, x in columns])), [t for _, x in columns for t in x])
 
 
 def spo_adamw_update(tensors, d_scale, d_step, d_lr, params, d_status):
