@@ -715,7 +715,9 @@ int32_t spo_grad_norm(const spo_grad_tensor* grads /* host */, int32_t n_grads, 
  *              j = 1 .. 255, as fp32), at or below the magnitude times the fp32 quotient 127^2 / s (255^4 / s); v > 0 takes code 1 at
  *              least.  Zeroed codes and scales are the start.  The update of w uses m and v before they are rounded to codes
  *     lr_scale, decay_scale   1 for the call's own
- *   No two tensors may share memory that is written, nor a gradient with what is written.
+ *   No two tensors may share memory that is written, nor a gradient with what is written: the caller's to see to (the list of the Python
+ *   binding checks it once).  d_scale, d_lr and d_step lie in no tensor that is written, d_step in no gradient, d_scale or d_lr:
+ *   SPO_ERR_INVALID_ARG
  *   d_scale    device in [1] fp32, optional (1): spo_grad_norm's out + 1
  *   d_lr       device in [1] fp32, optional: replaces params->lr (a captured step whose rate changes)
  *   d_step     device in/out [2] int32 (steps taken, 0), optional: t is one more than d_step[0], and the call leaves it so (calls

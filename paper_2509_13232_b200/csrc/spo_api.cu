@@ -892,6 +892,28 @@ int32_t spo_default_adamw_params(spo_adamw_params* p) {
   return SPO_OK;
 }
 
+// The same for words that every block of a step reads, or the last one writes, while others work on the tensors: whether n bytes from base on hold any
+// of them.  A call asks hundreds of times, so the range from the first word to the last is looked at before they are.
+struct Words {
+  struct { uintptr_t first, bytes; } word[3];
+  int count = 0;
+  uintptr_t first = 0, end = 0;
+  void add(const void* p, uintptr_t n) {
+    if (!p) return;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    first = count == 0 || at < first ? at : first;
+    end = at + n > end ? at + n : end;
+    word[count++] = {at, n};
+  }
+  bool in(const void* base, uintptr_t n) const {
+    const uintptr_t b = reinterpret_cast<uintptr_t>(base);
+    if (b >= end || b + n <= first) return false;
+    for (int i = 0; i < count; ++i)
+      if (b < word[i].first + word[i].bytes && word[i].first < b + n) return true;
+    return false;
+  }
+};
+
 int32_t spo_adamw_update(const spo_adamw_tensor* tensors, int32_t n_tensors, const float* d_scale, const float* d_lr, int32_t* d_step,
                          const spo_adamw_params* params, int32_t* d_status, void* stream) {
   const float big = 3.0e38f;
@@ -900,6 +922,12 @@ int32_t spo_adamw_update(const spo_adamw_tensor* tensors, int32_t n_tensors, con
   for (float b : {params->beta1, params->beta2})
     if (!(b >= 0.0f) || !(b < 1.0f)) return SPO_ERR_INVALID_ARG;
   if (!(params->eps >= 0x1p-100f) || !(params->eps < big) || params->step < 1) return SPO_ERR_INVALID_ARG;
+  Words words, counter;
+  counter.add(d_step, 8);
+  bool shared = (d_scale && counter.in(d_scale, 4)) || (d_lr && counter.in(d_lr, 4));
+  words.add(d_scale, 4);
+  words.add(d_lr, 4);
+  words.add(d_step, 8);
   for (int i = 0; i < n_tensors; ++i) {
     const spo_adamw_tensor& q = tensors[i];
     if (!float_type(q.w_dtype) || !float_type(q.g_dtype) || (q.state_bits != 8 && q.state_bits != 32)) return SPO_ERR_UNSUPPORTED_DTYPE;
@@ -912,9 +940,18 @@ int32_t spo_adamw_update(const spo_adamw_tensor* tensors, int32_t n_tensors, con
         (reinterpret_cast<uintptr_t>(q.copy) & 1) || ((reinterpret_cast<uintptr_t>(q.m) | reinterpret_cast<uintptr_t>(q.v)) & state) ||
         ((reinterpret_cast<uintptr_t>(q.m_scale) | reinterpret_cast<uintptr_t>(q.v_scale)) & 3))
       return SPO_ERR_BAD_ALIGNMENT;
+    if (q.n == 0) continue;
+    const uintptr_t n = (uintptr_t)q.n, each = q.state_bits >> 3;
+    shared = shared || words.in(q.w, n * float_size(q.w_dtype)) || words.in(q.m, n * each) || words.in(q.v, n * each) ||
+             counter.in(q.g, n * float_size(q.g_dtype)) || (q.copy && words.in(q.copy, n * 2));
+    if (q.state_bits == 8) {
+      const uintptr_t scales = (n + SPO_ADAMW_BLOCK - 1) / SPO_ADAMW_BLOCK * 4;
+      shared = shared || words.in(q.m_scale, scales) || words.in(q.v_scale, scales);
+    }
   }
   if (((reinterpret_cast<uintptr_t>(d_scale) | reinterpret_cast<uintptr_t>(d_lr) | reinterpret_cast<uintptr_t>(d_step)) & 3) != 0)
     return SPO_ERR_BAD_ALIGNMENT;
+  if (shared) return SPO_ERR_INVALID_ARG;
   if (!device_is_sm100()) return SPO_ERR_UNSUPPORTED_ARCH;
   cudaError_t e = launch_adamw(tensors, n_tensors, d_scale, d_lr, d_step, *params, d_status, (cudaStream_t)stream);
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);
