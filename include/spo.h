@@ -723,7 +723,8 @@ int32_t spo_grad_norm(const spo_grad_tensor* grads /* host */, int32_t n_grads, 
  *   d_step     device in/out [2] int32 (steps taken, 0), optional: t is one more than d_step[0], and the call leaves it so (calls
  *              that share it run one after the other).  NULL: t = params->step
  * An element whose g~ is not finite or above 2^60 in magnitude keeps its w, m and v (in 8 bits up to the rounding to the block's new scale)
- * and sets SPO_DEV_NONFINITE.  A factor or rate that is not finite sets it too, and then the step is neither taken nor counted.
+ * and sets SPO_DEV_NONFINITE.  A factor or rate that is not finite sets it too, and then the step is neither taken nor counted; so does a rate
+ * that, times the largest lr_scale of the call and the largest decay_k above one, is beyond 2^100 in magnitude.
  * Up to 400 tensors are one launch.  Tensors without elements are allowed; a call without any launches nothing and counts no step.
  */
 #define SPO_ADAMW_BLOCK 256

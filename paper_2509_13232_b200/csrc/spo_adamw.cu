@@ -15,6 +15,7 @@
 // denominator does not vanish beside a momentum that is not zero.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -217,6 +218,7 @@ constexpr int kTensorsMost = 400;                   // tensors per launch, 80 by
 constexpr int kTensorsSome = 136, kTensorsFew = 12;  // smaller tables for shorter lists: what a launch costs the host grows with them
 
 constexpr float kMFloor = 0x1p-100f, kVFloor = 0x1p-90f;     // least scales: 1 / scale and scale / 255^4 are normal numbers
+constexpr double kRateMost = 0x1p100;                         // of a tensor's rate, and that times its decay: 1 / (1 - b1^t) is up to 2^24
 constexpr float kSquareMost = 0x1p120f;                      // of a scaled gradient: beyond it (or NaN) the element is left out
 
 enum : uint32_t { kW16 = 1, kG16 = 2, kEight = 4, kAligned = 8 };
@@ -239,6 +241,7 @@ struct StepScalars {
   float log_b1, log_b2;                             // -inf for 0, whose powers are then 0
   float lr, b1, b1c, b2, b2c, eps;
   float one;                                        // 1: a product and a sum that must not become one multiply-add go through it
+  float lr_most;                                    // beyond it (or NaN) no step is taken: the same for all tensors of a call
   float rate, root;                                 // lr-free 1/(1 - b1^t) and 1/sqrt(1 - b2^t), where the host knows t
   uint32_t span;
   int32_t advance;                                  // the last launch of a call counts the step
@@ -595,7 +598,7 @@ __device__ __forceinline__ void make_constants(float2* consts, const StepScalars
   }
   __syncwarp();
   s.ready = true;
-  s.fine = fabsf(s.f) < INFINITY && fabsf(s.lr) < INFINITY;
+  s.fine = fabsf(s.f) < INFINITY && fabsf(s.lr) <= a.lr_most;
 }
 
 // A warp's share, `chunks` chunks from `base` on, as far as they are whole.  Returns the chunks (a bit each) that are left
@@ -788,6 +791,14 @@ cudaError_t launch_adamw(const spo_adamw_tensor* tensors, int count, const float
   // the launches of a call, the last of which counts the step: those that hold an element
   int end = count;
   while (end > 0 && tensors[end - 1].n == 0) --end;
+  float scale = 1e-30f, decay = 1.0f;
+  for (int i = 0; i < end; ++i) {
+    const float one = tensors[i].n ? fabsf(tensors[i].lr_scale) : 0.0f, other = tensors[i].n ? fabsf(tensors[i].decay_scale * p.weight_decay) : 0.0f;
+    scale = one > scale ? one : scale;
+    decay = other > decay ? other : decay;
+  }
+  const double most = kRateMost / ((double)scale * decay);
+  a.lr_most = decay < INFINITY ? most < FLT_MAX ? (float)most : FLT_MAX : -1.0f;
   for (int from = 0; from < end;) {
     const int left = end - from, take = left < kTensorsMost ? left : kTensorsMost;
     a.advance = take == left;
