@@ -389,10 +389,10 @@ __device__ __forceinline__ float warp_sums(float a, float b, int lane) {
 }
 
 // From each warp's to the row's: mu, the point of this warp, becomes the mean (of CENTER), and the squared deviations from it are returned.
-// squares, off: the thread's own shares of S_w and E_w;  the counts are in st.  A lane takes a warp's (10 000 rows of 8192 of layer norm: 97 us
-// so, 132 where every thread goes through all warps); EACH: every thread all of them (24 000 aligned rows of 4096 of RMS norm, four warps each:
-// 70 us so, 77 by lanes).  (Also the barrier between the row's reads of the ring and the copies that follow.)
-template <bool CENTER, int NV, bool EACH>
+// squares, off: the thread's own shares of S_w and E_w;  the counts are in st.  A lane takes a warp (10 000 rows of 8192 of layer norm: 92 us
+// so, 132 where every thread goes through all warps);  EACH: every thread all of them (24 000 aligned rows of 4096 of RMS norm, four warps each:
+// 71 us so, 75 by lanes).  (Also the barrier between the row's reads of the ring and the copies that follow.)
+template <bool CENTER, int NV, int MOST, bool EACH>
 __device__ __forceinline__ float merge_warps(WarpStats* st, int lane, int warp, int warps, int d, float squares, float off, float& mu, float inv_d) {
   static_assert(!CENTER || !EACH, "the mean is summed by lanes");
   auto about = [&](const WarpStats& q) {
@@ -425,20 +425,21 @@ __device__ __forceinline__ float merge_warps(WarpStats* st, int lane, int warp, 
     for (int w = 0; w < warps; ++w) m2 += st[w].squares;
     return m2;
   }
-  const int lanes = 1 << (32 - __clz(warps - 1)), w = lane & (lanes - 1);            // warps, up to a power of two
+  constexpr int kLanes = MOST <= 128 ? 4 : 32;         // (warps are fewer or as many)
+  const int w = lane & (kLanes - 1);
   if (CENTER) {
     WarpStats q{0.0f, 0.0f, 0.0f, 0.0f};
     if (w < warps) q = st[w];
     float sum = fmaf(q.near, q.count, q.off);
-#pragma unroll 1
-    for (int o = 1; o < lanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     mu = sum * inv_d;
     m2 = about(q);                                     // (of a lane without a warp zero, but where mu is not finite)
   } else if (w < warps) {
     m2 = st[w].squares;
   }
-#pragma unroll 1
-  for (int o = 1; o < lanes; o <<= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+#pragma unroll
+  for (int o = 1; o < kLanes; o <<= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
   return m2;
 }
 
@@ -451,7 +452,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
   // the values (their loads would be put off; 24 000 rows of 4096 with a residual: 155 and 125 us).
   constexpr bool PACKED = RES && sizeof(X) == 2;
   // fp32 rows with a residual take up the registers of four blocks of 256 threads: one sum at a time (12 000 rows of 4096: 159 us so, 172 in
-  // pairs, with spills).
+  // pairs).
   constexpr bool TIGHT = RES && CENTER && sizeof(X) == 4;
   __shared__ WarpStats s_stats[2][32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
@@ -556,7 +557,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
         }
       }
     }
-    const float m2 = merge_warps<CENTER, NV, !CENTER && MOST <= 128>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
+    const float m2 = merge_warps<CENTER, NV, MOST, !CENTER && MOST <= 128>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
     buf ^= 1;                                          // (of rows that are not masked: two barriers lie between two uses of a buffer)
     const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
     if (tid == 0) {
@@ -715,7 +716,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
         if (CENTER) off = add2(off, c);
       }
     }
-    const float m2 = merge_warps<CENTER, NV, false>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
+    const float m2 = merge_warps<CENTER, NV, MOST, false>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
     buf ^= 1;
     const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
     if (tid == 0) {
