@@ -632,8 +632,9 @@ int32_t spo_muon_update(void* W, int32_t W_dtype, float* momentum, const void* G
  *   rstd = 1 / sqrt( mean_j (h_j - mu)^2 + eps );      y_j = (h_j - mu) rstd weight_j + bias_j.
  * Statistics in fp32, the squares about the mean; y is rounded once.
  *
- *   x         device in  [T] rows of d elements, fp32 or bf16 (dtype), row pitch ldx >= d elements: the last-token rows of a padded
- *             batch need no copy
+ *   x         device in  [T] rows of d elements, fp32 or bf16 (dtype), row pitch ldx >= d elements: rows of a wider buffer (the last-token
+ *             rows of a padded batch, a slice of columns) need no copy where the first of them begins on 16 bytes, as every pointer of
+ *             these two calls has to
  *   residual  device in  [T][d], type of x, optional;   h  device out [T][d], type of x: required with residual and only then.
  *             h may be x (ldx = d) or residual
  *   weight, bias   device in [d], fp32 or bf16 (w_dtype), each optional (NULL: 1 and 0)
@@ -665,7 +666,8 @@ int32_t spo_layernorm_fwd(const void* x, int64_t ldx, const void* residual, int3
  *   mask      rows with mask 0 give dx = 0 and add nothing to dweight and dbias, whatever they hold
  *   dx        device out [T][d], type of x; may be dy (where the types agree), dh or x (ldx = d)
  *   dweight, dbias   device out [d], fp32 or bf16 (dw_dtype), each optional; overwritten, or added to when dw_accumulate != 0.  Summed
- *             over all rows in fp32, in an order that depends on T, d and the device alone: results repeat bit for bit
+ *             over all rows in fp32, in an order that depends on T, d, ldx, the types of dy and x, whether there is a dh, and the device: the
+ *             same call repeats bit for bit, and calls that differ in one of these may round differently
  *   ws        device scratch, spo_workspace_bytes(SPO_WS_LAYERNORM_BWD, T, d, 0, 0, 0, 0) bytes; it serves shorter calls too.  Optional
  *             where neither dweight nor dbias is wanted
  * T = 0 zeroes dweight and dbias (unless accumulating).  The call sets no status bit: what is not finite goes where the formula takes it.

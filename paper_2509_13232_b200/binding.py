@@ -575,7 +575,7 @@ def _vectors(c, first, second, names, d, default):
 
 def spo_layernorm_fwd(x, residual, weight, bias, mask, y, h, mean, rstd, d_status, eps=1e-6, kind=NORM_LAYER):
     """y = the layer norm (kind=NORM_RMS: the RMS norm) of the rows of x, or of h = x + residual where both tensors are given.  x may be
-    a slice of a wider buffer (rows contiguous); weight, bias, mask, mean and rstd may be None."""
+    a slice of a wider buffer (rows contiguous, the first one beginning on 16 bytes); weight, bias, mask, mean and rstd may be None."""
     c = _Args()
     f32 = c.torch.float32
     T, d, ld = _hidden_rows(c, "x", x)

@@ -233,7 +233,7 @@ struct Tensor {
   float lr_scale, decay;
   uint32_t first, kind;
 };
-static_assert(sizeof(Tensor) == 80, "two tables have to fit the parameters of a kernel");
+static_assert(sizeof(Tensor) == 80, "kTensorsMost of them have to fit the parameters of a kernel");
 
 struct StepScalars {
   const float *d_scale, *d_lr;

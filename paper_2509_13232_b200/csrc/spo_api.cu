@@ -855,7 +855,7 @@ int32_t spo_layernorm_bwd(const void* dy, int32_t dy_dtype, const void* x, int64
   return e == cudaSuccess ? SPO_OK : cuda_fail(e);
 }
 
-static constexpr int64_t kElementsMost = (int64_t)1 << 33;         // of one tensor: chunk numbers of a launch fit 32 bits
+static constexpr int64_t kElementsMost = (int64_t)1 << 33;         // of one tensor; a launch counts chunks of 256 in 32 bits (2^40 elements, more than memory holds)
 
 int32_t spo_grad_norm(const spo_grad_tensor* grads, int32_t n_grads, float max_norm, float grad_scale, float* out, void* ws,
                       size_t ws_bytes, int32_t* d_status, void* stream) {

@@ -7,9 +7,9 @@
 //
 // Both directions are bound by HBM, as far as their instructions let them: each input is read once and each output written once.  A row
 // belongs to a block, which keeps it in registers (forward) or shared memory (backward) between the reduction over it and its output.
-// At 6550 GB/s of a copy: forward, 24 000 bf16 rows of 4096 with a residual 125 us (6270 GB/s), without 71 us (5500; 18 instructions an element
-// are in the way), layer norm with a bias 92 (4270); backward, the same rows with fp32 dy, dh and a mask 154 us (6360), layer norm with dw and
-// db 130 (4530).
+// At 6550 GB/s of a copy: forward, 24 000 bf16 rows of 4096 with a residual 126 us (6250 GB/s), without 71 us (5540; 14 instructions an element
+// are in the way), layer norm with a bias 90 (4370; 20 instructions); backward, the same rows with fp32 dy, dh and a mask 155 us (6340), layer norm
+// with dw and db 132 (4460; 31 instructions).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
