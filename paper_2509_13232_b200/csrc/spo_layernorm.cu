@@ -376,7 +376,9 @@ cudaError_t allow_shared(Kernel kernel, std::atomic<int> (&ready)[64]) {
 // (Without E_w what near_w is rounded by counts where the columns of different warps have different means: fp32 rows with a mean of 1000
 // deviations had the variance off by 1e-4.)  A point that is not finite gives way to zero, so that the mean is that of the formula.
 struct __align__(16) WarpStats { float near, count, squares, off; };
-__device__ __forceinline__ float point_near(float mean) { return fabsf(mean) < INFINITY ? mean : 0.0f; }
+// ONE: a single warp of one chunk a thread, whose point is the row's mean.
+template <bool ONE>
+__device__ __forceinline__ float point_near(float mean) { return ONE || fabsf(mean) < INFINITY ? mean : 0.0f; }
 
 // The sums of a and of b over a warp, by as many exchanges as of one: a's in lanes 0 to 15, b's in lanes 16 to 31.
 __device__ __forceinline__ float warp_sums(float a, float b, int lane) {
@@ -392,7 +394,7 @@ __device__ __forceinline__ float warp_sums(float a, float b, int lane) {
 // squares, off: the thread's own shares of S_w and E_w;  the counts are in st.  A lane takes a warp (10 000 rows of 8192 of layer norm: 92 us
 // so, 132 where every thread goes through all warps);  EACH: every thread all of them (24 000 aligned rows of 4096 of RMS norm, four warps each:
 // 71 us so, 75 by lanes).  (Also the barrier between the row's reads of the ring and the copies that follow.)
-template <bool CENTER, int NV, int MOST, bool EACH>
+template <bool CENTER, int MOST, bool EACH>
 __device__ __forceinline__ float merge_warps(WarpStats* st, int lane, int warp, int warps, int d, float squares, float off, float& mu, float inv_d) {
   static_assert(!CENTER || !EACH, "the mean is summed by lanes");
   auto about = [&](const WarpStats& q) {
@@ -401,7 +403,7 @@ __device__ __forceinline__ float merge_warps(WarpStats* st, int lane, int warp, 
   };
   if (warps == 1) {
     __syncwarp();
-    if (!CENTER || NV == 1) return warp_sum(squares);  // (about the mean already)
+    if (!CENTER || MOST == 32) return warp_sum(squares);  // (about the mean already)
     const float v = warp_sums(squares, off, lane);
     const WarpStats q{mu, (float)d, __shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16)};
     mu = fmaf(q.near, q.count, q.off) * inv_d;
@@ -539,7 +541,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
       }
     }
     if (r + 1 < rows) fetch(r + 1);
-    float mu = CENTER ? point_near(warp_sum(part.x + part.y) * inv_firsts) : 0.0f;
+    float mu = CENTER ? point_near<MOST == 32>(warp_sum(part.x + part.y) * inv_firsts) : 0.0f;
     part = both(0.0f);
     float2 off = both(0.0f);
 #pragma unroll
@@ -557,7 +559,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_kernel(FwdParams a, int sp
         }
       }
     }
-    const float m2 = merge_warps<CENTER, NV, MOST, !CENTER && MOST <= 128>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
+    const float m2 = merge_warps<CENTER, MOST, !CENTER && MOST <= 128>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
     buf ^= 1;                                          // (of rows that are not masked: two barriers lie between two uses of a buffer)
     const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
     if (tid == 0) {
@@ -698,7 +700,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
         for (int p = 0; p < P; ++p) f[i * P + p] = both(0.0f);
       }
     }
-    float mu = CENTER ? point_near(warp_sum(part.x + part.y) * inv_firsts) : 0.0f;
+    float mu = CENTER ? point_near<MOST == 32>(warp_sum(part.x + part.y) * inv_firsts) : 0.0f;
     part = both(0.0f);
     float2 off = both(0.0f);
 #pragma unroll
@@ -716,7 +718,7 @@ __global__ void __launch_bounds__(MOST, LEAST) ln_fwd_shift_kernel(FwdParams a, 
         if (CENTER) off = add2(off, c);
       }
     }
-    const float m2 = merge_warps<CENTER, NV, MOST, false>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
+    const float m2 = merge_warps<CENTER, MOST, false>(s_stats[buf], lane, warp, warps, d, part.x + part.y, off.x + off.y, mu, inv_d);
     buf ^= 1;
     const float var = m2 * inv_d, rstd = rsqrtf(var + a.eps);
     if (tid == 0) {
