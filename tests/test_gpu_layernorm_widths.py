@@ -17,10 +17,11 @@ FP32 = [125, 126, 128, 129, 2045, 2046, 2048, 2049, 2052, 4093, 4094, 4096, 4097
 @pytest.mark.parametrize("d,x16", [(d, True) for d in BF16] + [(d, False) for d in FP32])
 def test_both_sides_of_every_form(d, x16, kind):
     for T in (3, 170):
-        for extra in (dict(residual=True, masked=True, pad=3), dict(), dict(residual=True, pad=8), dict(bias=False, masked=True)):
+        some = 2 if T * d > 10**6 else 4                     # (the definitions in 64 bits take most of the time)
+        for extra in (dict(residual=True, masked=True, pad=3), dict(), dict(residual=True, pad=8), dict(bias=False, masked=True))[:some]:
             c = case(d + T, T, d, kind, x16, **{"y16": x16, "w16": not x16, **extra})
             check_fwd(c, run_fwd(c))
-        for dy16, dh, extra in ((False, True, dict(masked=True, pad=3)), (False, True, {}), (True, True, dict(pad=8)), (True, False, dict(masked=True))):
+        for dy16, dh, extra in ((False, True, dict(masked=True, pad=3)), (False, True, {}), (True, True, dict(pad=8)), (True, False, dict(masked=True)))[:some]:
             c = case(d + T, T, d, kind, x16, x16, not x16, bias=False, **extra)
             dy, dh = grads(d, c, dy16, dh)
             check_bwd(c, run_bwd(c, dy, dh), dy, dh)
